@@ -138,17 +138,18 @@ def _uniform(seed, what, shape, lo, hi):
 
 def _quantise(x):
     """e4m3 codes of rows x [..., D] and the exponent byte e of their scale
-    2^(e-127): the least power of two with amax <= 448 * scale over the row's
-    finite values.  A value that is not finite becomes the NaN code."""
+    2^(e-127): the least power of two with amax <= 448 * scale (at the largest,
+    codes stop at 240: 256 * 2^120 is past bf16's range).  A row with a value
+    that is not finite is NaN as a whole: e = 255, codes 0x7F."""
     x = x.float()
-    finite = torch.isfinite(x)
-    amax = torch.where(finite, x, torch.zeros_like(x)).abs().amax(-1)
-    bits = amax.view(torch.int32)
+    finite = torch.isfinite(x).all(-1)
+    bits = x.abs().amax(-1).view(torch.int32)
     e = (bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000).int()
-    e = e.clamp(min=0)
-    inv = ((254 - e) << 23).view(torch.float32)
-    code = (x * inv[..., None]).to(torch.float8_e4m3fn).view(torch.uint8)
-    return torch.where(finite, code, torch.full_like(code, 0x7F)), e.to(torch.uint8)
+    e = torch.where(finite, e.clamp(min=0), torch.full_like(e, 255))
+    inv = ((254 - e.clamp(max=247)) << 23).view(torch.float32)
+    top = torch.where(e == 247, torch.full_like(inv, 240.0), torch.full_like(inv, 448.0))[..., None]
+    code = torch.minimum(torch.maximum(x * inv[..., None], -top), top).to(torch.float8_e4m3fn).view(torch.uint8)
+    return torch.where(finite[..., None], code, torch.full_like(code, 0x7F)), e.to(torch.uint8)
 
 
 def _scale_of(e):
