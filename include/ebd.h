@@ -122,7 +122,9 @@ typedef struct {
   int32_t debug_flags; /* EBD_DEBUG_* (tests); 0 in normal use              */
   int32_t decode_mode; /* EBD_DECODE_*: EB decision or a baseline rule      */
   int32_t top_m;       /* EBD_DECODE_TOPM: commits per step (>= 1)          */
-  int32_t reserved;
+  int32_t paged;       /* 1: the handle also runs ebd_paged_attention, whose
+                          workspace it then holds (34 MB at 128-wide heads);
+                          0: it does not                                   */
 } ebd_config;
 
 typedef struct {
@@ -287,6 +289,95 @@ ebd_status ebd_merge_shard_states(ebd_handle* h, const float* states, int32_t sh
  * kernel: 2, three CTAs per SM, or 3, two), read at ebd_create, override the
  * choices. */
 ebd_status ebd_attention(ebd_handle* h, const ebd_step_args* a, void* stream);
+
+/* ---- Paged K/V cache ------------------------------------------------------
+ * No counterpart in the paper: the cache of Sec. 6.3 for many sequences of
+ * unequal length.  K and V of a sequence live in pages of page_size positions,
+ * in any order, found through a page table; position i of sequence b is place
+ * i % page_size of page page_table[b][i / page_size].  A pool holds one layer's
+ * K (or V) of every page, in bf16 or in 8 bits:
+ *
+ *   EBD_KV_E4M3  a row (one position, one head) of head_dim values x is held as
+ *     e4m3 codes round(x / 2^k), nearest even, and one exponent byte k + 127,
+ *     with the least k >= -127 for which the row's largest |x| is at most 448 *
+ *     2^k; at k = 120 codes stop at 240, as 256 * 2^120 is past bf16's range.
+ *     code * 2^k is a bf16 value, so reading back rounds nothing more.  A row
+ *     with a value that is not finite is NaN as a whole: exponent byte 255,
+ *     codes 0x7F.
+ *
+ * ebd_paged_write puts rows into the pages, ebd_paged_read takes them out, and
+ * ebd_paged_attention lets the rows of a chunk of new tokens (or single tokens)
+ * attend to what the pages hold, the chunk's own keys among it: write first.
+ * They use the handle's heads (n_heads_q, n_heads_kv, head_dim), max_batch (at
+ * most 4096 sequences a call) and max_rows, and none of its other sizes; a
+ * sequence may bring any number of rows.  The caller owns every buffer.  The
+ * functions check their arguments on the host and only enqueue, on `stream`. */
+#define EBD_KV_BF16 0
+#define EBD_KV_E4M3 1
+
+typedef struct {
+  void* k;                    /* device pools, 16-byte aligned:                  */
+  void* v;                    /* [n_pages][n_heads_kv][page_size][head_dim]      */
+  uint8_t* k_scale;           /* EBD_KV_E4M3: exponent bytes, 16-byte aligned,   */
+  uint8_t* v_scale;           /* [n_pages][n_heads_kv][page_size]; else unused   */
+  const int32_t* page_table;  /* [batch][max_pages]; a negative entry: no page   */
+  int64_t page_stride;        /* elements of k, and of v, from page to page, a
+                                 multiple of 16 bytes; 0: dense                 */
+  int32_t dtype;              /* EBD_KV_BF16 or EBD_KV_E4M3                      */
+  int32_t page_size;          /* a power of two, 16..256                         */
+  int32_t n_pages;            /* pages of the pools                              */
+  int32_t max_pages;          /* second dimension of page_table                  */
+} ebd_kv_pages;
+
+typedef struct {
+  int32_t batch;              /* B <= max_batch                                  */
+  int32_t rows;               /* R = cu_rows[B] <= max_rows (host copy)          */
+  const int32_t* cu_rows;     /* [B+1] row offsets, cu_rows[0] = 0               */
+  const int32_t* row_pos;     /* [R] position of each row, no two rows of a
+                                 sequence at one position (write, read)         */
+  const int32_t* kv_len;      /* [B] cached positions [0, kv_len), the new rows'
+                                 own at their end (attention)                   */
+  const uint16_t* q;          /* [R] rows [n_heads_q][head_dim] bf16             */
+  uint16_t* k;                /* [R] rows [n_heads_kv][head_dim] bf16: read by   */
+  uint16_t* v;                /* ebd_paged_write, written by ebd_paged_read      */
+  uint16_t* out;              /* [R][n_heads_q][head_dim] bf16 attention output  */
+  const uint8_t* skip;        /* ebd_paged_write: [R] rows with a non-zero byte
+                                 are not written (a step's mask: committed rows
+                                 only); NULL: all are                           */
+  int64_t q_stride;           /* elements from row to row of q, and of k and v,  */
+  int64_t kv_stride;          /* a multiple of 8 (slices of a fused projection's
+                                 rows); 0: dense                                */
+  float scale;                /* factor of q . k; 0: 1 / sqrt(head_dim)          */
+  int32_t causal;             /* 0: every row of a sequence sees all its cached
+                                 positions; 1: row i of its n rows sees those
+                                 before kv_len - n + i + 1                      */
+  int32_t max_new;            /* rows of the sequence that brings most, where the
+                                 caller knows it; 0: unknown.  It only chooses
+                                 how the call is run.                           */
+  int32_t reserved;
+} ebd_paged_args;
+
+/* Writes rows a->k, a->v into the pages at a->row_pos.  Rows outside the page
+ * table, or whose entry names no page of the pools, are skipped. */
+ebd_status ebd_paged_write(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a,
+                           void* stream);
+
+/* Reads the rows at a->row_pos back into a->k, a->v as bf16.  Rows outside the
+ * page table, or whose entry names no page, come back as zeros. */
+ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a,
+                          void* stream);
+
+/* Attention of the rows a->q over the pages (handles with ebd_config.paged = 1;
+ * EBD_ERR_STATE otherwise): softmax(scale * q k^T) v per query head, K/V head
+ * h of the n_heads_q / n_heads_kv query heads from h * that many on, with fp32
+ * sums and the probabilities rounded to bf16 where they multiply v; bf16 output.
+ * A row that sees no position gives zeros.  What pages hold past kv_len, and
+ * what a causal row does not see, has no part in its result, whatever it is.
+ * kv_len beyond the page table is cut to it; a position before kv_len whose
+ * entry names no page of the pools records EBD_ERR_BOUNDS (the call's outputs
+ * are then undefined). */
+ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a,
+                               void* stream);
 
 /* Synchronises `stream`, returns the first device-side failure recorded
  * since the last call (EBD_OK if none) and clears it. */

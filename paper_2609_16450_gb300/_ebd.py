@@ -6,7 +6,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, Structure, c_char_p, c_float, c_int32, c_size_t, c_uint64,
+from ctypes import (POINTER, Structure, c_char_p, c_float, c_int32, c_int64, c_size_t, c_uint64,
                     c_void_p)
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -39,7 +39,7 @@ class ebd_config(Structure):
                 ("l_min", c_int32), ("l_b", c_int32), ("eos_id", c_int32),
                 ("lps_enabled", c_int32), ("tau", c_float), ("tau_psi", c_float),
                 ("seed", c_uint64), ("debug_flags", c_int32), ("decode_mode", c_int32),
-                ("top_m", c_int32), ("reserved", c_int32)]
+                ("top_m", c_int32), ("paged", c_int32)]
 
 
 class ebd_step_args(Structure):
@@ -55,13 +55,32 @@ class ebd_step_args(Structure):
                 ("suffix", c_void_p)]
 
 
+EBD_KV_BF16 = 0
+EBD_KV_E4M3 = 1
+
+
+class ebd_kv_pages(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("page_table", c_void_p), ("page_stride", c_int64), ("dtype", c_int32),
+                ("page_size", c_int32), ("n_pages", c_int32), ("max_pages", c_int32)]
+
+
+class ebd_paged_args(Structure):
+    _fields_ = [("batch", c_int32), ("rows", c_int32), ("cu_rows", c_void_p),
+                ("row_pos", c_void_p), ("kv_len", c_void_p), ("q", c_void_p), ("k", c_void_p),
+                ("v", c_void_p), ("out", c_void_p), ("skip", c_void_p), ("q_stride", c_int64),
+                ("kv_stride", c_int64), ("scale", c_float), ("causal", c_int32),
+                ("max_new", c_int32), ("reserved", c_int32)]
+
+
 EXPORTS = ["ebd_create", "ebd_destroy", "ebd_bind_embedding", "ebd_step", "ebd_step_host",
            "ebd_decide", "ebd_lm_stats", "ebd_attention", "ebd_sync_status",
            "ebd_export_weights", "ebd_import_weights", "ebd_router_init_host",
            "ebd_weight_count", "ebd_lm_head_packed_bytes", "ebd_pack_lm_head",
            "ebd_profile_enable", "ebd_profile_read", "ebd_last_error",
            "ebd_version", "ebd_lm_stats_noalloc", "ebd_loop_window",
-           "ebd_loop_block_window", "ebd_lm_shard_state", "ebd_merge_shard_states"]
+           "ebd_loop_block_window", "ebd_lm_shard_state", "ebd_merge_shard_states",
+           "ebd_paged_write", "ebd_paged_read", "ebd_paged_attention"]
 
 _lib = None
 
@@ -89,6 +108,8 @@ def load(path: str = LIB_PATH):
     lib.ebd_bind_embedding.argtypes = [c_void_p, c_void_p, c_void_p]
     for fn in ("ebd_step", "ebd_step_host", "ebd_decide", "ebd_lm_stats", "ebd_attention"):
         getattr(lib, fn).argtypes = [c_void_p, P(ebd_step_args), c_void_p]
+    for fn in ("ebd_paged_write", "ebd_paged_read", "ebd_paged_attention"):
+        getattr(lib, fn).argtypes = [c_void_p, P(ebd_kv_pages), P(ebd_paged_args), c_void_p]
     lib.ebd_sync_status.argtypes = [c_void_p, c_void_p]
     lib.ebd_export_weights.argtypes = [c_void_p, c_void_p, P(c_size_t)]
     lib.ebd_import_weights.argtypes = [c_void_p, c_void_p, c_size_t]
@@ -174,6 +195,18 @@ def ebd_merge_shard_states(h, states_ptr: int, shards: int, args: ebd_step_args,
 
 def ebd_attention(h, args: ebd_step_args, stream: int = 0) -> int:
     return load().ebd_attention(h, ctypes.byref(args), c_void_p(stream))
+
+
+def ebd_paged_write(h, pages: ebd_kv_pages, args: ebd_paged_args, stream: int = 0) -> int:
+    return load().ebd_paged_write(h, ctypes.byref(pages), ctypes.byref(args), c_void_p(stream))
+
+
+def ebd_paged_read(h, pages: ebd_kv_pages, args: ebd_paged_args, stream: int = 0) -> int:
+    return load().ebd_paged_read(h, ctypes.byref(pages), ctypes.byref(args), c_void_p(stream))
+
+
+def ebd_paged_attention(h, pages: ebd_kv_pages, args: ebd_paged_args, stream: int = 0) -> int:
+    return load().ebd_paged_attention(h, ctypes.byref(pages), ctypes.byref(args), c_void_p(stream))
 
 
 def ebd_sync_status(h, stream: int = 0) -> int:

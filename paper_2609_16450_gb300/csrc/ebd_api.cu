@@ -13,6 +13,7 @@
 
 #include "ebd.h"
 #include "internal.h"
+#include "paged.h"
 #include "rows_image.h"
 
 namespace {
@@ -251,6 +252,10 @@ struct ebd_handle {
   cudaEvent_t ev[4] = {nullptr, nullptr, nullptr, nullptr};
   int profile = 0;
   int prof_mode = 0, prof_attn = 0;  // what the last ebd_step recorded
+  // ebd_paged_attention (cfg.paged): partial results of split tiles
+  float* paged_part = nullptr;
+  float* paged_part_ml = nullptr;
+  int* paged_tickets = nullptr;
   // ebd_step_host: the attention's inputs on a copy engine (set up with the handle)
   int copy_route = -1;               // -1 not set up yet, 0 unavailable, 1 ready
   cudaStream_t s_copy = nullptr;
@@ -324,6 +329,7 @@ ebd_status validate_config(const ebd_config* c, std::string& why) {
   if (c->decode_mode < EBD_DECODE_EB || c->decode_mode > EBD_DECODE_TOPM)
     return bad("decode_mode must be EBD_DECODE_EB, _THRESHOLD or _TOPM");
   if (c->decode_mode == EBD_DECODE_TOPM && c->top_m < 1) return bad("top_m must be >= 1");
+  if (c->paged != 0 && c->paged != 1) return bad("paged must be 0 or 1");
   return EBD_OK;
 }
 
@@ -937,6 +943,17 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     if ((e = cudaMemset(h->tickets, 0, static_cast<size_t>(slots) * sizeof(int))) != cudaSuccess)
       return bail(cuda_fail(h, e, "cudaMemset(tickets)"));
   }
+  if (cfg->paged) {
+    if ((e = paged_configure()) != cudaSuccess) return bail(cuda_fail(h, e, "paged attention attributes"));
+    const size_t ctas = static_cast<size_t>(h->num_sms) * kPagedCtasPerSm;
+    const size_t rows = ctas * 2 * kPagedRows;
+    if ((e = cudaMalloc(&h->paged_part, rows * (cfg->head_dim + 2) * sizeof(float))) != cudaSuccess)
+      return bail(cuda_fail(h, e, "cudaMalloc(paged attention partials)"));
+    h->paged_part_ml = h->paged_part + rows * cfg->head_dim;
+    if ((e = cudaMalloc(&h->paged_tickets, ctas * sizeof(int))) != cudaSuccess ||
+        (e = cudaMemset(h->paged_tickets, 0, ctas * sizeof(int))) != cudaSuccess)
+      return bail(cuda_fail(h, e, "cudaMalloc(paged attention tickets)"));
+  }
   if ((e = cudaMalloc(&h->d_status, sizeof(int))) != cudaSuccess)
     return bail(cuda_fail(h, e, "cudaMalloc(status)"));
   if ((e = cudaMemset(h->d_status, 0, sizeof(int))) != cudaSuccess)
@@ -1016,6 +1033,8 @@ void ebd_destroy(ebd_handle* h) {
   cudaFree(h->part_i);
   cudaFree(h->attn_part);
   cudaFree(h->tickets);
+  cudaFree(h->paged_part);
+  cudaFree(h->paged_tickets);
   cudaFree(h->d_status);
   cudaFreeHost(h->h_status);
   cudaFree(h->staging);
@@ -1534,6 +1553,170 @@ ebd_status ebd_profile_read(ebd_handle* h, float* ms) {
     if ((e = span(1, 3, &ms[2])) != cudaSuccess) return cuda_fail(h, e, "cudaEventElapsedTime");
     ms[0] = -1.f;
   }
+  return EBD_OK;
+}
+
+namespace {
+
+// Arguments that the three calls share; `name` begins the messages.
+ebd_status check_paged(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a) {
+  auto bad = [&](const char* m) { return fail(h, EBD_ERR_INVALID_ARG, m); };
+  if (c == nullptr || a == nullptr) return bad("pages and args must be set");
+  const ebd_config& f = h->cfg;
+  if (a->batch < 0 || a->batch > f.max_batch) return bad("batch out of range");
+  if (a->rows < 0 || a->rows > f.max_rows) return bad("rows out of range");
+  if (a->batch > kPagedMaxBatch) return fail(h, EBD_ERR_UNSUPPORTED, "more than 4096 sequences");
+  if (c->dtype != EBD_KV_BF16 && c->dtype != EBD_KV_E4M3) return bad("dtype must be EBD_KV_BF16 or EBD_KV_E4M3");
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)) != 0)
+    return bad("page_size must be a power of two from 16 to 256");
+  if (c->n_pages < 1 || c->max_pages < 1) return bad("n_pages and max_pages must be positive");
+  if (!c->k || !c->v || !c->page_table || !aligned(c->k, 16) || !aligned(c->v, 16))
+    return bad("the pools (16-byte aligned) and the page table must be set");
+  if (c->dtype == EBD_KV_E4M3 &&
+      (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)))
+    return bad("an e4m3 cache needs k_scale and v_scale, 16-byte aligned");
+  const int64_t page = static_cast<int64_t>(f.n_heads_kv) * c->page_size * f.head_dim;
+  const int64_t per16 = c->dtype == EBD_KV_E4M3 ? 16 : 8;  // elements of 16 bytes
+  if (c->page_stride != 0 && (c->page_stride < page || c->page_stride % per16 != 0))
+    return bad("page_stride must be 0, or a page or more and a multiple of 16 bytes");
+  if (a->rows > 0 && (!a->cu_rows || a->batch == 0)) return bad("rows need cu_rows and a batch");
+  return EBD_OK;
+}
+
+int64_t page_bytes(const ebd_handle* h, const ebd_kv_pages* c) {
+  const int64_t dense = static_cast<int64_t>(h->cfg.n_heads_kv) * c->page_size * h->cfg.head_dim;
+  return (c->page_stride != 0 ? c->page_stride : dense) * (c->dtype == EBD_KV_E4M3 ? 1 : 2);
+}
+
+int log2_of(int n) {
+  int l = 0;
+  while ((1 << l) < n) ++l;
+  return l;
+}
+
+// Tensor map of a pool, (element, place, head, page), in boxes of `box` keys of
+// one head: 64 bf16 or all e4m3 elements across, 128-byte rows swizzled.
+bool encode_pool(CUtensorMap* m, const void* base, const ebd_handle* h, const ebd_kv_pages* c, int box) {
+  auto fn = get_encode();
+  if (fn == nullptr) return false;
+  const bool e4m3 = c->dtype == EBD_KV_E4M3;
+  const cuuint64_t D = static_cast<cuuint64_t>(h->cfg.head_dim), row = D * (e4m3 ? 1 : 2);
+  const cuuint64_t dims[4] = {D, static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(h->cfg.n_heads_kv),
+                              static_cast<cuuint64_t>(c->n_pages)};
+  const cuuint64_t str[3] = {row, row * c->page_size, static_cast<cuuint64_t>(page_bytes(h, c))};
+  const cuuint32_t bx[4] = {static_cast<cuuint32_t>(e4m3 ? D : 64), static_cast<cuuint32_t>(box), 1, 1};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+            dims, str, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            e4m3 && D == 64 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+ebd_status paged_rows(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, bool write, void* stream) {
+  if (h == nullptr) return EBD_ERR_INVALID_ARG;
+  NvtxRange range(write ? "ebd_paged_write" : "ebd_paged_read");
+  ebd_status s = check_device(h);
+  if (s != EBD_OK) return s;
+  if ((s = check_paged(h, c, a)) != EBD_OK) return s;
+  if (a->rows == 0) return EBD_OK;
+  const ebd_config& f = h->cfg;
+  const int64_t width = static_cast<int64_t>(f.n_heads_kv) * f.head_dim;
+  const int64_t stride = a->kv_stride != 0 ? a->kv_stride : width;
+  if (!a->row_pos || !a->k || !a->v || !aligned(a->k, 16) || !aligned(a->v, 16))
+    return fail(h, EBD_ERR_INVALID_ARG, "row_pos, k and v (16-byte aligned) must be set");
+  if (stride < width || stride % 8 != 0)
+    return fail(h, EBD_ERR_INVALID_ARG, "kv_stride must be 0, or a row or more and a multiple of 8");
+  PagedRowsParams p{};
+  p.B = a->batch;
+  p.R = a->rows;
+  p.Hkv = f.n_heads_kv;
+  p.D = f.head_dim;
+  p.page_log2 = log2_of(c->page_size);
+  p.n_pages = c->n_pages;
+  p.max_pages = c->max_pages;
+  p.e4m3 = c->dtype == EBD_KV_E4M3;
+  p.page_stride = page_bytes(h, c);
+  p.cu_rows = a->cu_rows;
+  p.row_pos = a->row_pos;
+  p.page_table = c->page_table;
+  p.k_pool = static_cast<uint8_t*>(c->k);
+  p.v_pool = static_cast<uint8_t*>(c->v);
+  p.k_scale = c->k_scale;
+  p.v_scale = c->v_scale;
+  p.k = reinterpret_cast<__nv_bfloat16*>(a->k);
+  p.v = reinterpret_cast<__nv_bfloat16*>(a->v);
+  p.kv_stride = stride;
+  p.skip = write ? a->skip : nullptr;
+  cudaError_t e = write ? launch_paged_write(p, static_cast<cudaStream_t>(stream))
+                        : launch_paged_read(p, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, write ? "paged write launch" : "paged read launch");
+  return EBD_OK;
+}
+
+}  // namespace
+
+ebd_status ebd_paged_write(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, void* stream) {
+  return paged_rows(h, c, a, true, stream);
+}
+
+ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, void* stream) {
+  return paged_rows(h, c, a, false, stream);
+}
+
+ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, void* stream) {
+  if (h == nullptr) return EBD_ERR_INVALID_ARG;
+  NvtxRange range("ebd_paged_attention");
+  ebd_status s = check_device(h);
+  if (s != EBD_OK) return s;
+  if (h->paged_part == nullptr) return fail(h, EBD_ERR_STATE, "the handle was made without ebd_config.paged");
+  if ((s = check_paged(h, c, a)) != EBD_OK) return s;
+  if (a->rows == 0) return EBD_OK;
+  const ebd_config& f = h->cfg;
+  const int64_t width = static_cast<int64_t>(f.n_heads_q) * f.head_dim;
+  const int64_t stride = a->q_stride != 0 ? a->q_stride : width;
+  if (!a->kv_len || !a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16))
+    return fail(h, EBD_ERR_INVALID_ARG, "kv_len, q and out (16-byte aligned) must be set");
+  if (stride < width || stride % 8 != 0)
+    return fail(h, EBD_ERR_INVALID_ARG, "q_stride must be 0, or a row or more and a multiple of 8");
+  if (a->causal != 0 && a->causal != 1) return fail(h, EBD_ERR_INVALID_ARG, "causal must be 0 or 1");
+  if (a->max_new < 0) return fail(h, EBD_ERR_INVALID_ARG, "max_new must not be negative");
+  if (!(a->scale == a->scale) || std::isinf(a->scale)) return fail(h, EBD_ERR_INVALID_ARG, "scale is not finite");
+  PagedParams p{};
+  p.B = a->batch;
+  p.R = a->rows;
+  p.Hq = f.n_heads_q;
+  p.Hkv = f.n_heads_kv;
+  p.group = f.n_heads_q / f.n_heads_kv;
+  p.causal = a->causal;
+  p.page_log2 = log2_of(c->page_size);
+  p.n_pages = c->n_pages;
+  p.max_pages = c->max_pages;
+  p.box_log2 = p.page_log2 < 6 ? p.page_log2 : 6;
+  p.above = 0;
+  p.upto = 0x7fffffff;
+  const float scale = a->scale != 0.f ? a->scale : 1.f / std::sqrt(static_cast<float>(f.head_dim));
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.cu_rows = a->cu_rows;
+  p.kv_len = a->kv_len;
+  p.page_table = c->page_table;
+  p.k_scale = c->k_scale;
+  p.v_scale = c->v_scale;
+  p.q = reinterpret_cast<const __nv_bfloat16*>(a->q);
+  p.q_stride = stride;
+  p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
+  p.part = h->paged_part;
+  p.part_ml = h->paged_part_ml;
+  p.tickets = h->paged_tickets;
+  p.status = h->d_status;
+  p.limit_ns = kLimitNs;
+  const int longest = a->max_new > 0 && a->max_new < a->rows ? a->max_new : a->rows;
+  const int64_t m = static_cast<int64_t>(longest) * p.group;
+  CUtensorMap tk, tv;
+  if (!encode_pool(&tk, c->k, h, c, 1 << p.box_log2) || !encode_pool(&tv, c->v, h, c, 1 << p.box_log2))
+    return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (pages) failed");
+  cudaError_t e = launch_paged_attention(tk, tv, p, f.head_dim, c->dtype == EBD_KV_E4M3, m <= 16 ? 1 : m <= 32 ? 2 : 4,
+                                         h->num_sms, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "paged attention launch");
   return EBD_OK;
 }
 

@@ -1,0 +1,861 @@
+// Attention over the paged K/V cache with few query rows per K/V head (single
+// tokens, short windows): o_i = sum_j p_ij v_j / sum_j p_ij with p_ij =
+// exp2(c q_i k_j - m_i), c = scale * log2 e, over the keys j that row i sees.
+//
+// A tile is up to 16, 32 or 64 packed rows (row of the sequence, query head of
+// the group) of one sequence and K/V head.  Each CTA takes an equal share of
+// all tiles' 64-key chunks (paged.h).
+//   warp 4: loads.  The rows of q, and per chunk K and V as TMA boxes of a
+//     page (or 64 keys of it), each operand into a slot of one ring.
+//   warps 0-3: the scores of 16 keys of every chunk each; the probabilities
+//     meet in shared memory, and each warp multiplies all of them with D / 4
+//     columns of V.  A warp's output is then D / 4 columns, not D, which keeps
+//     a tile of 32 rows within the registers of two or three CTAs per SM, and
+//     no outputs have to meet when a tile ends.  One barrier per chunk.
+// Products run on mma.sync with fp32 sums.  The order of the contraction over
+// D is free, as long as q and k share it: a lane takes its K in 16-byte pieces
+// as they lie in memory, without ldmatrix.
+//
+// 8-bit cache.  Scores: q is split into two e4m3 terms (its 8 significant bits
+// are 4 + 4; the row is scaled by a power of two so that its largest element
+// is in (224, 448], and elements below 2^-11 of that lose what is under 2^-19
+// of it), and both multiply the codes themselves (m16n8k32, whose sums are as
+// exact as those of bf16), so K needs no conversion; the key's scale, a power
+// of two, multiplies the score.  Values: codes become bf16 by moving their
+// bits (sign, then exponent and mantissa four lower: 2^-120 times the value)
+// and a bf16 multiplication by 2^120, exactly; the scale of a value's row
+// multiplies its probabilities, also exactly.
+// P is rounded to bf16, as the output is; its sum is of the unrounded values.
+//
+// The running maximum moves only when a score exceeds it by more than 8 (log2
+// units), so that exp2 stays below 256 and most chunks rescale nothing.
+#include <cuda_fp16.h>
+#include <type_traits>
+
+#include "paged.h"
+#include "ptx.cuh"
+
+namespace ebd {
+
+namespace {
+
+constexpr int kCH = 64;             // keys of a chunk
+constexpr int kThreads = 160;
+constexpr int kLeast = 3;           // chunks of a share, at least
+constexpr int kNever = 0x7fffffff;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+// D += A B, m16n8k32, e4m3 inputs, fp32 accumulators
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// the two e4m3 codes of (x, y), y in the upper byte
+__device__ __forceinline__ uint32_t e4m3x2(float x, float y) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_value(uint32_t c) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(c)));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+// 2^(e - 127) of an exponent byte
+__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e > 0 ? e << 23 : 1u << 22); }
+
+// CTAs per SM: as many as registers and a ring of two chunks or more allow.
+constexpr int ctas_per_sm(bool e4m3, int mb) { return e4m3 && mb <= 2 ? 3 : 2; }
+
+// Shared memory (offsets from a 1024-byte aligned base).
+template <int D, bool E4M3, int MB>
+struct Map {
+  static constexpr int T = 16 * MB;                               // tile rows
+  static constexpr uint32_t kOp = kCH * D * (E4M3 ? 1 : 2);       // K or V of a chunk
+  static constexpr uint32_t kQRow = 2 * D + 16;                   // padded: rows in distinct banks
+  static constexpr int kQSlots = MB == 2 ? 2 : 1;                 // one row block keeps q in registers
+  static constexpr uint32_t kAll = (ctas_per_sm(E4M3, MB) == 3 ? 75 : 113) * 1024 - 1024;
+  static constexpr uint32_t kFixed = kQSlots * T * kQRow + 2 * T * 128 + 3 * D * 4 + 2 * 4 * T * 4 + 4 * T * 4 +
+                                     T * 4 + 512;
+  static constexpr uint32_t kSlotBytes = kOp + (E4M3 ? 64 : 0) + 16;
+  static constexpr int S = (kAll - kFixed) / kSlotBytes > 16 ? 16 : (kAll - kFixed) / kSlotBytes;  // ring slots
+  static constexpr uint32_t kRing = 0;
+  static constexpr uint32_t kP = kRing + S * kOp;                 // [2][T][128 B]: P of a chunk
+  static constexpr uint32_t kScale = kP + 2 * T * 128;
+  static constexpr uint32_t kQ = kScale + S * (E4M3 ? 64 : 0);
+  static constexpr uint32_t kBad = kQ + kQSlots * T * kQRow;      // [3][D]
+  static constexpr uint32_t kXl = kBad + 3 * D * 4;               // [2][4][T] sums of the warps
+  static constexpr uint32_t kXm = kXl + 2 * 4 * T * 4;            // [4][T] maxima of the warps
+  static constexpr uint32_t kRowF = kXm + 4 * T * 4;              // [T] score factors of the rows
+  static constexpr uint32_t kBar = kRowF + T * 4;
+  static constexpr int kNBar = 2 * S + 2 * kQSlots;
+  static constexpr uint32_t kPlan = kBar + kNBar * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32 + 1) * 8;
+  static constexpr uint32_t kBytes = kMisc + 16;
+  static constexpr uint32_t kDyn = kBytes + 1024;
+  static_assert(S >= 4 && kBytes <= kAll && (kP % 1024) == 0 && (kQ % 16) == 0, "shared memory");
+};
+
+// What the chunks of a piece need: constant over a piece, or carried along.
+template <int MB>
+struct Rows {
+  int lim[MB][2];     // keys before this one are seen by rows g and g + 8 of each block
+  float f[MB][2];     // score factor
+  float m[MB][2], sub[MB][2];  // running maximum, and what is subtracted (0 while -inf)
+  float l[MB][2];     // sum of this lane's probabilities
+};
+
+__device__ __forceinline__ bool barrier_or(uint32_t id, uint32_t n, bool pred) {
+  uint32_t r;
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, %2, %3, p;\n"
+      " selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(r)
+      : "r"((uint32_t)pred), "r"(id), "r"(n)
+      : "memory");
+  return r != 0;
+}
+
+template <int D, bool E4M3, int MB>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
+    paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                      const PagedParams p) {
+  using L = Map<D, E4M3, MB>;
+  constexpr int T = L::T, S = L::S;
+  constexpr int NT = D / 32;                  // output column tiles of a warp
+  constexpr int NJ = E4M3 ? D / 64 : D / 32;  // 16-byte pieces of a K row per lane
+  constexpr int NB = E4M3 ? 1 : D / 64;       // boxes of 128-byte rows across D
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
+  uint64_t* empty = full + S;
+  uint64_t* qfull = empty + S;
+  uint64_t* qempty = qfull + L::kQSlots;
+  PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
+  auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc);
+  int* s_flag = reinterpret_cast<int*>(smem + L::kMisc + 4);
+  int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 8);
+  int* bad = reinterpret_cast<int*>(smem + L::kBad);
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&full[s], 1);
+      mbar_init(&empty[s], 4);
+    }
+    for (int s = 0; s < L::kQSlots; ++s) {
+      mbar_init(&qfull[s], 1);
+      mbar_init(&qempty[s], 4);
+    }
+    *abort = 0;
+    *s_bad = 0;
+    fence_mbar_init();
+  }
+  for (int i = tid; i < 3 * D; i += kThreads) bad[i] = kNever;
+  paged_plan<kThreads>(p, T, kCH, kLeast, plan, scan);
+  PagedWalk w;
+  if (!w.begin(p, *plan, T, kCH)) return;
+
+  if (warp == 4) {
+    // ------------------------------------------------------------ loads
+    const int np_log = 6 - p.box_log2, box = 1 << p.box_log2;
+    const int pc = lane & ((1 << np_log) - 1), part = lane >> np_log;
+    const int key_in = pc << p.box_log2;
+    int n = 0, pieces = 0;
+    bool ok = true;
+    do {
+      const int last = min(w.s.n - 1, (w.t * T + T - 1) / p.group);
+      const int rows = min(T, w.s.n * p.group - w.t * T);
+      {  // q: rows by lane, zeros past the tile's last
+        const int qs = pieces % L::kQSlots;
+        uint8_t* qd = smem + L::kQ + qs * T * L::kQRow;
+        ok = pieces < L::kQSlots ||
+             mbar_wait(&qempty[qs], static_cast<uint32_t>(pieces / L::kQSlots - 1) & 1u, p.limit_ns, abort);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        for (int i = rows * (D / 8) + lane; i < T * (D / 8); i += 32)
+          *reinterpret_cast<uint4*>(qd + (i / (D / 8)) * L::kQRow + (i % (D / 8)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        fence_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(&qfull[qs], static_cast<uint32_t>(rows) * D * 2);
+        __syncwarp();
+        for (int r = lane; r < rows; r += 32) {
+          const int m = w.t * T + r, i = m / p.group, hl = m - i * p.group;
+          bulk_load(qd + r * L::kQRow,
+                    p.q + (w.s.r0 + i) * p.q_stride + static_cast<long long>(w.h * p.group + hl) * D, D * 2, &qfull[qs]);
+        }
+        ++pieces;
+      }
+      const int lim = paged_limit(p, w.s, last);
+      const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
+      int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
+      for (int c = w.c0; c < w.c1 && ok; ++c) {
+        const int key = c * kCH + key_in;
+        const int first = (c * kCH) >> p.page_log2;
+        if (first >= win0 + 32 || first < win0) {
+          win0 = first & ~31;
+          win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
+        }
+        int page = __shfl_sync(0xffffffffu, win, ((key >> p.page_log2) - win0) & 31);
+        const bool mine = part < (E4M3 ? 2 : NB) && key < lim;
+        if (mine && (page < 0 || page >= p.n_pages)) {
+          atomicCAS(p.status, 0, EBD_ERR_BOUNDS);
+          page = 0;
+        }
+        const int pieces_here = min(max((lim - c * kCH + box - 1) >> p.box_log2, 0), 1 << np_log);
+        const uint32_t bytes = static_cast<uint32_t>(pieces_here) * box * (E4M3 ? D + 1 : 2 * D);
+        const int off = key & ((1 << p.page_log2) - 1);
+#pragma unroll
+        for (int v = 0; v < 2; ++v, ++n) {
+          const int s = n % S;
+          ok = ok && (n < S || mbar_wait(&empty[s], static_cast<uint32_t>(n / S - 1) & 1u, p.limit_ns, abort));
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(&full[s], bytes);
+          __syncwarp();
+          if (mine) {
+            uint8_t* d = smem + L::kRing + s * L::kOp;
+            if (E4M3 && part == 1)
+              bulk_load(smem + L::kScale + s * 64 + key_in,
+                        (v ? p.v_scale : p.k_scale) +
+                            ((static_cast<long long>(page) * p.Hkv + w.h) << p.page_log2) + off,
+                        box, &full[s]);
+            else
+              tma_load_4d(d + part * 8192 + key_in * (E4M3 ? D : 128), v ? &tm_v : &tm_k, &full[s], part * 64, off,
+                          w.h, page);
+          }
+        }
+      }
+    } while (ok && w.next(p));
+    if (!ok) {
+      if (lane == 0 && !*abort) {
+        *abort = 1;
+        atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
+      }
+      // the copies in flight land before the CTA can exit
+      for (int j = max(0, n - S); j < n; ++j)
+        mbar_wait(&full[j % S], static_cast<uint32_t>(j / S) & 1u, p.limit_ns, nullptr);
+      for (int j = max(0, pieces - L::kQSlots); j < pieces; ++j)
+        mbar_wait(&qfull[j % L::kQSlots], static_cast<uint32_t>(j / L::kQSlots) & 1u, p.limit_ns, nullptr);
+    }
+    return;
+  }
+
+  // -------------------------------------------------------------- products
+  const int g = lane >> 2, t4 = lane & 3;
+  const int kb = warp * 16;  // this warp's keys of a chunk
+  float* xm = reinterpret_cast<float*>(smem + L::kXm);
+  float* xl = reinterpret_cast<float*>(smem + L::kXl);
+  float* rowf = reinterpret_cast<float*>(smem + L::kRowF);
+  int nchunk = 0;
+  bool ok = true;
+  int slot = 0, pieces = 0;
+  uint32_t phase = 0;
+  auto step = [&]() {
+    if (++slot == S) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  };
+  do {
+    const int m0 = w.t * T;
+    const int mtot = w.s.n * p.group;
+    const int rows = min(T, mtot - m0);
+    const int lim_lo = paged_limit(p, w.s, m0 / p.group);
+    const int lim_hi = paged_limit(p, w.s, (m0 + rows - 1) / p.group);
+    const int len = w.s.len;
+    const int qs = pieces % L::kQSlots, par = pieces & 1;
+    uint8_t* qd = smem + L::kQ + qs * T * L::kQRow;
+    Rows<MB> R;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi) {
+        const int m = m0 + mb * 16 + hi * 8 + g;
+        R.lim[mb][hi] = m < mtot ? paged_limit(p, w.s, m / p.group) : kNever;
+        R.f[mb][hi] = p.scale_log2;
+        R.m[mb][hi] = -INFINITY;
+        R.sub[mb][hi] = 0.f;
+        R.l[mb][hi] = 0.f;
+      }
+    float o[MB][NT][4];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[mb][j][i] = 0.f;
+
+    ok = ok && mbar_wait(&qfull[qs], static_cast<uint32_t>(pieces / L::kQSlots) & 1u, p.limit_ns, abort);
+    ok = __all_sync(0xffffffffu, ok);
+    // the codes of row r, element pieces (2 t4 + j) * 16: a0/a2 words of high
+    // and low terms; returns the row's power-of-two factor
+    auto split_row = [&](int r, uint32_t (&hi)[NJ][4], uint32_t (&lo)[NJ][4]) -> float {
+      const uint8_t* q = qd + r * L::kQRow;
+      uint4 x[NJ][2];
+      uint32_t amax = 0;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          x[j][i] = *reinterpret_cast<const uint4*>(q + ((NJ * t4 + j) * 2 + i) * 16);
+          const uint32_t v[4] = {x[j][i].x, x[j][i].y, x[j][i].z, x[j][i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) amax = max(amax, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
+        }
+      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const bool finite = amax < 0x7F80u;
+      const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 127;
+      const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t v[4] = {x[j][i].x, x[j][i].y, x[j][i].z, x[j][i].w};
+          uint32_t h2[4], l2[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float a = __uint_as_float(v[k] << 16) * inv, b = __uint_as_float(v[k] & 0xFFFF0000u) * inv;
+            h2[k] = e4m3x2(a, b);
+            const float2 hv = e4m3x2_value(h2[k]);
+            l2[k] = e4m3x2(a - hv.x, b - hv.y);
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            // a row with a value that is not finite has NaN scores
+            hi[j][2 * i + k] = finite ? (h2[2 * k] | (h2[2 * k + 1] << 16)) : 0x7F7F7F7Fu;
+            lo[j][2 * i + k] = l2[2 * k] | (l2[2 * k + 1] << 16);
+          }
+        }
+      return scale_value(static_cast<uint32_t>(e)) * p.scale_log2;
+    };
+    // q fragments: of one row block in registers
+    uint32_t qa[MB == 1 ? (E4M3 ? 2 * NJ : NJ) : 1][2][4];  // [.. terms][row g, g + 8][4 words = 2 k-steps]
+    if constexpr (MB == 1) {
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+          uint32_t a[NJ][4], b[NJ][4];
+          R.f[0][hi] = split_row(hi * 8 + g, a, b);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              qa[2 * j][hi][k] = a[j][k];
+              qa[2 * j + 1][hi][k] = b[j][k];
+            }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            const uint4 x = *reinterpret_cast<const uint4*>(qd + (hi * 8 + g) * L::kQRow +
+                                                            ((j >> 1) * 8 + 2 * t4 + (j & 1)) * 16);
+            qa[j][hi][0] = x.x;
+            qa[j][hi][1] = x.y;
+            qa[j][hi][2] = x.z;
+            qa[j][hi][3] = x.w;
+          }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&qempty[qs]);
+    } else if constexpr (E4M3) {
+      // the warps share the rows, one per 4 lanes at a time, in place
+#pragma unroll
+      for (int r0 = 0; r0 < T / 4; r0 += 8) {
+        uint32_t a[NJ][4], b[NJ][4];
+        const int r = warp * (T / 4) + r0 + g;
+        const float f = split_row(r, a, b);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          uint8_t* q = qd + r * L::kQRow + (NJ * t4 + j) * 16;
+          *reinterpret_cast<uint4*>(q) = make_uint4(a[j][0], a[j][1], a[j][2], a[j][3]);
+          *reinterpret_cast<uint4*>(q + D) = make_uint4(b[j][0], b[j][1], b[j][2], b[j][3]);
+        }
+        if (t4 == 0) rowf[r] = f;
+      }
+      named_barrier(1, 128);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) R.f[mb][hi] = rowf[mb * 16 + hi * 8 + g];
+    }
+
+    // one chunk: EDGE where a key of it is past some row's limit
+    auto chunk = [&](int c, auto edge_c, bool fresh) {
+      constexpr bool EDGE = decltype(edge_c)::value;
+      const int key0 = c * kCH;
+      float s[MB][2][4];
+      ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
+      ok = __all_sync(0xffffffffu, ok);
+      [[maybe_unused]] float vs[2][2];  // scales of the values' rows
+      {
+        const uint8_t* kd = smem + L::kRing + slot * L::kOp;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[mb][nt][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          uint4 kx[2];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const int row = kb + nt * 8 + g;
+            uint32_t at;
+            if (E4M3 && D == 64)
+              at = row * 64 + t4 * 16;
+            else if (E4M3)
+              at = row * 128 + (((2 * t4 + j) ^ g) << 4);
+            else
+              at = (j >> 1) * 8192 + row * 128 + (((2 * t4 + (j & 1)) ^ g) << 4);
+            kx[nt] = *reinterpret_cast<const uint4*>(kd + at);
+          }
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int term = 0; term < (E4M3 ? 2 : 1); ++term) {
+              uint32_t x[2][4];  // rows g, g + 8
+#pragma unroll
+              for (int hi = 0; hi < 2; ++hi) {
+                if constexpr (MB == 1) {
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) x[hi][k] = qa[E4M3 ? 2 * j + term : j][hi][k];
+                } else {
+                  const uint8_t* q = qd + (mb * 16 + hi * 8 + g) * L::kQRow;
+                  const uint4 v = *reinterpret_cast<const uint4*>(
+                      q + (E4M3 ? term * D + (NJ * t4 + j) * 16 : ((j >> 1) * 8 + 2 * t4 + (j & 1)) * 16));
+                  x[hi][0] = v.x;
+                  x[hi][1] = v.y;
+                  x[hi][2] = v.z;
+                  x[hi][3] = v.w;
+                }
+              }
+              const uint32_t a0[4] = {x[0][0], x[1][0], x[0][1], x[1][1]};
+              const uint32_t a1[4] = {x[0][2], x[1][2], x[0][3], x[1][3]};
+#pragma unroll
+              for (int nt = 0; nt < 2; ++nt) {
+                if constexpr (E4M3) {
+                  mma_e4m3(s[mb][nt], a0, kx[nt].x, kx[nt].y);
+                  mma_e4m3(s[mb][nt], a1, kx[nt].z, kx[nt].w);
+                } else {
+                  mma_bf16(s[mb][nt], a0, kx[nt].x, kx[nt].y);
+                  mma_bf16(s[mb][nt], a1, kx[nt].z, kx[nt].w);
+                }
+              }
+            }
+        }
+        if constexpr (E4M3) {
+          const uint8_t* sc = smem + L::kScale + slot * 64 + kb;
+          float ks[2][2];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
+            ks[nt][0] = scale_value(two & 0xFFu);
+            ks[nt][1] = scale_value(two >> 8);
+          }
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[mb][nt][i] *= ks[nt][i & 1];
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[slot]);
+      step();
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (key0 + kb + nt * 8 + 2 * t4 + (i & 1) >= R.lim[mb][i >> 1]) s[mb][nt][i] = -INFINITY;
+      }
+      // V of the chunk: waited for here, as its rows' scales go into P
+      ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if constexpr (E4M3) {
+        const uint8_t* sc = smem + L::kScale + slot * 64 + kb;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
+          // a row that is NaN: its codes do not say so to P V
+          vs[nt][0] = (two & 0xFFu) == 0xFFu ? NAN : scale_value(two & 0xFFu);
+          vs[nt][1] = (two >> 8) == 0xFFu ? NAN : scale_value(two >> 8);
+        }
+      }
+      uint8_t* pd = smem + L::kP + (nchunk & 1) * T * 128;
+      // probabilities against the running maxima, into shared memory; the
+      // largest log2 of them
+      auto put_p = [&](bool sum) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -R.sub[mb][hi]);
+              const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -R.sub[mb][hi]);
+              top = fmaxf(top, fmaxf(y0, y1));
+              float e0 = ex2(y0), e1 = ex2(y1);
+              if (sum) R.l[mb][hi] += e0 + e1;
+              if constexpr (E4M3) {
+                // what a row does not see stays out, whatever its scale is
+                e0 = EDGE && s[mb][nt][2 * hi] == -INFINITY ? 0.f : e0 * vs[nt][0];
+                e1 = EDGE && s[mb][nt][2 * hi + 1] == -INFINITY ? 0.f : e1 * vs[nt][1];
+              }
+              const int r = mb * 16 + hi * 8 + g;
+              *reinterpret_cast<uint32_t*>(pd + r * 128 + (((2 * warp + nt) ^ g) << 4) + t4 * 4) = bf16x2(e0, e1);
+            }
+        return top;
+      };
+      float l0[MB][2];
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) l0[mb][hi] = R.l[mb][hi];
+      bool raise = fresh;
+      if (!fresh) raise = put_p(true) > 8.f;
+      if (barrier_or(1, 128, raise)) {
+        // new running maxima, of all warps' scores
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            float x = -INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) x = fmaxf(x, s[mb][nt][2 * hi + e] * R.f[mb][hi]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            if (t4 == 0) xm[warp * T + mb * 16 + hi * 8 + g] = x;
+          }
+        named_barrier(1, 128);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int hi = 0; hi < 2; ++hi) {
+            const float* q = xm + mb * 16 + hi * 8 + g;
+            const float mn = fmaxf(R.m[mb][hi], fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T])));
+            const float alpha = mn == R.m[mb][hi] ? 1.f : ex2(R.m[mb][hi] - mn);  // 0 from -inf
+            R.m[mb][hi] = mn;
+            R.sub[mb][hi] = mn == -INFINITY ? 0.f : mn;
+            R.l[mb][hi] = l0[mb][hi] * alpha;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              o[mb][j][2 * hi] *= alpha;
+              o[mb][j][2 * hi + 1] *= alpha;
+            }
+          }
+        put_p(true);
+        named_barrier(1, 128);
+      }
+      ++nchunk;
+
+      // P V: this warp's D / 4 columns
+      const uint8_t* vd = smem + L::kRing + slot * L::kOp;
+      // an element of a key that some row does not see, and that is not finite:
+      // kept out of the product and noted, for the rows that do see it (8-bit
+      // rows say so by their scale, above)
+      [[maybe_unused]] const bool scrub = EDGE && p.causal;
+      [[maybe_unused]] auto note = [&](int key, int d, int kind) {
+        atomicMin(&bad[kind * D + d], key);
+        *reinterpret_cast<volatile int*>(s_bad) = 1;
+      };
+      const uint32_t pb = smem_u32(pd);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        if (EDGE && key0 + ks * 16 >= lim_hi) break;
+        uint32_t a[MB][4];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          const int row = mb * 16 + (lane & 15);
+          ldsm_x4(pb + row * 128 + (((2 * ks + (lane >> 4)) ^ (lane & 7)) << 4), a[mb][0], a[mb][1], a[mb][2], a[mb][3]);
+        }
+        if constexpr (E4M3) {
+          uint32_t v[2][2];  // [nt][e]: NT bytes of key ks * 16 + nt * 8 + 2 t4 + e
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int row = ks * 16 + nt * 8 + 2 * t4 + e;
+              const int d = warp * (D / 4) + g * NT;
+              if constexpr (D == 128)
+                v[nt][e] = *reinterpret_cast<const uint32_t*>(vd + row * 128 + (((d >> 4) ^ (row & 7)) << 4) + (d & 15));
+              else
+                v[nt][e] = *reinterpret_cast<const uint16_t*>(vd + row * 64 + d);
+              if constexpr (EDGE) {
+                const int key = key0 + row;
+                if (key >= len) v[nt][e] = 0u;
+              }
+            }
+#pragma unroll
+          for (int hf = 0; hf < NT / 2; ++hf) {
+            uint32_t b[2][2];  // [column tile 2 hf + .][nt]
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+              // bytes (key 0, d), (key 0, d + 1), (key 1, d), (key 1, d + 1)
+              const uint32_t x = __byte_perm(v[nt][0], v[nt][1], hf ? 0x7632 : 0x5410);
+              const uint32_t d1 = (x & 0x80008000u) | ((x >> 4) & 0x07F007F0u);
+              const uint32_t d0 = ((x << 8) & 0x80008000u) | ((x << 4) & 0x07F007F0u);
+              b[0][nt] = mul_bf16x2(d0, 0x7B807B80u);  // 2^120
+              b[1][nt] = mul_bf16x2(d1, 0x7B807B80u);
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+              for (int mb = 0; mb < MB; ++mb) mma_bf16(o[mb][2 * hf + q], a[mb], b[q][0], b[q][1]);
+          }
+        } else {
+          const uint32_t vb = smem_u32(vd);
+          // matrices of an ldmatrix: keys 0-7 and 8-15 of one column tile, then of the next
+          const int vrow = ks * 16 + (lane & 15);
+#pragma unroll
+          for (int j = 0; j < NT; j += 2) {
+            uint32_t b[4];
+            const int ct = warp * NT + j;  // column tile
+            ldsm_x4_t(vb + (ct >> 3) * 8192 + vrow * 128 + ((((ct & 7) + (lane >> 4)) ^ (lane & 7)) << 4), b[0], b[1],
+                      b[2], b[3]);
+            if constexpr (EDGE) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const int key = key0 + ks * 16 + (i & 1) * 8 + 2 * t4 + e;
+                  const uint32_t x = (b[i] >> (16 * e)) & 0xFFFFu;
+                  bool drop = key >= len;
+                  if (!drop && scrub && key >= lim_lo && (x & 0x7F80u) == 0x7F80u) {
+                    note(key, (ct + (i >> 1)) * 8 + g, (x & 0x7Fu) ? 0 : (x & 0x8000u) ? 2 : 1);
+                    drop = true;
+                  }
+                  if (drop) b[i] &= e ? 0x0000FFFFu : 0xFFFF0000u;
+                }
+            }
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+              mma_bf16(o[mb][j], a[mb], b[0], b[1]);
+              mma_bf16(o[mb][j + 1], a[mb], b[2], b[3]);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[slot]);
+      step();
+    };
+
+    for (int c = w.c0; c < w.c1; ++c) {
+      if ((c + 1) * kCH > lim_lo)
+        chunk(c, std::true_type{}, c == w.c0);
+      else
+        chunk(c, std::false_type{}, c == w.c0);
+    }
+    if (!ok && lane == 0 && !*abort) {
+      *abort = 1;
+      atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
+    }
+    if constexpr (MB > 1) {
+      if constexpr (E4M3) fence_async();  // q was rewritten in place
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&qempty[qs]);
+    }
+    ++pieces;
+
+    // ---- results: this warp's columns; the rows' sums are of all four warps
+    float* wl = xl + par * 4 * T;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi) {
+        float l = R.l[mb][hi];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if (t4 == 0) wl[warp * T + mb * 16 + hi * 8 + g] = l;
+      }
+    named_barrier(1, 128);
+    const bool whole = w.whole();
+    const bool any_bad = *reinterpret_cast<volatile int*>(s_bad) != 0;
+    const int own_slot = 2 * static_cast<int>(blockIdx.x) + (w.c0 == 0 ? 1 : 0);
+    float* part = p.part + static_cast<long long>(own_slot) * kPagedRows * D;
+    float* part_ml = p.part_ml + static_cast<long long>(own_slot) * kPagedRows * 2;
+    if (!*abort) {
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+          const int r = mb * 16 + hi * 8 + g;
+          if (r >= rows) continue;
+          const float l = (wl[r] + wl[T + r]) + (wl[2 * T + r] + wl[3 * T + r]);
+          const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          // this lane's elements of the row: an 8-bit cache's NT columns of
+          // fragment column 2 t4, then those of 2 t4 + 1, which follow on
+          // them; a bf16 cache's columns 2 t4 and 2 t4 + 1 of each tile
+          float x[2 * NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[E4M3 ? e * NT + j : 2 * j + e] = o[mb][j][2 * hi + e] * inv;
+          if (any_bad) {
+            const int lim = R.lim[mb][hi];
+#pragma unroll
+            for (int k = 0; k < 2 * NT; ++k) {
+              const int d = warp * (D / 4) + (E4M3 ? 2 * NT * t4 + k : (k >> 1) * 8 + 2 * t4 + (k & 1));
+              if (lim > bad[D + d]) x[k] += INFINITY;
+              if (lim > bad[2 * D + d]) x[k] -= INFINITY;
+              if (lim > bad[d]) x[k] = NAN;
+            }
+          }
+          const int m = m0 + r, i = m / p.group, h = m - i * p.group;
+          __nv_bfloat16* od = p.out + (static_cast<long long>(w.s.r0 + i) * p.Hq + w.h * p.group + h) * D + warp * (D / 4);
+          float* pd = part + r * D + warp * (D / 4);
+          if constexpr (E4M3) {
+            if (whole) {
+#pragma unroll
+              for (int k = 0; k < NT; k += 2)
+                *reinterpret_cast<uint2*>(od + 2 * NT * t4 + 2 * k) =
+                    make_uint2(bf16x2(x[2 * k], x[2 * k + 1]), bf16x2(x[2 * k + 2], x[2 * k + 3]));
+            } else {
+#pragma unroll
+              for (int k = 0; k < 2 * NT; k += 4)
+                *reinterpret_cast<float4*>(pd + 2 * NT * t4 + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              if (whole)
+                *reinterpret_cast<uint32_t*>(od + j * 8 + 2 * t4) = bf16x2(x[2 * j], x[2 * j + 1]);
+              else
+                *reinterpret_cast<float2*>(pd + j * 8 + 2 * t4) = make_float2(x[2 * j], x[2 * j + 1]);
+            }
+          }
+          if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(R.m[mb][hi], l);
+        }
+    }
+    if (any_bad) {
+      named_barrier(1, 128);
+      for (int i = tid; i < 3 * D; i += 128) bad[i] = kNever;
+      if (tid == 0) *s_bad = 0;
+      named_barrier(1, 128);
+    }
+    if (!whole) {
+      // ---- the last CTA of a split tile puts its parts together, in order
+      __threadfence();
+      named_barrier(1, 128);
+      const long long ua = w.u - w.c0;  // the tile's first chunk
+      const int first = paged_owner(*plan, ua);
+      const int np = paged_owner(*plan, ua + w.nch - 1) - first + 1;
+      if (tid == 0) *s_flag = atomicAdd(&p.tickets[first], 1) == np - 1;
+      named_barrier(1, 128);
+      if (*s_flag) {
+        __threadfence();
+        if (tid == 0) p.tickets[first] = 0;
+        auto at = [&](int k) { return k == 0 ? 2 * first + 1 : 2 * (first + k); };
+        constexpr int D4 = D / 4;
+        for (int it = tid; it < rows * D4; it += 128) {
+          const int r = it / D4, d = (it - r * D4) * 4;
+          float mx = -INFINITY;
+          for (int k = 0; k < np; ++k) mx = fmaxf(mx, __ldcg(p.part_ml + (static_cast<long long>(at(k)) * kPagedRows + r) * 2));
+          float l = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int k = 0; k < np; ++k) {
+            const long long row = static_cast<long long>(at(k)) * kPagedRows + r;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
+            const float4 z = __ldcg(reinterpret_cast<const float4*>(p.part + row * D + d));
+            const float wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
+            l = fmaf(wgt, ml.y, l);
+            if (ml.x == -INFINITY) continue;  // a part that the row sees nothing of
+            acc.x = fmaf(wgt, z.x, acc.x);
+            acc.y = fmaf(wgt, z.y, acc.y);
+            acc.z = fmaf(wgt, z.z, acc.z);
+            acc.w = fmaf(wgt, z.w, acc.w);
+          }
+          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+          const int m = m0 + r, i = m / p.group, hl = m - i * p.group;
+          *reinterpret_cast<uint2*>(p.out + (static_cast<long long>(w.s.r0 + i) * p.Hq + w.h * p.group + hl) * D + d) =
+              make_uint2(bf16x2(acc.x * inv, acc.y * inv), bf16x2(acc.z * inv, acc.w * inv));
+        }
+      }
+      named_barrier(1, 128);  // s_flag is free again
+    }
+  } while (w.next(p));
+}
+
+template <int D, bool E4M3, int MB>
+cudaError_t configure() {
+  return cudaFuncSetAttribute(paged_attn_kernel<D, E4M3, MB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Map<D, E4M3, MB>::kDyn);
+}
+template <int D, bool E4M3>
+cudaError_t launch(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int mb, int sms, cudaStream_t st) {
+  auto go = [&](auto c) {
+    constexpr int MB = decltype(c)::value;
+    paged_attn_kernel<D, E4M3, MB><<<sms * ctas_per_sm(E4M3, MB), kThreads, Map<D, E4M3, MB>::kDyn, st>>>(k, v, p);
+  };
+  if (mb == 1)
+    go(std::integral_constant<int, 1>{});
+  else if (mb == 2)
+    go(std::integral_constant<int, 2>{});
+  else
+    go(std::integral_constant<int, 4>{});
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t paged_configure() {
+  cudaError_t e;
+  if ((e = configure<64, false, 1>()) != cudaSuccess) return e;
+  if ((e = configure<64, false, 2>()) != cudaSuccess) return e;
+  if ((e = configure<64, true, 1>()) != cudaSuccess) return e;
+  if ((e = configure<64, true, 2>()) != cudaSuccess) return e;
+  if ((e = configure<64, false, 4>()) != cudaSuccess) return e;
+  if ((e = configure<64, true, 4>()) != cudaSuccess) return e;
+  if ((e = configure<128, false, 4>()) != cudaSuccess) return e;
+  if ((e = configure<128, true, 4>()) != cudaSuccess) return e;
+  if ((e = configure<128, false, 1>()) != cudaSuccess) return e;
+  if ((e = configure<128, false, 2>()) != cudaSuccess) return e;
+  if ((e = configure<128, true, 1>()) != cudaSuccess) return e;
+  return configure<128, true, 2>();
+}
+
+cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int D, bool e4m3,
+                                   int row_blocks, int sms, cudaStream_t st) {
+  if (D == 64) return e4m3 ? launch<64, true>(k, v, p, row_blocks, sms, st) : launch<64, false>(k, v, p, row_blocks, sms, st);
+  return e4m3 ? launch<128, true>(k, v, p, row_blocks, sms, st) : launch<128, false>(k, v, p, row_blocks, sms, st);
+}
+
+}  // namespace ebd
