@@ -123,7 +123,7 @@ typedef struct {
   int32_t decode_mode; /* EBD_DECODE_*: EB decision or a baseline rule      */
   int32_t top_m;       /* EBD_DECODE_TOPM: commits per step (>= 1)          */
   int32_t paged;       /* 1: the handle also runs ebd_paged_attention, whose
-                          workspace it then holds (34 MB at 128-wide heads);
+                          workspace it then holds (40 MB at 128-wide heads);
                           0: it does not                                   */
 } ebd_config;
 
@@ -347,7 +347,7 @@ typedef struct {
   int64_t q_stride;           /* elements from row to row of q, and of k and v,  */
   int64_t kv_stride;          /* a multiple of 8 (slices of a fused projection's
                                  rows); 0: dense                                */
-  float scale;                /* factor of q . k; 0: 1 / sqrt(head_dim)          */
+  float scale;                /* factor of q . k, positive; 0: 1 / sqrt(head_dim) */
   int32_t causal;             /* 0: every row of a sequence sees all its cached
                                  positions; 1: row i of its n rows sees those
                                  before kv_len - n + i + 1                      */

@@ -255,7 +255,7 @@ struct ebd_handle {
   // ebd_paged_attention (cfg.paged): partial results of split tiles
   float* paged_part = nullptr;
   float* paged_part_ml = nullptr;
-  int* paged_tickets = nullptr;
+  PagedCut* paged_cuts = nullptr;
   // ebd_step_host: the attention's inputs on a copy engine (set up with the handle)
   int copy_route = -1;               // -1 not set up yet, 0 unavailable, 1 ready
   cudaStream_t s_copy = nullptr;
@@ -944,15 +944,16 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
       return bail(cuda_fail(h, e, "cudaMemset(tickets)"));
   }
   if (cfg->paged) {
-    if ((e = paged_configure()) != cudaSuccess) return bail(cuda_fail(h, e, "paged attention attributes"));
+    if ((e = paged_configure()) != cudaSuccess || (e = paged_tc_configure()) != cudaSuccess)
+      return bail(cuda_fail(h, e, "paged attention attributes"));
     const size_t ctas = static_cast<size_t>(h->num_sms) * kPagedCtasPerSm;
-    const size_t rows = ctas * 2 * kPagedRows;
+    const size_t narrow = ctas * 2 * kPagedRows, wide = static_cast<size_t>(h->num_sms) * 2 * kPagedTcRows;
+    const size_t rows = narrow > wide ? narrow : wide;
     if ((e = cudaMalloc(&h->paged_part, rows * (cfg->head_dim + 2) * sizeof(float))) != cudaSuccess)
       return bail(cuda_fail(h, e, "cudaMalloc(paged attention partials)"));
     h->paged_part_ml = h->paged_part + rows * cfg->head_dim;
-    if ((e = cudaMalloc(&h->paged_tickets, ctas * sizeof(int))) != cudaSuccess ||
-        (e = cudaMemset(h->paged_tickets, 0, ctas * sizeof(int))) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(paged attention tickets)"));
+    if ((e = cudaMalloc(&h->paged_cuts, ctas * sizeof(PagedCut))) != cudaSuccess)
+      return bail(cuda_fail(h, e, "cudaMalloc(paged attention)"));
   }
   if ((e = cudaMalloc(&h->d_status, sizeof(int))) != cudaSuccess)
     return bail(cuda_fail(h, e, "cudaMalloc(status)"));
@@ -1034,7 +1035,7 @@ void ebd_destroy(ebd_handle* h) {
   cudaFree(h->attn_part);
   cudaFree(h->tickets);
   cudaFree(h->paged_part);
-  cudaFree(h->paged_tickets);
+  cudaFree(h->paged_cuts);
   cudaFree(h->d_status);
   cudaFreeHost(h->h_status);
   cudaFree(h->staging);
@@ -1680,7 +1681,7 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
     return fail(h, EBD_ERR_INVALID_ARG, "q_stride must be 0, or a row or more and a multiple of 8");
   if (a->causal != 0 && a->causal != 1) return fail(h, EBD_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (a->max_new < 0) return fail(h, EBD_ERR_INVALID_ARG, "max_new must not be negative");
-  if (!(a->scale == a->scale) || std::isinf(a->scale)) return fail(h, EBD_ERR_INVALID_ARG, "scale is not finite");
+  if (!(a->scale >= 0.f) || std::isinf(a->scale)) return fail(h, EBD_ERR_INVALID_ARG, "scale must be finite and not negative");
   PagedParams p{};
   p.B = a->batch;
   p.R = a->rows;
@@ -1691,9 +1692,6 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   p.page_log2 = log2_of(c->page_size);
   p.n_pages = c->n_pages;
   p.max_pages = c->max_pages;
-  p.box_log2 = p.page_log2 < 6 ? p.page_log2 : 6;
-  p.above = 0;
-  p.upto = 0x7fffffff;
   const float scale = a->scale != 0.f ? a->scale : 1.f / std::sqrt(static_cast<float>(f.head_dim));
   p.scale_log2 = scale * 1.4426950408889634f;
   p.cu_rows = a->cu_rows;
@@ -1706,16 +1704,41 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   p.out = reinterpret_cast<__nv_bfloat16*>(a->out);
   p.part = h->paged_part;
   p.part_ml = h->paged_part_ml;
-  p.tickets = h->paged_tickets;
+  p.cuts = h->paged_cuts;
   p.status = h->d_status;
   p.limit_ns = kLimitNs;
-  const int longest = a->max_new > 0 && a->max_new < a->rows ? a->max_new : a->rows;
-  const int64_t m = static_cast<int64_t>(longest) * p.group;
-  CUtensorMap tk, tv;
+  // rows per tile: of the longest sequence, or, where that is unknown, of the mean one
+  const int64_t longest = a->max_new > 0 && a->max_new < a->rows ? a->max_new
+                          : a->max_new > 0                       ? a->rows
+                                                                 : (a->rows + a->batch - 1) / a->batch;
+  const int64_t m = longest * p.group;
+  const bool e4m3 = c->dtype == EBD_KV_E4M3;
+  const bool wide = f.head_dim == 128 && p.group <= kPagedTcGroup && m > 64;
+  p.box_log2 = wide ? (p.page_log2 < 7 ? p.page_log2 : 7) : p.page_log2 < 6 ? p.page_log2 : 6;
+  p.part_rows = wide ? kPagedTcRows : kPagedRows;
+  // tiles stay whole where none can have many chunks (64 keys, or 128 in the tcgen05 kernel)
+  p.uncut = static_cast<int64_t>(c->max_pages) * c->page_size <= kPagedUncutKeys ? 1 : 0;
+  CUtensorMap tq, tk, tv;
   if (!encode_pool(&tk, c->k, h, c, 1 << p.box_log2) || !encode_pool(&tv, c->v, h, c, 1 << p.box_log2))
     return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (pages) failed");
-  cudaError_t e = launch_paged_attention(tk, tv, p, f.head_dim, c->dtype == EBD_KV_E4M3, m <= 16 ? 1 : m <= 32 ? 2 : 4,
-                                         h->num_sms, static_cast<cudaStream_t>(stream));
+  cudaError_t e;
+  const int mb = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+  if (wide) {
+    // q as (element, head, row), in boxes of the group's heads of as many rows as a tile of 128 holds
+    const uint64_t dims[3] = {static_cast<uint64_t>(f.head_dim), static_cast<uint64_t>(f.n_heads_q),
+                              static_cast<uint64_t>(a->rows)};
+    const uint64_t str[2] = {static_cast<uint64_t>(f.head_dim) * 2, static_cast<uint64_t>(stride) * 2};
+    const int tokens = 128 / p.group;
+    const uint32_t box[3] = {64, static_cast<uint32_t>(p.group), static_cast<uint32_t>(tokens)};
+    if (!encode_bf16(&tq, a->q, 3, dims, str, box))
+      return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (q) failed");
+    e = launch_paged_tc(tq, tk, tv, p, e4m3, m <= tokens * p.group, h->num_sms, static_cast<cudaStream_t>(stream));
+  } else {
+    e = launch_paged_attention(tk, tv, p, f.head_dim, e4m3, mb, h->num_sms, static_cast<cudaStream_t>(stream));
+  }
+  if (e == cudaSuccess && !p.uncut)
+    e = launch_paged_join(p, f.head_dim, wide ? h->num_sms : paged_attention_ctas(e4m3, mb, h->num_sms),
+                          static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "paged attention launch");
   return EBD_OK;
 }

@@ -157,7 +157,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
   auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
   volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc);
-  int* s_flag = reinterpret_cast<int*>(smem + L::kMisc + 4);
   int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 8);
   int* bad = reinterpret_cast<int*>(smem + L::kBad);
 
@@ -177,6 +176,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   }
   for (int i = tid; i < 3 * D; i += kThreads) bad[i] = kNever;
   paged_plan<kThreads>(p, T, kCH, kLeast, plan, scan);
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == kThreads - 1) paged_cut(p, *plan, T, kCH);
   PagedWalk w;
   if (!w.begin(p, *plan, T, kCH)) return;
 
@@ -708,9 +709,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     named_barrier(1, 128);
     const bool whole = w.whole();
     const bool any_bad = *reinterpret_cast<volatile int*>(s_bad) != 0;
-    const int own_slot = 2 * static_cast<int>(blockIdx.x) + (w.c0 == 0 ? 1 : 0);
-    float* part = p.part + static_cast<long long>(own_slot) * kPagedRows * D;
-    float* part_ml = p.part_ml + static_cast<long long>(own_slot) * kPagedRows * 2;
+    float* part = p.part + static_cast<long long>(w.part()) * p.part_rows * D;
+    float* part_ml = p.part_ml + static_cast<long long>(w.part()) * p.part_rows * 2;
     if (!*abort) {
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
@@ -770,48 +770,63 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       if (tid == 0) *s_bad = 0;
       named_barrier(1, 128);
     }
-    if (!whole) {
-      // ---- the last CTA of a split tile puts its parts together, in order
-      __threadfence();
-      named_barrier(1, 128);
-      const long long ua = w.u - w.c0;  // the tile's first chunk
-      const int first = paged_owner(*plan, ua);
-      const int np = paged_owner(*plan, ua + w.nch - 1) - first + 1;
-      if (tid == 0) *s_flag = atomicAdd(&p.tickets[first], 1) == np - 1;
-      named_barrier(1, 128);
-      if (*s_flag) {
-        __threadfence();
-        if (tid == 0) p.tickets[first] = 0;
-        auto at = [&](int k) { return k == 0 ? 2 * first + 1 : 2 * (first + k); };
-        constexpr int D4 = D / 4;
-        for (int it = tid; it < rows * D4; it += 128) {
-          const int r = it / D4, d = (it - r * D4) * 4;
-          float mx = -INFINITY;
-          for (int k = 0; k < np; ++k) mx = fmaxf(mx, __ldcg(p.part_ml + (static_cast<long long>(at(k)) * kPagedRows + r) * 2));
-          float l = 0.f;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int k = 0; k < np; ++k) {
-            const long long row = static_cast<long long>(at(k)) * kPagedRows + r;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + row * 2));
-            const float4 z = __ldcg(reinterpret_cast<const float4*>(p.part + row * D + d));
-            const float wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);
-            l = fmaf(wgt, ml.y, l);
-            if (ml.x == -INFINITY) continue;  // a part that the row sees nothing of
-            acc.x = fmaf(wgt, z.x, acc.x);
-            acc.y = fmaf(wgt, z.y, acc.y);
-            acc.z = fmaf(wgt, z.z, acc.z);
-            acc.w = fmaf(wgt, z.w, acc.w);
-          }
-          const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-          const int m = m0 + r, i = m / p.group, hl = m - i * p.group;
-          *reinterpret_cast<uint2*>(p.out + (static_cast<long long>(w.s.r0 + i) * p.Hq + w.h * p.group + hl) * D + d) =
-              make_uint2(bf16x2(acc.x * inv, acc.y * inv), bf16x2(acc.z * inv, acc.w * inv));
+  } while (w.next(p));
+}
+
+// The parts of the tile that CTA blockIdx.x of the attention begins: a warp per
+// row, a lane per D / 32 columns, so that a part's row is one load.
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
+  constexpr int V = D / 32;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the attention's results
+  const PagedCut cut = p.cuts[blockIdx.x];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto part = [&](int k) {
+    const int c = static_cast<int>(blockIdx.x);
+    return static_cast<long long>(k == 0 ? 2 * c + 1 : 2 * (c + k)) * p.part_rows;
+  };
+  if (cut.parts == 0) return;
+  for (int r = blockIdx.y * 8 + warp; r < cut.rows; r += 8 * gridDim.y) {
+    float mx = -INFINITY;
+    for (int k = lane; k < cut.parts; k += 32) mx = fmaxf(mx, p.part_ml[(part(k) + r) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    float l = 0.f, acc[V] = {};
+    for (int k0 = 0; k0 < cut.parts; k0 += 32) {
+      float wgt = 0.f;
+      if (k0 + lane < cut.parts) {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (part(k0 + lane) + r) * 2);
+        wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);  // 0: a part that the row sees nothing of
+        l = fmaf(wgt, ml.y, l);
+      }
+      const int n = min(32, cut.parts - k0);
+#pragma unroll 8
+      for (int k = 0; k < n; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, wgt, k);
+        const float* z = p.part + (part(k0 + k) + r) * D + lane * V;
+        if constexpr (V == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(z);
+          acc[0] = fmaf(wk, x.x, acc[0]);
+          acc[1] = fmaf(wk, x.y, acc[1]);
+          acc[2] = fmaf(wk, x.z, acc[2]);
+          acc[3] = fmaf(wk, x.w, acc[3]);
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(z);
+          acc[0] = fmaf(wk, x.x, acc[0]);
+          acc[1] = fmaf(wk, x.y, acc[1]);
         }
       }
-      named_barrier(1, 128);  // s_flag is free again
     }
-  } while (w.next(p));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+    const int m = cut.m0 + r, i = m / p.group, h = m - i * p.group;
+    __nv_bfloat16* od = p.out + (static_cast<long long>(cut.r0 + i) * p.Hq + cut.h * p.group + h) * D + lane * V;
+    if constexpr (V == 4)
+      *reinterpret_cast<uint2*>(od) = make_uint2(bf16x2(acc[0] * inv, acc[1] * inv), bf16x2(acc[2] * inv, acc[3] * inv));
+    else
+      *reinterpret_cast<uint32_t*>(od) = bf16x2(acc[0] * inv, acc[1] * inv);
+  }
 }
 
 template <int D, bool E4M3, int MB>
@@ -850,6 +865,23 @@ cudaError_t paged_configure() {
   if ((e = configure<128, false, 2>()) != cudaSuccess) return e;
   if ((e = configure<128, true, 1>()) != cudaSuccess) return e;
   return configure<128, true, 2>();
+}
+
+cudaError_t launch_paged_join(const PagedParams& p, int D, int ctas, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas, p.part_rows / 32, 1);
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return D == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64>, p) : cudaLaunchKernelEx(&cfg, paged_join_kernel<128>, p);
+}
+
+int paged_attention_ctas(bool e4m3, int row_blocks, int sms) {
+  return sms * ctas_per_sm(e4m3, row_blocks);
 }
 
 cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int D, bool e4m3,

@@ -1,0 +1,900 @@
+// Attention over the paged K/V cache with many query rows per K/V head (chunks
+// of a prompt, windows of grouped heads) on the 5th-generation tensor cores.
+// The mathematics, the 8-bit cache's exact forms of q and V, and the treatment
+// of values that are not finite are those of k_paged_attn.cu.
+//
+// A work item is two tiles of up to 128 packed rows of one sequence and K/V
+// head; each CTA, one per SM, takes an equal share of all items' steps of 128
+// keys (paged.h).  The two tiles run as two streams, S = Q K^T and O += P V of
+// one on the tensor cores while the other's softmax runs.  Where a launch's
+// sequences have no more rows than one tile, the streams are the same rows over
+// alternate steps, put together in the end.
+//   TMEM: S of stream 0 and 1 (128 columns each), O of stream 0 and 1 (D
+//     each).  P, in bf16, overwrites the S that it came from and is the A
+//     operand of P V from there.
+//   warps 0-3, 4-7: softmax of stream 0, 1, a thread per row;
+//   warps 8-11: 8-bit caches: V's codes become bf16, times their row's scale,
+//     and K's exponent bytes become factors; bf16 ones: only the steps that
+//     end in keys which rows do not see;
+//   warp 12: loads of q and K; warp 14: loads of V; warp 13: the MMAs.
+// 8-bit K and the two 4-bit terms of q multiply as they are (kind::f8f6f4, at
+// twice the rate of bf16: the two terms cost what bf16 would).
+#include <cuda_fp16.h>
+#include <type_traits>
+
+#include "paged.h"
+#include "ptx.cuh"
+
+namespace ebd {
+
+namespace {
+
+constexpr int kStep = 128;     // keys of a step
+constexpr int kThreads = 512;
+constexpr int kLeast = 4;      // steps of a share, at least
+constexpr int kNever = 0x7fffffff;
+constexpr uint32_t kTmemCols = 512;
+// Notes of values that are not finite, per item in turn.  The warps that take
+// them are at most three items ahead of a softmax that reads them: an item is
+// begun when every softmax warp has left the steps of the one before, and V is
+// loaded two steps ahead, which may be two items.
+constexpr int kBads = 4;
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2(float x, float y) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_value(uint32_t c) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(c)));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e > 0 ? e << 23 : 1u << 22); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// two 32-bit floats at a time
+__device__ __forceinline__ void fma2(float& x, float& y, float f, float a) {
+  asm("{\n .reg .b64 v, m, c;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %2};\n mov.b64 c, {%3, %3};\n"
+      " fma.rn.f32x2 v, v, m, c;\n mov.b64 {%0, %1}, v;\n}"
+      : "+f"(x), "+f"(y)
+      : "f"(f), "f"(a));
+}
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {
+  asm("{\n .reg .b64 v, m;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %3};\n mul.rn.f32x2 v, v, m;\n"
+      " mov.b64 {%0, %1}, v;\n}"
+      : "+f"(x), "+f"(y)
+      : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+  asm("{\n .reg .b64 v, m;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %3};\n add.rn.f32x2 v, v, m;\n"
+      " mov.b64 {%0, %1}, v;\n}"
+      : "+f"(x), "+f"(y)
+      : "f"(a), "f"(b));
+}
+
+// 32 lanes x 32 columns, without the wait
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,"
+      "%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// Completes the loads above; the values pass through it, so that no use of
+// them can be moved ahead.
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,"
+      "%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+      "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// MMAs with descriptors as low words and a shared high word: bf16 or e4m3 A
+// and B from shared memory, and bf16 A from TMEM.
+__device__ __forceinline__ void umma_e4m3_lo(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc,
+                                             uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 ad, bd;\n setp.ne.b32 p, %5, 0;\n"
+      " mov.b64 ad, {%1, %3};\n mov.b64 bd, {%2, %3};\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t hi, uint32_t idesc,
+                                             uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 bd;\n setp.ne.b32 p, %5, 0;\n mov.b64 bd, {%2, %3};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], bd, %4, p;\n}\n" ::"r"(d),
+      "r"(a_tmem), "r"(b_lo), "r"(hi), "r"(idesc), "r"(acc));
+}
+__device__ __forceinline__ uint32_t swz(int r, int c) {
+  return static_cast<uint32_t>(r * 128 + ((c ^ (r & 7)) << 4));
+}
+template <int N>
+__device__ __forceinline__ void regs_inc() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_dec() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+// 512 threads start with 128 registers each; the softmax's 256 take 176 and
+// the others 80: 256 * 176 + 256 * 80 = 512 * 128.
+constexpr int kSoftmaxRegs = 176, kOtherRegs = 80;
+
+template <int D, bool E4M3>
+struct Map {
+  static constexpr int NB = D / 64;
+  static constexpr uint32_t kTile = 128 * D * 2;             // q of a stream: bf16, or its two terms
+  static constexpr uint32_t kK = kStep * D * (E4M3 ? 1 : 2);  // a step's K
+  static constexpr uint32_t kV = kStep * D * 2;               // a step's V in bf16
+  static constexpr int kKs = E4M3 ? 3 : 2, kVs = 2;           // ring slots
+  // K's factors: the softmax has read those of a step when its P V is done, and
+  // the warps that write them for step g have waited for P V of step g - 4
+  static constexpr int kFs = 4;
+  static constexpr uint32_t kQ = 0;
+  static constexpr uint32_t kK0 = kQ + 2 * kTile;
+  static constexpr uint32_t kV0 = kK0 + kKs * kK;
+  static constexpr uint32_t kRaw = kV0 + kVs * kV;            // 8-bit V as loaded
+  static constexpr uint32_t kKe = kRaw + (E4M3 ? kVs * kStep * D : 0);  // exponent bytes
+  static constexpr uint32_t kVe = kKe + kKs * kStep;
+  static constexpr uint32_t kKf = kVe + kVs * kStep;          // [kFs][kStep] K's factors
+  static constexpr uint32_t kRowF = kKf + (E4M3 ? kFs * kStep * 4 : 0);  // [2][128]
+  static constexpr uint32_t kMl = kRowF + 2 * 128 * 4;        // [128][2] stream 1's (maximum, sum)
+  static constexpr uint32_t kBad = kMl + 128 * 8;             // [kBads][3][D]
+  static constexpr uint32_t kBar = kBad + kBads * 3 * D * 4;
+  // k full, empty, factors; v full, empty, raw full, raw empty; s, p, o full
+  // and o free of 2 streams; q full, ready, empty; drain
+  static constexpr int kNBar = 2 * kKs + kFs + 4 * kVs + 8 + 4;
+  static constexpr uint32_t kPlan = kBar + kNBar * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32 + 1) * 8;
+  static constexpr uint32_t kBytes = kMisc + 32;
+  static constexpr uint32_t kDyn = kBytes + 1024;
+  static_assert(kDyn <= 227 * 1024 && 2 * kTile >= 128 * 64 * 4 + kTile, "shared memory");
+};
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(kThreads, 1)
+    paged_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                    const __grid_constant__ CUtensorMap tm_v, const PagedParams p, const int one) {
+  using L = Map<D, E4M3>;
+  constexpr int NB = L::NB;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBar);
+  uint64_t* kfull = bars;
+  uint64_t* kempty = kfull + L::kKs;
+  uint64_t* kfact = kempty + L::kKs;
+  uint64_t* vfull = kfact + L::kFs;    // V in bf16 (8-bit caches: converted)
+  uint64_t* vempty = vfull + L::kVs;
+  uint64_t* rfull = vempty + L::kVs;   // 8-bit V as loaded; bf16: V's last rows seen to
+  uint64_t* rempty = rfull + L::kVs;
+  uint64_t* s_full = rempty + L::kVs;  // [2] by stream
+  uint64_t* p_full = s_full + 2;
+  uint64_t* o_full = p_full + 2;
+  uint64_t* o_free = o_full + 2;
+  uint64_t* q_full = o_free + 2;
+  uint64_t* q_ready = q_full + 1;
+  uint64_t* q_empty = q_ready + 1;
+  uint64_t* drain = q_empty + 1;
+  PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
+  auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMisc);
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc + 4);
+  int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 16);  // [kBads] by item
+  int* bad = reinterpret_cast<int*>(smem + L::kBad);
+  float* rowf = reinterpret_cast<float*>(smem + L::kRowF);
+
+  // rows of a tile: whole tokens, so that its q is a box of (64 columns, heads
+  // of the group, tokens)
+  const int tile = 128 / p.group * p.group;
+  const int T = one ? tile : 2 * tile;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int s = 0; s < L::kKs; ++s) {
+      mbar_init(&kfull[s], 1);
+      mbar_init(&kempty[s], E4M3 ? 5 : 1);  // the MMAs, and the warps that read its exponents
+    }
+    for (int s = 0; s < L::kFs; ++s) mbar_init(&kfact[s], 4);
+    for (int s = 0; s < L::kVs; ++s) {
+      mbar_init(&vfull[s], E4M3 ? 4 : 1);
+      mbar_init(&vempty[s], E4M3 ? 1 : 5);  // the MMAs, and the warps that see to its last rows
+      mbar_init(&rfull[s], E4M3 ? 1 : 4);
+      mbar_init(&rempty[s], 4);
+    }
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(&s_full[x], 1);
+      mbar_init(&p_full[x], 4);
+      mbar_init(&o_full[x], 1);
+      mbar_init(&o_free[x], 4);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_ready, 8);
+    mbar_init(q_empty, 9);  // the MMAs, and the softmax warps
+    mbar_init(drain, 1);
+    *abort = 0;
+    for (int i = 0; i < kBads; ++i) s_bad[i] = 0;
+    fence_mbar_init();
+  }
+  for (int i = tid; i < kBads * 3 * D; i += kThreads) bad[i] = kNever;
+  if (warp == 13) tmem_alloc(tmem_holder, kTmemCols);
+  tc_fence_before();
+  paged_plan<kThreads>(p, T, kStep, kLeast, plan, scan);  // ends in a barrier of all threads
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == kThreads - 1) paged_cut(p, *plan, T, kStep);  // of a warp without other work
+  PagedWalk w;
+  const bool work = w.begin(p, *plan, T, kStep);
+  auto gave_up = [&]() {
+    if (!*abort) {
+      *abort = 1;
+      atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
+    }
+  };
+  // steps of stream x of a piece of n: all of them, or every other one
+  auto rows_here = [&]() { return min(T, w.s.n * p.group - w.t * T); };
+  auto steps_of = [&](int x, int n) { return one ? (n + 1 - x) / 2 : (x == 0 || rows_here() > tile ? n : 0); };
+  // the first and the last of the item's limits
+  auto lim_first = [&]() { return paged_limit(p, w.s, w.t * T / p.group); };
+  auto lim_last = [&]() { return paged_limit(p, w.s, (w.t * T + rows_here() - 1) / p.group); };
+
+  if (warp >= 12) {
+    regs_dec<kOtherRegs>();
+    if (work && (warp == 12 || warp == 14)) {
+      // ---------------------------------------------------------- loads
+      const bool is_k = warp == 12;
+      const int slots = is_k ? L::kKs : L::kVs;
+      uint64_t* fullb = is_k ? kfull : (E4M3 ? rfull : vfull);
+      uint64_t* emptyb = is_k ? kempty : (E4M3 ? rempty : vempty);
+      uint8_t* ring = smem + (is_k ? L::kK0 : (E4M3 ? L::kRaw : L::kV0));
+      uint8_t* ering = smem + (is_k ? L::kKe : L::kVe);
+      const uint32_t op = E4M3 ? kStep * D : L::kV;
+      const CUtensorMap* tm = is_k ? &tm_k : &tm_v;
+      const uint8_t* scales = is_k ? p.k_scale : p.v_scale;
+      const int np_log = 7 - p.box_log2, box = 1 << p.box_log2;
+      const int pc = lane & ((1 << np_log) - 1), part = lane >> np_log;
+      const int key_in = pc << p.box_log2;
+      int n = 0, items = 0;
+      bool ok = true;
+      do {
+        if (is_k) {  // q
+          ok = items == 0 || mbar_wait(q_empty, static_cast<uint32_t>(items - 1) & 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          const int tiles = !one && rows_here() > tile ? 2 : 1;
+          if (lane == 0) mbar_arrive_expect_tx(q_full, static_cast<uint32_t>(tiles) * tile * D * 2);
+          __syncwarp();
+          if (lane < tiles * NB) {
+            const int x = lane / NB, hf = lane % NB;
+            tma_load_3d(smem + L::kQ + x * L::kTile + hf * 16384, &tm_q, q_full, hf * 64, w.h * p.group,
+                        w.s.r0 + (w.t * T + x * tile) / p.group);
+          }
+          ++items;
+        }
+        const int lim = lim_last();
+        const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
+        int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
+        for (int c = w.c0; c < w.c1; ++c, ++n) {
+          const int key = c * kStep + key_in;
+          const int first = (c * kStep) >> p.page_log2;
+          if (first >= win0 + 32 || first < win0) {
+            win0 = first & ~31;
+            win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
+          }
+          int page = __shfl_sync(0xffffffffu, win, ((key >> p.page_log2) - win0) & 31);
+          const bool mine = part < (E4M3 ? 2 : NB) && key < lim;
+          if (mine && (page < 0 || page >= p.n_pages)) {
+            atomicCAS(p.status, 0, EBD_ERR_BOUNDS);
+            page = 0;
+          }
+          const int pieces = min(max((lim - c * kStep + box - 1) >> p.box_log2, 0), 1 << np_log);
+          const int s = n % slots;
+          ok = n < slots || mbar_wait(&emptyb[s], static_cast<uint32_t>(n / slots - 1) & 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0)
+            mbar_arrive_expect_tx(&fullb[s], static_cast<uint32_t>(pieces) * box * (E4M3 ? D + 1 : 2 * D));
+          __syncwarp();
+          if (mine) {
+            const int off = key & ((1 << p.page_log2) - 1);
+            if (E4M3 && part == 1)
+              bulk_load(ering + s * kStep + key_in,
+                        scales + ((static_cast<long long>(page) * p.Hkv + w.h) << p.page_log2) + off, box, &fullb[s]);
+            else
+              tma_load_4d(ring + s * op + part * 16384 + key_in * 128, tm, &fullb[s], part * 64, off, w.h, page);
+          }
+        }
+      } while (ok && w.next(p));
+      if (!ok) {
+        if (lane == 0) gave_up();
+        // the copies in flight land before the CTA can exit
+        for (int j = max(0, n - slots); j < n; ++j)
+          mbar_wait(&fullb[j % slots], static_cast<uint32_t>(j / slots) & 1u, p.limit_ns, nullptr);
+        if (is_k && items > 0) mbar_wait(q_full, static_cast<uint32_t>(items - 1) & 1u, p.limit_ns, nullptr);
+      }
+    } else if (work && warp == 13) {
+      // ---------------------------------------------------------- MMAs
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint32_t idesc_s = E4M3 ? (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24) : umma_idesc_bf16(128, 128);
+      const uint32_t idesc_o = umma_idesc_bf16(128, D) | (1u << 16);  // B (V) MN-major
+      const uint32_t hi = static_cast<uint32_t>(umma_desc_sw128(0) >> 32);
+      const uint32_t q_lo = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + L::kQ)));
+      const uint32_t k_lo0 = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + L::kK0)));
+      // V: 64-column blocks 16384 bytes apart (leading byte offset)
+      const uint32_t v_lo0 = ((smem_u32(smem + L::kV0) >> 4) & 0x3FFFu) | ((16384u >> 4) << 16);
+      int kn = 0, vn = 0, en = 0, items = 0;  // K and V steps, V steps seen to, before this item
+      int done[2] = {0, 0};           // steps of each stream before this item
+      int outs[2] = {0, 0};           // items that each stream had steps of
+      bool ok = true;
+      do {
+        const int n = w.c1 - w.c0;
+        const int ns[2] = {steps_of(0, n), steps_of(1, n)};
+        const int edge0 = E4M3 ? n : max(0, min(n, lim_first() / kStep - w.c0));  // V steps from here are seen to
+        ok = __all_sync(0xffffffffu, mbar_wait(E4M3 ? q_ready : q_full, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort));
+        tc_fence_after();
+        const int last = one ? (ns[0] > ns[1] ? 0 : 1) : (ns[1] > 0 ? 1 : 0);  // stream of the item's last S
+        for (int i = 0; i <= ns[0] && ok; ++i) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (i > 0 && i - 1 < ns[x]) {  // O += P V
+              const int st = one ? 2 * (i - 1) + x : i - 1;
+              const int s = (vn + st) % L::kVs;
+              const uint32_t ph = static_cast<uint32_t>((vn + st) / L::kVs) & 1u;
+              bool g = mbar_wait(&p_full[x], static_cast<uint32_t>(done[x] + i - 1) & 1u, p.limit_ns, abort) &&
+                       mbar_wait(&vfull[s], ph, p.limit_ns, abort);
+              if (!E4M3 && st >= edge0) {
+                const int e = en + st - edge0;
+                g = g && mbar_wait(&rfull[e & 1], static_cast<uint32_t>(e >> 1) & 1u, p.limit_ns, abort);
+              }
+              if (i == 1 && outs[x] > 0)
+                g = g && mbar_wait(&o_free[x], static_cast<uint32_t>(outs[x] - 1) & 1u, p.limit_ns, abort);
+              ok = __all_sync(0xffffffffu, g);
+              if (!ok) break;
+              tc_fence_after();
+              const uint32_t v_lo = v_lo0 + static_cast<uint32_t>(s) * (L::kV >> 4);
+              const uint32_t d = tm + 256u + static_cast<uint32_t>(x * D);
+              const uint32_t a = tm + static_cast<uint32_t>(x * 128);
+              if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kStep / 16; ++kk)
+                  umma_bf16_ts(d, a + static_cast<uint32_t>(kk * 8), v_lo + static_cast<uint32_t>(kk * (2048 >> 4)), hi,
+                               idesc_o, kk != 0 || i > 1 ? 1u : 0u);
+                if (one || x == 1 || ns[1] == 0) umma_commit(&vempty[s]);
+                if (i == ns[x]) umma_commit(&o_full[x]);
+              }
+              __syncwarp();
+            }
+            if (i < ns[x]) {  // S = Q K^T
+              const int st = one ? 2 * i + x : i;
+              const int s = (kn + st) % L::kKs;
+              ok = __all_sync(0xffffffffu, mbar_wait(&kfull[s], static_cast<uint32_t>((kn + st) / L::kKs) & 1u,
+                                                     p.limit_ns, abort));
+              if (!ok) break;
+              tc_fence_after();
+              const uint32_t ql = q_lo + (one ? 0u : static_cast<uint32_t>(x) * (L::kTile >> 4));
+              const uint32_t kl = k_lo0 + static_cast<uint32_t>(s) * (L::kK >> 4);
+              const uint32_t d = tm + static_cast<uint32_t>(x * 128);
+              if (elect_one()) {
+                if constexpr (E4M3) {
+#pragma unroll
+                  for (int term = 0; term < 2; ++term)
+#pragma unroll
+                    for (int kk = 0; kk < D / 32; ++kk)
+                      umma_e4m3_lo(d, ql + static_cast<uint32_t>(term * (16384 >> 4) + kk * 2),
+                                   kl + static_cast<uint32_t>(kk * 2), hi, idesc_s, term + kk > 0 ? 1u : 0u);
+                } else {
+#pragma unroll
+                  for (int kk = 0; kk < D / 16; ++kk)
+                    umma_bf16_lo(d, ql + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                                 kl + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), hi, idesc_s,
+                                 kk > 0 ? 1u : 0u);
+                }
+                umma_commit(&s_full[x]);
+                if (one || x == 1 || ns[1] == 0) umma_commit(&kempty[s]);
+                if (x == last && i == ns[x] - 1) umma_commit(q_empty);
+              }
+              __syncwarp();
+            }
+          }
+        }
+        kn += n;
+        vn += n;
+        en += n - edge0;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          done[x] += ns[x];
+          outs[x] += ns[x] > 0 ? 1 : 0;
+        }
+        ++items;
+      } while (ok && w.next(p));
+      if (!ok) {
+        if (lane == 0) gave_up();
+        if (elect_one()) umma_commit(drain);  // completes once every MMA issued so far is done
+        __syncwarp();
+        mbar_wait(drain, 0, p.limit_ns, nullptr);
+      }
+    }
+  } else if (warp >= 8) {
+    // ------------------------------------------------------------ V's codes, K's factors, last rows
+    regs_dec<kOtherRegs>();
+    const int r = tid - 256;  // key of a step
+    int kn = 0, vn = 0, en = 0, items = 0;
+    bool ok = work;
+    if (work) do {
+      const int n = w.c1 - w.c0;
+      const int lo = lim_first(), hi = lim_last();
+      int* badp = bad + (items % kBads) * 3 * D;
+      if (*reinterpret_cast<volatile int*>(&s_bad[items % kBads]) != 0) {  // of an item long done
+        named_barrier(2, 128);
+        for (int i = r; i < 3 * D; i += 128) badp[i] = kNever;
+        if (r == 0) *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) = 0;
+        named_barrier(2, 128);
+      }
+      // rows from `hi` on nobody sees; of those from `lo` on, hidden from some
+      // rows, what is not finite is kept out and noted for the rows that see it
+      auto note = [&](int key, int d, int kind) {
+        atomicMin(&badp[kind * D + d], key);
+        *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) = 1;
+      };
+      if constexpr (E4M3) {
+        auto factors = [&](int j) {
+          const int s = (kn + j) % L::kKs;
+          ok = ok && mbar_wait(&kfull[s], static_cast<uint32_t>((kn + j) / L::kKs) & 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+          const int fs = (kn + j) % L::kFs;
+          reinterpret_cast<float*>(smem + L::kKf)[fs * kStep + r] = scale_value((smem + L::kKe)[s * kStep + r]);
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&kfact[fs]);
+            mbar_arrive(&kempty[s]);
+          }
+        };
+        factors(0);
+        for (int j = 0; j < n; ++j) {
+          if (j + 1 < n) factors(j + 1);
+          const int s = (vn + j) % L::kVs;
+          const uint32_t ph = static_cast<uint32_t>((vn + j) / L::kVs) & 1u;
+          ok = ok && mbar_wait(&rfull[s], ph, p.limit_ns, abort);
+          if (vn + j >= L::kVs) ok = ok && mbar_wait(&vempty[s], ph ^ 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+          const int key = (w.c0 + j) * kStep + r;
+          const uint32_t e = (smem + L::kVe)[s * kStep + r];
+          // 2^(120 + k): codes moved into place are 2^-120 times their value
+          uint32_t m = (min(e, 134u) + 120u) << 7;
+          uint32_t m2 = e > 134u ? (e - 7u) << 7 : 0x3F80u;  // past that, the rest of the scale: 2^(e - 134)
+          if (e == 255u) m = m2 = 0x7FC0u;
+          if (key >= hi) {
+            m = 0u;
+            m2 = 0x3F80u;
+          } else if (e == 255u && key >= lo) {
+            for (int d = 0; d < D; ++d) note(key, d, 0);
+            m = 0u;
+            m2 = 0x3F80u;
+          }
+          m |= m << 16;
+          m2 |= m2 << 16;
+          const bool two = __any_sync(0xffffffffu, m2 != 0x3F803F80u);
+          const uint8_t* src = smem + L::kRaw + s * kStep * D;
+          uint8_t* dst = smem + L::kV0 + s * L::kV;
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint4 x4 = *reinterpret_cast<const uint4*>(src + swz(r, c));
+            const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+            uint32_t y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              // bytes d0, d1, d2, d3 -> (d0, d1), (d2, d3)
+              const uint32_t a = __byte_perm(x[i], 0u, 0x1404), b = __byte_perm(x[i], 0u, 0x3424);
+              y[2 * i] = mul_bf16x2((a & 0x80008000u) | ((a >> 4) & 0x07F007F0u), m);
+              y[2 * i + 1] = mul_bf16x2((b & 0x80008000u) | ((b >> 4) & 0x07F007F0u), m);
+            }
+            if (two) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) y[i] = mul_bf16x2(y[i], m2);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int ch = 2 * c + i;  // 16 bytes of bf16 columns
+              *reinterpret_cast<uint4*>(dst + (ch >> 3) * 16384 + swz(r, ch & 7)) =
+                  make_uint4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+            }
+          }
+          fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&vfull[s]);
+            mbar_arrive(&rempty[s]);
+          }
+        }
+      } else {
+        // bf16: only the steps that hold keys past `lo`
+        const int edge0 = max(0, min(n, lo / kStep - w.c0));
+        for (int j = 0; j < n; ++j) {
+          const int s = (vn + j) % L::kVs;
+          ok = ok && mbar_wait(&vfull[s], static_cast<uint32_t>((vn + j) / L::kVs) & 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+          const int key = (w.c0 + j) * kStep + r;
+          uint8_t* v = smem + L::kV0 + s * L::kV;
+          if (ok && j >= edge0 && key >= lo) {
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+              uint4* q = reinterpret_cast<uint4*>(v + (c >> 3) * 16384 + swz(r, c & 7));
+              if (key >= hi) {
+                *q = make_uint4(0u, 0u, 0u, 0u);
+                continue;
+              }
+              const uint4 x4 = *q;
+              uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+              bool any = false;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t b = (x[i] >> (16 * h)) & 0xFFFFu;
+                  if ((b & 0x7F80u) == 0x7F80u) {
+                    note(key, c * 8 + 2 * i + h, (b & 0x7Fu) ? 0 : (b & 0x8000u) ? 2 : 1);
+                    x[i] &= h ? 0x0000FFFFu : 0xFFFF0000u;
+                    any = true;
+                  }
+                }
+              if (any) *q = make_uint4(x[0], x[1], x[2], x[3]);
+            }
+          }
+          if (j >= edge0) fence_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (j >= edge0) mbar_arrive(&rfull[(en + j - edge0) & 1]);
+            mbar_arrive(&vempty[s]);
+          }
+        }
+        en += n - edge0;
+      }
+      kn += n;
+      vn += n;
+      ++items;
+    } while (w.next(p));
+    if (!ok && work && lane == 0) gave_up();
+  } else {
+    // ------------------------------------------------------------ softmax: stream x, a thread per row
+    regs_inc<kSoftmaxRegs>();
+    const int x = warp >> 2, row = tid & 127;
+    const uint32_t quad = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + quad + static_cast<uint32_t>(x * 128);
+    const uint32_t to = tmem + quad + 256u + static_cast<uint32_t>(x * D);
+    int kn = 0, items = 0, done = 0, outs = 0;
+    bool ok = work;
+    if (work) do {
+      const int n = w.c1 - w.c0;
+      const int mine = steps_of(x, n);
+      const int rows = rows_here();
+      const int m_row = w.t * T + (one ? 0 : x * tile) + row;  // packed row
+      const bool valid = row < tile && (one ? 0 : x * tile) + row < rows;
+      const int lim = valid ? paged_limit(p, w.s, m_row / p.group) : kNever;
+      const int lo = lim_first();
+      float f = p.scale_log2;
+      // also where nothing of q is needed here: a stream without steps must not
+      // give q back (below) before the item has it
+      ok = ok && mbar_wait(q_full, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if constexpr (E4M3) {
+        // q as two e4m3 terms, in place: the row's 128 bytes of columns 0..63
+        // become its high terms, those of 64..127 its low ones
+        if (x == 0 || (!one && mine > 0)) {
+          uint8_t* q = smem + L::kQ + x * L::kTile;
+          uint4 v[D / 8];
+          uint32_t amax = 0;
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            v[c] = *reinterpret_cast<const uint4*>(q + (c >> 3) * 16384 + swz(row, c & 7));
+            const uint32_t u[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) amax = max(amax, max(u[k] & 0x7FFFu, (u[k] >> 16) & 0x7FFFu));
+          }
+          const bool finite = amax < 0x7F80u;
+          const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 127;
+          const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t h[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint4 vv = v[2 * c + (i >> 1)];
+              const uint32_t u0 = i & 1 ? vv.z : vv.x, u1 = i & 1 ? vv.w : vv.y;
+              const float a = __uint_as_float(u0 << 16) * inv, b = __uint_as_float(u0 & 0xFFFF0000u) * inv;
+              const float cc = __uint_as_float(u1 << 16) * inv, d = __uint_as_float(u1 & 0xFFFF0000u) * inv;
+              const uint32_t h0 = e4m3x2(a, b), h1 = e4m3x2(cc, d);
+              const float2 f0 = e4m3x2_value(h0), f1 = e4m3x2_value(h1);
+              h[i] = finite ? h0 | (h1 << 16) : 0x7F7F7F7Fu;
+              l[i] = e4m3x2(a - f0.x, b - f0.y) | (e4m3x2(cc - f1.x, d - f1.y) << 16);
+            }
+            *reinterpret_cast<uint4*>(q + swz(row, c)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(q + 16384 + swz(row, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+          }
+          rowf[x * 128 + row] = scale_value(static_cast<uint32_t>(e)) * p.scale_log2;
+          fence_async();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_ready);
+        if (one && x == 1) {
+          ok = ok && mbar_wait(q_ready, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort);
+          ok = __all_sync(0xffffffffu, ok);
+        }
+        f = rowf[(one ? 0 : x * 128) + row];
+      }
+      float m = -INFINITY, sub = 0.f, l = 0.f;
+      for (int i = 0; i < mine; ++i) {
+        const int st = one ? 2 * i + x : i;
+        const int key0 = (w.c0 + st) * kStep;
+        const bool edge = key0 + kStep > lo;
+        ok = ok && mbar_wait(&s_full[x], static_cast<uint32_t>(done + i) & 1u, p.limit_ns, abort);
+        const int ks = (kn + st) % L::kFs;
+        if constexpr (E4M3)
+          ok = ok && mbar_wait(&kfact[ks], static_cast<uint32_t>((kn + st) / L::kFs) & 1u, p.limit_ns, abort);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+        float s[128];
+        auto load = [&]() {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(ts + static_cast<uint32_t>(32 * c), s + 32 * c);
+          tmem_ld_wait<128>(s);
+          if constexpr (E4M3) {
+            const float4* kf = reinterpret_cast<const float4*>(smem + L::kKf + ks * kStep * 4);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              const float4 k4 = kf[c];
+              mul2(s[4 * c], s[4 * c + 1], k4.x, k4.y);
+              mul2(s[4 * c + 2], s[4 * c + 3], k4.z, k4.w);
+            }
+          }
+          if (edge) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (key0 + c >= lim) s[c] = -INFINITY;
+          }
+        };
+        load();
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 128; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[c + 2 * k], s[c + 2 * k + 1]);
+        const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * f;
+        const bool raise = top > m + 8.f;
+        if (__any_sync(0xffffffffu, raise)) {
+          const float alpha = raise && m > -INFINITY ? ex2(m - top) : (raise ? 0.f : 1.f);
+          if (raise) {
+            m = top;
+            sub = top;
+            l *= alpha;
+          }
+          // S(i) is complete, so P V of the step before it is: O may be rescaled
+          if (i > 0) {
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+              float o[32];
+              tmem_ld32(to + static_cast<uint32_t>(c), o);
+              tmem_ld_wait<32>(o);
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] *= alpha;
+              uint32_t ob[32];
+#pragma unroll
+              for (int k = 0; k < 32; ++k) ob[k] = __float_as_uint(o[k]);
+              tmem_st32(to + static_cast<uint32_t>(c), ob);
+            }
+            tmem_st_wait();
+            load();
+          }
+        }
+        float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            float& u = s[64 * h + 2 * c];
+            float& v = s[64 * h + 2 * c + 1];
+            fma2(u, v, f, -sub);
+            u = ex2(u);
+            v = ex2(v);
+            if (c & 1)
+              add2(b0, b1, u, v);
+            else
+              add2(a0, a1, u, v);
+            pk[c] = bf16x2(u, v);
+          }
+          tmem_st32(ts + static_cast<uint32_t>(32 * h), pk);
+        }
+        l += (a0 + a1) + (b0 + b1);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[x]);
+      }
+      kn += n;
+      done += mine;
+      if (!ok && lane == 0) gave_up();
+      if (!one) {  // q is free for the next item while this one's results are written
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_empty);
+      }
+
+      // ---- the item's results
+      if (mine > 0) ok = ok && mbar_wait(&o_full[x], static_cast<uint32_t>(outs) & 1u, p.limit_ns, abort);
+      ok = __all_sync(0xffffffffu, ok);
+      outs += mine > 0 ? 1 : 0;
+      tc_fence_after();
+      const bool whole = w.whole();
+      const int rr = (one ? 0 : x * tile) + row;  // row of the item
+      float2* ml1 = reinterpret_cast<float2*>(smem + L::kMl);
+      float4* xo = reinterpret_cast<float4*>(smem + L::kQ + L::kTile);  // 64 columns of stream 1's O
+      float wa = 1.f, wb = 0.f;
+      if (one) {  // the two streams' rows together: stream 1 hands over
+        if (x == 1) ml1[row] = make_float2(m, l);
+        named_barrier(1, 256);
+        if (x == 0) {
+          const float2 z = ml1[row];
+          const float mm = fmaxf(m, z.x);
+          wa = m == -INFINITY ? 0.f : ex2(m - mm);
+          wb = z.x == -INFINITY ? 0.f : ex2(z.x - mm);
+          l = (wa > 0.f ? l * wa : 0.f * l) + z.y * wb;
+          m = mm;
+        }
+      }
+      const bool any_bad = *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) != 0;
+      const int* badp = bad + (items % kBads) * 3 * D;
+      const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+      const int i_tok = m_row / p.group, h_grp = m_row - i_tok * p.group;
+      __nv_bfloat16* od = p.out + (static_cast<long long>(w.s.r0 + i_tok) * p.Hq + w.h * p.group + h_grp) * D;
+      float* pd = p.part + (static_cast<long long>(w.part()) * p.part_rows + rr) * D;
+#pragma unroll
+      for (int hf = 0; hf < D / 64; ++hf) {
+        if (one) {
+          if (x == 1) {
+            if (mine > 0) {
+#pragma unroll
+              for (int c = 0; c < 64; c += 32) {
+                float o[32];
+                tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
+                tmem_ld_wait<32>(o);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4)
+                  xo[((c + k) / 4) * 128 + row] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              }
+            }
+          }
+          named_barrier(1, 256);
+        }
+        if (!one || x == 0) {
+#pragma unroll
+          for (int c = 0; c < 64; c += 32) {
+            float o[32];
+            if (mine > 0) {
+              tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
+              tmem_ld_wait<32>(o);
+            }
+            if (one && n > 1) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 4) {
+                const float4 z = xo[((c + k) / 4) * 128 + row];
+                o[k] = fmaf(z.x, wb, o[k] * wa);
+                o[k + 1] = fmaf(z.y, wb, o[k + 1] * wa);
+                o[k + 2] = fmaf(z.z, wb, o[k + 2] * wa);
+                o[k + 3] = fmaf(z.w, wb, o[k + 3] * wa);
+              }
+            }
+            if (valid && mine > 0 && !*abort) {
+              if (any_bad) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) {
+                  const int d = hf * 64 + c + k;
+                  if (lim > badp[D + d]) o[k] += INFINITY;
+                  if (lim > badp[2 * D + d]) o[k] -= INFINITY;
+                  if (lim > badp[d]) o[k] = NAN;
+                }
+              }
+              if (whole) {
+#pragma unroll
+                for (int k = 0; k < 32; k += 8)
+                  *reinterpret_cast<uint4*>(od + hf * 64 + c + k) =
+                      make_uint4(bf16x2(o[k] * inv, o[k + 1] * inv), bf16x2(o[k + 2] * inv, o[k + 3] * inv),
+                                 bf16x2(o[k + 4] * inv, o[k + 5] * inv), bf16x2(o[k + 6] * inv, o[k + 7] * inv));
+              } else {
+#pragma unroll
+                for (int k = 0; k < 32; k += 4)
+                  *reinterpret_cast<float4*>(pd + hf * 64 + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              }
+            }
+          }
+        }
+        if (one) named_barrier(1, 256);
+      }
+      if (!whole && valid && (!one || x == 0))
+        *reinterpret_cast<float2*>(p.part_ml + (static_cast<long long>(w.part()) * p.part_rows + rr) * 2) =
+            make_float2(m, l);
+      tc_fence_before();
+      if (one) fence_async();  // the exchange lay where q is loaded
+      __syncwarp();
+      if (lane == 0) {
+        if (mine > 0) mbar_arrive(&o_free[x]);
+        if (one) mbar_arrive(q_empty);
+      }
+      ++items;
+    } while (w.next(p));
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 13) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int D, bool E4M3>
+cudaError_t configure() {
+  return cudaFuncSetAttribute(paged_tc_kernel<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, Map<D, E4M3>::kDyn);
+}
+
+}  // namespace
+
+cudaError_t paged_tc_configure() {
+  cudaError_t e;
+  if ((e = configure<128, false>()) != cudaSuccess) return e;
+  return configure<128, true>();
+}
+
+cudaError_t launch_paged_tc(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p,
+                            bool e4m3, bool one, int sms, cudaStream_t st) {
+  if (e4m3)
+    paged_tc_kernel<128, true><<<sms, kThreads, Map<128, true>::kDyn, st>>>(q, k, v, p, one ? 1 : 0);
+  else
+    paged_tc_kernel<128, false><<<sms, kThreads, Map<128, false>::kDyn, st>>>(q, k, v, p, one ? 1 : 0);
+  return cudaGetLastError();
+}
+
+}  // namespace ebd

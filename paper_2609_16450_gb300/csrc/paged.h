@@ -30,12 +30,18 @@ cudaError_t launch_paged_write(const PagedRowsParams& p, cudaStream_t st);
 cudaError_t launch_paged_read(const PagedRowsParams& p, cudaStream_t st);
 
 // ------------------------------------------------------------------ attention
+// A tile in parts: the first is part 2 c + 1 of the CTA c that it begins in, the
+// k-th after it part 2 (c + k).
+struct PagedCut {
+  int parts;  // 0: none
+  int rows, m0, r0, h;  // packed rows, the first of them, the sequence's first row, K/V head
+};
 struct PagedParams {
   int B, R, Hq, Hkv, group;
   int causal;
   int page_log2, n_pages, max_pages;
   int box_log2;                // keys of a tensor-map box (at most a page)
-  int above, upto;             // sequences with above < rows * group <= upto are this launch's
+  int part_rows;               // rows of a partial result
   float scale_log2;            // softmax scale * log2(e)
   const int* cu_rows;
   const int* kv_len;
@@ -44,16 +50,26 @@ struct PagedParams {
   const __nv_bfloat16* q;
   long long q_stride;          // elements from row to row
   __nv_bfloat16* out;          // [R][Hq][D]
-  float* part;                 // [CTAs][2][tile rows][D] partial sums of split tiles,
-  float* part_ml;              // [CTAs][2][tile rows][2] their (maximum, sum)
-  int* tickets;                // [CTAs] by the CTA that a split tile begins in; zero between launches
+  int uncut;                   // shares end where tiles do: no partial results
+  float* part;                 // [CTAs][2][part_rows][D] partial sums of cut tiles,
+  float* part_ml;              // [CTAs][2][part_rows][2] their (maximum, sum)
+  struct PagedCut* cuts;       // [CTAs] the tile that a CTA's share begins and others end
   int* status;
   uint64_t limit_ns;
 };
-// tile rows and CTAs of the two kernels (their workspace)
-constexpr int kPagedRows = 64;      // mma.sync kernel: at most, per tile
-constexpr int kPagedCtasPerSm = 3;  // at most
+// Rows of a tile and CTAs per SM of the two kernels, at most (their workspace).
+constexpr int kPagedRows = 64, kPagedCtasPerSm = 3;  // mma.sync
+constexpr int kPagedTcRows = 256;                    // tcgen05, one CTA per SM
+constexpr int kPagedTcGroup = 128;                   // query heads of a group that the tcgen05 kernel takes
+constexpr int kPagedUncutKeys = 256;                 // caches of so many keys per sequence: tiles stay whole
 cudaError_t paged_configure();
+cudaError_t paged_tc_configure();
+// tcgen05, 128-wide heads; one: tiles of at most 128 rows, their steps in two streams
+cudaError_t launch_paged_tc(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p,
+                            bool e4m3, bool one, int sms, cudaStream_t st);
+// the parts of cut tiles put together, a programmatic dependent of either kernel of `ctas` CTAs
+cudaError_t launch_paged_join(const PagedParams& p, int D, int ctas, cudaStream_t st);
+int paged_attention_ctas(bool e4m3, int row_blocks, int sms);
 cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int D,
                                    bool e4m3, int row_blocks, int sms, cudaStream_t st);
 
@@ -64,9 +80,11 @@ cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, c
 // work is its chunks of CH keys (one at least).  All chunks, in that order, are
 // cut into equal contiguous shares, one per CTA, so that ragged lengths and few
 // long sequences load every SM alike; a tile cut by a share's end leaves
-// partial results, which the last CTA of the tile to finish puts together.
+// partial results, which a second kernel puts together, a warp per row: by the
+// last CTA of the tile to finish, 19 parts of 252 rows took 190 us.  Where no
+// tile has many chunks, shares are of whole tiles (uncut), and there is none.
 struct PagedSeq {
-  int r0, n, len;  // first row, rows (0: not of this launch), cached positions
+  int r0, n, len;  // first row, rows, cached positions
   int tiles;
 };
 __device__ __forceinline__ PagedSeq paged_seq(const PagedParams& p, int b, int T) {
@@ -76,8 +94,6 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedParams& p, int b, int T
   const long long cap = static_cast<long long>(p.max_pages) << p.page_log2;
   const int len = p.kv_len[b];
   s.len = len < 0 ? 0 : (len > cap ? static_cast<int>(cap) : len);
-  const long long m = static_cast<long long>(s.n) * p.group;
-  if (m <= p.above || m > p.upto) s.n = 0;
   s.tiles = static_cast<int>((static_cast<long long>(s.n) * p.group + T - 1) / T);
   return s;
 }
@@ -85,7 +101,7 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedParams& p, int b, int T
 __device__ __forceinline__ int paged_limit(const PagedParams& p, const PagedSeq& s, int i) {
   return p.causal ? min(max(s.len - s.n + i + 1, 0), s.len) : s.len;
 }
-// chunks of tile t
+// chunks of tile t, and units of work: chunks, or tiles where none is cut
 __device__ __forceinline__ int paged_chunks(const PagedParams& p, const PagedSeq& s, int t, int T, int CH) {
   const int last = min(s.n - 1, static_cast<int>(((static_cast<long long>(t) + 1) * T - 1) / p.group));
   return max(1, (paged_limit(p, s, last) + CH - 1) / CH);
@@ -93,6 +109,7 @@ __device__ __forceinline__ int paged_chunks(const PagedParams& p, const PagedSeq
 __device__ __forceinline__ long long paged_units(const PagedParams& p, const PagedSeq& s, int T, int CH) {
   long long u = 0;
   if (s.n == 0) return 0;
+  if (p.uncut) return static_cast<long long>(s.tiles) * p.Hkv;
   if (!p.causal) return static_cast<long long>(s.tiles) * p.Hkv * paged_chunks(p, s, 0, T, CH);
   for (int t = 0; t < s.tiles; ++t) u += paged_chunks(p, s, t, T, CH);
   return u * p.Hkv;
@@ -128,7 +145,7 @@ __device__ __forceinline__ void paged_plan(const PagedParams& p, int T, int CH, 
     if (w < warp) before += scan[w];
     total += scan[w];
   }
-  const long long most = (total + least - 1) / least;
+  const long long most = p.uncut ? total : (total + least - 1) / least;
   const int shares = most < gridDim.x ? static_cast<int>(most) : static_cast<int>(gridDim.x);
   long long u0 = 0, u1 = 0;
   if (static_cast<int>(blockIdx.x) < shares) {
@@ -149,11 +166,11 @@ __device__ __forceinline__ void paged_plan(const PagedParams& p, int T, int CH, 
       if (u0 < at + u) {
         int t = 0;
         for (; t < s.tiles; ++t) {
-          const long long w = static_cast<long long>(paged_chunks(p, s, t, T, CH)) * p.Hkv;
+          const long long w = static_cast<long long>(p.uncut ? 1 : paged_chunks(p, s, t, T, CH)) * p.Hkv;
           if (u0 < at + w) break;
           at += w;
         }
-        const int nch = paged_chunks(p, s, t, T, CH);
+        const int nch = p.uncut ? 1 : paged_chunks(p, s, t, T, CH);
         st->b = b;
         st->t = t;
         st->h = static_cast<int>((u0 - at) / nch);
@@ -176,7 +193,7 @@ struct PagedWalk {
   __device__ __forceinline__ void piece(const PagedParams& p, int c) {
     nch = paged_chunks(p, s, t, T, CH);
     c0 = c;
-    c1 = u1 - u < nch - c ? c + static_cast<int>(u1 - u) : nch;
+    c1 = !p.uncut && u1 - u < nch - c ? c + static_cast<int>(u1 - u) : nch;
   }
   __device__ __forceinline__ bool begin(const PagedParams& p, const PagedStart& st, int T_, int CH_) {
     T = T_;
@@ -192,7 +209,7 @@ struct PagedWalk {
     return true;
   }
   __device__ __forceinline__ bool next(const PagedParams& p) {
-    u += c1 - c0;
+    u += p.uncut ? 1 : c1 - c0;
     if (u >= u1) return false;
     if (++h == p.Hkv) {
       h = 0;
@@ -206,13 +223,33 @@ struct PagedWalk {
     return true;
   }
   __device__ __forceinline__ bool whole() const { return c0 == 0 && c1 == nch; }
+  // where this piece's partial result goes
+  __device__ __forceinline__ int part() const { return 2 * static_cast<int>(blockIdx.x) + (c0 == 0 ? 1 : 0); }
 };
-// the CTA whose share holds chunk u
+// the CTA whose share holds unit u
 __device__ __forceinline__ int paged_owner(const PagedStart& st, long long u) {
   int c = static_cast<int>(u * st.shares / st.total);
   while (c > 0 && st.total * c / st.shares > u) --c;
   while (st.total * (c + 1) / st.shares <= u) ++c;
   return c;
+}
+// What this CTA's share leaves to be put together (one thread, after
+// paged_plan): the tile that its last piece begins and does not end.
+__device__ __forceinline__ void paged_cut(const PagedParams& p, const PagedStart& st, int T, int CH) {
+  PagedCut cut{};
+  PagedWalk w;
+  if (!p.uncut && w.begin(p, st, T, CH)) {
+    do {
+      if (w.c0 == 0 && w.c1 < w.nch) {
+        cut.parts = paged_owner(st, w.u + w.nch - 1) - static_cast<int>(blockIdx.x) + 1;
+        cut.m0 = w.t * T;
+        cut.rows = min(T, w.s.n * p.group - cut.m0);
+        cut.r0 = w.s.r0;
+        cut.h = w.h;
+      }
+    } while (w.next(p));
+  }
+  p.cuts[blockIdx.x] = cut;
 }
 #endif
 

@@ -246,10 +246,23 @@ def test_attention_split_over_a_long_cache(dtype, heads, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,n", [("llada", 65), ("llada", 128), ("llada", 129), ("dream", 18), ("dream", 19),
+                                     ("dream", 37), ("mqa", 33)])
+@pytest.mark.parametrize("kv", [140, 128, 256, 129, 1500])
+def test_attention_tiles(dtype, causal, heads, n, kv):
+    """One tile of up to 128 packed rows, two, three; one step of 128 keys and more."""
+    _check(heads, dtype, 128, [n], [kv], causal, seed=n + kv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
 def test_attention_causal_rows_that_see_nothing(dtype):
     """More new rows than cached positions: the first ones see none."""
-    out = _check("dream", dtype, 16, [20, 3], [7, 3], True, seed=3)
-    assert (out[:13] == 0).all() and (out[13:20] != 0).any()
+    for heads in ("dream", "tiny"):
+        out = _check(heads, dtype, 16, [20, 3], [7, 3], True, seed=3)
+        assert (out[:13] == 0).all() and (out[13:20] != 0).any()
+    out = _check("llada", dtype, 16, [300], [100], True, seed=3)
+    assert (out[:200] == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
@@ -401,7 +414,7 @@ def test_refusals():
             assert fn(h.h, pages(), args(**kw)) == E.EBD_ERR_INVALID_ARG, kw
     for kw in (dict(kv_len=None), dict(q=None), dict(out=None), dict(q=t.data_ptr() + 2), dict(out=t.data_ptr() + 4),
                dict(q_stride=1), dict(q_stride=28 * 128 + 4), dict(causal=2), dict(max_new=-1),
-               dict(scale=math.nan), dict(scale=math.inf)):
+               dict(scale=math.nan), dict(scale=math.inf), dict(scale=-1.0)):
         assert E.ebd_paged_attention(h.h, pages(), args(**kw)) == E.EBD_ERR_INVALID_ARG, kw
         assert E.ebd_last_error(h.h)
     for fn in every:
