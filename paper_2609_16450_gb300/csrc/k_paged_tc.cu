@@ -14,9 +14,10 @@
 //     operand of P V from there.
 //   warps 0-3, 4-7: softmax of stream 0, 1, a thread per row;
 //   warps 8-11: 8-bit caches: V's codes become bf16, times their row's scale,
-//     and K's exponent bytes become factors; bf16 ones: only the steps that
-//     end in keys which rows do not see;
-//   warp 12: loads of q and K; warp 14: loads of V; warp 13: the MMAs.
+//     and K's exponent bytes become factors of the scores; bf16 ones: only the
+//     steps that end in keys which rows do not see;
+//   warp 12: loads of q and K; warp 14: loads of V; warps 13, 15: the MMAs of
+//     stream 0, 1.
 // 8-bit K and the two 4-bit terms of q multiply as they are (kind::f8f6f4, at
 // twice the rate of bf16: the two terms cost what bf16 would).
 #include <cuda_fp16.h>
@@ -172,9 +173,10 @@ struct Map {
   static constexpr uint32_t kK = kStep * D * (E4M3 ? 1 : 2);  // a step's K
   static constexpr uint32_t kV = kStep * D * 2;               // a step's V in bf16
   static constexpr int kKs = E4M3 ? 3 : 2, kVs = 2;           // ring slots
-  // K's factors: the softmax has read those of a step when its P V is done, and
-  // the warps that write them for step g have waited for P V of step g - 4
-  static constexpr int kFs = 4;
+  // K's factors.  Step g's are written once K of step g is there, so once S of
+  // step g - 3 was computed, so, in either form of the streams, once the softmax
+  // is through with step g - 5.
+  static constexpr int kFs = 5;
   static constexpr uint32_t kQ = 0;
   static constexpr uint32_t kK0 = kQ + 2 * kTile;
   static constexpr uint32_t kV0 = kK0 + kKs * kK;
@@ -182,13 +184,13 @@ struct Map {
   static constexpr uint32_t kKe = kRaw + (E4M3 ? kVs * kStep * D : 0);  // exponent bytes
   static constexpr uint32_t kVe = kKe + kKs * kStep;
   static constexpr uint32_t kKf = kVe + kVs * kStep;          // [kFs][kStep] K's factors
-  static constexpr uint32_t kRowF = kKf + (E4M3 ? kFs * kStep * 4 : 0);  // [2][128]
+  static constexpr uint32_t kRowF = kKf + (E4M3 ? kFs * kStep * 2 : 0);  // [2][128]
   static constexpr uint32_t kMl = kRowF + 2 * 128 * 4;        // [128][2] stream 1's (maximum, sum)
   static constexpr uint32_t kBad = kMl + 128 * 8;             // [kBads][3][D]
   static constexpr uint32_t kBar = kBad + kBads * 3 * D * 4;
   // k full, empty, factors; v full, empty, raw full, raw empty; s, p, o full
-  // and o free of 2 streams; q full, ready, empty; drain
-  static constexpr int kNBar = 2 * kKs + kFs + 4 * kVs + 8 + 4;
+  // and o free of 2 streams; q full, ready, empty; drain and turn of 2 streams
+  static constexpr int kNBar = 2 * kKs + kFs + 4 * kVs + 8 + 7;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
   static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32 + 1) * 8;
   static constexpr uint32_t kBytes = kMisc + 32;
@@ -220,7 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_full = o_free + 2;
   uint64_t* q_ready = q_full + 1;
   uint64_t* q_empty = q_ready + 1;
-  uint64_t* drain = q_empty + 1;
+  uint64_t* drain = q_empty + 1;   // [2]
+  uint64_t* turn = drain + 2;      // [2]
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
   auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMisc);
@@ -237,12 +240,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < L::kKs; ++s) {
       mbar_init(&kfull[s], 1);
-      mbar_init(&kempty[s], E4M3 ? 5 : 1);  // the MMAs, and the warps that read its exponents
+      mbar_init(&kempty[s], E4M3 ? 6 : 2);  // the two streams' MMAs, and the warps that read its exponents
     }
     for (int s = 0; s < L::kFs; ++s) mbar_init(&kfact[s], 4);
     for (int s = 0; s < L::kVs; ++s) {
       mbar_init(&vfull[s], E4M3 ? 4 : 1);
-      mbar_init(&vempty[s], E4M3 ? 1 : 5);  // the MMAs, and the warps that see to its last rows
+      mbar_init(&vempty[s], E4M3 ? 2 : 6);  // the two streams' MMAs, and the warps that see to its last rows
       mbar_init(&rfull[s], E4M3 ? 1 : 4);
       mbar_init(&rempty[s], 4);
     }
@@ -254,8 +257,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(q_full, 1);
     mbar_init(q_ready, 8);
-    mbar_init(q_empty, 9);  // the MMAs, and the softmax warps
-    mbar_init(drain, 1);
+    mbar_init(q_empty, 10);  // the two streams' MMAs, and the softmax warps
+    mbar_init(&drain[0], 1);
+    mbar_init(&drain[1], 1);
+    mbar_init(&turn[0], 1);
+    mbar_init(&turn[1], 1);
     *abort = 0;
     for (int i = 0; i < kBads; ++i) s_bad[i] = 0;
     fence_mbar_init();
@@ -267,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (tid == kThreads - 1) paged_cut(p, *plan, T, kStep);  // of a warp without other work
+  if (tid == 256) paged_cut(p, *plan, T, kStep);
   PagedWalk w;
   const bool work = w.begin(p, *plan, T, kStep);
   auto gave_up = [&]() {
@@ -313,6 +319,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int x = lane / NB, hf = lane % NB;
             tma_load_3d(smem + L::kQ + x * L::kTile + hf * 16384, &tm_q, q_full, hf * 64, w.h * p.group,
                         w.s.r0 + (w.t * T + x * tile) / p.group);
+            PagedWalk next = w;  // the next item's q into L2
+            if (next.next(p))
+              asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(&tm_q),
+                           "r"(hf * 64), "r"(next.h * p.group), "r"(next.s.r0 + (next.t * T + x * tile) / p.group)
+                           : "memory");
           }
           ++items;
         }
@@ -357,8 +368,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           mbar_wait(&fullb[j % slots], static_cast<uint32_t>(j / slots) & 1u, p.limit_ns, nullptr);
         if (is_k && items > 0) mbar_wait(q_full, static_cast<uint32_t>(items - 1) & 1u, p.limit_ns, nullptr);
       }
-    } else if (work && warp == 13) {
-      // ---------------------------------------------------------- MMAs
+    } else if (work) {
+      // ---------------------------------------------------------- MMAs of stream x
+      const int x = warp == 13 ? 0 : 1;
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       const uint32_t idesc_s = E4M3 ? (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24) : umma_idesc_bf16(128, 128);
       const uint32_t idesc_o = umma_idesc_bf16(128, D) | (1u << 16);  // B (V) MN-major
@@ -367,103 +379,134 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t k_lo0 = static_cast<uint32_t>(umma_desc_sw128(smem_u32(smem + L::kK0)));
       // V: 64-column blocks 16384 bytes apart (leading byte offset)
       const uint32_t v_lo0 = ((smem_u32(smem + L::kV0) >> 4) & 0x3FFFu) | ((16384u >> 4) << 16);
-      int kn = 0, vn = 0, en = 0, items = 0;  // K and V steps, V steps seen to, before this item
-      int done[2] = {0, 0};           // steps of each stream before this item
-      int outs[2] = {0, 0};           // items that each stream had steps of
+      // A turn is P V of a step and S of the next.  All that it needs is waited
+      // for before the probabilities, its last operand.  A warp of its own for
+      // each stream, as one warp's waits and issues took as long as its MMAs,
+      // which idled meanwhile; and turns alternate, as MMAs of both streams
+      // mixed end together, both softmaxes then run at once, and the tensor
+      // cores wait for them (4480 cycles a step instead of ~3000).
+      const uint32_t ts = __shfl_sync(0xffffffffu, tm + static_cast<uint32_t>(x * 128), 0);
+      const uint32_t to = tm + 256u + static_cast<uint32_t>(x * D);
+      int kn = 0, en = 0;  // steps, and steps whose V is seen to, before this item
+      uint32_t qph = 0, pph = 0, fph = 1, tph = x == 0 ? 1 : 0;  // q, p_full, o_free (free at first), turn (stream 0's)
       bool ok = true;
+      // Steps in order: a step that is the other stream's is passed when it has
+      // landed, with this stream's share of its slot's release, so that no wait
+      // is ever two phases of its barrier away.
+      int kpos = 0, vpos = 0;
+      auto k_there = [&](int st) {
+        return mbar_wait(&kfull[st % L::kKs], static_cast<uint32_t>(st / L::kKs) & 1u, p.limit_ns, abort);
+      };
+      auto v_there = [&](int st) {
+        return mbar_wait(&vfull[st % L::kVs], static_cast<uint32_t>(st / L::kVs) & 1u, p.limit_ns, abort);
+      };
+      auto pass_k = [&](int to_step) {
+        for (; kpos < to_step; ++kpos) {
+          ok = ok && __all_sync(0xffffffffu, k_there(kpos));
+          if (lane == 0) mbar_arrive(&kempty[kpos % L::kKs]);
+        }
+      };
+      auto pass_v = [&](int to_step) {
+        for (; vpos < to_step; ++vpos) {
+          ok = ok && __all_sync(0xffffffffu, v_there(vpos));
+          if (lane == 0) mbar_arrive(&vempty[vpos % L::kVs]);
+        }
+      };
       do {
         const int n = w.c1 - w.c0;
-        const int ns[2] = {steps_of(0, n), steps_of(1, n)};
+        const int mine = steps_of(x, n), turns = steps_of(0, n) + 1;
         const int edge0 = E4M3 ? n : max(0, min(n, lim_first() / kStep - w.c0));  // V steps from here are seen to
-        ok = __all_sync(0xffffffffu, mbar_wait(E4M3 ? q_ready : q_full, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort));
-        tc_fence_after();
-        const int last = one ? (ns[0] > ns[1] ? 0 : 1) : (ns[1] > 0 ? 1 : 0);  // stream of the item's last S
-        for (int i = 0; i <= ns[0] && ok; ++i) {
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            if (i > 0 && i - 1 < ns[x]) {  // O += P V
-              const int st = one ? 2 * (i - 1) + x : i - 1;
-              const int s = (vn + st) % L::kVs;
-              const uint32_t ph = static_cast<uint32_t>((vn + st) / L::kVs) & 1u;
-              bool g = mbar_wait(&p_full[x], static_cast<uint32_t>(done[x] + i - 1) & 1u, p.limit_ns, abort) &&
-                       mbar_wait(&vfull[s], ph, p.limit_ns, abort);
-              if (!E4M3 && st >= edge0) {
-                const int e = en + st - edge0;
-                g = g && mbar_wait(&rfull[e & 1], static_cast<uint32_t>(e >> 1) & 1u, p.limit_ns, abort);
-              }
-              if (i == 1 && outs[x] > 0)
-                g = g && mbar_wait(&o_free[x], static_cast<uint32_t>(outs[x] - 1) & 1u, p.limit_ns, abort);
-              ok = __all_sync(0xffffffffu, g);
-              if (!ok) break;
-              tc_fence_after();
-              const uint32_t v_lo = v_lo0 + static_cast<uint32_t>(s) * (L::kV >> 4);
-              const uint32_t d = tm + 256u + static_cast<uint32_t>(x * D);
-              const uint32_t a = tm + static_cast<uint32_t>(x * 128);
-              if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < kStep / 16; ++kk)
-                  umma_bf16_ts(d, a + static_cast<uint32_t>(kk * 8), v_lo + static_cast<uint32_t>(kk * (2048 >> 4)), hi,
-                               idesc_o, kk != 0 || i > 1 ? 1u : 0u);
-                if (one || x == 1 || ns[1] == 0) umma_commit(&vempty[s]);
-                if (i == ns[x]) umma_commit(&o_full[x]);
-              }
-              __syncwarp();
+        const uint32_t ql = q_lo + (one ? 0u : static_cast<uint32_t>(x) * (L::kTile >> 4));
+        ok = __all_sync(0xffffffffu, mbar_wait(E4M3 ? q_ready : q_full, qph, p.limit_ns, abort));
+        if (!ok) break;
+        qph ^= 1u;
+        for (int i = 0; i < turns && ok; ++i) {
+          const bool pv = i > 0 && i - 1 < mine, qk = i < mine;
+          const int kst = kn + (one ? 2 * i + x : i), vst = kst - (one ? 2 : 1);
+          if (qk) pass_k(kst);
+          if (pv) pass_v(vst);
+          if (mine == 0 && i < n) {
+            pass_k(kn + i + 1);
+            pass_v(kn + i + 1);
+          }
+          const int ks = kst % L::kKs, vs = vst % L::kVs;
+          const uint32_t v_lo = v_lo0 + static_cast<uint32_t>(vs) * (L::kV >> 4);
+          const uint32_t kl = k_lo0 + static_cast<uint32_t>(ks) * (L::kK >> 4);
+          bool g = true;
+          if (qk) g = k_there(kst);
+          if (pv) {
+            g = g && v_there(vst);
+            if constexpr (!E4M3) {
+              const int e = en + vst - kn - edge0;
+              if (vst - kn >= edge0) g = g && mbar_wait(&rfull[e & 1], static_cast<uint32_t>(e >> 1) & 1u, p.limit_ns, abort);
             }
-            if (i < ns[x]) {  // S = Q K^T
-              const int st = one ? 2 * i + x : i;
-              const int s = (kn + st) % L::kKs;
-              ok = __all_sync(0xffffffffu, mbar_wait(&kfull[s], static_cast<uint32_t>((kn + st) / L::kKs) & 1u,
-                                                     p.limit_ns, abort));
-              if (!ok) break;
-              tc_fence_after();
-              const uint32_t ql = q_lo + (one ? 0u : static_cast<uint32_t>(x) * (L::kTile >> 4));
-              const uint32_t kl = k_lo0 + static_cast<uint32_t>(s) * (L::kK >> 4);
-              const uint32_t d = tm + static_cast<uint32_t>(x * 128);
-              if (elect_one()) {
-                if constexpr (E4M3) {
+            if (i == 1) {
+              g = g && mbar_wait(o_free + x, fph, p.limit_ns, abort);
+              fph ^= 1u;
+            }
+            g = g && mbar_wait(p_full + x, pph, p.limit_ns, abort);
+            pph ^= 1u;
+          }
+          g = g && mbar_wait(turn + x, tph, p.limit_ns, abort);
+          tph ^= 1u;
+          ok = ok && __all_sync(0xffffffffu, g);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            if (pv) {
 #pragma unroll
-                  for (int term = 0; term < 2; ++term)
+              for (int kk = 0; kk < kStep / 16; ++kk)
+                umma_bf16_ts(to, ts + static_cast<uint32_t>(kk * 8), v_lo + static_cast<uint32_t>(kk * (2048 >> 4)), hi,
+                             idesc_o, kk != 0 || i > 1 ? 1u : 0u);
+              umma_commit(&vempty[vs]);
+              if (i == mine) umma_commit(o_full + x);
+            }
+            if (qk) {
+              if constexpr (E4M3) {
 #pragma unroll
-                    for (int kk = 0; kk < D / 32; ++kk)
-                      umma_e4m3_lo(d, ql + static_cast<uint32_t>(term * (16384 >> 4) + kk * 2),
-                                   kl + static_cast<uint32_t>(kk * 2), hi, idesc_s, term + kk > 0 ? 1u : 0u);
-                } else {
+                for (int term = 0; term < 2; ++term)
 #pragma unroll
-                  for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16_lo(d, ql + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
-                                 kl + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), hi, idesc_s,
-                                 kk > 0 ? 1u : 0u);
-                }
-                umma_commit(&s_full[x]);
-                if (one || x == 1 || ns[1] == 0) umma_commit(&kempty[s]);
-                if (x == last && i == ns[x] - 1) umma_commit(q_empty);
+                  for (int kk = 0; kk < D / 32; ++kk)
+                    umma_e4m3_lo(ts, ql + static_cast<uint32_t>(term * (16384 >> 4) + kk * 2),
+                                 kl + static_cast<uint32_t>(kk * 2), hi, idesc_s, term + kk > 0 ? 1u : 0u);
+              } else {
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                  umma_bf16_lo(ts, ql + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                               kl + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), hi, idesc_s,
+                               kk > 0 ? 1u : 0u);
               }
-              __syncwarp();
+              umma_commit(s_full + x);
+              umma_commit(&kempty[ks]);
+              if (i == mine - 1) umma_commit(q_empty);
             }
           }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(turn + (x ^ 1));
+          if (qk) kpos = kst + 1;
+          if (pv) vpos = vst + 1;
         }
+        if (!ok) break;
+        if (mine == 0) {
+          if (lane == 0) mbar_arrive(q_empty);
+        }
+        pass_k(kn + n);
+        pass_v(kn + n);
         kn += n;
-        vn += n;
         en += n - edge0;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          done[x] += ns[x];
-          outs[x] += ns[x] > 0 ? 1 : 0;
-        }
-        ++items;
       } while (ok && w.next(p));
       if (!ok) {
         if (lane == 0) gave_up();
-        if (elect_one()) umma_commit(drain);  // completes once every MMA issued so far is done
+        if (elect_one()) umma_commit(drain + x);  // completes once every MMA issued so far is done
         __syncwarp();
-        mbar_wait(drain, 0, p.limit_ns, nullptr);
+        mbar_wait(drain + x, 0, p.limit_ns, nullptr);
       }
     }
   } else if (warp >= 8) {
     // ------------------------------------------------------------ V's codes, K's factors, last rows
     regs_dec<kOtherRegs>();
     const int r = tid - 256;  // key of a step
-    int kn = 0, vn = 0, en = 0, items = 0;
+    int vn = 0, en = 0, items = 0;
     bool ok = work;
     if (work) do {
       const int n = w.c1 - w.c0;
@@ -483,11 +526,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       if constexpr (E4M3) {
         auto factors = [&](int j) {
-          const int s = (kn + j) % L::kKs;
-          ok = ok && mbar_wait(&kfull[s], static_cast<uint32_t>((kn + j) / L::kKs) & 1u, p.limit_ns, abort);
+          const int s = (vn + j) % L::kKs, fs = (vn + j) % L::kFs;
+          ok = ok && mbar_wait(&kfull[s], static_cast<uint32_t>((vn + j) / L::kKs) & 1u, p.limit_ns, abort);
           ok = __all_sync(0xffffffffu, ok);
-          const int fs = (kn + j) % L::kFs;
-          reinterpret_cast<float*>(smem + L::kKf)[fs * kStep + r] = scale_value((smem + L::kKe)[s * kStep + r]);
+          const uint32_t e = (smem + L::kKe)[s * kStep + r];  // 2^(e - 127) in bf16
+          reinterpret_cast<uint16_t*>(smem + L::kKf)[fs * kStep + r] = static_cast<uint16_t>(e > 0 ? e << 7 : 0x40u);
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(&kfact[fs]);
@@ -521,10 +564,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           const bool two = __any_sync(0xffffffffu, m2 != 0x3F803F80u);
           const uint8_t* src = smem + L::kRaw + s * kStep * D;
           uint8_t* dst = smem + L::kV0 + s * L::kV;
+          uint4 in[D / 16];
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) in[c] = *reinterpret_cast<const uint4*>(src + swz(r, c));
 #pragma unroll
           for (int c = 0; c < D / 16; ++c) {
-            const uint4 x4 = *reinterpret_cast<const uint4*>(src + swz(r, c));
-            const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
+            const uint32_t x[4] = {in[c].x, in[c].y, in[c].z, in[c].w};
             uint32_t y[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -594,7 +639,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         en += n - edge0;
       }
-      kn += n;
       vn += n;
       ++items;
     } while (w.next(p));
@@ -666,7 +710,28 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         f = rowf[(one ? 0 : x * 128) + row];
       }
-      float m = -INFINITY, sub = 0.f, l = 0.f;
+      // Probabilities are taken against a reference `ref` near the row's running
+      // maximum (2^(y - ref), y in log2 units): the first step's maximum, moved
+      // up after a step that went more than 8 past it, for the next one.  A step
+      // is read twice, its maximum first, only at the item's begin, for a row's
+      // first key that it sees, and where a score is more than 24 past `ref`
+      // (sums and O stay far inside 32 bits up to there).  So the maximum is not
+      // waited for, and few registers hold scores.
+      float ref = 0.f, l = 0.f, alpha = 1.f;
+      bool started = false, pend = false;  // a key seen; O to be scaled by alpha
+      auto rescale = [&](float a) {
+#pragma unroll
+        for (int c = 0; c < D; c += 32) {
+          float o[32];
+          uint32_t ob[32];
+          tmem_ld32(to + static_cast<uint32_t>(c), o);
+          tmem_ld_wait<32>(o);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) ob[k] = __float_as_uint(o[k] * a);
+          tmem_st32(to + static_cast<uint32_t>(c), ob);
+        }
+        tmem_st_wait();
+      };
       for (int i = 0; i < mine; ++i) {
         const int st = one ? 2 * i + x : i;
         const int key0 = (w.c0 + st) * kStep;
@@ -677,79 +742,93 @@ __global__ void __launch_bounds__(kThreads, 1)
           ok = ok && mbar_wait(&kfact[ks], static_cast<uint32_t>((kn + st) / L::kFs) & 1u, p.limit_ns, abort);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
-        float s[128];
-        auto load = [&]() {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(ts + static_cast<uint32_t>(32 * c), s + 32 * c);
-          tmem_ld_wait<128>(s);
+        // S(i) is complete, so P V of the step before it is: O may be rescaled
+        if (__any_sync(0xffffffffu, pend)) rescale(pend ? alpha : 1.f);
+        pend = false;
+        // scores 32 c .. 32 c + 31, once loaded: K's factors, what the row does not see
+        auto finish = [&](int c, float* s) {
           if constexpr (E4M3) {
-            const float4* kf = reinterpret_cast<const float4*>(smem + L::kKf + ks * kStep * 4);
+            const uint4* kf = reinterpret_cast<const uint4*>(smem + L::kKf + (ks * kStep + 32 * c) * 2);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const float4 k4 = kf[c];
-              mul2(s[4 * c], s[4 * c + 1], k4.x, k4.y);
-              mul2(s[4 * c + 2], s[4 * c + 3], k4.z, k4.w);
+            for (int k = 0; k < 4; ++k) {
+              const uint4 k8 = kf[k];
+              const uint32_t u[4] = {k8.x, k8.y, k8.z, k8.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                mul2(s[8 * k + 2 * e], s[8 * k + 2 * e + 1], __uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xFFFF0000u));
             }
           }
           if (edge) {
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (key0 + c >= lim) s[c] = -INFINITY;
+            for (int k = 0; k < 32; ++k)
+              if (key0 + 32 * c + k >= lim) s[k] = -INFINITY;
           }
         };
-        load();
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        uint32_t pk[64];
+        float sum, top;
+        bool exact = i == 0;
+        for (;;) {
+          if (exact) {
+            float mx = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 128; c += 8)
+            for (int c = 0; c < 4; ++c) {
+              float s[32];
+              tmem_ld32(ts + static_cast<uint32_t>(32 * c), s);
+              tmem_ld_wait<32>(s);
+              finish(c, s);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], s[c + 2 * k], s[c + 2 * k + 1]);
-        const float top = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * f;
-        const bool raise = top > m + 8.f;
-        if (__any_sync(0xffffffffu, raise)) {
-          const float alpha = raise && m > -INFINITY ? ex2(m - top) : (raise ? 0.f : 1.f);
-          if (raise) {
-            m = top;
-            sub = top;
-            l *= alpha;
-          }
-          // S(i) is complete, so P V of the step before it is: O may be rescaled
-          if (i > 0) {
-#pragma unroll
-            for (int c = 0; c < D; c += 32) {
-              float o[32];
-              tmem_ld32(to + static_cast<uint32_t>(c), o);
-              tmem_ld_wait<32>(o);
-#pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] *= alpha;
-              uint32_t ob[32];
-#pragma unroll
-              for (int k = 0; k < 32; ++k) ob[k] = __float_as_uint(o[k]);
-              tmem_st32(to + static_cast<uint32_t>(c), ob);
+              for (int k = 0; k < 32; k += 2) mx = max3(mx, s[k], s[k + 1]);
             }
-            tmem_st_wait();
-            load();
+            mx *= f;
+            float a = 1.f;
+            if (mx > -INFINITY && (!started || mx > ref)) {
+              if (started) a = ex2(ref - mx);
+              l *= a;
+              ref = mx;
+              started = true;
+            }
+            if (i > 0 && __any_sync(0xffffffffu, valid && a != 1.f)) rescale(a);
           }
-        }
-        float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f;
+          float s[2][32];
+          tmem_ld32(ts, s[0]);
+          tmem_ld_wait<32>(s[0]);
+          float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t pk[32];
+          for (int c = 0; c < 4; ++c) {
+            float* v = s[c & 1];
+            if (c < 3) tmem_ld32(ts + static_cast<uint32_t>(32 * (c + 1)), s[(c + 1) & 1]);
+            finish(c, v);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            float& u = s[64 * h + 2 * c];
-            float& v = s[64 * h + 2 * c + 1];
-            fma2(u, v, f, -sub);
-            u = ex2(u);
-            v = ex2(v);
-            if (c & 1)
-              add2(b0, b1, u, v);
-            else
-              add2(a0, a1, u, v);
-            pk[c] = bf16x2(u, v);
+            for (int k = 0; k < 32; k += 4) {
+              fma2(v[k], v[k + 1], f, -ref);
+              fma2(v[k + 2], v[k + 3], f, -ref);
+              t0 = max3(t0, v[k], v[k + 1]);
+              t1 = max3(t1, v[k + 2], v[k + 3]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[k + e] = ex2(v[k + e]);
+              add2(a0, a1, v[k], v[k + 1]);
+              add2(b0, b1, v[k + 2], v[k + 3]);
+              pk[16 * c + k / 2] = bf16x2(v[k], v[k + 1]);
+              pk[16 * c + k / 2 + 1] = bf16x2(v[k + 2], v[k + 3]);
+            }
+            if (c < 3) tmem_ld_wait<32>(s[(c + 1) & 1]);
           }
-          tmem_st32(ts + static_cast<uint32_t>(32 * h), pk);
+          top = fmaxf(t0, t1);
+          sum = (a0 + a1) + (b0 + b1);
+          // rows past the tile hold what memory held: they have no say
+          const bool again = valid && (top > 24.f || (!started && top > -INFINITY));
+          if (exact || !__any_sync(0xffffffffu, again)) break;
+          exact = true;
         }
-        l += (a0 + a1) + (b0 + b1);
+        tmem_st32(ts, pk);
+        tmem_st32(ts + 32u, pk + 32);
+        l += sum;
+        if (valid && top > 8.f && started) {
+          alpha = ex2(-top);
+          ref += top;
+          l *= alpha;
+          pend = true;
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -758,10 +837,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       kn += n;
       done += mine;
       if (!ok && lane == 0) gave_up();
-      if (!one) {  // q is free for the next item while this one's results are written
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_empty);
-      }
 
       // ---- the item's results
       if (mine > 0) ok = ok && mbar_wait(&o_full[x], static_cast<uint32_t>(outs) & 1u, p.limit_ns, abort);
@@ -770,6 +845,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_after();
       const bool whole = w.whole();
       const int rr = (one ? 0 : x * tile) + row;  // row of the item
+      const float tail = pend ? alpha : 1.f;
+      float m = l == 0.f ? -INFINITY : ref;
       float2* ml1 = reinterpret_cast<float2*>(smem + L::kMl);
       float4* xo = reinterpret_cast<float4*>(smem + L::kQ + L::kTile);  // 64 columns of stream 1's O
       float wa = 1.f, wb = 0.f;
@@ -781,42 +858,59 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float mm = fmaxf(m, z.x);
           wa = m == -INFINITY ? 0.f : ex2(m - mm);
           wb = z.x == -INFINITY ? 0.f : ex2(z.x - mm);
-          l = (wa > 0.f ? l * wa : 0.f * l) + z.y * wb;
+          l = l * wa + z.y * wb;
           m = mm;
         }
       }
       const bool any_bad = *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) != 0;
       const int* badp = bad + (items % kBads) * 3 * D;
       const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+      // Rows go out through shared memory, a warp's 32 where its part of q lay
+      // (every S of the item is complete), so that a store is of whole rows:
+      // straight from the row's lane, 16 bytes a row, they took 9 to 18 thousand
+      // cycles an item.
       const int i_tok = m_row / p.group, h_grp = m_row - i_tok * p.group;
-      __nv_bfloat16* od = p.out + (static_cast<long long>(w.s.r0 + i_tok) * p.Hq + w.h * p.group + h_grp) * D;
-      float* pd = p.part + (static_cast<long long>(w.part()) * p.part_rows + rr) * D;
+      const long long at = whole ? (static_cast<long long>(w.s.r0 + i_tok) * p.Hq + w.h * p.group + h_grp) * D
+                                 : (static_cast<long long>(w.part()) * p.part_rows + rr) * D;
+      uint8_t* stage = smem + L::kQ + (one ? 0 : x * L::kTile) + (warp & 3) * 8192;
+      const uint32_t live = __ballot_sync(0xffffffffu, valid && mine > 0 && !*abort);
+      // 16-byte pieces of 256-byte rows: piece c of row r at c ^ (r % 16)
+      auto put = [&](int c, uint4 v) { *reinterpret_cast<uint4*>(stage + lane * 256 + ((c ^ (lane & 15)) << 4)) = v; };
+      auto send = [&](auto&& to_global) {
+        __syncwarp();
+#pragma unroll 4
+        for (int k = 0; k < 16; ++k) {
+          const int r = 2 * k + (lane >> 4), c = lane & 15;
+          const long long o = __shfl_sync(0xffffffffu, at, r);
+          if ((live >> r) & 1u) to_global(o, c, *reinterpret_cast<const uint4*>(stage + r * 256 + ((c ^ (r & 15)) << 4)));
+        }
+        __syncwarp();
+      };
 #pragma unroll
       for (int hf = 0; hf < D / 64; ++hf) {
         if (one) {
-          if (x == 1) {
-            if (mine > 0) {
+          if (x == 1 && mine > 0) {
 #pragma unroll
-              for (int c = 0; c < 64; c += 32) {
-                float o[32];
-                tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
-                tmem_ld_wait<32>(o);
+            for (int c = 0; c < 64; c += 32) {
+              float o[32];
+              tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
+              tmem_ld_wait<32>(o);
 #pragma unroll
-                for (int k = 0; k < 32; k += 4)
-                  xo[((c + k) / 4) * 128 + row] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-              }
+              for (int k = 0; k < 32; k += 4)
+                xo[((c + k) / 4) * 128 + row] =
+                    make_float4(o[k] * tail, o[k + 1] * tail, o[k + 2] * tail, o[k + 3] * tail);
             }
           }
           named_barrier(1, 256);
         }
-        if (!one || x == 0) {
+        if ((!one || x == 0) && mine > 0) {
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
             float o[32];
-            if (mine > 0) {
-              tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
-              tmem_ld_wait<32>(o);
-            }
+            tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
+            tmem_ld_wait<32>(o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] *= tail;
             if (one && n > 1) {
 #pragma unroll
               for (int k = 0; k < 32; k += 4) {
@@ -827,41 +921,44 @@ __global__ void __launch_bounds__(kThreads, 1)
                 o[k + 3] = fmaf(z.w, wb, o[k + 3] * wa);
               }
             }
-            if (valid && mine > 0 && !*abort) {
-              if (any_bad) {
+            if (any_bad) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                  const int d = hf * 64 + c + k;
-                  if (lim > badp[D + d]) o[k] += INFINITY;
-                  if (lim > badp[2 * D + d]) o[k] -= INFINITY;
-                  if (lim > badp[d]) o[k] = NAN;
-                }
-              }
-              if (whole) {
-#pragma unroll
-                for (int k = 0; k < 32; k += 8)
-                  *reinterpret_cast<uint4*>(od + hf * 64 + c + k) =
-                      make_uint4(bf16x2(o[k] * inv, o[k + 1] * inv), bf16x2(o[k + 2] * inv, o[k + 3] * inv),
-                                 bf16x2(o[k + 4] * inv, o[k + 5] * inv), bf16x2(o[k + 6] * inv, o[k + 7] * inv));
-              } else {
-#pragma unroll
-                for (int k = 0; k < 32; k += 4)
-                  *reinterpret_cast<float4*>(pd + hf * 64 + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              for (int k = 0; k < 32; ++k) {
+                const int d = hf * 64 + c + k;
+                if (lim > badp[D + d]) o[k] += INFINITY;
+                if (lim > badp[2 * D + d]) o[k] -= INFINITY;
+                if (lim > badp[d]) o[k] = NAN;
               }
             }
+            if (whole) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 8)
+                put((hf * 64 + c + k) / 8,
+                    make_uint4(bf16x2(o[k] * inv, o[k + 1] * inv), bf16x2(o[k + 2] * inv, o[k + 3] * inv),
+                               bf16x2(o[k + 4] * inv, o[k + 5] * inv), bf16x2(o[k + 6] * inv, o[k + 7] * inv)));
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; k += 4)
+                put((c + k) / 4, make_uint4(__float_as_uint(o[k]), __float_as_uint(o[k + 1]), __float_as_uint(o[k + 2]),
+                                            __float_as_uint(o[k + 3])));
+            }
           }
+          if (!whole)
+            send([&](long long o, int c, uint4 v) { *reinterpret_cast<uint4*>(p.part + o + hf * 64 + c * 4) = v; });
         }
         if (one) named_barrier(1, 256);
       }
+      if (whole && (!one || x == 0))
+        send([&](long long o, int c, uint4 v) { *reinterpret_cast<uint4*>(p.out + o + c * 8) = v; });
       if (!whole && valid && (!one || x == 0))
         *reinterpret_cast<float2*>(p.part_ml + (static_cast<long long>(w.part()) * p.part_rows + rr) * 2) =
             make_float2(m, l);
       tc_fence_before();
-      if (one) fence_async();  // the exchange lay where q is loaded
+      fence_async();  // rows and exchange lay where q is loaded
       __syncwarp();
       if (lane == 0) {
         if (mine > 0) mbar_arrive(&o_free[x]);
-        if (one) mbar_arrive(q_empty);
+        mbar_arrive(q_empty);
       }
       ++items;
     } while (w.next(p));
