@@ -308,10 +308,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       int n = 0, items = 0;
       bool ok = true;
       do {
-        if (is_k) {  // q
+        auto load_q = [&]() {
           ok = items == 0 || mbar_wait(q_empty, static_cast<uint32_t>(items - 1) & 1u, p.limit_ns, abort);
           ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
+          if (!ok) return;
           const int tiles = !one && rows_here() > tile ? 2 : 1;
           if (lane == 0) mbar_arrive_expect_tx(q_full, static_cast<uint32_t>(tiles) * tile * D * 2);
           __syncwarp();
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                            : "memory");
           }
           ++items;
-        }
+        };
         const int lim = lim_last();
         const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
         int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
@@ -358,6 +358,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         scales + ((static_cast<long long>(page) * p.Hkv + w.h) << p.page_log2) + off, box, &fullb[s]);
             else
               tma_load_4d(ring + s * op + part * 16384 + key_in * 128, tm, &fullb[s], part * 64, off, w.h, page);
+          }
+          // K of the item's first steps goes ahead of its q, which waits for the last item's results
+          if (is_k && c == min(w.c0 + slots, w.c1) - 1) load_q();
+          if (!ok) {
+            ++n;
+            break;
           }
         }
       } while (ok && w.next(p));
@@ -432,8 +438,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int ks = kst % L::kKs, vs = vst % L::kVs;
           const uint32_t v_lo = v_lo0 + static_cast<uint32_t>(vs) * (L::kV >> 4);
           const uint32_t kl = k_lo0 + static_cast<uint32_t>(ks) * (L::kK >> 4);
-          bool g = true;
-          if (qk) g = k_there(kst);
+          bool g = mbar_wait(turn + x, tph, p.limit_ns, abort);
+          tph ^= 1u;
+          if (qk) g = g && k_there(kst);
           if (pv) {
             g = g && v_there(vst);
             if constexpr (!E4M3) {
@@ -447,8 +454,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             g = g && mbar_wait(p_full + x, pph, p.limit_ns, abort);
             pph ^= 1u;
           }
-          g = g && mbar_wait(turn + x, tph, p.limit_ns, abort);
-          tph ^= 1u;
           ok = ok && __all_sync(0xffffffffu, g);
           if (!ok) break;
           tc_fence_after();
@@ -466,23 +471,28 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int term = 0; term < 2; ++term)
 #pragma unroll
-                  for (int kk = 0; kk < D / 32; ++kk)
+                  for (int kk = 0; kk < D / 32; ++kk) {
+                    if (term == 1 && kk == 0) mbar_arrive(turn + (x ^ 1));
                     umma_e4m3_lo(ts, ql + static_cast<uint32_t>(term * (16384 >> 4) + kk * 2),
                                  kl + static_cast<uint32_t>(kk * 2), hi, idesc_s, term + kk > 0 ? 1u : 0u);
+                  }
               } else {
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk)
+                for (int kk = 0; kk < D / 16; ++kk) {
+                  if (kk == D / 32) mbar_arrive(turn + (x ^ 1));  // half a product ahead: issue waits on the pipe
                   umma_bf16_lo(ts, ql + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
                                kl + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), hi, idesc_s,
                                kk > 0 ? 1u : 0u);
+                }
               }
               umma_commit(s_full + x);
               umma_commit(&kempty[ks]);
               if (i == mine - 1) umma_commit(q_empty);
+            } else {
+              mbar_arrive(turn + (x ^ 1));
             }
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(turn + (x ^ 1));
           if (qk) kpos = kst + 1;
           if (pv) vpos = vst + 1;
         }
@@ -606,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int key = (w.c0 + j) * kStep + r;
           uint8_t* v = smem + L::kV0 + s * L::kV;
           if (ok && j >= edge0 && key >= lo) {
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < D / 8; ++c) {
               uint4* q = reinterpret_cast<uint4*>(v + (c >> 3) * 16384 + swz(r, c & 7));
               if (key >= hi) {
@@ -614,20 +624,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 continue;
               }
               const uint4 x4 = *q;
-              uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
-              bool any = false;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const uint32_t b = (x[i] >> (16 * h)) & 0xFFFFu;
-                  if ((b & 0x7F80u) == 0x7F80u) {
-                    note(key, c * 8 + 2 * i + h, (b & 0x7Fu) ? 0 : (b & 0x8000u) ? 2 : 1);
-                    x[i] &= h ? 0x0000FFFFu : 0xFFFF0000u;
-                    any = true;
-                  }
-                }
-              if (any) *q = make_uint4(x[0], x[1], x[2], x[3]);
+              // an exponent of ones carries into the sign's bit
+              auto ones = [](uint32_t u) { return (u & 0x7F807F80u) + 0x00800080u; };
+              if (((ones(x4.x) | ones(x4.y) | ones(x4.z) | ones(x4.w)) & 0x80008000u) == 0) continue;
+              uint16_t* e = reinterpret_cast<uint16_t*>(q);
+#pragma unroll 1
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t u = e[i];
+                if ((u & 0x7F80u) != 0x7F80u) continue;
+                note(key, c * 8 + i, (u & 0x7Fu) ? 0 : (u & 0x8000u) ? 2 : 1);
+                e[i] = 0;
+              }
             }
           }
           if (j >= edge0) fence_async();
@@ -711,12 +718,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         f = rowf[(one ? 0 : x * 128) + row];
       }
       // Probabilities are taken against a reference `ref` near the row's running
-      // maximum (2^(y - ref), y in log2 units): the first step's maximum, moved
-      // up after a step that went more than 8 past it, for the next one.  A step
-      // is read twice, its maximum first, only at the item's begin, for a row's
-      // first key that it sees, and where a score is more than 24 past `ref`
-      // (sums and O stay far inside 32 bits up to there).  So the maximum is not
-      // waited for, and few registers hold scores.
+      // maximum (2^(y - ref), y in log2 units): its first score's half step's
+      // maximum, moved up after a step that went more than 8 past it, for the
+      // next one.  Only where a row sees its first key, or a score is more than 24
+      // past `ref` (sums and O stay far inside 32 bits up to there), is a half
+      // step done again, and `ref` moves first: by a whole number, so that
+      // what P has of the step's first half scales exactly.  So the maximum is
+      // never waited for.
       float ref = 0.f, l = 0.f, alpha = 1.f;
       bool started = false, pend = false;  // a key seen; O to be scaled by alpha
       auto rescale = [&](float a) {
@@ -764,64 +772,69 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (key0 + 32 * c + k >= lim) s[k] = -INFINITY;
           }
         };
-        uint32_t pk[64];
-        float sum, top;
-        bool exact = i == 0;
-        for (;;) {
-          if (exact) {
-            float mx = -INFINITY;
+        float sum = 0.f, top = -INFINITY;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {  // 64 keys; few instructions, that they stay cached
+          uint32_t pk[32];
+          float hs, ht;
+          for (;;) {
+            float s[2][32];
+            tmem_ld32(ts + static_cast<uint32_t>(64 * h), s[0]);
+            tmem_ld_wait<32>(s[0]);
+            tmem_ld32(ts + static_cast<uint32_t>(64 * h + 32), s[1]);
+            float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              float s[32];
-              tmem_ld32(ts + static_cast<uint32_t>(32 * c), s);
-              tmem_ld_wait<32>(s);
-              finish(c, s);
+            for (int c = 0; c < 2; ++c) {
+              float* v = s[c];
+              finish(2 * h + c, v);
 #pragma unroll
-              for (int k = 0; k < 32; k += 2) mx = max3(mx, s[k], s[k + 1]);
+              for (int k = 0; k < 32; k += 4) {
+                fma2(v[k], v[k + 1], f, -ref);
+                fma2(v[k + 2], v[k + 3], f, -ref);
+                t0 = max3(t0, v[k], v[k + 1]);
+                t1 = max3(t1, v[k + 2], v[k + 3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k + e] = ex2(v[k + e]);
+                add2(a0, a1, v[k], v[k + 1]);
+                add2(b0, b1, v[k + 2], v[k + 3]);
+                pk[16 * c + k / 2] = bf16x2(v[k], v[k + 1]);
+                pk[16 * c + k / 2 + 1] = bf16x2(v[k + 2], v[k + 3]);
+              }
+              if (c == 0) tmem_ld_wait<32>(s[1]);
             }
-            mx *= f;
+            ht = fmaxf(t0, t1);
+            hs = (a0 + a1) + (b0 + b1);
+            // rows past the tile hold what memory held: they have no say
+            const bool again = valid && (started ? ht > 24.f : ht > -INFINITY);
+            if (!__any_sync(0xffffffffu, again)) break;
             float a = 1.f;
-            if (mx > -INFINITY && (!started || mx > ref)) {
-              if (started) a = ex2(ref - mx);
+            if (again) {
+              const float up = started ? ceilf(ht) : ht;
+              a = started ? ex2(-up) : 1.f;  // nothing to scale before a row's first key
+              ref += up;
               l *= a;
-              ref = mx;
+              sum *= a;
+              top -= up;
               started = true;
             }
-            if (i > 0 && __any_sync(0xffffffffu, valid && a != 1.f)) rescale(a);
-          }
-          float s[2][32];
-          tmem_ld32(ts, s[0]);
-          tmem_ld_wait<32>(s[0]);
-          float a0 = 0.f, a1 = 0.f, b0 = 0.f, b1 = 0.f, t0 = -INFINITY, t1 = -INFINITY;
+            if (__any_sync(0xffffffffu, a != 1.f)) {
+              if (i > 0) rescale(a);
+              if (h == 1) {  // P of the first half: in place, exactly
+                const uint32_t a2 = bf16x2(a, a);
+                float q[32];
+                tmem_ld32(ts, q);
+                tmem_ld_wait<32>(q);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float* v = s[c & 1];
-            if (c < 3) tmem_ld32(ts + static_cast<uint32_t>(32 * (c + 1)), s[(c + 1) & 1]);
-            finish(c, v);
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              fma2(v[k], v[k + 1], f, -ref);
-              fma2(v[k + 2], v[k + 3], f, -ref);
-              t0 = max3(t0, v[k], v[k + 1]);
-              t1 = max3(t1, v[k + 2], v[k + 3]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[k + e] = ex2(v[k + e]);
-              add2(a0, a1, v[k], v[k + 1]);
-              add2(b0, b1, v[k + 2], v[k + 3]);
-              pk[16 * c + k / 2] = bf16x2(v[k], v[k + 1]);
-              pk[16 * c + k / 2 + 1] = bf16x2(v[k + 2], v[k + 3]);
+                for (int k = 0; k < 32; ++k) pk[k] = mul_bf16x2(__float_as_uint(q[k]), a2);
+                tmem_st32(ts, pk);
+                tmem_st_wait();
+              }
             }
-            if (c < 3) tmem_ld_wait<32>(s[(c + 1) & 1]);
           }
-          top = fmaxf(t0, t1);
-          sum = (a0 + a1) + (b0 + b1);
-          // rows past the tile hold what memory held: they have no say
-          const bool again = valid && (top > 24.f || (!started && top > -INFINITY));
-          if (exact || !__any_sync(0xffffffffu, again)) break;
-          exact = true;
+          tmem_st32(ts + static_cast<uint32_t>(32 * h), pk);
+          sum += hs;
+          top = fmaxf(top, ht);
         }
-        tmem_st32(ts, pk);
-        tmem_st32(ts + 32u, pk + 32);
         l += sum;
         if (valid && top > 8.f && started) {
           alpha = ex2(-top);
@@ -874,6 +887,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  : (static_cast<long long>(w.part()) * p.part_rows + rr) * D;
       uint8_t* stage = smem + L::kQ + (one ? 0 : x * L::kTile) + (warp & 3) * 8192;
       const uint32_t live = __ballot_sync(0xffffffffu, valid && mine > 0 && !*abort);
+      // what a row sees of values that are not finite, added: infinities, or NaN
+      auto blot = [&](int d) {
+        float z = 0.f;
+        if (lim > badp[D + d]) z += INFINITY;
+        if (lim > badp[2 * D + d]) z -= INFINITY;
+        return lim > badp[d] ? NAN : z;
+      };
       // 16-byte pieces of 256-byte rows: piece c of row r at c ^ (r % 16)
       auto put = [&](int c, uint4 v) { *reinterpret_cast<uint4*>(stage + lane * 256 + ((c ^ (lane & 15)) << 4)) = v; };
       auto send = [&](auto&& to_global) {
@@ -886,11 +906,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
       };
-#pragma unroll
-      for (int hf = 0; hf < D / 64; ++hf) {
+#pragma unroll 1
+      for (int hf = 0; hf < D / 64; ++hf) {  // few instructions: they are fetched once an item
         if (one) {
           if (x == 1 && mine > 0) {
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < 64; c += 32) {
               float o[32];
               tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
@@ -904,7 +924,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           named_barrier(1, 256);
         }
         if ((!one || x == 0) && mine > 0) {
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < 64; c += 32) {
             float o[32];
             tmem_ld32(to + static_cast<uint32_t>(hf * 64 + c), o);
@@ -923,12 +943,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (any_bad) {
 #pragma unroll
-              for (int k = 0; k < 32; ++k) {
-                const int d = hf * 64 + c + k;
-                if (lim > badp[D + d]) o[k] += INFINITY;
-                if (lim > badp[2 * D + d]) o[k] -= INFINITY;
-                if (lim > badp[d]) o[k] = NAN;
-              }
+              for (int k = 0; k < 32; ++k) o[k] += blot(hf * 64 + c + k);
             }
             if (whole) {
 #pragma unroll
