@@ -16,16 +16,17 @@
 // D is free, as long as q and k share it: a lane takes its K in 16-byte pieces
 // as they lie in memory, without ldmatrix.
 //
-// 8-bit cache.  Scores: q is split into two e4m3 terms (its 8 significant bits
-// are 4 + 4; the row is scaled by a power of two so that its largest element
-// is in (224, 448], and elements below 2^-11 of that lose what is under 2^-19
-// of it), and both multiply the codes themselves (m16n8k32, whose sums are as
-// exact as those of bf16), so K needs no conversion; the key's scale, a power
-// of two, multiplies the score.  Values: codes become bf16 by moving their
-// bits (sign, then exponent and mantissa four lower: 2^-120 times the value)
-// and a bf16 multiplication by 2^120, exactly; the scale of a value's row
-// multiplies its probabilities, also exactly.
-// P is rounded to bf16, as the output is; its sum is of the unrounded values.
+// 8-bit cache.  Codes become f16, exactly and in one instruction a pair (an
+// e4m3 mma.sync is these conversions too, besides as many again for q).  q
+// becomes f16 after its row is scaled by a power of two so that its largest
+// element is in [2^14, 2^15): elements above 2^-29 of that are exact.  The key's
+// scale, a power of two, multiplies the score; that of a value's row multiplies
+// its probability, relative to the largest seen so far (a common power of two,
+// E0), so that the products stay in f16's range: at most 2^15, and to 2^-24 with
+// what f16's subnormals hold, 2^-39 of the largest.  O is multiplied by E0's
+// power at the end.
+// P is rounded to f16 (bf16 where the cache is); its sum is of the unrounded
+// values.
 //
 // The running maximum moves only when a score exceeds it by more than 8 (log2
 // units), so that exp2 stays below 256 and most chunks rescale nothing.
@@ -56,35 +57,30 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       "l"(src), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
-// D += A B, m16n8k32, e4m3 inputs, fp32 accumulators
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+// D += A B, m16n8k16, f16 inputs, fp32 accumulators
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// the values of four e4m3 codes, in pairs
+__device__ __forceinline__ void e4m3x4_f16(uint32_t c, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(c));
 }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// the two e4m3 codes of (x, y), y in the upper byte
-__device__ __forceinline__ uint32_t e4m3x2(float x, float y) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y), "f"(x));
-  return r;
-}
-__device__ __forceinline__ float2 e4m3x2_value(uint32_t c) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(c)));
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
 // 2^(e - 127) of an exponent byte
-__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(e > 0 ? e << 23 : 1u << 22); }
+__device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(max(e << 23, 1u << 22)); }
 
 // CTAs per SM: as many as registers and a ring of two chunks or more allow.
 constexpr int ctas_per_sm(bool e4m3, int mb) { return e4m3 && mb <= 2 ? 3 : 2; }
@@ -108,7 +104,8 @@ struct Map {
   static constexpr uint32_t kBad = kQ + kQSlots * T * kQRow;      // [3][D]
   static constexpr uint32_t kXl = kBad + 3 * D * 4;               // [2][4][T] sums of the warps
   static constexpr uint32_t kXm = kXl + 2 * 4 * T * 4;            // [4][T] maxima of the warps
-  static constexpr uint32_t kRowF = kXm + 4 * T * 4;              // [T] score factors of the rows
+  static constexpr uint32_t kXe = kXm + 4 * T * 4;                // [4] largest exponents of the warps
+  static constexpr uint32_t kRowF = kXe + 16;                     // [T] score factors of the rows
   static constexpr uint32_t kBar = kRowF + T * 4;
   static constexpr int kNBar = 2 * S + 2 * kQSlots;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
@@ -148,8 +145,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   constexpr int NJ = E4M3 ? D / 64 : D / 32;  // 16-byte pieces of a K row per lane
   constexpr int NB = E4M3 ? 1 : D / 64;       // boxes of 128-byte rows across D
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);  // an offset: accesses stay LDS and STS
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
   uint64_t* empty = full + S;
   uint64_t* qfull = empty + S;
@@ -271,6 +267,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   const int kb = warp * 16;  // this warp's keys of a chunk
   float* xm = reinterpret_cast<float*>(smem + L::kXm);
   float* xl = reinterpret_cast<float*>(smem + L::kXl);
+  [[maybe_unused]] int* xe = reinterpret_cast<int*>(smem + L::kXe);
   float* rowf = reinterpret_cast<float*>(smem + L::kRowF);
   int nchunk = 0;
   bool ok = true;
@@ -290,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     const int lim_hi = paged_limit(p, w.s, (m0 + rows - 1) / p.group);
     const int len = w.s.len;
     const int qs = pieces % L::kQSlots, par = pieces & 1;
+    [[maybe_unused]] int E0 = 0;  // exponent byte that values' scales are relative to
     uint8_t* qd = smem + L::kQ + qs * T * L::kQRow;
     Rows<MB> R;
 #pragma unroll
@@ -313,63 +311,50 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 
     ok = ok && mbar_wait(&qfull[qs], static_cast<uint32_t>(pieces / L::kQSlots) & 1u, p.limit_ns, abort);
     ok = __all_sync(0xffffffffu, ok);
-    // the codes of row r, element pieces (2 t4 + j) * 16: a0/a2 words of high
-    // and low terms; returns the row's power-of-two factor
-    auto split_row = [&](int r, uint32_t (&hi)[NJ][4], uint32_t (&lo)[NJ][4]) -> float {
+    // row r in f16: this lane's pieces of 16 elements, (NJ t4 + j) * 16 and on, as
+    // 8 words each; returns the row's score factor
+    auto f16_row = [&](int r, uint32_t (&y)[NJ][8]) -> float {
       const uint8_t* q = qd + r * L::kQRow;
-      uint4 x[NJ][2];
-      uint32_t amax = 0;
+      uint32_t x[NJ][8], amax = 0;
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          x[j][i] = *reinterpret_cast<const uint4*>(q + ((NJ * t4 + j) * 2 + i) * 16);
-          const uint32_t v[4] = {x[j][i].x, x[j][i].y, x[j][i].z, x[j][i].w};
+          const uint4 v = *reinterpret_cast<const uint4*>(q + ((NJ * t4 + j) * 2 + i) * 16);
+          x[j][4 * i] = v.x;
+          x[j][4 * i + 1] = v.y;
+          x[j][4 * i + 2] = v.z;
+          x[j][4 * i + 3] = v.w;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) amax = max(amax, max(v[k] & 0x7FFFu, (v[k] >> 16) & 0x7FFFu));
+          for (int k = 0; k < 4; ++k) amax = max(amax, max(x[j][4 * i + k] & 0x7FFFu, (x[j][4 * i + k] >> 16) & 0x7FFFu));
         }
       amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
       const bool finite = amax < 0x7F80u;
-      const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 127;
-      const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+      const uint32_t e = finite ? min(268u - (amax >> 7), 254u) : 127u;  // 2^(e - 127) * |largest| in [2^14, 2^15)
+      const float up = __uint_as_float(e << 23);
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t v[4] = {x[j][i].x, x[j][i].y, x[j][i].z, x[j][i].w};
-          uint32_t h2[4], l2[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float a = __uint_as_float(v[k] << 16) * inv, b = __uint_as_float(v[k] & 0xFFFF0000u) * inv;
-            h2[k] = e4m3x2(a, b);
-            const float2 hv = e4m3x2_value(h2[k]);
-            l2[k] = e4m3x2(a - hv.x, b - hv.y);
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            // a row with a value that is not finite has NaN scores
-            hi[j][2 * i + k] = finite ? (h2[2 * k] | (h2[2 * k + 1] << 16)) : 0x7F7F7F7Fu;
-            lo[j][2 * i + k] = l2[2 * k] | (l2[2 * k + 1] << 16);
-          }
+        for (int k = 0; k < 8; ++k) {
+          const float a = __uint_as_float(x[j][k] << 16) * up, b = __uint_as_float(x[j][k] & 0xFFFF0000u) * up;
+          y[j][k] = finite ? f16x2(a, b) : 0x7FFF7FFFu;  // a row with a value that is not finite has NaN scores
         }
-      return scale_value(static_cast<uint32_t>(e)) * p.scale_log2;
+      return scale_value(254u - e) * p.scale_log2;
     };
     // q fragments: of one row block in registers
-    uint32_t qa[MB == 1 ? (E4M3 ? 2 * NJ : NJ) : 1][2][4];  // [.. terms][row g, g + 8][4 words = 2 k-steps]
+    constexpr int QW = E4M3 ? 8 : 4;          // words of a piece of q
+    uint32_t qa[MB == 1 ? NJ : 1][2][QW];     // [piece][row g, g + 8]
     if constexpr (MB == 1) {
       if constexpr (E4M3) {
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
-          uint32_t a[NJ][4], b[NJ][4];
-          R.f[0][hi] = split_row(hi * 8 + g, a, b);
+          uint32_t y[NJ][8];
+          R.f[0][hi] = f16_row(hi * 8 + g, y);
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              qa[2 * j][hi][k] = a[j][k];
-              qa[2 * j + 1][hi][k] = b[j][k];
-            }
+            for (int k = 0; k < 8; ++k) qa[j][hi][k] = y[j][k];
         }
       } else {
 #pragma unroll
@@ -390,16 +375,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       // the warps share the rows, one per 4 lanes at a time, in place
 #pragma unroll
       for (int r0 = 0; r0 < T / 4; r0 += 8) {
-        uint32_t a[NJ][4], b[NJ][4];
+        uint32_t y[NJ][8];
         const int r = warp * (T / 4) + r0 + g;
-        const float f = split_row(r, a, b);
-        __syncwarp();
+        const float f = f16_row(r, y);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          uint8_t* q = qd + r * L::kQRow + (NJ * t4 + j) * 16;
-          *reinterpret_cast<uint4*>(q) = make_uint4(a[j][0], a[j][1], a[j][2], a[j][3]);
-          *reinterpret_cast<uint4*>(q + D) = make_uint4(b[j][0], b[j][1], b[j][2], b[j][3]);
-        }
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(qd + r * L::kQRow + ((NJ * t4 + j) * 2 + i) * 16) =
+                make_uint4(y[j][4 * i], y[j][4 * i + 1], y[j][4 * i + 2], y[j][4 * i + 3]);
         if (t4 == 0) rowf[r] = f;
       }
       named_barrier(1, 128);
@@ -416,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       float s[MB][2][4];
       ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
       ok = __all_sync(0xffffffffu, ok);
-      [[maybe_unused]] float vs[2][2];  // scales of the values' rows
+      [[maybe_unused]] uint32_t ve[2][2];  // exponents of the values' rows
       {
         const uint8_t* kd = smem + L::kRing + slot * L::kOp;
 #pragma unroll
@@ -440,39 +424,51 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
               at = (j >> 1) * 8192 + row * 128 + (((2 * t4 + (j & 1)) ^ g) << 4);
             kx[nt] = *reinterpret_cast<const uint4*>(kd + at);
           }
+          uint32_t kw[2][QW];  // K of the piece, in the words of q's type
 #pragma unroll
-          for (int mb = 0; mb < MB; ++mb)
+          for (int nt = 0; nt < 2; ++nt) {
+            const uint32_t u[4] = {kx[nt].x, kx[nt].y, kx[nt].z, kx[nt].w};
 #pragma unroll
-            for (int term = 0; term < (E4M3 ? 2 : 1); ++term) {
-              uint32_t x[2][4];  // rows g, g + 8
+            for (int k = 0; k < 4; ++k) {
+              if constexpr (E4M3)
+                e4m3x4_f16(u[k], kw[nt][2 * k], kw[nt][2 * k + 1]);
+              else
+                kw[nt][k] = u[k];
+            }
+          }
 #pragma unroll
-              for (int hi = 0; hi < 2; ++hi) {
-                if constexpr (MB == 1) {
+          for (int mb = 0; mb < MB; ++mb) {
+            uint32_t x[2][QW];  // rows g, g + 8
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) x[hi][k] = qa[E4M3 ? 2 * j + term : j][hi][k];
-                } else {
-                  const uint8_t* q = qd + (mb * 16 + hi * 8 + g) * L::kQRow;
+            for (int hi = 0; hi < 2; ++hi) {
+              if constexpr (MB == 1) {
+#pragma unroll
+                for (int k = 0; k < QW; ++k) x[hi][k] = qa[j][hi][k];
+              } else {
+                const uint8_t* q = qd + (mb * 16 + hi * 8 + g) * L::kQRow;
+#pragma unroll
+                for (int i = 0; i < QW / 4; ++i) {
                   const uint4 v = *reinterpret_cast<const uint4*>(
-                      q + (E4M3 ? term * D + (NJ * t4 + j) * 16 : ((j >> 1) * 8 + 2 * t4 + (j & 1)) * 16));
-                  x[hi][0] = v.x;
-                  x[hi][1] = v.y;
-                  x[hi][2] = v.z;
-                  x[hi][3] = v.w;
-                }
-              }
-              const uint32_t a0[4] = {x[0][0], x[1][0], x[0][1], x[1][1]};
-              const uint32_t a1[4] = {x[0][2], x[1][2], x[0][3], x[1][3]};
-#pragma unroll
-              for (int nt = 0; nt < 2; ++nt) {
-                if constexpr (E4M3) {
-                  mma_e4m3(s[mb][nt], a0, kx[nt].x, kx[nt].y);
-                  mma_e4m3(s[mb][nt], a1, kx[nt].z, kx[nt].w);
-                } else {
-                  mma_bf16(s[mb][nt], a0, kx[nt].x, kx[nt].y);
-                  mma_bf16(s[mb][nt], a1, kx[nt].z, kx[nt].w);
+                      q + (E4M3 ? (NJ * t4 + j) * 2 + i : (j >> 1) * 8 + 2 * t4 + (j & 1)) * 16);
+                  x[hi][4 * i] = v.x;
+                  x[hi][4 * i + 1] = v.y;
+                  x[hi][4 * i + 2] = v.z;
+                  x[hi][4 * i + 3] = v.w;
                 }
               }
             }
+#pragma unroll
+            for (int k = 0; k < QW; k += 2) {
+              const uint32_t a[4] = {x[0][k], x[1][k], x[0][k + 1], x[1][k + 1]};
+#pragma unroll
+              for (int nt = 0; nt < 2; ++nt) {
+                if constexpr (E4M3)
+                  mma_f16(s[mb][nt], a, kw[nt][k], kw[nt][k + 1]);
+                else
+                  mma_bf16(s[mb][nt], a, kw[nt][k], kw[nt][k + 1]);
+              }
+            }
+          }
         }
         if constexpr (E4M3) {
           const uint8_t* sc = smem + L::kScale + slot * 64 + kb;
@@ -511,16 +507,29 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
           const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
-          // a row that is NaN: its codes do not say so to P V
-          vs[nt][0] = (two & 0xFFu) == 0xFFu ? NAN : scale_value(two & 0xFFu);
-          vs[nt][1] = (two >> 8) == 0xFFu ? NAN : scale_value(two >> 8);
+          ve[nt][0] = two & 0xFFu;
+          ve[nt][1] = two >> 8;
+          if constexpr (EDGE) {  // past what is seen nothing is known of them
+            if (key0 + kb + nt * 8 + 2 * t4 >= lim_hi) ve[nt][0] = 0u;
+            if (key0 + kb + nt * 8 + 2 * t4 + 1 >= lim_hi) ve[nt][1] = 0u;
+          }
         }
       }
+      auto value_scale = [&](uint32_t e) {  // a row that is NaN: its codes do not say so to P V
+        return e == 255u ? NAN : __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(e) - E0 + 127, 0)) << 23);
+      };
       uint8_t* pd = smem + L::kP + (nchunk & 1) * T * 128;
       // probabilities against the running maxima, into shared memory; the
       // largest log2 of them
-      auto put_p = [&](bool sum) {
+      auto put_p = [&]() {
         float top = -INFINITY;
+        [[maybe_unused]] float vs[2][2];
+        if constexpr (E4M3) {
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) vs[nt][e] = value_scale(ve[nt][e]);
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -531,14 +540,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
               const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -R.sub[mb][hi]);
               top = fmaxf(top, fmaxf(y0, y1));
               float e0 = ex2(y0), e1 = ex2(y1);
-              if (sum) R.l[mb][hi] += e0 + e1;
+              R.l[mb][hi] += e0 + e1;
               if constexpr (E4M3) {
                 // what a row does not see stays out, whatever its scale is
                 e0 = EDGE && s[mb][nt][2 * hi] == -INFINITY ? 0.f : e0 * vs[nt][0];
                 e1 = EDGE && s[mb][nt][2 * hi + 1] == -INFINITY ? 0.f : e1 * vs[nt][1];
               }
               const int r = mb * 16 + hi * 8 + g;
-              *reinterpret_cast<uint32_t*>(pd + r * 128 + (((2 * warp + nt) ^ g) << 4) + t4 * 4) = bf16x2(e0, e1);
+              *reinterpret_cast<uint32_t*>(pd + r * 128 + (((2 * warp + nt) ^ g) << 4) + t4 * 4) =
+                  E4M3 ? f16x2(e0, e1) : bf16x2(e0, e1);
             }
         return top;
       };
@@ -548,9 +558,20 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) l0[mb][hi] = R.l[mb][hi];
       bool raise = fresh;
-      if (!fresh) raise = put_p(true) > 8.f;
+      [[maybe_unused]] int emax = 0;
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) emax = max(emax, ve[nt][e] == 255u ? 0 : static_cast<int>(ve[nt][e]));
+      }
+      if (!fresh) raise = put_p() > 8.f || (E4M3 && emax > E0 + 7);
       if (barrier_or(1, 128, raise)) {
-        // new running maxima, of all warps' scores
+        // new running maxima, of all warps' scores, and E0
+        if constexpr (E4M3) {
+          const int top_e = __reduce_max_sync(0xffffffffu, emax);
+          if (lane == 0) xe[warp] = top_e;
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -565,6 +586,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
             if (t4 == 0) xm[warp * T + mb * 16 + hi * 8 + g] = x;
           }
         named_barrier(1, 128);
+        float down = 1.f;
+        if constexpr (E4M3) {
+          const int e = max(max(max(xe[0], xe[1]), max(xe[2], xe[3])), E0);
+          down = __uint_as_float(static_cast<uint32_t>(max(E0 - e + 127, 0)) << 23);
+          E0 = e;
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
@@ -577,11 +604,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
             R.l[mb][hi] = l0[mb][hi] * alpha;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-              o[mb][j][2 * hi] *= alpha;
-              o[mb][j][2 * hi + 1] *= alpha;
+              o[mb][j][2 * hi] *= alpha * down;
+              o[mb][j][2 * hi + 1] *= alpha * down;
             }
           }
-        put_p(true);
+        put_p();
         named_barrier(1, 128);
       }
       ++nchunk;
@@ -620,6 +647,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
                 v[nt][e] = *reinterpret_cast<const uint16_t*>(vd + row * 64 + d);
               if constexpr (EDGE) {
                 const int key = key0 + row;
+                // codes of a NaN row: the probabilities say it, where the row is seen
+                const uint32_t nan = ((v[nt][e] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+                v[nt][e] &= ~((nan >> 7) * 0xFFu);
                 if (key >= len) v[nt][e] = 0u;
               }
             }
@@ -627,18 +657,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           for (int hf = 0; hf < NT / 2; ++hf) {
             uint32_t b[2][2];  // [column tile 2 hf + .][nt]
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-              // bytes (key 0, d), (key 0, d + 1), (key 1, d), (key 1, d + 1)
-              const uint32_t x = __byte_perm(v[nt][0], v[nt][1], hf ? 0x7632 : 0x5410);
-              const uint32_t d1 = (x & 0x80008000u) | ((x >> 4) & 0x07F007F0u);
-              const uint32_t d0 = ((x << 8) & 0x80008000u) | ((x << 4) & 0x07F007F0u);
-              b[0][nt] = mul_bf16x2(d0, 0x7B807B80u);  // 2^120
-              b[1][nt] = mul_bf16x2(d1, 0x7B807B80u);
-            }
+            for (int nt = 0; nt < 2; ++nt)  // bytes (key 0, d), (key 1, d), (key 0, d + 1), (key 1, d + 1)
+              e4m3x4_f16(__byte_perm(v[nt][0], v[nt][1], hf ? 0x7362 : 0x5140), b[0][nt], b[1][nt]);
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-              for (int mb = 0; mb < MB; ++mb) mma_bf16(o[mb][2 * hf + q], a[mb], b[q][0], b[q][1]);
+              for (int mb = 0; mb < MB; ++mb) mma_f16(o[mb][2 * hf + q], a[mb], b[q][0], b[q][1]);
           }
         } else {
           const uint32_t vb = smem_u32(vd);
@@ -719,7 +743,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           const int r = mb * 16 + hi * 8 + g;
           if (r >= rows) continue;
           const float l = (wl[r] + wl[T + r]) + (wl[2 * T + r] + wl[3 * T + r]);
-          const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
           // this lane's elements of the row: an 8-bit cache's NT columns of
           // fragment column 2 t4, then those of 2 t4 + 1, which follow on
           // them; a bf16 cache's columns 2 t4 and 2 t4 + 1 of each tile
@@ -727,7 +751,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) x[E4M3 ? e * NT + j : 2 * j + e] = o[mb][j][2 * hi + e] * inv;
+            for (int e = 0; e < 2; ++e) {
+              // an 8-bit cache's O is relative to E0 (two factors: each in range)
+              const float z = E4M3 ? o[mb][j][2 * hi + e] * scale_value(static_cast<uint32_t>(E0)) : o[mb][j][2 * hi + e];
+              x[E4M3 ? e * NT + j : 2 * j + e] = z * inv;
+            }
           if (any_bad) {
             const int lim = R.lim[mb][hi];
 #pragma unroll

@@ -205,8 +205,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using L = Map<D, E4M3>;
   constexpr int NB = L::NB;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                             ~static_cast<uintptr_t>(1023));
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);  // an offset: accesses stay LDS and STS
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBar);
   uint64_t* kfull = bars;
   uint64_t* kempty = kfull + L::kKs;
