@@ -1681,6 +1681,7 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
     return fail(h, EBD_ERR_INVALID_ARG, "q_stride must be 0, or a row or more and a multiple of 8");
   if (a->causal != 0 && a->causal != 1) return fail(h, EBD_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (a->max_new < 0) return fail(h, EBD_ERR_INVALID_ARG, "max_new must not be negative");
+  if (f.n_heads_q / f.n_heads_kv > 1024) return fail(h, EBD_ERR_UNSUPPORTED, "more than 1024 query heads per K/V head");
   if (!(a->scale >= 0.f) || std::isinf(a->scale)) return fail(h, EBD_ERR_INVALID_ARG, "scale must be finite and not negative");
   PagedParams p{};
   p.B = a->batch;
@@ -1688,10 +1689,13 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   p.Hq = f.n_heads_q;
   p.Hkv = f.n_heads_kv;
   p.group = f.n_heads_q / f.n_heads_kv;
+  p.group_inv = static_cast<unsigned>((0x100000000ull + p.group - 1) / p.group);
   p.causal = a->causal;
   p.page_log2 = log2_of(c->page_size);
   p.n_pages = c->n_pages;
   p.max_pages = c->max_pages;
+  const int64_t cap = static_cast<int64_t>(c->max_pages) * c->page_size;
+  p.cap = cap < 0x7fffffff ? static_cast<int>(cap) : 0x7fffffff;
   const float scale = a->scale != 0.f ? a->scale : 1.f / std::sqrt(static_cast<float>(f.head_dim));
   p.scale_log2 = scale * 1.4426950408889634f;
   p.cu_rows = a->cu_rows;
@@ -1714,7 +1718,10 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   const int64_t m = longest * p.group;
   const bool e4m3 = c->dtype == EBD_KV_E4M3;
   const bool wide = f.head_dim == 128 && p.group <= kPagedTcGroup && m > 64;
-  p.box_log2 = wide ? (p.page_log2 < 7 ? p.page_log2 : 7) : p.page_log2 < 6 ? p.page_log2 : 6;
+  // keys of a tensor-map box: a page, or a chunk's part of it
+  const int mb = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+  const int chunk_log2 = log2_of(wide ? 128 : paged_chunk_keys(e4m3, mb));
+  p.box_log2 = p.page_log2 < chunk_log2 ? p.page_log2 : chunk_log2;
   p.part_rows = wide ? kPagedTcRows : kPagedRows;
   // tiles stay whole where none can have many chunks (64 keys, or 128 in the tcgen05 kernel)
   p.uncut = static_cast<int64_t>(c->max_pages) * c->page_size <= kPagedUncutKeys ? 1 : 0;
@@ -1722,7 +1729,6 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   if (!encode_pool(&tk, c->k, h, c, 1 << p.box_log2) || !encode_pool(&tv, c->v, h, c, 1 << p.box_log2))
     return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (pages) failed");
   cudaError_t e;
-  const int mb = m <= 16 ? 1 : m <= 32 ? 2 : 4;
   if (wide) {
     // q as (element, head, row), in boxes of the group's heads of as many rows as a tile of 128 holds
     const uint64_t dims[3] = {static_cast<uint64_t>(f.head_dim), static_cast<uint64_t>(f.n_heads_q),

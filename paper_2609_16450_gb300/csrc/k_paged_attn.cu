@@ -4,10 +4,10 @@
 //
 // A tile is up to 16, 32 or 64 packed rows (row of the sequence, query head of
 // the group) of one sequence and K/V head.  Each CTA takes an equal share of
-// all tiles' 64-key chunks (paged.h).
+// all tiles' chunks of 64 keys, or 128 of an 8-bit cache (paged.h).
 //   warp 4: loads.  The rows of q, and per chunk K and V as TMA boxes of a
-//     page (or 64 keys of it), each operand into a slot of one ring.
-//   warps 0-3: the scores of 16 keys of every chunk each; the probabilities
+//     page (or a chunk's part of it), each operand into a slot of one ring.
+//   warps 0-3: the scores of a quarter of every chunk's keys each; the probabilities
 //     meet in shared memory, and each warp multiplies all of them with D / 4
 //     columns of V.  A warp's output is then D / 4 columns, not D, which keeps
 //     a tile of 32 rows within the registers of two or three CTAs per SM, and
@@ -40,9 +40,8 @@ namespace ebd {
 
 namespace {
 
-constexpr int kCH = 64;             // keys of a chunk
 constexpr int kThreads = 160;
-constexpr int kLeast = 3;           // chunks of a share, at least
+constexpr int kLeastKeys = 192;     // keys of a share, at least
 constexpr int kNever = 0x7fffffff;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -57,12 +56,17 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       "l"(src), "r"(bytes), "r"(smem_u32(bar))
       : "memory");
 }
-// D += A B, m16n8k16, f16 inputs, fp32 accumulators
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// D += A B, m16n8k16, f16 (bf16) inputs, fp32 accumulators
+template <bool F16>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (F16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t r;
@@ -84,43 +88,46 @@ __device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_floa
 
 // CTAs per SM: as many as registers and a ring of two chunks or more allow.
 constexpr int ctas_per_sm(bool e4m3, int mb) { return e4m3 && mb <= 2 ? 3 : 2; }
+// q's fragments of one row block stay in registers
+constexpr bool q_in_registers(bool e4m3, int mb) { return mb == 1; }
 
 // Shared memory (offsets from a 1024-byte aligned base).
 template <int D, bool E4M3, int MB>
 struct Map {
   static constexpr int T = 16 * MB;                               // tile rows
-  static constexpr uint32_t kOp = kCH * D * (E4M3 ? 1 : 2);       // K or V of a chunk
+  static constexpr int CH = paged_chunk_keys(E4M3, MB);
+  static constexpr uint32_t kOp = CH * D * (E4M3 ? 1 : 2);       // K or V of a chunk
   static constexpr uint32_t kQRow = 2 * D + 16;                   // padded: rows in distinct banks
-  static constexpr int kQSlots = MB == 2 ? 2 : 1;                 // one row block keeps q in registers
+  static constexpr uint32_t kFrag = q_in_registers(E4M3, MB) ? 0 : T * 2 * D;  // q as fragments
   static constexpr uint32_t kAll = (ctas_per_sm(E4M3, MB) == 3 ? 75 : 113) * 1024 - 1024;
-  static constexpr uint32_t kFixed = kQSlots * T * kQRow + 2 * T * 128 + 3 * D * 4 + 2 * 4 * T * 4 + 4 * T * 4 +
-                                     T * 4 + 512;
-  static constexpr uint32_t kSlotBytes = kOp + (E4M3 ? 64 : 0) + 16;
+  static constexpr uint32_t kFixed = T * kQRow + kFrag + 4 * T * CH + 3 * D * 4 + 2 * 4 * T * 4 + 4 * T * 4 +
+                                     T * 4 + 640;
+  static constexpr uint32_t kSlotBytes = kOp + (E4M3 ? CH : 0) + 16;
   static constexpr int S = (kAll - kFixed) / kSlotBytes > 16 ? 16 : (kAll - kFixed) / kSlotBytes;  // ring slots
   static constexpr uint32_t kRing = 0;
-  static constexpr uint32_t kP = kRing + S * kOp;                 // [2][T][128 B]: P of a chunk
-  static constexpr uint32_t kScale = kP + 2 * T * 128;
-  static constexpr uint32_t kQ = kScale + S * (E4M3 ? 64 : 0);
-  static constexpr uint32_t kBad = kQ + kQSlots * T * kQRow;      // [3][D]
+  static constexpr uint32_t kP = kRing + S * kOp;                 // [2][64-key blocks][T][128 B]: P of a chunk
+  static constexpr uint32_t kScale = kP + 4 * T * CH;
+  static constexpr uint32_t kQ = kScale + S * (E4M3 ? CH : 0);
+  static constexpr uint32_t kQF = kQ + T * kQRow;                 // [MB][D / 16][32 lanes][16 B]
+  static constexpr uint32_t kBad = kQF + kFrag;                   // [3][D]
   static constexpr uint32_t kXl = kBad + 3 * D * 4;               // [2][4][T] sums of the warps
   static constexpr uint32_t kXm = kXl + 2 * 4 * T * 4;            // [4][T] maxima of the warps
   static constexpr uint32_t kXe = kXm + 4 * T * 4;                // [4] largest exponents of the warps
   static constexpr uint32_t kRowF = kXe + 16;                     // [T] score factors of the rows
   static constexpr uint32_t kBar = kRowF + T * 4;
-  static constexpr int kNBar = 2 * S + 2 * kQSlots;
+  static constexpr int kNBar = 2 * S + 2;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
-  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32 + 1) * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + 2 * (kThreads / 32) * 8;
   static constexpr uint32_t kBytes = kMisc + 16;
   static constexpr uint32_t kDyn = kBytes + 1024;
-  static_assert(S >= 4 && kBytes <= kAll && (kP % 1024) == 0 && (kQ % 16) == 0, "shared memory");
+  static_assert(S >= 3 && kBytes <= kAll && (kP % 1024) == 0 && (kQ % 16) == 0, "shared memory");
 };
 
 // What the chunks of a piece need: constant over a piece, or carried along.
 template <int MB>
 struct Rows {
-  int lim[MB][2];     // keys before this one are seen by rows g and g + 8 of each block
-  float f[MB][2];     // score factor
-  float m[MB][2], sub[MB][2];  // running maximum, and what is subtracted (0 while -inf)
+  float f[MB][2];     // score factor of rows g and g + 8 of each block
+  float m[MB][2];     // running maximum
   float l[MB][2];     // sum of this lane's probabilities
 };
 
@@ -140,7 +147,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     paged_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                       const PagedParams p) {
   using L = Map<D, E4M3, MB>;
-  constexpr int T = L::T, S = L::S;
+  constexpr int T = L::T, S = L::S, CH = L::CH;
+  constexpr int NK = CH / 32;                 // key tiles of a warp
   constexpr int NT = D / 32;                  // output column tiles of a warp
   constexpr int NJ = E4M3 ? D / 64 : D / 32;  // 16-byte pieces of a K row per lane
   constexpr int NB = E4M3 ? 1 : D / 64;       // boxes of 128-byte rows across D
@@ -149,9 +157,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
   uint64_t* empty = full + S;
   uint64_t* qfull = empty + S;
-  uint64_t* qempty = qfull + L::kQSlots;
+  uint64_t* qempty = qfull + 1;
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
-  auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
+  auto& scan = *reinterpret_cast<unsigned long long(*)[2][kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
   volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc);
   int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 8);
   int* bad = reinterpret_cast<int*>(smem + L::kBad);
@@ -162,48 +170,46 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       mbar_init(&full[s], 1);
       mbar_init(&empty[s], 4);
     }
-    for (int s = 0; s < L::kQSlots; ++s) {
-      mbar_init(&qfull[s], 1);
-      mbar_init(&qempty[s], 4);
-    }
+    mbar_init(qfull, 1);
+    mbar_init(qempty, 4);
     *abort = 0;
     *s_bad = 0;
     fence_mbar_init();
   }
   for (int i = tid; i < 3 * D; i += kThreads) bad[i] = kNever;
-  paged_plan<kThreads>(p, T, kCH, kLeast, plan, scan);
+  paged_plan<kThreads>(p, T, CH, kLeastKeys / CH, plan, scan);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (tid == kThreads - 1) paged_cut(p, *plan, T, kCH);
-  PagedWalk w;
-  if (!w.begin(p, *plan, T, kCH)) return;
+  PagedWalk<T, CH> w;
+  if (!w.begin(p, *plan, T)) {
+    if (tid == 0) p.cuts[blockIdx.x] = PagedCut{};
+    return;
+  }
 
   if (warp == 4) {
     // ------------------------------------------------------------ loads
-    const int np_log = 6 - p.box_log2, box = 1 << p.box_log2;
+    const int np_log = (CH == 128 ? 7 : 6) - p.box_log2, box = 1 << p.box_log2;
     const int pc = lane & ((1 << np_log) - 1), part = lane >> np_log;
     const int key_in = pc << p.box_log2;
     int n = 0, pieces = 0;
     bool ok = true;
     do {
-      const int last = min(w.s.n - 1, (w.t * T + T - 1) / p.group);
+      const int last = min(w.s.n - 1, paged_row(p, w.t * T + T - 1));
       const int rows = min(T, w.s.n * p.group - w.t * T);
       {  // q: rows by lane, zeros past the tile's last
-        const int qs = pieces % L::kQSlots;
-        uint8_t* qd = smem + L::kQ + qs * T * L::kQRow;
-        ok = pieces < L::kQSlots ||
-             mbar_wait(&qempty[qs], static_cast<uint32_t>(pieces / L::kQSlots - 1) & 1u, p.limit_ns, abort);
+        uint8_t* qd = smem + L::kQ;
+        ok = pieces == 0 || mbar_wait(qempty, static_cast<uint32_t>(pieces - 1) & 1u, p.limit_ns, abort);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         for (int i = rows * (D / 8) + lane; i < T * (D / 8); i += 32)
           *reinterpret_cast<uint4*>(qd + (i / (D / 8)) * L::kQRow + (i % (D / 8)) * 16) = make_uint4(0u, 0u, 0u, 0u);
         fence_async();
         __syncwarp();
-        if (lane == 0) mbar_arrive_expect_tx(&qfull[qs], static_cast<uint32_t>(rows) * D * 2);
+        if (lane == 0) mbar_arrive_expect_tx(qfull, static_cast<uint32_t>(rows) * D * 2);
         __syncwarp();
         for (int r = lane; r < rows; r += 32) {
-          const int m = w.t * T + r, i = m / p.group, hl = m - i * p.group;
+          const int m = w.t * T + r, i = paged_row(p, m), hl = m - i * p.group;
           bulk_load(qd + r * L::kQRow,
-                    p.q + (w.s.r0 + i) * p.q_stride + static_cast<long long>(w.h * p.group + hl) * D, D * 2, &qfull[qs]);
+                    p.q + (w.s.r0 + i) * p.q_stride + static_cast<long long>(w.h * p.group + hl) * D, D * 2, qfull);
         }
         ++pieces;
       }
@@ -211,8 +217,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
       int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
       for (int c = w.c0; c < w.c1 && ok; ++c) {
-        const int key = c * kCH + key_in;
-        const int first = (c * kCH) >> p.page_log2;
+        const int key = c * CH + key_in;
+        const int first = (c * CH) >> p.page_log2;
         if (first >= win0 + 32 || first < win0) {
           win0 = first & ~31;
           win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
@@ -223,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           atomicCAS(p.status, 0, EBD_ERR_BOUNDS);
           page = 0;
         }
-        const int pieces_here = min(max((lim - c * kCH + box - 1) >> p.box_log2, 0), 1 << np_log);
+        const int pieces_here = min(max((lim - c * CH + box - 1) >> p.box_log2, 0), 1 << np_log);
         const uint32_t bytes = static_cast<uint32_t>(pieces_here) * box * (E4M3 ? D + 1 : 2 * D);
         const int off = key & ((1 << p.page_log2) - 1);
 #pragma unroll
@@ -237,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           if (mine) {
             uint8_t* d = smem + L::kRing + s * L::kOp;
             if (E4M3 && part == 1)
-              bulk_load(smem + L::kScale + s * 64 + key_in,
+              bulk_load(smem + L::kScale + s * CH + key_in,
                         (v ? p.v_scale : p.k_scale) +
                             ((static_cast<long long>(page) * p.Hkv + w.h) << p.page_log2) + off,
                         box, &full[s]);
@@ -247,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           }
         }
       }
+      if (lane == 0 && w.u + (w.c1 - w.c0) >= w.u1) w.leave(p, *plan);
     } while (ok && w.next(p));
     if (!ok) {
       if (lane == 0 && !*abort) {
@@ -256,51 +263,59 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       // the copies in flight land before the CTA can exit
       for (int j = max(0, n - S); j < n; ++j)
         mbar_wait(&full[j % S], static_cast<uint32_t>(j / S) & 1u, p.limit_ns, nullptr);
-      for (int j = max(0, pieces - L::kQSlots); j < pieces; ++j)
-        mbar_wait(&qfull[j % L::kQSlots], static_cast<uint32_t>(j / L::kQSlots) & 1u, p.limit_ns, nullptr);
+      if (pieces > 0) mbar_wait(qfull, static_cast<uint32_t>(pieces - 1) & 1u, p.limit_ns, nullptr);
     }
     return;
   }
 
   // -------------------------------------------------------------- products
   const int g = lane >> 2, t4 = lane & 3;
-  const int kb = warp * 16;  // this warp's keys of a chunk
+  const int kb = warp * (CH / 4);  // this warp's keys of a chunk
   float* xm = reinterpret_cast<float*>(smem + L::kXm);
   float* xl = reinterpret_cast<float*>(smem + L::kXl);
   [[maybe_unused]] int* xe = reinterpret_cast<int*>(smem + L::kXe);
   float* rowf = reinterpret_cast<float*>(smem + L::kRowF);
   int nchunk = 0;
   bool ok = true;
-  int slot = 0, pieces = 0;
-  uint32_t phase = 0;
-  auto step = [&]() {
-    if (++slot == S) {
-      slot = 0;
+  int pieces = 0;
+  // ring slots of the next K and the next V; they take turns in the ring
+  int kslot = 0, vslot = 1;
+  uint32_t kphase = 0, vphase = 0;
+  auto step = [](int& slot, uint32_t& phase) {
+    slot += 2;
+    if (slot >= S) {
+      slot -= S;
       phase ^= 1u;
     }
+  };
+  auto landed = [&](int slot, uint32_t phase) {
+    ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
+    ok = __all_sync(0xffffffffu, ok);
   };
   do {
     const int m0 = w.t * T;
     const int mtot = w.s.n * p.group;
     const int rows = min(T, mtot - m0);
-    const int lim_lo = paged_limit(p, w.s, m0 / p.group);
-    const int lim_hi = paged_limit(p, w.s, (m0 + rows - 1) / p.group);
+    const int lim_lo = paged_limit(p, w.s, paged_row(p, m0));
+    const int lim_hi = paged_limit(p, w.s, paged_row(p, m0 + rows - 1));
     const int len = w.s.len;
-    const int qs = pieces % L::kQSlots, par = pieces & 1;
+    const int par = pieces & 1;
     [[maybe_unused]] int E0 = 0;  // exponent byte that values' scales are relative to
-    uint8_t* qd = smem + L::kQ + qs * T * L::kQRow;
+    const uint8_t* qd = smem + L::kQ;
     Rows<MB> R;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
       for (int hi = 0; hi < 2; ++hi) {
-        const int m = m0 + mb * 16 + hi * 8 + g;
-        R.lim[mb][hi] = m < mtot ? paged_limit(p, w.s, m / p.group) : kNever;
         R.f[mb][hi] = p.scale_log2;
         R.m[mb][hi] = -INFINITY;
-        R.sub[mb][hi] = 0.f;
         R.l[mb][hi] = 0.f;
       }
+    // keys before this one are seen by row hi * 8 + g of block mb
+    auto limit = [&](int mb, int hi) {
+      const int m = m0 + mb * 16 + hi * 8 + g;
+      return m < mtot ? paged_limit(p, w.s, paged_row(p, m)) : kNever;
+    };
     float o[MB][NT][4];
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
@@ -309,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[mb][j][i] = 0.f;
 
-    ok = ok && mbar_wait(&qfull[qs], static_cast<uint32_t>(pieces / L::kQSlots) & 1u, p.limit_ns, abort);
+    ok = ok && mbar_wait(qfull, static_cast<uint32_t>(pieces) & 1u, p.limit_ns, abort);
     ok = __all_sync(0xffffffffu, ok);
     // row r in f16: this lane's pieces of 16 elements, (NJ t4 + j) * 16 and on, as
     // 8 words each; returns the row's score factor
@@ -342,50 +357,58 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         }
       return scale_value(254u - e) * p.scale_log2;
     };
-    // q fragments: of one row block in registers
-    constexpr int QW = E4M3 ? 8 : 4;          // words of a piece of q
-    uint32_t qa[MB == 1 ? NJ : 1][2][QW];     // [piece][row g, g + 8]
-    if constexpr (MB == 1) {
+    // q as fragments: word pairs (2 i, 2 i + 1) of a row's pieces are A registers
+    // hi and 2 + hi of contraction step i, in registers or shared memory
+    constexpr int QW = E4M3 ? 8 : 4;  // words of a piece of q
+    constexpr int KS = D / 16;        // contraction steps: QW / 2 per piece
+    constexpr bool QREG = q_in_registers(E4M3, MB);
+    uint32_t qa[QREG ? KS : 1][4];
+    auto row_words = [&](int r, uint32_t (&y)[NJ][QW]) -> float {
       if constexpr (E4M3) {
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-          uint32_t y[NJ][8];
-          R.f[0][hi] = f16_row(hi * 8 + g, y);
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) qa[j][hi][k] = y[j][k];
-        }
+        return f16_row(r, y);
       } else {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int j = 0; j < NJ; ++j) {
+          const uint4 x = *reinterpret_cast<const uint4*>(qd + r * L::kQRow + ((j >> 1) * 8 + 2 * t4 + (j & 1)) * 16);
+          y[j][0] = x.x;
+          y[j][1] = x.y;
+          y[j][2] = x.z;
+          y[j][3] = x.w;
+        }
+        return p.scale_log2;
+      }
+    };
+    if constexpr (QREG) {
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            const uint4 x = *reinterpret_cast<const uint4*>(qd + (hi * 8 + g) * L::kQRow +
-                                                            ((j >> 1) * 8 + 2 * t4 + (j & 1)) * 16);
-            qa[j][hi][0] = x.x;
-            qa[j][hi][1] = x.y;
-            qa[j][hi][2] = x.z;
-            qa[j][hi][3] = x.w;
-          }
+      for (int hi = 0; hi < 2; ++hi) {
+        uint32_t y[NJ][QW];
+        R.f[0][hi] = row_words(hi * 8 + g, y);
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          qa[i][hi] = y[i / (QW / 2)][2 * (i % (QW / 2))];
+          qa[i][2 + hi] = y[i / (QW / 2)][2 * (i % (QW / 2)) + 1];
+        }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&qempty[qs]);
-    } else if constexpr (E4M3) {
-      // the warps share the rows, one per 4 lanes at a time, in place
+      if (lane == 0) mbar_arrive(qempty);
+    } else {
+      // the warps share the rows, one per 4 lanes at a time
 #pragma unroll
-      for (int r0 = 0; r0 < T / 4; r0 += 8) {
-        uint32_t y[NJ][8];
-        const int r = warp * (T / 4) + r0 + g;
-        const float f = f16_row(r, y);
+      for (int r0 = 0; r0 < (MB == 1 ? 8 : T / 4); r0 += 8) {
+        if (MB == 1 && warp > 1) break;
+        uint32_t y[NJ][QW];
+        const int r = (MB == 1 ? warp * 8 : warp * (T / 4) + r0) + g;
+        const float f = row_words(r, y);
+        uint32_t* qf = reinterpret_cast<uint32_t*>(smem + L::kQF) + ((r >> 4) * KS * 32 + (r & 7) * 4 + t4) * 4 + ((r >> 3) & 1);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<uint4*>(qd + r * L::kQRow + ((NJ * t4 + j) * 2 + i) * 16) =
-                make_uint4(y[j][4 * i], y[j][4 * i + 1], y[j][4 * i + 2], y[j][4 * i + 3]);
+        for (int i = 0; i < KS; ++i) {
+          qf[i * 128] = y[i / (QW / 2)][2 * (i % (QW / 2))];
+          qf[i * 128 + 2] = y[i / (QW / 2)][2 * (i % (QW / 2)) + 1];
+        }
         if (t4 == 0) rowf[r] = f;
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(qempty);
       named_barrier(1, 128);
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb)
@@ -393,119 +416,106 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         for (int hi = 0; hi < 2; ++hi) R.f[mb][hi] = rowf[mb * 16 + hi * 8 + g];
     }
 
-    // one chunk: EDGE where a key of it is past some row's limit
-    auto chunk = [&](int c, auto edge_c, bool fresh) {
-      constexpr bool EDGE = decltype(edge_c)::value;
-      const int key0 = c * kCH;
-      float s[MB][2][4];
-      ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
-      ok = __all_sync(0xffffffffu, ok);
-      [[maybe_unused]] uint32_t ve[2][2];  // exponents of the values' rows
-      {
-        const uint8_t* kd = smem + L::kRing + slot * L::kOp;
+    // scores of this warp's keys of the chunk in ring slot `slot`
+    auto scores = [&](int slot, float (&s)[MB][NK][4]) {
+      const uint8_t* kd = smem + L::kRing + slot * L::kOp;
+      // where there are few, two sums of each, so that MMAs wait less for one another
+      constexpr bool TWO = MB * NK < 4;
+      [[maybe_unused]] float s2[NK][4];
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
+      for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+        for (int i = 0; i < 4; ++i) {
+          s2[nt][i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[mb][nt][i] = 0.f;
+          for (int mb = 0; mb < MB; ++mb) s[mb][nt][i] = 0.f;
+        }
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          uint4 kx[2];
+      for (int j = 0; j < NJ; ++j) {
+        uint32_t kw[NK][QW];  // K of the piece, in the words of q's type
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
-            const int row = kb + nt * 8 + g;
-            uint32_t at;
-            if (E4M3 && D == 64)
-              at = row * 64 + t4 * 16;
-            else if (E4M3)
-              at = row * 128 + (((2 * t4 + j) ^ g) << 4);
+        for (int nt = 0; nt < NK; ++nt) {
+          const int row = kb + nt * 8 + g;
+          uint32_t at;
+          if (E4M3 && D == 64)
+            at = row * 64 + t4 * 16;
+          else if (E4M3)
+            at = row * 128 + (((2 * t4 + j) ^ g) << 4);
+          else
+            at = (j >> 1) * 8192 + row * 128 + (((2 * t4 + (j & 1)) ^ g) << 4);
+          const uint4 x = *reinterpret_cast<const uint4*>(kd + at);
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (E4M3)
+              e4m3x4_f16(u[k], kw[nt][2 * k], kw[nt][2 * k + 1]);
             else
-              at = (j >> 1) * 8192 + row * 128 + (((2 * t4 + (j & 1)) ^ g) << 4);
-            kx[nt] = *reinterpret_cast<const uint4*>(kd + at);
+              kw[nt][k] = u[k];
           }
-          uint32_t kw[2][QW];  // K of the piece, in the words of q's type
+        }
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
-            const uint32_t u[4] = {kx[nt].x, kx[nt].y, kx[nt].z, kx[nt].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if constexpr (E4M3)
-                e4m3x4_f16(u[k], kw[nt][2 * k], kw[nt][2 * k + 1]);
-              else
-                kw[nt][k] = u[k];
-            }
-          }
+        for (int k = 0; k < QW / 2; ++k) {
+          const int i = j * (QW / 2) + k;
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb) {
-            uint32_t x[2][QW];  // rows g, g + 8
+            if constexpr (QREG) {
 #pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-              if constexpr (MB == 1) {
+              for (int nt = 0; nt < NK; ++nt) mma<E4M3>(TWO && (i & 1) ? s2[nt] : s[0][nt], qa[i], kw[nt][2 * k], kw[nt][2 * k + 1]);
+            } else {
+              const uint4 x = *reinterpret_cast<const uint4*>(smem + L::kQF + ((mb * KS + i) * 32 + lane) * 16);
+              const uint32_t a[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                for (int k = 0; k < QW; ++k) x[hi][k] = qa[j][hi][k];
-              } else {
-                const uint8_t* q = qd + (mb * 16 + hi * 8 + g) * L::kQRow;
-#pragma unroll
-                for (int i = 0; i < QW / 4; ++i) {
-                  const uint4 v = *reinterpret_cast<const uint4*>(
-                      q + (E4M3 ? (NJ * t4 + j) * 2 + i : (j >> 1) * 8 + 2 * t4 + (j & 1)) * 16);
-                  x[hi][4 * i] = v.x;
-                  x[hi][4 * i + 1] = v.y;
-                  x[hi][4 * i + 2] = v.z;
-                  x[hi][4 * i + 3] = v.w;
-                }
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < QW; k += 2) {
-              const uint32_t a[4] = {x[0][k], x[1][k], x[0][k + 1], x[1][k + 1]};
-#pragma unroll
-              for (int nt = 0; nt < 2; ++nt) {
-                if constexpr (E4M3)
-                  mma_f16(s[mb][nt], a, kw[nt][k], kw[nt][k + 1]);
-                else
-                  mma_bf16(s[mb][nt], a, kw[nt][k], kw[nt][k + 1]);
-              }
+              for (int nt = 0; nt < NK; ++nt) mma<E4M3>(TWO && (i & 1) ? s2[nt] : s[mb][nt], a, kw[nt][2 * k], kw[nt][2 * k + 1]);
             }
           }
-        }
-        if constexpr (E4M3) {
-          const uint8_t* sc = smem + L::kScale + slot * 64 + kb;
-          float ks[2][2];
-#pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
-            const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
-            ks[nt][0] = scale_value(two & 0xFFu);
-            ks[nt][1] = scale_value(two >> 8);
-          }
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) s[mb][nt][i] *= ks[nt][i & 1];
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[slot]);
-      step();
-      if constexpr (EDGE) {
+      if constexpr (TWO) {
+#pragma unroll
+        for (int nt = 0; nt < NK; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[0][nt][i] += s2[nt][i];
+      }
+      if constexpr (E4M3) {
+        const uint8_t* sc = smem + L::kScale + slot * CH + kb;
+        float ks[NK][2];
+#pragma unroll
+        for (int nt = 0; nt < NK; ++nt) {
+          const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
+          ks[nt][0] = scale_value(two & 0xFFu);
+          ks[nt][1] = scale_value(two >> 8);
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+          for (int nt = 0; nt < NK; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[mb][nt][i] *= ks[nt][i & 1];
+      }
+    };
+
+    // probabilities of chunk c into shared memory; EDGE where a key of it is past some row's limit
+    auto softmax = [&](int c, auto edge_c, bool fresh, float (&s)[MB][NK][4]) {
+      constexpr bool EDGE = decltype(edge_c)::value;
+      const int key0 = c * CH;
+      [[maybe_unused]] uint32_t ve[NK][2];  // exponents of the values' rows
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+          const int lim[2] = {limit(mb, 0), limit(mb, 1)};
+#pragma unroll
+          for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (key0 + kb + nt * 8 + 2 * t4 + (i & 1) >= R.lim[mb][i >> 1]) s[mb][nt][i] = -INFINITY;
+              if (key0 + kb + nt * 8 + 2 * t4 + (i & 1) >= lim[i >> 1]) s[mb][nt][i] = -INFINITY;
+        }
       }
       // V of the chunk: waited for here, as its rows' scales go into P
-      ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
-      ok = __all_sync(0xffffffffu, ok);
+      landed(vslot, vphase);
       if constexpr (E4M3) {
-        const uint8_t* sc = smem + L::kScale + slot * 64 + kb;
+        const uint8_t* sc = smem + L::kScale + vslot * CH + kb;
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < NK; ++nt) {
           const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
           ve[nt][0] = two & 0xFFu;
           ve[nt][1] = two >> 8;
@@ -518,50 +528,51 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       auto value_scale = [&](uint32_t e) {  // a row that is NaN: its codes do not say so to P V
         return e == 255u ? NAN : __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(e) - E0 + 127, 0)) << 23);
       };
-      uint8_t* pd = smem + L::kP + (nchunk & 1) * T * 128;
-      // probabilities against the running maxima, into shared memory; the
-      // largest log2 of them
+      uint8_t* pd = smem + L::kP + (nchunk & 1) * T * CH * 2;
+      // probabilities against the running maxima, into shared memory, and their
+      // sums; the largest log2 of them
+      float ls[MB][2];
       auto put_p = [&]() {
         float top = -INFINITY;
-        [[maybe_unused]] float vs[2][2];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) ls[mb][0] = ls[mb][1] = 0.f;
+        [[maybe_unused]] float vs[NK][2];
         if constexpr (E4M3) {
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+          for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) vs[nt][e] = value_scale(ve[nt][e]);
         }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+          for (int hi = 0; hi < 2; ++hi) {
+            const float sub = R.m[mb][hi] == -INFINITY ? 0.f : R.m[mb][hi];
 #pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-              const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -R.sub[mb][hi]);
-              const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -R.sub[mb][hi]);
+            for (int nt = 0; nt < NK; ++nt) {
+              const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -sub);
+              const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -sub);
               top = fmaxf(top, fmaxf(y0, y1));
               float e0 = ex2(y0), e1 = ex2(y1);
-              R.l[mb][hi] += e0 + e1;
+              ls[mb][hi] += e0 + e1;
               if constexpr (E4M3) {
                 // what a row does not see stays out, whatever its scale is
                 e0 = EDGE && s[mb][nt][2 * hi] == -INFINITY ? 0.f : e0 * vs[nt][0];
                 e1 = EDGE && s[mb][nt][2 * hi + 1] == -INFINITY ? 0.f : e1 * vs[nt][1];
               }
               const int r = mb * 16 + hi * 8 + g;
-              *reinterpret_cast<uint32_t*>(pd + r * 128 + (((2 * warp + nt) ^ g) << 4) + t4 * 4) =
+              const int k8 = warp * NK + nt;  // of the chunk's groups of 8 keys
+              *reinterpret_cast<uint32_t*>(pd + (k8 >> 3) * T * 128 + r * 128 + (((k8 & 7) ^ g) << 4) + t4 * 4) =
                   E4M3 ? f16x2(e0, e1) : bf16x2(e0, e1);
             }
+          }
         return top;
       };
-      float l0[MB][2];
-#pragma unroll
-      for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) l0[mb][hi] = R.l[mb][hi];
       bool raise = fresh;
       [[maybe_unused]] int emax = 0;
       if constexpr (E4M3) {
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) emax = max(emax, ve[nt][e] == 255u ? 0 : static_cast<int>(ve[nt][e]));
       }
@@ -578,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           for (int hi = 0; hi < 2; ++hi) {
             float x = -INFINITY;
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+            for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e) x = fmaxf(x, s[mb][nt][2 * hi + e] * R.f[mb][hi]);
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
@@ -600,8 +611,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
             const float mn = fmaxf(R.m[mb][hi], fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T])));
             const float alpha = mn == R.m[mb][hi] ? 1.f : ex2(R.m[mb][hi] - mn);  // 0 from -inf
             R.m[mb][hi] = mn;
-            R.sub[mb][hi] = mn == -INFINITY ? 0.f : mn;
-            R.l[mb][hi] = l0[mb][hi] * alpha;
+            R.l[mb][hi] *= alpha;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               o[mb][j][2 * hi] *= alpha * down;
@@ -611,10 +621,22 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         put_p();
         named_barrier(1, 128);
       }
-      ++nchunk;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) R.l[mb][hi] += ls[mb][hi];
+    };
 
-      // P V: this warp's D / 4 columns
-      const uint8_t* vd = smem + L::kRing + slot * L::kOp;
+    // P V of chunk c: this warp's D / 4 columns; and the next chunk's scores, whose
+    // MMAs fill the gaps between these
+    auto values = [&](int c, auto edge_c, float (&s)[MB][NK][4]) {
+      constexpr bool EDGE = decltype(edge_c)::value;
+      const int key0 = c * CH;
+      const bool more = c + 1 < w.c1;
+      if (more) landed(kslot, kphase);
+      scores(kslot, s);  // of the last chunk, what the slot holds: not used
+      const uint8_t* vd = smem + L::kRing + vslot * L::kOp;
+      const uint8_t* pd = smem + L::kP + (nchunk & 1) * T * CH * 2;
       // an element of a key that some row does not see, and that is not finite:
       // kept out of the product and noted, for the rows that do see it (8-bit
       // rows say so by their scale, above)
@@ -625,13 +647,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       };
       const uint32_t pb = smem_u32(pd);
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
+      for (int ks = 0; ks < CH / 16; ++ks) {
         if (EDGE && key0 + ks * 16 >= lim_hi) break;
         uint32_t a[MB][4];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
           const int row = mb * 16 + (lane & 15);
-          ldsm_x4(pb + row * 128 + (((2 * ks + (lane >> 4)) ^ (lane & 7)) << 4), a[mb][0], a[mb][1], a[mb][2], a[mb][3]);
+          ldsm_x4(pb + (ks >> 2) * T * 128 + row * 128 + (((2 * (ks & 3) + (lane >> 4)) ^ (lane & 7)) << 4), a[mb][0],
+                  a[mb][1], a[mb][2], a[mb][3]);
         }
         if constexpr (E4M3) {
           uint32_t v[2][2];  // [nt][e]: NT bytes of key ks * 16 + nt * 8 + 2 t4 + e
@@ -662,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
             for (int q = 0; q < 2; ++q)
 #pragma unroll
-              for (int mb = 0; mb < MB; ++mb) mma_f16(o[mb][2 * hf + q], a[mb], b[q][0], b[q][1]);
+              for (int mb = 0; mb < MB; ++mb) mma<true>(o[mb][2 * hf + q], a[mb], b[q][0], b[q][1]);
           }
         } else {
           const uint32_t vb = smem_u32(vd);
@@ -691,31 +714,40 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
             }
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
-              mma_bf16(o[mb][j], a[mb], b[0], b[1]);
-              mma_bf16(o[mb][j + 1], a[mb], b[2], b[3]);
+              mma<false>(o[mb][j], a[mb], b[0], b[1]);
+              mma<false>(o[mb][j + 1], a[mb], b[2], b[3]);
             }
           }
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[slot]);
-      step();
+      if (lane == 0) {
+        mbar_arrive(&empty[vslot]);
+        if (more) mbar_arrive(&empty[kslot]);
+      }
+      step(vslot, vphase);
+      if (more) step(kslot, kphase);
+      ++nchunk;
     };
 
+    float s[MB][NK][4];
+    landed(kslot, kphase);
+    scores(kslot, s);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&empty[kslot]);
+    step(kslot, kphase);
     for (int c = w.c0; c < w.c1; ++c) {
-      if ((c + 1) * kCH > lim_lo)
-        chunk(c, std::true_type{}, c == w.c0);
-      else
-        chunk(c, std::false_type{}, c == w.c0);
+      if ((c + 1) * CH > lim_lo) {
+        softmax(c, std::true_type{}, c == w.c0, s);
+        values(c, std::true_type{}, s);
+      } else {
+        softmax(c, std::false_type{}, c == w.c0, s);
+        values(c, std::false_type{}, s);
+      }
     }
     if (!ok && lane == 0 && !*abort) {
       *abort = 1;
       atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
-    }
-    if constexpr (MB > 1) {
-      if constexpr (E4M3) fence_async();  // q was rewritten in place
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&qempty[qs]);
     }
     ++pieces;
 
@@ -757,7 +789,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
               x[E4M3 ? e * NT + j : 2 * j + e] = z * inv;
             }
           if (any_bad) {
-            const int lim = R.lim[mb][hi];
+            const int lim = limit(mb, hi);
 #pragma unroll
             for (int k = 0; k < 2 * NT; ++k) {
               const int d = warp * (D / 4) + (E4M3 ? 2 * NT * t4 + k : (k >> 1) * 8 + 2 * t4 + (k & 1));
@@ -766,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
               if (lim > bad[d]) x[k] = NAN;
             }
           }
-          const int m = m0 + r, i = m / p.group, h = m - i * p.group;
+          const int m = m0 + r, i = paged_row(p, m), h = m - i * p.group;
           __nv_bfloat16* od = p.out + (static_cast<long long>(w.s.r0 + i) * p.Hq + w.h * p.group + h) * D + warp * (D / 4);
           float* pd = part + r * D + warp * (D / 4);
           if constexpr (E4M3) {
@@ -848,7 +880,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    const int m = cut.m0 + r, i = m / p.group, h = m - i * p.group;
+    const int m = cut.m0 + r, i = paged_row(p, m), h = m - i * p.group;
     __nv_bfloat16* od = p.out + (static_cast<long long>(cut.r0 + i) * p.Hq + cut.h * p.group + h) * D + lane * V;
     if constexpr (V == 4)
       *reinterpret_cast<uint2*>(od) = make_uint2(bf16x2(acc[0] * inv, acc[1] * inv), bf16x2(acc[2] * inv, acc[3] * inv));

@@ -192,7 +192,7 @@ struct Map {
   // and o free of 2 streams; q full, ready, empty; drain and turn of 2 streams
   static constexpr int kNBar = 2 * kKs + kFs + 4 * kVs + 8 + 7;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
-  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32 + 1) * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + 2 * (kThreads / 32) * 8;
   static constexpr uint32_t kBytes = kMisc + 32;
   static constexpr uint32_t kDyn = kBytes + 1024;
   static_assert(kDyn <= 227 * 1024 && 2 * kTile >= 128 * 64 * 4 + kTile, "shared memory");
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain = q_empty + 1;   // [2]
   uint64_t* turn = drain + 2;      // [2]
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
-  auto& scan = *reinterpret_cast<long long(*)[kThreads / 32 + 1]>(smem + L::kPlan + sizeof(PagedStart));
+  auto& scan = *reinterpret_cast<unsigned long long(*)[2][kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMisc);
   volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc + 4);
   int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 16);  // [kBads] by item
@@ -272,9 +272,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (tid == 256) paged_cut(p, *plan, T, kStep);
-  PagedWalk w;
-  const bool work = w.begin(p, *plan, T, kStep);
+  PagedWalk<0, kStep> w;
+  const bool work = w.begin(p, *plan, T);
+  if (!work && tid == 0) p.cuts[blockIdx.x] = PagedCut{};
   auto gave_up = [&]() {
     if (!*abort) {
       *abort = 1;
@@ -285,8 +285,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto rows_here = [&]() { return min(T, w.s.n * p.group - w.t * T); };
   auto steps_of = [&](int x, int n) { return one ? (n + 1 - x) / 2 : (x == 0 || rows_here() > tile ? n : 0); };
   // the first and the last of the item's limits
-  auto lim_first = [&]() { return paged_limit(p, w.s, w.t * T / p.group); };
-  auto lim_last = [&]() { return paged_limit(p, w.s, (w.t * T + rows_here() - 1) / p.group); };
+  auto lim_first = [&]() { return paged_limit(p, w.s, paged_row(p, w.t * T)); };
+  auto lim_last = [&]() { return paged_limit(p, w.s, paged_row(p, w.t * T + rows_here() - 1)); };
 
   if (warp >= 12) {
     regs_dec<kOtherRegs>();
@@ -317,11 +317,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (lane < tiles * NB) {
             const int x = lane / NB, hf = lane % NB;
             tma_load_3d(smem + L::kQ + x * L::kTile + hf * 16384, &tm_q, q_full, hf * 64, w.h * p.group,
-                        w.s.r0 + (w.t * T + x * tile) / p.group);
-            PagedWalk next = w;  // the next item's q into L2
+                        w.s.r0 + paged_row(p, w.t * T + x * tile));
+            PagedWalk<0, kStep> next = w;  // the next item's q into L2
             if (next.next(p))
               asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(&tm_q),
-                           "r"(hf * 64), "r"(next.h * p.group), "r"(next.s.r0 + (next.t * T + x * tile) / p.group)
+                           "r"(hf * 64), "r"(next.h * p.group), "r"(next.s.r0 + paged_row(p, next.t * T + x * tile))
                            : "memory");
           }
           ++items;
@@ -365,6 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
         }
+        if (is_k && lane == 0 && w.u + (w.c1 - w.c0) >= w.u1) w.leave(p, *plan);
       } while (ok && w.next(p));
       if (!ok) {
         if (lane == 0) gave_up();
@@ -664,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int rows = rows_here();
       const int m_row = w.t * T + (one ? 0 : x * tile) + row;  // packed row
       const bool valid = row < tile && (one ? 0 : x * tile) + row < rows;
-      const int lim = valid ? paged_limit(p, w.s, m_row / p.group) : kNever;
+      const int lim = valid ? paged_limit(p, w.s, paged_row(p, m_row)) : kNever;
       const int lo = lim_first();
       float f = p.scale_log2;
       // also where nothing of q is needed here: a stream without steps must not
@@ -881,7 +882,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // (every S of the item is complete), so that a store is of whole rows:
       // straight from the row's lane, 16 bytes a row, they took 9 to 18 thousand
       // cycles an item.
-      const int i_tok = m_row / p.group, h_grp = m_row - i_tok * p.group;
+      const int i_tok = paged_row(p, m_row), h_grp = m_row - i_tok * p.group;
       const long long at = whole ? (static_cast<long long>(w.s.r0 + i_tok) * p.Hq + w.h * p.group + h_grp) * D
                                  : (static_cast<long long>(w.part()) * p.part_rows + rr) * D;
       uint8_t* stage = smem + L::kQ + (one ? 0 : x * L::kTile) + (warp & 3) * 8192;

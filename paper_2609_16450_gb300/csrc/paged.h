@@ -38,8 +38,10 @@ struct PagedCut {
 };
 struct PagedParams {
   int B, R, Hq, Hkv, group;
+  unsigned group_inv;          // ceil(2^32 / group): m / group = mulhi(m, group_inv) for m * group < 2^32
   int causal;
   int page_log2, n_pages, max_pages;
+  int cap;                     // positions of a sequence's pages
   int box_log2;                // keys of a tensor-map box (at most a page)
   int part_rows;               // rows of a partial result
   float scale_log2;            // softmax scale * log2(e)
@@ -70,6 +72,9 @@ cudaError_t launch_paged_tc(const CUtensorMap& q, const CUtensorMap& k, const CU
 // the parts of cut tiles put together, a programmatic dependent of either kernel of `ctas` CTAs
 cudaError_t launch_paged_join(const PagedParams& p, int D, int ctas, cudaStream_t st);
 int paged_attention_ctas(bool e4m3, int row_blocks, int sms);
+// keys of a chunk of the mma.sync kernel: what a chunk costs besides its products
+// is the same, so as many as shared memory holds three operands of
+constexpr int paged_chunk_keys(bool e4m3, int row_blocks) { return e4m3 && row_blocks < 2 ? 128 : 64; }
 cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int D,
                                    bool e4m3, int row_blocks, int sms, cudaStream_t st);
 
@@ -87,14 +92,16 @@ struct PagedSeq {
   int r0, n, len;  // first row, rows, cached positions
   int tiles;
 };
+// row of its sequence that packed row m is of
+__device__ __forceinline__ int paged_row(const PagedParams& p, int m) {
+  return p.group == 1 ? m : static_cast<int>(__umulhi(static_cast<unsigned>(m), p.group_inv));
+}
 __device__ __forceinline__ PagedSeq paged_seq(const PagedParams& p, int b, int T) {
   PagedSeq s;
   s.r0 = min(max(p.cu_rows[b], 0), p.R);
   s.n = min(max(p.cu_rows[b + 1], s.r0), p.R) - s.r0;
-  const long long cap = static_cast<long long>(p.max_pages) << p.page_log2;
-  const int len = p.kv_len[b];
-  s.len = len < 0 ? 0 : (len > cap ? static_cast<int>(cap) : len);
-  s.tiles = static_cast<int>((static_cast<long long>(s.n) * p.group + T - 1) / T);
+  s.len = min(max(p.kv_len[b], 0), p.cap);
+  s.tiles = (s.n * p.group + T - 1) / T;
   return s;
 }
 // keys that row i of the sequence sees: those before this one
@@ -103,119 +110,155 @@ __device__ __forceinline__ int paged_limit(const PagedParams& p, const PagedSeq&
 }
 // chunks of tile t, and units of work: chunks, or tiles where none is cut
 __device__ __forceinline__ int paged_chunks(const PagedParams& p, const PagedSeq& s, int t, int T, int CH) {
-  const int last = min(s.n - 1, static_cast<int>(((static_cast<long long>(t) + 1) * T - 1) / p.group));
+  const int last = min(s.n - 1, paged_row(p, (t + 1) * T - 1));
   return max(1, (paged_limit(p, s, last) + CH - 1) / CH);
 }
-__device__ __forceinline__ long long paged_units(const PagedParams& p, const PagedSeq& s, int T, int CH) {
-  long long u = 0;
+__device__ __forceinline__ unsigned long long paged_units(const PagedParams& p, const PagedSeq& s, int T, int CH) {
+  unsigned u = 0;
   if (s.n == 0) return 0;
-  if (p.uncut) return static_cast<long long>(s.tiles) * p.Hkv;
-  if (!p.causal) return static_cast<long long>(s.tiles) * p.Hkv * paged_chunks(p, s, 0, T, CH);
-  for (int t = 0; t < s.tiles; ++t) u += paged_chunks(p, s, t, T, CH);
-  return u * p.Hkv;
+  if (!p.causal)
+    u = s.tiles * static_cast<unsigned>(paged_chunks(p, s, 0, T, CH));
+  else
+    for (int t = 0; t < s.tiles; ++t) u += paged_chunks(p, s, t, T, CH);
+  return static_cast<unsigned long long>(u) * p.Hkv;
 }
 
-// Where a CTA's share begins (in shared memory, written by paged_plan).
+// Where a CTA's share begins (in shared memory, written by paged_plan).  With q =
+// total / shares and r = total % shares, the first r shares have q + 1 units.
 struct PagedStart {
-  long long total, u0, u1;  // chunks in all; this CTA's are [u0, u1)
-  int shares;               // CTAs that have one
+  unsigned total, q, r;
+  unsigned u0, u1;          // this CTA's units are [u0, u1)
+  int uncut;                // units are tiles
   int b, t, h, c;           // sequence, tile, head and chunk of u0
 };
+__device__ __forceinline__ unsigned paged_share(const PagedStart& st, unsigned c) { return c * st.q + min(c, st.r); }
+// the CTA whose share holds unit u
+__device__ __forceinline__ int paged_owner(const PagedStart& st, unsigned u) {
+  const unsigned big = st.r * (st.q + 1);
+  return static_cast<int>(u < big ? u / (st.q + 1) : st.r + (u - big) / st.q);
+}
 // All NT threads of the block.  `least`: chunks of a share, at least, so that
-// a small call is not cut into more pieces than it is worth.
+// a small call is not cut into more pieces than it is worth.  Calls of 2^31
+// chunks and more have whole tiles as units.
 template <int NT>
 __device__ __forceinline__ void paged_plan(const PagedParams& p, int T, int CH, int least, PagedStart* st,
-                                           long long (&scan)[NT / 32 + 1]) {
+                                           unsigned long long (&scan)[2][NT / 32]) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (p.B + NT - 1) / NT;
   const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) mine += paged_units(p, paged_seq(p, b, T), T, CH);
-  long long inc = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += v;
+  unsigned long long chunks = 0, tiles = 0;
+  for (int b = b0; b < b1; ++b) {
+    const PagedSeq s = paged_seq(p, b, T);
+    chunks += paged_units(p, s, T, CH);
+    tiles += static_cast<unsigned>(s.tiles * p.Hkv);
   }
-  if (lane == 31) scan[warp] = inc;
+  unsigned long long inc[2] = {chunks, tiles};
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const unsigned long long v = __shfl_up_sync(0xffffffffu, inc[k], o);
+      if (lane >= o) inc[k] += v;
+    }
+  if (lane == 31) {
+    scan[0][warp] = inc[0];
+    scan[1][warp] = inc[1];
+  }
   __syncthreads();
-  long long before = 0, total = 0;
+  unsigned long long all = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) all += scan[0][w];
+  const int uncut = p.uncut || all >> 31 ? 1 : 0;
+  unsigned before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
+    if (w < warp) before += static_cast<unsigned>(scan[uncut][w]);
+    total += static_cast<unsigned>(scan[uncut][w]);
   }
-  const long long most = p.uncut ? total : (total + least - 1) / least;
-  const int shares = most < gridDim.x ? static_cast<int>(most) : static_cast<int>(gridDim.x);
-  long long u0 = 0, u1 = 0;
-  if (static_cast<int>(blockIdx.x) < shares) {
-    u0 = total * blockIdx.x / shares;
-    u1 = total * (blockIdx.x + 1) / shares;
+  const unsigned most = uncut ? total : (total + least - 1) / least;
+  const unsigned shares = max(1u, min(most, gridDim.x));
+  PagedStart s0;
+  s0.total = total;
+  s0.q = total / shares;
+  s0.r = total - s0.q * shares;
+  s0.uncut = uncut;
+  s0.u0 = s0.u1 = 0;
+  if (blockIdx.x < shares) {
+    s0.u0 = paged_share(s0, blockIdx.x);
+    s0.u1 = paged_share(s0, blockIdx.x + 1);
   }
   if (tid == 0) {
     st->total = total;
-    st->shares = shares;
-    st->u0 = u0;
-    st->u1 = u1;
+    st->q = s0.q;
+    st->r = s0.r;
+    st->uncut = uncut;
+    st->u0 = s0.u0;
+    st->u1 = s0.u1;
   }
-  long long at = before + inc - mine;
-  if (u0 < u1 && u0 >= at && u0 < at + mine) {
+  const unsigned mine = static_cast<unsigned>(uncut ? tiles : chunks);
+  unsigned at = before + static_cast<unsigned>(uncut ? inc[1] : inc[0]) - mine;
+  if (s0.u0 < s0.u1 && s0.u0 >= at && s0.u0 < at + mine) {
     for (int b = b0; b < b1; ++b) {
       const PagedSeq s = paged_seq(p, b, T);
-      const long long u = paged_units(p, s, T, CH);
-      if (u0 < at + u) {
-        int t = 0;
-        for (; t < s.tiles; ++t) {
-          const long long w = static_cast<long long>(p.uncut ? 1 : paged_chunks(p, s, t, T, CH)) * p.Hkv;
-          if (u0 < at + w) break;
-          at += w;
-        }
-        const int nch = p.uncut ? 1 : paged_chunks(p, s, t, T, CH);
-        st->b = b;
-        st->t = t;
-        st->h = static_cast<int>((u0 - at) / nch);
-        st->c = static_cast<int>((u0 - at) % nch);
-        break;
+      const unsigned u = uncut ? s.tiles * p.Hkv : static_cast<unsigned>(paged_units(p, s, T, CH));
+      if (s0.u0 >= at + u) {
+        at += u;
+        continue;
       }
-      at += u;
+      int t = 0;
+      unsigned nch = 1;
+      for (;; ++t) {
+        nch = uncut ? 1 : paged_chunks(p, s, t, T, CH);
+        if (s0.u0 < at + nch * p.Hkv) break;
+        at += nch * p.Hkv;
+      }
+      st->b = b;
+      st->t = t;
+      st->h = static_cast<int>((s0.u0 - at) / nch);
+      st->c = static_cast<int>((s0.u0 - at) % nch);
+      break;
     }
   }
   __syncthreads();
 }
 
-// A walk over a share's pieces of tiles, the same in every warp.
+// A walk over a share's pieces of tiles, the same in every warp.  Tiles of CT
+// rows (0: of the T that begin is given), chunks of CCH keys.
+template <int CT, int CCH>
 struct PagedWalk {
   PagedSeq s;
-  long long u, u1;  // next chunk of the share, and its end
+  unsigned u, u1;  // next unit of the share, and its end
   int b, t, h;
   int c0, c1, nch;  // the piece: chunks [c0, c1) of the tile's nch
-  int T, CH;
+  int rt;
+  bool uncut;
+  __device__ __forceinline__ int T() const { return CT != 0 ? CT : rt; }
   __device__ __forceinline__ void piece(const PagedParams& p, int c) {
-    nch = paged_chunks(p, s, t, T, CH);
+    nch = paged_chunks(p, s, t, T(), CCH);
     c0 = c;
-    c1 = !p.uncut && u1 - u < nch - c ? c + static_cast<int>(u1 - u) : nch;
+    c1 = !uncut && u1 - u < static_cast<unsigned>(nch - c) ? c + static_cast<int>(u1 - u) : nch;
   }
-  __device__ __forceinline__ bool begin(const PagedParams& p, const PagedStart& st, int T_, int CH_) {
-    T = T_;
-    CH = CH_;
+  __device__ __forceinline__ bool begin(const PagedParams& p, const PagedStart& st, int T_) {
+    rt = T_;
+    uncut = st.uncut != 0;
     u = st.u0;
     u1 = st.u1;
     if (u >= u1) return false;
     b = st.b;
     t = st.t;
     h = st.h;
-    s = paged_seq(p, b, T);
+    s = paged_seq(p, b, T());
     piece(p, st.c);
     return true;
   }
   __device__ __forceinline__ bool next(const PagedParams& p) {
-    u += p.uncut ? 1 : c1 - c0;
+    u += uncut ? 1 : c1 - c0;
     if (u >= u1) return false;
     if (++h == p.Hkv) {
       h = 0;
       if (++t == s.tiles) {
         t = 0;
-        do s = paged_seq(p, ++b, T);
+        do s = paged_seq(p, ++b, T());
         while (s.tiles == 0);  // ends: chunks are left
       }
     }
@@ -225,32 +268,20 @@ struct PagedWalk {
   __device__ __forceinline__ bool whole() const { return c0 == 0 && c1 == nch; }
   // where this piece's partial result goes
   __device__ __forceinline__ int part() const { return 2 * static_cast<int>(blockIdx.x) + (c0 == 0 ? 1 : 0); }
-};
-// the CTA whose share holds unit u
-__device__ __forceinline__ int paged_owner(const PagedStart& st, long long u) {
-  int c = static_cast<int>(u * st.shares / st.total);
-  while (c > 0 && st.total * c / st.shares > u) --c;
-  while (st.total * (c + 1) / st.shares <= u) ++c;
-  return c;
-}
-// What this CTA's share leaves to be put together (one thread, after
-// paged_plan): the tile that its last piece begins and does not end.
-__device__ __forceinline__ void paged_cut(const PagedParams& p, const PagedStart& st, int T, int CH) {
-  PagedCut cut{};
-  PagedWalk w;
-  if (!p.uncut && w.begin(p, st, T, CH)) {
-    do {
-      if (w.c0 == 0 && w.c1 < w.nch) {
-        cut.parts = paged_owner(st, w.u + w.nch - 1) - static_cast<int>(blockIdx.x) + 1;
-        cut.m0 = w.t * T;
-        cut.rows = min(T, w.s.n * p.group - cut.m0);
-        cut.r0 = w.s.r0;
-        cut.h = w.h;
-      }
-    } while (w.next(p));
+  // What this CTA's share leaves to be put together (one thread, at the
+  // share's last piece): the tile that it begins and does not end.
+  __device__ __forceinline__ void leave(const PagedParams& p, const PagedStart& st) const {
+    PagedCut cut{};
+    if (c0 == 0 && c1 < nch) {
+      cut.parts = paged_owner(st, u + nch - 1) - static_cast<int>(blockIdx.x) + 1;
+      cut.m0 = t * T();
+      cut.rows = min(T(), s.n * p.group - cut.m0);
+      cut.r0 = s.r0;
+      cut.h = h;
+    }
+    p.cuts[blockIdx.x] = cut;
   }
-  p.cuts[blockIdx.x] = cut;
-}
+};
 #endif
 
 }  // namespace ebd
