@@ -1648,8 +1648,8 @@ ebd_status paged_rows(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args
   p.v = reinterpret_cast<__nv_bfloat16*>(a->v);
   p.kv_stride = stride;
   p.skip = write ? a->skip : nullptr;
-  cudaError_t e = write ? launch_paged_write(p, static_cast<cudaStream_t>(stream))
-                        : launch_paged_read(p, static_cast<cudaStream_t>(stream));
+  cudaError_t e = write ? launch_paged_write(p, h->num_sms, static_cast<cudaStream_t>(stream))
+                        : launch_paged_read(p, h->num_sms, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, write ? "paged write launch" : "paged read launch");
   return EBD_OK;
 }
@@ -1720,11 +1720,18 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   const bool wide = f.head_dim == 128 && p.group <= kPagedTcGroup && m > 64;
   // keys of a tensor-map box: a page, or a chunk's part of it
   const int mb = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-  const int chunk_log2 = log2_of(wide ? 128 : paged_chunk_keys(e4m3, mb));
+  const int chunk_log2 = wide ? kPagedTcStepLog2 : kPagedChunkLog2;
   p.box_log2 = p.page_log2 < chunk_log2 ? p.page_log2 : chunk_log2;
   p.part_rows = wide ? kPagedTcRows : kPagedRows;
-  // tiles stay whole where none can have many chunks (64 keys, or 128 in the tcgen05 kernel)
-  p.uncut = static_cast<int64_t>(c->max_pages) * c->page_size <= kPagedUncutKeys ? 1 : 0;
+  const int ctas = wide ? h->num_sms : paged_attention_ctas(e4m3, mb, h->num_sms);
+  const int tokens = wide ? 128 / p.group : 0;          // of a tile of 128 rows
+  const bool one = wide && m <= tokens * p.group;       // (see launch_paged_tc)
+  const int64_t T = wide ? (one ? 1 : 2) * tokens * p.group : 16 * mb;
+  const int64_t tiles = f.n_heads_kv * ((static_cast<int64_t>(a->rows) * p.group + T - 1) / T);  // at least
+  // Tiles stay whole where none can have many chunks, or where chunks might not
+  // be countable in 31 bits.
+  const int64_t chunks = (p.cap >> chunk_log2) + 1;
+  p.uncut = p.cap <= kPagedUncutKeys || (tiles + static_cast<int64_t>(f.n_heads_kv) * a->batch) * chunks >= 0x7fffffff;
   CUtensorMap tq, tk, tv;
   if (!encode_pool(&tk, c->k, h, c, 1 << p.box_log2) || !encode_pool(&tv, c->v, h, c, 1 << p.box_log2))
     return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (pages) failed");
@@ -1734,17 +1741,14 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
     const uint64_t dims[3] = {static_cast<uint64_t>(f.head_dim), static_cast<uint64_t>(f.n_heads_q),
                               static_cast<uint64_t>(a->rows)};
     const uint64_t str[2] = {static_cast<uint64_t>(f.head_dim) * 2, static_cast<uint64_t>(stride) * 2};
-    const int tokens = 128 / p.group;
     const uint32_t box[3] = {64, static_cast<uint32_t>(p.group), static_cast<uint32_t>(tokens)};
     if (!encode_bf16(&tq, a->q, 3, dims, str, box))
       return fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled (q) failed");
-    e = launch_paged_tc(tq, tk, tv, p, e4m3, m <= tokens * p.group, h->num_sms, static_cast<cudaStream_t>(stream));
+    e = launch_paged_tc(tq, tk, tv, p, e4m3, one, h->num_sms, static_cast<cudaStream_t>(stream));
   } else {
     e = launch_paged_attention(tk, tv, p, f.head_dim, e4m3, mb, h->num_sms, static_cast<cudaStream_t>(stream));
   }
-  if (e == cudaSuccess && !p.uncut)
-    e = launch_paged_join(p, f.head_dim, wide ? h->num_sms : paged_attention_ctas(e4m3, mb, h->num_sms),
-                          static_cast<cudaStream_t>(stream));
+  if (e == cudaSuccess && !p.uncut) e = launch_paged_join(p, f.head_dim, ctas, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "paged attention launch");
   return EBD_OK;
 }

@@ -13,8 +13,11 @@
 // value that is not finite is NaN as a whole (exponent byte 255, codes 0x7F), so
 // that the attention learns of it from the scale, not from every code.
 //
-// Both kernels move bytes: a block per row (what a sequence's lookup costs is
-// then paid once), 16 bytes of bf16 per thread and turn.
+// Both kernels move bytes.  A block is a row, or a part of one: 256 threads by U
+// pieces of 16 bytes of bf16, U = 4 where there are blocks enough for all SMs, so
+// that what a row's lookup costs (three loads, one after another) is shared by
+// more bytes, and 1 where there are not, so that a window of 32 rows is spread
+// over them.  A write loads its rows while it looks its page up.
 #include <cuda_fp8.h>
 
 #include "paged.h"
@@ -25,12 +28,12 @@ namespace {
 
 // Sequence, page and place in it of row r: false where the row has none.
 __device__ __forceinline__ bool row_slot(const PagedRowsParams& p, int r, long long& page, int& off) {
+  const int pos = p.row_pos[r];
   // the row's sequence: as many as end at or before it
   int b = 0;
   for (int i = threadIdx.x; i - static_cast<int>(threadIdx.x) < p.B; i += blockDim.x)
     b += __syncthreads_count(i < p.B && p.cu_rows[i + 1] <= r);
   if (b >= p.B) return false;
-  const int pos = p.row_pos[r];
   const int i = pos >> p.page_log2;
   if (pos < 0 || i >= p.max_pages) return false;
   const int pg = p.page_table[static_cast<long long>(b) * p.max_pages + i];
@@ -40,30 +43,63 @@ __device__ __forceinline__ bool row_slot(const PagedRowsParams& p, int r, long l
   return true;
 }
 
-template <int D, bool E4M3>
+// A piece of a row: 8 values of a head's K or V.
+template <int D>
+struct Piece {
+  bool in, is_v;
+  int head, l;  // l: which 8
+  __device__ __forceinline__ Piece(const PagedRowsParams& p, int it) {
+    const int per = p.Hkv * (D / 8);  // pieces of K, and of V
+    in = it < 2 * per;
+    is_v = it >= per;
+    const int j = is_v ? it - per : it;
+    head = j / (D / 8);
+    l = j % (D / 8);
+  }
+  __device__ __forceinline__ __nv_bfloat16* row(const PagedRowsParams& p, int r) const {
+    return (is_v ? p.v : p.k) + r * p.kv_stride + head * D + l * 8;
+  }
+  // element of the pools that it lies at in its page, and byte of the scales
+  __device__ __forceinline__ long long at(const PagedRowsParams& p, int off) const {
+    return ((static_cast<long long>(head) << p.page_log2) + off) * D + l * 8;
+  }
+  __device__ __forceinline__ uint8_t* pool(const PagedRowsParams& p, long long page) const {
+    return (is_v ? p.v_pool : p.k_pool) + page * p.page_stride;
+  }
+  __device__ __forceinline__ uint8_t* scale(const PagedRowsParams& p, long long page, int off) const {
+    return (is_v ? p.v_scale : p.k_scale) + (((page * p.Hkv + head) << p.page_log2) + off);
+  }
+};
+
+template <int D, bool E4M3, int U>
 __global__ void __launch_bounds__(256) paged_write_kernel(const PagedRowsParams p) {
   constexpr int LPR = D / 8;  // lanes per row of a head, 8 values each
-  const int r = blockIdx.x;
+  const int r = blockIdx.x, it0 = blockIdx.y * U * blockDim.x + threadIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const bool skip = p.skip != nullptr && p.skip[r] != 0;
+  if (U > 1 && skip) return;  // a row's bytes count, not its latency
+  uint4 x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const Piece<D> c(p, it0 + u * blockDim.x);
+    if (c.in) x[u] = __ldcs(reinterpret_cast<const uint4*>(c.row(p, r)));
+  }
   long long page;
   int off;
-  if (p.skip != nullptr && p.skip[r] != 0) return;
-  if (!row_slot(p, r, page, off)) return;
-  const int per = p.Hkv * LPR;  // 16-byte pieces of K, and of V
-  for (int it = threadIdx.x; it < 2 * per; it += blockDim.x) {
-    const bool is_v = it >= per;
-    const int j = is_v ? it - per : it;
-    const int head = j / LPR, l = j % LPR;
-    const uint4 x = *reinterpret_cast<const uint4*>((is_v ? p.v : p.k) + r * p.kv_stride + head * D + l * 8);
-    const long long slot = (static_cast<long long>(head) << p.page_log2) + off;
-    uint8_t* pool = (is_v ? p.v_pool : p.k_pool) + page * p.page_stride;
+  if (!row_slot(p, r, page, off) || skip) return;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const Piece<D> c(p, it0 + u * blockDim.x);
+    if (!c.in) break;
     if constexpr (!E4M3) {
-      *reinterpret_cast<uint4*>(pool + (slot * D + l * 8) * 2) = x;
+      *reinterpret_cast<uint4*>(c.pool(p, page) + c.at(p, off) * 2) = x[u];
     } else {
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
       uint32_t amax = 0;  // bits of the largest |value|; past infinity's for NaN
 #pragma unroll
       for (int i = 0; i < 4; ++i) amax = max(amax, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
-      // per is a multiple of LPR and the loop's stride of 32: a row's lanes are in it together
+      // pieces of K and of V are multiples of LPR, and the block's threads of 32: a row's lanes are in it together
       const uint32_t lanes = (LPR == 16 ? 0xFFFFu : 0xFFu) << ((threadIdx.x & 31) & ~(LPR - 1));
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(lanes, amax, o));
@@ -76,79 +112,92 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const PagedRowsParams 
       for (int i = 0; i < 4; ++i) {
         const float lo = __uint_as_float(w[i] << 16) * inv, hi = __uint_as_float(w[i] & 0xFFFF0000u) * inv;
         const float2 y = make_float2(fminf(fmaxf(lo, -top), top), fminf(fmaxf(hi, -top), top));
-        const uint32_t c = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
-        code[i >> 1] |= c << (16 * (i & 1));
+        const uint32_t c2 = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
+        code[i >> 1] |= c2 << (16 * (i & 1));
       }
       if (!finite) code[0] = code[1] = 0x7F7F7F7Fu;
-      *reinterpret_cast<uint2*>(pool + slot * D + l * 8) = make_uint2(code[0], code[1]);
-      if (l == 0) {
-        const long long at = ((page * p.Hkv + head) << p.page_log2) + off;
-        (is_v ? p.v_scale : p.k_scale)[at] = static_cast<uint8_t>(e);
-      }
+      *reinterpret_cast<uint2*>(c.pool(p, page) + c.at(p, off)) = make_uint2(code[0], code[1]);
+      if (c.l == 0) *c.scale(p, page, off) = static_cast<uint8_t>(e);
     }
   }
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, int U>
 __global__ void __launch_bounds__(256) paged_read_kernel(const PagedRowsParams p) {
-  constexpr int LPR = D / 8;
-  const int r = blockIdx.x;
+  const int r = blockIdx.x, it0 = blockIdx.y * U * blockDim.x + threadIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   long long page = 0;
   int off = 0;
   const bool held = row_slot(p, r, page, off);
-  const int per = p.Hkv * LPR;
-  for (int it = threadIdx.x; it < 2 * per; it += blockDim.x) {
-    const bool is_v = it >= per;
-    const int j = is_v ? it - per : it;
-    const int head = j / LPR, l = j % LPR;
-    const long long slot = (static_cast<long long>(head) << p.page_log2) + off;
-    const uint8_t* pool = (is_v ? p.v_pool : p.k_pool) + page * p.page_stride;
-    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-    if (held) {
-      if constexpr (!E4M3) {
-        x = *reinterpret_cast<const uint4*>(pool + (slot * D + l * 8) * 2);
-      } else {
-        const uint2 c = *reinterpret_cast<const uint2*>(pool + slot * D + l * 8);
-        const long long at = ((page * p.Hkv + head) << p.page_log2) + off;
-        const uint32_t e = (is_v ? p.v_scale : p.k_scale)[at];
-        const float scale = __uint_as_float(e > 0 ? e << 23 : 1u << 22);  // 2^(e - 127)
-        uint32_t w[4];
+  uint4 x[U];
+  uint32_t e[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t two = (i < 2 ? c.x : c.y) >> (16 * (i & 1));
-          const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-          const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);  // exact
-          w[i] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        x = make_uint4(w[0], w[1], w[2], w[3]);
-      }
+  for (int u = 0; u < U; ++u) {
+    const Piece<D> c(p, it0 + u * blockDim.x);
+    x[u] = make_uint4(0u, 0u, 0u, 0u);
+    e[u] = 0;
+    if (!c.in || !held) continue;
+    if constexpr (!E4M3) {
+      x[u] = __ldcs(reinterpret_cast<const uint4*>(c.pool(p, page) + c.at(p, off) * 2));
+    } else {
+      const uint2 code = __ldcs(reinterpret_cast<const uint2*>(c.pool(p, page) + c.at(p, off)));
+      x[u].x = code.x;
+      x[u].y = code.y;
+      e[u] = *c.scale(p, page, off);
     }
-    *reinterpret_cast<uint4*>((is_v ? p.v : p.k) + r * p.kv_stride + head * D + l * 8) = x;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const Piece<D> c(p, it0 + u * blockDim.x);
+    if (!c.in) break;
+    if constexpr (E4M3) {
+      const float scale = __uint_as_float(e[u] > 0 ? e[u] << 23 : 1u << 22);  // 2^(e - 127)
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = (i < 2 ? x[u].x : x[u].y) >> (16 * (i & 1));
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);  // exact
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      x[u] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    *reinterpret_cast<uint4*>(c.row(p, r)) = x[u];
   }
 }
 
-int block_threads(const PagedRowsParams& p) {
-  const int n = 2 * p.Hkv * (p.D / 8);
-  return n >= 256 ? 256 : (n + 31) / 32 * 32;
+// By dtype and head width; many pieces per thread where blocks abound.
+template <class K>
+cudaError_t launch_rows(const PagedRowsParams& p, int sms, cudaStream_t st, const K& kernel) {
+  const int pieces = 2 * p.Hkv * (p.D / 8);
+  const int threads = pieces >= 256 ? 256 : (pieces + 31) / 32 * 32;
+  const bool many = p.R * static_cast<long long>(pieces) >= 4LL * 1024 * sms;
+  const int each = threads * (many ? 4 : 1);
+  return paged_launch(kernel(many), dim3(p.R, (pieces + each - 1) / each, 1), threads, 0, st, p);
 }
 
 }  // namespace
 
-cudaError_t launch_paged_write(const PagedRowsParams& p, cudaStream_t st) {
-  if (p.R <= 0) return cudaSuccess;
-  const auto k = p.D == 64 ? (p.e4m3 ? paged_write_kernel<64, true> : paged_write_kernel<64, false>)
-                           : (p.e4m3 ? paged_write_kernel<128, true> : paged_write_kernel<128, false>);
-  k<<<p.R, block_threads(p), 0, st>>>(p);
-  return cudaGetLastError();
+cudaError_t launch_paged_write(const PagedRowsParams& p, int sms, cudaStream_t st) {
+  return launch_rows(p, sms, st, [&](bool many) {
+    if (p.D == 64)
+      return p.e4m3 ? (many ? paged_write_kernel<64, true, 4> : paged_write_kernel<64, true, 1>)
+                    : (many ? paged_write_kernel<64, false, 4> : paged_write_kernel<64, false, 1>);
+    return p.e4m3 ? (many ? paged_write_kernel<128, true, 4> : paged_write_kernel<128, true, 1>)
+                  : (many ? paged_write_kernel<128, false, 4> : paged_write_kernel<128, false, 1>);
+  });
 }
 
-cudaError_t launch_paged_read(const PagedRowsParams& p, cudaStream_t st) {
-  if (p.R <= 0) return cudaSuccess;
-  const auto k = p.D == 64 ? (p.e4m3 ? paged_read_kernel<64, true> : paged_read_kernel<64, false>)
-                           : (p.e4m3 ? paged_read_kernel<128, true> : paged_read_kernel<128, false>);
-  k<<<p.R, block_threads(p), 0, st>>>(p);
-  return cudaGetLastError();
+cudaError_t launch_paged_read(const PagedRowsParams& p, int sms, cudaStream_t st) {
+  return launch_rows(p, sms, st, [&](bool many) {
+    if (p.D == 64)
+      return p.e4m3 ? (many ? paged_read_kernel<64, true, 4> : paged_read_kernel<64, true, 1>)
+                    : (many ? paged_read_kernel<64, false, 4> : paged_read_kernel<64, false, 1>);
+    return p.e4m3 ? (many ? paged_read_kernel<128, true, 4> : paged_read_kernel<128, true, 1>)
+                  : (many ? paged_read_kernel<128, false, 4> : paged_read_kernel<128, false, 1>);
+  });
 }
 
 }  // namespace ebd

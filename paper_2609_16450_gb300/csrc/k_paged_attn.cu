@@ -42,6 +42,7 @@ namespace {
 
 constexpr int kThreads = 160;
 constexpr int kLeastKeys = 192;     // keys of a share, at least
+constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -87,19 +88,19 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
 __device__ __forceinline__ float scale_value(uint32_t e) { return __uint_as_float(max(e << 23, 1u << 22)); }
 
 // CTAs per SM: as many as registers and a ring of two chunks or more allow.
-constexpr int ctas_per_sm(bool e4m3, int mb) { return e4m3 && mb <= 2 ? 3 : 2; }
-// q's fragments of one row block stay in registers
-constexpr bool q_in_registers(bool e4m3, int mb) { return mb == 1; }
+constexpr int ctas_per_sm(bool e4m3, int mb) { return !e4m3 ? 2 : mb == 1 ? 4 : mb == 2 ? 3 : 2; }
+// q's fragments of one row block stay in registers where these suffice
+constexpr bool q_in_registers(bool e4m3, int mb) { return !e4m3 && mb == 1; }
 
 // Shared memory (offsets from a 1024-byte aligned base).
 template <int D, bool E4M3, int MB>
 struct Map {
   static constexpr int T = 16 * MB;                               // tile rows
-  static constexpr int CH = paged_chunk_keys(E4M3, MB);
+  static constexpr int CH = 1 << kPagedChunkLog2;
   static constexpr uint32_t kOp = CH * D * (E4M3 ? 1 : 2);       // K or V of a chunk
   static constexpr uint32_t kQRow = 2 * D + 16;                   // padded: rows in distinct banks
   static constexpr uint32_t kFrag = q_in_registers(E4M3, MB) ? 0 : T * 2 * D;  // q as fragments
-  static constexpr uint32_t kAll = (ctas_per_sm(E4M3, MB) == 3 ? 75 : 113) * 1024 - 1024;
+  static constexpr uint32_t kAll = (ctas_per_sm(E4M3, MB) == 4 ? 56 : ctas_per_sm(E4M3, MB) == 3 ? 75 : 113) * 1024 - 1024;
   static constexpr uint32_t kFixed = T * kQRow + kFrag + 4 * T * CH + 3 * D * 4 + 2 * 4 * T * 4 + 4 * T * 4 +
                                      T * 4 + 640;
   static constexpr uint32_t kSlotBytes = kOp + (E4M3 ? CH : 0) + 16;
@@ -117,7 +118,7 @@ struct Map {
   static constexpr uint32_t kBar = kRowF + T * 4;
   static constexpr int kNBar = 2 * S + 2;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
-  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + 2 * (kThreads / 32) * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + 8 * 4;
   static constexpr uint32_t kBytes = kMisc + 16;
   static constexpr uint32_t kDyn = kBytes + 1024;
   static_assert(S >= 3 && kBytes <= kAll && (kP % 1024) == 0 && (kQ % 16) == 0, "shared memory");
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   uint64_t* qfull = empty + S;
   uint64_t* qempty = qfull + 1;
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
-  auto& scan = *reinterpret_cast<unsigned long long(*)[2][kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
+  auto& scan = *reinterpret_cast<unsigned(*)[kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
   volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc);
   int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 8);
   int* bad = reinterpret_cast<int*>(smem + L::kBad);
@@ -177,6 +178,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     fence_mbar_init();
   }
   for (int i = tid; i < 3 * D; i += kThreads) bad[i] = kNever;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   paged_plan<kThreads>(p, T, CH, kLeastKeys / CH, plan, scan);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   PagedWalk<T, CH> w;
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 
   if (warp == 4) {
     // ------------------------------------------------------------ loads
-    const int np_log = (CH == 128 ? 7 : 6) - p.box_log2, box = 1 << p.box_log2;
+    const int np_log = kPagedChunkLog2 - p.box_log2, box = 1 << p.box_log2;
     const int pc = lane & ((1 << np_log) - 1), part = lane >> np_log;
     const int key_in = pc << p.box_log2;
     int n = 0, pieces = 0;
@@ -195,6 +197,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     do {
       const int last = min(w.s.n - 1, paged_row(p, w.t * T + T - 1));
       const int rows = min(T, w.s.n * p.group - w.t * T);
+      const int lim = paged_limit(p, w.s, last);
+      const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
+      // page ids of 32 pages, one per lane; the first while q is seen to
+      int win0 = ((w.c0 * CH) >> p.page_log2) & ~31;
+      int win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
       {  // q: rows by lane, zeros past the tile's last
         uint8_t* qd = smem + L::kQ;
         ok = pieces == 0 || mbar_wait(qempty, static_cast<uint32_t>(pieces - 1) & 1u, p.limit_ns, abort);
@@ -213,13 +220,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         }
         ++pieces;
       }
-      const int lim = paged_limit(p, w.s, last);
-      const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
-      int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
       for (int c = w.c0; c < w.c1 && ok; ++c) {
         const int key = c * CH + key_in;
         const int first = (c * CH) >> p.page_log2;
-        if (first >= win0 + 32 || first < win0) {
+        if (first >= win0 + 32) {
           win0 = first & ~31;
           win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
         }
@@ -833,59 +837,83 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   } while (w.next(p));
 }
 
-// The parts of the tile that CTA blockIdx.x of the attention begins: a warp per
-// row, a lane per D / 32 columns, so that a part's row is one load.
+// The parts of the tile that CTA blockIdx.x of the attention begins, put
+// together in order: kJoinRows rows per warp, their loads all in flight, a lane
+// per D / 32 columns, so that a part's row is one load.
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedParams p) {
-  constexpr int V = D / 32;
+  constexpr int V = D / 32, RB = kJoinRows;
+  const int lane = threadIdx.x & 31;
+  const int r0 = (blockIdx.y * 8 + (threadIdx.x >> 5)) * RB;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the attention's results
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const PagedCut cut = p.cuts[blockIdx.x];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto part = [&](int k) {
-    const int c = static_cast<int>(blockIdx.x);
-    return static_cast<long long>(k == 0 ? 2 * c + 1 : 2 * (c + k)) * p.part_rows;
-  };
-  if (cut.parts == 0) return;
-  for (int r = blockIdx.y * 8 + warp; r < cut.rows; r += 8 * gridDim.y) {
-    float mx = -INFINITY;
-    for (int k = lane; k < cut.parts; k += 32) mx = fmaxf(mx, p.part_ml[(part(k) + r) * 2]);
+  if (cut.parts == 0 || r0 >= cut.rows) return;
+  auto part = [&](int k) { return static_cast<long long>(k == 0 ? 2 * cut.first + 1 : 2 * (cut.first + k)) * p.part_rows; };
+  float mx[RB], l[RB], acc[RB][V];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    float l = 0.f, acc[V] = {};
-    for (int k0 = 0; k0 < cut.parts; k0 += 32) {
-      float wgt = 0.f;
-      if (k0 + lane < cut.parts) {
-        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (part(k0 + lane) + r) * 2);
-        wgt = ml.x == -INFINITY ? 0.f : ex2(ml.x - mx);  // 0: a part that the row sees nothing of
-        l = fmaf(wgt, ml.y, l);
-      }
-      const int n = min(32, cut.parts - k0);
-#pragma unroll 8
-      for (int k = 0; k < n; ++k) {
-        const float wk = __shfl_sync(0xffffffffu, wgt, k);
-        const float* z = p.part + (part(k0 + k) + r) * D + lane * V;
+  for (int i = 0; i < RB; ++i) {
+    mx[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[i][j] = 0.f;
+  }
+  auto row = [&](int i) { return min(r0 + i, cut.rows - 1); };
+  for (int k0 = 0; k0 < cut.parts; k0 += 32) {
+    // with the new parts the maximum may rise; -inf: a part that the row sees nothing of
+    float2 ml[RB];
+    float wgt[RB];
+    const bool in = k0 + lane < cut.parts;
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+      ml[i] = in ? __ldcg(reinterpret_cast<const float2*>(p.part_ml + (part(k0 + lane) + row(i)) * 2))
+                 : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      float x = ml[i].x;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+      x = fmaxf(x, mx[i]);
+      const float f = mx[i] == -INFINITY ? 0.f : ex2(mx[i] - x);
+      mx[i] = x;
+      l[i] *= f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) acc[i][j] *= f;
+      wgt[i] = ml[i].x == -INFINITY ? 0.f : ex2(ml[i].x - x);
+      l[i] = fmaf(wgt[i], ml[i].y, l[i]);
+    }
+    const int n = min(32, cut.parts - k0);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float* z = p.part + part(k0 + k) * D + lane * V;
+#pragma unroll
+      for (int i = 0; i < RB; ++i) {
+        const float wk = __shfl_sync(0xffffffffu, wgt[i], k);
         if constexpr (V == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(z);
-          acc[0] = fmaf(wk, x.x, acc[0]);
-          acc[1] = fmaf(wk, x.y, acc[1]);
-          acc[2] = fmaf(wk, x.z, acc[2]);
-          acc[3] = fmaf(wk, x.w, acc[3]);
+          const float4 x = __ldcg(reinterpret_cast<const float4*>(z + row(i) * D));
+          acc[i][0] = fmaf(wk, x.x, acc[i][0]);
+          acc[i][1] = fmaf(wk, x.y, acc[i][1]);
+          acc[i][2] = fmaf(wk, x.z, acc[i][2]);
+          acc[i][3] = fmaf(wk, x.w, acc[i][3]);
         } else {
-          const float2 x = *reinterpret_cast<const float2*>(z);
-          acc[0] = fmaf(wk, x.x, acc[0]);
-          acc[1] = fmaf(wk, x.y, acc[1]);
+          const float2 x = __ldcg(reinterpret_cast<const float2*>(z + row(i) * D));
+          acc[i][0] = fmaf(wk, x.x, acc[i][0]);
+          acc[i][1] = fmaf(wk, x.y, acc[i][1]);
         }
       }
     }
+  }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    const int m = cut.m0 + r, i = paged_row(p, m), h = m - i * p.group;
-    __nv_bfloat16* od = p.out + (static_cast<long long>(cut.r0 + i) * p.Hq + cut.h * p.group + h) * D + lane * V;
-    if constexpr (V == 4)
-      *reinterpret_cast<uint2*>(od) = make_uint2(bf16x2(acc[0] * inv, acc[1] * inv), bf16x2(acc[2] * inv, acc[3] * inv));
-    else
-      *reinterpret_cast<uint32_t*>(od) = bf16x2(acc[0] * inv, acc[1] * inv);
+  for (int i = 0; i < RB; ++i) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+    if (r0 + i >= cut.rows) break;
+    const float inv = l[i] > 0.f || l[i] != l[i] ? 1.f / l[i] : 0.f;
+    const int m = cut.m0 + r0 + i, n = paged_row(p, m), h = m - n * p.group;
+    __nv_bfloat162* od = reinterpret_cast<__nv_bfloat162*>(
+        p.out + (static_cast<long long>(cut.r0 + n) * p.Hq + cut.h * p.group + h) * D + lane * V);
+#pragma unroll
+    for (int k = 0; k < V / 2; ++k) od[k] = __floats2bfloat162_rn(acc[i][2 * k] * inv, acc[i][2 * k + 1] * inv);
   }
 }
 
@@ -898,15 +926,12 @@ template <int D, bool E4M3>
 cudaError_t launch(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int mb, int sms, cudaStream_t st) {
   auto go = [&](auto c) {
     constexpr int MB = decltype(c)::value;
-    paged_attn_kernel<D, E4M3, MB><<<sms * ctas_per_sm(E4M3, MB), kThreads, Map<D, E4M3, MB>::kDyn, st>>>(k, v, p);
+    return paged_launch(paged_attn_kernel<D, E4M3, MB>, sms * ctas_per_sm(E4M3, MB), kThreads, Map<D, E4M3, MB>::kDyn, st,
+                        k, v, p);
   };
-  if (mb == 1)
-    go(std::integral_constant<int, 1>{});
-  else if (mb == 2)
-    go(std::integral_constant<int, 2>{});
-  else
-    go(std::integral_constant<int, 4>{});
-  return cudaGetLastError();
+  if (mb == 1) return go(std::integral_constant<int, 1>{});
+  if (mb == 2) return go(std::integral_constant<int, 2>{});
+  return go(std::integral_constant<int, 4>{});
 }
 
 }  // namespace
@@ -928,16 +953,8 @@ cudaError_t paged_configure() {
 }
 
 cudaError_t launch_paged_join(const PagedParams& p, int D, int ctas, cudaStream_t st) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(ctas, p.part_rows / 32, 1);
-  cfg.blockDim = dim3(256, 1, 1);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return D == 64 ? cudaLaunchKernelEx(&cfg, paged_join_kernel<64>, p) : cudaLaunchKernelEx(&cfg, paged_join_kernel<128>, p);
+  return paged_launch(D == 64 ? paged_join_kernel<64> : paged_join_kernel<128>, dim3(ctas, p.part_rows / (8 * kJoinRows), 1),
+                      256, 0, st, p);
 }
 
 int paged_attention_ctas(bool e4m3, int row_blocks, int sms) {

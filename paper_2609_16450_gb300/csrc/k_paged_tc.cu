@@ -30,7 +30,7 @@ namespace ebd {
 
 namespace {
 
-constexpr int kStep = 128;     // keys of a step
+constexpr int kStep = 1 << kPagedTcStepLog2;     // keys of a step
 constexpr int kThreads = 512;
 constexpr int kLeast = 4;      // steps of a share, at least
 constexpr int kNever = 0x7fffffff;
@@ -192,7 +192,7 @@ struct Map {
   // and o free of 2 streams; q full, ready, empty; drain and turn of 2 streams
   static constexpr int kNBar = 2 * kKs + kFs + 4 * kVs + 8 + 7;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
-  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + 2 * (kThreads / 32) * 8;
+  static constexpr uint32_t kMisc = kPlan + sizeof(PagedStart) + (kThreads / 32) * 4;
   static constexpr uint32_t kBytes = kMisc + 32;
   static constexpr uint32_t kDyn = kBytes + 1024;
   static_assert(kDyn <= 227 * 1024 && 2 * kTile >= 128 * 64 * 4 + kTile, "shared memory");
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain = q_empty + 1;   // [2]
   uint64_t* turn = drain + 2;      // [2]
   PagedStart* plan = reinterpret_cast<PagedStart*>(smem + L::kPlan);
-  auto& scan = *reinterpret_cast<unsigned long long(*)[2][kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
+  auto& scan = *reinterpret_cast<unsigned(*)[kThreads / 32]>(smem + L::kPlan + sizeof(PagedStart));
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMisc);
   volatile int* abort = reinterpret_cast<volatile int*>(smem + L::kMisc + 4);
   int* s_bad = reinterpret_cast<int*>(smem + L::kMisc + 16);  // [kBads] by item
@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_mbar_init();
   }
   for (int i = tid; i < kBads * 3 * D; i += kThreads) bad[i] = kNever;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (warp == 13) tmem_alloc(tmem_holder, kTmemCols);
   tc_fence_before();
   paged_plan<kThreads>(p, T, kStep, kLeast, plan, scan);  // ends in a barrier of all threads
@@ -328,11 +329,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         const int lim = lim_last();
         const int* table = p.page_table + static_cast<long long>(w.b) * p.max_pages;
-        int win0 = -32, win = 0;  // page ids of 32 pages, one per lane
+        int win0 = ((w.c0 * kStep) >> p.page_log2) & ~31;  // page ids of 32 pages, one per lane
+        int win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
         for (int c = w.c0; c < w.c1; ++c, ++n) {
           const int key = c * kStep + key_in;
           const int first = (c * kStep) >> p.page_log2;
-          if (first >= win0 + 32 || first < win0) {
+          if (first >= win0 + 32) {
             win0 = first & ~31;
             win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
           }
@@ -1003,10 +1005,8 @@ cudaError_t paged_tc_configure() {
 cudaError_t launch_paged_tc(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p,
                             bool e4m3, bool one, int sms, cudaStream_t st) {
   if (e4m3)
-    paged_tc_kernel<128, true><<<sms, kThreads, Map<128, true>::kDyn, st>>>(q, k, v, p, one ? 1 : 0);
-  else
-    paged_tc_kernel<128, false><<<sms, kThreads, Map<128, false>::kDyn, st>>>(q, k, v, p, one ? 1 : 0);
-  return cudaGetLastError();
+    return paged_launch(paged_tc_kernel<128, true>, sms, kThreads, Map<128, true>::kDyn, st, q, k, v, p, one ? 1 : 0);
+  return paged_launch(paged_tc_kernel<128, false>, sms, kThreads, Map<128, false>::kDyn, st, q, k, v, p, one ? 1 : 0);
 }
 
 }  // namespace ebd

@@ -26,14 +26,31 @@ struct PagedRowsParams {
   long long kv_stride;         // elements from row to row
   const uint8_t* skip;         // [R] or null
 };
-cudaError_t launch_paged_write(const PagedRowsParams& p, cudaStream_t st);
-cudaError_t launch_paged_read(const PagedRowsParams& p, cudaStream_t st);
+// Every kernel of the paged cache is a programmatic dependent of the one before
+// it on the stream: it reads global memory only after griddepcontrol.wait, and
+// lets the next one's blocks in as soon as it has read its plan.
+template <class... A>
+cudaError_t paged_launch(void (*kernel)(A...), dim3 grid, int threads, uint32_t smem, cudaStream_t st, const A&... a) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a...);
+}
+cudaError_t launch_paged_write(const PagedRowsParams& p, int sms, cudaStream_t st);
+cudaError_t launch_paged_read(const PagedRowsParams& p, int sms, cudaStream_t st);
 
 // ------------------------------------------------------------------ attention
 // A tile in parts: the first is part 2 c + 1 of the CTA c that it begins in, the
 // k-th after it part 2 (c + k).
 struct PagedCut {
-  int parts;  // 0: none
+  int parts, first;     // their number (0: none), and the CTA of the first
   int rows, m0, r0, h;  // packed rows, the first of them, the sequence's first row, K/V head
 };
 struct PagedParams {
@@ -60,7 +77,7 @@ struct PagedParams {
   uint64_t limit_ns;
 };
 // Rows of a tile and CTAs per SM of the two kernels, at most (their workspace).
-constexpr int kPagedRows = 64, kPagedCtasPerSm = 3;  // mma.sync
+constexpr int kPagedRows = 64, kPagedCtasPerSm = 4;  // mma.sync
 constexpr int kPagedTcRows = 256;                    // tcgen05, one CTA per SM
 constexpr int kPagedTcGroup = 128;                   // query heads of a group that the tcgen05 kernel takes
 constexpr int kPagedUncutKeys = 256;                 // caches of so many keys per sequence: tiles stay whole
@@ -72,9 +89,8 @@ cudaError_t launch_paged_tc(const CUtensorMap& q, const CUtensorMap& k, const CU
 // the parts of cut tiles put together, a programmatic dependent of either kernel of `ctas` CTAs
 cudaError_t launch_paged_join(const PagedParams& p, int D, int ctas, cudaStream_t st);
 int paged_attention_ctas(bool e4m3, int row_blocks, int sms);
-// keys of a chunk of the mma.sync kernel: what a chunk costs besides its products
-// is the same, so as many as shared memory holds three operands of
-constexpr int paged_chunk_keys(bool e4m3, int row_blocks) { return e4m3 && row_blocks < 2 ? 128 : 64; }
+constexpr int kPagedChunkLog2 = 6;                   // keys of a chunk of the mma.sync kernel
+constexpr int kPagedTcStepLog2 = 7;                  // and of a step of the tcgen05 kernel
 cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, const PagedParams& p, int D,
                                    bool e4m3, int row_blocks, int sms, cudaStream_t st);
 
@@ -85,9 +101,10 @@ cudaError_t launch_paged_attention(const CUtensorMap& k, const CUtensorMap& v, c
 // work is its chunks of CH keys (one at least).  All chunks, in that order, are
 // cut into equal contiguous shares, one per CTA, so that ragged lengths and few
 // long sequences load every SM alike; a tile cut by a share's end leaves
-// partial results, which a second kernel puts together, a warp per row: by the
-// last CTA of the tile to finish, 19 parts of 252 rows took 190 us.  Where no
-// tile has many chunks, shares are of whole tiles (uncut), and there is none.
+// partial results, which a second kernel puts together, a warp per few rows.  (By
+// the last of the tile's CTAs instead, 19 parts of 252 rows took 190 us, and 2 or
+// 3 parts of 7 rows 2 us more than by the kernel.)  Where no tile has many chunks,
+// shares are of whole tiles (uncut), and there is nothing to join.
 struct PagedSeq {
   int r0, n, len;  // first row, rows, cached positions
   int tiles;
@@ -113,22 +130,23 @@ __device__ __forceinline__ int paged_chunks(const PagedParams& p, const PagedSeq
   const int last = min(s.n - 1, paged_row(p, (t + 1) * T - 1));
   return max(1, (paged_limit(p, s, last) + CH - 1) / CH);
 }
-__device__ __forceinline__ unsigned long long paged_units(const PagedParams& p, const PagedSeq& s, int T, int CH) {
+__device__ __forceinline__ unsigned paged_units(const PagedParams& p, const PagedSeq& s, int T, int CH) {
   unsigned u = 0;
   if (s.n == 0) return 0;
+  if (p.uncut) return s.tiles * p.Hkv;
   if (!p.causal)
     u = s.tiles * static_cast<unsigned>(paged_chunks(p, s, 0, T, CH));
   else
     for (int t = 0; t < s.tiles; ++t) u += paged_chunks(p, s, t, T, CH);
-  return static_cast<unsigned long long>(u) * p.Hkv;
+  return u * p.Hkv;
 }
 
 // Where a CTA's share begins (in shared memory, written by paged_plan).  With q =
 // total / shares and r = total % shares, the first r shares have q + 1 units.
+// (The host sees to it that units fit 31 bits.)
 struct PagedStart {
-  unsigned total, q, r;
+  unsigned q, r;
   unsigned u0, u1;          // this CTA's units are [u0, u1)
-  int uncut;                // units are tiles
   int b, t, h, c;           // sequence, tile, head and chunk of u0
 };
 __device__ __forceinline__ unsigned paged_share(const PagedStart& st, unsigned c) { return c * st.q + min(c, st.r); }
@@ -138,69 +156,50 @@ __device__ __forceinline__ int paged_owner(const PagedStart& st, unsigned u) {
   return static_cast<int>(u < big ? u / (st.q + 1) : st.r + (u - big) / st.q);
 }
 // All NT threads of the block.  `least`: chunks of a share, at least, so that
-// a small call is not cut into more pieces than it is worth.  Calls of 2^31
-// chunks and more have whole tiles as units.
+// a small call is not cut into more pieces than it is worth.
 template <int NT>
 __device__ __forceinline__ void paged_plan(const PagedParams& p, int T, int CH, int least, PagedStart* st,
-                                           unsigned long long (&scan)[2][NT / 32]) {
+                                           unsigned (&scan)[NT / 32]) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (p.B + NT - 1) / NT;
   const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-  unsigned long long chunks = 0, tiles = 0;
-  for (int b = b0; b < b1; ++b) {
-    const PagedSeq s = paged_seq(p, b, T);
-    chunks += paged_units(p, s, T, CH);
-    tiles += static_cast<unsigned>(s.tiles * p.Hkv);
-  }
-  unsigned long long inc[2] = {chunks, tiles};
+  unsigned mine = 0;
+  for (int b = b0; b < b1; ++b) mine += paged_units(p, paged_seq(p, b, T), T, CH);
+  unsigned inc = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const unsigned long long v = __shfl_up_sync(0xffffffffu, inc[k], o);
-      if (lane >= o) inc[k] += v;
-    }
-  if (lane == 31) {
-    scan[0][warp] = inc[0];
-    scan[1][warp] = inc[1];
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
   }
+  if (lane == 31) scan[warp] = inc;
   __syncthreads();
-  unsigned long long all = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 32; ++w) all += scan[0][w];
-  const int uncut = p.uncut || all >> 31 ? 1 : 0;
   unsigned before = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) before += static_cast<unsigned>(scan[uncut][w]);
-    total += static_cast<unsigned>(scan[uncut][w]);
+    const unsigned v = scan[w];
+    if (w < warp) before += v;
+    total += v;
   }
-  const unsigned most = uncut ? total : (total + least - 1) / least;
+  const unsigned most = p.uncut ? total : (total + least - 1) / least;
   const unsigned shares = max(1u, min(most, gridDim.x));
-  PagedStart s0;
-  s0.total = total;
+  PagedStart s0{};
   s0.q = total / shares;
   s0.r = total - s0.q * shares;
-  s0.uncut = uncut;
-  s0.u0 = s0.u1 = 0;
   if (blockIdx.x < shares) {
     s0.u0 = paged_share(s0, blockIdx.x);
     s0.u1 = paged_share(s0, blockIdx.x + 1);
   }
   if (tid == 0) {
-    st->total = total;
     st->q = s0.q;
     st->r = s0.r;
-    st->uncut = uncut;
     st->u0 = s0.u0;
     st->u1 = s0.u1;
   }
-  const unsigned mine = static_cast<unsigned>(uncut ? tiles : chunks);
-  unsigned at = before + static_cast<unsigned>(uncut ? inc[1] : inc[0]) - mine;
+  unsigned at = before + inc - mine;
   if (s0.u0 < s0.u1 && s0.u0 >= at && s0.u0 < at + mine) {
     for (int b = b0; b < b1; ++b) {
       const PagedSeq s = paged_seq(p, b, T);
-      const unsigned u = uncut ? s.tiles * p.Hkv : static_cast<unsigned>(paged_units(p, s, T, CH));
+      const unsigned u = paged_units(p, s, T, CH);
       if (s0.u0 >= at + u) {
         at += u;
         continue;
@@ -208,7 +207,7 @@ __device__ __forceinline__ void paged_plan(const PagedParams& p, int T, int CH, 
       int t = 0;
       unsigned nch = 1;
       for (;; ++t) {
-        nch = uncut ? 1 : paged_chunks(p, s, t, T, CH);
+        nch = p.uncut ? 1 : paged_chunks(p, s, t, T, CH);
         if (s0.u0 < at + nch * p.Hkv) break;
         at += nch * p.Hkv;
       }
@@ -231,16 +230,14 @@ struct PagedWalk {
   int b, t, h;
   int c0, c1, nch;  // the piece: chunks [c0, c1) of the tile's nch
   int rt;
-  bool uncut;
   __device__ __forceinline__ int T() const { return CT != 0 ? CT : rt; }
   __device__ __forceinline__ void piece(const PagedParams& p, int c) {
     nch = paged_chunks(p, s, t, T(), CCH);
     c0 = c;
-    c1 = !uncut && u1 - u < static_cast<unsigned>(nch - c) ? c + static_cast<int>(u1 - u) : nch;
+    c1 = !p.uncut && u1 - u < static_cast<unsigned>(nch - c) ? c + static_cast<int>(u1 - u) : nch;
   }
   __device__ __forceinline__ bool begin(const PagedParams& p, const PagedStart& st, int T_) {
     rt = T_;
-    uncut = st.uncut != 0;
     u = st.u0;
     u1 = st.u1;
     if (u >= u1) return false;
@@ -252,7 +249,7 @@ struct PagedWalk {
     return true;
   }
   __device__ __forceinline__ bool next(const PagedParams& p) {
-    u += uncut ? 1 : c1 - c0;
+    u += p.uncut ? 1 : c1 - c0;
     if (u >= u1) return false;
     if (++h == p.Hkv) {
       h = 0;
@@ -268,20 +265,25 @@ struct PagedWalk {
   __device__ __forceinline__ bool whole() const { return c0 == 0 && c1 == nch; }
   // where this piece's partial result goes
   __device__ __forceinline__ int part() const { return 2 * static_cast<int>(blockIdx.x) + (c0 == 0 ? 1 : 0); }
-  // What this CTA's share leaves to be put together (one thread, at the
-  // share's last piece): the tile that it begins and does not end.
+  __device__ __forceinline__ PagedCut cut(const PagedParams& p, const PagedStart& st) const {
+    PagedCut x;
+    x.first = paged_owner(st, u - c0);
+    x.parts = paged_owner(st, u - c0 + nch - 1) - x.first + 1;
+    x.m0 = t * T();
+    x.rows = min(T(), s.n * p.group - x.m0);
+    x.r0 = s.r0;
+    x.h = h;
+    return x;
+  }
+  // The last piece of a share: the tile that it begins and does not end, to be
+  // put together (one thread).
   __device__ __forceinline__ void leave(const PagedParams& p, const PagedStart& st) const {
-    PagedCut cut{};
-    if (c0 == 0 && c1 < nch) {
-      cut.parts = paged_owner(st, u + nch - 1) - static_cast<int>(blockIdx.x) + 1;
-      cut.m0 = t * T();
-      cut.rows = min(T(), s.n * p.group - cut.m0);
-      cut.r0 = s.r0;
-      cut.h = h;
-    }
-    p.cuts[blockIdx.x] = cut;
+    PagedCut x{};
+    if (c0 == 0 && c1 < nch) x = cut(p, st);
+    p.cuts[blockIdx.x] = x;
   }
 };
+
 #endif
 
 }  // namespace ebd
