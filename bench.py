@@ -597,12 +597,13 @@ def run_loop_bench(args):
     mode = {"eb": 0, "threshold": 1, "topm": 2}[args.decode]
     full = full_sequence(sh)
     h = rt.Handle(lp.config_for_loop(sh, max_window=sh.gen_len if full else 64, decode_mode=mode,
-                                     top_m=args.top_m), w.w_emb)
+                                     top_m=args.top_m, paged=int(args.cache == "paged")), w.w_emb)
     if args.w_layout == "packed":
         w = rt.pack_weights(h, w)
     win = lambda s, p: synth.loop_window_inputs(sh, s, p)
     kv = lambda p: synth.loop_kv(sh, p)
-    opts = dict(keep=False, block=sh.l_b, cache=args.cache, append=args.append)
+    opts = dict(keep=False, block=sh.l_b, cache=args.cache, append=args.append,
+                kv_dtype=args.kv_dtype)
     if full:
         opts.update(window="full", attention=False)
     lp.run_loop(h, sh, w, win, kv, **opts)  # warm-up loop
@@ -628,7 +629,9 @@ def run_loop_bench(args):
                        "decode": args.decode + (f" (m={args.top_m})" if args.decode == "topm" else ""),
                        "fixed_block": sh.l_b if args.decode != "eb" else None,
                        "kv_cache": ("dual: the window also attends to the positions after it"
-                                    if args.cache == "dual" else "prefix") +
+                                    if args.cache == "dual" else
+                                    f"paged, {args.kv_dtype}: each step writes its window's rows and "
+                                    f"attends to the pages" if args.cache == "paged" else "prefix") +
                                    ("; committed rows appended to the cache by each step, which "
                                     "starts with the prompt only" if args.append and args.cache == "prefix"
                                     else "; committed rows appended by each step" if args.append else ""),
@@ -727,14 +730,20 @@ def main():
     ap.add_argument("--decode", choices=["eb", "threshold", "topm"], default="eb",
                     help="decision of the loop configs: EB, or a baseline's fixed-block rule")
     ap.add_argument("--top-m", type=int, default=1, help="commits per step of --decode topm")
-    ap.add_argument("--cache", choices=["prefix", "dual"], default="prefix",
-                    help="dual: each window also attends to the cached rest of its response")
+    ap.add_argument("--cache", choices=["prefix", "dual", "paged"], default="prefix",
+                    help="dual: each window also attends to the cached rest of its response; paged: "
+                         "the loop configs on a paged cache")
+    ap.add_argument("--kv-dtype", choices=["bf16", "e4m3"], default="bf16",
+                    help="what the pages of --cache paged hold")
     ap.add_argument("--append", action="store_true",
                     help="write committed rows' K/V into the cache every step")
     ap.add_argument("--w-layout", choices=["packed", "rowmajor"], default="packed",
                     help="W_lm tiled once by ebd_pack_lm_head (default) or row-major")
     args = ap.parse_args()
     args.warmup = max(args.warmup, 3)
+    if args.cache == "paged" and (args.append or args.impl == "reference" or
+                                  not args.config.startswith("loop_") or full_sequence(shape_for(args.config))):
+        ap.error("--cache paged is for the loop configs with windows, without --append")
 
     world = int(os.environ.get("WORLD_SIZE", "1"))
     rank = int(os.environ.get("RANK", "0"))

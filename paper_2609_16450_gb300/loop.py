@@ -11,6 +11,11 @@ first prefix + frontier rows (prefix cache) and, with cache='dual', also to
 the positions right of the window (dual cache, Sec. 6.3).  With append=True
 each step writes the K/V of the rows it commits into the cache
 (ebd_step_args.kv_append); the cache then starts with the prompt only.
+With cache='paged' the K/V live in a PagedCache: the prompt's rows are written
+into it piece by piece, every step writes its window's rows into pages reserved
+as the window moves on (ebd_paged_write) and attends to all positions up to the
+window's end (ebd_paged_attention), and the cache is read back at the end
+(ebd_paged_read).
 This module only marshals buffers; the window rule and every step of the
 method run in the library."""
 from __future__ import annotations
@@ -23,6 +28,7 @@ import torch
 
 from . import _ebd as E
 from . import runtime as rt
+from .paged import PagedCache
 
 MASK_TOKEN = -1
 
@@ -58,10 +64,10 @@ class LoopResult:
 
 
 def config_for_loop(shape, max_window: int = 64, decode_mode: int = E.EBD_DECODE_EB,
-                    top_m: int = 1) -> E.ebd_config:
+                    top_m: int = 1, paged: int = 0) -> E.ebd_config:
     return rt.config_for(shape, max_batch=1, max_window=max_window, max_rows=max_window,
                          max_prefix=shape.prefix + shape.gen_len, decode_mode=decode_mode,
-                         top_m=top_m)
+                         top_m=top_m, paged=paged)
 
 
 def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
@@ -69,20 +75,25 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
              max_steps: Optional[int] = None, max_window: int = 64,
              keep: bool = True, stream: Optional[torch.cuda.Stream] = None,
              block: int = 32, cache: str = "prefix", append: bool = False,
-             window: str = "block") -> LoopResult:
+             window: str = "block", page_size: int = 64, kv_dtype: str = "bf16") -> LoopResult:
     """window_inputs(step, positions) -> (hidden, q, k_win, v_win) as bf16 bit
     arrays; kv_rows(positions) -> (k, v).  Positions are absolute.  Under the
     handle's baseline decode modes the window is the active fixed block of
     `block` positions (ebd_loop_block_window).  cache: 'prefix' or 'dual';
     append: the step appends committed rows' K/V to the cache, which starts
     with the prompt's K/V only (with 'dual', with every position's, the
-    positions right of the window standing for the K/V a dual cache holds)."""
-    if cache not in ("prefix", "dual"):
-        raise ValueError("cache must be 'prefix' or 'dual'")
+    positions right of the window standing for the K/V a dual cache holds).
+    cache='paged' (a handle of ebd_config.paged = 1): pages of page_size
+    positions in kv_dtype, 'bf16' or 'e4m3'; the attention's outputs are bf16."""
+    if cache not in ("prefix", "dual", "paged"):
+        raise ValueError("cache must be 'prefix', 'dual' or 'paged'")
+    paged = cache == "paged"
+    if paged and append:
+        raise ValueError("the paged cache takes every window's rows: it has no append")
     if window not in ("block", "full"):
         raise ValueError("window must be 'block' or 'full'")
     full = window == "full"  # the full-sequence setting: the window is the whole response
-    if full and (attention or append):
+    if full and (attention or append or paged):
         raise ValueError("the full-sequence window runs without the window attention")
     fixed = h.cfg.decode_mode != E.EBD_DECODE_EB
     dev = "cuda"
@@ -116,13 +127,26 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
     attn_out = torch.empty((W, Hq, D), **f32) if attention else None
     kc = vc = None
     sfx = torch.zeros((2,), **i32)
-    if attention or append:
+    dense = not paged and (attention or append)
+    if dense:
         n0 = P0 if (append and cache == "prefix") else P0 + L
         kk, vv = kv_rows(np.arange(n0, dtype=np.int32))
         kc = torch.zeros((1, P0 + L, Hkv, D), dtype=torch.int16, device=dev)
         vc = torch.zeros((1, P0 + L, Hkv, D), dtype=torch.int16, device=dev)
         kc[0, :n0] = rt._dev(kk, dev).reshape(n0, Hkv, D)
         vc[0, :n0] = rt._dev(vv, dev).reshape(n0, Hkv, D)
+    if paged:
+        n_pages = (P0 + L + page_size - 1) // page_size
+        kv_len = torch.zeros((1,), **i32)
+        attn_p = torch.empty((W, Hq, D), dtype=torch.bfloat16, device=dev)
+        with torch.cuda.stream(stream):
+            pages = PagedCache(h, n_pages, 1, n_pages, page_size, kv_dtype)
+            pages.reserve(0, P0, stream)
+            for at in range(0, P0, W):  # the prompt, in pieces that the handle's rows hold
+                pos = np.arange(at, min(at + W, P0), dtype=np.int32)
+                kk, vv = kv_rows(pos)
+                pages.write(rt._dev(np.array([0, len(pos)], np.int32), dev), rt._dev(pos, dev),
+                            rt._dev(kk, dev).view(-1, Hkv, D), rt._dev(vv, dev).view(-1, Hkv, D), stream=stream)
     ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     res = LoopResult(tokens=None, steps=0)
     step = 0
@@ -151,13 +175,16 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
             pl.copy_(torch.tensor([P0 + lo], dtype=torch.int32))
             rp[:R].copy_(torch.from_numpy(positions))
             sfx.copy_(torch.tensor([P0 + hi, L - hi], dtype=torch.int32))
+            if paged:
+                kv_len.copy_(torch.tensor([P0 + hi], dtype=torch.int32))
+                pages.reserve(0, P0 + hi, stream)
         a = E.ebd_step_args()
         a.batch, a.rows = 1, R
         a.cu_rows, a.prefix_len, a.row_pos = cu.data_ptr(), pl.data_ptr(), rp.data_ptr()
         a.hidden, a.q, a.k_win, a.v_win = hid.data_ptr(), q.data_ptr(), kw.data_ptr(), vw.data_ptr()
-        if attention or append:
+        if dense:
             a.k_cache, a.v_cache = kc.data_ptr(), vc.data_ptr()
-        if attention:
+        if attention and not paged:
             a.attn_out = attn_out.data_ptr()
             if cache == "dual":
                 a.suffix = sfx.data_ptr()
@@ -175,6 +202,10 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
             snap = dict(tokens=tokens[lo:hi].cpu().numpy(), mask=mask_h[lo:hi].copy(),
                         in_block=ib_h[lo:hi].copy(), meta=meta_h.copy())
         ev0.record(stream)
+        if paged:
+            pages.write(cu, rp[:R], kw[:R], vw[:R], stream=stream)
+            if attention:
+                pages.attention(q[:R], cu, kv_len, attn_p[:R], stream=stream)
         E.check(E.ebd_step(h.h, a, sid), h.h)
         ev1.record(stream)
         st = h.sync_status(stream)
@@ -199,12 +230,24 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
                 argmax=argmax[:R].cpu().numpy(), conf=outs["conf"][:R].cpu().numpy(),
                 lbs_logit=outs["lbs_logit"][:R].cpu().numpy(),
                 lps_prob=outs["lps_prob"][:R].cpu().numpy(),
-                attn_out=attn_out[:R].cpu().numpy() if attention else None, device_us=us,
+                attn_out=((attn_p if paged else attn_out)[:R].float().cpu().numpy()
+                          if attention else None), device_us=us,
                 entropy=outs["entropy"][:R].cpu().numpy(), ent_norm=outs["ent_norm"][:R].cpu().numpy(),
                 gap=outs["gap"][:R].cpu().numpy(), before=snap, after=after))
         step += 1
     res.tokens = tokens.cpu().numpy()
     res.steps = step
+    if paged:
+        n = P0 + L
+        with torch.cuda.stream(stream):
+            kc, vc = (torch.empty((1, n, Hkv, D), dtype=torch.int16, device=dev) for _ in range(2))
+            for at in range(0, n, W):
+                pos = np.arange(at, min(at + W, n), dtype=np.int32)
+                pages.read(rt._dev(np.array([0, len(pos)], np.int32), dev), rt._dev(pos, dev),
+                           kc[0, at: at + W], vc[0, at: at + W], stream=stream)
+        st = h.sync_status(stream)
+        if st != 0:
+            raise E.EbdError(st, E.ebd_last_error(h.h))
     if kc is not None:
         res.k_cache, res.v_cache = kc[0].cpu().numpy(), vc[0].cpu().numpy()
     return res
