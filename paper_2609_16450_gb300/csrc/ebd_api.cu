@@ -1577,6 +1577,7 @@ ebd_status check_paged(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_arg
       (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)))
     return bad("an e4m3 cache needs k_scale and v_scale, 16-byte aligned");
   const int64_t page = static_cast<int64_t>(f.n_heads_kv) * c->page_size * f.head_dim;
+  if (page > 0x3fffffff) return fail(h, EBD_ERR_UNSUPPORTED, "a page of more than 2^30 elements");
   const int64_t per16 = c->dtype == EBD_KV_E4M3 ? 16 : 8;  // elements of 16 bytes
   if (c->page_stride != 0 && (c->page_stride < page || c->page_stride % per16 != 0))
     return bad("page_stride must be 0, or a page or more and a multiple of 16 bytes");

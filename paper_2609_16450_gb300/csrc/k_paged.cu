@@ -43,31 +43,39 @@ __device__ __forceinline__ bool row_slot(const PagedRowsParams& p, int r, long l
   return true;
 }
 
-// A piece of a row: 8 values of a head's K or V.
+// A piece of a row: 8 values of a head's K or V.  Its places within a row and
+// within a page fit 32 bits (the host sees to it): both kernels are bound by
+// what they issue as much as by what they move.
 template <int D>
 struct Piece {
   bool in, is_v;
-  int head, l;  // l: which 8
+  int j;  // of K's (V's) pieces of the row
   __device__ __forceinline__ Piece(const PagedRowsParams& p, int it) {
     const int per = p.Hkv * (D / 8);  // pieces of K, and of V
     in = it < 2 * per;
     is_v = it >= per;
-    const int j = is_v ? it - per : it;
-    head = j / (D / 8);
-    l = j % (D / 8);
+    j = is_v ? it - per : it;
   }
-  __device__ __forceinline__ __nv_bfloat16* row(const PagedRowsParams& p, int r) const {
-    return (is_v ? p.v : p.k) + r * p.kv_stride + head * D + l * 8;
+  __device__ __forceinline__ __nv_bfloat16* row(const PagedRowsParams& p, long long at) const {
+    return (is_v ? p.v : p.k) + at + j * 8;
   }
-  // element of the pools that it lies at in its page, and byte of the scales
-  __device__ __forceinline__ long long at(const PagedRowsParams& p, int off) const {
-    return ((static_cast<long long>(head) << p.page_log2) + off) * D + l * 8;
+  // element that it lies at in its page, and byte of the page's scales
+  __device__ __forceinline__ int at(const PagedRowsParams& p, int off) const {
+    return scale_at(p, off) * D + j % (D / 8) * 8;
   }
-  __device__ __forceinline__ uint8_t* pool(const PagedRowsParams& p, long long page) const {
-    return (is_v ? p.v_pool : p.k_pool) + page * p.page_stride;
+  __device__ __forceinline__ int scale_at(const PagedRowsParams& p, int off) const {
+    return ((j / (D / 8)) << p.page_log2) + off;
   }
-  __device__ __forceinline__ uint8_t* scale(const PagedRowsParams& p, long long page, int off) const {
-    return (is_v ? p.v_scale : p.k_scale) + (((page * p.Hkv + head) << p.page_log2) + off);
+};
+// The page in the pools and in the scales.
+struct Page {
+  uint8_t *k, *v, *ks, *vs;
+  __device__ __forceinline__ Page(const PagedRowsParams& p, long long page) {
+    k = p.k_pool + page * p.page_stride;
+    v = p.v_pool + page * p.page_stride;
+    const long long s = (page * p.Hkv) << p.page_log2;
+    ks = p.k_scale + s;
+    vs = p.v_scale + s;
   }
 };
 
@@ -75,6 +83,7 @@ template <int D, bool E4M3, int U>
 __global__ void __launch_bounds__(256) paged_write_kernel(const PagedRowsParams p) {
   constexpr int LPR = D / 8;  // lanes per row of a head, 8 values each
   const int r = blockIdx.x, it0 = blockIdx.y * U * blockDim.x + threadIdx.x;
+  const long long src = r * p.kv_stride;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const bool skip = p.skip != nullptr && p.skip[r] != 0;
@@ -83,41 +92,50 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const PagedRowsParams 
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const Piece<D> c(p, it0 + u * blockDim.x);
-    if (c.in) x[u] = __ldcs(reinterpret_cast<const uint4*>(c.row(p, r)));
+    if (c.in) x[u] = __ldcs(reinterpret_cast<const uint4*>(c.row(p, src)));
   }
   long long page;
   int off;
   if (!row_slot(p, r, page, off) || skip) return;
+  const Page pg(p, page);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const Piece<D> c(p, it0 + u * blockDim.x);
     if (!c.in) break;
+    uint8_t* pool = c.is_v ? pg.v : pg.k;
     if constexpr (!E4M3) {
-      *reinterpret_cast<uint4*>(c.pool(p, page) + c.at(p, off) * 2) = x[u];
+      *reinterpret_cast<uint4*>(pool + 2 * static_cast<long long>(c.at(p, off))) = x[u];
     } else {
       const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-      uint32_t amax = 0;  // bits of the largest |value|; past infinity's for NaN
-#pragma unroll
-      for (int i = 0; i < 4; ++i) amax = max(amax, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+      // bits of the largest |value|; past infinity's for NaN
+      uint32_t two = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu),
+                              __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
       // pieces of K and of V are multiples of LPR, and the block's threads of 32: a row's lanes are in it together
       const uint32_t lanes = (LPR == 16 ? 0xFFFFu : 0xFFu) << ((threadIdx.x & 31) & ~(LPR - 1));
 #pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(lanes, amax, o));
+      for (int o = LPR / 2; o > 0; o >>= 1) two = __vmaxu2(two, __shfl_xor_sync(lanes, two, o));
+      const uint32_t amax = max(two & 0xFFFFu, two >> 16);
       const bool finite = amax < 0x7F80u;
       const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 255;
       const float inv = __uint_as_float(static_cast<uint32_t>(254 - min(e, 247)) << 23);  // 2^(127 - e)
-      const float top = e == 247 ? 240.f : 448.f;
-      uint32_t code[2] = {0u, 0u};
+      float y[8];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float lo = __uint_as_float(w[i] << 16) * inv, hi = __uint_as_float(w[i] & 0xFFFF0000u) * inv;
-        const float2 y = make_float2(fminf(fmaxf(lo, -top), top), fminf(fmaxf(hi, -top), top));
-        const uint32_t c2 = __nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3);
-        code[i >> 1] |= c2 << (16 * (i & 1));
+        y[2 * i] = __uint_as_float(w[i] << 16) * inv;
+        y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) * inv;
       }
+      if (e == 247) {  // below, no code is past 448
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(y[i], -240.f), 240.f);
+      }
+      uint32_t code[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        code[i] = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i], y[4 * i + 1]), __NV_SATFINITE, __NV_E4M3) |
+                  __nv_cvt_float2_to_fp8x2(make_float2(y[4 * i + 2], y[4 * i + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
       if (!finite) code[0] = code[1] = 0x7F7F7F7Fu;
-      *reinterpret_cast<uint2*>(c.pool(p, page) + c.at(p, off)) = make_uint2(code[0], code[1]);
-      if (c.l == 0) *c.scale(p, page, off) = static_cast<uint8_t>(e);
+      *reinterpret_cast<uint2*>(pool + c.at(p, off)) = make_uint2(code[0], code[1]);
+      if (c.j % LPR == 0) (c.is_v ? pg.vs : pg.ks)[c.scale_at(p, off)] = static_cast<uint8_t>(e);
     }
   }
 }
@@ -125,11 +143,13 @@ __global__ void __launch_bounds__(256) paged_write_kernel(const PagedRowsParams 
 template <int D, bool E4M3, int U>
 __global__ void __launch_bounds__(256) paged_read_kernel(const PagedRowsParams p) {
   const int r = blockIdx.x, it0 = blockIdx.y * U * blockDim.x + threadIdx.x;
+  const long long dst = r * p.kv_stride;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   long long page = 0;
   int off = 0;
   const bool held = row_slot(p, r, page, off);
+  const Page pg(p, page);
   uint4 x[U];
   uint32_t e[U];
 #pragma unroll
@@ -138,13 +158,14 @@ __global__ void __launch_bounds__(256) paged_read_kernel(const PagedRowsParams p
     x[u] = make_uint4(0u, 0u, 0u, 0u);
     e[u] = 0;
     if (!c.in || !held) continue;
+    const uint8_t* pool = c.is_v ? pg.v : pg.k;
     if constexpr (!E4M3) {
-      x[u] = __ldcs(reinterpret_cast<const uint4*>(c.pool(p, page) + c.at(p, off) * 2));
+      x[u] = __ldcs(reinterpret_cast<const uint4*>(pool + 2 * static_cast<long long>(c.at(p, off))));
     } else {
-      const uint2 code = __ldcs(reinterpret_cast<const uint2*>(c.pool(p, page) + c.at(p, off)));
+      const uint2 code = __ldcs(reinterpret_cast<const uint2*>(pool + c.at(p, off)));
       x[u].x = code.x;
       x[u].y = code.y;
-      e[u] = *c.scale(p, page, off);
+      e[u] = (c.is_v ? pg.vs : pg.ks)[c.scale_at(p, off)];
     }
   }
 #pragma unroll
@@ -152,7 +173,7 @@ __global__ void __launch_bounds__(256) paged_read_kernel(const PagedRowsParams p
     const Piece<D> c(p, it0 + u * blockDim.x);
     if (!c.in) break;
     if constexpr (E4M3) {
-      const float scale = __uint_as_float(e[u] > 0 ? e[u] << 23 : 1u << 22);  // 2^(e - 127)
+      const float scale = __uint_as_float(max(e[u] << 23, 1u << 22));  // 2^(e - 127)
       uint32_t w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -164,7 +185,7 @@ __global__ void __launch_bounds__(256) paged_read_kernel(const PagedRowsParams p
       }
       x[u] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    *reinterpret_cast<uint4*>(c.row(p, r)) = x[u];
+    *reinterpret_cast<uint4*>(c.row(p, dst)) = x[u];
   }
 }
 

@@ -183,8 +183,8 @@ struct Map {
   static constexpr uint32_t kRaw = kV0 + kVs * kV;            // 8-bit V as loaded
   static constexpr uint32_t kKe = kRaw + (E4M3 ? kVs * kStep * D : 0);  // exponent bytes
   static constexpr uint32_t kVe = kKe + kKs * kStep;
-  static constexpr uint32_t kKf = kVe + kVs * kStep;          // [kFs][kStep] K's factors
-  static constexpr uint32_t kRowF = kKf + (E4M3 ? kFs * kStep * 2 : 0);  // [2][128]
+  static constexpr uint32_t kKf = kVe + kVs * kStep;          // [kFs][kStep] K's factors, f32
+  static constexpr uint32_t kRowF = kKf + (E4M3 ? kFs * kStep * 4 : 0);  // [2][128]
   static constexpr uint32_t kMl = kRowF + 2 * 128 * 4;        // [128][2] stream 1's (maximum, sum)
   static constexpr uint32_t kBad = kMl + 128 * 8;             // [kBads][3][D]
   static constexpr uint32_t kBar = kBad + kBads * 3 * D * 4;
@@ -541,8 +541,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int s = (vn + j) % L::kKs, fs = (vn + j) % L::kFs;
           ok = ok && mbar_wait(&kfull[s], static_cast<uint32_t>((vn + j) / L::kKs) & 1u, p.limit_ns, abort);
           ok = __all_sync(0xffffffffu, ok);
-          const uint32_t e = (smem + L::kKe)[s * kStep + r];  // 2^(e - 127) in bf16
-          reinterpret_cast<uint16_t*>(smem + L::kKf)[fs * kStep + r] = static_cast<uint16_t>(e > 0 ? e << 7 : 0x40u);
+          reinterpret_cast<float*>(smem + L::kKf)[fs * kStep + r] = scale_value((smem + L::kKe)[s * kStep + r]);
           __syncwarp();
           if (lane == 0) {
             mbar_arrive(&kfact[fs]);
@@ -675,49 +674,48 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = ok && mbar_wait(q_full, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort);
       ok = __all_sync(0xffffffffu, ok);
       if constexpr (E4M3) {
-        // q as two e4m3 terms, in place: the row's 128 bytes of columns 0..63
-        // become its high terms, those of 64..127 its low ones
+        // q as two e4m3 terms, in place, 8 lanes a row: the row's 128 bytes of columns
+        // 0..63 become its high terms, those of 64..127 its low ones.  (A thread per
+        // row, unrolled, took 14000 cycles, most of them to fetch the instructions.)
         if (x == 0 || (!one && mine > 0)) {
           uint8_t* q = smem + L::kQ + x * L::kTile;
-          uint4 v[D / 8];
-          uint32_t amax = 0;
+          const int c = lane & 7;
+#pragma unroll 1
+          for (int r = (warp & 3) * 4 + (lane >> 3); r < 128; r += 16) {
+            uint4 v[2];
+            uint32_t amax = 0;
 #pragma unroll
-          for (int c = 0; c < D / 8; ++c) {
-            v[c] = *reinterpret_cast<const uint4*>(q + (c >> 3) * 16384 + swz(row, c & 7));
-            const uint32_t u[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+            for (int k = 0; k < 2; ++k) {
+              v[k] = *reinterpret_cast<const uint4*>(q + (c >> 2) * 16384 + swz(r, (2 * c + k) & 7));
+              const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) amax = max(amax, max(u[k] & 0x7FFFu, (u[k] >> 16) & 0x7FFFu));
-          }
-          const bool finite = amax < 0x7F80u;
-          const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 127;
-          const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+              for (int e = 0; e < 4; ++e) amax = max(amax, max(u[e] & 0x7FFFu, (u[e] >> 16) & 0x7FFFu));
+            }
 #pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t h[4], l[4];
+            for (int o = 4; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            const bool finite = amax < 0x7F80u;
+            const int e = finite ? max(0, static_cast<int>(amax >> 7) - 8 + ((amax & 0x7Fu) > 0x60u ? 1 : 0)) : 127;
+            const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+            uint32_t h[4], lw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint4 vv = v[2 * c + (i >> 1)];
-              const uint32_t u0 = i & 1 ? vv.z : vv.x, u1 = i & 1 ? vv.w : vv.y;
+            for (int k = 0; k < 4; ++k) {
+              const uint4 vv = v[k >> 1];
+              const uint32_t u0 = k & 1 ? vv.z : vv.x, u1 = k & 1 ? vv.w : vv.y;
               const float a = __uint_as_float(u0 << 16) * inv, b = __uint_as_float(u0 & 0xFFFF0000u) * inv;
               const float cc = __uint_as_float(u1 << 16) * inv, d = __uint_as_float(u1 & 0xFFFF0000u) * inv;
               const uint32_t h0 = e4m3x2(a, b), h1 = e4m3x2(cc, d);
               const float2 f0 = e4m3x2_value(h0), f1 = e4m3x2_value(h1);
-              h[i] = finite ? h0 | (h1 << 16) : 0x7F7F7F7Fu;
-              l[i] = e4m3x2(a - f0.x, b - f0.y) | (e4m3x2(cc - f1.x, d - f1.y) << 16);
+              h[k] = finite ? h0 | (h1 << 16) : 0x7F7F7F7Fu;
+              lw[k] = e4m3x2(a - f0.x, b - f0.y) | (e4m3x2(cc - f1.x, d - f1.y) << 16);
             }
-            *reinterpret_cast<uint4*>(q + swz(row, c)) = make_uint4(h[0], h[1], h[2], h[3]);
-            *reinterpret_cast<uint4*>(q + 16384 + swz(row, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+            *reinterpret_cast<uint4*>(q + swz(r, c)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(q + 16384 + swz(r, c)) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+            if (c == 0) rowf[x * 128 + r] = scale_value(static_cast<uint32_t>(e)) * p.scale_log2;
           }
-          rowf[x * 128 + row] = scale_value(static_cast<uint32_t>(e)) * p.scale_log2;
           fence_async();
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(q_ready);
-        if (one && x == 1) {
-          ok = ok && mbar_wait(q_ready, static_cast<uint32_t>(items) & 1u, p.limit_ns, abort);
-          ok = __all_sync(0xffffffffu, ok);
-        }
-        f = rowf[(one ? 0 : x * 128) + row];
       }
       // Probabilities are taken against a reference `ref` near the row's running
       // maximum (2^(y - ref), y in log2 units): its first score's half step's
@@ -751,6 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if constexpr (E4M3)
           ok = ok && mbar_wait(&kfact[ks], static_cast<uint32_t>((kn + st) / L::kFs) & 1u, p.limit_ns, abort);
         ok = __all_sync(0xffffffffu, ok);
+        if (E4M3 && i == 0) f = rowf[(one ? 0 : x * 128) + row];  // there before S was begun
         tc_fence_after();
         // S(i) is complete, so P V of the step before it is: O may be rescaled
         if (__any_sync(0xffffffffu, pend)) rescale(pend ? alpha : 1.f);
@@ -758,14 +757,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         // scores 32 c .. 32 c + 31, once loaded: K's factors, what the row does not see
         auto finish = [&](int c, float* s) {
           if constexpr (E4M3) {
-            const uint4* kf = reinterpret_cast<const uint4*>(smem + L::kKf + (ks * kStep + 32 * c) * 2);
+            const float4* kf = reinterpret_cast<const float4*>(smem + L::kKf + (ks * kStep + 32 * c) * 4);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint4 k8 = kf[k];
-              const uint32_t u[4] = {k8.x, k8.y, k8.z, k8.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                mul2(s[8 * k + 2 * e], s[8 * k + 2 * e + 1], __uint_as_float(u[e] << 16), __uint_as_float(u[e] & 0xFFFF0000u));
+            for (int k = 0; k < 8; ++k) {
+              const float4 z = kf[k];
+              mul2(s[4 * k], s[4 * k + 1], z.x, z.y);
+              mul2(s[4 * k + 2], s[4 * k + 3], z.z, z.w);
             }
           }
           if (edge) {
