@@ -50,6 +50,20 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
   asm volatile(
@@ -292,10 +306,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       phase ^= 1u;
     }
   };
-  auto landed = [&](int slot, uint32_t phase) {
-    ok = ok && mbar_wait(&full[slot], phase, p.limit_ns, abort);
+  // A wait that finds its operand there costs 150 cycles, most of them the
+  // barrier's answer: asked for ahead (peek), it comes beside other work.
+  auto peek = [&](int slot, uint32_t phase) { return mbar_test(&full[slot], phase); };
+  auto landed = [&](int slot, uint32_t phase, bool there) {
+    ok = ok && (there || mbar_wait(&full[slot], phase, p.limit_ns, abort));
     ok = __all_sync(0xffffffffu, ok);
   };
+  bool v_there = false, k_there = false;
   do {
     const int m0 = w.t * T;
     const int mtot = w.s.n * p.group;
@@ -515,7 +533,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         }
       }
       // V of the chunk: waited for here, as its rows' scales go into P
-      landed(vslot, vphase);
+      landed(vslot, vphase, v_there);
+      k_there = c + 1 < w.c1 && peek(kslot, kphase);
       if constexpr (E4M3) {
         const uint8_t* sc = smem + L::kScale + vslot * CH + kb;
 #pragma unroll
@@ -556,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
             for (int nt = 0; nt < NK; ++nt) {
               const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -sub);
               const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -sub);
-              top = fmaxf(top, fmaxf(y0, y1));
+              top = max3(top, y0, y1);
               float e0 = ex2(y0), e1 = ex2(y1);
               ls[mb][hi] += e0 + e1;
               if constexpr (E4M3) {
@@ -637,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       constexpr bool EDGE = decltype(edge_c)::value;
       const int key0 = c * CH;
       const bool more = c + 1 < w.c1;
-      if (more) landed(kslot, kphase);
+      if (more) landed(kslot, kphase, k_there);
       scores(kslot, s);  // of the last chunk, what the slot holds: not used
       const uint8_t* vd = smem + L::kRing + vslot * L::kOp;
       const uint8_t* pd = smem + L::kP + (nchunk & 1) * T * CH * 2;
@@ -730,13 +749,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         if (more) mbar_arrive(&empty[kslot]);
       }
       step(vslot, vphase);
+      v_there = more && peek(vslot, vphase);
       if (more) step(kslot, kphase);
       ++nchunk;
     };
 
     float s[MB][NK][4];
-    landed(kslot, kphase);
+    landed(kslot, kphase, false);
     scores(kslot, s);
+    v_there = peek(vslot, vphase);
     __syncwarp();
     if (lane == 0) mbar_arrive(&empty[kslot]);
     step(kslot, kphase);
