@@ -21,15 +21,18 @@
 // becomes f16 after its row is scaled by a power of two so that its largest
 // element is in [2^14, 2^15): elements above 2^-29 of that are exact.  The key's
 // scale, a power of two, multiplies the score; that of a value's row multiplies
-// its probability, relative to the largest seen so far (a common power of two,
-// E0), so that the products stay in f16's range: at most 2^15, and to 2^-24 with
-// what f16's subnormals hold, 2^-39 of the largest.  O is multiplied by E0's
-// power at the end.
+// its probability, relative to the largest scale seen so far (a common power of
+// two, E0).  A row's probabilities are taken not against its largest score but
+// against its largest product of probability and value's scale, which becomes
+// 2^kUp: so f16 holds products down to 2^-31 of the row's own largest, whatever
+// other keys' values are.  The sum is of the same probabilities without the
+// scales, in 32 bits; scales count as 2^-40 E0 at least in that maximum, which
+// bounds it.  O is multiplied by E0's power at the end.
 // P is rounded to f16 (bf16 where the cache is); its sum is of the unrounded
 // values.
 //
-// The running maximum moves only when a score exceeds it by more than 8 (log2
-// units), so that exp2 stays below 256 and most chunks rescale nothing.
+// The running maximum moves only when a score (a product) exceeds it by more than
+// 8 (log2 units), so that exp2 stays below 256 and most chunks rescale nothing.
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -44,6 +47,8 @@ constexpr int kThreads = 160;
 constexpr int kLeastKeys = 192;     // keys of a share, at least
 constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
+constexpr float kUp = 7.f;          // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)
+constexpr int kSpan = 40;           // and of the scales' span that its reference follows
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -127,8 +132,7 @@ struct Map {
   static constexpr uint32_t kBad = kQF + kFrag;                   // [3][D]
   static constexpr uint32_t kXl = kBad + 3 * D * 4;               // [2][4][T] sums of the warps
   static constexpr uint32_t kXm = kXl + 2 * 4 * T * 4;            // [4][T] maxima of the warps
-  static constexpr uint32_t kXe = kXm + 4 * T * 4;                // [4] largest exponents of the warps
-  static constexpr uint32_t kRowF = kXe + 16;                     // [T] score factors of the rows
+  static constexpr uint32_t kRowF = kXm + 4 * T * 4;                     // [T] score factors of the rows
   static constexpr uint32_t kBar = kRowF + T * 4;
   static constexpr int kNBar = 2 * S + 2;
   static constexpr uint32_t kPlan = kBar + kNBar * 8;
@@ -291,7 +295,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   const int kb = warp * (CH / 4);  // this warp's keys of a chunk
   float* xm = reinterpret_cast<float*>(smem + L::kXm);
   float* xl = reinterpret_cast<float*>(smem + L::kXl);
-  [[maybe_unused]] int* xe = reinterpret_cast<int*>(smem + L::kXe);
   float* rowf = reinterpret_cast<float*>(smem + L::kRowF);
   int nchunk = 0;
   bool ok = true;
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     const int lim_hi = paged_limit(p, w.s, paged_row(p, m0 + rows - 1));
     const int len = w.s.len;
     const int par = pieces & 1;
-    [[maybe_unused]] int E0 = 0;  // exponent byte that values' scales are relative to
+    [[maybe_unused]] int E0 = 0;  // exponent byte that values' scales are relative to (O with them)
     const uint8_t* qd = smem + L::kQ;
     Rows<MB> R;
 #pragma unroll
@@ -551,12 +554,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       auto value_scale = [&](uint32_t e) {  // a row that is NaN: its codes do not say so to P V
         return e == 255u ? NAN : __uint_as_float(static_cast<uint32_t>(max(static_cast<int>(e) - E0 + 127, 0)) << 23);
       };
+      // log2 of a value's scale, as the row's reference counts it: a small integer n
+      // as the float n, from 1.5 * 2^23 + n (a conversion would be waited for)
+      auto value_log2 = [&](uint32_t e) {
+        return __int_as_float(0x4B400000 + max(static_cast<int>(e) - E0, -kSpan)) - 12582912.f;
+      };
       uint8_t* pd = smem + L::kP + (nchunk & 1) * T * CH * 2;
-      // probabilities against the running maxima, into shared memory, and their
-      // sums; the largest log2 of them
+      // probabilities against the running references, into shared memory, and their
+      // sums; the largest of them (8-bit caches: of their products with scales)
       float ls[MB][2];
       auto put_p = [&]() {
-        float top = -INFINITY;
+        float top = 0.f;
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) ls[mb][0] = ls[mb][1] = 0.f;
         [[maybe_unused]] float vs[NK][2];
@@ -570,12 +578,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int hi = 0; hi < 2; ++hi) {
-            const float sub = R.m[mb][hi] == -INFINITY ? 0.f : R.m[mb][hi];
+            const float sub = R.m[mb][hi] == -INFINITY ? 0.f : R.m[mb][hi] - (E4M3 ? kUp : 0.f);
 #pragma unroll
             for (int nt = 0; nt < NK; ++nt) {
               const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -sub);
               const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -sub);
-              top = max3(top, y0, y1);
               float e0 = ex2(y0), e1 = ex2(y1);
               ls[mb][hi] += e0 + e1;
               if constexpr (E4M3) {
@@ -583,6 +590,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
                 e0 = EDGE && s[mb][nt][2 * hi] == -INFINITY ? 0.f : e0 * vs[nt][0];
                 e1 = EDGE && s[mb][nt][2 * hi + 1] == -INFINITY ? 0.f : e1 * vs[nt][1];
               }
+              top = max3(top, e0, e1);
               const int r = mb * 16 + hi * 8 + g;
               const int k8 = warp * NK + nt;  // of the chunk's groups of 8 keys
               *reinterpret_cast<uint32_t*>(pd + (k8 >> 3) * T * 128 + r * 128 + (((k8 & 7) ^ g) << 4) + t4 * 4) =
@@ -592,19 +600,33 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         return top;
       };
       bool raise = fresh;
-      [[maybe_unused]] int emax = 0;
-      if constexpr (E4M3) {
+      if (!fresh) {
+        raise = put_p() > (E4M3 ? 32768.f : 256.f);
+        if constexpr (E4M3) {  // scales far past E0 (a NaN row's byte among them: rare enough)
+          uint32_t emax = 0;
 #pragma unroll
-        for (int nt = 0; nt < NK; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) emax = max(emax, ve[nt][e] == 255u ? 0 : static_cast<int>(ve[nt][e]));
+          for (int nt = 0; nt < NK; ++nt) emax = max(emax, max(ve[nt][0], ve[nt][1]));
+          raise = raise || static_cast<int>(emax) > E0 + 7;
+        }
       }
-      if (!fresh) raise = put_p() > 8.f || (E4M3 && emax > E0 + 7);
       if (barrier_or(1, 128, raise)) {
         // new running maxima, of all warps' scores, and E0
+        [[maybe_unused]] float dv[NK][2];
+        float down = 1.f, shift = 0.f;
         if constexpr (E4M3) {
-          const int top_e = __reduce_max_sync(0xffffffffu, emax);
-          if (lane == 0) xe[warp] = top_e;
+          static_assert(CH == 64, "two exponents per lane");
+          const uint32_t two = *reinterpret_cast<const uint16_t*>(smem + L::kScale + vslot * CH + 2 * lane);
+          uint32_t a = two & 0xFFu, b = two >> 8;
+          if (a == 255u || (EDGE && key0 + 2 * lane >= lim_hi)) a = 0u;
+          if (b == 255u || (EDGE && key0 + 2 * lane + 1 >= lim_hi)) b = 0u;
+          const int e = max(static_cast<int>(__reduce_max_sync(0xffffffffu, max(a, b))), E0);
+          down = __uint_as_float(static_cast<uint32_t>(max(E0 - e + 127, 0)) << 23);
+          shift = static_cast<float>(min(e - E0, kSpan));
+          E0 = e;
+#pragma unroll
+          for (int nt = 0; nt < NK; ++nt)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) dv[nt][k] = value_log2(ve[nt][k]);
         }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
@@ -614,24 +636,19 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
             for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) x = fmaxf(x, s[mb][nt][2 * hi + e] * R.f[mb][hi]);
+              for (int e = 0; e < 2; ++e)
+                x = fmaxf(x, E4M3 ? fmaf(s[mb][nt][2 * hi + e], R.f[mb][hi], dv[nt][e]) : s[mb][nt][2 * hi + e] * R.f[mb][hi]);
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
             x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
             if (t4 == 0) xm[warp * T + mb * 16 + hi * 8 + g] = x;
           }
         named_barrier(1, 128);
-        float down = 1.f;
-        if constexpr (E4M3) {
-          const int e = max(max(max(xe[0], xe[1]), max(xe[2], xe[3])), E0);
-          down = __uint_as_float(static_cast<uint32_t>(max(E0 - e + 127, 0)) << 23);
-          E0 = e;
-        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int hi = 0; hi < 2; ++hi) {
             const float* q = xm + mb * 16 + hi * 8 + g;
-            const float mn = fmaxf(R.m[mb][hi], fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T])));
+            const float mn = fmaxf(R.m[mb][hi] - shift, fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T])));
             const float alpha = mn == R.m[mb][hi] ? 1.f : ex2(R.m[mb][hi] - mn);  // 0 from -inf
             R.m[mb][hi] = mn;
             R.l[mb][hi] *= alpha;
@@ -800,7 +817,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           const int r = mb * 16 + hi * 8 + g;
           if (r >= rows) continue;
           const float l = (wl[r] + wl[T + r]) + (wl[2 * T + r] + wl[3 * T + r]);
-          float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          constexpr float one = E4M3 ? 1.f / 128.f : 1.f;  // 2^-kUp
+          float inv = !whole ? one : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
           // this lane's elements of the row: an 8-bit cache's NT columns of
           // fragment column 2 t4, then those of 2 t4 + 1, which follow on
           // them; a bf16 cache's columns 2 t4 and 2 t4 + 1 of each tile
@@ -809,9 +827,9 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              // an 8-bit cache's O is relative to E0 (two factors: each in range)
-              const float z = E4M3 ? o[mb][j][2 * hi + e] * scale_value(static_cast<uint32_t>(E0)) : o[mb][j][2 * hi + e];
-              x[E4M3 ? e * NT + j : 2 * j + e] = z * inv;
+              // an 8-bit cache's O is relative to E0
+              const float z = o[mb][j][2 * hi + e] * inv;
+              x[E4M3 ? e * NT + j : 2 * j + e] = E4M3 ? z * scale_value(static_cast<uint32_t>(E0)) : z;
             }
           if (any_bad) {
             const int lim = limit(mb, hi);
@@ -846,7 +864,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
                 *reinterpret_cast<float2*>(pd + j * 8 + 2 * t4) = make_float2(x[2 * j], x[2 * j + 1]);
             }
           }
-          if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(R.m[mb][hi], l);
+          if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(R.m[mb][hi], l * one);
         }
     }
     if (any_bad) {

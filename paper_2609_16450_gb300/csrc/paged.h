@@ -55,7 +55,7 @@ struct PagedCut {
 };
 struct PagedParams {
   int B, R, Hq, Hkv, group;
-  unsigned group_inv;          // ceil(2^32 / group): m / group = mulhi(m, group_inv) for m * group < 2^32
+  unsigned group_inv;          // ceil(2^32 / group): m / group = mulhi(m, group_inv) for m * group < 2^32 (4096 rows, 1024 heads at most)
   int causal;
   int page_log2, n_pages, max_pages;
   int cap;                     // positions of a sequence's pages

@@ -357,6 +357,22 @@ def test_attention_keys_that_rise(dtype):
     _check("mqa", dtype, 16, [90], [777], False, seed=2, edit=ramp, gains=(2.0, 1.0, 1.0))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n", [("dream", 3), ("tiny", 20), ("gqa64", 5), ("llada", 40), ("mqa", 100)])
+@pytest.mark.parametrize("what", ["wide", "zero"])
+def test_attention_values_of_wide_range(dtype, heads, n, what):
+    """Values from 2^-30 to 2^30, or none, position by position, and sharp scores:
+    a row's result is that of the keys it looks at, whatever the others hold."""
+    def wide(c):
+        rng = np.random.default_rng(12)
+        k, v = (_bf16(rng, (c.n_pages, c.hkv, c.page, c.D)) for _ in range(2))
+        by = (c.n_pages, c.hkv, c.page, 1)
+        f = np.exp2(rng.integers(-30, 31, by)) if what == "wide" else (rng.random(by) < 0.5) * 1.0
+        c.fill(k, (v * torch.from_numpy(f.astype(np.float32)).cuda()).bfloat16())
+
+    _check(heads, dtype, 64, [n], [700], False, seed=11, gains=(6.0, 1.0, 1.0), edit=wide)
+
+
 def test_attention_on_another_stream():
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
