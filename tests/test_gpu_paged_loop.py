@@ -130,3 +130,56 @@ def test_cache_on_a_stream_of_its_own():
                                  kv, 4, True, 0.125)
             assert bool(((out.double().cpu() - ref).abs() <= tol).all())
     h.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,rows,kv", [((28, 4, 128), [1, 1, 1], [300, 77, 2000]), ((32, 32, 128), [80, 70], [200, 900])])
+def test_calls_in_a_graph(dtype, heads, rows, kv):
+    """Write, attention and read captured together and replayed on new rows:
+    what the calls give one by one."""
+    from paper_2609_16450_gb300 import _ebd as E
+    from paper_2609_16450_gb300 import runtime as rt
+    from paper_2609_16450_gb300.paged import PagedCache
+    hq, hkv, D = heads
+    n, dev = sum(rows), "cuda"
+    h = pr.handle(E, rt, heads, len(rows), n)
+    g = torch.Generator(device=dev).manual_seed(3)
+    normal = lambda *s: torch.randn(s, generator=g, device=dev).bfloat16()
+    c = PagedCache(h, 64, len(rows), 40, 64, dtype)
+    for t in (c.k, c.v):
+        t.copy_(torch.randint(0, 120, t.shape, generator=g, device=dev) if dtype == "e4m3" else normal(*t.shape))
+    for t in (c.k_scale, c.v_scale):
+        if t is not None:
+            t.fill_(118)
+    for b, m in enumerate(kv):
+        c.reserve(b, m)
+    cu = torch.from_numpy(pr.cu_rows(rows)).cuda()
+    pos = torch.from_numpy(np.concatenate([np.arange(m - r, m) for r, m in zip(rows, kv)]).astype(np.int32)).cuda()
+    kvl = torch.tensor(kv, dtype=torch.int32, device=dev)
+    q, k, v = normal(n, hq, D), normal(n, hkv, D), normal(n, hkv, D)
+    out, bk, bv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+
+    def calls(stream):
+        c.write(cu, pos, k, v, stream=stream)
+        c.attention(q, cu, kvl, out, causal=True, max_new=max(rows), stream=stream)
+        c.read(cu, pos, bk, bv, stream=stream)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        calls(st)
+    for _ in range(3):
+        for t in (q, k, v):
+            t.copy_(normal(*t.shape))
+        for _ in range(4):
+            graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, bk, bv)]
+        calls(torch.cuda.current_stream())
+        assert h.sync_status() == 0
+        for a, b in zip(got, (out, bk, bv)):
+            assert torch.equal(a, b)
+        if dtype == "bf16":
+            assert torch.equal(bk, k) and torch.equal(bv, v)
+    h.close()
