@@ -1720,12 +1720,12 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   const bool e4m3 = c->dtype == EBD_KV_E4M3;
   // tcgen05 from 65 packed rows, as mma.sync then reads a tile's keys again for
   // every 64 (16 x 65 rows of 32 heads over 2113 keys: bf16 123 us against 300, 8
-  // bits 165 against 299); from 33 where caches are long (48 rows over 2096 keys,
-  // bf16 26.8 against 30.0; over 560, 25.6 against 21.2; 35 rows of a group over
-  // 30005 8-bit keys 45.5 against 53.9, 56 over 4104 31.3 against 27.7).  Up to 32,
-  // mma.sync: 16 x 32 rows over 2080 keys, bf16 96.5 against 117.7, 8 bits 81 and 163.
+  // bits 165 against 299); from 33 where caches are long (bf16: 4 x 48 rows over 948
+  // keys 31 against 37, 35 of a group over 605 20.5 against 15.4; 8 bits: 56 of a
+  // group over 4008 23 against 29, 16 x 48 rows over 948 111 against 90).  Up to 32,
+  // mma.sync: 16 x 32 rows over 2080 keys, bf16 96 against 118, 8 bits 81 and 163.
   const bool wide = f.head_dim == 128 && p.group <= kPagedTcGroup &&
-                    (m > 64 || (m > 32 && p.cap > (e4m3 ? 4 * kPagedLongKeys : kPagedLongKeys)));
+                    (m > 64 || (m > 32 && p.cap > (e4m3 ? kPagedLongKeysE4m3 : kPagedLongKeys)));
   // keys of a tensor-map box: a page, or a chunk's part of it
   const int mb = m <= 16 ? 1 : m <= 32 ? 2 : 4;
   const int chunk_log2 = wide ? kPagedTcStepLog2 : kPagedChunkLog2;

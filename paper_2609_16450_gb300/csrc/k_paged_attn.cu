@@ -4,13 +4,13 @@
 //
 // A tile is up to 16, 32 or 64 packed rows (row of the sequence, query head of
 // the group) of one sequence and K/V head.  Each CTA takes an equal share of
-// all tiles' chunks of 64 keys, or 128 of an 8-bit cache (paged.h).
+// all tiles' chunks of 64 keys (paged.h).
 //   warp 4: loads.  The rows of q, and per chunk K and V as TMA boxes of a
 //     page (or a chunk's part of it), each operand into a slot of one ring.
 //   warps 0-3: the scores of a quarter of every chunk's keys each; the probabilities
 //     meet in shared memory, and each warp multiplies all of them with D / 4
 //     columns of V.  A warp's output is then D / 4 columns, not D, which keeps
-//     a tile of 32 rows within the registers of two or three CTAs per SM, and
+//     a tile of 32 rows within the registers of two to four CTAs per SM, and
 //     no outputs have to meet when a tile ends.  One barrier per chunk.
 // Products run on mma.sync with fp32 sums.  The order of the contraction over
 // D is free, as long as q and k share it: a lane takes its K in 16-byte pieces
@@ -33,6 +33,13 @@
 //
 // The running maximum moves only when a score (a product) exceeds it by more than
 // 8 (log2 units), so that exp2 stays below 256 and most chunks rescale nothing.
+//
+// Measured, 128-wide heads: 64 tokens over ~4096 8-bit keys, 28 / 4 heads, 49.5 us
+// (207 MB: at the HBM rate once it streams; four CTAs per SM, with two 55.8); 16
+// tokens over ~2011 bf16 keys, 32 heads, 67 us (5.8 TB/s, the HBM rate); 64 windows
+// of 32 rows over ~1056 8-bit keys, 32 heads, 133 us (3.3 TB/s: latencies and issue,
+// 1110 cycles a chunk and SM, of which its MMAs are 518; three CTAs per SM, with
+// four 151, with two 190).
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -44,7 +51,11 @@ namespace ebd {
 namespace {
 
 constexpr int kThreads = 160;
-constexpr int kLeastKeys = 192;     // keys of a share, at least
+// Keys of a share, at least: 64, 128, 192, 384 take 32 rows over 632 keys of 32 heads
+// 16.0, 14.6, 16.3, 18.9 us, and where a tile is three shares of three chunks (544
+// keys) 128 takes 16.0 and 192 13.3; single tokens over 2001 keys of 28 / 4 heads
+// 17.3, 13.8, 13.5, 14.5.
+constexpr int kLeastKeys = 192;
 constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
 constexpr float kUp = 7.f;          // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)

@@ -84,7 +84,7 @@ constexpr int kPagedTcGroup = 128;                   // query heads of a group t
 // over 441 8-bit keys 10.3 us against 12.1, 16 x 32 rows over 472 30.9 against
 // 36.3; up to 1024, 32 rows over 982 would take 21.9 instead of 18.0).
 constexpr int kPagedUncutKeys = 512;
-constexpr int kPagedLongKeys = 1024;                 // and from here on caches are long (ebd_paged_attention)
+constexpr int kPagedLongKeys = 768, kPagedLongKeysE4m3 = 2048;  // past these caches are long (ebd_paged_attention)
 cudaError_t paged_configure();
 cudaError_t paged_tc_configure();
 // tcgen05, 128-wide heads; one: tiles of at most 128 rows, their steps in two streams
