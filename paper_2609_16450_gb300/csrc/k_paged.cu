@@ -20,8 +20,9 @@
 // search for the largest are one then: J = 2 where there are blocks enough for all
 // SMs, 1 where there are not, so that a window of 32 rows is spread over them.  A
 // write loads its rows while it looks its page up.  4096 rows of 32 128-wide heads
-// in 8 bits: written in 16.1 us (20.4 with K and V apart; J = 1 17.5, 4 19.6), 6.3
-// TB/s; read in 13.9 (17.4; 15.0, 15.7).
+// in 8 bits, on one set of buffers: written in 16.1 us (20.4 with K and V apart;
+// J = 1 17.5, 4 19.6), read in 13.9 (17.4; 15.0, 15.7); on several in turn 18.8 and
+// 18.4, 5.4 TB/s.
 #include <cuda_fp8.h>
 
 #include "paged.h"
