@@ -533,8 +533,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int n = w.c1 - w.c0;
       const int lo = lim_first(), hi = lim_last();
       int* badp = bad + (items % kBads) * 3 * D;
-      if (*reinterpret_cast<volatile int*>(&s_bad[items % kBads]) != 0) {  // of an item long done
-        named_barrier(2, 128);
+      // Notes of an item long done go first.  The four warps drift by up to two
+      // steps, so none may take a note of this item before all have looked:
+      // what they see, and the barrier below with it, would differ by warp.
+      const bool used = *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) != 0;
+      named_barrier(2, 128);
+      if (used) {
         for (int i = r; i < 3 * D; i += 128) badp[i] = kNever;
         if (r == 0) *reinterpret_cast<volatile int*>(&s_bad[items % kBads]) = 0;
         named_barrier(2, 128);

@@ -1,0 +1,66 @@
+"""The paged attention where its kernels' waits, references and records could go
+wrong: values that are not finite in many places, scores past what 32 bits
+resolve, values of very unequal size, calls that give up."""
+import math
+
+import numpy as np
+import pytest
+
+from tests import paged_ref as pr
+from tests.test_gpu_paged import HEADS, _close, _run
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def _reference(c, q, heads, lens, kv, causal, scale=0.0):
+    hq, hkv, D = HEADS[heads]
+    k, v = ([c.rows_of(i, b, m) for b, m in enumerate(kv)] for i in (0, 1))
+    return pr.attend(q.double(), k, v, lens, kv, hq // hkv, causal, scale or 1 / math.sqrt(D))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n,kv", [("llada", 100, 128), ("llada", 150, 256), ("mqa", 9, 128), ("dream", 37, 140)])
+def test_causal_nan_values_all_over_many_short_tiles(dtype, heads, n, kv):
+    """Tiles of one and two steps, several per SM, each with value rows that are
+    NaN among the keys that only some of its rows see, in the key ranges of
+    several warps: the rows before them are as without them."""
+    hq, hkv, D = HEADS[heads]
+    page, batch = 64, min(4096 // n, max(28, 500 // hkv))
+    lens, kvs = [n] * batch, [kv] * batch
+    rng = np.random.default_rng(17)
+    # (sequence, head, key, element): up to 5 a head
+    b, h = (x.ravel() for x in np.meshgrid(np.arange(batch), np.arange(hkv), indexing="ij"))
+    b, h = np.repeat(b, 5), np.repeat(h, 5)
+    keep = rng.random(b.size) < 0.6
+    b, h = b[keep], h[keep]
+    key = rng.integers(kv - n, kv, b.size)
+    d = rng.integers(0, D, b.size)
+    was = {}
+
+    def edit(c):
+        at = [torch.from_numpy(x.astype(np.int64)).cuda() for x in (c.table_h[b, key // page], h, key % page)]
+        was.update(at=at, v=c.v.clone(), vs=None if c.vs is None else c.vs.clone())
+        if dtype == "e4m3":
+            c.v[tuple(at)] = 0x7F
+            c.vs[tuple(at)] = 255
+        else:
+            c.v[tuple(at) + (torch.from_numpy(d).cuda(),)] = math.nan
+
+    c, q, out = _run(heads, dtype, page, lens, kvs, True, seed=21, edit=edit)
+    # first key of each (sequence, head, element) that is NaN
+    first = np.full((batch, hkv, D), kv + 1)
+    if dtype == "e4m3":
+        np.minimum.at(first, (b, h), key[:, None])
+    else:
+        np.minimum.at(first, (b, h, d), key)
+    limit = kv - n + np.arange(n) + 1
+    bad = limit[None, :, None, None] > first[:, None]                       # [batch][n][hkv][D]
+    bad = torch.from_numpy(np.repeat(bad, hq // hkv, axis=2).reshape(batch * n, hq, D)).cuda()
+    assert torch.isnan(out[bad].float()).all()
+    c.v.copy_(was["v"])
+    if c.vs is not None:
+        c.vs.copy_(was["vs"])
+    ref, tol = _reference(c, q, heads, lens, kvs, True)
+    _close(torch.where(bad, ref.bfloat16(), out), ref, tol)
