@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "paged.h"
+#include "paged_math.h"
 #include "ptx.cuh"
 
 namespace ebd {
@@ -89,12 +90,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 // two 32-bit floats at a time
-__device__ __forceinline__ void fma2(float& x, float& y, float f, float a) {
-  asm("{\n .reg .b64 v, m, c;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %2};\n mov.b64 c, {%3, %3};\n"
-      " fma.rn.f32x2 v, v, m, c;\n mov.b64 {%0, %1}, v;\n}"
-      : "+f"(x), "+f"(y)
-      : "f"(f), "f"(a));
-}
 __device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {
   asm("{\n .reg .b64 v, m;\n mov.b64 v, {%0, %1};\n mov.b64 m, {%2, %3};\n mul.rn.f32x2 v, v, m;\n"
       " mov.b64 {%0, %1}, v;\n}"
@@ -737,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // past `ref` (sums and O stay far inside 32 bits up to there), is a half
       // step done again, and `ref` moves first: by a whole number, so that
       // what P has of the step's first half scales exactly.  So the maximum is
-      // never waited for.
+      // never waited for.  (How far, and why a few moves are enough: paged_math.h.)
       float ref = 0.f, l = 0.f, alpha = 1.f;
       bool started = false, pend = false;  // a key seen; O to be scaled by alpha
       auto rescale = [&](float a) {
@@ -767,16 +762,23 @@ __global__ void __launch_bounds__(kThreads, 1)
         // S(i) is complete, so P V of the step before it is: O may be rescaled
         if (__any_sync(0xffffffffu, pend)) rescale(pend ? alpha : 1.f);
         pend = false;
-        // scores 32 c .. 32 c + 31, once loaded: K's factors, what the row does not see
+        // scores 32 c .. 32 c + 31, once loaded: times their factors, which are
+        // multiplied first, as either may be past what the other brings back into
+        // range; and what the row does not see
         auto finish = [&](int c, float* s) {
           if constexpr (E4M3) {
             const float4* kf = reinterpret_cast<const float4*>(smem + L::kKf + (ks * kStep + 32 * c) * 4);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-              const float4 z = kf[k];
+              float4 z = kf[k];
+              mul2(z.x, z.y, f, f);
+              mul2(z.z, z.w, f, f);
               mul2(s[4 * k], s[4 * k + 1], z.x, z.y);
               mul2(s[4 * k + 2], s[4 * k + 3], z.z, z.w);
             }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) mul2(s[k], s[k + 1], f, f);
           }
           if (edge) {
 #pragma unroll
@@ -789,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int h = 0; h < 2; ++h) {  // 64 keys; few instructions, that they stay cached
           uint32_t pk[32];
           float hs, ht;
-          for (;;) {
+          for (int moves = 0;; ++moves) {
             float s[2][32];
             tmem_ld32(ts + static_cast<uint32_t>(64 * h), s[0]);
             tmem_ld_wait<32>(s[0]);
@@ -801,8 +803,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               finish(2 * h + c, v);
 #pragma unroll
               for (int k = 0; k < 32; k += 4) {
-                fma2(v[k], v[k + 1], f, -ref);
-                fma2(v[k + 2], v[k + 3], f, -ref);
+                add2(v[k], v[k + 1], -ref, -ref);
+                add2(v[k + 2], v[k + 3], -ref, -ref);
                 t0 = max3(t0, v[k], v[k + 1]);
                 t1 = max3(t1, v[k + 2], v[k + 3]);
 #pragma unroll
@@ -817,17 +819,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             ht = fmaxf(t0, t1);
             hs = (a0 + a1) + (b0 + b1);
             // rows past the tile hold what memory held: they have no say
-            const bool again = valid && (started ? ht > 24.f : ht > -INFINITY);
+            const bool again = valid && moves < kPagedMoves && paged_far(ht, started);
             if (!__any_sync(0xffffffffu, again)) break;
             float a = 1.f;
             if (again) {
-              const float up = started ? ceilf(ht) : ht;
-              a = started ? ex2(-up) : 1.f;  // nothing to scale before a row's first key
-              ref += up;
+              const float lost = paged_move(ht, ref, started);
+              a = ex2(-lost);
               l *= a;
               sum *= a;
-              top -= up;
-              started = true;
+              top -= lost;
             }
             if (__any_sync(0xffffffffu, a != 1.f)) {
               if (i > 0) rescale(a);

@@ -64,3 +64,59 @@ def test_causal_nan_values_all_over_many_short_tiles(dtype, heads, n, kv):
         c.vs.copy_(was["vs"])
     ref, tol = _reference(c, q, heads, lens, kvs, True)
     _close(torch.where(bad, ref.bfloat16(), out), ref, tol)
+
+
+# packed rows on either kernel, over caches that are whole and cut into parts
+HUGE = [("llada", 70, 500), ("mqa", 20, 3000), ("dream", 40, 500), ("llada", 200, 3000)]
+
+
+def _bound(ref, v, lens, group):
+    """What rounding a probability and the result to bf16 may change (as in paged_ref.attend)."""
+    mag = torch.cat([vv.abs().mean(0).repeat_interleave(group, 0).expand(n, -1, -1) for n, vv in zip(lens, v)])
+    return 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -12) * mag + 1e-30
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n,kv", HUGE)
+@pytest.mark.parametrize("size", [1e4, 1e5, 1e9, 1e17])
+def test_equal_scores_of_any_size_share_alike(dtype, heads, n, kv, size):
+    """All keys of a head alike, with scores past what 32 bits resolve: every
+    row's result is its values' mean."""
+    hq, hkv, D = HEADS[heads]
+
+    def alike(c):
+        rng = np.random.default_rng(3)
+        k = torch.from_numpy(rng.standard_normal((1, hkv, 1, D)).astype(np.float32) * np.float32(size)).cuda()
+        v = torch.from_numpy(rng.standard_normal((c.n_pages, hkv, c.page, D)).astype(np.float32)).cuda()
+        c.fill(k.expand(c.n_pages, hkv, c.page, D).bfloat16().contiguous(), v.bfloat16())
+
+    c, q, out = _run(heads, dtype, 64, [n], [kv], False, seed=31, gains=(size, 1.0, 1.0), edit=alike)
+    v = [c.rows_of(1, 0, kv)]
+    ref = v[0].mean(0).repeat_interleave(hq // hkv, 0).expand(n, -1, -1)
+    _close(out, ref, _bound(ref, v, [n], hq // hkv))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n,kv", HUGE)
+@pytest.mark.parametrize("size", [1e4, 1e5, 1e9, 1e17])
+def test_scores_of_any_size_pick_the_largest(dtype, heads, n, kv, size):
+    """Scores past what 32 bits resolve: rows whose largest score stands out by
+    more than their rounding have that key's values, all have a mean of values."""
+    hq, hkv, D = HEADS[heads]
+    c, q, out = _run(heads, dtype, 64, [n], [kv], False, seed=32, gains=(size, size, 1.0))
+    k, v = (c.rows_of(i, 0, kv) for i in (0, 1))
+    o = out.double()
+    assert torch.isfinite(o).all()
+    for h in range(hq):
+        kk, vv = k[:, h // (hq // hkv)], v[:, h // (hq // hkv)]
+        s = q[:, h].double() @ kk.T / math.sqrt(D)
+        assert (o[:, h] <= vv.amax(0) + 2.0 ** -7 * vv.abs().amax(0)).all()
+        assert (o[:, h] >= vv.amin(0) - 2.0 ** -7 * vv.abs().amax(0)).all()
+        top = s.topk(2, -1)
+        # rounding of a score: 2^-17 of sum |q||k| scale (paged_ref.attend), twice
+        err = 2.0 ** -16 * (q[:, h].double().abs() @ kk.abs().T / math.sqrt(D)).amax(-1)
+        clear = top.values[:, 0] - top.values[:, 1] > err + 40.0
+        assert clear.any()
+        want = vv[top.indices[clear, 0]]
+        # P and its sum: one probability, rounded or not
+        assert ((o[clear, h] - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -30).all()
