@@ -834,6 +834,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (h == 1) {  // P of the first half: in place, exactly
                 const uint32_t a2 = bf16x2(a, a);
                 float q[32];
+                tmem_st_wait();  // its store, which loads do not wait for by themselves
                 tmem_ld32(ts, q);
                 tmem_ld_wait<32>(q);
 #pragma unroll

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from tests import paged_ref as pr
-from tests.test_gpu_paged import HEADS, _close, _run
+from tests.test_gpu_paged import HEADS, _args, _close, _lib, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -18,6 +18,20 @@ def _reference(c, q, heads, lens, kv, causal, scale=0.0):
     hq, hkv, D = HEADS[heads]
     k, v = ([c.rows_of(i, b, m) for b, m in enumerate(kv)] for i in (0, 1))
     return pr.attend(q.double(), k, v, lens, kv, hq // hkv, causal, scale or 1 / math.sqrt(D))
+
+
+def _attend(c, heads, q, lens, kv, causal=False):
+    """The attention of rows q over a cache that is there."""
+    E, rt = _lib()
+    h = pr.handle(E, rt, HEADS[heads], len(lens), sum(lens))
+    cu = torch.from_numpy(pr.cu_rows(lens)).cuda()
+    kvl = torch.tensor(kv, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 3.0)
+    a = _args(E, len(lens), sum(lens), cu, kv_len=kvl, q=q, out=out, causal=int(causal), max_new=max(lens))
+    E.check(E.ebd_paged_attention(h.h, c.pages(E), a, rt.stream_handle(None)), h.h)
+    assert h.sync_status() == 0
+    h.close()
+    return out
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
@@ -120,3 +134,42 @@ def test_scores_of_any_size_pick_the_largest(dtype, heads, n, kv, size):
         want = vv[top.indices[clear, 0]]
         # P and its sum: one probability, rounded or not
         assert ((o[clear, h] - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n,kv", [("llada", 70, 128), ("llada", 70, 300), ("llada", 200, 300), ("mqa", 20, 3000),
+                                        ("dream", 40, 128)])
+@pytest.mark.parametrize("gap", [26.0, 31.0])
+def test_second_halves_of_steps_far_above_the_first(dtype, heads, n, kv, gap):
+    """Of every 128 keys the last 64 score some 2^gap above the others, whose
+    values are as much larger: what a row has of a step's first half counts,
+    although its reference moves past 2^24 of it in the second."""
+    hq, hkv, D = HEADS[heads]
+    rng = np.random.default_rng(5)
+    # a direction per K/V head that q and the second halves' keys share
+    u = rng.standard_normal((hkv, D)).astype(np.float32)
+    u /= np.linalg.norm(u, axis=-1, keepdims=True)
+    want = gap * math.log(2) * math.sqrt(D)  # q . k
+
+    def edit(c):
+        k = rng.standard_normal((c.n_pages, hkv, c.page, D)).astype(np.float32) * 0.1
+        v = rng.standard_normal(k.shape).astype(np.float32)
+        for i in range(c.max_pages):
+            pg = int(c.table_h[0, i])
+            if i % 2:
+                k[pg] += 0.1 * want * u[:, None]
+            else:
+                v[pg] *= 2.0 ** gap
+        c.fill(torch.from_numpy(k).cuda().bfloat16(), torch.from_numpy(v).cuda().bfloat16())
+
+    c = pr.Cache(HEADS[heads], dtype, 64, [kv], seed=4)
+    edit(c)
+    q = np.repeat(10.0 * u, hq // hkv, axis=0)[None] + 0.3 * rng.standard_normal((n, hq, D))
+    q = torch.from_numpy(q.astype(np.float32)).cuda().bfloat16()
+    out = _attend(c, heads, q, [n], [kv])
+    ref, tol = _reference(c, q, heads, [n], [kv], False)
+    _close(out, ref, tol)
+    # both halves of the steps count
+    p = torch.softmax(q[:, 0].double() @ c.rows_of(0, 0, kv)[:, 0].T / math.sqrt(D), -1)
+    lo = p[:, torch.arange(kv, device="cuda") % 128 < 64].sum(-1) * 2.0 ** gap
+    assert 2.0 ** -4 < float(lo.median()) < 2.0 ** 4
