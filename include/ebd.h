@@ -94,6 +94,9 @@ typedef int32_t ebd_status;
 #define EBD_DEBUG_FORCE_COPY_TIMEOUT 2 /* ebd_step_host: the attention waits for
                                      a copy-stream ticket that is never
                                      written, with a 20 ms limit */
+#define EBD_DEBUG_PAGED_GIVE_UP 4 /* every second ebd_paged_attention of the
+                                     handle gives up its loads at once, as
+                                     after a wait that ran out */
 
 typedef struct {
   /* backbone shapes */

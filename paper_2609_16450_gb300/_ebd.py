@@ -22,6 +22,7 @@ EBD_ERR_STATE = -6
 EBD_ERR_BOUNDS = -7
 EBD_DEBUG_FORCE_TIMEOUT = 1
 EBD_DEBUG_FORCE_COPY_TIMEOUT = 2
+EBD_DEBUG_PAGED_GIVE_UP = 4
 EBD_DECODE_EB = 0
 EBD_DECODE_THRESHOLD = 1
 EBD_DECODE_TOPM = 2

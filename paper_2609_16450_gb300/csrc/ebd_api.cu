@@ -256,6 +256,7 @@ struct ebd_handle {
   float* paged_part = nullptr;
   float* paged_part_ml = nullptr;
   PagedCut* paged_cuts = nullptr;
+  bool paged_odd = false;            // EBD_DEBUG_PAGED_GIVE_UP: an odd number of calls so far
   // ebd_step_host: the attention's inputs on a copy engine (set up with the handle)
   int copy_route = -1;               // -1 not set up yet, 0 unavailable, 1 ready
   cudaStream_t s_copy = nullptr;
@@ -1712,6 +1713,10 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   p.cuts = h->paged_cuts;
   p.status = h->d_status;
   p.limit_ns = kLimitNs;
+  if (f.debug_flags & EBD_DEBUG_PAGED_GIVE_UP) {
+    p.give_up = h->paged_odd ? 1 : 0;
+    h->paged_odd = !h->paged_odd;
+  }
   // rows per tile: of the longest sequence, or, where that is unknown, of the mean one
   const int64_t longest = a->max_new > 0 && a->max_new < a->rows ? a->max_new
                           : a->max_new > 0                       ? a->rows

@@ -210,11 +210,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
   asm volatile("griddepcontrol.wait;" ::: "memory");
   paged_plan<kThreads>(p, T, CH, kLeastKeys / CH, plan, scan);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // no tile of this CTA's to be put together, until the thread that says so here
+  // has seen its share to the end: a share that is given up leaves no other call's
+  if (tid == 128) p.cuts[blockIdx.x] = PagedCut{};
   PagedWalk<T, CH> w;
-  if (!w.begin(p, *plan, T)) {
-    if (tid == 0) p.cuts[blockIdx.x] = PagedCut{};
-    return;
-  }
+  if (!w.begin(p, *plan, T)) return;
 
   if (warp == 4) {
     // ------------------------------------------------------------ loads
@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       int win = win0 + lane < p.max_pages ? table[win0 + lane] : -1;
       {  // q: rows by lane, zeros past the tile's last
         uint8_t* qd = smem + L::kQ;
-        ok = pieces == 0 || mbar_wait(qempty, static_cast<uint32_t>(pieces - 1) & 1u, p.limit_ns, abort);
+        ok = !p.give_up &&
+             (pieces == 0 || mbar_wait(qempty, static_cast<uint32_t>(pieces - 1) & 1u, p.limit_ns, abort));
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         for (int i = rows * (D / 8) + lane; i < T * (D / 8); i += 32)

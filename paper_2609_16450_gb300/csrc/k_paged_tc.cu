@@ -279,7 +279,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   PagedWalk<0, kStep> w;
   const bool work = w.begin(p, *plan, T);
-  if (!work && tid == 0) p.cuts[blockIdx.x] = PagedCut{};
+  // no tile to be put together yet (as in k_paged_attn.cu)
+  if (tid == 12 * 32) p.cuts[blockIdx.x] = PagedCut{};
   auto gave_up = [&]() {
     if (!*abort) {
       *abort = 1;
@@ -350,7 +351,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const int pieces = min(max((lim - c * kStep + box - 1) >> p.box_log2, 0), 1 << np_log);
           const int s = n % slots;
-          ok = n < slots || mbar_wait(&emptyb[s], static_cast<uint32_t>(n / slots - 1) & 1u, p.limit_ns, abort);
+          ok = !p.give_up &&
+               (n < slots || mbar_wait(&emptyb[s], static_cast<uint32_t>(n / slots - 1) & 1u, p.limit_ns, abort));
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           if (lane == 0)

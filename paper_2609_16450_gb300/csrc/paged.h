@@ -75,6 +75,7 @@ struct PagedParams {
   struct PagedCut* cuts;       // [CTAs] the tile that a CTA's share begins and others end
   int* status;
   uint64_t limit_ns;
+  int give_up;                 // tests: loads give up at once, as after a wait that ran out
 };
 // Rows of a tile and CTAs per SM of the two kernels, at most (their workspace).
 constexpr int kPagedRows = 64, kPagedCtasPerSm = 4;  // mma.sync

@@ -173,3 +173,42 @@ def test_second_halves_of_steps_far_above_the_first(dtype, heads, n, kv, gap):
     p = torch.softmax(q[:, 0].double() @ c.rows_of(0, 0, kv)[:, 0].T / math.sqrt(D), -1)
     lo = p[:, torch.arange(kv, device="cuda") % 128 < 64].sum(-1) * 2.0 ** gap
     assert 2.0 ** -4 < float(lo.median()) < 2.0 ** 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n", [("dream", 2), ("llada", 30), ("mqa", 40), ("dream", 40)])
+def test_a_call_that_gives_up_writes_nothing_of_an_earlier_one(dtype, heads, n):
+    """A call of two sequences over long caches, whose tiles are put together
+    from parts; then one of a single row or tile that gives up: it reports so, and
+    no row past its own is written.  The next call is as ever."""
+    E, rt = _lib()
+    hq, hkv, D = HEADS[heads]
+    kv = [4000, 9000]
+    rng = np.random.default_rng(8)
+    c = pr.Cache(HEADS[heads], dtype, 64, kv, seed=8)
+    x = [torch.from_numpy(rng.standard_normal((c.n_pages, hkv, 64, D)).astype(np.float32)).cuda().bfloat16() for _ in range(2)]
+    c.fill(*x)
+    q = torch.from_numpy(rng.standard_normal((2 * n, hq, D)).astype(np.float32)).cuda().bfloat16()
+    cfg = E.ebd_config(
+        d_model=64, vocab=64, n_heads_q=hq, n_heads_kv=hkv, head_dim=D, d_base=64, max_batch=2, max_window=1,
+        max_rows=2 * n, max_prefix=0, gen_len=1, g_max=5, l_min=8, l_b=32, eos_id=63, lps_enabled=1, tau=0.9,
+        tau_psi=0.89, debug_flags=E.EBD_DEBUG_PAGED_GIVE_UP, paged=1)
+    h = rt.Handle(cfg)
+    out = torch.full((2 * n, hq, D), 3.0, dtype=torch.bfloat16, device="cuda")
+
+    def call(lens):
+        cu = torch.from_numpy(pr.cu_rows(lens)).cuda()
+        kvl = torch.tensor(kv[: len(lens)], dtype=torch.int32, device="cuda")
+        a = _args(E, len(lens), sum(lens), cu, kv_len=kvl, q=q, out=out, max_new=max(lens))
+        E.check(E.ebd_paged_attention(h.h, c.pages(E), a, rt.stream_handle(None)), h.h)
+        return h.sync_status()
+
+    assert call([n, n]) == 0
+    ref, tol = _reference(c, q, heads, [n, n], kv, False)
+    _close(out, ref, tol)
+    out.fill_(5.0)
+    assert call([1]) == E.EBD_ERR_TIMEOUT
+    assert (out[1:] == 5.0).all()
+    assert call([n, n]) == 0
+    _close(out, ref, tol)
+    h.close()
