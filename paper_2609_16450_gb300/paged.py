@@ -84,7 +84,11 @@ def _rows(t: torch.Tensor, what: str, heads: int, dim: int) -> int:
         raise ValueError(f"{what}: bf16 [rows][{heads}][{dim}] expected, not {t.dtype} {list(t.shape)}")
     if t.shape[0] and (t.stride(2) != 1 or t.stride(1) != dim):
         raise ValueError(f"{what}: a row's heads must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    if t.shape[0] < 2:
+        return 0
+    if t.stride(0) < heads * dim:  # rows that overlap; a stride of 0 (an expanded row) is dense to the C calls
+        raise ValueError(f"{what}: rows must not overlap (stride {t.stride(0)} of rows of {heads * dim})")
+    return t.stride(0)
 
 
 class PagedCache:
@@ -140,8 +144,14 @@ class PagedCache:
             raise ValueError("more sequences than the table has")
         E.check(fn(self.h.h, self._struct, a, rt.stream_handle(stream)), self.h.h)
 
+    def _here(self, **tensors):
+        for what, t in tensors.items():
+            if t.device != self.k.device:
+                raise ValueError(f"{what} is on {t.device}, the cache on {self.k.device}")
+
     def _args(self, rows: int, cu_rows: torch.Tensor) -> E.ebd_paged_args:
         _ints(cu_rows, "cu_rows")
+        self._here(cu_rows=cu_rows)
         a = E.ebd_paged_args()
         a.batch, a.rows, a.cu_rows = cu_rows.numel() - 1, rows, cu_rows.data_ptr()
         return a
@@ -154,6 +164,7 @@ class PagedCache:
         if row_pos.numel() != k.shape[0]:
             raise ValueError("row_pos: one position per row")
         _ints(row_pos, "row_pos")
+        self._here(row_pos=row_pos, k=k, v=v)
         a.row_pos, a.k, a.v, a.kv_stride = row_pos.data_ptr(), k.data_ptr(), v.data_ptr(), stride
         return a
 
@@ -164,6 +175,7 @@ class PagedCache:
         if skip is not None:
             if skip.dtype not in (torch.uint8, torch.bool) or skip.numel() != a.rows or not skip.is_contiguous():
                 raise ValueError("skip: one byte per row")
+            self._here(skip=skip)
             a.skip = skip.data_ptr()
         self._call(E.ebd_paged_write, a, stream)
 
@@ -182,6 +194,7 @@ class PagedCache:
         _rows(out, "out", self.heads_q, self.dim)
         if out.shape != q.shape or not out.is_contiguous():
             raise ValueError("out: contiguous, of q's shape")
+        self._here(q=q, kv_len=kv_len, out=out)
         a.q, a.out, a.kv_len = q.data_ptr(), out.data_ptr(), kv_len.data_ptr()
         a.causal, a.scale, a.max_new = int(causal), scale, max_new
         self._call(E.ebd_paged_attention, a, stream)
