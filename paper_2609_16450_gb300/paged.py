@@ -49,7 +49,7 @@ class PageTable:
     def reserve(self, seq: int, length: int) -> bool:
         """Pages for positions [0, length) of a sequence; those it has stay.
         Says whether the table changed."""
-        self._check(seq)
+        self._check(seq, length)
         need = (length + self.page_size - 1) // self.page_size
         have = int(self.held[seq])
         if need > self.table.shape[1]:
@@ -64,7 +64,7 @@ class PageTable:
     def release(self, seq: int, length: int = 0) -> bool:
         """Gives back the pages past position `length`: of the whole sequence,
         or of what a rejected draft cached.  Says whether the table changed."""
-        self._check(seq)
+        self._check(seq, length)
         keep, have = (length + self.page_size - 1) // self.page_size, int(self.held[seq])
         for i in range(have - 1, keep - 1, -1):
             self._free.append(int(self.table[seq, i]))
@@ -72,9 +72,11 @@ class PageTable:
         self.held[seq] = min(have, keep)
         return keep < have
 
-    def _check(self, seq: int):
+    def _check(self, seq: int, length: int):
         if not 0 <= seq < self.table.shape[0]:
             raise ValueError(f"no sequence {seq}")
+        if length < 0:
+            raise ValueError(f"a length of {length}")
 
 
 def _rows(t: torch.Tensor, what: str, heads: int, dim: int) -> int:

@@ -74,3 +74,14 @@ def test_tensors_of_another_device_are_refused(cache):
         with pytest.raises(ValueError, match=what):
             cache.attention(**dict(here, **{what: here[what].to("meta")}))
     assert not cache.calls
+
+
+def test_lengths_below_zero_are_refused():
+    """A negative length would put the table's empty entries among the free pages."""
+    t = paged.PageTable(8, 2, 5, 16)
+    t.reserve(0, 20)
+    for call in (t.reserve, t.release):
+        for length in (-1, -16, -40):
+            with pytest.raises(ValueError, match="length"):
+                call(0, length)
+    assert t.release(0) and sorted(t._free) == list(range(8))
