@@ -602,8 +602,7 @@ AttnPlan attn_plan(const ebd_handle* h, int batch, int rows) {
 }
 
 ebd_status run_attention(ebd_handle* h, const ebd_step_args* a, cudaStream_t st,
-                         bool pdl = false, bool wait_prior = false, const unsigned* ready = nullptr,
-                         unsigned ready_ticket = 0) {
+                         bool pdl = false, const unsigned* ready = nullptr, unsigned ready_ticket = 0) {
   const ebd_config& c = h->cfg;
   const int D = c.head_dim, Hkv = c.n_heads_kv;
   CUtensorMap kc, vc, kw, vw;
@@ -657,7 +656,7 @@ ebd_status run_attention(ebd_handle* h, const ebd_step_args* a, cudaStream_t st,
   p.tickets = h->tickets;
   p.status = h->d_status;
   p.limit_ns = kLimitNs;
-  p.wait_prior = wait_prior ? 1 : 0;
+  p.wait_prior = pdl ? 1 : 0;
   p.ready = ready;
   p.ready_ticket = ready_ticket;
   if (ready != nullptr && (c.debug_flags & EBD_DEBUG_FORCE_COPY_TIMEOUT)) {
@@ -1237,10 +1236,9 @@ namespace {
 // attention feeds neither of the others, so unless every kernel is timed on
 // its own (profile mode 1) it is launched as a programmatic dependent of the
 // decision: it fills the SMs the decision's clusters leave idle.  The append
-// reads the mask the decision writes: it is a programmatic dependent of the
-// attention and waits for it, and the attention, in that case, waits for the
-// decision before it exits.  The attention reads no cache position the
-// append writes.
+// reads the mask the decision writes, as a paged write after the step may: they
+// are programmatic dependents of the attention and wait for it, and it completes
+// after the decision.  The attention reads no cache position the append writes.
 ebd_status step_run(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, const StepRoute* rt) {
   const bool attn = a->attn_out != nullptr;
   ebd_status s;
@@ -1262,12 +1260,11 @@ ebd_status step_run(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, cons
   if (prof == 1 && (e0 = record(h->ev[2], st)) != cudaSuccess)
     return cuda_fail(h, e0, "profile event");
   const bool pdl_attn = prof != 1;
-  if (attn && (s = run_attention(h, a, st, pdl_attn, a->kv_append != 0, rt ? rt->ready : nullptr,
-                                 rt ? rt->ready_ticket : 0u)) != EBD_OK)
+  if (attn && (s = run_attention(h, a, st, pdl_attn, rt ? rt->ready : nullptr, rt ? rt->ready_ticket : 0u)) != EBD_OK)
     return s;
   if (a->kv_append) {
     const ebd_config& c = h->cfg;
-    // a programmatic dependent only of a kernel that waits for the decision
+    // a programmatic dependent only of a kernel that completes after the decision
     e = launch_kv_append(a->k_cache, a->v_cache, a->k_win, a->v_win, a->cu_rows, a->row_pos,
                          rt != nullptr ? rt->mask_out : a->mask, a->batch, a->rows, c.max_prefix,
                          c.n_heads_kv * c.head_dim, st, attn && pdl_attn);

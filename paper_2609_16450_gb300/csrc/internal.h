@@ -62,7 +62,7 @@ struct AttnParams {
   int* tickets;             // [B*Hkv*max_qtiles]
   int* status;
   uint64_t limit_ns;
-  int wait_prior;           // every CTA waits for the grid it depends on before exiting
+  int wait_prior;           // completes after the grid that it is a programmatic dependent of
   const unsigned* ready;     // non-null: q and the window K/V are being copied in by
   unsigned ready_ticket;    // another stream, which then writes ready_ticket to *ready
 };
@@ -126,7 +126,7 @@ constexpr int kLmPairMinRows = 65;
 void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair = false);
 // pdl: launched as a programmatic dependent of the kernel before it on
 // `st` (that kernel's CTAs release it early; the attention reads nothing the
-// earlier kernel writes)
+// earlier kernel writes, and with p.wait_prior it completes after it)
 cudaError_t launch_attention(const CUtensorMap& kc, const CUtensorMap& vc, const CUtensorMap& kw,
                              const CUtensorMap& vw, const AttnParams& p, cudaStream_t st,
                              bool pdl = false);

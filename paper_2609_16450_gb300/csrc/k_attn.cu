@@ -1075,10 +1075,16 @@ __device__ __forceinline__ bool wait_ready(const AttnParams& p) {
   return s_ok != 0;
 }
 
-// The whole kernel; with p.wait_prior every CTA, whichever way it finishes,
-// waits for the grid it is a programmatic dependent of (the decision) before
-// it exits, so that a kernel launched after this one as its dependent sees
-// that grid complete as well.
+// With p.wait_prior this grid completes no earlier than the one that it is a
+// programmatic dependent of (the decision), so that a kernel launched after this
+// one as its dependent sees that grid complete as well: the grid's last CTA waits
+// for it before it exits (the others make room for CTAs yet to start).
+__device__ __forceinline__ void complete_after_prior(const AttnParams& p) {
+  if (p.wait_prior && blockIdx.x == gridDim.x - 1 && blockIdx.y == gridDim.y - 1 && blockIdx.z == gridDim.z - 1)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// The whole kernel.
 // PER_SM CTAs per SM: three take 168 registers a thread, which spills a few.
 template <int D, int PER_SM>
 __global__ void __launch_bounds__(kAttnThreads, PER_SM)
@@ -1086,7 +1092,7 @@ __global__ void __launch_bounds__(kAttnThreads, PER_SM)
                 const __grid_constant__ CUtensorMap tm_kw, const __grid_constant__ CUtensorMap tm_vw,
                 const AttnParams p) {
   if (p.ready == nullptr || wait_ready(p)) attn_body<D>(tm_kc, tm_vc, tm_kw, tm_vw, p);
-  if (p.wait_prior) asm volatile("griddepcontrol.wait;" ::: "memory");
+  complete_after_prior(p);
 }
 
 template <int D>
@@ -1095,7 +1101,7 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1)
                    const __grid_constant__ CUtensorMap tm_kw, const __grid_constant__ CUtensorMap tm_vw,
                    const AttnParams p) {
   if (p.ready == nullptr || wait_ready(p)) attn_tc_body<D>(tm_kc, tm_vc, tm_kw, tm_vw, p);
-  if (p.wait_prior) asm volatile("griddepcontrol.wait;" ::: "memory");
+  complete_after_prior(p);
 }
 
 cudaError_t attn_configure() {

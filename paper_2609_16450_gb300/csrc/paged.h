@@ -28,7 +28,9 @@ struct PagedRowsParams {
 };
 // Every kernel of the paged cache is a programmatic dependent of the one before
 // it on the stream: it reads global memory only after griddepcontrol.wait, and
-// lets the next one's blocks in as soon as it has read its plan.
+// lets the next one's blocks in as soon as it has read its plan.  A kernel before
+// it that is such a dependent itself has to complete after its own prior one (it
+// waits for it as here does every thread, or see complete_after_prior in k_attn.cu).
 template <class... A>
 cudaError_t paged_launch(void (*kernel)(A...), dim3 grid, int threads, uint32_t smem, cudaStream_t st, const A&... a) {
   cudaLaunchConfig_t cfg{};
