@@ -25,9 +25,9 @@
 // two, E0).  A row's probabilities are taken not against its largest score but
 // against its largest product of probability and value's scale, which becomes
 // 2^kUp: so f16 holds products down to 2^-31 of the row's own largest, whatever
-// other keys' values are.  The sum is of the same probabilities without the
-// scales, in 32 bits; scales count as 2^-40 E0 at least in that maximum, which
-// bounds it.  O is multiplied by E0's power at the end.
+// other keys' values are (scores past 2^22: paged_math.h).  The sum is of the same
+// probabilities without the scales, in 32 bits; scales count as 2^-40 E0 at least
+// in that maximum, which bounds it.  O is multiplied by E0's power at the end.
 // P is rounded to f16 (bf16 where the cache is); its sum is of the unrounded
 // values.
 //
@@ -44,6 +44,7 @@
 #include <type_traits>
 
 #include "paged.h"
+#include "paged_math.h"
 #include "ptx.cuh"
 
 namespace ebd {
@@ -58,7 +59,7 @@ constexpr int kThreads = 160;
 constexpr int kLeastKeys = 192;
 constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
-constexpr float kUp = 7.f;          // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)
+constexpr float kUp = kPagedUp;     // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)
 constexpr int kSpan = 40;           // and of the scales' span that its reference follows
 
 __device__ __forceinline__ float ex2(float x) {
@@ -156,8 +157,8 @@ struct Map {
 // What the chunks of a piece need: constant over a piece, or carried along.
 template <int MB>
 struct Rows {
-  float f[MB][2];     // score factor of rows g and g + 8 of each block
-  float m[MB][2];     // running maximum
+  float f[MB][2];     // 8-bit caches: the scores' power of two of rows g and g + 8 of each block
+  float m[MB][2];     // what is taken off the scores: the running maximum, or near it
   float l[MB][2];     // sum of this lane's probabilities
 };
 
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
       for (int hi = 0; hi < 2; ++hi) {
-        R.f[mb][hi] = p.scale_log2;
+        R.f[mb][hi] = 1.f;
         R.m[mb][hi] = -INFINITY;
         R.l[mb][hi] = 0.f;
       }
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           const float a = __uint_as_float(x[j][k] << 16) * up, b = __uint_as_float(x[j][k] & 0xFFFF0000u) * up;
           y[j][k] = finite ? f16x2(a, b) : 0x7FFF7FFFu;  // a row with a value that is not finite has NaN scores
         }
-      return scale_value(254u - e) * p.scale_log2;
+      return scale_value(254u - e);
     };
     // q as fragments: word pairs (2 i, 2 i + 1) of a row's pieces are A registers
     // hi and 2 + hi of contraction step i, in registers or shared memory
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           y[j][2] = x.z;
           y[j][3] = x.w;
         }
-        return p.scale_log2;
+        return 1.f;
       }
     };
     if constexpr (QREG) {
@@ -453,7 +454,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         for (int hi = 0; hi < 2; ++hi) R.f[mb][hi] = rowf[mb * 16 + hi * 8 + g];
     }
 
-    // scores of this warp's keys of the chunk in ring slot `slot`
+    // scores of this warp's keys of the chunk in ring slot `slot`, rounded in log2
+    // units (paged_math.h), but for a power of two per row in 8-bit caches
     auto scores = [&](int slot, float (&s)[MB][NK][4]) {
       const uint8_t* kd = smem + L::kRing + slot * L::kOp;
       // where there are few, two sums of each, so that MMAs wait less for one another
@@ -519,8 +521,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
         for (int nt = 0; nt < NK; ++nt) {
           const uint32_t two = *reinterpret_cast<const uint16_t*>(sc + nt * 8 + 2 * t4);
-          ks[nt][0] = scale_value(two & 0xFFu);
-          ks[nt][1] = scale_value(two >> 8);
+          ks[nt][0] = scale_value(two & 0xFFu) * p.scale_log2;
+          ks[nt][1] = scale_value(two >> 8) * p.scale_log2;
         }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
@@ -528,6 +530,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[mb][nt][i] *= ks[nt][i & 1];
+      } else {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+          for (int nt = 0; nt < NK; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[mb][nt][i] = __fmul_rn(s[mb][nt][i], p.scale_log2);
       }
     };
 
@@ -575,6 +584,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
       // probabilities against the running references, into shared memory, and their
       // sums; the largest of them (8-bit caches: of their products with scales)
       float ls[MB][2];
+      auto log2_score = [&](int mb, int hi, int nt, int e, float add) {
+        const float y = s[mb][nt][2 * hi + e];
+        return E4M3 ? fmaf(y, R.f[mb][hi], add) : __fadd_rn(y, add);
+      };
       auto put_p = [&]() {
         float top = 0.f;
 #pragma unroll
@@ -590,12 +603,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int hi = 0; hi < 2; ++hi) {
-            const float sub = R.m[mb][hi] == -INFINITY ? 0.f : R.m[mb][hi] - (E4M3 ? kUp : 0.f);
+            const float sub = R.m[mb][hi] == -INFINITY ? 0.f : R.m[mb][hi];
 #pragma unroll
             for (int nt = 0; nt < NK; ++nt) {
-              const float y0 = fmaf(s[mb][nt][2 * hi], R.f[mb][hi], -sub);
-              const float y1 = fmaf(s[mb][nt][2 * hi + 1], R.f[mb][hi], -sub);
-              float e0 = ex2(y0), e1 = ex2(y1);
+              float e0 = ex2(log2_score(mb, hi, nt, 0, -sub)), e1 = ex2(log2_score(mb, hi, nt, 1, -sub));
               ls[mb][hi] += e0 + e1;
               if constexpr (E4M3) {
                 // what a row does not see stays out, whatever its scale is
@@ -640,27 +651,45 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
             for (int k = 0; k < 2; ++k) dv[nt][k] = value_log2(ve[nt][k]);
         }
+        // the largest of this warp's keys' scores (8-bit caches: with their values'
+        // scales, but for the scores themselves where those are coarse) by row;
+        // says whether any is
+        auto largest = [&](auto plain_c) {
+          constexpr bool PLAIN = decltype(plain_c)::value;
+          bool any = false;
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
+          for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-          for (int hi = 0; hi < 2; ++hi) {
-            float x = -INFINITY;
+            for (int hi = 0; hi < 2; ++hi) {
+              float x = -INFINITY;
 #pragma unroll
-            for (int nt = 0; nt < NK; ++nt)
+              for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
-              for (int e = 0; e < 2; ++e)
-                x = fmaxf(x, E4M3 ? fmaf(s[mb][nt][2 * hi + e], R.f[mb][hi], dv[nt][e]) : s[mb][nt][2 * hi + e] * R.f[mb][hi]);
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            if (t4 == 0) xm[warp * T + mb * 16 + hi * 8 + g] = x;
+                for (int e = 0; e < 2; ++e) x = fmaxf(x, log2_score(mb, hi, nt, e, E4M3 && !PLAIN ? dv[nt][e] : 0.f));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+              any = any || fabsf(x) >= kPagedCoarse;  // (-inf with them: then nothing changes)
+              float* at = xm + warp * T + mb * 16 + hi * 8 + g;
+              if (t4 == 0 && (!PLAIN || paged_coarse(*at))) *at = x;
+            }
+          return any;
+        };
+        const bool coarse = largest(std::false_type{});
+        if constexpr (E4M3) {
+          if (barrier_or(1, 128, coarse)) {
+            largest(std::true_type{});
+            named_barrier(1, 128);
           }
-        named_barrier(1, 128);
+        } else {
+          named_barrier(1, 128);
+        }
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
           for (int hi = 0; hi < 2; ++hi) {
             const float* q = xm + mb * 16 + hi * 8 + g;
-            const float mn = fmaxf(R.m[mb][hi] - shift, fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T])));
+            const float top = fmaxf(fmaxf(q[0], q[T]), fmaxf(q[2 * T], q[3 * T]));
+            const float mn = E4M3 ? paged_product_ref(R.m[mb][hi] - shift, top) : fmaxf(R.m[mb][hi], top);
             const float alpha = mn == R.m[mb][hi] ? 1.f : ex2(R.m[mb][hi] - mn);  // 0 from -inf
             R.m[mb][hi] = mn;
             R.l[mb][hi] *= alpha;
@@ -829,8 +858,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           const int r = mb * 16 + hi * 8 + g;
           if (r >= rows) continue;
           const float l = (wl[r] + wl[T + r]) + (wl[2 * T + r] + wl[3 * T + r]);
-          constexpr float one = E4M3 ? 1.f / 128.f : 1.f;  // 2^-kUp
-          float inv = !whole ? one : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
           // this lane's elements of the row: an 8-bit cache's NT columns of
           // fragment column 2 t4, then those of 2 t4 + 1, which follow on
           // them; a bf16 cache's columns 2 t4 and 2 t4 + 1 of each tile
@@ -876,7 +904,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
                 *reinterpret_cast<float2*>(pd + j * 8 + 2 * t4) = make_float2(x[2 * j], x[2 * j + 1]);
             }
           }
-          if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(R.m[mb][hi], l * one);
+          if (!whole && warp == 0 && t4 == 0) *reinterpret_cast<float2*>(part_ml + 2 * r) = make_float2(R.m[mb][hi], l);
         }
     }
     if (any_bad) {

@@ -12,8 +12,9 @@
 namespace ebd {
 
 // A row's probabilities are 2^(y - ref), y its scores in log2 units, rounded to
-// 32 bits before the reference is taken off (not in one fused operation): what is
-// left of y against a reference near it is then exact, however large y is.
+// 32 bits before the reference is taken off (not in one fused operation, but for a
+// power of two): what is left of y against a reference near it is then exact,
+// however large y is.
 //
 // The tcgen05 kernel does a half step of 64 keys again, after moving the
 // reference, where the largest y - ref, `top`, is past 24.  A row without a
@@ -37,5 +38,15 @@ EBD_HD float paged_move(float top, float& ref, bool& started) {
   started = true;
   return lost;
 }
+
+// The mma.sync kernel's 8-bit caches' P is f16, and holds probabilities times their
+// values' scales.  What is taken off a row's scores is its largest product of both,
+// `top` in log2 units, less kPagedUp, so that this product becomes 2^kPagedUp.  Past
+// 2^22 (steps of 0.5), where 32 bits soon do not resolve offsets from a score any
+// more, `top` is the largest score itself: no product is past 2^8 then, the
+// rounding of the difference in it, and such keys' probabilities are 1 at least.
+constexpr float kPagedUp = 7.f, kPagedCoarse = 4194304.f;
+EBD_HD bool paged_coarse(float top) { return fabsf(top) >= kPagedCoarse && top > -INFINITY; }
+EBD_HD float paged_product_ref(float m, float top) { return fmaxf(m, top - kPagedUp); }
 
 }  // namespace ebd

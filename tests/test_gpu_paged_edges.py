@@ -81,7 +81,8 @@ def test_causal_nan_values_all_over_many_short_tiles(dtype, heads, n, kv):
 
 
 # packed rows on either kernel, over caches that are whole and cut into parts
-HUGE = [("llada", 70, 500), ("mqa", 20, 3000), ("dream", 40, 500), ("llada", 200, 3000)]
+HUGE = [("llada", 70, 500), ("mqa", 20, 3000), ("dream", 40, 500), ("llada", 200, 3000),
+        ("dream", 2, 500), ("llada", 20, 3000), ("tiny", 40, 700), ("gqa64", 5, 500)]
 
 
 def _bound(ref, v, lens, group):

@@ -1,6 +1,7 @@
 """The arithmetic that the paged attention's softmax rests on, compiled for the
 host: how a row's reference moves."""
 import ctypes
+import math
 import os
 import shutil
 import subprocess
@@ -26,6 +27,8 @@ extern "C" int settle(float y, float* ref, int* started, float* left, float* los
   *started = s;
   return moves;
 }
+extern "C" float product_ref(float m, float top) { return paged_product_ref(m, top); }
+extern "C" int coarse(float ref) { return paged_coarse(ref); }
 extern "C" int most_moves() { return kPagedMoves; }
 """
 
@@ -41,6 +44,8 @@ def lib(tmp_path_factory):
                     "-o", str(d / "m.so")], check=True)
     m = ctypes.CDLL(str(d / "m.so"))
     f = ctypes.POINTER(ctypes.c_float)
+    m.product_ref.argtypes, m.product_ref.restype = [ctypes.c_float] * 2, ctypes.c_float
+    m.coarse.argtypes = [ctypes.c_float]
     m.settle.argtypes = [ctypes.c_float, f, ctypes.POINTER(ctypes.c_int), f, f]
     return m
 
@@ -90,3 +95,27 @@ def test_scores_that_are_infinite_or_nan_end_too(lib):
         for r in (0.0, 1e9, -3e38, 3e38, np.inf):
             for started in (0, 1):
                 assert Row(lib, r, started).settle(float(y))[0] <= lib.most_moves()
+
+
+def test_products_stay_in_range_of_f16_for_scores_of_any_size(lib):
+    """Keys of a row with scores y and value scales 2^d, d in [-40, 0]: against the
+    reference the largest product 2^(y - ref + d) is 2^7 (2^8 at most where 32 bits
+    do not resolve that), and the largest score's probability is not lost."""
+    rng = np.random.default_rng(2)
+    f = np.float32
+    coarse = 0
+    for trial in range(4000):
+        x = _scores(rng, 1)[0]
+        # scores that differ by log2 units where these resolve, and by units of x's last place
+        y = np.concatenate([[x], x - f(60) * rng.random(4).astype(f), x - rng.integers(0, 3, 4).astype(f) * np.spacing(abs(x))])
+        d = rng.integers(-40, 1, y.size).astype(f)
+        top = (y + d).max()
+        large = lib.coarse(float(top))
+        coarse += large
+        if large:  # the largest score in its place
+            top = y.max()
+        left = y - f(lib.product_ref(-math.inf, float(top)))
+        most = float((left + d).max())
+        assert left.max() >= 0 and (most <= 8 if large else abs(most - 7) <= 0.75)
+    assert coarse > 1000 and not lib.coarse(-math.inf)
+    assert lib.product_ref(-math.inf, -math.inf) == -math.inf and lib.product_ref(5.0, -math.inf) == 5.0
