@@ -26,8 +26,9 @@
 // against its largest product of probability and value's scale, which becomes
 // 2^kUp: so f16 holds products down to 2^-31 of the row's own largest, whatever
 // other keys' values are (scores past 2^22: paged_math.h).  The sum is of the same
-// probabilities without the scales, in 32 bits; scales count as 2^-40 E0 at least
-// in that maximum, which bounds it.  O is multiplied by E0's power at the end.
+// probabilities without the scales, in 32 bits: scales count as 2^-40 E0 at least
+// in that maximum, and where E0 rises the reference falls no further than leaves
+// the sum below 2^kSum.  O is multiplied by E0's power at the end.
 // P is rounded to f16 (bf16 where the cache is); its sum is of the unrounded
 // values.
 //
@@ -61,10 +62,16 @@ constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
 constexpr float kUp = kPagedUp;     // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)
 constexpr int kSpan = 40;           // and of the scales' span that its reference follows
+constexpr float kSum = 100.f;       // and of a lane's sum of probabilities, where the reference falls
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -662,6 +669,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
               float x = -INFINITY;
+              if (E4M3 && !PLAIN) x = R.m[mb][hi] + (lg2(R.l[mb][hi]) + (kUp - kSum));  // -inf: no sum yet
 #pragma unroll
               for (int nt = 0; nt < NK; ++nt)
 #pragma unroll
@@ -858,7 +866,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           const int r = mb * 16 + hi * 8 + g;
           if (r >= rows) continue;
           const float l = (wl[r] + wl[T + r]) + (wl[2 * T + r] + wl[3 * T + r]);
-          const float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          float inv = !whole ? 1.f : l > 0.f || l != l ? 1.f / l : 0.f;  // a row that sees nothing: zeros
+          // an 8-bit cache's O is relative to E0: a scale past 1 goes into the divisor,
+          // as O may be as small as the sum is large
+          const float e0 = E4M3 ? scale_value(static_cast<uint32_t>(E0)) : 1.f;
+          if (E4M3 && e0 > 1.f) inv *= e0;
+          const float rest = e0 > 1.f ? 1.f : e0;
           // this lane's elements of the row: an 8-bit cache's NT columns of
           // fragment column 2 t4, then those of 2 t4 + 1, which follow on
           // them; a bf16 cache's columns 2 t4 and 2 t4 + 1 of each tile
@@ -867,9 +880,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              // an 8-bit cache's O is relative to E0
               const float z = o[mb][j][2 * hi + e] * inv;
-              x[E4M3 ? e * NT + j : 2 * j + e] = E4M3 ? z * scale_value(static_cast<uint32_t>(E0)) : z;
+              x[E4M3 ? e * NT + j : 2 * j + e] = E4M3 ? z * rest : z;
             }
           if (any_bad) {
             const int lim = limit(mb, hi);

@@ -213,3 +213,40 @@ def test_a_call_that_gives_up_writes_nothing_of_an_earlier_one(dtype, heads, n):
     assert call([n, n]) == 0
     _close(out, ref, tol)
     h.close()
+
+
+def _along(rng, heads, c, kv, score, value):
+    """Fills a cache so that key j scores score[j] log2 units above key noise and
+    its values are about value[j]; returns rows of q."""
+    hq, hkv, D = HEADS[heads]
+    u = rng.standard_normal((hkv, D)).astype(np.float32)
+    u /= np.linalg.norm(u, axis=-1, keepdims=True)
+    k = 0.1 * rng.standard_normal((c.n_pages, hkv, c.page, D)).astype(np.float32)
+    v = rng.standard_normal(k.shape).astype(np.float32)
+    for j in range(kv):
+        at = (int(c.table_h[0, j // c.page]), slice(None), j % c.page)
+        k[at] += 0.1 * math.log(2) * math.sqrt(D) * score[j] * u
+        v[at] *= np.float32(value[j])
+    c.fill(torch.from_numpy(k).cuda().bfloat16(), torch.from_numpy(v).cuda().bfloat16())
+    q = np.repeat(10.0 * u, hq // hkv, axis=0)[None] + 0.1 * rng.standard_normal((8, hq, D))
+    return torch.from_numpy(q.astype(np.float32)).cuda().bfloat16()
+
+
+FEW = ["dream", "tiny", "gqa64", "llada"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads", FEW)
+@pytest.mark.parametrize("steps", [(-60, -20, 20, 60), (-40, -25, -10, 5, 20, 35), (-84, -42, 0, 42, 84)])
+def test_values_that_grow_behind_the_keys_that_count(dtype, heads, steps):
+    """Values larger chunk by chunk, all of a row's weight on the first chunk: the
+    row has that chunk's values."""
+    kv = 64 * len(steps)
+    rng = np.random.default_rng(13)
+    c = pr.Cache(HEADS[heads], dtype, 64, [kv], seed=3)
+    score = np.where(np.arange(kv) < 64, 400.0, 0.0)
+    q = _along(rng, heads, c, kv, score, np.repeat(np.exp2(np.array(steps, float)), 64))
+    out = _attend(c, heads, q, [8], [kv])
+    ref, tol = _reference(c, q, heads, [8], [kv], False)
+    assert float(ref.abs().max()) < 2.0 ** (steps[0] + 4)
+    _close(out, ref, tol)
