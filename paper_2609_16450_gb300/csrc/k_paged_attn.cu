@@ -26,9 +26,9 @@
 // against its largest product of probability and value's scale, which becomes
 // 2^kUp: so f16 holds products down to 2^-31 of the row's own largest, whatever
 // other keys' values are (scores past 2^22: paged_math.h).  The sum is of the same
-// probabilities without the scales, in 32 bits: scales count as 2^-40 E0 at least
-// in that maximum, and where E0 rises the reference falls no further than leaves
-// the sum below 2^kSum.  O is multiplied by E0's power at the end.
+// probabilities without the scales, in 32 bits: scales count as 2^-kSpan E0 at
+// least in that maximum, and where E0 rises the reference falls no further than
+// leaves the sum below 2^kSum.  O is multiplied by E0's power at the end.
 // P is rounded to f16 (bf16 where the cache is); its sum is of the unrounded
 // values.
 //
@@ -61,8 +61,8 @@ constexpr int kLeastKeys = 192;
 constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;
 constexpr float kUp = kPagedUp;     // 8-bit caches: log2 of a row's largest product (2^15 until its reference moves)
-constexpr int kSpan = 40;           // and of the scales' span that its reference follows
-constexpr float kSum = 100.f;       // and of a lane's sum of probabilities, where the reference falls
+constexpr int kSpan = 90;           // and of the scales' span that its reference follows
+constexpr float kSum = 100.f;       // and of a lane's sum of probabilities, past which the reference moves
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -637,6 +637,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(E4M3, MB))
 #pragma unroll
           for (int nt = 0; nt < NK; ++nt) emax = max(emax, max(ve[nt][0], ve[nt][1]));
           raise = raise || static_cast<int>(emax) > E0 + 7;
+          // keys whose values are small or zero: their products do not tell, and
+          // infinity times such a scale would be NaN
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) raise = raise || fmaxf(ls[mb][0], ls[mb][1]) > 0x1p100f;
         }
       }
       if (barrier_or(1, 128, raise)) {

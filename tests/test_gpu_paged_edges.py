@@ -250,3 +250,20 @@ def test_values_that_grow_behind_the_keys_that_count(dtype, heads, steps):
     ref, tol = _reference(c, q, heads, [8], [kv], False)
     assert float(ref.abs().max()) < 2.0 ** (steps[0] + 4)
     _close(out, ref, tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads", FEW)
+@pytest.mark.parametrize("gap", [60.0, 100.0, 126.0, 140.0, 300.0, 2000.0])
+@pytest.mark.parametrize("small", [0.0, 2.0 ** -30])
+def test_a_key_far_above_the_others_whose_values_are_small(dtype, heads, gap, small):
+    """Values past 2^9, but small or zero ones at some key of the second chunk that
+    scores far above all others: its values are the row's."""
+    kv = 200
+    rng = np.random.default_rng(14)
+    c = pr.Cache(HEADS[heads], dtype, 64, [kv], seed=3)
+    key = np.arange(kv) == 101
+    q = _along(rng, heads, c, kv, np.where(key, gap, 0.0), np.where(key, small, 2.0 ** 12))
+    out = _attend(c, heads, q, [8], [kv])
+    ref, tol = _reference(c, q, heads, [8], [kv], False)
+    _close(out, ref, tol)
