@@ -126,8 +126,11 @@ typedef struct {
   int32_t decode_mode; /* EBD_DECODE_*: EB decision or a baseline rule      */
   int32_t top_m;       /* EBD_DECODE_TOPM: commits per step (>= 1)          */
   int32_t paged;       /* 1: the handle also runs ebd_paged_attention, whose
-                          workspace it then holds (40 MB at 128-wide heads);
-                          0: it does not                                   */
+                          workspace it then holds (40 MB at 128-wide heads).
+                          What the decoding step needs it sets up when its
+                          first function is called, ebd_bind_embedding as a
+                          rule (in a stream capture: EBD_ERR_STATE), not with
+                          ebd_create.  0: it does not, and sets up all there */
 } ebd_config;
 
 typedef struct {

@@ -250,6 +250,7 @@ struct ebd_handle {
   DecideSlots rows_slots{};         // its clusters that fit the GPU
   RowsParams rowsp{};               // image and scratch pointers, filled at create
   cudaEvent_t ev[4] = {nullptr, nullptr, nullptr, nullptr};
+  bool decoding = false;             // the members above are there (setup_decoding)
   int profile = 0;
   int prof_mode = 0, prof_attn = 0;  // what the last ebd_step recorded
   // ebd_paged_attention (cfg.paged): partial results of split tiles
@@ -858,6 +859,171 @@ ebd_status ebd_router_init_host(const ebd_config* cfg, void* host, size_t* bytes
   return EBD_OK;
 }
 
+namespace {
+void free_decoding(ebd_handle* h) {
+  if (h->s_copy) cudaStreamDestroy(h->s_copy);
+  if (h->ev_fork) cudaEventDestroy(h->ev_fork);
+  if (h->ev_join) cudaEventDestroy(h->ev_join);
+  cudaFree(h->d_ready);
+  cudaFree(h->d_blob);
+  cudaFree(h->d_tok);
+  cudaFree(h->part_f);
+  cudaFree(h->part_i);
+  cudaFree(h->attn_part);
+  cudaFree(h->tickets);
+  cudaFree(h->staging);
+  cudaFree(h->d_rows);
+  cudaFree(h->rows_scratch);
+  h->s_copy = nullptr;
+  h->ev_fork = h->ev_join = nullptr;
+  h->d_ready = nullptr;
+  h->d_blob = nullptr;
+  h->d_tok = nullptr;
+  h->part_f = nullptr;
+  h->part_i = nullptr;
+  h->attn_part = nullptr;
+  h->tickets = nullptr;
+  h->staging = nullptr;
+  h->d_rows = nullptr;
+  h->rows_scratch = nullptr;
+  h->copy_route = -1;
+}
+
+// What the functions of the decoding step need: the routers, the statistics'
+// partials, the window attention's and the decision's scratch, the staging.
+ebd_status setup_decoding(ebd_handle* h) {
+  const ebd_config* cfg = &h->cfg;
+  cudaError_t e;
+  ebd_status s;
+  auto drop = [&](ebd_status code) {
+    free_decoding(h);
+    return code;
+  };
+  if ((e = lm_configure()) != cudaSuccess) return drop(cuda_fail(h, e, "LM-head attributes"));
+  if ((e = attn_configure()) != cudaSuccess) return drop(cuda_fail(h, e, "attention attributes"));
+  if ((e = decide_rows_configure(h->rows_slots)) != cudaSuccess)
+    return drop(cuda_fail(h, e, "decision attributes"));
+
+  h->layout = router_layout(cfg->d_base, cfg->gen_len);
+  h->h_blob.resize(layout_count(h->layout));
+  router_init(cfg->seed, h->layout, h->h_blob.data());
+  if ((e = cudaMalloc(&h->d_blob, h->h_blob.size() * 2)) != cudaSuccess)
+    return drop(cuda_fail(h, e, "cudaMalloc(router blob)"));
+  if ((e = cudaMalloc(&h->d_tok, static_cast<size_t>(cfg->vocab) * 64 * 4)) != cudaSuccess)
+    return drop(cuda_fail(h, e, "cudaMalloc(token table)"));
+  if ((s = upload_router(h)) != EBD_OK) return drop(s);
+
+  // LM-head partials: one state per (row, CTA)
+  h->lm_units = (cfg->vocab + kUnit - 1) / kUnit;
+  h->grid_lm = lm_grid(h->num_sms, h->lm_units);
+  {  // a handle whose steps may take the paired LM head leaves room for its partials
+    int pair_min = kLmPairMinRows;
+    if (const char* env = getenv("EBD_LM_PAIR_MIN")) pair_min = atoi(env) > 0 ? atoi(env) : kMaxGroupRows + 1;
+    const int pg = lm_pair_grid(h->num_sms, h->lm_units);
+    if (cfg->max_rows >= pair_min && pg > h->grid_lm) h->grid_lm = pg;
+  }
+  const size_t np = static_cast<size_t>(cfg->max_rows) * h->grid_lm;
+  if ((e = cudaMalloc(&h->part_f, np * sizeof(float4))) != cudaSuccess)
+    return drop(cuda_fail(h, e, "cudaMalloc(partials)"));
+  if ((e = cudaMalloc(&h->part_i, np * sizeof(int))) != cudaSuccess)
+    return drop(cuda_fail(h, e, "cudaMalloc(partials)"));
+  // attention split-KV workspace
+  {
+    const int tile = 64;
+    const int aw = cfg->max_window < kMaxWindow ? cfg->max_window : kMaxWindow;
+    h->attn_max_qtiles = (aw * (cfg->n_heads_q / cfg->n_heads_kv) + tile - 1) / tile;
+    if (const char* env = getenv("EBD_ATTN_KERNEL")) h->attn_force_tc = strcmp(env, "mma") == 0 ? 0 : 1;
+    if (const char* env = getenv("EBD_ATTN_SPLITS")) {
+      const int n = atoi(env);
+      h->attn_force_splits = n < 1 ? 1 : n > kMaxAttnSplits ? kMaxAttnSplits : n;
+    }
+    if (const char* env = getenv("EBD_ATTN_STAGES")) h->attn_force_stages = atoi(env) == 2 ? 2 : kAttnStages;
+    // partials of any launch that splits its tiles
+    const int slots = cfg->max_batch * cfg->n_heads_kv * h->attn_max_qtiles;
+    size_t parts = static_cast<size_t>(slots) * (h->attn_force_splits != 0 ? h->attn_force_splits : kMaxAttnSplits);
+    if (h->attn_force_splits == 0) {
+      const size_t most = static_cast<size_t>(kAttnParts) * h->num_sms;
+      if (parts > most) parts = most;
+      if (attn_chunks(*cfg) < kAttnSplitChunks) parts = 0;
+    }
+    if (parts > 0) {
+      if ((e = cudaMalloc(&h->attn_part, parts * tile * (cfg->head_dim + 2) * 4)) != cudaSuccess)
+        return drop(cuda_fail(h, e, "cudaMalloc(attention partials)"));
+      h->attn_part_ml = h->attn_part + parts * tile * cfg->head_dim;
+    }
+    if ((e = cudaMalloc(&h->tickets, static_cast<size_t>(slots) * sizeof(int))) != cudaSuccess)
+      return drop(cuda_fail(h, e, "cudaMalloc(tickets)"));
+    if ((e = cudaMemset(h->tickets, 0, static_cast<size_t>(slots) * sizeof(int))) != cudaSuccess)
+      return drop(cuda_fail(h, e, "cudaMemset(tickets)"));
+  }
+  // staging for ebd_step_host
+  {
+    const size_t R = cfg->max_rows, B = cfg->max_batch;
+    const size_t d = cfg->d_model, Hq = cfg->n_heads_q, Hkv = cfg->n_heads_kv, D = cfg->head_dim;
+    size_t bytes = 0;
+    auto add = [&](size_t n) { bytes += (n + 255) / 256 * 256; };
+    add((B + 1) * 4); add(B * 4); add(R * 4); add(R * d * 2); add(R * Hq * D * 2);
+    add(R * Hkv * D * 2); add(R * Hkv * D * 2); add(R * 4); add(R); add(R); add(B * 8);
+    add(R * Hq * D * 4); for (int i = 0; i < 6; ++i) add(R * 4); add(R * 4); add(R);
+    add(B * 8);  // suffix ranges
+    h->staging_bytes = bytes;
+    if ((e = cudaMalloc(&h->staging, bytes)) != cudaSuccess)
+      return drop(cuda_fail(h, e, "cudaMalloc(staging)"));
+  }
+  // the copy stream of ebd_step_host, set up here rather than at its first
+  // call, which may come while a stream is being captured into a graph
+  if (cfg->max_window <= kMaxWindow) (void)copy_route_ready(h);
+  {  // scratch of the decision
+    const int planes = cfg->max_window > kMaxWindow ? 3 : 2;
+    const size_t cap = scratch_rows(cfg->max_rows, cfg->max_batch);
+    const size_t R = cfg->max_rows;
+    size_t bytes = 0;
+    auto add = [&](size_t n) {
+      const size_t at = bytes;
+      bytes += (n + 255) / 256 * 256;
+      return at;
+    };
+    const bool wide = planes == 3;
+    const size_t o_kv = add(4 * planes * cap * 128 * 2), o_O = add(cap * 4), o_P = add(cap * 4),
+                 o_c = add((R + 1) * 4), o_e = add((R + 1) * 4), o_g = add((R + 1) * 4), o_a = add((R + 1) * 4),
+                 o_kvp = add(wide ? 4 * planes * cap * 32 * 2 : 0), o_z = add(wide ? cap * 128 * 4 : 0),
+                 o_q = add(wide ? planes * cap * 128 * 2 : 0);
+    if ((e = cudaMalloc(&h->rows_scratch, bytes)) != cudaSuccess)
+      return drop(cuda_fail(h, e, "cudaMalloc(decision scratch)"));
+    uint8_t* b0 = h->rows_scratch;
+    RowsParams& q = h->rowsp;
+    q.cap_rows = static_cast<int>(cap);
+    q.spare_row = cfg->max_rows;
+    q.kv = reinterpret_cast<__nv_bfloat16*>(b0 + o_kv);
+    q.kvp = reinterpret_cast<__nv_bfloat16*>(b0 + o_kvp);
+    q.z = reinterpret_cast<float*>(b0 + o_z);
+    q.q = reinterpret_cast<__nv_bfloat16*>(b0 + o_q);
+    q.O = reinterpret_cast<float*>(b0 + o_O);
+    q.P = reinterpret_cast<float*>(b0 + o_P);
+    q.s_conf = reinterpret_cast<float*>(b0 + o_c);
+    q.s_ent = reinterpret_cast<float*>(b0 + o_e);
+    q.s_gap = reinterpret_cast<float*>(b0 + o_g);
+    q.s_arg = reinterpret_cast<int*>(b0 + o_a);
+  }
+  h->decoding = true;
+  return EBD_OK;
+}
+
+// Handles that page take only what paging needs until the decoding step is used.
+ebd_status decoding_ready(ebd_handle* h, cudaStream_t st) {
+  if (h->decoding) return EBD_OK;
+  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(st, &cs);
+  if (e != cudaSuccess) return cuda_fail(h, e, "cudaStreamIsCapturing");
+  if (cs == cudaStreamCaptureStatusActive)
+    return fail(h, EBD_ERR_STATE, "the decoding step of a paging handle has to be set up before a capture (ebd_bind_embedding)");
+  const ebd_status s = setup_decoding(h);
+  if (s != EBD_OK) return s;
+  e = cudaDeviceSynchronize();
+  return e == cudaSuccess ? EBD_OK : cuda_fail(h, e, "create");
+}
+}  // namespace
+
 ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
   if (out == nullptr) return EBD_ERR_INVALID_ARG;
   *out = nullptr;
@@ -886,63 +1052,6 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     return bail(fail(h, EBD_ERR_UNSUPPORTED, "the library is compiled for sm_103a (GB300) only"));
   if (get_encode() == nullptr)
     return bail(fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable"));
-  if ((e = lm_configure()) != cudaSuccess) return bail(cuda_fail(h, e, "LM-head attributes"));
-  if ((e = attn_configure()) != cudaSuccess) return bail(cuda_fail(h, e, "attention attributes"));
-  if ((e = decide_rows_configure(h->rows_slots)) != cudaSuccess)
-    return bail(cuda_fail(h, e, "decision attributes"));
-
-  h->layout = router_layout(cfg->d_base, cfg->gen_len);
-  h->h_blob.resize(layout_count(h->layout));
-  router_init(cfg->seed, h->layout, h->h_blob.data());
-  if ((e = cudaMalloc(&h->d_blob, h->h_blob.size() * 2)) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMalloc(router blob)"));
-  if ((e = cudaMalloc(&h->d_tok, static_cast<size_t>(cfg->vocab) * 64 * 4)) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMalloc(token table)"));
-  if ((s = upload_router(h)) != EBD_OK) return bail(s);
-
-  // LM-head partials: one state per (row, CTA)
-  h->lm_units = (cfg->vocab + kUnit - 1) / kUnit;
-  h->grid_lm = lm_grid(h->num_sms, h->lm_units);
-  {  // a handle whose steps may take the paired LM head leaves room for its partials
-    int pair_min = kLmPairMinRows;
-    if (const char* env = getenv("EBD_LM_PAIR_MIN")) pair_min = atoi(env) > 0 ? atoi(env) : kMaxGroupRows + 1;
-    const int pg = lm_pair_grid(h->num_sms, h->lm_units);
-    if (cfg->max_rows >= pair_min && pg > h->grid_lm) h->grid_lm = pg;
-  }
-  const size_t np = static_cast<size_t>(cfg->max_rows) * h->grid_lm;
-  if ((e = cudaMalloc(&h->part_f, np * sizeof(float4))) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMalloc(partials)"));
-  if ((e = cudaMalloc(&h->part_i, np * sizeof(int))) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMalloc(partials)"));
-  // attention split-KV workspace
-  {
-    const int tile = 64;
-    const int aw = cfg->max_window < kMaxWindow ? cfg->max_window : kMaxWindow;
-    h->attn_max_qtiles = (aw * (cfg->n_heads_q / cfg->n_heads_kv) + tile - 1) / tile;
-    if (const char* env = getenv("EBD_ATTN_KERNEL")) h->attn_force_tc = strcmp(env, "mma") == 0 ? 0 : 1;
-    if (const char* env = getenv("EBD_ATTN_SPLITS")) {
-      const int n = atoi(env);
-      h->attn_force_splits = n < 1 ? 1 : n > kMaxAttnSplits ? kMaxAttnSplits : n;
-    }
-    if (const char* env = getenv("EBD_ATTN_STAGES")) h->attn_force_stages = atoi(env) == 2 ? 2 : kAttnStages;
-    // partials of any launch that splits its tiles
-    const int slots = cfg->max_batch * cfg->n_heads_kv * h->attn_max_qtiles;
-    size_t parts = static_cast<size_t>(slots) * (h->attn_force_splits != 0 ? h->attn_force_splits : kMaxAttnSplits);
-    if (h->attn_force_splits == 0) {
-      const size_t most = static_cast<size_t>(kAttnParts) * h->num_sms;
-      if (parts > most) parts = most;
-      if (attn_chunks(*cfg) < kAttnSplitChunks) parts = 0;
-    }
-    if (parts > 0) {
-      if ((e = cudaMalloc(&h->attn_part, parts * tile * (cfg->head_dim + 2) * 4)) != cudaSuccess)
-        return bail(cuda_fail(h, e, "cudaMalloc(attention partials)"));
-      h->attn_part_ml = h->attn_part + parts * tile * cfg->head_dim;
-    }
-    if ((e = cudaMalloc(&h->tickets, static_cast<size_t>(slots) * sizeof(int))) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(tickets)"));
-    if ((e = cudaMemset(h->tickets, 0, static_cast<size_t>(slots) * sizeof(int))) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMemset(tickets)"));
-  }
   if (cfg->paged) {
     if ((e = paged_configure()) != cudaSuccess || (e = paged_tc_configure()) != cudaSuccess)
       return bail(cuda_fail(h, e, "paged attention attributes"));
@@ -961,58 +1070,10 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     return bail(cuda_fail(h, e, "cudaMemset(status)"));
   if ((e = cudaMallocHost(&h->h_status, sizeof(int))) != cudaSuccess)
     return bail(cuda_fail(h, e, "cudaMallocHost(status)"));
-  // staging for ebd_step_host
-  {
-    const size_t R = cfg->max_rows, B = cfg->max_batch;
-    const size_t d = cfg->d_model, Hq = cfg->n_heads_q, Hkv = cfg->n_heads_kv, D = cfg->head_dim;
-    size_t bytes = 0;
-    auto add = [&](size_t n) { bytes += (n + 255) / 256 * 256; };
-    add((B + 1) * 4); add(B * 4); add(R * 4); add(R * d * 2); add(R * Hq * D * 2);
-    add(R * Hkv * D * 2); add(R * Hkv * D * 2); add(R * 4); add(R); add(R); add(B * 8);
-    add(R * Hq * D * 4); for (int i = 0; i < 6; ++i) add(R * 4); add(R * 4); add(R);
-    add(B * 8);  // suffix ranges
-    h->staging_bytes = bytes;
-    if ((e = cudaMalloc(&h->staging, bytes)) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(staging)"));
-  }
-  // the copy stream of ebd_step_host, set up here rather than at its first
-  // call, which may come while a stream is being captured into a graph
-  if (cfg->max_window <= kMaxWindow) (void)copy_route_ready(h);
-  {  // scratch of the decision
-    const int planes = cfg->max_window > kMaxWindow ? 3 : 2;
-    const size_t cap = scratch_rows(cfg->max_rows, cfg->max_batch);
-    const size_t R = cfg->max_rows;
-    size_t bytes = 0;
-    auto add = [&](size_t n) {
-      const size_t at = bytes;
-      bytes += (n + 255) / 256 * 256;
-      return at;
-    };
-    const bool wide = planes == 3;
-    const size_t o_kv = add(4 * planes * cap * 128 * 2), o_O = add(cap * 4), o_P = add(cap * 4),
-                 o_c = add((R + 1) * 4), o_e = add((R + 1) * 4), o_g = add((R + 1) * 4), o_a = add((R + 1) * 4),
-                 o_kvp = add(wide ? 4 * planes * cap * 32 * 2 : 0), o_z = add(wide ? cap * 128 * 4 : 0),
-                 o_q = add(wide ? planes * cap * 128 * 2 : 0);
-    if ((e = cudaMalloc(&h->rows_scratch, bytes)) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(decision scratch)"));
-    uint8_t* b0 = h->rows_scratch;
-    RowsParams& q = h->rowsp;
-    q.cap_rows = static_cast<int>(cap);
-    q.spare_row = cfg->max_rows;
-    q.kv = reinterpret_cast<__nv_bfloat16*>(b0 + o_kv);
-    q.kvp = reinterpret_cast<__nv_bfloat16*>(b0 + o_kvp);
-    q.z = reinterpret_cast<float*>(b0 + o_z);
-    q.q = reinterpret_cast<__nv_bfloat16*>(b0 + o_q);
-    q.O = reinterpret_cast<float*>(b0 + o_O);
-    q.P = reinterpret_cast<float*>(b0 + o_P);
-    q.s_conf = reinterpret_cast<float*>(b0 + o_c);
-    q.s_ent = reinterpret_cast<float*>(b0 + o_e);
-    q.s_gap = reinterpret_cast<float*>(b0 + o_g);
-    q.s_arg = reinterpret_cast<int*>(b0 + o_a);
-  }
   for (int i = 0; i < 4; ++i)
     if ((e = cudaEventCreate(&h->ev[i])) != cudaSuccess)
       return bail(cuda_fail(h, e, "cudaEventCreate"));
+  if (!cfg->paged && (s = setup_decoding(h)) != EBD_OK) return bail(s);
   if ((e = cudaDeviceSynchronize()) != cudaSuccess) return bail(cuda_fail(h, e, "create"));
   *out = h;
   return EBD_OK;
@@ -1024,23 +1085,11 @@ void ebd_destroy(ebd_handle* h) {
   cudaGetDevice(&prev);
   if (prev != h->device) cudaSetDevice(h->device);
   cudaDeviceSynchronize();
-  if (h->s_copy) cudaStreamDestroy(h->s_copy);
-  if (h->ev_fork) cudaEventDestroy(h->ev_fork);
-  if (h->ev_join) cudaEventDestroy(h->ev_join);
-  cudaFree(h->d_ready);
-  cudaFree(h->d_blob);
-  cudaFree(h->d_tok);
-  cudaFree(h->part_f);
-  cudaFree(h->part_i);
-  cudaFree(h->attn_part);
-  cudaFree(h->tickets);
+  free_decoding(h);
   cudaFree(h->paged_part);
   cudaFree(h->paged_cuts);
   cudaFree(h->d_status);
   cudaFreeHost(h->h_status);
-  cudaFree(h->staging);
-  cudaFree(h->d_rows);
-  cudaFree(h->rows_scratch);
   for (int i = 0; i < 4; ++i)
     if (h->ev[i]) cudaEventDestroy(h->ev[i]);
   if (prev >= 0 && prev != h->device) cudaSetDevice(prev);
@@ -1055,12 +1104,14 @@ ebd_status ebd_bind_embedding(ebd_handle* h, const uint16_t* w_emb, void* stream
   if (s != EBD_OK) return s;
   if (w_emb == nullptr || !aligned(w_emb, 16))
     return fail(h, EBD_ERR_INVALID_ARG, "w_emb must be a 16-byte aligned device pointer");
+  if ((s = decoding_ready(h, static_cast<cudaStream_t>(stream))) != EBD_OK) return s;
   h->w_emb = w_emb;
   return fold(h, static_cast<cudaStream_t>(stream));
 }
 
 ebd_status ebd_export_weights(const ebd_handle* h, void* host, size_t* bytes) {
   if (h == nullptr || bytes == nullptr) return EBD_ERR_INVALID_ARG;
+  if (!h->decoding) return ebd_router_init_host(&h->cfg, host, bytes);  // drawn, not imported yet
   const size_t need = h->h_blob.size() * 2;
   if (host == nullptr) {
     *bytes = need;
@@ -1074,9 +1125,10 @@ ebd_status ebd_export_weights(const ebd_handle* h, void* host, size_t* bytes) {
 
 ebd_status ebd_import_weights(ebd_handle* h, const void* host, size_t bytes) {
   if (h == nullptr || host == nullptr) return EBD_ERR_INVALID_ARG;
-  if (bytes != h->h_blob.size() * 2) return fail(h, EBD_ERR_INVALID_ARG, "weight blob size mismatch");
   ebd_status s = check_device(h);
   if (s != EBD_OK) return s;
+  if ((s = decoding_ready(h, nullptr)) != EBD_OK) return s;
+  if (bytes != h->h_blob.size() * 2) return fail(h, EBD_ERR_INVALID_ARG, "weight blob size mismatch");
   cudaError_t e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return cuda_fail(h, e, "import");
   std::memcpy(h->h_blob.data(), host, bytes);
@@ -1315,7 +1367,7 @@ ebd_status ebd_lm_stats(ebd_handle* h, const ebd_step_args* a, void* stream) {
   if ((s = check_args(h, a, false, true, false)) != EBD_OK) return s;
   if (a->rows == 0) return EBD_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if ((s = run_lm(h, a, st)) != EBD_OK) return s;
+  if ((s = decoding_ready(h, st)) != EBD_OK || (s = run_lm(h, a, st)) != EBD_OK) return s;
   const float inv = static_cast<float>(1.0 / std::log(static_cast<double>(h->cfg.vocab)));
   cudaError_t e = launch_merge_stats(h->part_f, h->part_i, a->rows, h->grid_lm, h->cfg.vocab, inv,
                                      a->conf, a->entropy, a->ent_norm, a->gap, a->argmax,
@@ -1337,7 +1389,7 @@ ebd_status ebd_lm_shard_state(ebd_handle* h, const ebd_step_args* a, int32_t v_o
   if (state == nullptr || !aligned(state, 16))
     return fail(h, EBD_ERR_INVALID_ARG, "state must be a 16-byte aligned device pointer");
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if ((s = run_lm(h, a, st, false, v_off, v_count)) != EBD_OK) return s;
+  if ((s = decoding_ready(h, st)) != EBD_OK || (s = run_lm(h, a, st, false, v_off, v_count)) != EBD_OK) return s;
   cudaError_t e = launch_shard_state(h->part_f, h->part_i, a->rows, h->grid_lm, state, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "shard state launch");
   return EBD_OK;
@@ -1370,6 +1422,7 @@ ebd_status ebd_attention(ebd_handle* h, const ebd_step_args* a, void* stream) {
   if (s != EBD_OK) return s;
   if ((s = check_args(h, a, true, false, false)) != EBD_OK) return s;
   if (a->rows == 0 || a->batch == 0) return EBD_OK;
+  if ((s = decoding_ready(h, static_cast<cudaStream_t>(stream))) != EBD_OK) return s;
   return run_attention(h, a, static_cast<cudaStream_t>(stream));
 }
 
