@@ -240,6 +240,7 @@ struct ebd_handle {
   int attn_max_qtiles = 1;
   // EBD_ATTN_KERNEL (1: tcgen05, 0: mma.sync), _SPLITS and _STAGES, where set
   int attn_force_tc = -1, attn_force_splits = 0, attn_force_stages = 0;
+  uint8_t* workspace = nullptr;  // the status word, and what paging needs
   int* d_status = nullptr;
   int* h_status = nullptr;  // pinned: where ebd_sync_status reads the word
   uint8_t* staging = nullptr;
@@ -860,6 +861,30 @@ ebd_status ebd_router_init_host(const ebd_config* cfg, void* host, size_t* bytes
 }
 
 namespace {
+// Pinned words that ebd_sync_status reads the device's status through, out of
+// pages that the process keeps: pinning and unpinning one takes 105 and 175 us,
+// most of what a handle that only pages takes to make and destroy.
+std::mutex g_words_mu;
+std::vector<int*> g_words;  // not in use
+int* take_word(cudaError_t& e) {
+  std::lock_guard<std::mutex> lock(g_words_mu);
+  e = cudaSuccess;
+  if (g_words.empty()) {
+    constexpr int kWords = 1024;
+    int* page = nullptr;
+    if ((e = cudaHostAlloc(&page, kWords * sizeof(int), cudaHostAllocPortable)) != cudaSuccess) return nullptr;
+    for (int i = 0; i < kWords; ++i) g_words.push_back(page + i);
+  }
+  int* w = g_words.back();
+  g_words.pop_back();
+  return w;
+}
+void give_word(int* w) {
+  if (w == nullptr) return;
+  std::lock_guard<std::mutex> lock(g_words_mu);
+  g_words.push_back(w);
+}
+
 void free_decoding(ebd_handle* h) {
   if (h->s_copy) cudaStreamDestroy(h->s_copy);
   if (h->ev_fork) cudaEventDestroy(h->ev_fork);
@@ -1052,24 +1077,32 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     return bail(fail(h, EBD_ERR_UNSUPPORTED, "the library is compiled for sm_103a (GB300) only"));
   if (get_encode() == nullptr)
     return bail(fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable"));
+  size_t part_rows = 0, cuts = 0;
   if (cfg->paged) {
     if ((e = paged_configure()) != cudaSuccess || (e = paged_tc_configure()) != cudaSuccess)
       return bail(cuda_fail(h, e, "paged attention attributes"));
     const size_t ctas = static_cast<size_t>(h->num_sms) * kPagedCtasPerSm;
     const size_t narrow = ctas * 2 * kPagedRows, wide = static_cast<size_t>(h->num_sms) * 2 * kPagedTcRows;
-    const size_t rows = narrow > wide ? narrow : wide;
-    if ((e = cudaMalloc(&h->paged_part, rows * (cfg->head_dim + 2) * sizeof(float))) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(paged attention partials)"));
-    h->paged_part_ml = h->paged_part + rows * cfg->head_dim;
-    if ((e = cudaMalloc(&h->paged_cuts, ctas * sizeof(PagedCut))) != cudaSuccess)
-      return bail(cuda_fail(h, e, "cudaMalloc(paged attention)"));
+    part_rows = narrow > wide ? narrow : wide;
+    cuts = ctas;
   }
-  if ((e = cudaMalloc(&h->d_status, sizeof(int))) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMalloc(status)"));
+  {  // the paged attention's partials and records, and the status word: one allocation
+    const size_t floats = part_rows * (cfg->head_dim + 2), bytes = floats * sizeof(float) + cuts * sizeof(PagedCut);
+    uint8_t* m = nullptr;
+    if ((e = cudaMalloc(&m, bytes + sizeof(int))) != cudaSuccess)
+      return bail(cuda_fail(h, e, "cudaMalloc(paged attention partials, status)"));
+    h->workspace = m;
+    if (cfg->paged) {
+      h->paged_part = reinterpret_cast<float*>(m);
+      h->paged_part_ml = h->paged_part + part_rows * cfg->head_dim;
+      h->paged_cuts = reinterpret_cast<PagedCut*>(m + floats * sizeof(float));
+    }
+    h->d_status = reinterpret_cast<int*>(m + bytes);
+  }
   if ((e = cudaMemset(h->d_status, 0, sizeof(int))) != cudaSuccess)
     return bail(cuda_fail(h, e, "cudaMemset(status)"));
-  if ((e = cudaMallocHost(&h->h_status, sizeof(int))) != cudaSuccess)
-    return bail(cuda_fail(h, e, "cudaMallocHost(status)"));
+  h->h_status = take_word(e);
+  if (e != cudaSuccess) return bail(cuda_fail(h, e, "cudaHostAlloc(status)"));
   for (int i = 0; i < 4; ++i)
     if ((e = cudaEventCreate(&h->ev[i])) != cudaSuccess)
       return bail(cuda_fail(h, e, "cudaEventCreate"));
@@ -1086,10 +1119,8 @@ void ebd_destroy(ebd_handle* h) {
   if (prev != h->device) cudaSetDevice(h->device);
   cudaDeviceSynchronize();
   free_decoding(h);
-  cudaFree(h->paged_part);
-  cudaFree(h->paged_cuts);
-  cudaFree(h->d_status);
-  cudaFreeHost(h->h_status);
+  cudaFree(h->workspace);
+  give_word(h->h_status);
   for (int i = 0; i < 4; ++i)
     if (h->ev[i]) cudaEventDestroy(h->ev[i]);
   if (prev >= 0 && prev != h->device) cudaSetDevice(prev);
