@@ -267,3 +267,27 @@ def test_a_key_far_above_the_others_whose_values_are_small(dtype, heads, gap, sm
     out = _attend(c, heads, q, [8], [kv])
     ref, tol = _reference(c, q, heads, [8], [kv], False)
     _close(out, ref, tol)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("heads,n,kv,gain", [("llada", 70, 500, 12.0), ("mqa", 60, 3000, 60.0), ("dream", 40, 900, 12.0),
+                                             ("llada", 200, 1500, 12.0)])
+def test_rows_that_look_at_one_key_have_its_values(dtype, heads, n, kv, gain):
+    """Sharp rows over caches that take tcgen05: a row whose other keys weigh less
+    than 2^-20 together has its key's values, as they are in the cache."""
+    hq, hkv, D = HEADS[heads]
+    c, q, out = _run(heads, dtype, 64, [n], [kv], False, seed=33, gains=(gain, 1.0, 1.0))
+    k, v = (c.rows_of(i, 0, kv) for i in (0, 1))
+    seen = 0
+    for h in range(hq):
+        kk, vv = k[:, h // (hq // hkv)], v[:, h // (hq // hkv)]
+        p = torch.softmax(q[:, h].double() @ kk.T / math.sqrt(D), -1)
+        top = p.max(-1)
+        one = 1 - top.values < 2.0 ** -20
+        # others' weight times what they hold, and 32-bit sums, far below bf16's half step
+        want = vv[top.indices[one]]
+        far = (1 - top.values[one])[:, None] * vv.abs().amax() > 2.0 ** -12 * want.abs()
+        got = out[one, h].double()
+        assert (far | (got == want)).all()
+        seen += int((~far).sum())
+    assert seen > 1000
