@@ -379,7 +379,8 @@ ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_
  * sums and the probabilities rounded to 16 bits where they multiply v (few rows
  * over an 8-bit cache: f16, so what is below 2^-31 of a row's largest product of
  * probability and value's scale may vanish); bf16 output.  More than 1024 query
- * heads per K/V head: EBD_ERR_UNSUPPORTED.
+ * heads per K/V head, or 2^31 - 256 positions of max_pages pages:
+ * EBD_ERR_UNSUPPORTED.
  * A row that sees no position gives zeros.  What pages hold past kv_len, and
  * what a causal row does not see, has no part in its result, whatever it is.
  * kv_len beyond the page table is cut to it; a position before kv_len whose

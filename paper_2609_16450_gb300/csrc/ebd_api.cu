@@ -1765,6 +1765,9 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   if (a->causal != 0 && a->causal != 1) return fail(h, EBD_ERR_INVALID_ARG, "causal must be 0 or 1");
   if (a->max_new < 0) return fail(h, EBD_ERR_INVALID_ARG, "max_new must not be negative");
   if (f.n_heads_q / f.n_heads_kv > 1024) return fail(h, EBD_ERR_UNSUPPORTED, "more than 1024 query heads per K/V head");
+  const int64_t cap = static_cast<int64_t>(c->max_pages) * c->page_size;
+  if (cap > 0x7fffff00)  // a step past the last position is counted in 32 bits as well
+    return fail(h, EBD_ERR_UNSUPPORTED, "a page table of more than 2^31 - 256 positions");
   if (!(a->scale >= 0.f) || std::isinf(a->scale)) return fail(h, EBD_ERR_INVALID_ARG, "scale must be finite and not negative");
   PagedParams p{};
   p.B = a->batch;
@@ -1777,8 +1780,7 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   p.page_log2 = log2_of(c->page_size);
   p.n_pages = c->n_pages;
   p.max_pages = c->max_pages;
-  const int64_t cap = static_cast<int64_t>(c->max_pages) * c->page_size;
-  p.cap = cap < 0x7fffffff ? static_cast<int>(cap) : 0x7fffffff;
+  p.cap = static_cast<int>(cap);
   const float scale = a->scale != 0.f ? a->scale : 1.f / std::sqrt(static_cast<float>(f.head_dim));
   p.scale_log2 = scale * 1.4426950408889634f;
   p.cu_rows = a->cu_rows;

@@ -291,3 +291,20 @@ def test_rows_that_look_at_one_key_have_its_values(dtype, heads, n, kv, gain):
         assert (far | (got == want)).all()
         seen += int((~far).sum())
     assert seen > 1000
+
+
+def test_page_tables_wider_than_positions_count_are_refused():
+    """kv_len is cut to the page table; past 2^31 - 256 positions the last steps'
+    ends would not fit 32 bits."""
+    E, rt = _lib()
+    c = pr.Cache(HEADS["tiny"], "bf16", 256, [100])
+    h = pr.handle(E, rt, HEADS["tiny"], 1, 1)
+    cu = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    a = _args(E, 1, 1, cu, kv_len=cu[1:], q=q, out=torch.empty_like(q))
+    for pages in (1 << 23, (1 << 31) - 1):
+        p = c.pages(E)
+        p.max_pages = pages
+        assert E.ebd_paged_attention(h.h, p, a, rt.stream_handle(None)) == E.EBD_ERR_UNSUPPORTED
+    assert h.sync_status() == 0
+    h.close()
