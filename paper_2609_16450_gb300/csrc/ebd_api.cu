@@ -862,27 +862,31 @@ ebd_status ebd_router_init_host(const ebd_config* cfg, void* host, size_t* bytes
 
 namespace {
 // Pinned words that ebd_sync_status reads the device's status through, out of
-// pages that the process keeps: pinning and unpinning one takes 105 and 175 us,
-// most of what a handle that only pages takes to make and destroy.
+// pages that the process keeps: pinning and unpinning one takes 105 and 175 us, and
+// a handle that only pages 90 and 50 to make and destroy without.
 std::mutex g_words_mu;
-std::vector<int*> g_words;  // not in use
+std::vector<int*>& free_words() {  // never destroyed: a handle may outlive the library's statics
+  static auto* words = new std::vector<int*>;
+  return *words;
+}
 int* take_word(cudaError_t& e) {
   std::lock_guard<std::mutex> lock(g_words_mu);
+  std::vector<int*>& words = free_words();
   e = cudaSuccess;
-  if (g_words.empty()) {
+  if (words.empty()) {
     constexpr int kWords = 1024;
     int* page = nullptr;
     if ((e = cudaHostAlloc(&page, kWords * sizeof(int), cudaHostAllocPortable)) != cudaSuccess) return nullptr;
-    for (int i = 0; i < kWords; ++i) g_words.push_back(page + i);
+    for (int i = 0; i < kWords; ++i) words.push_back(page + i);
   }
-  int* w = g_words.back();
-  g_words.pop_back();
+  int* w = words.back();
+  words.pop_back();
   return w;
 }
 void give_word(int* w) {
   if (w == nullptr) return;
   std::lock_guard<std::mutex> lock(g_words_mu);
-  g_words.push_back(w);
+  free_words().push_back(w);
 }
 
 void free_decoding(ebd_handle* h) {
