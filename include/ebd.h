@@ -332,7 +332,10 @@ typedef struct {
   int32_t dtype;              /* EBD_KV_BF16 or EBD_KV_E4M3                      */
   int32_t page_size;          /* a power of two, 16..256                         */
   int32_t n_pages;            /* pages of the pools                              */
-  int32_t max_pages;          /* second dimension of page_table                  */
+  int32_t max_pages;          /* second dimension of page_table; the attention
+                                 chooses how it runs by it, as by max_new (the
+                                 lengths are on the device): no wider than the
+                                 longest sequence needs is fastest              */
 } ebd_kv_pages;
 
 typedef struct {
@@ -376,11 +379,15 @@ ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_
 /* Attention of the rows a->q over the pages (handles with ebd_config.paged = 1;
  * EBD_ERR_STATE otherwise): softmax(scale * q k^T) v per query head, K/V head
  * h of the n_heads_q / n_heads_kv query heads from h * that many on, with fp32
- * sums and the probabilities rounded to 16 bits where they multiply v (few rows
- * over an 8-bit cache: f16, so what is below 2^-31 of a row's largest product of
- * probability and value's scale may vanish); bf16 output.  More than 1024 query
- * heads per K/V head, or 2^31 - 256 positions of max_pages pages:
- * EBD_ERR_UNSUPPORTED.
+ * sums and the probabilities rounded to 16 bits where they multiply v (bf16; few
+ * rows over an 8-bit cache: f16, so what is below 2^-31 of a row's largest product
+ * of probability and value's scale may vanish, scales counting as 2^-90 of the
+ * sequence's largest at least); many rows over an 8-bit cache have q as two e4m3
+ * terms, which is exact but for elements below 2^-9 of the row's largest, off by
+ * up to 2^-17 of that one.  Sums of probability times value are held in 32 bits
+ * before they are divided, and may overflow where values pass 2^80; so may scores
+ * of 8-bit keys past 2^100.  bf16 output.  More than 1024 query heads per K/V
+ * head, or a page table of more than 2^31 - 256 positions: EBD_ERR_UNSUPPORTED.
  * A row that sees no position gives zeros.  What pages hold past kv_len, and
  * what a causal row does not see, has no part in its result, whatever it is.
  * kv_len beyond the page table is cut to it; a position before kv_len whose

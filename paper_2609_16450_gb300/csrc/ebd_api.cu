@@ -1811,11 +1811,12 @@ ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_p
   const int64_t m = longest * p.group;
   const bool e4m3 = c->dtype == EBD_KV_E4M3;
   // tcgen05 from 65 packed rows, as mma.sync then reads a tile's keys again for
-  // every 64 (16 x 65 rows of 32 heads over 2113 keys: bf16 123 us against 300, 8
-  // bits 165 against 299); from 33 where caches are long (bf16: 4 x 48 rows over 948
-  // keys 31 against 37, 35 of a group over 605 20.5 against 15.4; 8 bits: 56 of a
-  // group over 4008 23 against 29, 16 x 48 rows over 948 111 against 90).  Up to 32,
-  // mma.sync: 16 x 32 rows over 2080 keys, bf16 96 against 118, 8 bits 81 and 163.
+  // every 64 (16 x 65 rows of 32 heads over 2113 keys: bf16 123 us against 306, 8
+  // bits 179 against 315); from 33 where caches may be long (bf16: 4 x 48 rows over
+  // 948 keys 31 against 36, 35 of a group over 605 21.2 against 20.1; 8 bits: 56 of a
+  // group over 4008 23.5 against 24.3, 16 x 48 rows over 948 115 against 97).  Up to
+  // 32, mma.sync: 16 x 32 rows over 2080 keys, bf16 96 against 117, 8 bits 84 and 178.
+  // How long they are only the device knows: the page table's width stands for it.
   const bool wide = f.head_dim == 128 && p.group <= kPagedTcGroup &&
                     (m > 64 || (m > 32 && p.cap > (e4m3 ? kPagedLongKeysE4m3 : kPagedLongKeys)));
   // keys of a tensor-map box: a page, or a chunk's part of it

@@ -35,12 +35,12 @@
 // The running maximum moves only when a score (a product) exceeds it by more than
 // 8 (log2 units), so that exp2 stays below 256 and most chunks rescale nothing.
 //
-// Measured, 128-wide heads: 64 tokens over ~4096 8-bit keys, 28 / 4 heads, 49.5 us
-// (207 MB: at the HBM rate once it streams; four CTAs per SM, with two 55.8); 16
-// tokens over ~2011 bf16 keys, 32 heads, 67 us (5.8 TB/s, the HBM rate); 64 windows
-// of 32 rows over ~1056 8-bit keys, 32 heads, 133 us (3.3 TB/s: latencies and issue,
-// 1110 cycles a chunk and SM, of which its MMAs are 518; three CTAs per SM, with
-// four 151, with two 190).
+// Measured, 128-wide heads: 64 tokens over ~4096 8-bit keys, 28 / 4 heads, 49.9 us
+// (207 MB: at the HBM rate once it streams; four CTAs per SM; with two 12 % more);
+// 16 tokens over ~2011 bf16 keys, 32 heads, 68 us (5.8 TB/s, the HBM rate); 64
+// windows of 32 rows over ~1056 8-bit keys, 32 heads, 136 us (3.25 TB/s: latencies
+// and issue, 1130 cycles a chunk and SM, of which its MMAs are 518; three CTAs per
+// SM, with four 13 % more, with two 43 %).
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -53,10 +53,11 @@ namespace ebd {
 namespace {
 
 constexpr int kThreads = 160;
-// Keys of a share, at least: 64, 128, 192, 384 take 32 rows over 632 keys of 32 heads
-// 16.0, 14.6, 16.3, 18.9 us, and where a tile is three shares of three chunks (544
-// keys) 128 takes 16.0 and 192 13.3; single tokens over 2001 keys of 28 / 4 heads
-// 17.3, 13.8, 13.5, 14.5.
+// Keys of a share, at least: of small calls (1 to 16 sequences of 1 to 32 rows; 32 /
+// 32, 28 / 4 and 4 / 4 heads; both caches) over 530 to 3000 keys, 64, 128, 256 and
+// 384 take 1.054, 1.002, 1.027 and 1.093 times as long as 192, in the geometric mean
+// of 532 calls.  By length 128 and 192 take turns, as chunks divide: 192 is 8 %
+// slower at 600 to 640 and 1000 keys, 7 to 11 % faster at 530 to 560 and 900.
 constexpr int kLeastKeys = 192;
 constexpr int kJoinRows = 4;        // rows of a joining warp
 constexpr int kNever = 0x7fffffff;

@@ -21,12 +21,14 @@
 // 8-bit K and q in two e4m3 terms multiply as they are (kind::f8f6f4, at twice the
 // rate of bf16: the two terms cost what bf16 would).
 //
-// Measured: 2 x 1000 rows over 8000 bf16 keys (causal), 28 / 4 heads, 188 us (1140
-// TFLOP/s, 60 %): two tiles' step of 128 keys takes 3400 cycles, its MMAs 2064, as a
-// stream's S (1450 from its turn), softmax (1620) and P (410) follow one another; 61
-// rows over 60061 8-bit keys 88 us: 4400 a step, V's conversion and K's factors
-// sharing the issue slots.  All eight softmax warps on one stream at a time, two
-// threads per row: 189 and 103 us; P handed over in halves: 192 and 89.
+// Measured: 2 x 1000 rows over 8000 bf16 keys (causal), 28 / 4 heads, 195 to 197 us
+// (1100 TFLOP/s, 57 %): two tiles' step of 128 keys takes some 3500 cycles, its MMAs
+// 2064, as a stream's S (1450 from its turn), softmax (1620 and more) and P (410)
+// follow one another; 61 rows over 60061 8-bit keys 94 us: 4600 a step, V's
+// conversion and K's factors sharing the issue slots.  Tried while they took 188 and
+// 88: all eight softmax warps on one stream at a time, two threads per row, 189 and
+// 103; P handed over in halves 192 and 89.  Scores rounded before the reference is
+// taken off, K's factors times the row's first, cost 1 % and 4 %.
 #include <cuda_fp16.h>
 #include <type_traits>
 
@@ -41,7 +43,8 @@ namespace {
 constexpr int kStep = 1 << kPagedTcStepLog2;     // keys of a step
 constexpr int kThreads = 512;
 // Steps of a share, at least: 1, 2, 4, 8 take 128 rows over 728 bf16 keys of 32 heads
-// 19.7, 18.6, 26.1, 30.1 us, 40 rows over 3040 8-bit keys of 28 / 4 27.7, 25.3, 27.7, 35.6.
+// 19.6, 18.6, 26.3, 31.0 us, 40 rows over 3040 8-bit keys of 28 / 4 28.2, 25.6, 28.6,
+// 37.2, over 740 bf16 keys 17.9, 19.0, 27.9, 34.8.
 constexpr int kLeast = 2;
 constexpr int kNever = 0x7fffffff;
 constexpr uint32_t kTmemCols = 512;

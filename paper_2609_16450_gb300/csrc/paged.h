@@ -83,9 +83,9 @@ struct PagedParams {
 constexpr int kPagedRows = 64, kPagedCtasPerSm = 4;  // mma.sync
 constexpr int kPagedTcRows = 256;                    // tcgen05, one CTA per SM
 constexpr int kPagedTcGroup = 128;                   // query heads of a group that the tcgen05 kernel takes
-// Caches of at most so many keys per sequence: tiles stay whole (32 heads, one row
-// over 441 8-bit keys 10.3 us against 12.1, 16 x 32 rows over 472 30.9 against
-// 36.3; up to 1024, 32 rows over 982 would take 21.9 instead of 18.0).
+// Page tables of at most so many positions per sequence: tiles stay whole (32 heads,
+// one row over 441 8-bit keys 10.5 us against 12.3, 16 x 32 rows over 472 32.2
+// against 37.3; up to 1024, 32 rows over 982 would take 22.8 instead of 19.0).
 constexpr int kPagedUncutKeys = 512;
 constexpr int kPagedLongKeys = 768, kPagedLongKeysE4m3 = 2048;  // past these caches are long (ebd_paged_attention)
 cudaError_t paged_configure();
