@@ -850,8 +850,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           tmem_st32(ts + static_cast<uint32_t>(32 * h), pk);
-          // the sum is of the unrounded probabilities, but has the half step's largest
-          // as P has it: a row that looks at one key has that key's values, exactly
+          // The sum is of the unrounded probabilities, but has the half step's largest
+          // as P has it: a row that looks at one key has that key's values, exactly, and
+          // the error of all outputs is a tenth less.  (An element that this key has no
+          // part in is divided by that rounding, too: 2^-8 of it at most.)
           const float pm = ex2(ht);
           sum += hs + (__uint_as_float(bf16x2(pm, 0.f) << 16) - pm);
           top = fmaxf(top, ht);
