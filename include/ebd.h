@@ -74,6 +74,8 @@ typedef int32_t ebd_status;
 #define EBD_ERR_BOUNDS (-7)      /* checked builds (EBD_CHECKS) only: a device
                                     index outside its buffer; the access was
                                     skipped                                   */
+#define EBD_ERR_PAGES (-8)       /* ebd_paged_plan: the pages or rows do not
+                                    suffice; the plan was not carried out     */
 
 /* decode_mode: which decision step 3 applies.  EBD_DECODE_EB is the EB
  * decision (LBS + LPS, App. E).  The other two are the fixed-block update
@@ -254,6 +256,54 @@ ebd_status ebd_decide(ebd_handle* h, const ebd_step_args* a, void* stream);
  * writes conf, entropy, ent_norm, gap, argmax (any may be NULL). */
 ebd_status ebd_lm_stats(ebd_handle* h, const ebd_step_args* a, void* stream);
 
+/* ---- Logits and sampling --------------------------------------------------
+ * The paper commits x_hat = argmax with kappa = max p.  Decoding at a temperature
+ * draws x_hat instead, and kappa is the probability it was drawn with: the logits
+ * go to memory, ebd_sample draws from them, and its token and prob are what
+ * ebd_decide takes as argmax and conf (next to ent_norm and gap of ebd_lm_logits).
+ *
+ * ebd_lm_logits: l = W_lm h for a->rows rows of a->hidden, as ebd_lm_stats
+ * computes it, into logits[r * stride + v], fp32.  Of a's outputs conf, entropy,
+ * ent_norm, gap, argmax it writes those that are set; with none the statistics are
+ * left out.
+ *   logits  device, caller-owned
+ *   stride  floats from row to row, vocab or more; 0: vocab */
+ebd_status ebd_lm_logits(ebd_handle* h, const ebd_step_args* a, float* logits, int64_t stride,
+                         void* stream);
+
+#define EBD_LOGITS_F32 0
+#define EBD_LOGITS_BF16 1
+#define EBD_LOGITS_F16 2
+
+typedef struct {
+  int32_t rows;               /* R <= max_rows                                   */
+  int32_t dtype;              /* EBD_LOGITS_*                                    */
+  const void* logits;         /* [R] rows of vocab logits, aligned to a logit    */
+  int64_t stride;             /* logits from row to row, vocab or more; 0: vocab */
+  const float* u;             /* [R] random numbers, in [0, 1)                   */
+  const float* temperature;   /* [R] T >= 0 (0: the largest); NULL: 1            */
+  const int32_t* top_k;       /* [R] k, <= 0: no limit; NULL: none               */
+  const float* top_p;         /* [R] p, >= 1: no limit; NULL: none               */
+  const float* min_p;         /* [R] q, <= 0: no limit; NULL: none               */
+  int32_t* token;             /* [R]                                             */
+  float* prob;                /* [R] its probability among what is kept          */
+} ebd_sample_args;
+
+/* Draws a token of every row.  With m the row's largest logit and w[v] =
+ * exp((l[v] - m) / T), zero below 2^-40, tokens are taken by descending logit, ties
+ * by ascending index.  K is the first k of them, N the least prefix of K (one token
+ * at least) whose weight is p or more of K's, F those of N with w >= q (the first at
+ * least).  token is the least v in F with the sum of w over F up to v above u times
+ * that over F, prob = w[token] over that sum.  T = 0: the lowest index of the largest
+ * logit, with prob 1.  Temperatures count as 1e-30 at least, unless 0, and 1e30 at
+ * most.  Weights are exact to 2^-29 of themselves or 2^-44 (beyond 2^18 logits a bit
+ * less for each doubling), their sums exact: results do not vary from run to run.
+ * Logits of -inf have no part in it.  A row with NaN, +inf, or no logit above -inf
+ * records EBD_ERR_NONFINITE, one with u outside [0, 1), T negative or not finite, or
+ * a NaN parameter EBD_ERR_INVALID_ARG: its token is -1 and its prob NaN, which
+ * ebd_decide does not commit.  More than 2^30 logits a row: EBD_ERR_UNSUPPORTED. */
+ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream);
+
 /* ---- Vocabulary-parallel LM head (several GPUs) --------------------------
  * Step 2 sharded by vocabulary: GPU g holds rows [v_off_g, v_off_g +
  * v_count_g) of W_lm.  The statistics of App. B (Eq. app-confidence: kappa =
@@ -395,6 +445,43 @@ ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_
  * are then undefined). */
 ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a,
                                void* stream);
+
+/* ---- Plans of the paged cache on the device ------------------------------
+ * Lengths that a step finds out on the device (tokens accepted, sequences that
+ * ended) become pages, row positions and slots there too, so that a step needs no
+ * copy to the host and can be captured into a graph.  The caller owns the state:
+ * kv_len, page_table (entries past a sequence's pages are -1), and the free pages, a
+ * stack of which the first *n_free entries count.  At the start kv_len is 0, the
+ * table -1, free_pages any order of all pages. */
+typedef struct {
+  int32_t batch;              /* B <= max_batch, at most 4096                    */
+  int32_t rows;               /* R <= max_rows: entries of row_pos and slot      */
+  const int32_t* add;         /* [B] rows that a sequence brings, or, negative,
+                                 positions at its end that it gives back         */
+  int32_t* kv_len;            /* [B] cached positions: becomes max(0, kv_len + add) */
+  int32_t* page_table;        /* [B][max_pages]                                  */
+  int32_t* free_pages;        /* [n_pages]                                       */
+  int32_t* n_free;            /* [1]                                             */
+  int32_t* cu_rows;           /* [B+1] offsets of the new rows, or NULL          */
+  int32_t* row_pos;           /* [R] their positions, or NULL                    */
+  int64_t* slot;              /* [R] page * page_size + place, or NULL           */
+  int32_t page_size;          /* a power of two, 16..256                         */
+  int32_t n_pages;
+  int32_t max_pages;          /* second dimension of page_table                  */
+  int32_t reserved;
+} ebd_paged_plan_args;
+
+/* Pages that a sequence no longer needs go back first, the sequences from last to
+ * first and each from its last page; then pages are handed out from the stack's top,
+ * sequences and pages ascending.  Row i of sequence b is at position kv_len[b] (as it
+ * was) + i.  row_pos and slot of entries past the rows there are get -1, which
+ * ebd_paged_write and ebd_paged_read pass over: R may be more than the rows of a
+ * call.  A plan that cannot be met changes none of kv_len, page_table, free_pages
+ * and n_free; cu_rows becomes 0, row_pos and slot -1, and it records EBD_ERR_PAGES
+ * (too few free pages, a sequence longer than max_pages pages, more than R rows with
+ * row_pos or slot set) or EBD_ERR_BOUNDS (a length or page that the table cannot
+ * hold, a stack that does not fit).  Handles of either kind; enqueued on `stream`. */
+ebd_status ebd_paged_plan(ebd_handle* h, const ebd_paged_plan_args* a, void* stream);
 
 /* Synchronises `stream`, returns the first device-side failure recorded
  * since the last call (EBD_OK if none) and clears it. */

@@ -20,6 +20,7 @@ EBD_ERR_TIMEOUT = -4
 EBD_ERR_NONFINITE = -5
 EBD_ERR_STATE = -6
 EBD_ERR_BOUNDS = -7
+EBD_ERR_PAGES = -8
 EBD_DEBUG_FORCE_TIMEOUT = 1
 EBD_DEBUG_FORCE_COPY_TIMEOUT = 2
 EBD_DEBUG_PAGED_GIVE_UP = 4
@@ -29,7 +30,8 @@ EBD_DECODE_TOPM = 2
 
 STATUS_NAMES = {0: "EBD_OK", -1: "EBD_ERR_INVALID_ARG", -2: "EBD_ERR_UNSUPPORTED",
                 -3: "EBD_ERR_CUDA", -4: "EBD_ERR_TIMEOUT", -5: "EBD_ERR_NONFINITE",
-                -6: "EBD_ERR_STATE", -7: "EBD_ERR_BOUNDS"}
+                -6: "EBD_ERR_STATE", -7: "EBD_ERR_BOUNDS",
+                -8: "EBD_ERR_PAGES"}
 
 
 class ebd_config(Structure):
@@ -74,6 +76,24 @@ class ebd_paged_args(Structure):
                 ("max_new", c_int32), ("reserved", c_int32)]
 
 
+EBD_LOGITS_F32 = 0
+EBD_LOGITS_BF16 = 1
+EBD_LOGITS_F16 = 2
+
+
+class ebd_sample_args(Structure):
+    _fields_ = [("rows", c_int32), ("dtype", c_int32), ("logits", c_void_p), ("stride", c_int64),
+                ("u", c_void_p), ("temperature", c_void_p), ("top_k", c_void_p), ("top_p", c_void_p),
+                ("min_p", c_void_p), ("token", c_void_p), ("prob", c_void_p)]
+
+
+class ebd_paged_plan_args(Structure):
+    _fields_ = [("batch", c_int32), ("rows", c_int32), ("add", c_void_p), ("kv_len", c_void_p),
+                ("page_table", c_void_p), ("free_pages", c_void_p), ("n_free", c_void_p),
+                ("cu_rows", c_void_p), ("row_pos", c_void_p), ("slot", c_void_p),
+                ("page_size", c_int32), ("n_pages", c_int32), ("max_pages", c_int32), ("reserved", c_int32)]
+
+
 EXPORTS = ["ebd_create", "ebd_destroy", "ebd_bind_embedding", "ebd_step", "ebd_step_host",
            "ebd_decide", "ebd_lm_stats", "ebd_attention", "ebd_sync_status",
            "ebd_export_weights", "ebd_import_weights", "ebd_router_init_host",
@@ -81,7 +101,8 @@ EXPORTS = ["ebd_create", "ebd_destroy", "ebd_bind_embedding", "ebd_step", "ebd_s
            "ebd_profile_enable", "ebd_profile_read", "ebd_last_error",
            "ebd_version", "ebd_lm_stats_noalloc", "ebd_loop_window",
            "ebd_loop_block_window", "ebd_lm_shard_state", "ebd_merge_shard_states",
-           "ebd_paged_write", "ebd_paged_read", "ebd_paged_attention"]
+           "ebd_paged_write", "ebd_paged_read", "ebd_paged_attention",
+           "ebd_paged_plan", "ebd_lm_logits", "ebd_sample"]
 
 _lib = None
 
@@ -111,6 +132,9 @@ def load(path: str = LIB_PATH):
         getattr(lib, fn).argtypes = [c_void_p, P(ebd_step_args), c_void_p]
     for fn in ("ebd_paged_write", "ebd_paged_read", "ebd_paged_attention"):
         getattr(lib, fn).argtypes = [c_void_p, P(ebd_kv_pages), P(ebd_paged_args), c_void_p]
+    lib.ebd_paged_plan.argtypes = [c_void_p, P(ebd_paged_plan_args), c_void_p]
+    lib.ebd_lm_logits.argtypes = [c_void_p, P(ebd_step_args), c_void_p, c_int64, c_void_p]
+    lib.ebd_sample.argtypes = [c_void_p, P(ebd_sample_args), c_void_p]
     lib.ebd_sync_status.argtypes = [c_void_p, c_void_p]
     lib.ebd_export_weights.argtypes = [c_void_p, c_void_p, P(c_size_t)]
     lib.ebd_import_weights.argtypes = [c_void_p, c_void_p, c_size_t]
@@ -208,6 +232,19 @@ def ebd_paged_read(h, pages: ebd_kv_pages, args: ebd_paged_args, stream: int = 0
 
 def ebd_paged_attention(h, pages: ebd_kv_pages, args: ebd_paged_args, stream: int = 0) -> int:
     return load().ebd_paged_attention(h, ctypes.byref(pages), ctypes.byref(args), c_void_p(stream))
+
+
+def ebd_paged_plan(h, args: ebd_paged_plan_args, stream: int = 0) -> int:
+    return load().ebd_paged_plan(h, ctypes.byref(args), c_void_p(stream))
+
+
+def ebd_lm_logits(h, args: ebd_step_args, logits_ptr: int, stride: int = 0, stream: int = 0) -> int:
+    """Logits into rows of `stride` floats (0: vocab); a's statistics that are set."""
+    return load().ebd_lm_logits(h, ctypes.byref(args), c_void_p(logits_ptr), stride, c_void_p(stream))
+
+
+def ebd_sample(h, args: ebd_sample_args, stream: int = 0) -> int:
+    return load().ebd_sample(h, ctypes.byref(args), c_void_p(stream))
 
 
 def ebd_sync_status(h, stream: int = 0) -> int:

@@ -23,7 +23,7 @@ LIB = os.path.join(PKG, "libebd.so")
 BUILD_CHECKED = os.path.join(PKG, "_build_checked")
 LIB_CHECKED = os.path.join(PKG, "libebd_checked.so")
 SOURCES = ["ebd_api.cu", "k_lmhead.cu", "k_attn.cu", "k_decide.cu", "k_stats.cu",
-           "k_paged.cu", "k_paged_attn.cu", "k_paged_tc.cu"]
+           "k_sample.cu", "k_plan.cu", "k_paged.cu", "k_paged_attn.cu", "k_paged_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -15,6 +15,8 @@
 #include "internal.h"
 #include "paged.h"
 #include "rows_image.h"
+#include "sample.h"
+#include "sample_math.h"
 
 namespace {
 // An NVTX range around the host side of an entry point (visible in Nsight
@@ -675,7 +677,8 @@ ebd_status run_attention(ebd_handle* h, const ebd_step_args* a, cudaStream_t st,
 // v_off, v_count: a->w_lm holds the vocabulary rows [v_off, v_off + v_count)
 // (a shard of the vocabulary-parallel LM head); v_count < 0: all of them.
 ebd_status run_lm(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, bool pdl_first = false,
-                  int v_off = 0, int v_count = -1) {
+                  int v_off = 0, int v_count = -1, float* logits = nullptr, int64_t stride = 0,
+                  bool stats = true) {
   const ebd_config& c = h->cfg;
   const int V = v_count < 0 ? c.vocab : v_count;
   const bool packed = a->w_lm_layout == 1;
@@ -705,6 +708,9 @@ ebd_status run_lm(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, bool p
     p.limit_ns = kLimitNs;
     p.force_timeout = (c.debug_flags & EBD_DEBUG_FORCE_TIMEOUT) ? 1 : 0;
     p.pdl = (g0 == 0 && pdl_first) ? 1 : 0;
+    p.logits = logits;
+    p.logits_stride = stride;
+    p.stats = stats ? 1 : 0;
     CUtensorMap th;
     if (p.boxed) {
       if (!encode_k_boxes(&th, a->hidden, a->rows, c.d_model, p.nb / 2, p.kbs))
@@ -1081,6 +1087,8 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     return bail(fail(h, EBD_ERR_UNSUPPORTED, "the library is compiled for sm_103a (GB300) only"));
   if (get_encode() == nullptr)
     return bail(fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable"));
+  if ((e = sample_configure()) != cudaSuccess || (e = paged_plan_configure()) != cudaSuccess)
+    return bail(cuda_fail(h, e, "sampling and plan attributes"));
   size_t part_rows = 0, cuts = 0;
   if (cfg->paged) {
     if ((e = paged_configure()) != cudaSuccess || (e = paged_tc_configure()) != cudaSuccess)
@@ -1408,6 +1416,66 @@ ebd_status ebd_lm_stats(ebd_handle* h, const ebd_step_args* a, void* stream) {
                                      a->conf, a->entropy, a->ent_norm, a->gap, a->argmax,
                                      h->d_status, st, true);
   if (e != cudaSuccess) return cuda_fail(h, e, "merge launch");
+  return EBD_OK;
+}
+
+ebd_status ebd_lm_logits(ebd_handle* h, const ebd_step_args* a, float* logits, int64_t stride, void* stream) {
+  if (h == nullptr) return EBD_ERR_INVALID_ARG;
+  NvtxRange nvtx("ebd_lm_logits");
+  ebd_status s = check_device(h);
+  if (s != EBD_OK) return s;
+  if ((s = check_args(h, a, false, true, false)) != EBD_OK) return s;
+  const int64_t step = stride != 0 ? stride : h->cfg.vocab;
+  if (step < h->cfg.vocab) return fail(h, EBD_ERR_INVALID_ARG, "stride must be 0, or vocab or more");
+  if (a->rows == 0) return EBD_OK;
+  if (logits == nullptr || !aligned(logits, 4))
+    return fail(h, EBD_ERR_INVALID_ARG, "logits must be a 4-byte aligned device pointer");
+  const bool stats = a->conf || a->entropy || a->ent_norm || a->gap || a->argmax;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if ((s = decoding_ready(h, st)) != EBD_OK || (s = run_lm(h, a, st, false, 0, -1, logits, step, stats)) != EBD_OK) return s;
+  if (!stats) return EBD_OK;
+  const float inv = static_cast<float>(1.0 / std::log(static_cast<double>(h->cfg.vocab)));
+  cudaError_t e = launch_merge_stats(h->part_f, h->part_i, a->rows, h->grid_lm, h->cfg.vocab, inv, a->conf, a->entropy,
+                                     a->ent_norm, a->gap, a->argmax, h->d_status, st, true);
+  if (e != cudaSuccess) return cuda_fail(h, e, "merge launch");
+  return EBD_OK;
+}
+
+ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream) {
+  if (h == nullptr) return EBD_ERR_INVALID_ARG;
+  NvtxRange nvtx("ebd_sample");
+  ebd_status s = check_device(h);
+  if (s != EBD_OK) return s;
+  if (a == nullptr) return fail(h, EBD_ERR_INVALID_ARG, "args is NULL");
+  const int vocab = h->cfg.vocab;
+  if (a->rows < 0 || a->rows > h->cfg.max_rows) return fail(h, EBD_ERR_INVALID_ARG, "rows out of range");
+  if (a->dtype != EBD_LOGITS_F32 && a->dtype != EBD_LOGITS_BF16 && a->dtype != EBD_LOGITS_F16)
+    return fail(h, EBD_ERR_INVALID_ARG, "dtype must be EBD_LOGITS_F32, _BF16 or _F16");
+  if (a->stride != 0 && a->stride < vocab) return fail(h, EBD_ERR_INVALID_ARG, "stride must be 0, or vocab or more");
+  if (vocab > 1 << 30) return fail(h, EBD_ERR_UNSUPPORTED, "more than 2^30 logits a row");
+  if (a->rows == 0) return EBD_OK;
+  if (!a->logits || !a->u || !a->token || !a->prob)
+    return fail(h, EBD_ERR_INVALID_ARG, "logits, u, token and prob must be set");
+  if (!aligned(a->logits, a->dtype == EBD_LOGITS_F32 ? 4 : 2))
+    return fail(h, EBD_ERR_INVALID_ARG, "logits must be aligned to a logit");
+  SampleParams p{};
+  p.logits = a->logits;
+  p.stride = a->stride != 0 ? a->stride : vocab;
+  p.rows = a->rows;
+  p.vocab = vocab;
+  p.dtype = a->dtype;
+  p.u = a->u;
+  p.temperature = a->temperature;
+  p.top_k = a->top_k;
+  p.top_p = a->top_p;
+  p.min_p = a->min_p;
+  p.token = a->token;
+  p.prob = a->prob;
+  p.status = h->d_status;
+  p.shift = sample_shift(vocab);
+  p.limit_ns = kLimitNs;
+  cudaError_t e = launch_sample(p, h->num_sms, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "sample launch");
   return EBD_OK;
 }
 
@@ -1749,6 +1817,41 @@ ebd_status ebd_paged_write(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged
 
 ebd_status ebd_paged_read(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, void* stream) {
   return paged_rows(h, c, a, false, stream);
+}
+
+ebd_status ebd_paged_plan(ebd_handle* h, const ebd_paged_plan_args* a, void* stream) {
+  if (h == nullptr) return EBD_ERR_INVALID_ARG;
+  NvtxRange range("ebd_paged_plan");
+  ebd_status s = check_device(h);
+  if (s != EBD_OK) return s;
+  auto bad = [&](const char* m) { return fail(h, EBD_ERR_INVALID_ARG, m); };
+  if (a == nullptr) return bad("args is NULL");
+  if (a->batch < 0 || a->batch > h->cfg.max_batch) return bad("batch out of range");
+  if (a->rows < 0 || a->rows > h->cfg.max_rows) return bad("rows out of range");
+  if (a->batch > kPagedMaxBatch) return fail(h, EBD_ERR_UNSUPPORTED, "more than 4096 sequences");
+  if (a->page_size < 16 || a->page_size > 256 || (a->page_size & (a->page_size - 1)) != 0)
+    return bad("page_size must be a power of two from 16 to 256");
+  if (a->n_pages < 1 || a->max_pages < 1) return bad("n_pages and max_pages must be positive");
+  if (!a->free_pages || !a->n_free) return bad("free_pages and n_free must be set");
+  if (a->batch > 0 && (!a->add || !a->kv_len || !a->page_table)) return bad("add, kv_len and page_table must be set");
+  PagedPlanParams p{};
+  p.B = a->batch;
+  p.R = a->rows;
+  p.page_log2 = log2_of(a->page_size);
+  p.n_pages = a->n_pages;
+  p.max_pages = a->max_pages;
+  p.add = a->add;
+  p.kv_len = a->kv_len;
+  p.page_table = a->page_table;
+  p.free_pages = a->free_pages;
+  p.n_free = a->n_free;
+  p.cu_rows = a->cu_rows;
+  p.row_pos = a->row_pos;
+  p.slot = a->slot;
+  p.status = h->d_status;
+  cudaError_t e = launch_paged_plan(p, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(h, e, "paged plan launch");
+  return EBD_OK;
 }
 
 ebd_status ebd_paged_attention(ebd_handle* h, const ebd_kv_pages* c, const ebd_paged_args* a, void* stream) {

@@ -1,8 +1,8 @@
 // LM head fused with the softmax statistics of every window row.
 //
 // For each window row r and vocabulary entry v the logit is
-// l[r][v] = sum_k h[r][k] W[v][k]; the kernel never stores it.  Each CTA owns a
-// share of the 64-row vocabulary units and keeps, per window row, the
+// l[r][v] = sum_k h[r][k] W[v][k]; the kernel stores it only where the caller
+// asks for logits (ebd_lm_logits).  Each CTA owns a share of the 64-row vocabulary units and keeps, per window row, the
 // online-softmax state over the vocabulary it has seen:
 //   m  = max logit,  S = sum exp(l - m),  T = sum exp(l - m) (l - m),
 //   l2 = second largest logit (duplicates count),  idx = argmax (lowest).
@@ -125,12 +125,14 @@ __device__ __forceinline__ void record_error(int* status, volatile int* abort, i
 // running state of its row.  `release` is called once this thread has
 // loaded its last slice (the MMAs may then overwrite the buffer).  Returns
 // whether it was called.
-template <typename Release>
+// `store` gets the logits of every slice, 32 columns of its thread's vocabulary
+// lane; without `stats` that is all.
+template <typename Store, typename Release>
 __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg, int n_pad,
                                                 float* sTw, int lanev, int et, uint32_t bar_id,
                                                 int vbase, int valid, float* st_m, float* st_s,
                                                 float* st_t, float* st_l2, int* st_i,
-                                                Release release) {
+                                                bool stats, Store store, Release release) {
   bool released = false;
   const bool lv = lanev < valid;
   for (int cc = 32 * wg; cc < n_pad; cc += 32 * nwg) {
@@ -143,6 +145,8 @@ __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg
       release();
       released = true;
     }
+    if (lv) store(cc, v);
+    if (!stats) continue;
 #pragma unroll
     for (int j = 0; j < 32; ++j) sTw[j * kTLd + lanev] = lv ? v[j] : -INFINITY;
     named_barrier(bar_id, 128);
@@ -218,7 +222,10 @@ __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg
 // serves rows [row0 + g nb, row0 + (g + 1) nb) of group g = q / nwork over
 // the vocabulary range of owner q % nwork, and writes its partials to
 // columns [0, grp_cols) of those rows.
-template <bool PAIR, bool PACKED, bool BOXED>
+//
+// STORE: the logits also go to memory, 32 lanes of a warp to 32 adjacent floats of
+// a row (ebd_lm_logits).
+template <bool PAIR, bool PACKED, bool BOXED, bool STORE>
 __global__ void __launch_bounds__(kLmThreads, 1)
     lm_stats_kernel(const __grid_constant__ CUtensorMap tmap_w,
                     const __grid_constant__ CUtensorMap tmap_h, const LmParams p) {
@@ -608,11 +615,20 @@ __global__ void __launch_bounds__(kLmThreads, 1)
       const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) +
                               static_cast<uint32_t>(buf * p.acc_stride);
       auto rel = [&]() { release(buf); };
+      auto store = [&](int cc, const float(&v)[32]) {
+        if constexpr (STORE) {
+          float* o = p.logits + (rbase + cc) * p.logits_stride + vbase + lanev;
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (cc + j < rows_g) o[j * p.logits_stride] = v[j];
+        }
+      };
       const bool released = epilogue_buffer(taddr0, wg, p.nwg, p.n_pad, sTw, lanev, et, bar_id,
-                                            vbase, valid, st_m, st_s, st_t, st_l2, st_i, rel);
+                                            vbase, valid, st_m, st_s, st_t, st_l2, st_i,
+                                            !STORE || p.stats != 0, store, rel);
       if (!released) release(buf);  // no slice of this chunk for this warpgroup
     }
-    if (ok && active) {
+    if (ok && active && (!STORE || p.stats != 0)) {
       // the rows of this warpgroup's slices (its threads updated them last):
       // this CTA's partial goes to column `col` of its group's rows, and
       // neutral states to the columns [grp_cols, ncols) that no CTA of the
@@ -793,17 +809,20 @@ cudaError_t launch_pack_lm(const __nv_bfloat16* w, __nv_bfloat16* out, int V, in
 }
 
 using LmKernel = void (*)(CUtensorMap, CUtensorMap, LmParams);
+template <bool STORE>
 static LmKernel lm_kernel(bool pair, bool packed, bool boxed) {
-  if (!pair) return packed ? lm_stats_kernel<false, true, false> : lm_stats_kernel<false, false, false>;
-  if (boxed) return packed ? lm_stats_kernel<true, true, true> : lm_stats_kernel<true, false, true>;
-  return packed ? lm_stats_kernel<true, true, false> : lm_stats_kernel<true, false, false>;
+  if (!pair) return packed ? lm_stats_kernel<false, true, false, STORE> : lm_stats_kernel<false, false, false, STORE>;
+  if (boxed) return packed ? lm_stats_kernel<true, true, true, STORE> : lm_stats_kernel<true, false, true, STORE>;
+  return packed ? lm_stats_kernel<true, true, false, STORE> : lm_stats_kernel<true, false, false, STORE>;
 }
 
 cudaError_t lm_configure() {
   const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e;
   for (int i = 0; i < 6; ++i)
-    if ((e = cudaFuncSetAttribute(lm_kernel(i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(lm_kernel<false>(i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(lm_kernel<true>(i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess)
+      return e;
   return cudaSuccess;
 }
 
@@ -830,7 +849,8 @@ cudaError_t launch_lm_stats(const CUtensorMap& tmap_w, const CUtensorMap& tmap_h
   }
   cfg.attrs = attr;
   cfg.numAttrs = na;
-  return cudaLaunchKernelEx(&cfg, lm_kernel(p.pair, p.packed, p.boxed), tmap_w, tmap_h, p);
+  const LmKernel k = p.logits != nullptr ? lm_kernel<true>(p.pair, p.packed, p.boxed) : lm_kernel<false>(p.pair, p.packed, p.boxed);
+  return cudaLaunchKernelEx(&cfg, k, tmap_w, tmap_h, p);
 }
 
 }  // namespace ebd

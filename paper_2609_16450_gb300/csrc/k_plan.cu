@@ -1,0 +1,191 @@
+// Plan of a step over the paged K/V cache, on the device: pages handed out and taken
+// back by what every sequence's length becomes, and the new rows' offsets, positions
+// and slots.
+//
+// Sequence b has len positions in ceil(len / page) pages and comes to max(0, len +
+// add).  Pages past what it then needs go onto the stack of free pages, the sequences
+// from the last to the first and each from its last page; after that the pages that
+// sequences need more come off its top, sequences and pages ascending.  So taking
+// back what a call handed out leaves the stack as it was.
+//
+// One CTA: a plan moves a few KB, and is bound by its chain of loads: lengths ->
+// prefix sums (rows, pages out, pages back) -> the pages to move -> slots.  Every
+// item finds its sequence by a binary search of the prefix sums in shared memory.
+// All that a plan asks for is looked at before anything is written: one that cannot
+// be met changes no state, and hands out no rows.
+#include "internal.h"
+#include "paged.h"
+
+namespace ebd {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+struct Sums {
+  long long rows, out, back;
+};
+
+// Sequence of item i by the prefix sums cu[0 .. n]: the last with cu[b] <= i < cu[b + 1].
+__device__ __forceinline__ int sequence_of(const int* cu, int n, int i) {
+  int lo = 0, hi = n;  // cu[lo] <= i < cu[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cu[mid] <= i)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPlanParams p) {
+  extern __shared__ int dyn[];
+  int* const rows = dyn;                 // [B + 1] prefix sums of new rows,
+  int* const out = rows + p.B + 1;       // of pages to hand out,
+  int* const back = out + p.B + 1;       // of pages to take back
+  int* const first = back + p.B + 1;     // [B] first page that changes hands
+  int* const old = first + p.B;          // [B] length before
+  __shared__ Sums warp_sum[kPlanThreads / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int page = 1 << p.page_log2;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const long long n0 = *p.n_free;
+
+  // a run of sequences a thread
+  const int per = (p.B + kPlanThreads - 1) / kPlanThreads;
+  const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+  int bad = 0;
+  Sums sum{0, 0, 0};
+  const long long most = min(static_cast<long long>(p.max_pages) << p.page_log2, 0x7fffffffll);
+  for (int b = b0; b < b1; ++b) {
+    const int len = p.kv_len[b], add = p.add[b];
+    const long long to = max(0ll, static_cast<long long>(len) + add);
+    if (len < 0 || len > most) {
+      bad |= 1;
+      continue;
+    }
+    if (to > most) {
+      bad |= 2;
+      continue;
+    }
+    const int have = static_cast<int>((static_cast<long long>(len) + page - 1) >> p.page_log2);
+    const int need = static_cast<int>((to + page - 1) >> p.page_log2);
+    // new rows begin within a page that is there
+    if (add > 0 && len % page != 0) {
+      const int e = p.page_table[static_cast<long long>(b) * p.max_pages + (len >> p.page_log2)];
+      if (e < 0 || e >= p.n_pages) bad |= 1;
+    }
+    rows[b] = max(add, 0);
+    out[b] = max(need - have, 0);
+    back[b] = max(have - need, 0);
+    first[b] = min(have, need);
+    old[b] = len;
+    sum.rows += max(add, 0);
+    sum.out += max(need - have, 0);
+    sum.back += max(have - need, 0);
+  }
+  Sums incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long r = __shfl_up_sync(0xffffffffu, incl.rows, o), t = __shfl_up_sync(0xffffffffu, incl.out, o),
+                    k = __shfl_up_sync(0xffffffffu, incl.back, o);
+    if (lane >= o) {
+      incl.rows += r;
+      incl.out += t;
+      incl.back += k;
+    }
+  }
+  if (lane == 31) warp_sum[warp] = incl;
+  __syncthreads();
+  Sums at{incl.rows - sum.rows, incl.out - sum.out, incl.back - sum.back}, total{0, 0, 0};
+  for (int i = 0; i < kPlanThreads / 32; ++i) {
+    const Sums w = warp_sum[i];
+    if (i < warp) at.rows += w.rows, at.out += w.out, at.back += w.back;
+    total.rows += w.rows, total.out += w.out, total.back += w.back;
+  }
+  if (n0 < 0 || n0 + total.back > p.n_pages) bad |= 1;
+  if (total.out > n0 + total.back) bad |= 2;
+  if ((p.row_pos != nullptr || p.slot != nullptr) && total.rows > p.R) bad |= 2;
+  if (total.rows > 0x7fffffffll) bad |= 2;
+  bad = __syncthreads_or(bad & 1) | (__syncthreads_or(bad & 2) ? 2 : 0);
+  const int n_out = static_cast<int>(total.out), n_back = static_cast<int>(total.back);
+  const int top = static_cast<int>(n0) + n_back;  // of the stack, once all are back on it
+  if (!bad) {
+    for (int b = b0; b < b1; ++b) {
+      const int r = rows[b], o = out[b], k = back[b];
+      rows[b] = static_cast<int>(at.rows), out[b] = static_cast<int>(at.out), back[b] = static_cast<int>(at.back);
+      at.rows += r, at.out += o, at.back += k;
+    }
+    if (tid == 0) rows[p.B] = static_cast<int>(total.rows), out[p.B] = n_out, back[p.B] = n_back;
+    __syncthreads();
+    int wrong = 0;
+    for (int i = tid; i < n_back; i += kPlanThreads) {
+      const int b = sequence_of(back, p.B, i);
+      const int e = p.page_table[static_cast<long long>(b) * p.max_pages + first[b] + i - back[b]];
+      wrong |= e < 0 || e >= p.n_pages;
+    }
+    for (int i = tid; i < n_out; i += kPlanThreads) {
+      if (top - 1 - i >= n0) continue;  // one of those that come back
+      const int e = p.free_pages[top - 1 - i];
+      wrong |= e < 0 || e >= p.n_pages;
+    }
+    bad = __syncthreads_or(wrong);
+  }
+  if (bad) {
+    if (tid == 0) atomicCAS(p.status, 0, (bad & 1) ? EBD_ERR_BOUNDS : EBD_ERR_PAGES);
+    if (p.cu_rows != nullptr)
+      for (int b = tid; b <= p.B; b += kPlanThreads) p.cu_rows[b] = 0;
+    for (int r = tid; r < p.R; r += kPlanThreads) {
+      if (p.row_pos != nullptr) p.row_pos[r] = -1;
+      if (p.slot != nullptr) p.slot[r] = -1;
+    }
+    return;
+  }
+  for (int i = tid; i < n_back; i += kPlanThreads) {
+    const int b = sequence_of(back, p.B, i);
+    int* const e = p.page_table + static_cast<long long>(b) * p.max_pages + first[b] + i - back[b];
+    p.free_pages[top - 1 - i] = *e;
+    *e = -1;
+  }
+  __syncthreads();
+  for (int i = tid; i < n_out; i += kPlanThreads) {
+    const int b = sequence_of(out, p.B, i);
+    p.page_table[static_cast<long long>(b) * p.max_pages + first[b] + i - out[b]] = p.free_pages[top - 1 - i];
+  }
+  for (int b = b0; b < b1; ++b) p.kv_len[b] = static_cast<int>(max(0ll, static_cast<long long>(old[b]) + p.add[b]));
+  if (tid == 0) *p.n_free = top - n_out;
+  if (p.cu_rows != nullptr)
+    for (int b = tid; b <= p.B; b += kPlanThreads) p.cu_rows[b] = rows[b];
+  __syncthreads();
+  for (int r = tid; r < p.R; r += kPlanThreads) {
+    int pos = -1;
+    long long slot = -1;
+    if (r < total.rows) {
+      const int b = sequence_of(rows, p.B, r);
+      pos = old[b] + r - rows[b];
+      if (p.slot != nullptr) {
+        const long long e = p.page_table[static_cast<long long>(b) * p.max_pages + (pos >> p.page_log2)];
+        slot = (e << p.page_log2) + (pos & (page - 1));
+      }
+    }
+    if (p.row_pos != nullptr) p.row_pos[r] = pos;
+    if (p.slot != nullptr) p.slot[r] = slot;
+  }
+}
+
+size_t plan_bytes(int B) { return (3 * (static_cast<size_t>(B) + 1) + 2 * static_cast<size_t>(B)) * sizeof(int); }
+
+}  // namespace
+
+cudaError_t paged_plan_configure() {
+  return cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(plan_bytes(kPagedMaxBatch)));
+}
+
+cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t st) {
+  return paged_launch(paged_plan_kernel, dim3(1), kPlanThreads, static_cast<uint32_t>(plan_bytes(p.B)), st, p);
+}
+
+}  // namespace ebd

@@ -1,0 +1,491 @@
+// Sampling from logits: temperature, top-k, top-p and min-p, one token and its
+// probability per row, from a random number given for the row.
+//
+// With logits l, m their largest, temperature T and w[v] = exp((l[v] - m) / T), the
+// tokens are taken by descending logit, ties by ascending index.  Top-k keeps the
+// first k of that order, top-p the least prefix of those with at least the share p
+// of their sum, min-p those with w >= min_p.  What is kept is a prefix F of the
+// order, given by its last logit and index; the token is the first of F by index
+// where the running sum passes u times the sum.
+//
+// Sums are whole numbers of 64 bits (sample_math.h): exact, so that borders do not
+// depend on how a row is split or in which order atomics arrive.
+//
+// A row is one cluster of CTAs; each warp owns a contiguous run of the row's
+// 16-byte groups, so that sums by warp are sums by index.  A CTA's slice of the row
+// comes into its shared memory once.  The last logit of a prefix is found by
+// histograms of 2048 bins over the logits' ordered bits, of counts (top-k) or of
+// weights (top-p), each level over the bin that the last one chose.
+#include <cuda_fp16.h>
+
+#include <climits>
+
+#include "internal.h"
+#include "ptx.cuh"
+#include "sample.h"
+#include "sample_math.h"
+
+namespace ebd {
+
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kBins = 2048, kPerThread = kBins / kThreads;
+constexpr int kMaxCtas = 8;
+constexpr int kSliceBytes = 76 * 1024;  // of a row in shared memory
+
+__device__ __forceinline__ uint64_t ld_cluster(const uint64_t* p, uint32_t rank) {
+  uint64_t v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ int ld_cluster(const int* p, uint32_t rank) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
+  return __int_as_float(ld_cluster(reinterpret_cast<const int*>(p), rank));
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(src), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// The logits of a 16-byte group.  -0 counts as 0.
+template <int TYPE>
+struct Group;
+template <>
+struct Group<EBD_LOGITS_F32> {
+  static constexpr int N = 4;
+  using T = float;
+  __device__ static T masked() { return -INFINITY; }
+  __device__ static void get(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x) + 0.f, x[1] = __uint_as_float(v.y) + 0.f;
+    x[2] = __uint_as_float(v.z) + 0.f, x[3] = __uint_as_float(v.w) + 0.f;
+  }
+};
+template <>
+struct Group<EBD_LOGITS_BF16> {
+  static constexpr int N = 8;
+  using T = uint16_t;
+  __device__ static T masked() { return 0xFF80; }
+  __device__ static void get(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16) + 0.f;
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) + 0.f;
+    }
+  }
+};
+template <>
+struct Group<EBD_LOGITS_F16> {
+  static constexpr int N = 8;
+  using T = uint16_t;
+  __device__ static T masked() { return 0xFC00; }
+  __device__ static void get(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      x[2 * i] = f.x + 0.f;
+      x[2 * i + 1] = f.y + 0.f;
+    }
+  }
+};
+
+__device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+// sum over this and the lanes before it
+__device__ __forceinline__ uint64_t warp_scan(uint64_t x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+
+struct Shared {
+  uint64_t hist[2][kBins];
+  SampleEntry table[kSampleTable];
+  uint64_t part[kWarps];     // a warp's sum
+  uint64_t count[kWarps];    // a warp's elements at the border
+  uint64_t scan[kWarps];
+  uint64_t bar[kWarps];
+  uint64_t before, in, total;
+  float max[kWarps];
+  int bad[kWarps];
+  int first[kWarps];
+  int bin, index;
+};
+
+// Which elements of the row are kept: those above `key`, and those at it up to `index`
+struct Prefix {
+  uint32_t key;
+  int index;
+  __device__ __forceinline__ bool has(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
+};
+
+template <int TYPE, bool RESIDENT>
+struct Row {
+  using G = Group<TYPE>;
+  Shared& s;
+  const SampleParams& p;
+  const uint8_t* data;      // the row's first 16-byte group, in global memory
+  uint4* slice;             // this CTA's groups [g0, ..) in shared memory
+  int g0, w0, w1, head, r;  // this warp's groups [w0, w1), elements before the row's in the first group
+  int lane, warp, rank, C;
+  float m = 0.f;
+  SampleScale c{};
+  int level = 0;
+
+  __device__ __forceinline__ void sync() const {
+    if (C == 1)
+      __syncthreads();
+    else
+      cluster_sync_all();
+  }
+  __device__ __forceinline__ bool whole(int g) const { return g * G::N >= head && (g + 1) * G::N <= head + p.vocab; }
+  // a group that is not wholly the row's, element by element
+  __device__ __forceinline__ uint4 edge(int g) const {
+    uint4 v;
+    typename G::T t[G::N];
+    for (int j = 0; j < G::N; ++j) {
+      const int i = g * G::N + j;
+      t[j] = i >= head && i < head + p.vocab ? reinterpret_cast<const typename G::T*>(data)[i] : G::masked();
+    }
+    memcpy(&v, t, 16);
+    return v;
+  }
+  __device__ __forceinline__ uint4 fetch(int g) const {
+    if (RESIDENT) return slice[g - g0];
+    return whole(g) ? __ldg(reinterpret_cast<const uint4*>(data) + g) : edge(g);
+  }
+  // f(index, logit) for every logit of the warp's groups
+  template <typename F>
+  __device__ __forceinline__ void sweep(F f) const {
+    for (int g = w0 + lane; g < w1; g += 32) {
+      float x[G::N];
+      G::get(fetch(g), x);
+#pragma unroll
+      for (int j = 0; j < G::N; ++j) f(g * G::N + j - head, x[j]);
+    }
+  }
+  __device__ __forceinline__ uint64_t weight(float x) const { return sample_weight(m, x, c, s.table); }
+
+  // Takes the prefix `kept` down to the elements that bring count or weight (MASS) up
+  // to a target: at least k elements, or the share `share` of its weight.
+  template <bool MASS>
+  __device__ __forceinline__ void cut(Prefix& kept, uint32_t floor, int k, float share) {
+    uint32_t lo = max(floor, kept.key), hi = order_key(m);
+    uint64_t acc = 0, target = static_cast<uint64_t>(k);
+    for (bool first = true;; first = false) {
+      const int bits = 32 - __clz(hi - lo), shift = max(0, bits - 11);
+      uint64_t* h = s.hist[level++ & 1];
+      for (int i = threadIdx.x; i < kBins; i += kThreads) h[i] = 0;
+      __syncthreads();
+      sweep([&](int i, float x) {
+        const uint32_t q = order_key(x);
+        if (q < lo || q > hi || !kept.has(q, i)) return;
+        atomicAdd(reinterpret_cast<unsigned long long*>(h + ((q - lo) >> shift)),
+                  static_cast<unsigned long long>(MASS ? weight(x) : 1));
+      });
+      sync();
+      // bins from the highest down, four a thread
+      uint64_t n[kPerThread], sum = 0;
+#pragma unroll
+      for (int j = 0; j < kPerThread; ++j) {
+        const uint64_t* at = h + kBins - 1 - (threadIdx.x * kPerThread + j);
+        n[j] = 0;
+        for (int i = 0; i < C; ++i) n[j] += ld_cluster(at, i);
+        sum += n[j];
+      }
+      const uint64_t incl = warp_scan(sum, lane);
+      if (lane == 31) s.scan[warp] = incl;
+      if (threadIdx.x == 0) s.bin = -1;
+      __syncthreads();
+      uint64_t before = acc + incl - sum, total = 0;
+      for (int i = 0; i < kWarps; ++i) {
+        if (i < warp) before += s.scan[i];
+        total += s.scan[i];
+      }
+      if (first && MASS) target = sample_share(share, total);
+#pragma unroll
+      for (int j = 0; j < kPerThread; ++j) {
+        if (before < target && before + n[j] >= target) {
+          s.bin = kBins - 1 - (threadIdx.x * kPerThread + j);
+          s.before = before;
+          s.in = n[j];
+        }
+        before += n[j];
+      }
+      __syncthreads();
+      if (s.bin < 0) return;  // fewer than k are alive: all are kept
+      acc = s.before;
+      lo += static_cast<uint32_t>(s.bin) << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      if (shift == 0) break;
+    }
+    // equal logits: as many as it takes, by index
+    const uint64_t each = MASS ? weight(order_value(lo)) : 1;
+    const uint64_t take = (target - acc + each - 1) / each, have = s.in / each;
+    int last = kept.key == lo ? kept.index : INT_MAX;
+    if (take < have) {
+      uint64_t n = 0;
+      sweep([&](int i, float x) { n += order_key(x) == lo && i <= last; });
+      n = warp_sum(n);
+      if (lane == 0) s.count[warp] = n;
+      sync();
+      uint64_t before = 0;
+      int at = -1;  // the warp (of the cluster) that has the last one
+      for (int b = 0; at < 0 && b < C * kWarps; b += 32) {
+        const uint64_t v = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
+        const uint64_t incl = before + warp_scan(v, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, incl >= take);
+        if (hit != 0) at = b + __ffs(hit) - 1;
+        before = __shfl_sync(0xffffffffu, hit != 0 ? incl - v : incl, hit != 0 ? __ffs(hit) - 1 : 31);
+      }
+      if (at == rank * kWarps + warp) {
+        const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(order_key(x) == lo && i <= last); });
+        if (lane == 0) s.index = i;
+      }
+      sync();
+      last = ld_cluster(&s.index, at / kWarps);
+      // nobody writes s.index again before the next sync() of all
+    }
+    kept.key = lo;
+    kept.index = last;
+  }
+
+  // The index in this warp's run at which the sum of f first reaches `want` >= 1
+  template <typename F>
+  __device__ __forceinline__ int nth(uint64_t want, F f) const {
+    uint64_t before = 0;
+    for (int g = w0; g < w1; g += 32) {
+      float x[G::N];
+      uint64_t v[G::N], sum = 0;
+      if (g + lane < w1) {
+        G::get(fetch(g + lane), x);
+#pragma unroll
+        for (int j = 0; j < G::N; ++j) sum += v[j] = f((g + lane) * G::N + j - head, x[j]);
+      }
+      const uint64_t incl = before + warp_scan(sum, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, incl >= want);
+      if (hit != 0) {
+        const int l = __ffs(hit) - 1;
+        int i = -1;
+        if (lane == l) {
+          uint64_t at = incl - sum;
+#pragma unroll
+          for (int j = 0; j < G::N; ++j) {
+            at += v[j];
+            if (i < 0 && at >= want) i = (g + lane) * G::N + j - head;
+          }
+        }
+        return __shfl_sync(0xffffffffu, i, l);
+      }
+      before = __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return -1;
+  }
+};
+
+template <int TYPE, bool RESIDENT>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
+  using R = Row<TYPE, RESIDENT>;
+  using G = Group<TYPE>;
+  extern __shared__ __align__(16) uint8_t dyn[];
+  __shared__ Shared s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int C = p.ctas, rank = static_cast<int>(cluster_ctarank()), r = blockIdx.x / C;
+  if (tid < kWarps) mbar_init(&s.bar[tid], 1);
+  if (tid < kSampleTable) s.table[tid] = sample_entry(tid);
+  fence_mbar_init();
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  const uint8_t* row = static_cast<const uint8_t*>(p.logits) + static_cast<long long>(r) * p.stride * sizeof(typename G::T);
+  const uintptr_t base = reinterpret_cast<uintptr_t>(row) & ~static_cast<uintptr_t>(15);
+  const int head = static_cast<int>((reinterpret_cast<uintptr_t>(row) - base) / sizeof(typename G::T));
+  const int groups = static_cast<int>((static_cast<long long>(head) + p.vocab + G::N - 1) / G::N);
+  const int per = (groups + C - 1) / C, per_warp = (per + kWarps - 1) / kWarps;
+  const int g0 = min(groups, rank * per), g1 = min(groups, g0 + per);
+  const int w0 = min(g1, g0 + warp * per_warp), w1 = min(g1, w0 + per_warp);
+  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, w0, w1, head, r, lane, warp, rank, C};
+  R& x = row_;
+
+  int bad = 0;
+  if (RESIDENT && w0 < w1) {
+    const int f0 = x.whole(w0) ? w0 : w0 + 1, f1 = x.whole(w1 - 1) ? w1 : w1 - 1;
+    if (f0 < f1) {
+      const uint32_t bytes = static_cast<uint32_t>(f1 - f0) * 16u;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&s.bar[warp], bytes);
+        bulk_load(x.slice + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
+      }
+    }
+    if (lane == 0 && !x.whole(w0)) x.slice[w0 - g0] = x.edge(w0);
+    if (lane == 1 && w1 - 1 > w0 && !x.whole(w1 - 1)) x.slice[w1 - 1 - g0] = x.edge(w1 - 1);
+    if (f0 < f1 && !mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr)) {
+      bad = 2;
+      atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
+      mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr);  // the copy lands before this CTA ends
+    }
+    __syncwarp();
+  }
+
+  // the largest logit; NaN, infinity and rows of nothing are refused
+  float m = -INFINITY;
+  x.sweep([&](int, float v) {
+    m = fmaxf(m, v);
+    bad |= v != v;
+  });
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+  }
+  if (lane == 0) {
+    s.max[warp] = m;
+    s.bad[warp] = bad;
+  }
+  x.sync();
+  for (int i = lane; i < C * kWarps; i += 32) {
+    m = fmaxf(m, ld_cluster(&s.max[i % kWarps], i / kWarps));
+    bad |= ld_cluster(&s.bad[i % kWarps], i / kWarps);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+  }
+  const float T = p.temperature ? p.temperature[r] : 1.f, u = p.u[r];
+  const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
+  const int top_k = p.top_k ? p.top_k[r] : 0;
+  const bool finite = !bad && m > -INFINITY && m < INFINITY;
+  const bool valid = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p == top_p && min_p == min_p;
+  if (!finite || !valid) {
+    if (rank == 0 && tid == 0) {
+      atomicCAS(p.status, 0, finite ? EBD_ERR_INVALID_ARG : EBD_ERR_NONFINITE);
+      p.token[r] = -1;
+      p.prob[r] = __int_as_float(0x7FC00000);
+    }
+    x.sync();  // the others have read this CTA's shared memory
+    return;
+  }
+  x.m = m;
+  if (T == 0.f) {
+    int first = INT_MAX;
+    x.sweep([&](int i, float v) {
+      if (v == m) first = min(first, i);
+    });
+    first = __reduce_min_sync(0xffffffffu, first);
+    if (lane == 0) s.first[warp] = first;
+    x.sync();
+    if (rank == 0 && warp == 0) {
+      for (int i = lane; i < C * kWarps; i += 32) first = min(first, ld_cluster(&s.first[i % kWarps], i / kWarps));
+      first = __reduce_min_sync(0xffffffffu, first);
+      if (lane == 0) {
+        p.token[r] = first;
+        p.prob[r] = 1.f;
+      }
+    }
+    x.sync();
+    return;
+  }
+
+  x.c = sample_scale(T, p.shift);
+  // nothing that has weight lies below: 40 / log2(e) = 27.73, and room for rounding
+  const float low = m - 28.f * fminf(fmaxf(T, 1e-30f), 1e30f) - fabsf(m) * 9.5367431640625e-7f;
+  const uint32_t floor = order_key(low > -3.402823466e38f ? low : -3.402823466e38f);
+  Prefix kept{floor, INT_MAX};
+  if (top_k > 0 && top_k < p.vocab) x.template cut<false>(kept, floor, top_k, 0.f);
+  if (top_p < 1.f) x.template cut<true>(kept, floor, 0, top_p);
+  if (min_p > 0.f) {
+    const uint32_t q = order_key(sample_floor(m, T, min_p) + 0.f);
+    if (q > kept.key) kept = Prefix{q, INT_MAX};
+  }
+
+  // what every warp's run weighs, and where u points
+  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(order_key(v), i) ? x.weight(v) : 0; };
+  uint64_t sum = 0;
+  x.sweep([&](int i, float v) { sum += kept_weight(i, v); });
+  sum = warp_sum(sum);
+  if (lane == 0) s.part[warp] = sum;
+  x.sync();
+  uint64_t before = 0, total = 0;
+  for (int i = lane; i < C * kWarps; i += 32) {
+    const uint64_t v = ld_cluster(&s.part[i % kWarps], i / kWarps);
+    if (i < rank * kWarps + warp) before += v;
+    total += v;
+  }
+  before = warp_sum(before);
+  total = warp_sum(total);
+  const uint64_t at = sample_point(u, total);
+  if (before <= at && at < before + sum) {
+    const int i = x.nth(at - before + 1, kept_weight);
+    if (lane == 0) {
+      float v[G::N];
+      G::get(x.fetch((i + head) / G::N), v);
+      float l = 0.f;
+#pragma unroll
+      for (int j = 0; j < G::N; ++j)
+        if (j == (i + head) % G::N) l = v[j];
+      p.token[r] = i;
+      p.prob[r] = static_cast<float>(exp((static_cast<double>(l) - m) / static_cast<double>(fminf(fmaxf(T, 1e-30f), 1e30f))) /
+                                     ldexp(static_cast<double>(total), -p.shift));
+    }
+  }
+  x.sync();
+}
+
+using Kernel = void (*)(SampleParams);
+Kernel sample_kernel_of(int dtype, bool resident) {
+  switch (dtype) {
+    case EBD_LOGITS_F32: return resident ? sample_kernel<EBD_LOGITS_F32, true> : sample_kernel<EBD_LOGITS_F32, false>;
+    case EBD_LOGITS_BF16: return resident ? sample_kernel<EBD_LOGITS_BF16, true> : sample_kernel<EBD_LOGITS_BF16, false>;
+    default: return resident ? sample_kernel<EBD_LOGITS_F16, true> : sample_kernel<EBD_LOGITS_F16, false>;
+  }
+}
+
+}  // namespace
+
+cudaError_t sample_configure() {
+  for (int i = 0; i < 3; ++i) {
+    const cudaError_t e = cudaFuncSetAttribute(sample_kernel_of(i, true), cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
+  const long long size = p.dtype == EBD_LOGITS_F32 ? 4 : 2;
+  const long long bytes = p.vocab * size + 32;  // both ends rounded out
+  p.ctas = 1;
+  while (p.ctas < kMaxCtas && bytes / p.ctas > 32 * 1024) p.ctas *= 2;
+  const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
+  p.resident = slice <= kSliceBytes;
+  (void)num_sms;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * p.ctas, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = p.resident ? static_cast<size_t>(slice) : 0;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(p.ctas);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, sample_kernel_of(p.dtype, p.resident != 0), p);
+}
+
+}  // namespace ebd

@@ -33,6 +33,9 @@ struct LmParams {
   int* status;
   uint64_t limit_ns;
   int force_timeout;
+  float* logits;            // where the logits go too (the STORE kernels), rows logits_stride
+  long long logits_stride;  // floats apart
+  int stats;                // 0: the logits alone, no partial states
   int pdl;                  // a programmatic dependent of the kernel before it, which
                             // copies the hidden rows in: W loads start before the wait
 };

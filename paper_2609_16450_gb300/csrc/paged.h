@@ -26,6 +26,23 @@ struct PagedRowsParams {
   long long kv_stride;         // elements from row to row
   const uint8_t* skip;         // [R] or null
 };
+// ------------------------------------------------------------------ plans (k_plan.cu)
+struct PagedPlanParams {
+  int B, R;
+  int page_log2, n_pages, max_pages;
+  const int* add;              // [B]
+  int* kv_len;                 // [B]
+  int* page_table;             // [B][max_pages]
+  int* free_pages;             // [n_pages], the first *n_free of them free
+  int* n_free;
+  int* cu_rows;                // [B + 1], [R], [R]: may be null
+  int* row_pos;
+  int64_t* slot;
+  int* status;
+};
+cudaError_t paged_plan_configure();
+cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t st);
+
 // Every kernel of the paged cache is a programmatic dependent of the one before
 // it on the stream: it reads global memory only after griddepcontrol.wait, and
 // lets the next one's blocks in as soon as it has read its plan.  A kernel before
