@@ -13,9 +13,15 @@
 //
 // A row is one cluster of CTAs; each warp owns a contiguous run of the row's
 // 16-byte groups, so that sums by warp are sums by index.  A CTA's slice of the row
-// comes into its shared memory once.  The last logit of a prefix is found by
-// histograms of 2048 bins over the logits' ordered bits, of counts (top-k) or of
-// weights (top-p), each level over the bin that the last one chose.
+// comes into its shared memory once.
+//
+// The last logit of a prefix is found without sorting.  One sweep counts logits in
+// bins of equal width of y = (m - l) log2(e) / T.  They give the bin that top-k's
+// k-th lies in, and, as a bin's weights differ by a factor of 2^(1/51) at most,
+// bounds on the sums and so the few bins that top-p's border lies in.  One sweep sums
+// weights: above those bins, below them, and within them by the logits' ordered bits.
+// The bin that the border then lies in is taken apart the same way, until all of it
+// is wanted or its logits are equal, of which the first by index are taken.
 #include <cuda_fp16.h>
 
 #include <climits>
@@ -30,7 +36,9 @@ namespace ebd {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 2048, kPerThread = kBins / kThreads;
+constexpr int kBins = 2048;               // of y, counts
+constexpr float kBinScale = 51.15f;       // of them per unit of y: 40 * 51.15 = 2046
+constexpr int kFine = 1024, kFineBits = 10;  // of ordered bits, weights and counts
 constexpr int kMaxCtas = 8;
 constexpr int kSliceBytes = 76 * 1024;  // of a row in shared memory
 
@@ -42,6 +50,14 @@ __device__ __forceinline__ uint64_t ld_cluster(const uint64_t* p, uint32_t rank)
 __device__ __forceinline__ int ld_cluster(const int* p, uint32_t rank) {
   int v;
   asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 ld_cluster(const uint4* p, uint32_t rank) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(mapa_shared(smem_u32(p), rank))
+               : "memory");
   return v;
 }
 __device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
@@ -111,18 +127,33 @@ __device__ __forceinline__ uint64_t warp_scan(uint64_t x, int lane) {
   return x;
 }
 
+// Histograms of one level, in turn: every CTA's is read by the whole cluster, which
+// is done with it when the next level's are.
+struct alignas(16) Hist {
+  union {
+    uint32_t coarse[kBins];
+    struct {
+      uint64_t weight[kFine];
+      uint32_t count[kFine];
+    };
+  };
+};
+
 struct Shared {
-  uint64_t hist[2][kBins];
+  Hist hist[2];
   SampleEntry table[kSampleTable];
-  uint64_t part[kWarps];     // a warp's sum
-  uint64_t count[kWarps];    // a warp's elements at the border
+  uint64_t part[kWarps];     // a warp's sums: of what is kept for sure,
+  uint64_t rest[kWarps];     // of what is not;
+  uint64_t count[kWarps];    // its elements at the border
   uint64_t scan[kWarps];
+  float scan_f[kWarps];
   uint64_t bar[kWarps];
-  uint64_t before, in, total;
+  uint64_t before, in;
   float max[kWarps];
   int bad[kWarps];
   int first[kWarps];
-  int bin, index;
+  int bin, k_bin, k_whole, k_before, p_first, p_last, alone, index;
+  uint32_t bound[4];
 };
 
 // Which elements of the row are kept: those above `key`, and those at it up to `index`
@@ -179,88 +210,214 @@ struct Row {
   }
   __device__ __forceinline__ uint64_t weight(float x) const { return sample_weight(m, x, c, s.table); }
 
-  // Takes the prefix `kept` down to the elements that bring count or weight (MASS) up
-  // to a target: at least k elements, or the share `share` of its weight.
+  // Bin of a logit, by descending logits, and past the last for weights of zero
+  __device__ __forceinline__ int bin_of(float x) const {
+    const float y = sample_depth(m, x, c);
+    return y <= kSampleDead ? static_cast<int>(__float_as_uint(fmaf(y, kBinScale, 8388608.f)) & 0x7FFFFFu) : kBins;
+  }
+  // Least ordered bits with a bin of at most b (one warp)
+  __device__ __forceinline__ uint32_t bound(int b, uint32_t lo, uint32_t hi) const {
+    while (lo < hi) {
+      const uint32_t step = (hi - lo) / 32 + 1;
+      const uint32_t q = hi - lo >= lane * step ? lo + lane * step : hi;
+      const unsigned hit = __ballot_sync(0xffffffffu, bin_of(order_value(q)) <= b);
+      const int f = hit != 0 ? __ffs(hit) - 1 : 32;
+      const uint32_t below = __shfl_sync(0xffffffffu, q, f > 0 ? f - 1 : 0);
+      if (f < 32) hi = __shfl_sync(0xffffffffu, q, f);
+      if (f > 0) lo = min(hi, below + 1);
+      else hi = lo;
+    }
+    return lo;
+  }
+  // sum over this and the threads before it, and over all
+  template <typename T>
+  __device__ __forceinline__ T block_scan(T x, T* part, T& total) const {
+    T incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const T y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    __syncthreads();
+    if (lane == 31) part[warp] = incl;
+    __syncthreads();
+    T before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      const T y = part[i];
+      if (i < warp) before += y;
+      total += y;
+    }
+    return before + incl;
+  }
+  // sum over the cluster's warps
+  __device__ __forceinline__ uint64_t cluster_sum(const uint64_t* of) const {
+    uint64_t v = 0;
+    for (int i = lane; i < C * kWarps; i += 32) v += ld_cluster(of + i % kWarps, i / kWarps);
+    return warp_sum(v);
+  }
+
+  // Counts the row's logits by bin; finds top-k's bin (s.k_bin: kBins if all that have
+  // weight are wanted) with the number before it, and the bins s.p_first to s.p_last
+  // that top-p's border lies in.
+  __device__ __forceinline__ void count(int k, float share) {
+    Hist& h = s.hist[level++ & 1];
+    sweep([&](int, float x) {
+      const int b = bin_of(x);
+      if (b < kBins) atomicAdd(&h.coarse[b], 1u);
+    });
+    sync();
+    constexpr int N = kBins / kThreads;
+    static_assert(N == 4, "a thread's bins are one vector");
+    uint32_t n[N] = {0, 0, 0, 0};
+    for (int i = 0; i < C; ++i) {
+      const uint4 v = ld_cluster(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x, i);
+      n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w;
+    }
+    if (threadIdx.x == 0) s.k_bin = kBins, s.k_whole = 0, s.p_first = s.p_last = kBins - 1;
+    uint32_t all;
+    const uint32_t sum = n[0] + n[1] + n[2] + n[3];
+    uint32_t before = block_scan(sum, reinterpret_cast<uint32_t*>(s.scan), all) - sum;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint32_t want = k > 0 ? static_cast<uint32_t>(k) : all;
+      if (before < want && before + n[j] >= want && k > 0) {
+        s.k_bin = threadIdx.x * N + j;
+        s.k_before = static_cast<int>(before);
+        s.k_whole = before + n[j] == want;
+      }
+      const uint32_t left = want > before ? want - before : 0;
+      before += n[j];
+      n[j] = min(n[j], left);  // what top-k leaves
+    }
+    if (share < 1.f) {
+      // A bin's weights are between lo times and once its first's; 10^-4 is far more
+      // than all roundings here.
+      const float lo = exp2f(-1.f / kBinScale) * (1.f - 1e-4f);
+      float w[N], mass = 0.f, total;
+#pragma unroll
+      for (int j = 0; j < N; ++j) mass += w[j] = static_cast<float>(n[j]) * exp2f((0.5f - (threadIdx.x * N + j)) / kBinScale);
+      float to = block_scan(mass, s.scan_f, total) - mass;
+      const float least = share * total * lo * (1.f - 1e-4f), most = fminf(fmaxf(share * total * (1.f + 1e-4f), 1e-30f), total * lo * (1.f - 1e-4f));
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float next = to + w[j];
+        if ((to < least || threadIdx.x * N + j == 0) && next >= least) s.p_first = threadIdx.x * N + j;
+        if (to * lo < most && next * lo >= most) s.p_last = threadIdx.x * N + j;
+        to = next;
+      }
+    }
+    __syncthreads();
+  }
+
+  // Clears the next level's histograms
+  __device__ __forceinline__ void clear() {
+    uint4* h = reinterpret_cast<uint4*>(&s.hist[level & 1]);
+    for (int i = threadIdx.x; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads) h[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+  }
+  __device__ static int shift_of(uint32_t lo, uint32_t hi) { return max(0, 32 - __clz(hi - lo) - kFineBits); }
+
+  // Takes `kept` down to the elements with ordered bits above hi and, of those within
+  // [lo, hi], as many as bring their count or weight (MASS) up to `target`; with
+  // `counted` the level's histograms are there.
   template <bool MASS>
-  __device__ __forceinline__ void cut(Prefix& kept, uint32_t floor, int k, float share) {
-    uint32_t lo = max(floor, kept.key), hi = order_key(m);
-    uint64_t acc = 0, target = static_cast<uint64_t>(k);
-    for (bool first = true;; first = false) {
-      const int bits = 32 - __clz(hi - lo), shift = max(0, bits - 11);
-      uint64_t* h = s.hist[level++ & 1];
-      for (int i = threadIdx.x; i < kBins; i += kThreads) h[i] = 0;
-      __syncthreads();
-      sweep([&](int i, float x) {
-        const uint32_t q = order_key(x);
-        if (q < lo || q > hi || !kept.has(q, i)) return;
-        atomicAdd(reinterpret_cast<unsigned long long*>(h + ((q - lo) >> shift)),
-                  static_cast<unsigned long long>(MASS ? weight(x) : 1));
-      });
-      sync();
-      // bins from the highest down, four a thread
-      uint64_t n[kPerThread], sum = 0;
-#pragma unroll
-      for (int j = 0; j < kPerThread; ++j) {
-        const uint64_t* at = h + kBins - 1 - (threadIdx.x * kPerThread + j);
-        n[j] = 0;
-        for (int i = 0; i < C; ++i) n[j] += ld_cluster(at, i);
-        sum += n[j];
+  __device__ __forceinline__ void refine(Prefix& kept, uint32_t lo, uint32_t hi, uint64_t target, bool counted) {
+    for (;; counted = false) {
+      const int shift = shift_of(lo, hi);
+      Hist& h = s.hist[level & 1];
+      if (!counted) {
+        clear();
+        sweep([&](int i, float x) {
+          const uint32_t q = order_key(x);
+          if (q >= lo && q <= hi && kept.has(q, i)) add<MASS>(h, (hi - q) >> shift, x);
+        });
+        sync();
       }
-      const uint64_t incl = warp_scan(sum, lane);
-      if (lane == 31) s.scan[warp] = incl;
+      ++level;
+      constexpr int N = kFine / kThreads;
+      static_assert(N == 2, "a thread's bins are one vector");
+      uint64_t n[N] = {0, 0};
+      uint32_t one[N] = {0, 0};
+      for (int i = 0; i < C; ++i) {
+        const int2 v = ld_pair(h.count + threadIdx.x * N, i);
+        one[0] += v.x, one[1] += v.y;
+        if (MASS) {
+          const uint4 w = ld_cluster(reinterpret_cast<const uint4*>(h.weight) + threadIdx.x, i);
+          n[0] += w.x | static_cast<uint64_t>(w.y) << 32;
+          n[1] += w.z | static_cast<uint64_t>(w.w) << 32;
+        }
+      }
+      if (!MASS) n[0] = one[0], n[1] = one[1];
       if (threadIdx.x == 0) s.bin = -1;
-      __syncthreads();
-      uint64_t before = acc + incl - sum, total = 0;
-      for (int i = 0; i < kWarps; ++i) {
-        if (i < warp) before += s.scan[i];
-        total += s.scan[i];
-      }
-      if (first && MASS) target = sample_share(share, total);
+      uint64_t all;
+      uint64_t before = block_scan(n[0] + n[1], s.scan, all) - n[0] - n[1];
 #pragma unroll
-      for (int j = 0; j < kPerThread; ++j) {
+      for (int j = 0; j < N; ++j) {
         if (before < target && before + n[j] >= target) {
-          s.bin = kBins - 1 - (threadIdx.x * kPerThread + j);
+          s.bin = threadIdx.x * N + j;
           s.before = before;
           s.in = n[j];
+          s.alone = MASS ? one[j] == 1 : before + n[j] == target;
         }
         before += n[j];
       }
       __syncthreads();
-      if (s.bin < 0) return;  // fewer than k are alive: all are kept
-      acc = s.before;
-      lo += static_cast<uint32_t>(s.bin) << shift;
-      hi = min(hi, lo + ((1u << shift) - 1));
-      if (shift == 0) break;
-    }
-    // equal logits: as many as it takes, by index
-    const uint64_t each = MASS ? weight(order_value(lo)) : 1;
-    const uint64_t take = (target - acc + each - 1) / each, have = s.in / each;
-    int last = kept.key == lo ? kept.index : INT_MAX;
-    if (take < have) {
-      uint64_t n = 0;
-      sweep([&](int i, float x) { n += order_key(x) == lo && i <= last; });
-      n = warp_sum(n);
-      if (lane == 0) s.count[warp] = n;
-      sync();
-      uint64_t before = 0;
-      int at = -1;  // the warp (of the cluster) that has the last one
-      for (int b = 0; at < 0 && b < C * kWarps; b += 32) {
-        const uint64_t v = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
-        const uint64_t incl = before + warp_scan(v, lane);
-        const unsigned hit = __ballot_sync(0xffffffffu, incl >= take);
-        if (hit != 0) at = b + __ffs(hit) - 1;
-        before = __shfl_sync(0xffffffffu, hit != 0 ? incl - v : incl, hit != 0 ? __ffs(hit) - 1 : 31);
+      if (s.bin < 0) return;  // less than target in all
+      target -= s.before;
+      hi -= static_cast<uint32_t>(s.bin) << shift;
+      lo = hi - lo >= 1u << shift ? hi - ((1u << shift) - 1) : lo;
+      const bool whole = s.alone != 0;
+      if (whole || shift == 0) {
+        const int last = lo == kept.key ? kept.index : INT_MAX;
+        kept = Prefix{lo, whole ? last : first_by_index<MASS>(lo, last, target)};
+        return;
       }
-      if (at == rank * kWarps + warp) {
-        const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(order_key(x) == lo && i <= last); });
-        if (lane == 0) s.index = i;
-      }
-      sync();
-      last = ld_cluster(&s.index, at / kWarps);
-      // nobody writes s.index again before the next sync() of all
     }
-    kept.key = lo;
-    kept.index = last;
+  }
+  template <bool MASS>
+  __device__ __forceinline__ void add(Hist& h, uint32_t b, float x) const {
+    atomicAdd(&h.count[b], 1u);
+    if (MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&h.weight[b]), static_cast<unsigned long long>(weight(x)));
+  }
+  __device__ __forceinline__ int2 ld_pair(const uint32_t* p, uint32_t rank) const {
+    int2 v;
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];"
+                 : "=r"(v.x), "=r"(v.y)
+                 : "r"(mapa_shared(smem_u32(p), rank))
+                 : "memory");
+    return v;
+  }
+
+  // Of the logits equal to order_value(key), up to index `last`: the index of the one
+  // that brings their count or weight up to `target`; s.in is that of all.
+  template <bool MASS>
+  __device__ __forceinline__ int first_by_index(uint32_t key, int last, uint64_t target) {
+    const uint64_t each = MASS ? weight(order_value(key)) : 1;
+    const uint64_t take = (target + each - 1) / each, have = s.in / each;
+    if (take >= have) return last;
+    uint64_t n = 0;
+    sweep([&](int i, float x) { n += order_key(x) == key && i <= last; });
+    n = warp_sum(n);
+    if (lane == 0) s.count[warp] = n;
+    sync();
+    uint64_t before = 0;
+    int at = -1;  // the warp (of the cluster) that has the last one
+    for (int b = 0; at < 0 && b < C * kWarps; b += 32) {
+      const uint64_t v = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
+      const uint64_t incl = before + warp_scan(v, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, incl >= take);
+      if (hit != 0) at = b + __ffs(hit) - 1;
+      before = __shfl_sync(0xffffffffu, hit != 0 ? incl - v : incl, hit != 0 ? __ffs(hit) - 1 : 31);
+    }
+    if (at == rank * kWarps + warp) {
+      const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(order_key(x) == key && i <= last); });
+      if (lane == 0) s.index = i;
+    }
+    sync();
+    // nobody writes s.index again before the next sync() of all
+    return ld_cluster(&s.index, at / kWarps);
   }
 
   // The index in this warp's run at which the sum of f first reaches `want` >= 1
@@ -306,10 +463,16 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int C = p.ctas, rank = static_cast<int>(cluster_ctarank()), r = blockIdx.x / C;
   if (tid < kWarps) mbar_init(&s.bar[tid], 1);
   if (tid < kSampleTable) s.table[tid] = sample_entry(tid);
+  for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
+    reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
   fence_mbar_init();
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  const float T = p.temperature ? p.temperature[r] : 1.f, u = p.u[r];
+  const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
+  const int top_k = p.top_k ? p.top_k[r] : 0;
 
   const uint8_t* row = static_cast<const uint8_t*>(p.logits) + static_cast<long long>(r) * p.stride * sizeof(typename G::T);
   const uintptr_t base = reinterpret_cast<uintptr_t>(row) & ~static_cast<uintptr_t>(15);
@@ -366,9 +529,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     bad |= __shfl_xor_sync(0xffffffffu, bad, o);
   }
-  const float T = p.temperature ? p.temperature[r] : 1.f, u = p.u[r];
-  const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
-  const int top_k = p.top_k ? p.top_k[r] : 0;
   const bool finite = !bad && m > -INFINITY && m < INFINITY;
   const bool valid = T >= 0.f && T < INFINITY && u >= 0.f && u < 1.f && top_p == top_p && min_p == min_p;
   if (!finite || !valid) {
@@ -405,29 +565,89 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   // nothing that has weight lies below: 40 / log2(e) = 27.73, and room for rounding
   const float low = m - 28.f * fminf(fmaxf(T, 1e-30f), 1e30f) - fabsf(m) * 9.5367431640625e-7f;
   const uint32_t floor = order_key(low > -3.402823466e38f ? low : -3.402823466e38f);
+  const uint32_t top = order_key(m);
+  const bool by_k = top_k > 0 && top_k < p.vocab;
+  const uint32_t q_min = min_p > 0.f ? order_key(sample_floor(m, T, min_p) + 0.f) : 0;
+  bool by_p = top_p < 1.f;
   Prefix kept{floor, INT_MAX};
-  if (top_k > 0 && top_k < p.vocab) x.template cut<false>(kept, floor, top_k, 0.f);
-  if (top_p < 1.f) x.template cut<true>(kept, floor, 0, top_p);
-  if (min_p > 0.f) {
-    const uint32_t q = order_key(sample_floor(m, T, min_p) + 0.f);
-    if (q > kept.key) kept = Prefix{q, INT_MAX};
+  uint64_t sum = 0;
+  if (by_k || by_p) {
+    x.count(by_k ? top_k : 0, top_p);
+    const bool cut_k = by_k && s.k_bin < kBins;
+    // where top-k's bin and top-p's bins begin and end, a bound a warp
+    if (warp < 4) {
+      const int b = warp == 0 ? s.k_bin : warp == 1 ? s.k_bin - 1 : warp == 2 ? s.p_last : s.p_first - 1;
+      const uint32_t q = b >= kBins ? floor : b < 0 ? top + 1 : x.bound(b, floor, top);
+      if (lane == 0) s.bound[warp] = q;
+    }
+    __syncthreads();
+    const uint32_t k_lo = s.bound[0], k_hi = s.bound[1] - 1, p_lo = s.bound[2], p_hi = s.bound[3] - 1;
+    if (cut_k) {
+      if (s.k_whole)
+        kept.key = k_lo;
+      else
+        x.template refine<false>(kept, k_lo, k_hi, static_cast<uint64_t>(top_k - s.k_before), false);
+    }
+    by_p = by_p && q_min <= p_hi;  // else min-p keeps less, whatever top-p does
+    if (by_p) {
+      const uint32_t lo = max(p_lo, kept.key), hi = p_hi;
+      const int shift = x.shift_of(lo, hi);
+      uint64_t below = 0;
+      x.clear();
+      Hist& h = s.hist[x.level & 1];
+      x.sweep([&](int i, float v) {
+        const uint32_t q = order_key(v);
+        if (!kept.has(q, i)) return;
+        if (q >= lo && q <= hi) {
+          x.template add<true>(h, (hi - q) >> shift, v);
+        } else {
+          const uint64_t w = x.weight(v);
+          if (q > hi)
+            sum += w;
+          else
+            below += w;
+        }
+      });
+      const uint64_t above = warp_sum(sum), all = warp_sum(below + sum);
+      if (lane == 0) s.part[warp] = above, s.rest[warp] = all;
+      x.sync();
+      uint64_t within = 0;
+      // every CTA's bins, for the sum that the share is taken of
+      for (int i = 0; i < C; ++i) {
+        const uint4 w = ld_cluster(reinterpret_cast<const uint4*>(h.weight) + tid, i);
+        within += (w.x | static_cast<uint64_t>(w.y) << 32) + (w.z | static_cast<uint64_t>(w.w) << 32);
+      }
+      uint64_t total;
+      x.block_scan(within, s.scan, total);
+      const uint64_t share = sample_share(top_p, total + x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
+      x.template refine<true>(kept, lo, hi, share > over ? share - over : 1, true);
+      if (q_min > kept.key) kept = Prefix{q_min, INT_MAX};
+      x.sweep([&](int i, float v) {
+        const uint32_t q = order_key(v);
+        if (q >= lo && q <= hi && kept.has(q, i)) sum += x.weight(v);
+      });
+    }
+  }
+  if (!by_p) {
+    if (q_min > kept.key) kept = Prefix{q_min, INT_MAX};
+    x.sweep([&](int i, float v) {
+      if (kept.has(order_key(v), i)) sum += x.weight(v);
+    });
   }
 
   // what every warp's run weighs, and where u points
-  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(order_key(v), i) ? x.weight(v) : 0; };
-  uint64_t sum = 0;
-  x.sweep([&](int i, float v) { sum += kept_weight(i, v); });
   sum = warp_sum(sum);
-  if (lane == 0) s.part[warp] = sum;
+  if (lane == 0) s.count[warp] = sum;
   x.sync();
   uint64_t before = 0, total = 0;
   for (int i = lane; i < C * kWarps; i += 32) {
-    const uint64_t v = ld_cluster(&s.part[i % kWarps], i / kWarps);
+    const uint64_t v = ld_cluster(&s.count[i % kWarps], i / kWarps);
     if (i < rank * kWarps + warp) before += v;
     total += v;
   }
   before = warp_sum(before);
   total = warp_sum(total);
+  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(order_key(v), i) ? x.weight(v) : 0; };
   const uint64_t at = sample_point(u, total);
   if (before <= at && at < before + sum) {
     const int i = x.nth(at - before + 1, kept_weight);
