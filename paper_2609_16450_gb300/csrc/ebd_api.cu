@@ -16,7 +16,6 @@
 #include "paged.h"
 #include "rows_image.h"
 #include "sample.h"
-#include "sample_math.h"
 
 namespace {
 // An NVTX range around the host side of an entry point (visible in Nsight

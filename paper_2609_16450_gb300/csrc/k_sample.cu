@@ -42,14 +42,16 @@ constexpr int kFine = 1024, kFineBits = 10;  // of ordered bits, weights and cou
 constexpr int kMaxCtas = 8;
 constexpr int kSliceBytes = 76 * 1024;  // of a row in shared memory
 
+// Loads from a CTA of the cluster; volatile, so none moves across a barrier, and
+// several are in flight.
 __device__ __forceinline__ uint64_t ld_cluster(const uint64_t* p, uint32_t rank) {
   uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(smem_u32(p), rank)));
   return v;
 }
 __device__ __forceinline__ int ld_cluster(const int* p, uint32_t rank) {
   int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(mapa_shared(smem_u32(p), rank)));
   return v;
 }
 __device__ __forceinline__ uint4 ld_cluster(const uint4* p, uint32_t rank) {
@@ -57,7 +59,12 @@ __device__ __forceinline__ uint4 ld_cluster(const uint4* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                : "r"(mapa_shared(smem_u32(p), rank))
-               : "memory");
+              );
+  return v;
+}
+__device__ __forceinline__ uint2 ld_cluster(const uint2* p, uint32_t rank) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(mapa_shared(smem_u32(p), rank)));
   return v;
 }
 __device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
@@ -69,7 +76,7 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                : "memory");
 }
 
-// The logits of a 16-byte group.  -0 counts as 0.
+// The logits of a 16-byte group.
 template <int TYPE>
 struct Group;
 template <>
@@ -78,8 +85,8 @@ struct Group<EBD_LOGITS_F32> {
   using T = float;
   __device__ static T masked() { return -INFINITY; }
   __device__ static void get(const uint4& v, float (&x)[4]) {
-    x[0] = __uint_as_float(v.x) + 0.f, x[1] = __uint_as_float(v.y) + 0.f;
-    x[2] = __uint_as_float(v.z) + 0.f, x[3] = __uint_as_float(v.w) + 0.f;
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
   }
 };
 template <>
@@ -91,8 +98,8 @@ struct Group<EBD_LOGITS_BF16> {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16) + 0.f;
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u) + 0.f;
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
     }
   }
 };
@@ -106,8 +113,8 @@ struct Group<EBD_LOGITS_F16> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      x[2 * i] = f.x + 0.f;
-      x[2 * i + 1] = f.y + 0.f;
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
     }
   }
 };
@@ -141,7 +148,7 @@ struct alignas(16) Hist {
 
 struct Shared {
   Hist hist[2];
-  SampleEntry table[kSampleTable];
+  uint32_t table[kSampleTable];
   uint64_t part[kWarps];     // a warp's sums: of what is kept for sure,
   uint64_t rest[kWarps];     // of what is not;
   uint64_t count[kWarps];    // its elements at the border
@@ -154,14 +161,47 @@ struct Shared {
   int first[kWarps];
   int bin, k_bin, k_whole, k_before, p_first, p_last, alone, index;
   uint32_t bound[4];
+  SampleScale scale;
+  float floor_hi, floor_lo;  // T ln min_p
 };
 
-// Which elements of the row are kept: those above `key`, and those at it up to `index`
+// Which elements of the row are kept: those above `value`, and those equal to it up
+// to `index`.
 struct Prefix {
-  uint32_t key;
+  float value;
   int index;
-  __device__ __forceinline__ bool has(uint32_t k, int i) const { return k > key || (k == key && i <= index); }
+  __device__ __forceinline__ bool has(float x, int i) const { return x > value || (x == value && i <= index); }
 };
+
+// Two floats that are worked on at once
+struct Pair {
+  uint64_t v;
+  __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Pair(float a) : Pair(a, a) {}
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ Pair operator+(Pair a, const Pair& b) {
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ Pair operator*(Pair a, const Pair& b) {
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ Pair fma(Pair a, const Pair& b, const Pair& c) {
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return a;
+}
+__device__ __forceinline__ Pair operator-(Pair a, const Pair& b) { return fma(b, Pair(-1.f), a); }  // exact product
+// shifts by any amount: 0 from 32 on
+__device__ __forceinline__ uint32_t shl(uint32_t x, uint32_t n) {
+  asm("shl.b32 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(n));
+  return x;
+}
+__device__ __forceinline__ uint32_t shr(uint32_t x, uint32_t n) {
+  asm("shr.u32 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(n));
+  return x;
+}
 
 template <int TYPE, bool RESIDENT>
 struct Row {
@@ -198,17 +238,72 @@ struct Row {
     if (RESIDENT) return slice[g - g0];
     return whole(g) ? __ldg(reinterpret_cast<const uint4*>(data) + g) : edge(g);
   }
-  // f(index, logit) for every logit of the warp's groups
+  // f(index of the first, four logits) for the logits of the warp's groups
   template <typename F>
-  __device__ __forceinline__ void sweep(F f) const {
+  __device__ __forceinline__ void sweep4(F f) const {
     for (int g = w0 + lane; g < w1; g += 32) {
       float x[G::N];
       G::get(fetch(g), x);
 #pragma unroll
-      for (int j = 0; j < G::N; ++j) f(g * G::N + j - head, x[j]);
+      for (int j = 0; j < G::N; j += 4) {
+        const float y[4] = {x[j], x[j + 1], x[j + 2], x[j + 3]};
+        f(g * G::N + j - head, y);
+      }
     }
   }
+  // f(index, logit)
+  template <typename F>
+  __device__ __forceinline__ void sweep(F f) const {
+    sweep4([&](int i, const float(&x)[4]) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(i + j, x[j]);
+    });
+  }
   __device__ __forceinline__ uint64_t weight(float x) const { return sample_weight(m, x, c, s.table); }
+  // The weights of those of four logits that `keep` takes, 0 for the others: the
+  // operations of sample_weight, two logits at a time, without branches.  What is
+  // not kept has y = 64, and is shifted out.  -> whether any has weight
+  template <typename Keep>
+  __device__ __forceinline__ bool weights(const float (&x)[4], uint64_t (&w)[4], Keep keep) const {
+    const Pair mm(m), hi(c.hi);
+    const Pair l[2] = {Pair(x[0], x[1]), Pair(x[2], x[3])};
+    Pair s2[2] = {mm - l[0], mm - l[1]};
+    float p[4];
+    bool any = false;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) (s2[h] * hi).get(p[2 * h], p[2 * h + 1]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool k = p[j] <= kSampleDead && keep(j);
+      any |= k;
+      p[j] = k ? p[j] : 64.f;
+    }
+    if (!any) return false;
+    const Pair lo(c.lo), magic(kSampleMagic);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Pair pp(p[2 * h], p[2 * h + 1]);
+      const Pair b = s2[h] - mm, d = (mm - (s2[h] - b)) - (l[h] + b);
+      const Pair e = fma(d, hi, fma(s2[h], lo, fma(s2[h], hi, Pair(-p[2 * h], -p[2 * h + 1]))));
+      const Pair t = fma(pp, Pair(128.f), magic);
+      const Pair g = fma(t - magic, Pair(-0.0078125f), pp) + e;
+      const Pair y = g * fma(g, fma(g, Pair(kSampleC3), Pair(kSampleC2)), Pair(kSampleC1));
+      float tt[2];
+      t.get(tt[0], tt[1]);
+      uint32_t q[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) q[j] = s.table[__float_as_uint(tt[j]) & (kSampleTable - 1)];
+      float v[2];
+      fma(Pair(sample_entry_float(q[0]), sample_entry_float(q[1])), y, magic).get(v[0], v[1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t f = q[j] + __float_as_uint(v[j]) - kSampleMagicBits;
+        const uint32_t r = (__float_as_uint(tt[j]) >> 7) - (kSampleMagicBits >> 7) + 62 - c.shift;
+        w[2 * h + j] = static_cast<uint64_t>(shr(f, r)) << 32 | (shl(f, 32 - r) | shr(f, r - 32));
+      }
+    }
+    return true;
+  }
 
   // Bin of a logit, by descending logits, and past the last for weights of zero
   __device__ __forceinline__ int bin_of(float x) const {
@@ -251,10 +346,25 @@ struct Row {
     }
     return before + incl;
   }
+  // f of what every CTA of the cluster has at p, all loads in flight at once
+  template <typename T, typename F>
+  __device__ __forceinline__ void gather(const T* p, F f) const {
+    T v[kMaxCtas];
+#pragma unroll
+    for (int i = 0; i < kMaxCtas; ++i)
+      if (i < C) v[i] = ld_cluster(p, i);
+#pragma unroll
+    for (int i = 0; i < kMaxCtas; ++i)
+      if (i < C) f(v[i]);
+  }
   // sum over the cluster's warps
   __device__ __forceinline__ uint64_t cluster_sum(const uint64_t* of) const {
     uint64_t v = 0;
-    for (int i = lane; i < C * kWarps; i += 32) v += ld_cluster(of + i % kWarps, i / kWarps);
+#pragma unroll
+    for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
+      const int i = j * 32 + lane;
+      if (i < C * kWarps) v += ld_cluster(of + i % kWarps, i / kWarps);
+    }
     return warp_sum(v);
   }
 
@@ -271,10 +381,8 @@ struct Row {
     constexpr int N = kBins / kThreads;
     static_assert(N == 4, "a thread's bins are one vector");
     uint32_t n[N] = {0, 0, 0, 0};
-    for (int i = 0; i < C; ++i) {
-      const uint4 v = ld_cluster(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x, i);
-      n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w;
-    }
+    gather(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x,
+           [&](const uint4& v) { n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w; });
     if (threadIdx.x == 0) s.k_bin = kBins, s.k_whole = 0, s.p_first = s.p_last = kBins - 1;
     uint32_t all;
     const uint32_t sum = n[0] + n[1] + n[2] + n[3];
@@ -317,6 +425,10 @@ struct Row {
     for (int i = threadIdx.x; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads) h[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
   }
+  __device__ static uint32_t key(float x) { return order_key(x + 0.f); }  // -0 counts as 0
+  // The largest float with ordered bits up to hi: those of -0, which no logit has
+  // (key), stand for what is below 0
+  __device__ static float up_to(uint32_t hi) { return order_value(hi == 0x7FFFFFFFu ? hi - 1 : hi); }
   __device__ static int shift_of(uint32_t lo, uint32_t hi) { return max(0, 32 - __clz(hi - lo) - kFineBits); }
 
   // Takes `kept` down to the elements with ordered bits above hi and, of those within
@@ -329,9 +441,9 @@ struct Row {
       Hist& h = s.hist[level & 1];
       if (!counted) {
         clear();
+        const float f_lo = order_value(lo), f_hi = up_to(hi);
         sweep([&](int i, float x) {
-          const uint32_t q = order_key(x);
-          if (q >= lo && q <= hi && kept.has(q, i)) add<MASS>(h, (hi - q) >> shift, x);
+          if (x >= f_lo && x <= f_hi && kept.has(x, i)) add<MASS>(h, (hi - key(x)) >> shift, MASS ? weight(x) : 0);
         });
         sync();
       }
@@ -340,15 +452,12 @@ struct Row {
       static_assert(N == 2, "a thread's bins are one vector");
       uint64_t n[N] = {0, 0};
       uint32_t one[N] = {0, 0};
-      for (int i = 0; i < C; ++i) {
-        const int2 v = ld_pair(h.count + threadIdx.x * N, i);
-        one[0] += v.x, one[1] += v.y;
-        if (MASS) {
-          const uint4 w = ld_cluster(reinterpret_cast<const uint4*>(h.weight) + threadIdx.x, i);
-          n[0] += w.x | static_cast<uint64_t>(w.y) << 32;
-          n[1] += w.z | static_cast<uint64_t>(w.w) << 32;
-        }
-      }
+      gather(reinterpret_cast<const uint2*>(h.count) + threadIdx.x, [&](const uint2& v) { one[0] += v.x, one[1] += v.y; });
+      if (MASS)
+        gather(reinterpret_cast<const uint4*>(h.weight) + threadIdx.x, [&](const uint4& v) {
+          n[0] += v.x | static_cast<uint64_t>(v.y) << 32;
+          n[1] += v.z | static_cast<uint64_t>(v.w) << 32;
+        });
       if (!MASS) n[0] = one[0], n[1] = one[1];
       if (threadIdx.x == 0) s.bin = -1;
       uint64_t all;
@@ -370,49 +479,42 @@ struct Row {
       lo = hi - lo >= 1u << shift ? hi - ((1u << shift) - 1) : lo;
       const bool whole = s.alone != 0;
       if (whole || shift == 0) {
-        const int last = lo == kept.key ? kept.index : INT_MAX;
-        kept = Prefix{lo, whole ? last : first_by_index<MASS>(lo, last, target)};
+        const float v = order_value(lo);
+        const int last = v == kept.value ? kept.index : INT_MAX;
+        kept = Prefix{v, whole ? last : first_by_index<MASS>(v, last, target)};
         return;
       }
     }
   }
   template <bool MASS>
-  __device__ __forceinline__ void add(Hist& h, uint32_t b, float x) const {
+  __device__ __forceinline__ void add(Hist& h, uint32_t b, uint64_t w) const {
     atomicAdd(&h.count[b], 1u);
-    if (MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&h.weight[b]), static_cast<unsigned long long>(weight(x)));
-  }
-  __device__ __forceinline__ int2 ld_pair(const uint32_t* p, uint32_t rank) const {
-    int2 v;
-    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];"
-                 : "=r"(v.x), "=r"(v.y)
-                 : "r"(mapa_shared(smem_u32(p), rank))
-                 : "memory");
-    return v;
+    if (MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&h.weight[b]), static_cast<unsigned long long>(w));
   }
 
-  // Of the logits equal to order_value(key), up to index `last`: the index of the one
+  // Of the logits equal to v, up to index `last`: the index of the one
   // that brings their count or weight up to `target`; s.in is that of all.
   template <bool MASS>
-  __device__ __forceinline__ int first_by_index(uint32_t key, int last, uint64_t target) {
-    const uint64_t each = MASS ? weight(order_value(key)) : 1;
+  __device__ __forceinline__ int first_by_index(float v, int last, uint64_t target) {
+    const uint64_t each = MASS ? weight(v) : 1;
     const uint64_t take = (target + each - 1) / each, have = s.in / each;
     if (take >= have) return last;
     uint64_t n = 0;
-    sweep([&](int i, float x) { n += order_key(x) == key && i <= last; });
+    sweep([&](int i, float x) { n += x == v && i <= last; });
     n = warp_sum(n);
     if (lane == 0) s.count[warp] = n;
     sync();
     uint64_t before = 0;
     int at = -1;  // the warp (of the cluster) that has the last one
     for (int b = 0; at < 0 && b < C * kWarps; b += 32) {
-      const uint64_t v = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
-      const uint64_t incl = before + warp_scan(v, lane);
+      const uint64_t of = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
+      const uint64_t incl = before + warp_scan(of, lane);
       const unsigned hit = __ballot_sync(0xffffffffu, incl >= take);
       if (hit != 0) at = b + __ffs(hit) - 1;
-      before = __shfl_sync(0xffffffffu, hit != 0 ? incl - v : incl, hit != 0 ? __ffs(hit) - 1 : 31);
+      before = __shfl_sync(0xffffffffu, hit != 0 ? incl - of : incl, hit != 0 ? __ffs(hit) - 1 : 31);
     }
     if (at == rank * kWarps + warp) {
-      const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(order_key(x) == key && i <= last); });
+      const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(x == v && i <= last); });
       if (lane == 0) s.index = i;
     }
     sync();
@@ -462,17 +564,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = p.ctas, rank = static_cast<int>(cluster_ctarank()), r = blockIdx.x / C;
   if (tid < kWarps) mbar_init(&s.bar[tid], 1);
-  if (tid < kSampleTable) s.table[tid] = sample_entry(tid);
+  if (tid < kSampleTable) s.table[tid] = p.table[tid];
   for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
     reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
   fence_mbar_init();
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  const float T = p.temperature ? p.temperature[r] : 1.f, u = p.u[r];
-  const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
-  const int top_k = p.top_k ? p.top_k[r] : 0;
 
   const uint8_t* row = static_cast<const uint8_t*>(p.logits) + static_cast<long long>(r) * p.stride * sizeof(typename G::T);
   const uintptr_t base = reinterpret_cast<uintptr_t>(row) & ~static_cast<uintptr_t>(15);
@@ -484,19 +582,30 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, w0, w1, head, r, lane, warp, rank, C};
   R& x = row_;
 
+  const int f0 = w0 < w1 && !x.whole(w0) ? w0 + 1 : w0, f1 = w0 < w1 && !x.whole(w1 - 1) ? w1 - 1 : w1;
+  const bool loads = RESIDENT && f0 < f1;  // this warp, by a bulk copy
+  if (loads && lane == 0) {
+    const uint32_t bytes = static_cast<uint32_t>(f1 - f0) * 16u;
+    mbar_arrive_expect_tx(&s.bar[warp], bytes);
+    bulk_load(x.slice + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
+  }
+  const float T = p.temperature ? p.temperature[r] : 1.f, t = sample_temperature(T), u = p.u[r];
+  const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
+  const int top_k = p.top_k ? p.top_k[r] : 0;
+
+  // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by
+  // all of them, with the logarithm, the table and the shares, it was half the time
+  if (tid == kThreads - 32) s.scale = sample_scale(t, p.shift);
+  if (tid == kThreads - 64 && min_p > 0.f) {
+    const double x = static_cast<double>(t) * log(static_cast<double>(fminf(min_p, 1.f)));
+    s.floor_hi = static_cast<float>(x);
+    s.floor_lo = static_cast<float>(x - s.floor_hi);
+  }
   int bad = 0;
   if (RESIDENT && w0 < w1) {
-    const int f0 = x.whole(w0) ? w0 : w0 + 1, f1 = x.whole(w1 - 1) ? w1 : w1 - 1;
-    if (f0 < f1) {
-      const uint32_t bytes = static_cast<uint32_t>(f1 - f0) * 16u;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(&s.bar[warp], bytes);
-        bulk_load(x.slice + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
-      }
-    }
     if (lane == 0 && !x.whole(w0)) x.slice[w0 - g0] = x.edge(w0);
     if (lane == 1 && w1 - 1 > w0 && !x.whole(w1 - 1)) x.slice[w1 - 1 - g0] = x.edge(w1 - 1);
-    if (f0 < f1 && !mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr)) {
+    if (loads && !mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr)) {
       bad = 2;
       atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
       mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr);  // the copy lands before this CTA ends
@@ -506,10 +615,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   // the largest logit; NaN, infinity and rows of nothing are refused
   float m = -INFINITY;
-  x.sweep([&](int, float v) {
-    m = fmaxf(m, v);
-    bad |= v != v;
-  });
+  x.sweep([&](int, float v) { asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v)); });
+  bad |= m != m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -520,7 +627,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     s.bad[warp] = bad;
   }
   x.sync();
-  for (int i = lane; i < C * kWarps; i += 32) {
+#pragma unroll
+  for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
+    const int i = j * 32 + lane;
+    if (i >= C * kWarps) continue;
     m = fmaxf(m, ld_cluster(&s.max[i % kWarps], i / kWarps));
     bad |= ld_cluster(&s.bad[i % kWarps], i / kWarps);
   }
@@ -561,15 +671,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     return;
   }
 
-  x.c = sample_scale(T, p.shift);
+  x.c = s.scale;
   // nothing that has weight lies below: 40 / log2(e) = 27.73, and room for rounding
-  const float low = m - 28.f * fminf(fmaxf(T, 1e-30f), 1e30f) - fabsf(m) * 9.5367431640625e-7f;
-  const uint32_t floor = order_key(low > -3.402823466e38f ? low : -3.402823466e38f);
-  const uint32_t top = order_key(m);
+  const float low = m - 28.f * t - fabsf(m) * 9.5367431640625e-7f;
+  const uint32_t floor = order_key(low > -3.402823466e38f ? low : -3.402823466e38f), top = x.key(m);
   const bool by_k = top_k > 0 && top_k < p.vocab;
-  const uint32_t q_min = min_p > 0.f ? order_key(sample_floor(m, T, min_p) + 0.f) : 0;
+  const float least = min_p > 0.f ? sample_floor(m, s.floor_hi, s.floor_lo) : -INFINITY;
   bool by_p = top_p < 1.f;
-  Prefix kept{floor, INT_MAX};
+  Prefix kept{order_value(floor), INT_MAX};
   uint64_t sum = 0;
   if (by_k || by_p) {
     x.count(by_k ? top_k : 0, top_p);
@@ -584,54 +693,53 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const uint32_t k_lo = s.bound[0], k_hi = s.bound[1] - 1, p_lo = s.bound[2], p_hi = s.bound[3] - 1;
     if (cut_k) {
       if (s.k_whole)
-        kept.key = k_lo;
+        kept.value = order_value(k_lo);
       else
         x.template refine<false>(kept, k_lo, k_hi, static_cast<uint64_t>(top_k - s.k_before), false);
     }
-    by_p = by_p && q_min <= p_hi;  // else min-p keeps less, whatever top-p does
+    by_p = by_p && least <= x.up_to(p_hi);  // else min-p keeps less, whatever top-p does
     if (by_p) {
-      const uint32_t lo = max(p_lo, kept.key), hi = p_hi;
+      const uint32_t lo = max(p_lo, x.key(kept.value)), hi = p_hi;
+      const float f_lo = order_value(lo), f_hi = x.up_to(hi);
       const int shift = x.shift_of(lo, hi);
-      uint64_t below = 0;
+      uint64_t all = 0;
       x.clear();
       Hist& h = s.hist[x.level & 1];
-      x.sweep([&](int i, float v) {
-        const uint32_t q = order_key(v);
-        if (!kept.has(q, i)) return;
-        if (q >= lo && q <= hi) {
-          x.template add<true>(h, (hi - q) >> shift, v);
-        } else {
-          const uint64_t w = x.weight(v);
-          if (q > hi)
-            sum += w;
-          else
-            below += w;
+      x.sweep4([&](int i, const float(&v)[4]) {
+        uint64_t w[4];
+        if (!x.weights(v, w, [&](int j) { return kept.has(v[j], i + j); })) return;
+        bool within = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          all += w[j];
+          sum += v[j] > f_hi ? w[j] : 0;
+          within |= v[j] >= f_lo && v[j] <= f_hi;
         }
+        if (within)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (v[j] >= f_lo && v[j] <= f_hi && w[j] != 0) x.template add<true>(h, (hi - x.key(v[j])) >> shift, w[j]);
       });
-      const uint64_t above = warp_sum(sum), all = warp_sum(below + sum);
+      const uint64_t above = warp_sum(sum);
+      all = warp_sum(all);
       if (lane == 0) s.part[warp] = above, s.rest[warp] = all;
       x.sync();
-      uint64_t within = 0;
-      // every CTA's bins, for the sum that the share is taken of
-      for (int i = 0; i < C; ++i) {
-        const uint4 w = ld_cluster(reinterpret_cast<const uint4*>(h.weight) + tid, i);
-        within += (w.x | static_cast<uint64_t>(w.y) << 32) + (w.z | static_cast<uint64_t>(w.w) << 32);
-      }
-      uint64_t total;
-      x.block_scan(within, s.scan, total);
-      const uint64_t share = sample_share(top_p, total + x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
+      const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
       x.template refine<true>(kept, lo, hi, share > over ? share - over : 1, true);
-      if (q_min > kept.key) kept = Prefix{q_min, INT_MAX};
-      x.sweep([&](int i, float v) {
-        const uint32_t q = order_key(v);
-        if (q >= lo && q <= hi && kept.has(q, i)) sum += x.weight(v);
+      if (least > kept.value) kept = Prefix{least, INT_MAX};
+      x.sweep4([&](int i, const float(&v)[4]) {
+        uint64_t w[4];
+        if (!x.weights(v, w, [&](int j) { return v[j] <= f_hi && kept.has(v[j], i + j); })) return;
+        sum += (w[0] + w[1]) + (w[2] + w[3]);
       });
     }
   }
   if (!by_p) {
-    if (q_min > kept.key) kept = Prefix{q_min, INT_MAX};
-    x.sweep([&](int i, float v) {
-      if (kept.has(order_key(v), i)) sum += x.weight(v);
+    if (least > kept.value) kept = Prefix{least, INT_MAX};
+    x.sweep4([&](int i, const float(&v)[4]) {
+      uint64_t w[4];
+      if (!x.weights(v, w, [&](int j) { return kept.has(v[j], i + j); })) return;
+      sum += (w[0] + w[1]) + (w[2] + w[3]);
     });
   }
 
@@ -640,14 +748,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   if (lane == 0) s.count[warp] = sum;
   x.sync();
   uint64_t before = 0, total = 0;
-  for (int i = lane; i < C * kWarps; i += 32) {
+#pragma unroll
+  for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
+    const int i = j * 32 + lane;
+    if (i >= C * kWarps) continue;
     const uint64_t v = ld_cluster(&s.count[i % kWarps], i / kWarps);
     if (i < rank * kWarps + warp) before += v;
     total += v;
   }
   before = warp_sum(before);
   total = warp_sum(total);
-  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(order_key(v), i) ? x.weight(v) : 0; };
+  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(v, i) ? x.weight(v) : 0; };
   const uint64_t at = sample_point(u, total);
   if (before <= at && at < before + sum) {
     const int i = x.nth(at - before + 1, kept_weight);
@@ -659,8 +770,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       for (int j = 0; j < G::N; ++j)
         if (j == (i + head) % G::N) l = v[j];
       p.token[r] = i;
-      p.prob[r] = static_cast<float>(exp((static_cast<double>(l) - m) / static_cast<double>(fminf(fmaxf(T, 1e-30f), 1e30f))) /
-                                     ldexp(static_cast<double>(total), -p.shift));
+      const SampleTerm w = sample_term(m, l, x.c, s.table);
+      const double one = __hiloint2double((1023 - 30 - w.k + p.shift) << 20, 0);  // 2^(shift - 30 - k)
+      p.prob[r] = static_cast<float>(static_cast<double>(w.w) * one / static_cast<double>(total));
     }
   }
   x.sync();
@@ -688,6 +800,7 @@ cudaError_t sample_configure() {
 cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   const long long size = p.dtype == EBD_LOGITS_F32 ? 4 : 2;
   const long long bytes = p.vocab * size + 32;  // both ends rounded out
+  for (int j = 0; j < kSampleTable; ++j) p.table[j] = sample_entry(j);
   p.ctas = 1;
   while (p.ctas < kMaxCtas && bytes / p.ctas > 32 * 1024) p.ctas *= 2;
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;

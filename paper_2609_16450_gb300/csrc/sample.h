@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <cstdint>
 
+#include "sample_math.h"
+
 namespace ebd {
 
 struct SampleParams {
@@ -18,6 +20,7 @@ struct SampleParams {
   int ctas;                  // CTAs (a cluster) per row
   int resident;              // a CTA's slice of the row stays in its shared memory
   uint64_t limit_ns;
+  uint32_t table[kSampleTable];
 };
 
 cudaError_t sample_configure();

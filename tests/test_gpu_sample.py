@@ -134,6 +134,27 @@ def test_equal_logits(vocab):
     h.close()
 
 
+def test_borders_at_zero():
+    """-0 and 0 are equal, and between the smallest numbers on either side."""
+    vocab, rows = 4001, 64
+    h = handle(vocab)
+    g = np.random.default_rng(11)
+    tiny = np.array([0.0, -0.0, 1e-45, -1e-45, 3e-45, -3e-45, 1e-38, -1e-38, 2e-3, -2e-3, 5e-39], np.float32)
+    x = tiny[g.integers(0, len(tiny), (rows, vocab))]
+    x[::2, :40] = g.standard_normal((rows // 2, 40))
+    T = np.exp(g.uniform(np.log(1e-3), 0, rows)).astype(np.float32)
+    for filters in ("k", "p", "kpq"):
+        k = g.integers(1, vocab, rows).astype(np.int32) if "k" in filters else None
+        p = g.uniform(0, 1, rows).astype(np.float32) if "p" in filters else None
+        q = np.exp(g.uniform(-5, 0, rows)).astype(np.float32) if "q" in filters else None
+        u = g.uniform(0, 1, rows).astype(np.float32) * np.float32(1 - 2 ** -24)
+        logits = torch.from_numpy(x).cuda()
+        token, prob, status = sample(h, logits, u, T, k, p, q)
+        assert status == 0
+        verify(logits, T, k, p, q, u, token, prob)
+    h.close()
+
+
 def test_extreme_values():
     """Masks of the type's lowest value, logits of any size, temperatures from nothing
     to infinite, one logit left, u at both ends."""
