@@ -15,13 +15,15 @@
 // 16-byte groups, so that sums by warp are sums by index.  A CTA's slice of the row
 // comes into its shared memory once.
 //
-// The last logit of a prefix is found without sorting.  One sweep counts logits in
-// bins of equal width of y = (m - l) log2(e) / T.  They give the bin that top-k's
-// k-th lies in, and, as a bin's weights differ by a factor of 2^(1/51) at most,
-// bounds on the sums and so the few bins that top-p's border lies in.  One sweep sums
-// weights: above those bins, below them, and within them by the logits' ordered bits.
-// The bin that the border then lies in is taken apart the same way, until all of it
-// is wanted or its logits are equal, of which the first by index are taken.
+// The last logit of a prefix is found without sorting, in one of three ways.
+//   - Top-k of few: the least of what the CTAs' threads have as their largest logits,
+//     the (k / CTAs)-th of each CTA's, is a bound that k logits reach and not many
+//     more.  Those are listed, and one CTA does the rest with them in registers.
+//   - Top-p: one sweep counts logits in bins of y = (m - l) log2(e) / T, which bound
+//     the sums and so the few bins that the border lies in; a second sums what lies
+//     above them and lists what lies within, and again one CTA does the rest.
+//   - Where such a list would be too long (ties, most of all): histograms over the
+//     logits' ordered bits, each level over the bin that the last one chose.
 #include <cuda_fp16.h>
 
 #include <climits>
@@ -36,10 +38,12 @@ namespace ebd {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 2048;               // of y, counts
-constexpr float kBinScale = 51.15f;       // of them per unit of y: 40 * 51.15 = 2046
-constexpr int kFine = 1024, kFineBits = 10;  // of ordered bits, weights and counts
 constexpr int kMaxCtas = 8;
+constexpr int kBins = 2048;                  // of y, counts
+constexpr int kFine = 512, kFineBits = 9;    // of ordered bits, weights and counts
+constexpr int kLocal = 1024, kLocalBits = 10;  // of a list
+constexpr int kList = 2048, kItems = kList / kThreads;  // listed logits, of a CTA and of a row
+constexpr int kListMost = kThreads / 2;      // of a CTA's threads, for a list of top-k's
 constexpr int kSliceBytes = 76 * 1024;  // of a row in shared memory
 
 // Loads from a CTA of the cluster; volatile, so none moves across a barrier, and
@@ -61,6 +65,9 @@ __device__ __forceinline__ uint4 ld_cluster(const uint4* p, uint32_t rank) {
                : "r"(mapa_shared(smem_u32(p), rank))
               );
   return v;
+}
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t rank) {
+  return static_cast<uint32_t>(ld_cluster(reinterpret_cast<const int*>(p), rank));
 }
 __device__ __forceinline__ uint2 ld_cluster(const uint2* p, uint32_t rank) {
   uint2 v;
@@ -143,23 +150,50 @@ struct alignas(16) Hist {
       uint64_t weight[kFine];
       uint32_t count[kFine];
     };
+    uint64_t local[kLocal];
   };
 };
 
+// y to bins: the lesser of two lines, fine ones up to a knee and coarse ones from there
+// to 40.  Rounding keeps their order.
+struct Bins {
+  float fine, coarse, shift;
+  __device__ __forceinline__ int of(float y) const {
+    if (!(y <= kSampleDead)) return kBins;
+    return static_cast<int>(__float_as_uint(fminf(fmaf(y, fine, 8388608.f), fmaf(y, coarse, 8388608.f + shift))) & 0x7FFFFFu);
+  }
+  // where bin b begins
+  __device__ __forceinline__ float from(int b) const {
+    return fmaxf((static_cast<float>(b) - 0.5f) / fine, (static_cast<float>(b) - 0.5f - shift) / coarse);
+  }
+};
+__device__ __forceinline__ Bins make_bins(float knee) {
+  constexpr float kFew = 500.f, kMost = 1540.f;
+  if (!(knee < kSampleDead * 0.75f)) return {2040.f / kSampleDead, 2040.f / kSampleDead, 0.f};
+  knee = fmaxf(knee, 1e-3f);
+  const float fine = kMost / knee, coarse = kFew / (kSampleDead - knee);
+  return {fine, coarse, rintf(kMost - knee * coarse)};
+}
+
 struct Shared {
   Hist hist[2];
+  uint2 list[kList];         // logits (their bits) and indices
   uint32_t table[kSampleTable];
   uint64_t part[kWarps];     // a warp's sums: of what is kept for sure,
-  uint64_t rest[kWarps];     // of what is not;
-  uint64_t count[kWarps];    // its elements at the border
+  uint64_t rest[kWarps];     // of all that may be kept;
+  uint64_t count[kWarps];    // its elements at the border, or what of it is kept
   uint64_t scan[kWarps];
+  uint64_t chunk[kMaxCtas * kWarps];  // what every warp of the cluster has, of what is kept
   float scan_f[kWarps];
   uint64_t bar[kWarps];
-  uint64_t before, in;
-  float max[kWarps];
+  uint64_t before, in, want, total;
+  float max[kWarps], low[kWarps];
   int bad[kWarps];
   int first[kWarps];
-  int bin, k_bin, k_whole, k_before, p_first, p_last, alone, index;
+  float kth;                 // a bound of the row's k-th logit, of this CTA's threads'
+  int listed;
+  int bin, k_bin, k_whole, k_before, p_first, p_last, n_first, n_last, alone, index, owner, last;
+  float value;
   uint32_t bound[4];
   SampleScale scale;
   float floor_hi, floor_lo;  // T ln min_p
@@ -210,10 +244,12 @@ struct Row {
   const SampleParams& p;
   const uint8_t* data;      // the row's first 16-byte group, in global memory
   uint4* slice;             // this CTA's groups [g0, ..) in shared memory
-  int g0, w0, w1, head, r;  // this warp's groups [w0, w1), elements before the row's in the first group
+  int g0, g1, per_warp;     // its end, and the groups of a warp
+  int w0, w1, head, r;      // this warp's groups [w0, w1), elements before the row's in the first group
   int lane, warp, rank, C;
   float m = 0.f;
   SampleScale c{};
+  Bins bins{};
   int level = 0;
 
   __device__ __forceinline__ void sync() const {
@@ -306,10 +342,7 @@ struct Row {
   }
 
   // Bin of a logit, by descending logits, and past the last for weights of zero
-  __device__ __forceinline__ int bin_of(float x) const {
-    const float y = sample_depth(m, x, c);
-    return y <= kSampleDead ? static_cast<int>(__float_as_uint(fmaf(y, kBinScale, 8388608.f)) & 0x7FFFFFu) : kBins;
-  }
+  __device__ __forceinline__ int bin_of(float x) const { return bins.of(sample_depth(m, x, c)); }
   // Least ordered bits with a bin of at most b (one warp)
   __device__ __forceinline__ uint32_t bound(int b, uint32_t lo, uint32_t hi) const {
     while (lo < hi) {
@@ -383,14 +416,14 @@ struct Row {
     uint32_t n[N] = {0, 0, 0, 0};
     gather(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x,
            [&](const uint4& v) { n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w; });
-    if (threadIdx.x == 0) s.k_bin = kBins, s.k_whole = 0, s.p_first = s.p_last = kBins - 1;
+    if (threadIdx.x == 0) s.k_bin = kBins, s.k_whole = 0, s.p_first = s.p_last = kBins - 1, s.n_first = 0, s.n_last = INT_MAX;
     uint32_t all;
     const uint32_t sum = n[0] + n[1] + n[2] + n[3];
     uint32_t before = block_scan(sum, reinterpret_cast<uint32_t*>(s.scan), all) - sum;
+    const uint32_t want = k > 0 ? min(static_cast<uint32_t>(k), all) : all, first = min(before, want);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const uint32_t want = k > 0 ? static_cast<uint32_t>(k) : all;
-      if (before < want && before + n[j] >= want && k > 0) {
+      if (k > 0 && k <= all && before < want && before + n[j] >= want) {
         s.k_bin = threadIdx.x * N + j;
         s.k_before = static_cast<int>(before);
         s.k_whole = before + n[j] == want;
@@ -400,20 +433,30 @@ struct Row {
       n[j] = min(n[j], left);  // what top-k leaves
     }
     if (share < 1.f) {
-      // A bin's weights are between lo times and once its first's; 10^-4 is far more
-      // than all roundings here.
-      const float lo = exp2f(-1.f / kBinScale) * (1.f - 1e-4f);
-      float w[N], mass = 0.f, total;
-#pragma unroll
-      for (int j = 0; j < N; ++j) mass += w[j] = static_cast<float>(n[j]) * exp2f((0.5f - (threadIdx.x * N + j)) / kBinScale);
-      float to = block_scan(mass, s.scan_f, total) - mass;
-      const float least = share * total * lo * (1.f - 1e-4f), most = fminf(fmaxf(share * total * (1.f + 1e-4f), 1e-30f), total * lo * (1.f - 1e-4f));
+      // Sums of weights as they are at most and at least, a bin's all as heavy as where
+      // it begins or ends; 10^-4 is far more than all roundings here.
+      float most[N], least[N], sum_most = 0.f, sum_least = 0.f, all_most, all_least;
+      float edge = exp2f(-bins.from(threadIdx.x * N));
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float next = to + w[j];
-        if ((to < least || threadIdx.x * N + j == 0) && next >= least) s.p_first = threadIdx.x * N + j;
-        if (to * lo < most && next * lo >= most) s.p_last = threadIdx.x * N + j;
-        to = next;
+        const float next = exp2f(-bins.from(threadIdx.x * N + j + 1));
+        sum_most += most[j] = static_cast<float>(n[j]) * edge;
+        sum_least += least[j] = static_cast<float>(n[j]) * next;
+        edge = next;
+      }
+      float to_most = block_scan(sum_most, s.scan_f, all_most) - sum_most;
+      float to_least = block_scan(sum_least, reinterpret_cast<float*>(s.scan), all_least) - sum_least;
+      const float from = share * all_least * (1.f - 1e-4f);
+      const float upto = fminf(fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f), all_least * (1.f - 1e-4f));
+      uint32_t at = first;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int b = threadIdx.x * N + j;
+        if ((to_most < from || b == 0) && to_most + most[j] >= from) s.p_first = b, s.n_first = static_cast<int>(at);
+        at += n[j];
+        if (to_least < upto && to_least + least[j] >= upto) s.p_last = b, s.n_last = static_cast<int>(at);
+        to_most += most[j];
+        to_least += least[j];
       }
     }
     __syncthreads();
@@ -448,29 +491,22 @@ struct Row {
         sync();
       }
       ++level;
-      constexpr int N = kFine / kThreads;
-      static_assert(N == 2, "a thread's bins are one vector");
-      uint64_t n[N] = {0, 0};
-      uint32_t one[N] = {0, 0};
-      gather(reinterpret_cast<const uint2*>(h.count) + threadIdx.x, [&](const uint2& v) { one[0] += v.x, one[1] += v.y; });
+      static_assert(kFine == kThreads, "a bin a thread");
+      uint64_t n = 0;
+      uint32_t one = 0;
+      gather(h.count + threadIdx.x, [&](uint32_t v) { one += v; });
       if (MASS)
-        gather(reinterpret_cast<const uint4*>(h.weight) + threadIdx.x, [&](const uint4& v) {
-          n[0] += v.x | static_cast<uint64_t>(v.y) << 32;
-          n[1] += v.z | static_cast<uint64_t>(v.w) << 32;
-        });
-      if (!MASS) n[0] = one[0], n[1] = one[1];
+        gather(h.weight + threadIdx.x, [&](uint64_t v) { n += v; });
+      else
+        n = one;
       if (threadIdx.x == 0) s.bin = -1;
       uint64_t all;
-      uint64_t before = block_scan(n[0] + n[1], s.scan, all) - n[0] - n[1];
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (before < target && before + n[j] >= target) {
-          s.bin = threadIdx.x * N + j;
-          s.before = before;
-          s.in = n[j];
-          s.alone = MASS ? one[j] == 1 : before + n[j] == target;
-        }
-        before += n[j];
+      const uint64_t before = block_scan(n, s.scan, all) - n;
+      if (before < target && before + n >= target) {
+        s.bin = threadIdx.x;
+        s.before = before;
+        s.in = n;
+        s.alone = MASS ? one == 1 : before + n == target;
       }
       __syncthreads();
       if (s.bin < 0) return;  // less than target in all
@@ -504,54 +540,218 @@ struct Row {
     n = warp_sum(n);
     if (lane == 0) s.count[warp] = n;
     sync();
-    uint64_t before = 0;
-    int at = -1;  // the warp (of the cluster) that has the last one
-    for (int b = 0; at < 0 && b < C * kWarps; b += 32) {
-      const uint64_t of = b + lane < C * kWarps ? ld_cluster(&s.count[(b + lane) % kWarps], (b + lane) / kWarps) : 0;
-      const uint64_t incl = before + warp_scan(of, lane);
-      const unsigned hit = __ballot_sync(0xffffffffu, incl >= take);
-      if (hit != 0) at = b + __ffs(hit) - 1;
-      before = __shfl_sync(0xffffffffu, hit != 0 ? incl - of : incl, hit != 0 ? __ffs(hit) - 1 : 31);
-    }
-    if (at == rank * kWarps + warp) {
-      const int i = nth(take - before, [&](int i, float x) { return static_cast<uint64_t>(x == v && i <= last); });
-      if (lane == 0) s.index = i;
-    }
+    uint64_t v4[4], left = take;
+    load4(s.count, v4);
+    const int at = owner_of(v4, left);  // the warp (of the cluster) that has the last one
+    if (at / kWarps == rank) nth(at % kWarps, left, [&](int i, float x) -> uint64_t { return x == v && i <= last; });
     sync();
     // nobody writes s.index again before the next sync() of all
     return ld_cluster(&s.index, at / kWarps);
   }
 
-  // The index in this warp's run at which the sum of f first reaches `want` >= 1
+  // The index in the run of this CTA's warp `of` at which the sum of f first reaches
+  // `want` >= 1, found by all its warps: an iteration of that run each.
   template <typename F>
-  __device__ __forceinline__ int nth(uint64_t want, F f) const {
-    uint64_t before = 0;
-    for (int g = w0; g < w1; g += 32) {
+  __device__ __forceinline__ int nth(int of, uint64_t want, F f) {
+    const int r0 = min(g1, g0 + of * per_warp), r1 = min(g1, r0 + per_warp);
+    for (int base = r0; base < r1; base += 32 * kWarps) {
+      const int g = base + 32 * warp + lane;
       float x[G::N];
       uint64_t v[G::N], sum = 0;
-      if (g + lane < w1) {
-        G::get(fetch(g + lane), x);
+      if (g < r1) {
+        G::get(fetch(g), x);
 #pragma unroll
-        for (int j = 0; j < G::N; ++j) sum += v[j] = f((g + lane) * G::N + j - head, x[j]);
+        for (int j = 0; j < G::N; ++j) sum += v[j] = f(g * G::N + j - head, x[j]);
       }
-      const uint64_t incl = before + warp_scan(sum, lane);
-      const unsigned hit = __ballot_sync(0xffffffffu, incl >= want);
-      if (hit != 0) {
-        const int l = __ffs(hit) - 1;
+      uint64_t all;
+      const uint64_t incl = block_scan(sum, s.scan, all);
+      if (incl >= want && incl - sum < want) {  // one thread
+        uint64_t at = incl - sum;
         int i = -1;
-        if (lane == l) {
-          uint64_t at = incl - sum;
 #pragma unroll
-          for (int j = 0; j < G::N; ++j) {
-            at += v[j];
-            if (i < 0 && at >= want) i = (g + lane) * G::N + j - head;
-          }
+        for (int j = 0; j < G::N; ++j) {
+          at += v[j];
+          if (i < 0 && at >= want) i = g * G::N + j - head;
         }
-        return __shfl_sync(0xffffffffu, i, l);
+        s.index = i;
       }
-      before = __shfl_sync(0xffffffffu, incl, 31);
+      __syncthreads();
+      if (all >= want) return s.index;
+      want -= all;
     }
     return -1;
+  }
+  // Which of the cluster's warps has the sum of v, its warps' values, reach `want` >= 1,
+  // and what is left of `want` there (lane i of every warp: v of warps 4 i ..)
+  __device__ __forceinline__ int owner_of(const uint64_t (&v)[4], uint64_t& want) const {
+    const uint64_t sum = (v[0] + v[1]) + (v[2] + v[3]);
+    const uint64_t incl = warp_scan(sum, lane);
+    const int l = max(__ffs(__ballot_sync(0xffffffffu, incl >= want)) - 1, 0);
+    uint64_t left = want - (incl - sum);
+    int at = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (at == j && left > v[j]) {
+        left -= v[j];
+        at = j + 1;
+      }
+    want = __shfl_sync(0xffffffffu, left, l);
+    return __shfl_sync(0xffffffffu, 4 * lane + at, l);
+  }
+  // what the cluster's warps have at s.count + warp
+  __device__ __forceinline__ void load4(const uint64_t* of, uint64_t (&v)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = 4 * lane + j;
+      v[j] = i < C * kWarps ? ld_cluster(of + i % kWarps, i / kWarps) : 0;
+    }
+  }
+  // token and probability: this CTA's logit i
+  __device__ __forceinline__ void put(int i, float l, uint64_t total) const {
+    p.token[r] = i;
+    const SampleTerm w = sample_term(m, l, c, s.table);
+    const double one = __hiloint2double((1023 - 30 - w.k + c.shift) << 20, 0);  // 2^(shift - 30 - k)
+    p.prob[r] = static_cast<float>(static_cast<double>(w.w) * one / static_cast<double>(total));
+  }
+  // Draws from what is kept: warp `owner` of the cluster has the one that brings its
+  // kept sum up to `want`.
+  __device__ __forceinline__ void draw(const Prefix& kept, int owner, uint64_t want, uint64_t total) {
+    if (owner / kWarps != rank) return;
+    const int i = nth(owner % kWarps, want, [&](int i, float v) -> uint64_t { return kept.has(v, i) ? weight(v) : 0; });
+    if (threadIdx.x == 0 && i >= 0) {
+      float v[G::N];
+      G::get(fetch((i + head) / G::N), v);
+      float l = 0.f;
+#pragma unroll
+      for (int j = 0; j < G::N; ++j)
+        if (j == (i + head) % G::N) l = v[j];
+      put(i, l, total);
+    }
+  }
+
+  // ---- lists: logits of the whole row in one CTA's registers, kItems a thread
+  struct Items {
+    float x[kItems];
+    int i[kItems];
+    uint64_t w[kItems];
+  };
+  __device__ __forceinline__ void push(float x, int i) {
+    const int at = atomicAdd(&s.listed, 1);
+    if (at < kList) s.list[at] = make_uint2(__float_as_uint(x), static_cast<uint32_t>(i));
+  }
+  // Number of logits that the cluster's CTAs have listed
+  __device__ __forceinline__ int listed() const {
+    int n = 0;
+    gather(&s.listed, [&](int v) { n += min(v, kList + 1); });
+    return n;
+  }
+  // All of them, kList at most; places past them have no weight and -inf
+  __device__ __forceinline__ void take(Items& t) const {
+    int n[kMaxCtas] = {};
+#pragma unroll
+    for (int k = 0; k < kMaxCtas; ++k)
+      if (k < C) n[k] = ld_cluster(&s.listed, k);
+#pragma unroll
+    for (int q = 0; q < kItems; ++q) {
+      int at = threadIdx.x + q * kThreads, of = 0;
+#pragma unroll
+      for (int k = 0; k < kMaxCtas - 1; ++k)
+        if (of == k && at >= n[k]) {
+          at -= n[k];
+          of = k + 1;
+        }
+      t.x[q] = -INFINITY;
+      t.i[q] = -1;
+      if (of < C && at < min(n[of], kList)) {
+        const uint2 v = ld_cluster(&s.list[at], of);
+        t.x[q] = __uint_as_float(v.x);
+        t.i[q] = static_cast<int>(v.y);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kItems; ++q) t.w[q] = t.i[q] >= 0 ? weight(t.x[q]) : 0;
+  }
+  // One level: v by bin; the bin where their sum reaches `target` in s.bin, with the
+  // sum before it in s.before and its own in s.in
+  template <typename B>
+  __device__ __forceinline__ bool level_of(const uint64_t (&v)[kItems], uint64_t target, B bin) {
+    static_assert(kLocal == 2 * kThreads, "two bins a thread");
+    uint64_t* h = s.hist[1].local;
+    reinterpret_cast<uint4*>(h)[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kItems; ++q) {
+      if (v[q] == 0) continue;
+      const int b = bin(q);
+      if (b >= 0) atomicAdd(reinterpret_cast<unsigned long long*>(h + b), static_cast<unsigned long long>(v[q]));
+    }
+    __syncthreads();
+    const uint64_t n0 = h[2 * threadIdx.x], n1 = h[2 * threadIdx.x + 1];
+    if (threadIdx.x == 0) s.bin = -1;
+    uint64_t all;
+    const uint64_t before = block_scan(n0 + n1, s.scan, all) - n0 - n1;
+    if (before < target && before + n0 + n1 >= target) {
+      const bool second = before + n0 < target;
+      s.bin = 2 * threadIdx.x + second;
+      s.before = before + (second ? n0 : 0);
+      s.in = second ? n1 : n0;
+    }
+    __syncthreads();
+    return s.bin >= 0;
+  }
+  // The index at which the sum of v by index reaches `target`
+  __device__ __forceinline__ int list_nth(const Items& t, const uint64_t (&v)[kItems], uint64_t target) {
+    int lo = 0, hi = p.vocab - 1;
+    for (;;) {
+      const int shift = max(0, 32 - __clz(hi - lo) - kLocalBits);
+      if (!level_of(v, target, [&](int q) { return t.i[q] >= lo && t.i[q] <= hi ? (t.i[q] - lo) >> shift : -1; })) return -1;
+      target -= s.before;
+      lo += s.bin << shift;
+      hi = min(hi, lo + (1 << shift) - 1);
+      if (shift == 0) return lo;
+    }
+  }
+  // refine() of a list
+  template <bool MASS>
+  __device__ __forceinline__ void list_cut(const Items& t, Prefix& kept, uint32_t lo, uint32_t hi, uint64_t target) {
+    uint64_t v[kItems];
+    for (;;) {
+      const int shift = max(0, 32 - __clz(hi - lo) - kLocalBits);
+      const float f_lo = order_value(lo), f_hi = up_to(hi);
+#pragma unroll
+      for (int q = 0; q < kItems; ++q)
+        v[q] = t.i[q] >= 0 && t.x[q] >= f_lo && t.x[q] <= f_hi && kept.has(t.x[q], t.i[q]) ? (MASS ? t.w[q] : 1) : 0;
+      if (!level_of(v, target, [&](int q) { return static_cast<int>((hi - key(t.x[q])) >> shift); })) return;
+      target -= s.before;
+      hi -= static_cast<uint32_t>(s.bin) << shift;
+      lo = hi - lo >= 1u << shift ? hi - ((1u << shift) - 1) : lo;
+      const float value = order_value(lo), top = up_to(hi);
+      int last = value == kept.value ? kept.index : INT_MAX;
+      if (!MASS && target == s.in) {  // all of the bin
+        kept = Prefix{value, last};
+        return;
+      }
+      if (shift == 0) {
+        const uint64_t each = MASS ? weight(value) : 1, take = (target + each - 1) / each, have = s.in / each;
+        if (take < have) {
+#pragma unroll
+          for (int q = 0; q < kItems; ++q) v[q] = v[q] != 0 && t.x[q] == value;
+          last = list_nth(t, v, take);
+        }
+        kept = Prefix{value, last};
+        return;
+      }
+      if (MASS) {
+        int n = 0;
+#pragma unroll
+        for (int q = 0; q < kItems; ++q) n += v[q] != 0 && t.x[q] >= value && t.x[q] <= top;
+        const int threads = __syncthreads_count(n > 0);
+        if (!__syncthreads_or(n > 1) && threads == 1) {  // one logit, wanted
+          kept = Prefix{value, last};
+          return;
+        }
+      }
+    }
   }
 };
 
@@ -563,28 +763,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   __shared__ Shared s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = p.ctas, rank = static_cast<int>(cluster_ctarank()), r = blockIdx.x / C;
-  if (tid < kWarps) mbar_init(&s.bar[tid], 1);
-  if (tid < kSampleTable) s.table[tid] = p.table[tid];
-  for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
-    reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
-  fence_mbar_init();
-  __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  const uint8_t* row = static_cast<const uint8_t*>(p.logits) + static_cast<long long>(r) * p.stride * sizeof(typename G::T);
+  const uint8_t* row = static_cast<const uint8_t*>(p.logits) + r * p.stride * static_cast<long long>(sizeof(typename G::T));
   const uintptr_t base = reinterpret_cast<uintptr_t>(row) & ~static_cast<uintptr_t>(15);
   const int head = static_cast<int>((reinterpret_cast<uintptr_t>(row) - base) / sizeof(typename G::T));
   const int groups = static_cast<int>((static_cast<long long>(head) + p.vocab + G::N - 1) / G::N);
   const int per = (groups + C - 1) / C, per_warp = (per + kWarps - 1) / kWarps;
   const int g0 = min(groups, rank * per), g1 = min(groups, g0 + per);
   const int w0 = min(g1, g0 + warp * per_warp), w1 = min(g1, w0 + per_warp);
-  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, w0, w1, head, r, lane, warp, rank, C};
+  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, g1, per_warp, w0, w1, head, r, lane, warp, rank, C};
   R& x = row_;
 
   const int f0 = w0 < w1 && !x.whole(w0) ? w0 + 1 : w0, f1 = w0 < w1 && !x.whole(w1 - 1) ? w1 - 1 : w1;
   const bool loads = RESIDENT && f0 < f1;  // this warp, by a bulk copy
   if (loads && lane == 0) {
+    mbar_init(&s.bar[warp], 1);
+    fence_mbar_init();
     const uint32_t bytes = static_cast<uint32_t>(f1 - f0) * 16u;
     mbar_arrive_expect_tx(&s.bar[warp], bytes);
     bulk_load(x.slice + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
@@ -593,6 +788,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
   const int top_k = p.top_k ? p.top_k[r] : 0;
 
+  if (tid < kSampleTable) s.table[tid] = p.table[tid];
+  for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
+    reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) s.listed = 0;
   // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by
   // all of them, with the logarithm, the table and the shares, it was half the time
   if (tid == kThreads - 32) s.scale = sample_scale(t, p.shift);
@@ -601,6 +800,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     s.floor_hi = static_cast<float>(x);
     s.floor_lo = static_cast<float>(x - s.floor_hi);
   }
+  __syncwarp();  // the barrier is there
   int bad = 0;
   if (RESIDENT && w0 < w1) {
     if (lane == 0 && !x.whole(w0)) x.slice[w0 - g0] = x.edge(w0);
@@ -613,17 +813,35 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     __syncwarp();
   }
 
-  // the largest logit; NaN, infinity and rows of nothing are refused
-  float m = -INFINITY;
-  x.sweep([&](int, float v) { asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v)); });
+  // The largest logit; NaN, infinity and rows of nothing are refused.  And the largest
+  // of the threads' least: a few in a hundred lie below it, unless more are masked.
+  const bool by_k = top_k > 0 && top_k < p.vocab;
+  const int most = (top_k + C - 1) / C;  // of a CTA's largest, for a list
+  const bool few = by_k && top_k <= kList / 2 && most <= kListMost && T > 0.f;
+  float m = -INFINITY, low = INFINITY;
+  x.sweep([&](int, float v) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v));
+    low = fminf(low, v);
+  });
   bad |= m != m;
+  low = low < INFINITY ? low : -INFINITY;
+  if (few) {
+    // bit by bit, the 20 that matter: rounded down, it bounds all the same
+    const uint32_t mine = x.key(m);
+    uint32_t t = 0;
+    for (int bit = 31; bit >= 12; --bit)
+      if (__syncthreads_count(mine >= (t | 1u << bit)) >= most) t |= 1u << bit;
+    if (tid == 0) s.kth = t > 0x00800000u ? order_value(t) : -3.402823466e38f;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    low = fmaxf(low, __shfl_xor_sync(0xffffffffu, low, o));
     bad |= __shfl_xor_sync(0xffffffffu, bad, o);
   }
   if (lane == 0) {
     s.max[warp] = m;
+    s.low[warp] = low;
     s.bad[warp] = bad;
   }
   x.sync();
@@ -632,11 +850,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const int i = j * 32 + lane;
     if (i >= C * kWarps) continue;
     m = fmaxf(m, ld_cluster(&s.max[i % kWarps], i / kWarps));
+    low = fmaxf(low, ld_cluster(&s.low[i % kWarps], i / kWarps));
     bad |= ld_cluster(&s.bad[i % kWarps], i / kWarps);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    low = fmaxf(low, __shfl_xor_sync(0xffffffffu, low, o));
     bad |= __shfl_xor_sync(0xffffffffu, bad, o);
   }
   const bool finite = !bad && m > -INFINITY && m < INFINITY;
@@ -673,14 +893,53 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 
   x.c = s.scale;
   // nothing that has weight lies below: 40 / log2(e) = 27.73, and room for rounding
-  const float low = m - 28.f * t - fabsf(m) * 9.5367431640625e-7f;
-  const uint32_t floor = order_key(low > -3.402823466e38f ? low : -3.402823466e38f), top = x.key(m);
-  const bool by_k = top_k > 0 && top_k < p.vocab;
+  const float dead = m - 28.f * t - fabsf(m) * 9.5367431640625e-7f;
+  const uint32_t floor = order_key(dead > -3.402823466e38f ? dead : -3.402823466e38f), top = x.key(m);
   const float least = min_p > 0.f ? sample_floor(m, s.floor_hi, s.floor_lo) : -INFINITY;
   bool by_p = top_p < 1.f;
   Prefix kept{order_value(floor), INT_MAX};
   uint64_t sum = 0;
+
+  if (few) {
+    float bound = m;
+    x.gather(&s.kth, [&](float v) { bound = fminf(bound, v); });
+    x.sweep4([&](int i, const float(&v)[4]) {
+      if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= bound)) return;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (v[j] >= bound) x.push(v[j], i + j);
+    });
+    x.sync();
+    if (x.listed() <= kList) {
+      typename R::Items items;
+      if (rank == 0) x.take(items);
+      x.sync();  // the others are done
+      if (rank != 0) return;
+      kept = Prefix{-3.402823466e38f, INT_MAX};
+      x.template list_cut<false>(items, kept, x.key(bound), top, static_cast<uint64_t>(top_k));
+      uint64_t total, v[kItems];
+      auto weigh = [&]() {
+#pragma unroll
+        for (int q = 0; q < kItems; ++q) v[q] = items.i[q] >= 0 && kept.has(items.x[q], items.i[q]) ? items.w[q] : 0;
+        x.block_scan((v[0] + v[1]) + (v[2] + v[3]), s.scan, total);
+      };
+      static_assert(kItems == 4, "the sum above");
+      if (by_p) {
+        weigh();
+        x.template list_cut<true>(items, kept, max(floor, x.key(kept.value)), top, sample_share(top_p, total));
+      }
+      if (least > kept.value) kept = Prefix{least, INT_MAX};
+      weigh();
+      const int i = x.list_nth(items, v, sample_point(u, total) + 1);
+#pragma unroll
+      for (int q = 0; q < kItems; ++q)
+        if (items.i[q] == i && i >= 0) x.put(i, items.x[q], total);
+      return;
+    }
+  }
+
   if (by_k || by_p) {
+    x.bins = make_bins(sample_depth(m, low, x.c));
     x.count(by_k ? top_k : 0, top_p);
     const bool cut_k = by_k && s.k_bin < kBins;
     // where top-k's bin and top-p's bins begin and end, a bound a warp
@@ -702,8 +961,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       const uint32_t lo = max(p_lo, x.key(kept.value)), hi = p_hi;
       const float f_lo = order_value(lo), f_hi = x.up_to(hi);
       const int shift = x.shift_of(lo, hi);
+      const bool list = s.n_last - s.n_first <= kList;
       uint64_t all = 0;
-      x.clear();
+      if (!list) {
+        x.clear();
+      } else {
+        if (tid == 0) s.listed = 0;  // of top-k's, too long a list
+        __syncthreads();
+      }
       Hist& h = s.hist[x.level & 1];
       x.sweep4([&](int i, const float(&v)[4]) {
         uint64_t w[4];
@@ -715,15 +980,52 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           sum += v[j] > f_hi ? w[j] : 0;
           within |= v[j] >= f_lo && v[j] <= f_hi;
         }
-        if (within)
+        if (!within) return;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (v[j] >= f_lo && v[j] <= f_hi && w[j] != 0) x.template add<true>(h, (hi - x.key(v[j])) >> shift, w[j]);
+        for (int j = 0; j < 4; ++j) {
+          if (!(v[j] >= f_lo && v[j] <= f_hi) || w[j] == 0) continue;
+          if (list)
+            x.push(v[j], i + j);
+          else
+            x.template add<true>(h, (hi - x.key(v[j])) >> shift, w[j]);
+        }
       });
       const uint64_t above = warp_sum(sum);
       all = warp_sum(all);
       if (lane == 0) s.part[warp] = above, s.rest[warp] = all;
       x.sync();
+      if (list) {
+        if (rank == 0) {
+          typename R::Items items;
+          x.take(items);
+          const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
+          x.template list_cut<true>(items, kept, lo, hi, share > over ? share - over : 1);
+          if (least > kept.value) kept = Prefix{least, INT_MAX};
+          // what is kept of the list goes to the sums of the warps that have it
+          if (tid < kMaxCtas * kWarps) s.chunk[tid] = tid < C * kWarps ? ld_cluster(&s.part[tid % kWarps], tid / kWarps) : 0;
+          __syncthreads();
+#pragma unroll
+          for (int q = 0; q < kItems; ++q) {
+            if (items.i[q] < 0 || !kept.has(items.x[q], items.i[q])) continue;
+            const int g = (items.i[q] + head) / G::N, of = g / per;
+            atomicAdd(reinterpret_cast<unsigned long long*>(&s.chunk[of * kWarps + (g - of * per) / per_warp]),
+                      static_cast<unsigned long long>(items.w[q]));
+          }
+          __syncthreads();
+          uint64_t v[4], left;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = s.chunk[4 * lane + j];
+          const uint64_t total = warp_sum((v[0] + v[1]) + (v[2] + v[3]));
+          left = sample_point(u, total) + 1;
+          const int owner = x.owner_of(v, left);
+          if (tid == 0) s.owner = owner, s.want = left, s.total = total, s.value = kept.value, s.last = kept.index;
+        }
+        x.sync();
+        kept = Prefix{ld_cluster(&s.value, 0), ld_cluster(&s.last, 0)};
+        x.draw(kept, ld_cluster(&s.owner, 0), ld_cluster(&s.want, 0), ld_cluster(&s.total, 0));
+        x.sync();
+        return;
+      }
       const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
       x.template refine<true>(kept, lo, hi, share > over ? share - over : 1, true);
       if (least > kept.value) kept = Prefix{least, INT_MAX};
@@ -747,34 +1049,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   sum = warp_sum(sum);
   if (lane == 0) s.count[warp] = sum;
   x.sync();
-  uint64_t before = 0, total = 0;
-#pragma unroll
-  for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
-    const int i = j * 32 + lane;
-    if (i >= C * kWarps) continue;
-    const uint64_t v = ld_cluster(&s.count[i % kWarps], i / kWarps);
-    if (i < rank * kWarps + warp) before += v;
-    total += v;
-  }
-  before = warp_sum(before);
-  total = warp_sum(total);
-  auto kept_weight = [&](int i, float v) -> uint64_t { return kept.has(v, i) ? x.weight(v) : 0; };
-  const uint64_t at = sample_point(u, total);
-  if (before <= at && at < before + sum) {
-    const int i = x.nth(at - before + 1, kept_weight);
-    if (lane == 0) {
-      float v[G::N];
-      G::get(x.fetch((i + head) / G::N), v);
-      float l = 0.f;
-#pragma unroll
-      for (int j = 0; j < G::N; ++j)
-        if (j == (i + head) % G::N) l = v[j];
-      p.token[r] = i;
-      const SampleTerm w = sample_term(m, l, x.c, s.table);
-      const double one = __hiloint2double((1023 - 30 - w.k + p.shift) << 20, 0);  // 2^(shift - 30 - k)
-      p.prob[r] = static_cast<float>(static_cast<double>(w.w) * one / static_cast<double>(total));
-    }
-  }
+  uint64_t v[4];
+  x.load4(s.count, v);
+  const uint64_t total = warp_sum((v[0] + v[1]) + (v[2] + v[3]));
+  uint64_t left = sample_point(u, total) + 1;
+  const int owner = x.owner_of(v, left);
+  x.draw(kept, owner, left, total);
   x.sync();
 }
 
@@ -800,7 +1080,14 @@ cudaError_t sample_configure() {
 cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   const long long size = p.dtype == EBD_LOGITS_F32 ? 4 : 2;
   const long long bytes = p.vocab * size + 32;  // both ends rounded out
-  for (int j = 0; j < kSampleTable; ++j) p.table[j] = sample_entry(j);
+  struct Table {
+    uint32_t v[kSampleTable];
+    Table() {
+      for (int j = 0; j < kSampleTable; ++j) v[j] = sample_entry(j);
+    }
+  };
+  static const Table table;
+  std::memcpy(p.table, table.v, sizeof(p.table));
   p.ctas = 1;
   while (p.ctas < kMaxCtas && bytes / p.ctas > 32 * 1024) p.ctas *= 2;
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
@@ -811,13 +1098,15 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.dynamicSmemBytes = p.resident ? static_cast<size_t>(slice) : 0;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = static_cast<unsigned>(p.ctas);
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, sample_kernel_of(p.dtype, p.resident != 0), p);
 }
 
