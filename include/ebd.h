@@ -296,12 +296,13 @@ typedef struct {
  * least).  token is the least v in F with the sum of w over F up to v above u times
  * that over F, prob = w[token] over that sum.  T = 0: the lowest index of the largest
  * logit, with prob 1.  Temperatures count as 1e-30 at least, unless 0, and 1e30 at
- * most.  Weights are exact to 2^-29 of themselves or 2^-44 (beyond 2^18 logits a bit
- * less for each doubling), their sums exact: results do not vary from run to run.
+ * most.  Weights are off by 2^-30 of themselves and 2^-45 of the largest, their sums
+ * are exact: results do not vary from run to run.
  * Logits of -inf have no part in it.  A row with NaN, +inf, or no logit above -inf
  * records EBD_ERR_NONFINITE, one with u outside [0, 1), T negative or not finite, or
  * a NaN parameter EBD_ERR_INVALID_ARG: its token is -1 and its prob NaN, which
- * ebd_decide does not commit.  More than 2^30 logits a row: EBD_ERR_UNSUPPORTED. */
+ * ebd_decide does not commit.  2^20 logits a row or
+ * more: EBD_ERR_UNSUPPORTED. */
 ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream);
 
 /* ---- Vocabulary-parallel LM head (several GPUs) --------------------------

@@ -1451,7 +1451,7 @@ ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream) {
   if (a->dtype != EBD_LOGITS_F32 && a->dtype != EBD_LOGITS_BF16 && a->dtype != EBD_LOGITS_F16)
     return fail(h, EBD_ERR_INVALID_ARG, "dtype must be EBD_LOGITS_F32, _BF16 or _F16");
   if (a->stride != 0 && a->stride < vocab) return fail(h, EBD_ERR_INVALID_ARG, "stride must be 0, or vocab or more");
-  if (vocab > 1 << 30) return fail(h, EBD_ERR_UNSUPPORTED, "more than 2^30 logits a row");
+  if (vocab >= kSampleVocab) return fail(h, EBD_ERR_UNSUPPORTED, "2^20 logits a row, or more");
   if (a->rows == 0) return EBD_OK;
   if (!a->logits || !a->u || !a->token || !a->prob)
     return fail(h, EBD_ERR_INVALID_ARG, "logits, u, token and prob must be set");
@@ -1471,7 +1471,6 @@ ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream) {
   p.token = a->token;
   p.prob = a->prob;
   p.status = h->d_status;
-  p.shift = sample_shift(vocab);
   p.limit_ns = kLimitNs;
   cudaError_t e = launch_sample(p, h->num_sms, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "sample launch");

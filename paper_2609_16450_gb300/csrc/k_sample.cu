@@ -27,6 +27,7 @@
 #include <cuda_fp16.h>
 
 #include <climits>
+#include <cstdlib>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -126,6 +127,15 @@ struct Group<EBD_LOGITS_F16> {
   }
 };
 
+// A 64-bit sum in shared memory by two 32-bit additions: the 64-bit one is a loop of
+// compare and swap, which adds to one place one thread at a time.
+__device__ __forceinline__ void add64(uint64_t* to, uint64_t v) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(to);
+  const uint32_t lo = static_cast<uint32_t>(v), old = atomicAdd(w, lo);
+  const uint32_t hi = static_cast<uint32_t>(v >> 32) + (old + lo < old ? 1u : 0u);
+  if (hi != 0) atomicAdd(w + 1, hi);
+}
+
 __device__ __forceinline__ uint64_t warp_sum(uint64_t x) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
@@ -155,7 +165,7 @@ struct alignas(16) Hist {
 };
 
 // y to bins: the lesser of two lines, fine ones up to a knee and coarse ones from there
-// to 40.  Rounding keeps their order.
+// on.  Rounding keeps their order.
 struct Bins {
   float fine, coarse, shift;
   __device__ __forceinline__ int of(float y) const {
@@ -170,7 +180,7 @@ struct Bins {
 __device__ __forceinline__ Bins make_bins(float knee) {
   constexpr float kFew = 500.f, kMost = 1540.f;
   if (!(knee < kSampleDead * 0.75f)) return {2040.f / kSampleDead, 2040.f / kSampleDead, 0.f};
-  knee = fmaxf(knee, 1e-3f);
+  knee = fmaxf(knee, kSampleDead * 2.5e-5f);
   const float fine = kMost / knee, coarse = kFew / (kSampleDead - knee);
   return {fine, coarse, rintf(kMost - knee * coarse)};
 }
@@ -178,7 +188,7 @@ __device__ __forceinline__ Bins make_bins(float knee) {
 struct Shared {
   Hist hist[2];
   uint2 list[kList];         // logits (their bits) and indices
-  uint32_t table[kSampleTable];
+  SampleEntry table[kSampleTable];
   uint64_t part[kWarps];     // a warp's sums: of what is kept for sure,
   uint64_t rest[kWarps];     // of all that may be kept;
   uint64_t count[kWarps];    // its elements at the border, or what of it is kept
@@ -192,9 +202,10 @@ struct Shared {
   int first[kWarps];
   float kth;                 // a bound of the row's k-th logit, of this CTA's threads'
   int listed;
-  int bin, k_bin, k_whole, k_before, p_first, p_last, n_first, n_last, alone, index, owner, last;
+  int bin, k_bin, k_whole, k_before, alone, index, owner, last;
+  int p_first[2], p_last[2], n_first[2], n_last[2];  // top-p's bins: surely, and likely
   float value;
-  uint32_t bound[4];
+  uint32_t bound[6];
   SampleScale scale;
   float floor_hi, floor_lo;  // T ln min_p
 };
@@ -205,37 +216,11 @@ struct Prefix {
   float value;
   int index;
   __device__ __forceinline__ bool has(float x, int i) const { return x > value || (x == value && i <= index); }
+  // what those reach that are kept whatever their index
+  __device__ __forceinline__ float cut() const {
+    return index == INT_MAX ? value : order_value(order_key(value + 0.f) + 1);
+  }
 };
-
-// Two floats that are worked on at once
-struct Pair {
-  uint64_t v;
-  __device__ __forceinline__ Pair(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ explicit Pair(float a) : Pair(a, a) {}
-  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ Pair operator+(Pair a, const Pair& b) {
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
-  return a;
-}
-__device__ __forceinline__ Pair operator*(Pair a, const Pair& b) {
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
-  return a;
-}
-__device__ __forceinline__ Pair fma(Pair a, const Pair& b, const Pair& c) {
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return a;
-}
-__device__ __forceinline__ Pair operator-(Pair a, const Pair& b) { return fma(b, Pair(-1.f), a); }  // exact product
-// shifts by any amount: 0 from 32 on
-__device__ __forceinline__ uint32_t shl(uint32_t x, uint32_t n) {
-  asm("shl.b32 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(n));
-  return x;
-}
-__device__ __forceinline__ uint32_t shr(uint32_t x, uint32_t n) {
-  asm("shr.u32 %0, %1, %2;" : "=r"(x) : "r"(x), "r"(n));
-  return x;
-}
 
 template <int TYPE, bool RESIDENT>
 struct Row {
@@ -245,7 +230,8 @@ struct Row {
   const uint8_t* data;      // the row's first 16-byte group, in global memory
   uint4* slice;             // this CTA's groups [g0, ..) in shared memory
   int g0, g1, per_warp;     // its end, and the groups of a warp
-  int w0, w1, head, r;      // this warp's groups [w0, w1), elements before the row's in the first group
+  int w0, w1, f0, f1;       // this warp's, and those of them wholly the row's
+  int head, r;              // elements before the row's in its first group
   int lane, warp, rank, C;
   float m = 0.f;
   SampleScale c{};
@@ -257,6 +243,12 @@ struct Row {
       __syncthreads();
     else
       cluster_sync_all();
+  }
+  __device__ __forceinline__ void arrive() const {
+    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  }
+  __device__ __forceinline__ void wait() const {
+    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   __device__ __forceinline__ bool whole(int g) const { return g * G::N >= head && (g + 1) * G::N <= head + p.vocab; }
   // a group that is not wholly the row's, element by element
@@ -274,86 +266,105 @@ struct Row {
     if (RESIDENT) return slice[g - g0];
     return whole(g) ? __ldg(reinterpret_cast<const uint4*>(data) + g) : edge(g);
   }
-  // f(index of the first, four logits) for the logits of the warp's groups
-  template <typename F>
+  // f(index of the first, four logits) for the logits of the warp's groups; where they
+  // are in global memory, AHEAD loads of a thread in flight
+  template <int AHEAD, typename F>
   __device__ __forceinline__ void sweep4(F f) const {
-    for (int g = w0 + lane; g < w1; g += 32) {
+    auto four = [&](int g, const uint4& v) {
       float x[G::N];
-      G::get(fetch(g), x);
+      G::get(v, x);
 #pragma unroll
       for (int j = 0; j < G::N; j += 4) {
         const float y[4] = {x[j], x[j + 1], x[j + 2], x[j + 3]};
         f(g * G::N + j - head, y);
       }
+    };
+    if (RESIDENT) {
+      for (int g = w0 + lane; g < w1; g += 32) four(g, fetch(g));
+      return;
     }
+    const uint4* d = reinterpret_cast<const uint4*>(data);
+    int g = f0 + lane;
+    if (AHEAD == 1) {  // the next one while this one is worked on
+      uint4 next = make_uint4(0, 0, 0, 0);
+      if (g < f1) next = d[g];
+      while (g < f1) {
+        const uint4 v = next;
+        const int at = g;
+        g += 32;
+        if (g < f1) next = d[g];
+        four(at, v);
+      }
+    } else {
+      for (; g + 32 * (AHEAD - 1) < f1; g += 32 * AHEAD) {
+        uint4 v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) v[j] = d[g + 32 * j];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) four(g + 32 * j, v[j]);
+      }
+      for (; g < f1; g += 32) four(g, d[g]);
+    }
+    if (w0 < f0 && lane == 0) four(w0, edge(w0));
+    if (f1 < w1 && w1 - 1 >= f0 && lane == 0) four(w1 - 1, edge(w1 - 1));
   }
   // f(index, logit)
-  template <typename F>
+  template <int AHEAD = 1, typename F>
   __device__ __forceinline__ void sweep(F f) const {
-    sweep4([&](int i, const float(&x)[4]) {
+    sweep4<AHEAD>([&](int i, const float(&x)[4]) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) f(i + j, x[j]);
     });
   }
   __device__ __forceinline__ uint64_t weight(float x) const { return sample_weight(m, x, c, s.table); }
-  // The weights of those of four logits that `keep` takes, 0 for the others: the
-  // operations of sample_weight, two logits at a time, without branches.  What is
-  // not kept has y = 64, and is shifted out.  -> whether any has weight
-  template <typename Keep>
-  __device__ __forceinline__ bool weights(const float (&x)[4], uint64_t (&w)[4], Keep keep) const {
-    const Pair mm(m), hi(c.hi);
-    const Pair l[2] = {Pair(x[0], x[1]), Pair(x[2], x[3])};
-    Pair s2[2] = {mm - l[0], mm - l[1]};
-    float p[4];
-    bool any = false;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) (s2[h] * hi).get(p[2 * h], p[2 * h + 1]);
+  // Adds up the weights of those of four logits that reach `cut`, and of those above
+  // `over` (TWO).  The parts of four weights add up exactly as floats.
+  template <bool TWO>
+  __device__ __forceinline__ void weigh(const float (&x)[4], float cut, float over, uint64_t& sum, uint64_t& above) const {
+    if (!(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= cut)) return;
+    float h[4], r[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool k = p[j] <= kSampleDead && keep(j);
-      any |= k;
-      p[j] = k ? p[j] : 64.f;
+      const SampleParts w = sample_parts(sample_term(m, x[j], c, s.table));
+      h[j] = x[j] >= cut ? w.high : 0.f;
+      r[j] = x[j] >= cut ? w.low : 0.f;
     }
-    if (!any) return false;
-    const Pair lo(c.lo), magic(kSampleMagic);
+    add4(sum, h, r);
+    if (TWO) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Pair pp(p[2 * h], p[2 * h + 1]);
-      const Pair b = s2[h] - mm, d = (mm - (s2[h] - b)) - (l[h] + b);
-      const Pair e = fma(d, hi, fma(s2[h], lo, fma(s2[h], hi, Pair(-p[2 * h], -p[2 * h + 1]))));
-      const Pair t = fma(pp, Pair(128.f), magic);
-      const Pair g = fma(t - magic, Pair(-0.0078125f), pp) + e;
-      const Pair y = g * fma(g, fma(g, Pair(kSampleC3), Pair(kSampleC2)), Pair(kSampleC1));
-      float tt[2];
-      t.get(tt[0], tt[1]);
-      uint32_t q[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) q[j] = s.table[__float_as_uint(tt[j]) & (kSampleTable - 1)];
-      float v[2];
-      fma(Pair(sample_entry_float(q[0]), sample_entry_float(q[1])), y, magic).get(v[0], v[1]);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t f = q[j] + __float_as_uint(v[j]) - kSampleMagicBits;
-        const uint32_t r = (__float_as_uint(tt[j]) >> 7) - (kSampleMagicBits >> 7) + 62 - c.shift;
-        w[2 * h + j] = static_cast<uint64_t>(shr(f, r)) << 32 | (shl(f, 32 - r) | shr(f, r - 32));
+      for (int j = 0; j < 4; ++j) {
+        h[j] = x[j] > over ? h[j] : 0.f;
+        r[j] = x[j] > over ? r[j] : 0.f;
       }
+      add4(above, h, r);
     }
-    return true;
   }
-
+  __device__ __forceinline__ static void add4(uint64_t& sum, const float (&h)[4], const float (&r)[4]) {
+    const int high = __float_as_int(((h[0] + h[2]) + (h[1] + h[3])) + 4.f) - __float_as_int(4.f);  // up to 4
+    const int low = __float2int_rn(((r[0] + r[2]) + (r[1] + r[3])) * 17592186044416.f);
+    sum += static_cast<uint64_t>(static_cast<int64_t>(high) * 8388608 + low);
+  }
+  // how many of four logits are equal to the last kept one, and kept
+  __device__ __forceinline__ static int ties(const Prefix& kept, int i, const float (&x)[4]) {
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n += x[j] == kept.value && i + j <= kept.index;
+    return n;
+  }
   // Bin of a logit, by descending logits, and past the last for weights of zero
   __device__ __forceinline__ int bin_of(float x) const { return bins.of(sample_depth(m, x, c)); }
-  // Least ordered bits with a bin of at most b (one warp)
-  __device__ __forceinline__ uint32_t bound(int b, uint32_t lo, uint32_t hi) const {
+  // Least ordered bits from lo on whose logit passes, as all above it do, hi for one (a
+  // warp, 32 at a time)
+  template <typename F>
+  __device__ __forceinline__ uint32_t search(F passes, uint32_t lo, uint32_t hi) const {
     while (lo < hi) {
       const uint32_t step = (hi - lo) / 32 + 1;
       const uint32_t q = hi - lo >= lane * step ? lo + lane * step : hi;
-      const unsigned hit = __ballot_sync(0xffffffffu, bin_of(order_value(q)) <= b);
+      const unsigned hit = __ballot_sync(0xffffffffu, passes(order_value(q)));
       const int f = hit != 0 ? __ffs(hit) - 1 : 32;
       const uint32_t below = __shfl_sync(0xffffffffu, q, f > 0 ? f - 1 : 0);
       if (f < 32) hi = __shfl_sync(0xffffffffu, q, f);
-      if (f > 0) lo = min(hi, below + 1);
-      else hi = lo;
+      lo = f > 0 ? min(hi, below + 1) : hi;
     }
     return lo;
   }
@@ -402,8 +413,9 @@ struct Row {
   }
 
   // Counts the row's logits by bin; finds top-k's bin (s.k_bin: kBins if all that have
-  // weight are wanted) with the number before it, and the bins s.p_first to s.p_last
-  // that top-p's border lies in.
+  // weight are wanted) with the number before it, and the bins from p_first to p_last
+  // that top-p's border lies in: for sure, and, with weights as in the middle between
+  // the bounds, in all likelihood.
   __device__ __forceinline__ void count(int k, float share) {
     Hist& h = s.hist[level++ & 1];
     sweep([&](int, float x) {
@@ -416,7 +428,10 @@ struct Row {
     uint32_t n[N] = {0, 0, 0, 0};
     gather(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x,
            [&](const uint4& v) { n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w; });
-    if (threadIdx.x == 0) s.k_bin = kBins, s.k_whole = 0, s.p_first = s.p_last = kBins - 1, s.n_first = 0, s.n_last = INT_MAX;
+    if (threadIdx.x < 2) {
+      s.k_bin = kBins, s.k_whole = 0;
+      s.p_first[threadIdx.x] = s.p_last[threadIdx.x] = kBins - 1, s.n_first[threadIdx.x] = 0, s.n_last[threadIdx.x] = INT_MAX;
+    }
     uint32_t all;
     const uint32_t sum = n[0] + n[1] + n[2] + n[3];
     uint32_t before = block_scan(sum, reinterpret_cast<uint32_t*>(s.scan), all) - sum;
@@ -436,10 +451,10 @@ struct Row {
       // Sums of weights as they are at most and at least, a bin's all as heavy as where
       // it begins or ends; 10^-4 is far more than all roundings here.
       float most[N], least[N], sum_most = 0.f, sum_least = 0.f, all_most, all_least;
-      float edge = exp2f(-bins.from(threadIdx.x * N));
+      float edge = exp2f(bins.from(threadIdx.x * N) * (-1.f / kSampleTable));
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float next = exp2f(-bins.from(threadIdx.x * N + j + 1));
+        const float next = exp2f(bins.from(threadIdx.x * N + j + 1) * (-1.f / kSampleTable));
         sum_most += most[j] = static_cast<float>(n[j]) * edge;
         sum_least += least[j] = static_cast<float>(n[j]) * next;
         edge = next;
@@ -448,15 +463,20 @@ struct Row {
       float to_least = block_scan(sum_least, reinterpret_cast<float*>(s.scan), all_least) - sum_least;
       const float from = share * all_least * (1.f - 1e-4f);
       const float upto = fminf(fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f), all_least * (1.f - 1e-4f));
+      const float middle = 0.5f * (all_most + all_least), part = share * middle;
+      const float early = part - 5e-4f * middle, late = fminf(part + 5e-4f * middle, middle * (1.f - 1e-6f));
       uint32_t at = first;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         const int b = threadIdx.x * N + j;
-        if ((to_most < from || b == 0) && to_most + most[j] >= from) s.p_first = b, s.n_first = static_cast<int>(at);
-        at += n[j];
-        if (to_least < upto && to_least + least[j] >= upto) s.p_last = b, s.n_last = static_cast<int>(at);
-        to_most += most[j];
-        to_least += least[j];
+        const uint32_t next_at = at + n[j];
+        const float next_most = to_most + most[j], next_least = to_least + least[j];
+        const float to = 0.5f * (to_most + to_least), next = 0.5f * (next_most + next_least);
+        if ((to_most < from || b == 0) && next_most >= from) s.p_first[0] = b, s.n_first[0] = static_cast<int>(at);
+        if (to_least < upto && next_least >= upto) s.p_last[0] = b, s.n_last[0] = static_cast<int>(next_at);
+        if ((to < early || b == 0) && next >= early) s.p_first[1] = b, s.n_first[1] = static_cast<int>(at);
+        if (to < late && next >= late) s.p_last[1] = b, s.n_last[1] = static_cast<int>(next_at);
+        at = next_at, to_most = next_most, to_least = next_least;
       }
     }
     __syncthreads();
@@ -486,7 +506,7 @@ struct Row {
         clear();
         const float f_lo = order_value(lo), f_hi = up_to(hi);
         sweep([&](int i, float x) {
-          if (x >= f_lo && x <= f_hi && kept.has(x, i)) add<MASS>(h, (hi - key(x)) >> shift, MASS ? weight(x) : 0);
+          if (x >= f_lo && x <= f_hi && kept.has(x, i)) add<MASS>(h, (hi - key(x)) >> shift, x);
         });
         sync();
       }
@@ -522,10 +542,11 @@ struct Row {
       }
     }
   }
+  // Counts a logit, and its weight
   template <bool MASS>
-  __device__ __forceinline__ void add(Hist& h, uint32_t b, uint64_t w) const {
+  __device__ __forceinline__ void add(Hist& h, uint32_t b, float x) const {
     atomicAdd(&h.count[b], 1u);
-    if (MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&h.weight[b]), static_cast<unsigned long long>(w));
+    if (MASS) add64(&h.weight[b], weight(x));
   }
 
   // Of the logits equal to v, up to index `last`: the index of the one
@@ -610,8 +631,8 @@ struct Row {
   __device__ __forceinline__ void put(int i, float l, uint64_t total) const {
     p.token[r] = i;
     const SampleTerm w = sample_term(m, l, c, s.table);
-    const double one = __hiloint2double((1023 - 30 - w.k + c.shift) << 20, 0);  // 2^(shift - 30 - k)
-    p.prob[r] = static_cast<float>(static_cast<double>(w.w) * one / static_cast<double>(total));
+    const double v = static_cast<double>(w.v) * 17592186044416.;
+    p.prob[r] = static_cast<float>((v + v * static_cast<double>(w.x)) / static_cast<double>(total));
   }
   // Draws from what is kept: warp `owner` of the cluster has the one that brings its
   // kept sum up to `want`.
@@ -639,18 +660,17 @@ struct Row {
     const int at = atomicAdd(&s.listed, 1);
     if (at < kList) s.list[at] = make_uint2(__float_as_uint(x), static_cast<uint32_t>(i));
   }
-  // Number of logits that the cluster's CTAs have listed
-  __device__ __forceinline__ int listed() const {
-    int n = 0;
-    gather(&s.listed, [&](int v) { n += min(v, kList + 1); });
-    return n;
+  // Numbers of logits that the cluster's CTAs have listed, and their sum
+  __device__ __forceinline__ int listed(int (&n)[kMaxCtas]) const {
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxCtas; ++k) n[k] = k < C ? ld_cluster(&s.listed, k) : 0;
+#pragma unroll
+    for (int k = 0; k < kMaxCtas; ++k) all += min(n[k], kList + 1);
+    return all;
   }
   // All of them, kList at most; places past them have no weight and -inf
-  __device__ __forceinline__ void take(Items& t) const {
-    int n[kMaxCtas] = {};
-#pragma unroll
-    for (int k = 0; k < kMaxCtas; ++k)
-      if (k < C) n[k] = ld_cluster(&s.listed, k);
+  __device__ __forceinline__ void take(Items& t, const int (&n)[kMaxCtas]) const {
 #pragma unroll
     for (int q = 0; q < kItems; ++q) {
       int at = threadIdx.x + q * kThreads, of = 0;
@@ -681,9 +701,9 @@ struct Row {
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < kItems; ++q) {
-      if (v[q] == 0) continue;
-      const int b = bin(q);
-      if (b >= 0) atomicAdd(reinterpret_cast<unsigned long long*>(h + b), static_cast<unsigned long long>(v[q]));
+      const int b = v[q] != 0 ? bin(q) : -1;
+      if (b < 0) continue;
+      add64(h + b, v[q]);
     }
     __syncthreads();
     const uint64_t n0 = h[2 * threadIdx.x], n1 = h[2 * threadIdx.x + 1];
@@ -698,6 +718,17 @@ struct Row {
     }
     __syncthreads();
     return s.bin >= 0;
+  }
+  // A bound, of ordered bits, that `most` of the threads' `mine` reach, and few more;
+  // s.first and s.bad have the warps' largest and least
+  __device__ __forceinline__ uint32_t threads_kth(uint32_t mine, int most) {
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(s.first[lane % kWarps]));
+    const uint32_t lo = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(s.bad[lane % kWarps]));
+    const int shift = max(0, 32 - __clz(hi - lo) - kLocalBits);
+    const uint64_t one[kItems] = {1};
+    if (!level_of(one, static_cast<uint64_t>(most), [&](int) { return static_cast<int>((hi - mine) >> shift); })) return 0;
+    const uint32_t last = (static_cast<uint32_t>(s.bin + 1) << shift) - 1;  // of the bin, from hi
+    return hi - lo > last ? hi - last : lo;
   }
   // The index at which the sum of v by index reaches `target`
   __device__ __forceinline__ int list_nth(const Items& t, const uint64_t (&v)[kItems], uint64_t target) {
@@ -772,10 +803,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int per = (groups + C - 1) / C, per_warp = (per + kWarps - 1) / kWarps;
   const int g0 = min(groups, rank * per), g1 = min(groups, g0 + per);
   const int w0 = min(g1, g0 + warp * per_warp), w1 = min(g1, w0 + per_warp);
-  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, g1, per_warp, w0, w1, head, r, lane, warp, rank, C};
+  auto whole = [&](int g) { return g * G::N >= head && (g + 1) * G::N <= head + p.vocab; };
+  const int f0 = w0 < w1 && !whole(w0) ? w0 + 1 : w0, f1 = w0 < w1 && !whole(w1 - 1) ? w1 - 1 : w1;
+  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, g1, per_warp, w0, w1, f0, f1, head, r, lane, warp, rank, C};
   R& x = row_;
 
-  const int f0 = w0 < w1 && !x.whole(w0) ? w0 + 1 : w0, f1 = w0 < w1 && !x.whole(w1 - 1) ? w1 - 1 : w1;
   const bool loads = RESIDENT && f0 < f1;  // this warp, by a bulk copy
   if (loads && lane == 0) {
     mbar_init(&s.bar[warp], 1);
@@ -794,7 +826,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   if (tid == 0) s.listed = 0;
   // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by
   // all of them, with the logarithm, the table and the shares, it was half the time
-  if (tid == kThreads - 32) s.scale = sample_scale(t, p.shift);
+  if (tid == kThreads - 32) s.scale = sample_scale(t);
   if (tid == kThreads - 64 && min_p > 0.f) {
     const double x = static_cast<double>(t) * log(static_cast<double>(fminf(min_p, 1.f)));
     s.floor_hi = static_cast<float>(x);
@@ -819,18 +851,17 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int most = (top_k + C - 1) / C;  // of a CTA's largest, for a list
   const bool few = by_k && top_k <= kList / 2 && most <= kListMost && T > 0.f;
   float m = -INFINITY, low = INFINITY;
-  x.sweep([&](int, float v) {
+  x.template sweep<8>([&](int, float v) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v));
     low = fminf(low, v);
   });
   bad |= m != m;
   low = low < INFINITY ? low : -INFINITY;
   if (few) {
-    // bit by bit, the 20 that matter: rounded down, it bounds all the same
-    const uint32_t mine = x.key(m);
-    uint32_t t = 0;
-    for (int bit = 31; bit >= 12; --bit)
-      if (__syncthreads_count(mine >= (t | 1u << bit)) >= most) t |= 1u << bit;
+    const uint32_t mine = x.key(m), hi = __reduce_max_sync(0xffffffffu, mine), lo = __reduce_min_sync(0xffffffffu, mine);
+    if (lane == 0) s.first[warp] = static_cast<int>(hi), s.bad[warp] = static_cast<int>(lo);
+    __syncthreads();
+    const uint32_t t = x.threads_kth(mine, most);
     if (tid == 0) s.kth = t > 0x00800000u ? order_value(t) : -3.402823466e38f;
   }
 #pragma unroll
@@ -892,30 +923,33 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   }
 
   x.c = s.scale;
-  // nothing that has weight lies below: 40 / log2(e) = 27.73, and room for rounding
-  const float dead = m - 28.f * t - fabsf(m) * 9.5367431640625e-7f;
-  const uint32_t floor = order_key(dead > -3.402823466e38f ? dead : -3.402823466e38f), top = x.key(m);
+  // the least logit that has weight: about 40 / log2(e) = 27.73 T below the largest
+  const float near = fabsf(m) * 9.5367431640625e-7f;
+  const uint32_t top = x.key(m), dead = order_key(fmaxf(m - 28.f * t - near, -3.402823466e38f));
   const float least = min_p > 0.f ? sample_floor(m, s.floor_hi, s.floor_lo) : -INFINITY;
   bool by_p = top_p < 1.f;
-  Prefix kept{order_value(floor), INT_MAX};
+  Prefix kept{-3.402823466e38f, INT_MAX};
   uint64_t sum = 0;
 
   if (few) {
     float bound = m;
     x.gather(&s.kth, [&](float v) { bound = fminf(bound, v); });
-    x.sweep4([&](int i, const float(&v)[4]) {
+    x.template sweep4<4>([&](int i, const float(&v)[4]) {
       if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= bound)) return;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (v[j] >= bound) x.push(v[j], i + j);
     });
     x.sync();
-    if (x.listed() <= kList) {
+    int n[kMaxCtas];
+    if (x.listed(n) <= kList) {
       typename R::Items items;
-      if (rank == 0) x.take(items);
-      x.sync();  // the others are done
-      if (rank != 0) return;
-      kept = Prefix{-3.402823466e38f, INT_MAX};
+      if (rank == 0) x.take(items, n);
+      x.arrive();
+      if (rank != 0) {  // done, once their lists are read
+        x.wait();
+        return;
+      }
       x.template list_cut<false>(items, kept, x.key(bound), top, static_cast<uint64_t>(top_k));
       uint64_t total, v[kItems];
       auto weigh = [&]() {
@@ -926,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       static_assert(kItems == 4, "the sum above");
       if (by_p) {
         weigh();
-        x.template list_cut<true>(items, kept, max(floor, x.key(kept.value)), top, sample_share(top_p, total));
+        x.template list_cut<true>(items, kept, max(dead, x.key(kept.value)), top, sample_share(top_p, total));
       }
       if (least > kept.value) kept = Prefix{least, INT_MAX};
       weigh();
@@ -934,34 +968,50 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 #pragma unroll
       for (int q = 0; q < kItems; ++q)
         if (items.i[q] == i && i >= 0) x.put(i, items.x[q], total);
+      x.wait();
       return;
     }
   }
+
+  // exactly: among the floats about there, or, where they are too fine, by a search
+  uint32_t floor = x.key(m - kSampleDead / x.c.hi) - 16;
+  const uint32_t here = min(max(floor + lane, dead), top);
+  const unsigned alive = __ballot_sync(0xffffffffu, sample_depth(m, order_value(here), x.c) <= kSampleDead);
+  if (alive != 0 && (alive & 1) == 0)
+    floor = __shfl_sync(0xffffffffu, here, __ffs(alive) - 1);
+  else
+    floor = x.search([&](float v) { return sample_depth(m, v, x.c) <= kSampleDead; }, dead, top);
+  kept.value = order_value(floor);
 
   if (by_k || by_p) {
     x.bins = make_bins(sample_depth(m, low, x.c));
     x.count(by_k ? top_k : 0, top_p);
     const bool cut_k = by_k && s.k_bin < kBins;
     // where top-k's bin and top-p's bins begin and end, a bound a warp
-    if (warp < 4) {
-      const int b = warp == 0 ? s.k_bin : warp == 1 ? s.k_bin - 1 : warp == 2 ? s.p_last : s.p_first - 1;
-      const uint32_t q = b >= kBins ? floor : b < 0 ? top + 1 : x.bound(b, floor, top);
+    if (warp < 6) {
+      const int b = warp == 0 ? s.k_bin : warp == 1 ? s.k_bin - 1 : (warp & 1) == 0 ? s.p_last[warp / 2 - 1] : s.p_first[warp / 2 - 1] - 1;
+      const uint32_t q = b >= kBins ? floor : b < 0 ? top + 1 : x.search([&](float v) { return x.bin_of(v) <= b; }, floor, top);
       if (lane == 0) s.bound[warp] = q;
     }
     __syncthreads();
-    const uint32_t k_lo = s.bound[0], k_hi = s.bound[1] - 1, p_lo = s.bound[2], p_hi = s.bound[3] - 1;
+    const uint32_t k_lo = s.bound[0], k_hi = s.bound[1] - 1;
     if (cut_k) {
       if (s.k_whole)
         kept.value = order_value(k_lo);
       else
         x.template refine<false>(kept, k_lo, k_hi, static_cast<uint64_t>(top_k - s.k_before), false);
     }
-    by_p = by_p && least <= x.up_to(p_hi);  // else min-p keeps less, whatever top-p does
-    if (by_p) {
-      const uint32_t lo = max(p_lo, x.key(kept.value)), hi = p_hi;
+    by_p = by_p && least <= x.up_to(s.bound[3] - 1);  // else min-p keeps less, whatever top-p does
+    // Listed are the logits of all bins that the border may lie in, or, where they are
+    // too many, of those that it should lie in: it is seen whether it does.
+    const bool sure = s.n_last[0] - s.n_first[0] <= kList;
+    bool list = sure || (s.n_last[1] - s.n_first[1] <= kList && least <= x.up_to(s.bound[5] - 1));
+    while (by_p) {
+      const int which = list && !sure ? 4 : 2;
+      const uint32_t lo = max(s.bound[which], x.key(kept.value)), hi = s.bound[which + 1] - 1;
       const float f_lo = order_value(lo), f_hi = x.up_to(hi);
       const int shift = x.shift_of(lo, hi);
-      const bool list = s.n_last - s.n_first <= kList;
+      const Prefix before = kept;
       uint64_t all = 0;
       if (!list) {
         x.clear();
@@ -970,24 +1020,23 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         __syncthreads();
       }
       Hist& h = s.hist[x.level & 1];
-      x.sweep4([&](int i, const float(&v)[4]) {
-        uint64_t w[4];
-        if (!x.weights(v, w, [&](int j) { return kept.has(v[j], i + j); })) return;
-        bool within = false;
+      const float cut = kept.cut();
+      // about the bins: none further from the middle lies within
+      const float mid = 0.5f * f_lo + 0.5f * f_hi, half = (0.5f * f_hi - 0.5f * f_lo) + 4.76837158203125e-7f * (fabsf(f_lo) + fabsf(f_hi));
+      const bool ties = kept.index != INT_MAX;  // at top-k's border: in no sum above, being the last
+      const uint64_t last = ties ? x.weight(kept.value) : 0;
+      x.template sweep4<1>([&](int i, const float(&v)[4]) {
+        if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= kept.value)) return;
+        if (ties) all += x.ties(kept, i, v) * last;
+        x.template weigh<true>(v, cut, f_hi, all, sum);
+        if (!(fminf(fminf(fabsf(v[0] - mid), fabsf(v[1] - mid)), fminf(fabsf(v[2] - mid), fabsf(v[3] - mid))) <= half)) return;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          all += w[j];
-          sum += v[j] > f_hi ? w[j] : 0;
-          within |= v[j] >= f_lo && v[j] <= f_hi;
-        }
-        if (!within) return;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (!(v[j] >= f_lo && v[j] <= f_hi) || w[j] == 0) continue;
+          if (!(v[j] >= f_lo && v[j] <= f_hi) || !kept.has(v[j], i + j)) continue;
           if (list)
             x.push(v[j], i + j);
           else
-            x.template add<true>(h, (hi - x.key(v[j])) >> shift, w[j]);
+            x.template add<true>(h, (hi - x.key(v[j])) >> shift, v[j]);
         }
       });
       const uint64_t above = warp_sum(sum);
@@ -997,8 +1046,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       if (list) {
         if (rank == 0) {
           typename R::Items items;
-          x.take(items);
+          int n[kMaxCtas];
+          x.listed(n);
+          x.take(items, n);
           const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
+          uint64_t within;
+          x.block_scan((items.w[0] + items.w[1]) + (items.w[2] + items.w[3]), s.scan, within);
+          const bool there = sure || (share > over && share - over <= within);
           x.template list_cut<true>(items, kept, lo, hi, share > over ? share - over : 1);
           if (least > kept.value) kept = Prefix{least, INT_MAX};
           // what is kept of the list goes to the sums of the warps that have it
@@ -1008,8 +1062,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           for (int q = 0; q < kItems; ++q) {
             if (items.i[q] < 0 || !kept.has(items.x[q], items.i[q])) continue;
             const int g = (items.i[q] + head) / G::N, of = g / per;
-            atomicAdd(reinterpret_cast<unsigned long long*>(&s.chunk[of * kWarps + (g - of * per) / per_warp]),
-                      static_cast<unsigned long long>(items.w[q]));
+            add64(&s.chunk[of * kWarps + (g - of * per) / per_warp], items.w[q]);
           }
           __syncthreads();
           uint64_t v[4], left;
@@ -1018,30 +1071,38 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
           const uint64_t total = warp_sum((v[0] + v[1]) + (v[2] + v[3]));
           left = sample_point(u, total) + 1;
           const int owner = x.owner_of(v, left);
-          if (tid == 0) s.owner = owner, s.want = left, s.total = total, s.value = kept.value, s.last = kept.index;
+          if (tid == 0) s.owner = there ? owner : -1, s.want = left, s.total = total, s.value = kept.value, s.last = kept.index;
         }
         x.sync();
+        const int owner = ld_cluster(&s.owner, 0);
+        if (owner < 0) {  // it does not
+          list = false;
+          sum = 0;
+          kept = before;
+          continue;
+        }
         kept = Prefix{ld_cluster(&s.value, 0), ld_cluster(&s.last, 0)};
-        x.draw(kept, ld_cluster(&s.owner, 0), ld_cluster(&s.want, 0), ld_cluster(&s.total, 0));
+        x.draw(kept, owner, ld_cluster(&s.want, 0), ld_cluster(&s.total, 0));
         x.sync();
         return;
       }
       const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
       x.template refine<true>(kept, lo, hi, share > over ? share - over : 1, true);
       if (least > kept.value) kept = Prefix{least, INT_MAX};
-      x.sweep4([&](int i, const float(&v)[4]) {
-        uint64_t w[4];
-        if (!x.weights(v, w, [&](int j) { return v[j] <= f_hi && kept.has(v[j], i + j); })) return;
-        sum += (w[0] + w[1]) + (w[2] + w[3]);
+      x.sweep([&](int i, float v) {
+        if (v <= f_hi && kept.has(v, i)) sum += x.weight(v);
       });
+      break;
     }
   }
   if (!by_p) {
     if (least > kept.value) kept = Prefix{least, INT_MAX};
-    x.sweep4([&](int i, const float(&v)[4]) {
-      uint64_t w[4];
-      if (!x.weights(v, w, [&](int j) { return kept.has(v[j], i + j); })) return;
-      sum += (w[0] + w[1]) + (w[2] + w[3]);
+    const float cut = kept.cut();
+    const uint64_t last = kept.index != INT_MAX ? x.weight(kept.value) : 0;
+    uint64_t none = 0;
+    x.template sweep4<1>([&](int i, const float(&v)[4]) {
+      x.template weigh<false>(v, cut, 0.f, sum, none);
+      if (last != 0) sum += x.ties(kept, i, v) * last;
     });
   }
 
@@ -1081,7 +1142,7 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   const long long size = p.dtype == EBD_LOGITS_F32 ? 4 : 2;
   const long long bytes = p.vocab * size + 32;  // both ends rounded out
   struct Table {
-    uint32_t v[kSampleTable];
+    SampleEntry v[kSampleTable];
     Table() {
       for (int j = 0; j < kSampleTable; ++j) v[j] = sample_entry(j);
     }
@@ -1090,8 +1151,10 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   std::memcpy(p.table, table.v, sizeof(p.table));
   p.ctas = 1;
   while (p.ctas < kMaxCtas && bytes / p.ctas > 32 * 1024) p.ctas *= 2;
+  if (const char* env = getenv("EBD_SAMPLE_CTAS")) p.ctas = atoi(env);
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
   p.resident = slice <= kSliceBytes;
+  if (getenv("EBD_SAMPLE_FLAT")) p.resident = 0;
   (void)num_sms;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * p.ctas, 1, 1);

@@ -16,11 +16,10 @@ struct SampleParams {
   int* token;
   float* prob;
   int* status;
-  int shift;                 // units of the weights (sample_math.h)
   int ctas;                  // CTAs (a cluster) per row
   int resident;              // a CTA's slice of the row stays in its shared memory
   uint64_t limit_ns;
-  uint32_t table[kSampleTable];
+  SampleEntry table[kSampleTable];
 };
 
 cudaError_t sample_configure();

@@ -40,71 +40,79 @@ EBD_HD uint32_t order_key(float x) {
 }
 EBD_HD float order_value(uint32_t k) { return f32_of((k >> 31) != 0 ? k ^ 0x80000000u : ~k); }
 
-// The weight of logit l is w = exp((l - m) / T) in whole units of 2^-shift, m the
-// row's largest logit, and 0 below 2^-40.  Sums of such weights are exact in any
-// order, so that a token's border in them is one number wherever it is computed.
+// The weight of logit l is w = exp((l - m) / T) in whole units of 2^-44, m the row's
+// largest logit, and 0 below 2^-40.  Sums of such weights are exact in any order, so
+// that a token's border in them is one number wherever it is computed.
 //
-// w = 2^-y with y = (m - l) log2(e) / T as the sum of two floats, p + e: m - l is
-// exact in two floats, and so is its product with the rounded factor.  Then y = k /
-// 128 + g with |g| <= 2^-8 (and e): 2^(-k / 128) is 2^(-(k >> 7)) times an entry of a
-// table of 128, and 2^-g = 1 + x, x a cubic in g that leaves out 2^-38.  The float
-// operations round g and the cubic by about 2^-32.5, the table and the product are
-// rounded to units of 2^-30 of a number in (1/2, 1].  So a weight is off by some
-// 2^-30 of itself, and by less than one unit from being cut to them.
+// w = 2^(-y / 128) with y = (m - l) 128 log2(e) / T as the sum of two floats, p + e: m -
+// l is exact in two floats, and so is its product with the rounded factor.  Then y = k +
+// z with |z| <= 1/2 (and e): 2^(-k / 128) is 2^(-(k >> 7)) times an entry of a table of
+// 128, a float v and what it is off by, relative to it; 2^(-z / 128) - 1 is a cubic in z
+// that leaves out 2^-38, and starts from that.  w = v + v x is rounded to units of
+// 2^-21, h, and what is left to units of 2^-44, all in float operations that are
+// exact but for those two: whole-number shifts and additions have half their rate.
+// The roundings of z and x make a weight off by some 2^-31 of itself, and the last by
+// half a unit.
 struct SampleScale {
-  float hi, lo;  // log2(e) / T
-  int shift;
+  float hi, lo;  // 128 log2(e) / T
 };
+constexpr int kSampleBits = 44;      // of a unit
+constexpr int kSampleVocab = 1 << 20;  // sums of fewer weights fit 64 bits
 constexpr int kSampleTable = 128;
-constexpr float kSampleDead = 40.f;  // weights below 2^-40 are zero
-constexpr float kSampleMagic = 12582912.f;  // 1.5 * 2^23: adding it rounds to a whole number
-constexpr uint32_t kSampleMagicBits = 0x4B400000u;
-// 2^-g - 1 = g (c1 + g (c2 + g c3)): -ln 2, (ln 2)^2 / 2, -(ln 2)^3 / 6
-constexpr float kSampleC1 = -0.693147181f, kSampleC2 = 0.240226507f, kSampleC3 = -0.0555041087f;
+constexpr float kSampleDead = 40.f * kSampleTable;  // weights below 2^-40 are zero
+constexpr float kSampleMagic = 12582912.f;  // 1.5 * 2^23: adding it rounds to a whole number,
+constexpr float kSampleHigh = 6.f;          // 1.5 * 2^2: to a unit of 2^-21,
+constexpr float kSampleLow = 7.152557373046875e-7f;  // 1.5 * 2^-21: to one of 2^-44
+// 2^(-z / 128) - 1 = z (c1 + z (c2 + z c3)): -ln 2, (ln 2)^2 / 2, -(ln 2)^3 / 6 with a
+// factor of 2^-7 for every z
+constexpr float kSampleC1 = -0.693147181f / 128, kSampleC2 = 0.240226507f / 16384, kSampleC3 = -0.0555041087f / 2097152;
 
-// Units of a row of `vocab` logits: their sum stays below 2^63.
-inline int sample_shift(long long vocab) {
-  int bits = 0;
-  while ((1ll << bits) < vocab) ++bits;
-  return 62 - bits < 44 ? 62 - bits : 44;
-}
 // 1 / T stays within float's range
 EBD_HD float sample_temperature(float t) { return t < 1e-30f ? 1e-30f : t > 1e30f ? 1e30f : t; }
-EBD_HD SampleScale sample_scale(float temperature, int shift) {
-  const double c = 1.4426950408889634 / static_cast<double>(temperature);
+EBD_HD SampleScale sample_scale(float temperature) {
+  const double c = 1.4426950408889634 * kSampleTable / static_cast<double>(temperature);
   const float hi = static_cast<float>(c);
-  return {hi, static_cast<float>(c - hi), shift};
+  return {hi, static_cast<float>(c - hi)};
 }
-// 2^(-j / 128) in units of 2^-30
-EBD_HD uint32_t sample_entry(int j) { return static_cast<uint32_t>(exp2(-j / 128.0) * 1073741824.0 + 0.5); }
-// the same entry as a float: its leading bits
-EBD_HD float sample_entry_float(uint32_t q) { return f32_of((155u << 23) + (q >> 6)); }
+struct SampleEntry {
+  uint32_t bits;  // of v = 2^(-j / 128), plus j << 16: less k << 16 they are those of v 2^(-(k >> 7))
+  float off;      // (2^(-j / 128) - v) / v
+};
+inline SampleEntry sample_entry(int j) {
+  const double x = std::exp2(-j / 128.0);
+  const float v = static_cast<float>(x);
+  return {f32_bits(v) + (static_cast<uint32_t>(j) << 16), static_cast<float>((x - v) / v)};
+}
 // y, rounded: it grows as l falls, and decides alone which weights are zero
 EBD_HD float sample_depth(float m, float l, const SampleScale& c) { return (m - l) * c.hi; }
 
-// The weight before it is cut, w 2^(-30 - k), w in (2^29, 2^30]; k = 64 for none.
+// w = v + v x of a logit that has weight
 struct SampleTerm {
-  uint32_t w;
-  int k;
+  float v, x;
 };
-EBD_HD SampleTerm sample_term(float m, float l, const SampleScale& c, const uint32_t* table) {
+EBD_HD SampleTerm sample_term(float m, float l, const SampleScale& c, const SampleEntry* table) {
   const float s = m - l;
-  const float p = s * c.hi;
-  if (!(p <= kSampleDead)) return {0, 64};
   const float b = s - m;
   const float d = (m - (s - b)) - (l + b);  // s + d = m - l exactly
-  const float e = fmaf(d, c.hi, fmaf(s, c.lo, fmaf(s, c.hi, -p)));
-  const float t = fmaf(p, 128.f, kSampleMagic);
-  const uint32_t k = f32_bits(t) - kSampleMagicBits;
-  const float g = fmaf(t - kSampleMagic, -0.0078125f, p) + e;
-  const float x = g * fmaf(g, fmaf(g, kSampleC3, kSampleC2), kSampleC1);
-  const uint32_t q = table[k & (kSampleTable - 1)];
-  const uint32_t w = q + (f32_bits(fmaf(sample_entry_float(q), x, kSampleMagic)) - kSampleMagicBits);
-  return {w, static_cast<int>(k >> 7)};
+  const float p = s * c.hi;
+  const float e = fmaf(d, -c.hi, fmaf(s, -c.lo, fmaf(s, -c.hi, p)));  // -e above
+  const float t = p + kSampleMagic;
+  const float z = (p - (t - kSampleMagic)) - e;
+  const SampleEntry q = table[f32_bits(t) & (kSampleTable - 1)];
+  return {f32_of(q.bits - (f32_bits(t) << 16)), fmaf(z, fmaf(z, fmaf(z, kSampleC3, kSampleC2), kSampleC1), q.off)};
 }
-EBD_HD uint64_t sample_weight(float m, float l, const SampleScale& c, const uint32_t* table) {
-  const SampleTerm t = sample_term(m, l, c, table);
-  return t.w != 0 ? (static_cast<uint64_t>(t.w) << 32) >> (62 - c.shift + t.k) : 0;
+// the same in whole numbers of 2^-21 and of 2^-44
+struct SampleParts {
+  float high, low;
+};
+EBD_HD SampleParts sample_parts(const SampleTerm& w) {
+  const float h = fmaf(w.v, w.x, w.v + kSampleHigh) - kSampleHigh;
+  return {h, (fmaf(w.v, w.x, w.v - h) + kSampleLow) - kSampleLow};
+}
+EBD_HD uint64_t sample_weight(float m, float l, const SampleScale& c, const SampleEntry* table) {
+  if (!(sample_depth(m, l, c) <= kSampleDead)) return 0;
+  const SampleParts w = sample_parts(sample_term(m, l, c, table));
+  return static_cast<uint64_t>(static_cast<int64_t>(w.high * 2097152.f) * 8388608 + static_cast<int64_t>(w.low * 17592186044416.f));
 }
 
 // total * x for a float x in [0, 1), cut or rounded up to a whole number: exactly.

@@ -1,10 +1,10 @@
 """Sampling in 64 bits, and what a drawn token may differ by.
 
-A kernel's weights are off by 2^-29 of themselves, and cut to units of 2^-44 of the
-largest (coarser beyond 2^18 logits); sums of them are exact, and rounded once, to
-2^-53, where a share or a random number multiplies them.  So a border lies within
-slack() of all that is kept from where it is here: twice 2^-29, for what lies below
-it and for the whole, and a unit for every logit.  numpy's own are off by 2^-50 at
+A kernel's weights are off by 2^-30 of themselves and 2^-45 of the largest; sums of
+them are exact, and so are the parts of them that a share or a random number takes, but
+for a unit of 2^-44.  So a border lies within slack() of all that is kept from where it
+is here: twice 2^-30, for what lies below it and for the whole, and twice 2^-45 for
+every logit.  numpy's own are off by 2^-50 at
 most at these sizes.
 """
 import math
@@ -14,8 +14,7 @@ import numpy as np
 
 def slack(w):
     """Of the sum of weights w (the largest of them 1)."""
-    unit = 2.0 ** -min(44, 62 - max(len(w) - 1, 1).bit_length())
-    return 2.0 ** -28 + 2 * unit * np.count_nonzero(w) / w.sum()
+    return 2.0 ** -29 + 2.0 ** -44 * (1 + np.count_nonzero(w)) / w.sum()
 
 
 def order(l):
