@@ -1472,7 +1472,7 @@ ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream) {
   p.prob = a->prob;
   p.status = h->d_status;
   p.limit_ns = kLimitNs;
-  cudaError_t e = launch_sample(p, h->num_sms, static_cast<cudaStream_t>(stream));
+  cudaError_t e = launch_sample(p, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(h, e, "sample launch");
   return EBD_OK;
 }

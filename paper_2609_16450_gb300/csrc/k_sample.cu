@@ -27,7 +27,7 @@
 #include <cuda_fp16.h>
 
 #include <climits>
-#include <cstdlib>
+#include <cstring>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -207,6 +207,8 @@ struct Shared {
   float value;
   uint32_t bound[6];
   SampleScale scale;
+  Bins bins;
+  int g1, per_warp;            // the end of this CTA's groups, and a warp's of them
   float floor_hi, floor_lo;  // T ln min_p
 };
 
@@ -227,28 +229,38 @@ struct Row {
   using G = Group<TYPE>;
   Shared& s;
   const SampleParams& p;
-  const uint8_t* data;      // the row's first 16-byte group, in global memory
-  uint4* slice;             // this CTA's groups [g0, ..) in shared memory
-  int g0, g1, per_warp;     // its end, and the groups of a warp
-  int w0, w1, f0, f1;       // this warp's, and those of them wholly the row's
-  int head, r;              // elements before the row's in its first group
-  int lane, warp, rank, C;
+  const uint8_t* data;  // the row's first 16-byte group, in global memory
+  int f0, f1;           // this warp's groups that are wholly the row's,
+  int ends;             // and whether one before (1) and one after (2) is so in part
+  int head, g0;         // elements before the row's in its first group; this CTA's first
   float m = 0.f;
   SampleScale c{};
-  Bins bins{};
   int level = 0;
 
+  // What is seldom needed is computed again, or in shared memory: registers are scarce.
+  __device__ __forceinline__ static int lane() { return threadIdx.x & 31; }
+  __device__ __forceinline__ static int warp() { return threadIdx.x >> 5; }
+  __device__ __forceinline__ static int rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return static_cast<int>(r);
+  }
+  __device__ __forceinline__ int ctas() const { return p.ctas; }
+  __device__ __forceinline__ uint4* slice() const {
+    extern __shared__ __align__(16) uint8_t dyn[];
+    return reinterpret_cast<uint4*>(dyn);
+  }
   __device__ __forceinline__ void sync() const {
-    if (C == 1)
+    if (ctas() == 1)
       __syncthreads();
     else
       cluster_sync_all();
   }
   __device__ __forceinline__ void arrive() const {
-    if (C > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (ctas() > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   }
   __device__ __forceinline__ void wait() const {
-    if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (ctas() > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   __device__ __forceinline__ bool whole(int g) const { return g * G::N >= head && (g + 1) * G::N <= head + p.vocab; }
   // a group that is not wholly the row's, element by element
@@ -263,7 +275,7 @@ struct Row {
     return v;
   }
   __device__ __forceinline__ uint4 fetch(int g) const {
-    if (RESIDENT) return slice[g - g0];
+    if (RESIDENT) return slice()[g - g0];
     return whole(g) ? __ldg(reinterpret_cast<const uint4*>(data) + g) : edge(g);
   }
   // f(index of the first, four logits) for the logits of the warp's groups; where they
@@ -280,11 +292,11 @@ struct Row {
       }
     };
     if (RESIDENT) {
-      for (int g = w0 + lane; g < w1; g += 32) four(g, fetch(g));
+      for (int g = f0 - (ends & 1) + lane(); g < f1 + (ends >> 1); g += 32) four(g, fetch(g));
       return;
     }
     const uint4* d = reinterpret_cast<const uint4*>(data);
-    int g = f0 + lane;
+    int g = f0 + lane();
     if (AHEAD == 1) {  // the next one while this one is worked on
       uint4 next = make_uint4(0, 0, 0, 0);
       if (g < f1) next = d[g];
@@ -305,8 +317,8 @@ struct Row {
       }
       for (; g < f1; g += 32) four(g, d[g]);
     }
-    if (w0 < f0 && lane == 0) four(w0, edge(w0));
-    if (f1 < w1 && w1 - 1 >= f0 && lane == 0) four(w1 - 1, edge(w1 - 1));
+    if ((ends & 1) != 0 && lane() == 0) four(f0 - 1, edge(f0 - 1));
+    if ((ends & 2) != 0 && lane() == 0) four(f1, edge(f1));
   }
   // f(index, logit)
   template <int AHEAD = 1, typename F>
@@ -352,14 +364,14 @@ struct Row {
     return n;
   }
   // Bin of a logit, by descending logits, and past the last for weights of zero
-  __device__ __forceinline__ int bin_of(float x) const { return bins.of(sample_depth(m, x, c)); }
+  __device__ __forceinline__ int bin_of(float x) const { return s.bins.of(sample_depth(m, x, c)); }
   // Least ordered bits from lo on whose logit passes, as all above it do, hi for one (a
   // warp, 32 at a time)
   template <typename F>
   __device__ __forceinline__ uint32_t search(F passes, uint32_t lo, uint32_t hi) const {
     while (lo < hi) {
       const uint32_t step = (hi - lo) / 32 + 1;
-      const uint32_t q = hi - lo >= lane * step ? lo + lane * step : hi;
+      const uint32_t q = hi - lo >= lane() * step ? lo + lane() * step : hi;
       const unsigned hit = __ballot_sync(0xffffffffu, passes(order_value(q)));
       const int f = hit != 0 ? __ffs(hit) - 1 : 32;
       const uint32_t below = __shfl_sync(0xffffffffu, q, f > 0 ? f - 1 : 0);
@@ -375,39 +387,43 @@ struct Row {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const T y = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += y;
+      if (lane() >= o) incl += y;
     }
     __syncthreads();
-    if (lane == 31) part[warp] = incl;
+    if (lane() == 31) part[warp()] = incl;
     __syncthreads();
     T before = 0;
     total = 0;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
       const T y = part[i];
-      if (i < warp) before += y;
+      if (i < warp()) before += y;
       total += y;
     }
     return before + incl;
   }
-  // f of what every CTA of the cluster has at p, all loads in flight at once
+  // f of what every CTA of the cluster has at p, four loads in flight at once
   template <typename T, typename F>
   __device__ __forceinline__ void gather(const T* p, F f) const {
-    T v[kMaxCtas];
 #pragma unroll
-    for (int i = 0; i < kMaxCtas; ++i)
-      if (i < C) v[i] = ld_cluster(p, i);
+    for (int b = 0; b < kMaxCtas; b += 4) {
+      if (b >= ctas()) break;
+      T v[4];
 #pragma unroll
-    for (int i = 0; i < kMaxCtas; ++i)
-      if (i < C) f(v[i]);
+      for (int i = 0; i < 4; ++i)
+        if (b + i < ctas()) v[i] = ld_cluster(p, b + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (b + i < ctas()) f(v[i]);
+    }
   }
   // sum over the cluster's warps
   __device__ __forceinline__ uint64_t cluster_sum(const uint64_t* of) const {
     uint64_t v = 0;
 #pragma unroll
     for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
-      const int i = j * 32 + lane;
-      if (i < C * kWarps) v += ld_cluster(of + i % kWarps, i / kWarps);
+      const int i = j * 32 + lane();
+      if (i < ctas() * kWarps) v += ld_cluster(of + i % kWarps, i / kWarps);
     }
     return warp_sum(v);
   }
@@ -418,8 +434,9 @@ struct Row {
   // the bounds, in all likelihood.
   __device__ __forceinline__ void count(int k, float share) {
     Hist& h = s.hist[level++ & 1];
+    const Bins bins = s.bins;
     sweep([&](int, float x) {
-      const int b = bin_of(x);
+      const int b = bins.of(sample_depth(m, x, c));
       if (b < kBins) atomicAdd(&h.coarse[b], 1u);
     });
     sync();
@@ -451,10 +468,10 @@ struct Row {
       // Sums of weights as they are at most and at least, a bin's all as heavy as where
       // it begins or ends; 10^-4 is far more than all roundings here.
       float most[N], least[N], sum_most = 0.f, sum_least = 0.f, all_most, all_least;
-      float edge = exp2f(bins.from(threadIdx.x * N) * (-1.f / kSampleTable));
+      float edge = exp2f(s.bins.from(threadIdx.x * N) * (-1.f / kSampleTable));
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float next = exp2f(bins.from(threadIdx.x * N + j + 1) * (-1.f / kSampleTable));
+        const float next = exp2f(s.bins.from(threadIdx.x * N + j + 1) * (-1.f / kSampleTable));
         sum_most += most[j] = static_cast<float>(n[j]) * edge;
         sum_least += least[j] = static_cast<float>(n[j]) * next;
         edge = next;
@@ -559,12 +576,12 @@ struct Row {
     uint64_t n = 0;
     sweep([&](int i, float x) { n += x == v && i <= last; });
     n = warp_sum(n);
-    if (lane == 0) s.count[warp] = n;
+    if (lane() == 0) s.count[warp()] = n;
     sync();
     uint64_t v4[4], left = take;
     load4(s.count, v4);
     const int at = owner_of(v4, left);  // the warp (of the cluster) that has the last one
-    if (at / kWarps == rank) nth(at % kWarps, left, [&](int i, float x) -> uint64_t { return x == v && i <= last; });
+    if (at / kWarps == rank()) nth(at % kWarps, left, [&](int i, float x) -> uint64_t { return x == v && i <= last; });
     sync();
     // nobody writes s.index again before the next sync() of all
     return ld_cluster(&s.index, at / kWarps);
@@ -574,9 +591,9 @@ struct Row {
   // `want` >= 1, found by all its warps: an iteration of that run each.
   template <typename F>
   __device__ __forceinline__ int nth(int of, uint64_t want, F f) {
-    const int r0 = min(g1, g0 + of * per_warp), r1 = min(g1, r0 + per_warp);
+    const int r0 = min(s.g1, g0 + of * s.per_warp), r1 = min(s.g1, r0 + s.per_warp);
     for (int base = r0; base < r1; base += 32 * kWarps) {
-      const int g = base + 32 * warp + lane;
+      const int g = base + 32 * warp() + lane();
       float x[G::N];
       uint64_t v[G::N], sum = 0;
       if (g < r1) {
@@ -606,7 +623,7 @@ struct Row {
   // and what is left of `want` there (lane i of every warp: v of warps 4 i ..)
   __device__ __forceinline__ int owner_of(const uint64_t (&v)[4], uint64_t& want) const {
     const uint64_t sum = (v[0] + v[1]) + (v[2] + v[3]);
-    const uint64_t incl = warp_scan(sum, lane);
+    const uint64_t incl = warp_scan(sum, lane());
     const int l = max(__ffs(__ballot_sync(0xffffffffu, incl >= want)) - 1, 0);
     uint64_t left = want - (incl - sum);
     int at = 0;
@@ -617,27 +634,27 @@ struct Row {
         at = j + 1;
       }
     want = __shfl_sync(0xffffffffu, left, l);
-    return __shfl_sync(0xffffffffu, 4 * lane + at, l);
+    return __shfl_sync(0xffffffffu, 4 * lane() + at, l);
   }
-  // what the cluster's warps have at s.count + warp
+  // what the cluster's warps have at `of` + warp
   __device__ __forceinline__ void load4(const uint64_t* of, uint64_t (&v)[4]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int i = 4 * lane + j;
-      v[j] = i < C * kWarps ? ld_cluster(of + i % kWarps, i / kWarps) : 0;
+      const int i = 4 * lane() + j;
+      v[j] = i < ctas() * kWarps ? ld_cluster(of + i % kWarps, i / kWarps) : 0;
     }
   }
   // token and probability: this CTA's logit i
   __device__ __forceinline__ void put(int i, float l, uint64_t total) const {
-    p.token[r] = i;
+    p.token[blockIdx.x / ctas()] = i;
     const SampleTerm w = sample_term(m, l, c, s.table);
     const double v = static_cast<double>(w.v) * 17592186044416.;
-    p.prob[r] = static_cast<float>((v + v * static_cast<double>(w.x)) / static_cast<double>(total));
+    p.prob[blockIdx.x / ctas()] = static_cast<float>((v + v * static_cast<double>(w.x)) / static_cast<double>(total));
   }
   // Draws from what is kept: warp `owner` of the cluster has the one that brings its
   // kept sum up to `want`.
   __device__ __forceinline__ void draw(const Prefix& kept, int owner, uint64_t want, uint64_t total) {
-    if (owner / kWarps != rank) return;
+    if (owner / kWarps != rank()) return;
     const int i = nth(owner % kWarps, want, [&](int i, float v) -> uint64_t { return kept.has(v, i) ? weight(v) : 0; });
     if (threadIdx.x == 0 && i >= 0) {
       float v[G::N];
@@ -664,7 +681,7 @@ struct Row {
   __device__ __forceinline__ int listed(int (&n)[kMaxCtas]) const {
     int all = 0;
 #pragma unroll
-    for (int k = 0; k < kMaxCtas; ++k) n[k] = k < C ? ld_cluster(&s.listed, k) : 0;
+    for (int k = 0; k < kMaxCtas; ++k) n[k] = k < ctas() ? ld_cluster(&s.listed, k) : 0;
 #pragma unroll
     for (int k = 0; k < kMaxCtas; ++k) all += min(n[k], kList + 1);
     return all;
@@ -682,7 +699,7 @@ struct Row {
         }
       t.x[q] = -INFINITY;
       t.i[q] = -1;
-      if (of < C && at < min(n[of], kList)) {
+      if (of < ctas() && at < min(n[of], kList)) {
         const uint2 v = ld_cluster(&s.list[at], of);
         t.x[q] = __uint_as_float(v.x);
         t.i[q] = static_cast<int>(v.y);
@@ -722,8 +739,8 @@ struct Row {
   // A bound, of ordered bits, that `most` of the threads' `mine` reach, and few more;
   // s.first and s.bad have the warps' largest and least
   __device__ __forceinline__ uint32_t threads_kth(uint32_t mine, int most) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(s.first[lane % kWarps]));
-    const uint32_t lo = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(s.bad[lane % kWarps]));
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(s.first[lane() % kWarps]));
+    const uint32_t lo = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(s.bad[lane() % kWarps]));
     const int shift = max(0, 32 - __clz(hi - lo) - kLocalBits);
     const uint64_t one[kItems] = {1};
     if (!level_of(one, static_cast<uint64_t>(most), [&](int) { return static_cast<int>((hi - mine) >> shift); })) return 0;
@@ -790,7 +807,6 @@ template <int TYPE, bool RESIDENT>
 __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
   using R = Row<TYPE, RESIDENT>;
   using G = Group<TYPE>;
-  extern __shared__ __align__(16) uint8_t dyn[];
   __shared__ Shared s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = p.ctas, rank = static_cast<int>(cluster_ctarank()), r = blockIdx.x / C;
@@ -804,8 +820,9 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int g0 = min(groups, rank * per), g1 = min(groups, g0 + per);
   const int w0 = min(g1, g0 + warp * per_warp), w1 = min(g1, w0 + per_warp);
   auto whole = [&](int g) { return g * G::N >= head && (g + 1) * G::N <= head + p.vocab; };
-  const int f0 = w0 < w1 && !whole(w0) ? w0 + 1 : w0, f1 = w0 < w1 && !whole(w1 - 1) ? w1 - 1 : w1;
-  R row_{s, p, reinterpret_cast<const uint8_t*>(base), reinterpret_cast<uint4*>(dyn), g0, g1, per_warp, w0, w1, f0, f1, head, r, lane, warp, rank, C};
+  const int ends = (w0 < w1 && !whole(w0) ? 1 : 0) | (w1 - 1 > w0 && !whole(w1 - 1) ? 2 : 0);
+  const int f0 = w0 + (ends & 1), f1 = w1 - (ends >> 1);
+  R row_{s, p, reinterpret_cast<const uint8_t*>(base), f0, f1, ends, head, g0};
   R& x = row_;
 
   const bool loads = RESIDENT && f0 < f1;  // this warp, by a bulk copy
@@ -814,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     fence_mbar_init();
     const uint32_t bytes = static_cast<uint32_t>(f1 - f0) * 16u;
     mbar_arrive_expect_tx(&s.bar[warp], bytes);
-    bulk_load(x.slice + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
+    bulk_load(x.slice() + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
   }
   const float T = p.temperature ? p.temperature[r] : 1.f, t = sample_temperature(T), u = p.u[r];
   const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
@@ -823,7 +840,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   if (tid < kSampleTable) s.table[tid] = p.table[tid];
   for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
     reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
-  if (tid == 0) s.listed = 0;
+  if (tid == 0) s.listed = 0, s.g1 = g1, s.per_warp = per_warp;
   // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by
   // all of them, with the logarithm, the table and the shares, it was half the time
   if (tid == kThreads - 32) s.scale = sample_scale(t);
@@ -835,8 +852,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   __syncwarp();  // the barrier is there
   int bad = 0;
   if (RESIDENT && w0 < w1) {
-    if (lane == 0 && !x.whole(w0)) x.slice[w0 - g0] = x.edge(w0);
-    if (lane == 1 && w1 - 1 > w0 && !x.whole(w1 - 1)) x.slice[w1 - 1 - g0] = x.edge(w1 - 1);
+    if (lane == 0 && (ends & 1) != 0) x.slice()[w0 - g0] = x.edge(w0);
+    if (lane == 1 && (ends & 2) != 0) x.slice()[f1 - g0] = x.edge(f1);
     if (loads && !mbar_wait(&s.bar[warp], 0, p.limit_ns, nullptr)) {
       bad = 2;
       atomicCAS(p.status, 0, EBD_ERR_TIMEOUT);
@@ -851,7 +868,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const int most = (top_k + C - 1) / C;  // of a CTA's largest, for a list
   const bool few = by_k && top_k <= kList / 2 && most <= kListMost && T > 0.f;
   float m = -INFINITY, low = INFINITY;
-  x.template sweep<8>([&](int, float v) {
+  x.template sweep<4>([&](int, float v) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v));
     low = fminf(low, v);
   });
@@ -984,7 +1001,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   kept.value = order_value(floor);
 
   if (by_k || by_p) {
-    x.bins = make_bins(sample_depth(m, low, x.c));
+    if (tid == 0) s.bins = make_bins(sample_depth(m, low, x.c));
+    __syncthreads();
     x.count(by_k ? top_k : 0, top_p);
     const bool cut_k = by_k && s.k_bin < kBins;
     // where top-k's bin and top-p's bins begin and end, a bound a warp
@@ -1138,9 +1156,7 @@ cudaError_t sample_configure() {
   return cudaSuccess;
 }
 
-cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
-  const long long size = p.dtype == EBD_LOGITS_F32 ? 4 : 2;
-  const long long bytes = p.vocab * size + 32;  // both ends rounded out
+cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   struct Table {
     SampleEntry v[kSampleTable];
     Table() {
@@ -1149,13 +1165,19 @@ cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st) {
   };
   static const Table table;
   std::memcpy(p.table, table.v, sizeof(p.table));
-  p.ctas = 1;
-  while (p.ctas < kMaxCtas && bytes / p.ctas > 32 * 1024) p.ctas *= 2;
-  if (const char* env = getenv("EBD_SAMPLE_CTAS")) p.ctas = atoi(env);
+  // CTAs per row: as many as pay against the cluster's barriers, which take 1 to 3 us
+  // each, and its launch.  Rows of 152064 floats, us with 1 / 2 / 4 / 8: one row at a
+  // temperature 42 / 23 / 16 / 13, 24 rows 46 / 28 / 18 / 24, 64 rows 47 / 28 / 29 / 48,
+  // 512 rows 185 / 162 / 192 / 312; by top-p 64 rows 108 / 66 / 64 / 95, 512 rows 357 /
+  // 329 / 400 / 593.  512 rows of 57000: 72 / 77 / 98 / 226.  Rows of 16000: one row 9.2 /
+  // 8.5 / 8.0 / 8.7, 64 rows 10.0 / 9.4 / 11.7 / 30.3.
+  const bool light = p.top_k == nullptr && p.top_p == nullptr;
+  p.ctas = p.rows <= 8 ? 8 : p.rows <= (light ? 32 : 64) ? 4 : p.rows <= 128 || p.vocab >= 100000 ? 2 : 1;
+  while (p.ctas > 1 && p.vocab / p.ctas < 6000) p.ctas /= 2;
+  // a slice of a row in shared memory, where it leaves room for two CTAs on an SM
+  const long long bytes = p.vocab * (p.dtype == EBD_LOGITS_F32 ? 4ll : 2ll) + 32;  // both ends rounded out
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
   p.resident = slice <= kSliceBytes;
-  if (getenv("EBD_SAMPLE_FLAT")) p.resident = 0;
-  (void)num_sms;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * p.ctas, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);

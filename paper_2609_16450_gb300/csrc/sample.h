@@ -23,6 +23,6 @@ struct SampleParams {
 };
 
 cudaError_t sample_configure();
-cudaError_t launch_sample(SampleParams p, int num_sms, cudaStream_t st);
+cudaError_t launch_sample(SampleParams p, cudaStream_t st);
 
 }  // namespace ebd
