@@ -690,9 +690,10 @@ ebd_status run_lm(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, bool p
     if (const char* env = getenv("EBD_LM_PAIR_MIN")) pair_min = atoi(env) > 0 ? atoi(env) : kMaxGroupRows + 1;
     const int units = (V + kUnit - 1) / kUnit;
     const bool pair = rows >= pair_min && h->grid_lm >= lm_pair_grid(h->num_sms, units);
-    lm_plan(p, rows, V, c.d_model, h->num_sms, pair);
+    const LmOutputs outputs = logits == nullptr ? LmOutputs::kStats : stats ? LmOutputs::kBoth : LmOutputs::kLogits;
+    lm_plan(p, rows, V, c.d_model, h->num_sms, pair, outputs);
     // a shard's own grid may exceed the partial columns of the handle
-    if (p.grp_cols > h->grid_lm) lm_plan(p, rows, V, c.d_model, h->grid_lm, pair);
+    if (p.grp_cols > h->grid_lm) lm_plan(p, rows, V, c.d_model, h->grid_lm, pair, outputs);
     if (p.grp_cols > h->grid_lm) return fail(h, EBD_ERR_UNSUPPORTED, "LM head: grid exceeds the partials");
     p.ncols = h->grid_lm;
     p.part_rows = c.max_rows;
@@ -709,7 +710,6 @@ ebd_status run_lm(ebd_handle* h, const ebd_step_args* a, cudaStream_t st, bool p
     p.pdl = (g0 == 0 && pdl_first) ? 1 : 0;
     p.logits = logits;
     p.logits_stride = stride;
-    p.stats = stats ? 1 : 0;
     CUtensorMap th;
     if (p.boxed) {
       if (!encode_k_boxes(&th, a->hidden, a->rows, c.d_model, p.nb / 2, p.kbs))

@@ -123,7 +123,8 @@ int lm_grid(int num_sms, int n_units);       // CTAs of the unpaired LM head
 int lm_pair_grid(int num_sms, int n_units);  // CTAs of the paired (cta_group::2) LM head
 // rows of an LM-head launch from which CTA pairs run it (and up to kMaxGroupRows)
 constexpr int kLmPairMinRows = 65;
-void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair = false);
+void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair = false,
+             LmOutputs out = LmOutputs::kStats);
 // pdl: launched as a programmatic dependent of the kernel before it on
 // `st` (that kernel's CTAs release it early; the attention reads nothing the
 // earlier kernel writes, and with p.wait_prior it completes after it)

@@ -42,6 +42,11 @@ namespace {
 constexpr uint32_t kATile = 128 * 128;  // 128 rows x 64 bf16
 constexpr int kTLd = 132;               // transpose buffer row stride (floats)
 constexpr uint32_t kTBytes = 32 * kTLd * 4;  // transpose buffer of one epilogue warpgroup
+constexpr int kStoreSlices = 4;         // of 32 columns that an epilogue thread holds the sums of
+// Columns of W that go into one accumulator where logits are stored.  390 rows of
+// Dream-7B: 335 us with all of a chunk in one, 340 so; with the statistics, whose
+// epilogue has two segments' time, 436 (the statistics alone 296).
+constexpr int kStoreColumns = 512;
 
 __device__ __forceinline__ void state_merge(float& m, float& s, float& t, float& l2, int& idx,
                                             float bm, float bs, float bt, float bl2, int bidx) {
@@ -118,15 +123,69 @@ __device__ __forceinline__ void record_error(int* status, volatile int* abort, i
   atomicCAS(status, 0, code);
 }
 
-// Statistics of one accumulator buffer by one epilogue warpgroup, in slices
-// of 32 columns (window rows): each slice goes TMEM -> registers -> a
-// transpose in shared memory, after which 4 threads share a column and scan
-// its 128 vocabulary lanes (32 each); the column's state is merged into the
-// running state of its row.  `release` is called once this thread has
-// loaded its last slice (the MMAs may then overwrite the buffer).  Returns
-// whether it was called.
-// `store` gets the logits of every slice, 32 columns of its thread's vocabulary
-// lane; without `stats` that is all.
+// Statistics of a slice of 32 columns (window rows) by one epilogue warpgroup: the
+// logits go through a transpose in shared memory, after which 4 threads share a column
+// and scan its 128 vocabulary lanes (32 each); the column's state is merged into the
+// running state of its row.
+__device__ __forceinline__ void slice_stats(const float (&v)[32], int cc, int n_pad, float* sTw, int lanev, bool lv,
+                                            int et, uint32_t bar_id, int vbase, float* st_m, float* st_s, float* st_t,
+                                            float* st_l2, int* st_i) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) sTw[j * kTLd + lanev] = lv ? v[j] : -INFINITY;
+  named_barrier(bar_id, 128);
+  {
+    const int j = et >> 2, q = et & 3;
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = sTw[j * kTLd + q + 4 * i];
+    // branch-free scan: the threads of a warp see different data
+    float m = -INFINITY, l2 = -INFINITY;
+    int ii = -1;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      l2 = fmaxf(l2, fminf(m, x[i]));
+      ii = x[i] > m ? i : ii;  // strict: the first (lowest) index of the maximum
+      m = fmaxf(m, x[i]);
+    }
+    int idx = ii < 0 ? INT_MAX : vbase + q + 4 * ii;  // vbase includes the shard offset
+    float s = 0.f, t = 0.f;
+    if (m != -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float dl = x[i] - m;
+        const float e = __expf(dl);
+        s += e;
+        t = fmaf(e, e > 0.f ? dl : 0.f, t);  // masked lanes: e = 0, dl = -inf
+      }
+    }
+#pragma unroll
+    for (int off = 1; off <= 2; off <<= 1) {
+      const float bm = __shfl_xor_sync(0xffffffffu, m, off);
+      const float bs = __shfl_xor_sync(0xffffffffu, s, off);
+      const float bt = __shfl_xor_sync(0xffffffffu, t, off);
+      const float bl = __shfl_xor_sync(0xffffffffu, l2, off);
+      const int bi = __shfl_xor_sync(0xffffffffu, idx, off);
+      state_merge(m, s, t, l2, idx, bm, bs, bt, bl, bi);
+    }
+    const int r = cc + j;
+    if (q == 0 && r < n_pad) {
+      float M = st_m[r], S = st_s[r], T = st_t[r], L2 = st_l2[r];
+      int I = st_i[r];
+      state_merge(M, S, T, L2, I, m, s, t, l2, idx);
+      st_m[r] = M;
+      st_s[r] = S;
+      st_t[r] = T;
+      st_l2[r] = L2;
+      st_i[r] = I;
+    }
+  }
+  named_barrier(bar_id, 128);
+}
+
+// One accumulator buffer by one epilogue warpgroup, in slices of 32 columns: each goes
+// TMEM -> registers, then to `store` (its thread's vocabulary lane of 32 columns) and,
+// with `stats`, to slice_stats.  `release` is called once this thread has loaded its
+// last slice (the MMAs may then overwrite the buffer).  Returns whether it was called.
 template <typename Store, typename Release>
 __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg, int n_pad,
                                                 float* sTw, int lanev, int et, uint32_t bar_id,
@@ -147,56 +206,7 @@ __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg
     }
     if (lv) store(cc, v);
     if (!stats) continue;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) sTw[j * kTLd + lanev] = lv ? v[j] : -INFINITY;
-    named_barrier(bar_id, 128);
-    {
-      const int j = et >> 2, q = et & 3;
-      float x[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = sTw[j * kTLd + q + 4 * i];
-      // branch-free scan: the threads of a warp see different data
-      float m = -INFINITY, l2 = -INFINITY;
-      int ii = -1;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        l2 = fmaxf(l2, fminf(m, x[i]));
-        ii = x[i] > m ? i : ii;  // strict: the first (lowest) index of the maximum
-        m = fmaxf(m, x[i]);
-      }
-      int idx = ii < 0 ? INT_MAX : vbase + q + 4 * ii;  // vbase includes the shard offset
-      float s = 0.f, t = 0.f;
-      if (m != -INFINITY) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float dl = x[i] - m;
-          const float e = __expf(dl);
-          s += e;
-          t = fmaf(e, e > 0.f ? dl : 0.f, t);  // masked lanes: e = 0, dl = -inf
-        }
-      }
-#pragma unroll
-      for (int off = 1; off <= 2; off <<= 1) {
-        const float bm = __shfl_xor_sync(0xffffffffu, m, off);
-        const float bs = __shfl_xor_sync(0xffffffffu, s, off);
-        const float bt = __shfl_xor_sync(0xffffffffu, t, off);
-        const float bl = __shfl_xor_sync(0xffffffffu, l2, off);
-        const int bi = __shfl_xor_sync(0xffffffffu, idx, off);
-        state_merge(m, s, t, l2, idx, bm, bs, bt, bl, bi);
-      }
-      const int r = cc + j;
-      if (q == 0 && r < n_pad) {
-        float M = st_m[r], S = st_s[r], T = st_t[r], L2 = st_l2[r];
-        int I = st_i[r];
-        state_merge(M, S, T, L2, I, m, s, t, l2, idx);
-        st_m[r] = M;
-        st_s[r] = S;
-        st_t[r] = T;
-        st_l2[r] = L2;
-        st_i[r] = I;
-      }
-    }
-    named_barrier(bar_id, 128);
+    slice_stats(v, cc, n_pad, sTw, lanev, lv, et, bar_id, vbase, st_m, st_s, st_t, st_l2, st_i);
   }
   return released;
 }
@@ -223,12 +233,13 @@ __device__ __forceinline__ bool epilogue_buffer(uint32_t taddr0, int wg, int nwg
 // the vocabulary range of owner q % nwork, and writes its partials to
 // columns [0, grp_cols) of those rows.
 //
-// STORE: the logits also go to memory, 32 lanes of a warp to 32 adjacent floats of
-// a row (ebd_lm_logits).
-template <bool PAIR, bool PACKED, bool BOXED, bool STORE>
+// OUT: the statistics, the logits to memory (ebd_lm_logits; 32 lanes of a warp to 32
+// adjacent floats of a row), or both.
+template <bool PAIR, bool PACKED, bool BOXED, LmOutputs OUT>
 __global__ void __launch_bounds__(kLmThreads, 1)
     lm_stats_kernel(const __grid_constant__ CUtensorMap tmap_w,
                     const __grid_constant__ CUtensorMap tmap_h, const LmParams p) {
+  constexpr bool STORE = OUT != LmOutputs::kStats, STATS = OUT != LmOutputs::kLogits;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -480,14 +491,17 @@ __global__ void __launch_bounds__(kLmThreads, 1)
         else
           umma_commit(&empty[st]);
       };
-      for (int u = u0; u < u1 && ok; u += ustep, ++c) {
+      // an accumulator at a time: a chunk, or (STORE) a segment of a chunk's columns
+      const int seg = STORE ? p.seg : p.nks;
+      for (int u = u0, k0 = 0; u < u1 && ok; ++c) {
         const int buf = c % p.nbuf;
         const uint32_t bph = static_cast<uint32_t>(c / p.nbuf) & 1u;
         ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty[buf], bph ^ 1u, p.limit_ns, abort));
         if (!ok) break;
         tc_fence_after();
         const uint32_t d0 = tmem_u + static_cast<uint32_t>(buf * p.acc_stride);
-        for (int ks = 0; ks < p.nks; ++ks) {
+        const int k1 = min(k0 + seg, p.nks);
+        for (int ks = k0; ks < k1; ++ks) {
           ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, p.limit_ns, abort));
           if (!ok) break;
           tc_fence_after();
@@ -502,7 +516,7 @@ __global__ void __launch_bounds__(kLmThreads, 1)
               const uint32_t b_step = b_sub >> 4;
               const uint32_t sub_desc = static_cast<uint32_t>(hrows) * 8u;  // hrows x 128 B >> 4
               const uint32_t sub_cols = static_cast<uint32_t>(p.nb);
-              const uint32_t acc0 = ks != 0 ? 1u : 0u;
+              const uint32_t acc0 = ks != k0 ? 1u : 0u;
 #define EBD_STAGE(K, S) \
     mma_stage<K, S, PAIR>(d0, a_lo, b_lo, b_step, sub_desc, sub_cols, desc_hi, idesc, acc0)
               if (PAIR || p.nsub == 1) {
@@ -530,7 +544,7 @@ __global__ void __launch_bounds__(kLmThreads, 1)
                   const uint64_t ad = umma_desc_sw128(a_addr + j * kATile + kk * 32);
                   for (int sb = 0; sb < p.nsub; ++sb) {
                     const uint64_t bd = umma_desc_sw128(b_addr + j * b_sub + sb * hrows * 128 + kk * 32);
-                    const uint32_t acc = (ks | j | kk) != 0 ? 1u : 0u;
+                    const uint32_t acc = ((ks - k0) | j | kk) != 0 ? 1u : 0u;
                     const uint32_t dd = d0 + static_cast<uint32_t>(sb * p.nb);
                     if (PAIR)
                       umma_bf16_lo_pair(dd, static_cast<uint32_t>(ad), static_cast<uint32_t>(bd),
@@ -557,6 +571,11 @@ __global__ void __launch_bounds__(kLmThreads, 1)
             umma_commit(&acc_full[buf]);
         }
         __syncwarp();
+        k0 = k1;
+        if (k0 == p.nks) {
+          k0 = 0;
+          u += ustep;
+        }
       }
       if (!ok) {
         if (lane == 0 && !*abort) record_error(p.status, abort, EBD_ERR_TIMEOUT);
@@ -596,39 +615,81 @@ __global__ void __launch_bounds__(kLmThreads, 1)
         mbar_arrive(&acc_empty[buf]);
     };
     int c = 0;
-    for (int u = u0; u < u1 && ok; u += ustep, ++c) {
-      const int nu = min(kChunkUnits, u1 - u);
+    // waits for accumulator c, the same answer in the warpgroup's threads
+    auto accumulated = [&]() {
       const int buf = c % p.nbuf;
       const uint32_t bph = static_cast<uint32_t>(c / p.nbuf) & 1u;
-      bool w = mbar_wait_sleepy(&acc_full[buf], bph, p.limit_ns, abort);
+      const bool w = mbar_wait_sleepy(&acc_full[buf], bph, p.limit_ns, abort);
       ok = named_barrier_and(bar_id, 128, w);
-      if (!ok) {
-        if (et == 0 && !*abort) record_error(p.status, abort, EBD_ERR_TIMEOUT);
-        break;
-      }
-      tc_fence_after();
+      if (!ok && et == 0 && !*abort) record_error(p.status, abort, EBD_ERR_TIMEOUT);
+      if (ok) tc_fence_after();
+      return ok;
+    };
+    for (int u = u0; u < u1 && ok; u += ustep) {
+      const int nu = min(kChunkUnits, u1 - u);
       // this CTA's vocabulary rows of the chunk: units [u + ulo, u + ulo + 2)
       // of W, i.e. vocabulary indices from p.v_off + (u + ulo) * kUnit
       const int wbase = (u + ulo) * kUnit;
       const int valid = min(min(2, nu - ulo) * kUnit, p.V - wbase);
       const int vbase = p.v_off + wbase;
-      const uint32_t taddr0 = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) +
-                              static_cast<uint32_t>(buf * p.acc_stride);
-      auto rel = [&]() { release(buf); };
+      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
       auto store = [&](int cc, const float(&v)[32]) {
         if constexpr (STORE) {
           float* o = p.logits + (rbase + cc) * p.logits_stride + vbase + lanev;
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (cc + j < rows_g) o[j * p.logits_stride] = v[j];
+          for (int j = 0; j < 32; ++j) {
+            if (cc + j < rows_g) *o = v[j];
+            o += p.logits_stride;
+          }
         }
       };
-      const bool released = epilogue_buffer(taddr0, wg, p.nwg, p.n_pad, sTw, lanev, et, bar_id,
-                                            vbase, valid, st_m, st_s, st_t, st_l2, st_i,
-                                            !STORE || p.stats != 0, store, rel);
+      if (STORE && p.seg < p.nks) {
+        // The tensor cores cut what they add to an accumulator, some 2^-25 of it each
+        // time.  The segments of a chunk's columns have accumulators of their own, and
+        // are added here, rounded: 4096 columns in one are 4.4e-6 off (of the
+        // logits' size), in 8 segments of 512 3e-7, half a plain sum's in 32 bits.
+        float sum[kStoreSlices][32];
+#pragma unroll
+        for (int i = 0; i < kStoreSlices * 32; ++i) sum[i / 32][i % 32] = 0.f;
+        for (int k0 = 0; k0 < p.nks; k0 += p.seg, ++c) {
+          if (!accumulated()) break;
+          const int buf = c % p.nbuf;
+#pragma unroll
+          for (int i = 0; i < kStoreSlices; ++i) {
+            const int cc = 32 * (wg + i * p.nwg);
+            if (cc >= p.n_pad) break;
+#pragma unroll
+            for (int k = 0; k < 32; k += 16) {
+              if (cc + k >= p.n_pad) break;
+              float v[32];
+              tmem_ld_32x32b_x16(taddr + static_cast<uint32_t>(buf * p.acc_stride + cc + k), v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) sum[i][k + j] += v[j];
+            }
+          }
+          release(buf);
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < kStoreSlices; ++i) {
+          const int cc = 32 * (wg + i * p.nwg);
+          if (cc >= p.n_pad) break;
+          if (lanev < valid) store(cc, sum[i]);
+          if constexpr (STATS)
+            slice_stats(sum[i], cc, p.n_pad, sTw, lanev, lanev < valid, et, bar_id, vbase, st_m, st_s, st_t, st_l2, st_i);
+        }
+        continue;
+      }
+      if (!accumulated()) break;
+      const int buf = c % p.nbuf;
+      auto rel = [&]() { release(buf); };
+      const bool released = epilogue_buffer(taddr + static_cast<uint32_t>(buf * p.acc_stride), wg, p.nwg, p.n_pad, sTw, lanev,
+                                            et, bar_id, vbase, valid, st_m, st_s, st_t, st_l2, st_i,
+                                            STATS, store, rel);
       if (!released) release(buf);  // no slice of this chunk for this warpgroup
+      ++c;
     }
-    if (ok && active && (!STORE || p.stats != 0)) {
+    if (ok && active && STATS) {
       // the rows of this warpgroup's slices (its threads updated them last):
       // this CTA's partial goes to column `col` of its group's rows, and
       // neutral states to the columns [grp_cols, ncols) that no CTA of the
@@ -683,7 +744,8 @@ int lm_pair_grid(int num_sms, int n_units) {
   return 2 * np;
 }
 
-void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair) {
+void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair, LmOutputs out) {
+  p.out = out;
   p.V = V;
   p.d = d;
   p.rows = rows;
@@ -734,8 +796,11 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair) {
   p.nkb = (d + 63) / 64;
   p.nwg = p.nbuf == 1 || (p.rgroups > 1 && p.nkb <= 24) ? 2 : 1;
   if (const char* env = getenv("EBD_LM_NWG")) p.nwg = atoi(env) == 2 ? 2 : 1;
+  const bool store = out != LmOutputs::kStats;
+  if (store && p.n_pad > 32 * kStoreSlices) p.nwg = 2;
+  const uint32_t t_bytes = out == LmOutputs::kLogits ? 0 : kTBytes * static_cast<uint32_t>(p.nwg);
   const uint32_t st_bytes = static_cast<uint32_t>(p.n_pad) * 20u;
-  const uint32_t tail = kTBytes * static_cast<uint32_t>(p.nwg) + ((st_bytes + 7) / 8 * 8) +
+  const uint32_t tail = t_bytes + ((st_bytes + 7) / 8 * 8) +
                         (2 * 8 + 6) * 8 + 16;
   const uint32_t budget = 232448u - 1024u - tail;
   // hidden bytes per k-box in one CTA: all rows, or half of them in a pair
@@ -756,6 +821,8 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair) {
   while (kbs > 1 && budget / (static_cast<uint32_t>(kbs) * (kATile + b_box)) < 2) --kbs;
   p.kbs = kbs;
   p.nks = (p.nkb + kbs - 1) / kbs;
+  p.seg = p.nks;
+  if (store && p.nbuf == 2 && p.n_pad <= 64 * kStoreSlices) p.seg = kbs * 64 < kStoreColumns ? kStoreColumns / (kbs * 64) : 1;
   const uint32_t stage = static_cast<uint32_t>(kbs) * (kATile + b_box);
   int stages = static_cast<int>(budget / stage);
   if (stages > 8) stages = 8;
@@ -763,7 +830,7 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair) {
   p.off_a = 0;
   p.off_b = p.off_a + static_cast<uint32_t>(stages) * kbs * kATile;
   p.off_t = p.off_b + static_cast<uint32_t>(stages) * kbs * b_box;
-  p.off_st = p.off_t + kTBytes * static_cast<uint32_t>(p.nwg);
+  p.off_st = p.off_t + t_bytes;
   p.off_bar = (p.off_st + st_bytes + 7) / 8 * 8;
   p.smem_bytes = p.off_bar + static_cast<uint32_t>(2 * stages + 6) * 8u + 16u + 1024u;
 }
@@ -809,20 +876,26 @@ cudaError_t launch_pack_lm(const __nv_bfloat16* w, __nv_bfloat16* out, int V, in
 }
 
 using LmKernel = void (*)(CUtensorMap, CUtensorMap, LmParams);
-template <bool STORE>
+template <LmOutputs OUT>
 static LmKernel lm_kernel(bool pair, bool packed, bool boxed) {
-  if (!pair) return packed ? lm_stats_kernel<false, true, false, STORE> : lm_stats_kernel<false, false, false, STORE>;
-  if (boxed) return packed ? lm_stats_kernel<true, true, true, STORE> : lm_stats_kernel<true, false, true, STORE>;
-  return packed ? lm_stats_kernel<true, true, false, STORE> : lm_stats_kernel<true, false, false, STORE>;
+  if (!pair) return packed ? lm_stats_kernel<false, true, false, OUT> : lm_stats_kernel<false, false, false, OUT>;
+  if (boxed) return packed ? lm_stats_kernel<true, true, true, OUT> : lm_stats_kernel<true, false, true, OUT>;
+  return packed ? lm_stats_kernel<true, true, false, OUT> : lm_stats_kernel<true, false, false, OUT>;
+}
+static LmKernel lm_kernel(LmOutputs out, bool pair, bool packed, bool boxed) {
+  switch (out) {
+    case LmOutputs::kStats: return lm_kernel<LmOutputs::kStats>(pair, packed, boxed);
+    case LmOutputs::kLogits: return lm_kernel<LmOutputs::kLogits>(pair, packed, boxed);
+    default: return lm_kernel<LmOutputs::kBoth>(pair, packed, boxed);
+  }
 }
 
 cudaError_t lm_configure() {
   const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e;
-  for (int i = 0; i < 6; ++i)
-    if ((e = cudaFuncSetAttribute(lm_kernel<false>(i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(lm_kernel<true>(i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess)
-      return e;
+  for (LmOutputs out : {LmOutputs::kStats, LmOutputs::kLogits, LmOutputs::kBoth})
+    for (int i = 0; i < 6; ++i)
+      if ((e = cudaFuncSetAttribute(lm_kernel(out, i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess) return e;
   return cudaSuccess;
 }
 
@@ -849,8 +922,7 @@ cudaError_t launch_lm_stats(const CUtensorMap& tmap_w, const CUtensorMap& tmap_h
   }
   cfg.attrs = attr;
   cfg.numAttrs = na;
-  const LmKernel k = p.logits != nullptr ? lm_kernel<true>(p.pair, p.packed, p.boxed) : lm_kernel<false>(p.pair, p.packed, p.boxed);
-  return cudaLaunchKernelEx(&cfg, k, tmap_w, tmap_h, p);
+  return cudaLaunchKernelEx(&cfg, lm_kernel(p.out, p.pair, p.packed, p.boxed), tmap_w, tmap_h, p);
 }
 
 }  // namespace ebd

@@ -6,6 +6,9 @@
 
 namespace ebd {
 
+// what an LM-head launch is for
+enum class LmOutputs { kStats, kLogits, kBoth };
+
 struct LmParams {
   int V, d;                 // vocabulary rows of this launch's W, hidden size
   int v_off;                // vocabulary index of W's first row (a shard's offset; 0 otherwise)
@@ -15,6 +18,7 @@ struct LmParams {
   int grid;                 // CTAs (each writes one partial per row)
   int nkb;                  // ceil(d / 64) k-blocks of 64 columns
   int kbs, nks;             // k-blocks per pipeline stage, stages per vocabulary chunk
+  int seg;                  // STORE: stages of one accumulator; nks: a chunk is not split
   int packed;               // W is tiled: tile (unit, k-block) at row (unit*nkb + kb)*64
   int boxed;                // CTA pairs: a stage's hidden rows (and row-major W rows) come in
                             // as one 3-D box (d a multiple of 64)
@@ -33,9 +37,9 @@ struct LmParams {
   int* status;
   uint64_t limit_ns;
   int force_timeout;
-  float* logits;            // where the logits go too (the STORE kernels), rows logits_stride
-  long long logits_stride;  // floats apart
-  int stats;                // 0: the logits alone, no partial states
+  float* logits;            // where the logits go, rows logits_stride floats apart
+  long long logits_stride;
+  LmOutputs out;
   int pdl;                  // a programmatic dependent of the kernel before it, which
                             // copies the hidden rows in: W loads start before the wait
 };

@@ -57,32 +57,55 @@ def test_logits(rows, d, vocab, pad, packed):
     h.close()
 
 
-@pytest.mark.parametrize("rows", [5, 64, 130, 300])
-def test_statistics_beside_the_logits_are_ebd_lm_stats(rows):
-    """The same kernel path: bit for bit; and logits do not depend on them."""
+@pytest.mark.parametrize("rows,d", [(5, 256), (64, 1032), (130, 1536), (300, 2056), (512, 640)])
+def test_statistics_beside_the_logits(rows, d):
+    """They are the stored logits', as ebd_lm_stats computes them from its own: in 32 bits,
+    by fast exponentials (off by 2^-21 each and in their sums, what the entropy weighs
+    with |l - m| < 64 at most).  The logits do not depend on them."""
     E, rt = _lib()
-    d, vocab = 256, 4096
+    vocab = 4096
     h = handle(d, vocab, rows)
     x, w, held = inputs(d, vocab, rows, 1, h)
     names = ("conf", "entropy", "ent_norm", "gap", "argmax")
-    got = []
+    t = {n: torch.zeros(rows, dtype=torch.int32 if n == "argmax" else torch.float32, device="cuda") for n in names}
     outs = [torch.full((rows, vocab), 7.0, device="cuda") for _ in range(2)]
-    for call in range(3):
+    for call in range(2):
         a = args(x, held)
-        t = {n: torch.zeros(rows, dtype=torch.int32 if n == "argmax" else torch.float32, device="cuda") for n in names}
-        if call < 2:
+        if call == 0:
             for n in names:
                 setattr(a, n, t[n].data_ptr())
-        if call == 0:
-            E.check(E.ebd_lm_stats(h.h, a, rt.stream_handle(None)), h.h)
-        else:
-            E.check(E.ebd_lm_logits(h.h, a, outs[call - 1].data_ptr(), 0, rt.stream_handle(None)), h.h)
-        got.append(t)
+        E.check(E.ebd_lm_logits(h.h, a, outs[call].data_ptr(), 0, rt.stream_handle(None)), h.h)
     assert h.sync_status() == 0
-    for n in names:
-        assert torch.equal(got[0][n], got[1][n]), n
+    l = outs[0].double()
+    p = torch.softmax(l, 1)
+    top = l.topk(2, 1).values
+    want = dict(conf=p.max(1).values, entropy=-(p * p.log()).sum(1), gap=p.max(1).values - torch.exp(top[:, 1] - torch.logsumexp(l, 1)))
+    want["ent_norm"] = want["entropy"] / np.log(vocab)
+    for n, v in want.items():
+        assert ((t[n].double() - v).abs() <= 64 * 2.0 ** -20).all(), n
+    assert torch.equal(outs[0].argmax(1).int(), t["argmax"])
     assert torch.equal(outs[0], outs[1])
-    assert torch.equal(outs[0].argmax(1).int(), got[0]["argmax"])
+    h.close()
+
+
+@pytest.mark.parametrize("rows", [32, 200])
+def test_long_sums(rows):
+    """4096 columns: no worse than sums of 512 rounded down at every step and added, whose
+    error is at most 32 cuts of a partial sum (16 columns each) by 2^-23 and 8 roundings."""
+    E, rt = _lib()
+    d, vocab = 4096, 3000
+    h = handle(d, vocab, rows)
+    x, w, held = inputs(d, vocab, rows, 1, h)
+    out = torch.zeros((rows, vocab), device="cuda")
+    E.check(E.ebd_lm_logits(h.h, args(x, held), out.data_ptr(), 0, rt.stream_handle(None)), h.h)
+    assert h.sync_status() == 0
+    p = x.double()[:, None].view(rows, 1, 8, 512) * w.double()[None].view(1, vocab, 8, 512)[:, :500]
+    most = (p.abs().sum(3) * 32 * 2.0 ** -23).sum(2) + p.abs().sum((2, 3)) * 8 * 2.0 ** -24
+    assert ((out[:, :500].double() - p.sum((2, 3))).abs() <= most).all()
+    # and as a rule far better: a cut is of a partial sum, which is no larger than the
+    # segment's, 8^-1/2 of the logits as these go; the segments' errors add up as their sums do
+    rms = (out[:, :500].double() - p.sum((2, 3))).square().mean().sqrt() / p.sum((2, 3)).square().mean().sqrt()
+    assert rms < 32 * 2.0 ** -23 + 8 * 2.0 ** -24
     h.close()
 
 
