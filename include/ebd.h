@@ -296,7 +296,7 @@ typedef struct {
  * least).  token is the least v in F with the sum of w over F up to v above u times
  * that over F, prob = w[token] over that sum.  T = 0: the lowest index of the largest
  * logit, with prob 1.  Temperatures count as 1e-30 at least, unless 0, and 1e30 at
- * most.  Weights are off by 2^-30 of themselves and 2^-45 of the largest, their sums
+ * most.  Weights are off by 2^-30 of themselves and 2^-43 of the largest, their sums
  * are exact: results do not vary from run to run.
  * Logits of -inf have no part in it.  A row with NaN, +inf, or no logit above -inf
  * records EBD_ERR_NONFINITE, one with u outside [0, 1), T negative or not finite, or

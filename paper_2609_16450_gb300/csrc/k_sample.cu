@@ -353,8 +353,8 @@ struct Row {
   }
   __device__ __forceinline__ static void add4(uint64_t& sum, const float (&h)[4], const float (&r)[4]) {
     const int high = __float_as_int(((h[0] + h[2]) + (h[1] + h[3])) + 4.f) - __float_as_int(4.f);  // up to 4
-    const int low = __float2int_rn(((r[0] + r[2]) + (r[1] + r[3])) * 17592186044416.f);
-    sum += static_cast<uint64_t>(static_cast<int64_t>(high) * 8388608 + low);
+    const int low = __float2int_rn(((r[0] + r[2]) + (r[1] + r[3])) * kSampleUnits);
+    sum += static_cast<uint64_t>(static_cast<int64_t>(high) * 4194304 + low);
   }
   // how many of four logits are equal to the last kept one, and kept
   __device__ __forceinline__ static int ties(const Prefix& kept, int i, const float (&x)[4]) {
@@ -648,7 +648,7 @@ struct Row {
   __device__ __forceinline__ void put(int i, float l, uint64_t total) const {
     p.token[blockIdx.x / ctas()] = i;
     const SampleTerm w = sample_term(m, l, c, s.table);
-    const double v = static_cast<double>(w.v) * 17592186044416.;
+    const double v = static_cast<double>(w.v) * static_cast<double>(kSampleUnits);
     p.prob[blockIdx.x / ctas()] = static_cast<float>((v + v * static_cast<double>(w.x)) / static_cast<double>(total));
   }
   // Draws from what is kept: warp `owner` of the cluster has the one that brings its

@@ -40,7 +40,7 @@ EBD_HD uint32_t order_key(float x) {
 }
 EBD_HD float order_value(uint32_t k) { return f32_of((k >> 31) != 0 ? k ^ 0x80000000u : ~k); }
 
-// The weight of logit l is w = exp((l - m) / T) in whole units of 2^-44, m the row's
+// The weight of logit l is w = exp((l - m) / T) in whole units of 2^-43, m the row's
 // largest logit, and 0 below 2^-40.  Sums of such weights are exact in any order, so
 // that a token's border in them is one number wherever it is computed.
 //
@@ -49,20 +49,21 @@ EBD_HD float order_value(uint32_t k) { return f32_of((k >> 31) != 0 ? k ^ 0x8000
 // z with |z| <= 1/2 (and e): 2^(-k / 128) is 2^(-(k >> 7)) times an entry of a table of
 // 128, a float v and what it is off by, relative to it; 2^(-z / 128) - 1 is a cubic in z
 // that leaves out 2^-38, and starts from that.  w = v + v x is rounded to units of
-// 2^-21, h, and what is left to units of 2^-44, all in float operations that are
-// exact but for those two: whole-number shifts and additions have half their rate.
-// The roundings of z and x make a weight off by some 2^-31 of itself, and the last by
-// half a unit.
+// 2^-21, h, and what is left, 2^-22 and hardly more, to units of 2^-43, all in float
+// operations that are exact but for those two: whole-number shifts and additions have
+// half their rate.
+// The roundings of z and x make a weight off by some 2^-31 of itself, and the last two
+// by 5/8 of a unit.
 struct SampleScale {
   float hi, lo;  // 128 log2(e) / T
 };
-constexpr int kSampleBits = 44;      // of a unit
 constexpr int kSampleVocab = 1 << 20;  // sums of fewer weights fit 64 bits
 constexpr int kSampleTable = 128;
 constexpr float kSampleDead = 40.f * kSampleTable;  // weights below 2^-40 are zero
 constexpr float kSampleMagic = 12582912.f;  // 1.5 * 2^23: adding it rounds to a whole number,
 constexpr float kSampleHigh = 6.f;          // 1.5 * 2^2: to a unit of 2^-21,
-constexpr float kSampleLow = 7.152557373046875e-7f;  // 1.5 * 2^-21: to one of 2^-44
+constexpr float kSampleLow = 1.430511474609375e-6f;  // 1.5 * 2^-20: to one of 2^-43
+constexpr float kSampleUnits = 8796093022208.f;      // 2^43
 // 2^(-z / 128) - 1 = z (c1 + z (c2 + z c3)): -ln 2, (ln 2)^2 / 2, -(ln 2)^3 / 6 with a
 // factor of 2^-7 for every z
 constexpr float kSampleC1 = -0.693147181f / 128, kSampleC2 = 0.240226507f / 16384, kSampleC3 = -0.0555041087f / 2097152;
@@ -101,7 +102,7 @@ EBD_HD SampleTerm sample_term(float m, float l, const SampleScale& c, const Samp
   const SampleEntry q = table[f32_bits(t) & (kSampleTable - 1)];
   return {f32_of(q.bits - (f32_bits(t) << 16)), fmaf(z, fmaf(z, fmaf(z, kSampleC3, kSampleC2), kSampleC1), q.off)};
 }
-// the same in whole numbers of 2^-21 and of 2^-44
+// the same in whole numbers of 2^-21 and of 2^-43
 struct SampleParts {
   float high, low;
 };
@@ -112,7 +113,7 @@ EBD_HD SampleParts sample_parts(const SampleTerm& w) {
 EBD_HD uint64_t sample_weight(float m, float l, const SampleScale& c, const SampleEntry* table) {
   if (!(sample_depth(m, l, c) <= kSampleDead)) return 0;
   const SampleParts w = sample_parts(sample_term(m, l, c, table));
-  return static_cast<uint64_t>(static_cast<int64_t>(w.high * 2097152.f) * 8388608 + static_cast<int64_t>(w.low * 17592186044416.f));
+  return static_cast<uint64_t>(static_cast<int64_t>(w.high * 2097152.f) * 4194304 + static_cast<int64_t>(w.low * kSampleUnits));
 }
 
 // total * x for a float x in [0, 1), cut or rounded up to a whole number: exactly.

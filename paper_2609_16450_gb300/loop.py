@@ -16,6 +16,10 @@ into it piece by piece, every step writes its window's rows into pages reserved
 as the window moves on (ebd_paged_write) and attends to all positions up to the
 window's end (ebd_paged_attention), and the cache is read back at the end
 (ebd_paged_read).
+With plan='device' those pages are handed out by ebd_paged_plan: what the last window
+cached past the new window's start goes back, and the window's rows come.
+With `sampling` x_hat is drawn at a temperature (ebd_lm_logits, ebd_sample) and kappa is
+the probability it was drawn with; the decision then runs on them (ebd_decide).
 This module only marshals buffers; the window rule and every step of the
 method run in the library."""
 from __future__ import annotations
@@ -28,6 +32,7 @@ import torch
 
 from . import _ebd as E
 from . import runtime as rt
+from . import sampling as sp
 from .paged import PagedCache
 
 MASK_TOKEN = -1
@@ -75,7 +80,8 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
              max_steps: Optional[int] = None, max_window: int = 64,
              keep: bool = True, stream: Optional[torch.cuda.Stream] = None,
              block: int = 32, cache: str = "prefix", append: bool = False,
-             window: str = "block", page_size: int = 64, kv_dtype: str = "bf16") -> LoopResult:
+             window: str = "block", page_size: int = 64, kv_dtype: str = "bf16", plan: str = "host",
+             sampling: Optional[sp.Settings] = None, uniforms: Optional[Callable] = None) -> LoopResult:
     """window_inputs(step, positions) -> (hidden, q, k_win, v_win) as bf16 bit
     arrays; kv_rows(positions) -> (k, v).  Positions are absolute.  Under the
     handle's baseline decode modes the window is the active fixed block of
@@ -84,7 +90,9 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
     with the prompt's K/V only (with 'dual', with every position's, the
     positions right of the window standing for the K/V a dual cache holds).
     cache='paged' (a handle of ebd_config.paged = 1): pages of page_size
-    positions in kv_dtype, 'bf16' or 'e4m3'; the attention's outputs are bf16."""
+    positions in kv_dtype, 'bf16' or 'e4m3', planned on the 'host' or the 'device'; the
+    attention's outputs are bf16.  sampling: how x_hat is drawn, by uniforms(step,
+    positions) -> one number in [0, 1) per position; a step then does not append."""
     if cache not in ("prefix", "dual", "paged"):
         raise ValueError("cache must be 'prefix', 'dual' or 'paged'")
     paged = cache == "paged"
@@ -92,6 +100,10 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
         raise ValueError("the paged cache takes every window's rows: it has no append")
     if window not in ("block", "full"):
         raise ValueError("window must be 'block' or 'full'")
+    if plan not in ("host", "device") or (plan == "device" and not paged):
+        raise ValueError("plan must be 'host', or 'device' with the paged cache")
+    if sampling is not None and (append or uniforms is None):
+        raise ValueError("sampling needs uniforms, and appends nothing")
     full = window == "full"  # the full-sequence setting: the window is the whole response
     if full and (attention or append or paged):
         raise ValueError("the full-sequence window runs without the window attention")
@@ -137,16 +149,33 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
         vc[0, :n0] = rt._dev(vv, dev).reshape(n0, Hkv, D)
     if paged:
         n_pages = (P0 + L + page_size - 1) // page_size
+        device_plan = plan == "device"
         kv_len = torch.zeros((1,), **i32)
+        add = torch.zeros((1,), **i32)
+        cached = 0  # positions that the plan has
         attn_p = torch.empty((W, Hq, D), dtype=torch.bfloat16, device=dev)
         with torch.cuda.stream(stream):
-            pages = PagedCache(h, n_pages, 1, n_pages, page_size, kv_dtype)
-            pages.reserve(0, P0, stream)
+            pages = PagedCache(h, n_pages, 1, n_pages, page_size, kv_dtype, plan=plan)
+            if device_plan:
+                kv_len = pages.kv_len
+            else:
+                pages.reserve(0, P0, stream)
             for at in range(0, P0, W):  # the prompt, in pieces that the handle's rows hold
                 pos = np.arange(at, min(at + W, P0), dtype=np.int32)
                 kk, vv = kv_rows(pos)
-                pages.write(rt._dev(np.array([0, len(pos)], np.int32), dev), rt._dev(pos, dev),
-                            rt._dev(kk, dev).view(-1, Hkv, D), rt._dev(vv, dev).view(-1, Hkv, D), stream=stream)
+                if device_plan:
+                    add.copy_(torch.tensor([len(pos)], dtype=torch.int32))
+                    pages.plan(add, cu, rp, stream=stream)
+                    at_cu, at_pos = cu, rp[:len(pos)]
+                else:
+                    at_cu, at_pos = rt._dev(np.array([0, len(pos)], np.int32), dev), rt._dev(pos, dev)
+                pages.write(at_cu, at_pos, rt._dev(kk, dev).view(-1, Hkv, D), rt._dev(vv, dev).view(-1, Hkv, D),
+                            stream=stream)
+            cached = P0
+    if sampling is not None:
+        logits = torch.empty((W, shape.vocab), **f32)
+        u = torch.empty((W,), **f32)
+        drawn = sampling.rows(W, dev)
     ev0, ev1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     res = LoopResult(tokens=None, steps=0)
     step = 0
@@ -175,9 +204,19 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
             pl.copy_(torch.tensor([P0 + lo], dtype=torch.int32))
             rp[:R].copy_(torch.from_numpy(positions))
             sfx.copy_(torch.tensor([P0 + hi, L - hi], dtype=torch.int32))
-            if paged:
+            if paged and device_plan:
+                add.copy_(torch.tensor([P0 + lo - cached], dtype=torch.int32))
+                if cached > P0 + lo:
+                    pages.plan(add, stream=stream)
+                    cached = P0 + lo
+                add.copy_(torch.tensor([P0 + hi - cached], dtype=torch.int32))
+                pages.plan(add, cu, rp, stream=stream)
+                cached = P0 + hi
+            elif paged:
                 kv_len.copy_(torch.tensor([P0 + hi], dtype=torch.int32))
                 pages.reserve(0, P0 + hi, stream)
+            if sampling is not None:
+                u[:R].copy_(torch.from_numpy(np.ascontiguousarray(uniforms(step, positions), dtype=np.float32)))
         a = E.ebd_step_args()
         a.batch, a.rows = 1, R
         a.cu_rows, a.prefix_len, a.row_pos = cu.data_ptr(), pl.data_ptr(), rp.data_ptr()
@@ -206,7 +245,17 @@ def run_loop(h: rt.Handle, shape, weights: rt.DeviceWeights,
             pages.write(cu, rp[:R], kw[:R], vw[:R], stream=stream)
             if attention:
                 pages.attention(q[:R], cu, kv_len, attn_p[:R], stream=stream)
-        E.check(E.ebd_step(h.h, a, sid), h.h)
+        if sampling is None:
+            E.check(E.ebd_step(h.h, a, sid), h.h)
+        else:
+            with torch.cuda.stream(stream):
+                sp.lm_logits(h, hid[:R], weights, logits[:R],
+                             {k: outs[k][:R] for k in ("entropy", "ent_norm", "gap")}, stream)
+                sp.sample(h, logits[:R], u[:R], argmax[:R], outs["conf"][:R], stream=stream,
+                          **{k: None if t is None else t[:R] for k, t in drawn.items()})
+            if attention and not paged:
+                E.check(E.ebd_attention(h.h, a, sid), h.h)
+            E.check(E.ebd_decide(h.h, a, sid), h.h)
         ev1.record(stream)
         st = h.sync_status(stream)
         if st != 0:

@@ -10,6 +10,15 @@ that have ended serve others.
     table.write(cu_rows, row_pos, k, v)         # rows of new tokens, of any projection's strides
     table.attention(q, cu_rows, kv_len, out, causal=True)
     table.release(3)
+
+With plan="device" the lengths, the table and the free pages live on the device, and
+`plan` (ebd_paged_plan) moves pages by what every sequence's length becomes: a step
+whose lengths are found out on the device needs no copy to the host.
+
+    cache = PagedCache(h, n_pages=4096, sequences=64, max_pages=128, plan="device")
+    cache.plan(add, cu_rows, row_pos)           # add [B]: rows that come, or positions that go
+    cache.write(cu_rows, row_pos, k, v)
+    cache.attention(q, cu_rows, cache.kv_len, out, causal=True)
 """
 from __future__ import annotations
 
@@ -95,12 +104,15 @@ def _rows(t: torch.Tensor, what: str, heads: int, dim: int) -> int:
 
 class PagedCache:
     """One layer's pools, and the calls on the first sequences of the table.
-    `h`: a handle of ebd_config.paged = 1; its heads are the cache's."""
+    `h`: a handle of ebd_config.paged = 1; its heads are the cache's.  `plan`: where
+    pages are handed out, 'host' (reserve, release) or 'device' (plan)."""
 
     def __init__(self, h: rt.Handle, n_pages: int, sequences: int, max_pages: int,
-                 page_size: int = 64, dtype: str = "bf16", device="cuda"):
+                 page_size: int = 64, dtype: str = "bf16", device="cuda", plan: str = "host"):
         if dtype not in DTYPES:
             raise ValueError("dtype must be 'bf16' or 'e4m3'")
+        if plan not in ("host", "device"):
+            raise ValueError("plan must be 'host' or 'device'")
         c = h.cfg
         self.h, self.dtype, self.page_size = h, dtype, page_size
         self.heads_q, self.heads, self.dim = c.n_heads_q, c.n_heads_kv, c.head_dim
@@ -114,18 +126,65 @@ class PagedCache:
             self.k_scale = torch.zeros(shape, dtype=torch.uint8, device=device)
             self.v_scale = torch.zeros_like(self.k_scale)
         self.table = torch.from_numpy(self.pages.table.copy()).to(device)
+        self.on_device = plan == "device"
+        if self.on_device:
+            self.kv_len = torch.zeros(sequences, dtype=torch.int32, device=device)
+            self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
+            self.n_free = torch.full((1,), n_pages, dtype=torch.int32, device=device)
         self._struct = self.struct()
 
     # ------------------------------------------------------------ pages
     def reserve(self, seq: int, length: int, stream: Optional[torch.cuda.Stream] = None):
         """Pages for positions [0, length); later calls on `stream` see them."""
+        self._planned(False)
         if self.pages.reserve(seq, length):
             self._upload(seq, stream)
 
     def release(self, seq: int, length: int = 0, stream: Optional[torch.cuda.Stream] = None):
         """Gives back the pages past `length`; calls before it on `stream` still use them."""
+        self._planned(False)
         if self.pages.release(seq, length):
             self._upload(seq, stream)
+
+    def plan(self, add, cu_rows=None, row_pos=None, slot=None, stream=None):
+        """Lengths become max(0, kv_len + add) for the first sequences, add [B] int32, and
+        pages go back and out by them.  The new rows' offsets into cu_rows [B + 1], their
+        positions into row_pos [rows] and their places in the pools into slot [rows]
+        (int64), -1 past the rows there are.  What cannot be met changes nothing, hands out
+        no rows, and is EBD_ERR_PAGES at the handle's next sync_status."""
+        self._planned(True)
+        _ints(add, "add")
+        self._here(add=add)
+        if add.dim() != 1 or add.numel() > self.table.shape[0]:
+            raise ValueError("add: one number per sequence")
+        a = E.ebd_paged_plan_args()
+        a.batch, a.add, a.kv_len = add.numel(), add.data_ptr(), self.kv_len.data_ptr()
+        a.page_table, a.free_pages, a.n_free = self.table.data_ptr(), self.free_pages.data_ptr(), self.n_free.data_ptr()
+        a.page_size, a.n_pages, a.max_pages = self.page_size, self.pages.n_pages, self.table.shape[1]
+        if cu_rows is not None:
+            _ints(cu_rows, "cu_rows")
+            self._here(cu_rows=cu_rows)
+            if cu_rows.numel() != add.numel() + 1:
+                raise ValueError("cu_rows: one offset per sequence, and the end")
+            a.cu_rows = cu_rows.data_ptr()
+        rows = [t.numel() for t in (row_pos, slot) if t is not None]
+        if rows and min(rows) != max(rows):
+            raise ValueError("row_pos and slot: the same rows")
+        if row_pos is not None:
+            _ints(row_pos, "row_pos")
+            self._here(row_pos=row_pos)
+            a.row_pos = row_pos.data_ptr()
+        if slot is not None:
+            if slot.dtype != torch.int64 or not slot.is_contiguous():
+                raise ValueError("slot: contiguous int64 expected")
+            self._here(slot=slot)
+            a.slot = slot.data_ptr()
+        a.rows = rows[0] if rows else 0
+        E.check(E.ebd_paged_plan(self.h.h, a, rt.stream_handle(stream)), self.h.h)
+
+    def _planned(self, on_device: bool):
+        if on_device != self.on_device:
+            raise RuntimeError("pages are handed out on the " + ("device: plan()" if self.on_device else "host: reserve(), release()"))
 
     def _upload(self, seq, stream):
         with torch.cuda.stream(stream or torch.cuda.current_stream()):

@@ -1,9 +1,9 @@
 """Sampling in 64 bits, and what a drawn token may differ by.
 
-A kernel's weights are off by 2^-30 of themselves and 2^-45 of the largest; sums of
+A kernel's weights are off by 2^-30 of themselves and 2^-43 of the largest; sums of
 them are exact, and so are the parts of them that a share or a random number takes, but
-for a unit of 2^-44.  So a border lies within slack() of all that is kept from where it
-is here: twice 2^-30, for what lies below it and for the whole, and twice 2^-45 for
+for a unit of 2^-43.  So a border lies within slack() of all that is kept from where it
+is here: twice 2^-30, for what lies below it and for the whole, and twice 2^-43 for
 every logit.  numpy's own are off by 2^-50 at
 most at these sizes.
 """
@@ -14,7 +14,7 @@ import numpy as np
 
 def slack(w):
     """Of the sum of weights w (the largest of them 1)."""
-    return 2.0 ** -29 + 2.0 ** -44 * (1 + np.count_nonzero(w)) / w.sum()
+    return 2.0 ** -29 + 2.0 ** -42 * (1 + np.count_nonzero(w)) / w.sum()
 
 
 def order(l):
