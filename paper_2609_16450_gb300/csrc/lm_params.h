@@ -39,6 +39,7 @@ struct LmParams {
   int force_timeout;
   float* logits;            // where the logits go, rows logits_stride floats apart
   long long logits_stride;
+  int stream_out;           // they are more than L2 keeps
   LmOutputs out;
   int pdl;                  // a programmatic dependent of the kernel before it, which
                             // copies the hidden rows in: W loads start before the wait
