@@ -9,10 +9,11 @@
 // back what a call handed out leaves the stack as it was.
 //
 // One CTA: a plan moves a few KB, and is bound by its chain of loads: lengths ->
-// prefix sums (rows, pages out, pages back) -> the pages to move -> slots.  Every
-// item finds its sequence by a binary search of the prefix sums in shared memory.
-// All that a plan asks for is looked at before anything is written: one that cannot
-// be met changes no state, and hands out no rows.
+// prefix sums (rows, pages out, pages back) -> the pages to move.  Every item finds its
+// sequence by a binary search of the prefix sums in shared memory.  Pages that move are
+// read once, all at a time, and kept there; slots come from them too.  All that a plan
+// asks for is looked at before anything is written: one that cannot be met changes no
+// state, and hands out no rows.
 #include "internal.h"
 #include "paged.h"
 
@@ -20,10 +21,12 @@ namespace ebd {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024;  // at most
+constexpr int kPlanPages = 8192;    // pages out, and back, that shared memory holds
 
 struct Sums {
   long long rows, out, back;
+  int bad;  // 1: EBD_ERR_BOUNDS, 2: EBD_ERR_PAGES
 };
 
 // Sequence of item i by the prefix sums cu[0 .. n]: the last with cu[b] <= i < cu[b + 1].
@@ -46,37 +49,30 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
   int* const back = out + p.B + 1;       // of pages to take back
   int* const first = back + p.B + 1;     // [B] first page that changes hands
   int* const old = first + p.B;          // [B] length before
+  int* const now = old + p.B;            // [B] page that the first new row goes into, if it is there
+  int* const going = now + p.B;          // [p.pages] pages back,
+  int* const coming = going + p.pages;   // and out
   __shared__ Sums warp_sum[kPlanThreads / 32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
   const int page = 1 << p.page_log2;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const long long n0 = *p.n_free;
 
   // a run of sequences a thread
-  const int per = (p.B + kPlanThreads - 1) / kPlanThreads;
+  const int per = (p.B + threads - 1) / threads;
   const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-  int bad = 0;
-  Sums sum{0, 0, 0};
+  Sums sum{0, 0, 0, 0};
   const long long most = min(static_cast<long long>(p.max_pages) << p.page_log2, 0x7fffffffll);
   for (int b = b0; b < b1; ++b) {
     const int len = p.kv_len[b], add = p.add[b];
     const long long to = max(0ll, static_cast<long long>(len) + add);
-    if (len < 0 || len > most) {
-      bad |= 1;
-      continue;
-    }
-    if (to > most) {
-      bad |= 2;
+    if (len < 0 || len > most || to > most) {
+      sum.bad |= len < 0 || len > most ? 1 : 2;
       continue;
     }
     const int have = static_cast<int>((static_cast<long long>(len) + page - 1) >> p.page_log2);
     const int need = static_cast<int>((to + page - 1) >> p.page_log2);
-    // new rows begin within a page that is there
-    if (add > 0 && len % page != 0) {
-      const int e = p.page_table[static_cast<long long>(b) * p.max_pages + (len >> p.page_log2)];
-      if (e < 0 || e >= p.n_pages) bad |= 1;
-    }
     rows[b] = max(add, 0);
     out[b] = max(need - have, 0);
     back[b] = max(have - need, 0);
@@ -97,76 +93,95 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
       incl.back += k;
     }
   }
+  incl.bad = static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<unsigned>(sum.bad)));
   if (lane == 31) warp_sum[warp] = incl;
   __syncthreads();
-  Sums at{incl.rows - sum.rows, incl.out - sum.out, incl.back - sum.back}, total{0, 0, 0};
-  for (int i = 0; i < kPlanThreads / 32; ++i) {
+  Sums at{incl.rows - sum.rows, incl.out - sum.out, incl.back - sum.back, 0}, total{0, 0, 0, 0};
+  for (int i = 0; i < threads / 32; ++i) {
     const Sums w = warp_sum[i];
     if (i < warp) at.rows += w.rows, at.out += w.out, at.back += w.back;
-    total.rows += w.rows, total.out += w.out, total.back += w.back;
+    total.rows += w.rows, total.out += w.out, total.back += w.back, total.bad |= w.bad;
   }
+  int bad = total.bad;  // as all threads see it
   if (n0 < 0 || n0 + total.back > p.n_pages) bad |= 1;
-  if (total.out > n0 + total.back) bad |= 2;
+  if (total.out > n0 + total.back || total.rows > 0x7fffffffll) bad |= 2;
   if ((p.row_pos != nullptr || p.slot != nullptr) && total.rows > p.R) bad |= 2;
-  if (total.rows > 0x7fffffffll) bad |= 2;
-  bad = __syncthreads_or(bad & 1) | (__syncthreads_or(bad & 2) ? 2 : 0);
   const int n_out = static_cast<int>(total.out), n_back = static_cast<int>(total.back);
   const int top = static_cast<int>(n0) + n_back;  // of the stack, once all are back on it
+  // Item i of the pages back goes to place top - 1 - i of the stack, which is where item
+  // i of the pages out comes from.
+  const bool kept = n_out <= p.pages && n_back <= p.pages;
+  auto leaves = [&](int i) -> int* {
+    const int b = sequence_of(back, p.B, i);
+    return p.page_table + static_cast<long long>(b) * p.max_pages + first[b] + i - back[b];
+  };
+  auto comes = [&](int i) -> int* {
+    const int b = sequence_of(out, p.B, i);
+    return p.page_table + static_cast<long long>(b) * p.max_pages + first[b] + i - out[b];
+  };
   if (!bad) {
+    int wrong = 0;
     for (int b = b0; b < b1; ++b) {
-      const int r = rows[b], o = out[b], k = back[b];
+      const int r = rows[b], o = out[b], k = back[b], len = old[b];
       rows[b] = static_cast<int>(at.rows), out[b] = static_cast<int>(at.out), back[b] = static_cast<int>(at.back);
       at.rows += r, at.out += o, at.back += k;
+      // new rows begin within a page that is there
+      if (r > 0 && (len & (page - 1)) != 0) {
+        const int e = p.page_table[static_cast<long long>(b) * p.max_pages + (len >> p.page_log2)];
+        now[b] = e;
+        wrong |= e < 0 || e >= p.n_pages;
+      }
     }
     if (tid == 0) rows[p.B] = static_cast<int>(total.rows), out[p.B] = n_out, back[p.B] = n_back;
     __syncthreads();
-    int wrong = 0;
-    for (int i = tid; i < n_back; i += kPlanThreads) {
-      const int b = sequence_of(back, p.B, i);
-      const int e = p.page_table[static_cast<long long>(b) * p.max_pages + first[b] + i - back[b]];
+    for (int i = tid; i < n_back; i += threads) {
+      const int e = *leaves(i);
+      if (kept) going[i] = e;
       wrong |= e < 0 || e >= p.n_pages;
     }
-    for (int i = tid; i < n_out; i += kPlanThreads) {
-      if (top - 1 - i >= n0) continue;  // one of those that come back
+    for (int i = tid; i < n_out; i += threads) {
+      if (i < n_back) continue;  // one of those
       const int e = p.free_pages[top - 1 - i];
+      if (kept) coming[i] = e;
       wrong |= e < 0 || e >= p.n_pages;
     }
-    bad = __syncthreads_or(wrong);
+    if (__syncthreads_or(wrong)) bad = 1;
   }
   if (bad) {
     if (tid == 0) atomicCAS(p.status, 0, (bad & 1) ? EBD_ERR_BOUNDS : EBD_ERR_PAGES);
     if (p.cu_rows != nullptr)
-      for (int b = tid; b <= p.B; b += kPlanThreads) p.cu_rows[b] = 0;
-    for (int r = tid; r < p.R; r += kPlanThreads) {
+      for (int b = tid; b <= p.B; b += threads) p.cu_rows[b] = 0;
+    for (int r = tid; r < p.R; r += threads) {
       if (p.row_pos != nullptr) p.row_pos[r] = -1;
       if (p.slot != nullptr) p.slot[r] = -1;
     }
     return;
   }
-  for (int i = tid; i < n_back; i += kPlanThreads) {
-    const int b = sequence_of(back, p.B, i);
-    int* const e = p.page_table + static_cast<long long>(b) * p.max_pages + first[b] + i - back[b];
-    p.free_pages[top - 1 - i] = *e;
-    *e = -1;
-  }
-  __syncthreads();
-  for (int i = tid; i < n_out; i += kPlanThreads) {
-    const int b = sequence_of(out, p.B, i);
-    p.page_table[static_cast<long long>(b) * p.max_pages + first[b] + i - out[b]] = p.free_pages[top - 1 - i];
-  }
   for (int b = b0; b < b1; ++b) p.kv_len[b] = static_cast<int>(max(0ll, static_cast<long long>(old[b]) + p.add[b]));
   if (tid == 0) *p.n_free = top - n_out;
   if (p.cu_rows != nullptr)
-    for (int b = tid; b <= p.B; b += kPlanThreads) p.cu_rows[b] = rows[b];
-  __syncthreads();
-  for (int r = tid; r < p.R; r += kPlanThreads) {
+    for (int b = tid; b <= p.B; b += threads) p.cu_rows[b] = rows[b];
+  for (int i = tid; i < n_back; i += threads) {
+    int* const e = leaves(i);
+    p.free_pages[top - 1 - i] = kept ? going[i] : *e;
+    *e = -1;
+  }
+  if (!kept) __syncthreads();  // pages out may be among those on the stack by now
+  for (int i = tid; i < n_out; i += threads)
+    *comes(i) = !kept ? p.free_pages[top - 1 - i] : i < n_back ? going[i] : coming[i];
+  if (!kept) __syncthreads();  // slots read the table
+  for (int r = tid; r < p.R; r += threads) {
     int pos = -1;
     long long slot = -1;
     if (r < total.rows) {
       const int b = sequence_of(rows, p.B, r);
       pos = old[b] + r - rows[b];
       if (p.slot != nullptr) {
-        const long long e = p.page_table[static_cast<long long>(b) * p.max_pages + (pos >> p.page_log2)];
+        const int j = pos >> p.page_log2, i = out[b] + j - first[b];  // new pages are from `first` on
+        const long long e = !kept          ? p.page_table[static_cast<long long>(b) * p.max_pages + j]
+                            : j < first[b] ? now[b]
+                            : i < n_back   ? going[i]
+                                           : coming[i];
         slot = (e << p.page_log2) + (pos & (page - 1));
       }
     }
@@ -175,17 +190,26 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
   }
 }
 
-size_t plan_bytes(int B) { return (3 * (static_cast<size_t>(B) + 1) + 2 * static_cast<size_t>(B)) * sizeof(int); }
+size_t plan_bytes(int B, int pages) {
+  return (3 * (static_cast<size_t>(B) + 1) + 3 * static_cast<size_t>(B) + 2 * static_cast<size_t>(pages)) * sizeof(int);
+}
 
 }  // namespace
 
 cudaError_t paged_plan_configure() {
   return cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(plan_bytes(kPagedMaxBatch)));
+                              static_cast<int>(plan_bytes(kPagedMaxBatch, kPlanPages)));
 }
 
-cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t st) {
-  return paged_launch(paged_plan_kernel, dim3(1), kPlanThreads, static_cast<uint32_t>(plan_bytes(p.B)), st, p);
+cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st) {
+  // a thread for each sequence and row, as far as that goes: fewer start sooner, and
+  // meet at barriers sooner
+  const int items = p.B > p.R ? p.B : p.R;
+  const int threads = items >= kPlanThreads ? kPlanThreads : items <= 128 ? 128 : (items + 31) / 32 * 32;
+  // pages that may move: rows and a page more for each sequence, or as many back
+  const int pages = p.B + (p.R > p.B ? p.R : p.B);
+  p.pages = pages < kPlanPages ? pages : kPlanPages;
+  return paged_launch(paged_plan_kernel, dim3(1), threads, static_cast<uint32_t>(plan_bytes(p.B, p.pages)), st, p);
 }
 
 }  // namespace ebd

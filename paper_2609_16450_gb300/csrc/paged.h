@@ -39,9 +39,10 @@ struct PagedPlanParams {
   int* row_pos;
   int64_t* slot;
   int* status;
+  int pages;                   // pages out, and back, that shared memory holds
 };
 cudaError_t paged_plan_configure();
-cudaError_t launch_paged_plan(const PagedPlanParams& p, cudaStream_t st);
+cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st);
 
 // Every kernel of the paged cache is a programmatic dependent of the one before
 // it on the stream: it reads global memory only after griddepcontrol.wait, and

@@ -120,6 +120,23 @@ def test_taking_back_restores_the_stack():
     h.close()
 
 
+@pytest.mark.parametrize("batch,pages", [(1, 30000), (3, 9000), (70, 300)])
+def test_more_pages_than_a_cta_holds(batch, pages):
+    """Whole caches that come and go at once, lengths alone: pages handed out are those
+    that other sequences have just given back, and others."""
+    ref = Plan(batch * pages + 50, batch, pages, 16)
+    random.Random(2).shuffle(ref.free)
+    h = handle(batch, 64)
+    d = Device(ref, h, 64)
+    d.step([16 * pages - 5] * batch, outputs=False)
+    half = [(-16 * pages if b % 2 == 0 else 3) for b in range(batch)]
+    d.step(half, outputs=False)
+    d.step([(16 * pages - 40 if b % 2 == 0 else -16 * pages // 2) for b in range(batch)], outputs=False)
+    d.step([b % 2 for b in range(batch)])
+    d.step([(-16 * pages if b % 2 == 0 else min(20, 60 // batch)) for b in range(batch)])
+    h.close()
+
+
 def test_no_sequences_and_no_rows():
     ref = Plan(5, 0, 1, 16)
     h = handle(4, 8)
