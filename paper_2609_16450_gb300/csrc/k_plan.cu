@@ -21,12 +21,13 @@ namespace ebd {
 
 namespace {
 
-constexpr int kPlanThreads = 1024;  // at most
+constexpr int kPlanThreads = 512;  // at most
 constexpr int kPlanPages = 8192;    // pages out, and back, that shared memory holds
 
 struct Sums {
   long long rows, out, back;
-  int bad;  // 1: EBD_ERR_BOUNDS, 2: EBD_ERR_PAGES
+  int bad;   // 1: EBD_ERR_BOUNDS, 2: EBD_ERR_PAGES
+  int most;  // new rows of one sequence
 };
 
 // Sequence of item i by the prefix sums cu[0 .. n]: the last with cu[b] <= i < cu[b + 1].
@@ -49,7 +50,8 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
   int* const back = out + p.B + 1;       // of pages to take back
   int* const first = back + p.B + 1;     // [B] first page that changes hands
   int* const old = first + p.B;          // [B] length before
-  int* const now = old + p.B;            // [B] page that the first new row goes into, if it is there
+  int* const then = old + p.B;           // [B] and after
+  int* const now = then + p.B;           // [B] page that the first new row goes into, if it is there
   int* const going = now + p.B;          // [p.pages] pages back,
   int* const coming = going + p.pages;   // and out
   __shared__ Sums warp_sum[kPlanThreads / 32];
@@ -62,14 +64,13 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
   // a run of sequences a thread
   const int per = (p.B + threads - 1) / threads;
   const int b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-  Sums sum{0, 0, 0, 0};
+  Sums sum{0, 0, 0, 0, 0};
   const long long most = min(static_cast<long long>(p.max_pages) << p.page_log2, 0x7fffffffll);
-  for (int b = b0; b < b1; ++b) {
-    const int len = p.kv_len[b], add = p.add[b];
+  auto look = [&](int b, int len, int add) {
     const long long to = max(0ll, static_cast<long long>(len) + add);
     if (len < 0 || len > most || to > most) {
       sum.bad |= len < 0 || len > most ? 1 : 2;
-      continue;
+      return;
     }
     const int have = static_cast<int>((static_cast<long long>(len) + page - 1) >> p.page_log2);
     const int need = static_cast<int>((to + page - 1) >> p.page_log2);
@@ -78,9 +79,20 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
     back[b] = max(have - need, 0);
     first[b] = min(have, need);
     old[b] = len;
+    then[b] = static_cast<int>(to);
     sum.rows += max(add, 0);
     sum.out += max(need - have, 0);
     sum.back += max(have - need, 0);
+    sum.most = max(sum.most, add);
+  };
+  for (int b = b0; b < b1; b += 4) {  // four sequences' loads at once
+    int len[4], add[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (b + j < b1) len[j] = p.kv_len[b + j], add[j] = p.add[b + j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (b + j < b1) look(b + j, len[j], add[j]);
   }
   Sums incl = sum;
 #pragma unroll
@@ -94,13 +106,14 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
     }
   }
   incl.bad = static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<unsigned>(sum.bad)));
+  incl.most = __reduce_max_sync(0xffffffffu, sum.most);
   if (lane == 31) warp_sum[warp] = incl;
   __syncthreads();
-  Sums at{incl.rows - sum.rows, incl.out - sum.out, incl.back - sum.back, 0}, total{0, 0, 0, 0};
+  Sums at{incl.rows - sum.rows, incl.out - sum.out, incl.back - sum.back, 0, 0}, total{0, 0, 0, 0, 0};
   for (int i = 0; i < threads / 32; ++i) {
     const Sums w = warp_sum[i];
     if (i < warp) at.rows += w.rows, at.out += w.out, at.back += w.back;
-    total.rows += w.rows, total.out += w.out, total.back += w.back, total.bad |= w.bad;
+    total.rows += w.rows, total.out += w.out, total.back += w.back, total.bad |= w.bad, total.most = max(total.most, w.most);
   }
   int bad = total.bad;  // as all threads see it
   if (n0 < 0 || n0 + total.back > p.n_pages) bad |= 1;
@@ -157,7 +170,7 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
     }
     return;
   }
-  for (int b = b0; b < b1; ++b) p.kv_len[b] = static_cast<int>(max(0ll, static_cast<long long>(old[b]) + p.add[b]));
+  for (int b = b0; b < b1; ++b) p.kv_len[b] = then[b];
   if (tid == 0) *p.n_free = top - n_out;
   if (p.cu_rows != nullptr)
     for (int b = tid; b <= p.B; b += threads) p.cu_rows[b] = rows[b];
@@ -170,28 +183,35 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(const PagedPla
   for (int i = tid; i < n_out; i += threads)
     *comes(i) = !kept ? p.free_pages[top - 1 - i] : i < n_back ? going[i] : coming[i];
   if (!kept) __syncthreads();  // slots read the table
-  for (int r = tid; r < p.R; r += threads) {
-    int pos = -1;
-    long long slot = -1;
-    if (r < total.rows) {
-      const int b = sequence_of(rows, p.B, r);
-      pos = old[b] + r - rows[b];
-      if (p.slot != nullptr) {
-        const int j = pos >> p.page_log2, i = out[b] + j - first[b];  // new pages are from `first` on
-        const long long e = !kept          ? p.page_table[static_cast<long long>(b) * p.max_pages + j]
-                            : j < first[b] ? now[b]
-                            : i < n_back   ? going[i]
-                                           : coming[i];
-        slot = (e << p.page_log2) + (pos & (page - 1));
-      }
-    }
+  auto put = [&](int b, int r) {  // row r, of sequence b
+    const int pos = old[b] + r - rows[b];
     if (p.row_pos != nullptr) p.row_pos[r] = pos;
-    if (p.slot != nullptr) p.slot[r] = slot;
+    if (p.slot == nullptr) return;
+    const int j = pos >> p.page_log2, i = out[b] + j - first[b];  // new pages are from `first` on
+    const long long e = !kept          ? p.page_table[static_cast<long long>(b) * p.max_pages + j]
+                        : j < first[b] ? now[b]
+                        : i < n_back   ? going[i]
+                                       : coming[i];
+    p.slot[r] = (e << p.page_log2) + (pos & (page - 1));
+  };
+  // rows by their sequences where those have few, else each looks for its own
+  const bool few = total.most <= 4;
+  if (p.row_pos == nullptr && p.slot == nullptr) return;
+  if (few)
+    for (int b = b0; b < b1; ++b)
+      for (int r = rows[b]; r < rows[b + 1]; ++r) put(b, r);
+  for (int r = few ? static_cast<int>(total.rows) + tid : tid; r < p.R; r += threads) {
+    if (r < total.rows) {
+      put(sequence_of(rows, p.B, r), r);
+      continue;
+    }
+    if (p.row_pos != nullptr) p.row_pos[r] = -1;
+    if (p.slot != nullptr) p.slot[r] = -1;
   }
 }
 
 size_t plan_bytes(int B, int pages) {
-  return (3 * (static_cast<size_t>(B) + 1) + 3 * static_cast<size_t>(B) + 2 * static_cast<size_t>(pages)) * sizeof(int);
+  return (3 * (static_cast<size_t>(B) + 1) + 4 * static_cast<size_t>(B) + 2 * static_cast<size_t>(pages)) * sizeof(int);
 }
 
 }  // namespace
@@ -202,8 +222,10 @@ cudaError_t paged_plan_configure() {
 }
 
 cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st) {
-  // a thread for each sequence and row, as far as that goes: fewer start sooner, and
-  // meet at barriers sooner
+  // A thread for each sequence and row, as far as that goes: fewer start sooner, and
+  // meet at barriers sooner.  us for the two calls of 2048 sequences with 128 / 256 / 384 /
+  // 512 / 768 / 1024 threads at most: 31.8 / 19.5 / 14.3 / 14.9 / 14.9 / 17.4; of prompts of
+  // 2k rows 12.7 / 9.5 / 8.9 / 9.0 / 9.5 / 11.0.
   const int items = p.B > p.R ? p.B : p.R;
   const int threads = items >= kPlanThreads ? kPlanThreads : items <= 128 ? 128 : (items + 31) / 32 * 32;
   // pages that may move: rows and a page more for each sequence, or as many back
