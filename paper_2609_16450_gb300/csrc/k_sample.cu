@@ -16,9 +16,10 @@
 // comes into its shared memory once.
 //
 // The last logit of a prefix is found without sorting, in one of three ways.
-//   - Top-k of few: the least of what the CTAs' threads have as their largest logits,
-//     the (k / CTAs)-th of each CTA's, is a bound that k logits reach and not many
-//     more.  Those are listed, and one CTA does the rest with them in registers.
+//   - Top-k of few: every thread has the largest logit of each half of its own; the
+//     least, over the CTAs, of the (k / CTAs)-th of a CTA's is a bound that k logits
+//     reach and not many more.  Those are listed, and one CTA does the rest with them in
+//     registers.
 //   - Top-p: one sweep counts logits in bins of y = (m - l) log2(e) / T, which bound
 //     the sums and so the few bins that the border lies in; a second sums what lies
 //     above them and lists what lies within, and again one CTA does the rest.
@@ -44,7 +45,7 @@ constexpr int kBins = 2048;                  // of y, counts
 constexpr int kFine = 512, kFineBits = 9;    // of ordered bits, weights and counts
 constexpr int kLocal = 1024, kLocalBits = 10;  // of a list
 constexpr int kList = 2048, kItems = kList / kThreads;  // listed logits, of a CTA and of a row
-constexpr int kListMost = kThreads / 2;      // of a CTA's threads, for a list of top-k's
+constexpr int kListMost = kThreads;           // of a CTA's threads' two values, for a list of top-k's
 constexpr int kSliceBytes = 76 * 1024;  // of a row in shared memory
 
 // Loads from a CTA of the cluster; volatile, so none moves across a barrier, and
@@ -224,7 +225,8 @@ struct Prefix {
   }
 };
 
-template <int TYPE, bool RESIDENT>
+// W: logits whose weights a thread works on at once, 4 or 8.
+template <int TYPE, bool RESIDENT, int W>
 struct Row {
   using G = Group<TYPE>;
   Shared& s;
@@ -320,6 +322,59 @@ struct Row {
     if ((ends & 1) != 0 && lane() == 0) four(f0 - 1, edge(f0 - 1));
     if ((ends & 2) != 0 && lane() == 0) four(f1, edge(f1));
   }
+  // index of the k-th of W logits, from the first's: floats come in two groups, a
+  // warp's apart
+  __device__ __forceinline__ static constexpr int at(int k) { return G::N == 8 || k < 4 ? k : k - 4 + 32 * 4; }
+  // f(index of the first, W logits), at() apart; -inf where there are none
+  template <typename F>
+  __device__ __forceinline__ void sweep_wide(F f) const {
+    if constexpr (W == 4) {
+      sweep4<1>(f);
+      return;
+    } else {
+      constexpr int GROUPS = 8 / G::N;  // of a turn
+      const int first = f0 - (RESIDENT ? ends & 1 : 0), end = f1 + (RESIDENT ? ends >> 1 : 0);
+      auto load = [&](int g, uint4(&v)[GROUPS]) {
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k)
+          if (g + 32 * k < end) v[k] = RESIDENT ? slice()[g + 32 * k - g0] : reinterpret_cast<const uint4*>(data)[g + 32 * k];
+      };
+      auto give = [&](int g, const uint4(&v)[GROUPS], int last) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) {
+          float y[G::N];
+          G::get(v[k], y);
+#pragma unroll
+          for (int j = 0; j < G::N; ++j) x[k * G::N + j] = g + 32 * k < last ? y[j] : -INFINITY;
+        }
+        f(g * G::N - head, x);
+      };
+      uint4 next[GROUPS];
+      int g = first + lane();
+      load(g, next);
+      while (g < end) {
+        uint4 v[GROUPS];
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) v[k] = next[k];
+        const int here = g;
+        g += 32 * GROUPS;
+        load(g, next);
+        give(here, v, end);
+      }
+      if (!RESIDENT && lane() == 0) {
+        uint4 v[GROUPS];
+        if ((ends & 1) != 0) {
+          v[0] = edge(f0 - 1);
+          give(f0 - 1, v, f0);
+        }
+        if ((ends & 2) != 0) {
+          v[0] = edge(f1);
+          give(f1, v, f1 + 1);
+        }
+      }
+    }
+  }
   // f(index, logit)
   template <int AHEAD = 1, typename F>
   __device__ __forceinline__ void sweep(F f) const {
@@ -329,38 +384,50 @@ struct Row {
     });
   }
   __device__ __forceinline__ uint64_t weight(float x) const { return sample_weight(m, x, c, s.table); }
-  // Adds up the weights of those of four logits that reach `cut`, and of those above
-  // `over` (TWO).  The parts of four weights add up exactly as floats.
+  // Adds up the weights of those of W logits that reach `cut`, and of those above
+  // `over` (TWO).  Their parts add up exactly as floats.
   template <bool TWO>
-  __device__ __forceinline__ void weigh(const float (&x)[4], float cut, float over, uint64_t& sum, uint64_t& above) const {
-    if (!(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= cut)) return;
-    float h[4], r[4];
+  __device__ __forceinline__ void weigh(const float (&x)[W], float cut, float over, uint64_t& sum, uint64_t& above) const {
+    if (!(largest(x) >= cut)) return;
+    float h[W], r[W];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < W; ++j) {
       const SampleParts w = sample_parts(sample_term(m, x[j], c, s.table));
       h[j] = x[j] >= cut ? w.high : 0.f;
       r[j] = x[j] >= cut ? w.low : 0.f;
     }
-    add4(sum, h, r);
+    add_up(sum, h, r);
     if (TWO) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < W; ++j) {
         h[j] = x[j] > over ? h[j] : 0.f;
         r[j] = x[j] > over ? r[j] : 0.f;
       }
-      add4(above, h, r);
+      add_up(above, h, r);
     }
   }
-  __device__ __forceinline__ static void add4(uint64_t& sum, const float (&h)[4], const float (&r)[4]) {
-    const int high = __float_as_int(((h[0] + h[2]) + (h[1] + h[3])) + 4.f) - __float_as_int(4.f);  // up to 4
-    const int low = __float2int_rn(((r[0] + r[2]) + (r[1] + r[3])) * kSampleUnits);
+  __device__ __forceinline__ static float largest(const float (&x)[W]) {
+    float y = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    if constexpr (W == 8) y = fmaxf(y, fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    return y;
+  }
+  // (8 of 1 are 2^24 units of 2^-21, and 4 of 2^-21 2^24 units of 2^-43)
+  __device__ __forceinline__ static void add_up(uint64_t& sum, const float (&h)[W], const float (&r)[W]) {
+    float a = (h[0] + h[2]) + (h[1] + h[3]);
+    int low = __float2int_rn(((r[0] + r[2]) + (r[1] + r[3])) * kSampleUnits);
+    if constexpr (W == 8) {
+      a += (h[4] + h[6]) + (h[5] + h[7]);
+      low += __float2int_rn(((r[4] + r[6]) + (r[5] + r[7])) * kSampleUnits);
+    }
+    // floats from 4 to 8 have steps of 2^-21
+    const int high = W == 4 ? __float_as_int(a + 4.f) - __float_as_int(4.f) : __float2int_rn(a * 2097152.f);
     sum += static_cast<uint64_t>(static_cast<int64_t>(high) * 4194304 + low);
   }
-  // how many of four logits are equal to the last kept one, and kept
-  __device__ __forceinline__ static int ties(const Prefix& kept, int i, const float (&x)[4]) {
+  // how many of W logits are equal to the last kept one, and kept
+  __device__ __forceinline__ static int ties(const Prefix& kept, int i, const float (&x)[W]) {
     int n = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) n += x[j] == kept.value && i + j <= kept.index;
+    for (int j = 0; j < W; ++j) n += x[j] == kept.value && i + at(j) <= kept.index;
     return n;
   }
   // Bin of a logit, by descending logits, and past the last for weights of zero
@@ -736,16 +803,27 @@ struct Row {
     __syncthreads();
     return s.bin >= 0;
   }
-  // A bound, of ordered bits, that `most` of the threads' `mine` reach, and few more;
-  // s.first and s.bad have the warps' largest and least
-  __device__ __forceinline__ uint32_t threads_kth(uint32_t mine, int most) {
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, static_cast<uint32_t>(s.first[lane() % kWarps]));
-    const uint32_t lo = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(s.bad[lane() % kWarps]));
-    const int shift = max(0, 32 - __clz(hi - lo) - kLocalBits);
-    const uint64_t one[kItems] = {1};
-    if (!level_of(one, static_cast<uint64_t>(most), [&](int) { return static_cast<int>((hi - mine) >> shift); })) return 0;
-    const uint32_t last = (static_cast<uint32_t>(s.bin + 1) << shift) - 1;  // of the bin, from hi
-    return hi - lo > last ? hi - last : lo;
+  // A bound that `most` of the threads' two values reach, and few more: by bins of equal
+  // width from the largest to the least of them
+  __device__ __forceinline__ float threads_kth(float a, float b, int most) {
+    float hi = fmaxf(a, b), lo = fminf(a > -INFINITY ? a : INFINITY, b > -INFINITY ? b : INFINITY);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    }
+    if (lane() == 0) s.max[warp()] = hi, s.low[warp()] = lo;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) hi = fmaxf(hi, s.max[i]), lo = fminf(lo, s.low[i]);
+    const float scale = (kLocal - 1.f) / (hi - lo);  // not finite where there is nothing to tell apart
+    if (!(scale < 1e30f && scale > 0.f)) return lo < INFINITY ? lo : -3.402823466e38f;
+    const float x[kItems] = {a, b};
+    const uint64_t one[kItems] = {a > -INFINITY ? 1u : 0u, b > -INFINITY ? 1u : 0u};
+    if (!level_of(one, static_cast<uint64_t>(most), [&](int q) { return min(static_cast<int>((hi - x[q]) * scale), kLocal - 1); }))
+      return -3.402823466e38f;
+    const float t = hi - (static_cast<float>(s.bin) + 1.01f) / scale;  // and room for rounding
+    return fmaxf(lo, t - (fabsf(hi) + fabsf(t)) * 2.384185791015625e-7f);
   }
   // The index at which the sum of v by index reaches `target`
   __device__ __forceinline__ int list_nth(const Items& t, const uint64_t (&v)[kItems], uint64_t target) {
@@ -803,9 +881,10 @@ struct Row {
   }
 };
 
-template <int TYPE, bool RESIDENT>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams p) {
-  using R = Row<TYPE, RESIDENT>;
+template <int TYPE, bool RESIDENT, int PER_SM>
+__global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SampleParams p) {
+  constexpr int W = PER_SM == 1 ? 8 : 4;
+  using R = Row<TYPE, RESIDENT, W>;
   using G = Group<TYPE>;
   __shared__ Shared s;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -867,20 +946,21 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   const bool by_k = top_k > 0 && top_k < p.vocab;
   const int most = (top_k + C - 1) / C;  // of a CTA's largest, for a list
   const bool few = by_k && top_k <= kList / 2 && most <= kListMost && T > 0.f;
-  float m = -INFINITY, low = INFINITY;
-  x.template sweep<4>([&](int, float v) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v));
-    low = fminf(low, v);
+  float m = -INFINITY, other = -INFINITY, low = INFINITY;  // two halves of a thread's logits
+  x.template sweep4<4>([&](int, const float(&v)[4]) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v[0]));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(other) : "f"(v[1]));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(v[2]));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(other) : "f"(v[3]));
+    low = fminf(low, fminf(fminf(v[0], v[1]), fminf(v[2], v[3])));
   });
-  bad |= m != m;
+  bad |= m != m || other != other;
   low = low < INFINITY ? low : -INFINITY;
   if (few) {
-    const uint32_t mine = x.key(m), hi = __reduce_max_sync(0xffffffffu, mine), lo = __reduce_min_sync(0xffffffffu, mine);
-    if (lane == 0) s.first[warp] = static_cast<int>(hi), s.bad[warp] = static_cast<int>(lo);
-    __syncthreads();
-    const uint32_t t = x.threads_kth(mine, most);
-    if (tid == 0) s.kth = t > 0x00800000u ? order_value(t) : -3.402823466e38f;
+    const float kth = x.threads_kth(m, other, most);
+    if (tid == 0) s.kth = kth;
   }
+  m = fmaxf(m, other);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -1001,7 +1081,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
   kept.value = order_value(floor);
 
   if (by_k || by_p) {
-    if (tid == 0) s.bins = make_bins(sample_depth(m, low, x.c));
+    if (tid == 0) s.bins = make_bins(1.5f * sample_depth(m, low, x.c));
     __syncthreads();
     x.count(by_k ? top_k : 0, top_p);
     const bool cut_k = by_k && s.k_bin < kBins;
@@ -1043,16 +1123,19 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
       const float mid = 0.5f * f_lo + 0.5f * f_hi, half = (0.5f * f_hi - 0.5f * f_lo) + 4.76837158203125e-7f * (fabsf(f_lo) + fabsf(f_hi));
       const bool ties = kept.index != INT_MAX;  // at top-k's border: in no sum above, being the last
       const uint64_t last = ties ? x.weight(kept.value) : 0;
-      x.template sweep4<1>([&](int i, const float(&v)[4]) {
-        if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= kept.value)) return;
+      x.sweep_wide([&](int i, const float(&v)[W]) {
+        if (!(R::largest(v) >= kept.value)) return;
         if (ties) all += x.ties(kept, i, v) * last;
         x.template weigh<true>(v, cut, f_hi, all, sum);
-        if (!(fminf(fminf(fabsf(v[0] - mid), fabsf(v[1] - mid)), fminf(fabsf(v[2] - mid), fabsf(v[3] - mid))) <= half)) return;
+        float away = fabsf(v[0] - mid);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (!(v[j] >= f_lo && v[j] <= f_hi) || !kept.has(v[j], i + j)) continue;
+        for (int j = 1; j < W; ++j) away = fminf(away, fabsf(v[j] - mid));
+        if (!(away <= half)) return;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          if (!(v[j] >= f_lo && v[j] <= f_hi) || !kept.has(v[j], i + R::at(j))) continue;
           if (list)
-            x.push(v[j], i + j);
+            x.push(v[j], i + R::at(j));
           else
             x.template add<true>(h, (hi - x.key(v[j])) >> shift, v[j]);
         }
@@ -1118,7 +1201,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const float cut = kept.cut();
     const uint64_t last = kept.index != INT_MAX ? x.weight(kept.value) : 0;
     uint64_t none = 0;
-    x.template sweep4<1>([&](int i, const float(&v)[4]) {
+    x.sweep_wide([&](int i, const float(&v)[W]) {
       x.template weigh<false>(v, cut, 0.f, sum, none);
       if (last != 0) sum += x.ties(kept, i, v) * last;
     });
@@ -1138,19 +1221,26 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 }
 
 using Kernel = void (*)(SampleParams);
+template <int PER_SM>
 Kernel sample_kernel_of(int dtype, bool resident) {
   switch (dtype) {
-    case EBD_LOGITS_F32: return resident ? sample_kernel<EBD_LOGITS_F32, true> : sample_kernel<EBD_LOGITS_F32, false>;
-    case EBD_LOGITS_BF16: return resident ? sample_kernel<EBD_LOGITS_BF16, true> : sample_kernel<EBD_LOGITS_BF16, false>;
-    default: return resident ? sample_kernel<EBD_LOGITS_F16, true> : sample_kernel<EBD_LOGITS_F16, false>;
+    case EBD_LOGITS_F32:
+      return resident ? sample_kernel<EBD_LOGITS_F32, true, PER_SM> : sample_kernel<EBD_LOGITS_F32, false, PER_SM>;
+    case EBD_LOGITS_BF16:
+      return resident ? sample_kernel<EBD_LOGITS_BF16, true, PER_SM> : sample_kernel<EBD_LOGITS_BF16, false, PER_SM>;
+    default: return resident ? sample_kernel<EBD_LOGITS_F16, true, PER_SM> : sample_kernel<EBD_LOGITS_F16, false, PER_SM>;
   }
+}
+Kernel sample_kernel_of(int dtype, bool resident, bool alone) {
+  return alone ? sample_kernel_of<1>(dtype, resident) : sample_kernel_of<2>(dtype, resident);
 }
 
 }  // namespace
 
 cudaError_t sample_configure() {
-  for (int i = 0; i < 3; ++i) {
-    const cudaError_t e = cudaFuncSetAttribute(sample_kernel_of(i, true), cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+  for (int i = 0; i < 6; ++i) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(sample_kernel_of(i / 2, true, i & 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
@@ -1165,15 +1255,21 @@ cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   };
   static const Table table;
   std::memcpy(p.table, table.v, sizeof(p.table));
-  // CTAs per row: as many as pay against the cluster's barriers, which take 1 to 3 us
-  // each, and its launch.  Rows of 152064 floats, us with 1 / 2 / 4 / 8: one row at a
-  // temperature 42 / 23 / 16 / 13, 24 rows 46 / 28 / 18 / 24, 64 rows 47 / 28 / 29 / 48,
-  // 512 rows 185 / 162 / 192 / 312; by top-p 64 rows 108 / 66 / 64 / 95, 512 rows 357 /
-  // 329 / 400 / 593.  512 rows of 57000: 72 / 77 / 98 / 226.  Rows of 16000: one row 9.2 /
-  // 8.5 / 8.0 / 8.7, 64 rows 10.0 / 9.4 / 11.7 / 30.3.
-  const bool light = p.top_k == nullptr && p.top_p == nullptr;
-  p.ctas = p.rows <= 8 ? 8 : p.rows <= (light ? 32 : 64) ? 4 : p.rows <= 128 || p.vocab >= 100000 ? 2 : 1;
-  while (p.ctas > 1 && p.vocab / p.ctas < 6000) p.ctas /= 2;
+  // CTAs per row (a cluster).  Few rows: as many as run at once, one CTA on an SM (so
+  // many clusters of 8, 6, .. CTAs find room in the GPU's groups of SMs), with registers
+  // to spare and two loads in turn.  Rows of 152064 floats, us with 2 / 3 / 4 / 5 / 6 / 8
+  // CTAs, at a temperature: 14 rows 27 / 20 / 18 / 16 / 16 / 15, 20 rows 27 / 20 / 19 / 17
+  // / 16 / 28, 28 rows 27 / 21 / 19 / 18 / 29 / 30, 36 rows 27 / 21 / 19 / 31 / 31 / 42, 44
+  // rows 27 / 21 / 34 / 32 / 31 / 44.  Many rows: two CTAs on an SM; a cluster's barriers
+  // and its launch cost more than they bring, but for long rows: 512 rows of 152064 at a
+  // temperature 185 / 162 / 192 us with 1 / 2 / 4 CTAs, of 57000 72 / 77 / 98.
+  struct { int rows, ctas; } const fits[] = {{14, 8}, {20, 6}, {24, 5}, {36, 4}, {44, 3}, {76, 2}};
+  int alone = 0;
+  for (const auto& f : fits)
+    if (alone == 0 && p.rows <= f.rows) alone = f.ctas;
+  p.ctas = alone != 0 ? alone : p.rows <= 128 || p.vocab >= 100000 ? 2 : 1;
+  const int most = (p.vocab + 11999) / 12000;  // a CTA wants some logits: one row of 16000 9.2 / 8.5 / 8.0 / 8.7 us with 1 / 2 / 4 / 8
+  if (p.ctas > most) p.ctas = most;
   // a slice of a row in shared memory, where it leaves room for two CTAs on an SM
   const long long bytes = p.vocab * (p.dtype == EBD_LOGITS_F32 ? 4ll : 2ll) + 32;  // both ends rounded out
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
@@ -1192,7 +1288,7 @@ cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sample_kernel_of(p.dtype, p.resident != 0), p);
+  return cudaLaunchKernelEx(&cfg, sample_kernel_of(p.dtype, p.resident != 0, alone != 0), p);
 }
 
 }  // namespace ebd

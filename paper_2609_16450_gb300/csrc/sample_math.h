@@ -49,9 +49,9 @@ EBD_HD float order_value(uint32_t k) { return f32_of((k >> 31) != 0 ? k ^ 0x8000
 // z with |z| <= 1/2 (and e): 2^(-k / 128) is 2^(-(k >> 7)) times an entry of a table of
 // 128, a float v and what it is off by, relative to it; 2^(-z / 128) - 1 is a cubic in z
 // that leaves out 2^-38, and starts from that.  w = v + v x is rounded to units of
-// 2^-21, h, and what is left, 2^-22 and hardly more, to units of 2^-43, all in float
-// operations that are exact but for those two: whole-number shifts and additions have
-// half their rate.
+// 2^-21, h (v first, then v + v x, so that 2^-21 may be left), and what is left to
+// units of 2^-43, all in float operations that are exact but for those roundings:
+// whole-number shifts and additions have half their rate.
 // The roundings of z and x make a weight off by some 2^-31 of itself, and the last two
 // by 5/8 of a unit.
 struct SampleScale {

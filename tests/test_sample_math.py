@@ -63,8 +63,7 @@ def _weights(lib, m, T, l):
 @pytest.mark.parametrize("center", [0.0, 9.0, -400.0, 1e-4, 1e30])
 def test_weights(lib, T, center):
     """Off by 2^-30 of themselves, half a unit of 2^-43, and half a step of the float that
-    is rounded to units, 2^-22 and a bit at most (v is rounded to units of 2^-21 before v x,
-    2^-26 of 1 here, is added) and so 2^-46 (in 64 bits numpy's own exponent is off
+    is rounded to units, 2^-21 at most and so 2^-46 (in 64 bits numpy's own exponent is off
     by 2^-52 of x, 28 at most, and its exponential by 2^-52)."""
     rng = np.random.default_rng(1)
     t = min(max(float(np.float32(T)), float(np.float32(1e-30))), float(np.float32(1e30)))
