@@ -43,10 +43,12 @@ constexpr uint32_t kATile = 128 * 128;  // 128 rows x 64 bf16
 constexpr int kTLd = 132;               // transpose buffer row stride (floats)
 constexpr uint32_t kTBytes = 32 * kTLd * 4;  // transpose buffer of one epilogue warpgroup
 constexpr int kStoreSlices = 4;         // of 32 columns that an epilogue thread holds the sums of
-// Columns of W that go into one accumulator where logits are stored.  390 rows of
-// Dream-7B: 335 us with all of a chunk in one, 340 so; with the statistics, whose
-// epilogue has two segments' time, 436 (the statistics alone 296).
-constexpr int kStoreColumns = 512;
+// Columns of W that go into one accumulator where logits are stored, alone and in
+// pairs.  What is stored after a chunk has the time of two segments before the MMAs wait
+// for it, which the pairs feel: 390 rows of Dream-7B with 512 / 768 / 1024 / all of the
+// 3584 columns in one 370 / 340 / 329 / 322 us, 128 rows of LLaDA-8B 202 / 194 / 181 /
+// 176; errors 4.7e-7, 7.0e-7, 9.4e-7 and 3.8e-6 (a plain sum's in 32 bits 5.6e-7).
+constexpr int kStoreColumns = 512, kStoreColumnsPair = 768;
 
 __device__ __forceinline__ void state_merge(float& m, float& s, float& t, float& l2, int& idx,
                                             float bm, float bs, float bt, float bl2, int bidx) {
@@ -830,7 +832,10 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair, LmOutp
   p.kbs = kbs;
   p.nks = (p.nkb + kbs - 1) / kbs;
   p.seg = p.nks;
-  if (store && p.nbuf == 2 && p.n_pad <= 64 * kStoreSlices) p.seg = kbs * 64 < kStoreColumns ? kStoreColumns / (kbs * 64) : 1;
+  if (store && p.nbuf == 2 && p.n_pad <= 64 * kStoreSlices) {
+    const int columns = pair ? kStoreColumnsPair : kStoreColumns;
+    p.seg = kbs * 64 < columns ? columns / (kbs * 64) : 1;
+  }
   const uint32_t stage = static_cast<uint32_t>(kbs) * (kATile + b_box);
   int stages = static_cast<int>(budget / stage);
   if (stages > 8) stages = 8;
