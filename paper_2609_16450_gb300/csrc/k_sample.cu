@@ -13,7 +13,7 @@
 //
 // A row is one cluster of CTAs; each warp owns a contiguous run of the row's
 // 16-byte groups, so that sums by warp are sums by index.  A CTA's slice of the row
-// comes into its shared memory once.
+// comes into its shared memory once where it fits, else it is read again.
 //
 // The last logit of a prefix is found without sorting, in one of three ways.
 //   - Top-k of few: every thread has the largest logit of each half of its own; the
@@ -25,6 +25,16 @@
 //     above them and lists what lies within, and again one CTA does the rest.
 //   - Where such a list would be too long (ties, most of all): histograms over the
 //     logits' ordered bits, each level over the bin that the last one chose.
+//
+// What bounds it: not the bytes (512 rows of 152064 floats of mixed settings are 311 MB,
+// 46 us at the copy rate; 190 us), but the weights, some 40 instructions each (55 % of
+// the issue slots are taken then), an atomic operation a logit where bins are counted, and
+// for few rows the chain of phases: a row's first bytes 1 us, its largest logit 2 to 3, a
+// list and its CTA's work 5 to 8, every barrier of a cluster 1 to 2 (32 rows of 126464 by
+// top-k and top-p 20 us; 64 rows at a temperature 24; one row of 4096 6.4).
+// Histograms of weights over all of a row instead took 296 us for the 32 rows, 1837 for
+// the 512.  A slice of the row in shared memory pays for 16-bit rows (24 rows by
+// top-p 61 against 72 us read again from L2), and for floats is no better than L2.
 #include <cuda_fp16.h>
 
 #include <climits>
@@ -816,6 +826,7 @@ struct Row {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) hi = fmaxf(hi, s.max[i]), lo = fminf(lo, s.low[i]);
+    __syncthreads();  // the caller writes them anew
     const float scale = (kLocal - 1.f) / (hi - lo);  // not finite where there is nothing to tell apart
     if (!(scale < 1e30f && scale > 0.f)) return lo < INFINITY ? lo : -3.402823466e38f;
     const float x[kItems] = {a, b};
@@ -912,7 +923,7 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
     mbar_arrive_expect_tx(&s.bar[warp], bytes);
     bulk_load(x.slice() + (f0 - g0), x.data + static_cast<size_t>(f0) * 16, bytes, &s.bar[warp]);
   }
-  const float T = p.temperature ? p.temperature[r] : 1.f, t = sample_temperature(T), u = p.u[r];
+  const float T = p.temperature ? p.temperature[r] : 1.f, t = sample_temperature(T), u = p.u[r] + 0.f;  // -0 counts as 0
   const float top_p = p.top_p ? p.top_p[r] : 1.f, min_p = p.min_p ? p.min_p[r] : 0.f;
   const int top_k = p.top_k ? p.top_k[r] : 0;
 

@@ -226,6 +226,56 @@ def test_rows_that_are_refused(vocab):
     h.close()
 
 
+@pytest.mark.parametrize("vocab,rows", [(700, 3), (40000, 3), (152064, 30), (152064, 90)])
+def test_settings_at_their_ends(vocab, rows):
+    """Equal logits under top-k of few, u = -0, filters that are infinite, -0 or of one
+    token: each row its own."""
+    h = handle(vocab)
+    g = np.random.default_rng(8)
+    x = np.zeros((rows, vocab), np.float32)
+    x[1::3] = np.round(g.standard_normal((len(x[1::3]), vocab)) * 2) / 2
+    x[2::3, :5] = 1.0
+    T = np.full(rows, 0.9, np.float32)
+    inf = np.inf
+    k = g.choice([1, 2, 7, 300, 0, -5, 2 ** 31 - 1], rows).astype(np.int32)
+    p = g.choice([-inf, -0.0, 0.3, 1.0, inf], rows).astype(np.float32)
+    q = g.choice([-inf, -0.0, 0.5, 1.0, inf], rows).astype(np.float32)
+    u = g.choice([-0.0, 0.25, 1 - 2.0 ** -24], rows).astype(np.float32)
+    logits = torch.from_numpy(x).cuda()
+    token, prob, status = sample(h, logits, u, T, k, p, q)
+    assert status == 0
+    verify(logits, T, np.maximum(k, 0), np.maximum(p, 0), np.maximum(q, 0), np.abs(u), token, prob)
+    h.close()
+
+
+def test_calls_on_streams_of_their_own():
+    """Calls of several handles at once."""
+    E, rt = _lib()
+    vocab, rows = 60000, 40
+    hs = [handle(vocab) for _ in range(4)]
+    sets = []
+    for i in range(4):
+        logits, g = make(rows, vocab, seed=20 + i)
+        T, k, p, q, u = params(g, rows, vocab, "kpq")
+        dev = [_dev(u, torch.float32), _dev(T, torch.float32), _dev(k, torch.int32), _dev(p, torch.float32), _dev(q, torch.float32)]
+        token, prob = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, **F32)
+        a = E.ebd_sample_args()
+        a.rows, a.logits, a.token, a.prob = rows, logits.data_ptr(), token.data_ptr(), prob.data_ptr()
+        a.u, a.temperature, a.top_k, a.top_p, a.min_p = (t.data_ptr() for t in dev)
+        sets.append((logits, T, k, p, q, u, token, prob, a, dev))
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(sets):
+            E.check(E.ebd_sample(hs[i].h, s[8], rt.stream_handle(streams[i])), hs[i].h)
+    torch.cuda.synchronize()
+    for logits, T, k, p, q, u, token, prob, _, _ in sets:
+        verify(logits, T, k, p, q, u, token.cpu().numpy(), prob.cpu().numpy())
+    for h in hs:
+        assert h.sync_status() == 0
+        h.close()
+
+
 def test_every_token_of_a_small_row():
     """u over a fine grid: every token comes up as often as its probability says."""
     vocab, n = 9, 512
