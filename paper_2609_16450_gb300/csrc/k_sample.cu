@@ -214,9 +214,9 @@ struct Shared {
   float kth;                 // a bound of the row's k-th logit, of this CTA's threads'
   int listed;
   int bin, k_bin, k_whole, k_before, alone, index, owner, last;
-  int p_first[2], p_last[2], n_first[2], n_last[2];  // top-p's bins: surely, and likely
+  int p_first[3], p_last[3], n_first[3], n_last[3];  // top-p's bins: surely, likely, and still likely
   float value;
-  uint32_t bound[6];
+  uint32_t bound[8];
   SampleScale scale;
   Bins bins;
   int g1, per_warp;            // the end of this CTA's groups, and a warp's of them
@@ -508,7 +508,7 @@ struct Row {
   // Counts the row's logits by bin; finds top-k's bin (s.k_bin: kBins if all that have
   // weight are wanted) with the number before it, and the bins from p_first to p_last
   // that top-p's border lies in: for sure, and, with weights as in the middle between
-  // the bounds, in all likelihood.
+  // the bounds and 5 or 2 parts in 10^4 of their sum to either side, in all likelihood.
   __device__ __forceinline__ void count(int k, float share) {
     Hist& h = s.hist[level++ & 1];
     const Bins bins = s.bins;
@@ -522,7 +522,7 @@ struct Row {
     uint32_t n[N] = {0, 0, 0, 0};
     gather(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x,
            [&](const uint4& v) { n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w; });
-    if (threadIdx.x < 2) {
+    if (threadIdx.x < 3) {
       s.k_bin = kBins, s.k_whole = 0;
       s.p_first[threadIdx.x] = s.p_last[threadIdx.x] = kBins - 1, s.n_first[threadIdx.x] = 0, s.n_last[threadIdx.x] = INT_MAX;
     }
@@ -558,7 +558,8 @@ struct Row {
       const float from = share * all_least * (1.f - 1e-4f);
       const float upto = fminf(fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f), all_least * (1.f - 1e-4f));
       const float middle = 0.5f * (all_most + all_least), part = share * middle;
-      const float early = part - 5e-4f * middle, late = fminf(part + 5e-4f * middle, middle * (1.f - 1e-6f));
+      const float early[2] = {part - 5e-4f * middle, part - 2e-4f * middle};
+      const float late[2] = {fminf(part + 5e-4f * middle, middle * (1.f - 1e-6f)), fminf(part + 2e-4f * middle, middle * (1.f - 1e-6f))};
       uint32_t at = first;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -568,8 +569,11 @@ struct Row {
         const float to = 0.5f * (to_most + to_least), next = 0.5f * (next_most + next_least);
         if ((to_most < from || b == 0) && next_most >= from) s.p_first[0] = b, s.n_first[0] = static_cast<int>(at);
         if (to_least < upto && next_least >= upto) s.p_last[0] = b, s.n_last[0] = static_cast<int>(next_at);
-        if ((to < early || b == 0) && next >= early) s.p_first[1] = b, s.n_first[1] = static_cast<int>(at);
-        if (to < late && next >= late) s.p_last[1] = b, s.n_last[1] = static_cast<int>(next_at);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if ((to < early[k] || b == 0) && next >= early[k]) s.p_first[k + 1] = b, s.n_first[k + 1] = static_cast<int>(at);
+          if (to < late[k] && next >= late[k]) s.p_last[k + 1] = b, s.n_last[k + 1] = static_cast<int>(next_at);
+        }
         at = next_at, to_most = next_most, to_least = next_least;
       }
     }
@@ -1097,7 +1101,7 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
     x.count(by_k ? top_k : 0, top_p);
     const bool cut_k = by_k && s.k_bin < kBins;
     // where top-k's bin and top-p's bins begin and end, a bound a warp
-    if (warp < 6) {
+    if (warp < 8) {
       const int b = warp == 0 ? s.k_bin : warp == 1 ? s.k_bin - 1 : (warp & 1) == 0 ? s.p_last[warp / 2 - 1] : s.p_first[warp / 2 - 1] - 1;
       const uint32_t q = b >= kBins ? floor : b < 0 ? top + 1 : x.search([&](float v) { return x.bin_of(v) <= b; }, floor, top);
       if (lane == 0) s.bound[warp] = q;
@@ -1114,9 +1118,10 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
     // Listed are the logits of all bins that the border may lie in, or, where they are
     // too many, of those that it should lie in: it is seen whether it does.
     const bool sure = s.n_last[0] - s.n_first[0] <= kList;
-    bool list = sure || (s.n_last[1] - s.n_first[1] <= kList && least <= x.up_to(s.bound[5] - 1));
+    const int likely = s.n_last[1] - s.n_first[1] <= kList ? 1 : 2;
+    bool list = sure || (s.n_last[likely] - s.n_first[likely] <= kList && least <= x.up_to(s.bound[2 * likely + 3] - 1));
     while (by_p) {
-      const int which = list && !sure ? 4 : 2;
+      const int which = list && !sure ? 2 * likely + 2 : 2;
       const uint32_t lo = max(s.bound[which], x.key(kept.value)), hi = s.bound[which + 1] - 1;
       const float f_lo = order_value(lo), f_hi = x.up_to(hi);
       const int shift = x.shift_of(lo, hi);

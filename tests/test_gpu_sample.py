@@ -248,6 +248,36 @@ def test_settings_at_their_ends(vocab, rows):
     h.close()
 
 
+@pytest.mark.parametrize("rows", [9, 200])
+def test_top_p_where_bins_mislead(rows):
+    """Logits at the near ends of their bins of (m - l) / T above a border and at the far
+    ends below, and the other way round: weights taken as in the middle of their bins put
+    the border half a bin's width of weights off, in another bin."""
+    vocab = 152064
+    h = handle(vocab)
+    width = 40 / 2040  # of a bin, in powers of two, where masked logits are everywhere
+    g = np.random.default_rng(12)
+    x = np.full((rows, vocab), -np.inf, np.float32)
+    p = np.empty(rows, np.float32)
+    for r in range(rows):
+        near = 0.45 if r % 2 else -0.45
+        bins = np.repeat(np.arange(10, 50), 1900)
+        y = (bins + np.where(bins < 30, near, -near)) * width
+        l = np.concatenate([[0.0], -y * np.log(2)]).astype(np.float32)
+        at = g.permutation(vocab)[: len(l)]
+        x[r, at] = l
+        w = np.exp(l.astype(np.float64))
+        border = w[: 1 + 20 * 1900].sum() / w.sum()  # between the two kinds
+        p[r] = border + (r // 2 % 5 - 2) * 1.2e-3
+    u = g.uniform(0, 1, rows).astype(np.float32) * np.float32(1 - 2 ** -24)
+    u[::3] = np.float32(1 - 2.0 ** -24)
+    logits = torch.from_numpy(x).cuda()
+    token, prob, status = sample(h, logits, u, None, None, p, None)
+    assert status == 0
+    verify(logits, None, None, p, None, u, token, prob)
+    h.close()
+
+
 def test_calls_on_streams_of_their_own():
     """Calls of several handles at once."""
     E, rt = _lib()
