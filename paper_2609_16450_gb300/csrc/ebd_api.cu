@@ -1086,8 +1086,6 @@ ebd_status ebd_create(const ebd_config* cfg, ebd_handle** out) {
     return bail(fail(h, EBD_ERR_UNSUPPORTED, "the library is compiled for sm_103a (GB300) only"));
   if (get_encode() == nullptr)
     return bail(fail(h, EBD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable"));
-  if ((e = sample_configure()) != cudaSuccess || (e = paged_plan_configure()) != cudaSuccess)
-    return bail(cuda_fail(h, e, "sampling and plan attributes"));
   size_t part_rows = 0, cuts = 0;
   if (cfg->paged) {
     if ((e = paged_configure()) != cudaSuccess || (e = paged_tc_configure()) != cudaSuccess)

@@ -903,12 +903,15 @@ static LmKernel lm_kernel(LmOutputs out, bool pair, bool packed, bool boxed) {
   }
 }
 
+static cudaError_t lm_allow(LmKernel k) {
+  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+}
+// those that every handle may run; the others as they are launched, so that they are
+// loaded where they are called
 cudaError_t lm_configure() {
-  const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
   cudaError_t e;
-  for (LmOutputs out : {LmOutputs::kStats, LmOutputs::kLogits, LmOutputs::kBoth})
-    for (int i = 0; i < 6; ++i)
-      if ((e = cudaFuncSetAttribute(lm_kernel(out, i > 1, i & 1, i > 3), a, 232448)) != cudaSuccess) return e;
+  for (int i = 0; i < 6; ++i)
+    if ((e = lm_allow(lm_kernel(LmOutputs::kStats, i > 1, i & 1, i > 3))) != cudaSuccess) return e;
   return cudaSuccess;
 }
 
@@ -935,7 +938,12 @@ cudaError_t launch_lm_stats(const CUtensorMap& tmap_w, const CUtensorMap& tmap_h
   }
   cfg.attrs = attr;
   cfg.numAttrs = na;
-  return cudaLaunchKernelEx(&cfg, lm_kernel(p.out, p.pair, p.packed, p.boxed), tmap_w, tmap_h, p);
+  const LmKernel k = lm_kernel(p.out, p.pair, p.packed, p.boxed);
+  if (p.out != LmOutputs::kStats) {
+    const cudaError_t e = lm_allow(k);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaLaunchKernelEx(&cfg, k, tmap_w, tmap_h, p);
 }
 
 }  // namespace ebd

@@ -216,11 +216,6 @@ size_t plan_bytes(int B, int pages) {
 
 }  // namespace
 
-cudaError_t paged_plan_configure() {
-  return cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(plan_bytes(kPagedMaxBatch, kPlanPages)));
-}
-
 cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st) {
   // A thread for each sequence and row, as far as that goes: fewer start sooner, and
   // meet at barriers sooner.  us for the two calls of 2048 sequences with 128 / 256 / 384 /
@@ -231,7 +226,13 @@ cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st) {
   // pages that may move: rows and a page more for each sequence, or as many back
   const int pages = p.B + (p.R > p.B ? p.R : p.B);
   p.pages = pages < kPlanPages ? pages : kPlanPages;
-  return paged_launch(paged_plan_kernel, dim3(1), threads, static_cast<uint32_t>(plan_bytes(p.B, p.pages)), st, p);
+  const uint32_t bytes = static_cast<uint32_t>(plan_bytes(p.B, p.pages));
+  if (bytes > 40 * 1024) {  // past what a kernel has without being asked, next to its own 2 KB
+    const cudaError_t e = cudaFuncSetAttribute(paged_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               static_cast<int>(plan_bytes(kPagedMaxBatch, kPlanPages)));
+    if (e != cudaSuccess) return e;
+  }
+  return paged_launch(paged_plan_kernel, dim3(1), threads, bytes, st, p);
 }
 
 }  // namespace ebd

@@ -1253,15 +1253,6 @@ Kernel sample_kernel_of(int dtype, bool resident, bool alone) {
 
 }  // namespace
 
-cudaError_t sample_configure() {
-  for (int i = 0; i < 6; ++i) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(sample_kernel_of(i / 2, true, i & 1), cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaSuccess;
-}
-
 cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   struct Table {
     SampleEntry v[kSampleTable];
@@ -1290,6 +1281,11 @@ cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   const long long bytes = p.vocab * (p.dtype == EBD_LOGITS_F32 ? 4ll : 2ll) + 32;  // both ends rounded out
   const long long slice = ((bytes / 16 + p.ctas - 1) / p.ctas + 1) * 16;
   p.resident = slice <= kSliceBytes;
+  const Kernel kernel = sample_kernel_of(p.dtype, p.resident != 0, alone != 0);
+  if (p.resident) {  // here, so that a process loads the kernels that it calls alone: all took 17 ms
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceBytes);
+    if (e != cudaSuccess) return e;
+  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(p.rows) * p.ctas, 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
@@ -1304,7 +1300,7 @@ cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sample_kernel_of(p.dtype, p.resident != 0, alone != 0), p);
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 }  // namespace ebd

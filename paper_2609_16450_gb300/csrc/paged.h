@@ -41,7 +41,6 @@ struct PagedPlanParams {
   int* status;
   int pages;                   // pages out, and back, that shared memory holds
 };
-cudaError_t paged_plan_configure();
 cudaError_t launch_paged_plan(PagedPlanParams p, cudaStream_t st);
 
 // Every kernel of the paged cache is a programmatic dependent of the one before

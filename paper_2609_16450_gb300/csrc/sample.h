@@ -22,7 +22,6 @@ struct SampleParams {
   SampleEntry table[kSampleTable];
 };
 
-cudaError_t sample_configure();
 cudaError_t launch_sample(SampleParams p, cudaStream_t st);
 
 }  // namespace ebd

@@ -113,6 +113,20 @@ def test_types_and_strides(dtype, pad, offset):
         h.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab,rows", [(517, 100), (33001, 100), (33001, 200), (130003, 80)])
+def test_many_rows(dtype, vocab, rows):
+    """More rows than run at once: another kernel, on one or two CTAs a row."""
+    h = handle(vocab)
+    for filters in ("", "kp", "pq"):
+        logits, g = make(rows, vocab, dtype, 1, 3, seed=vocab + rows)
+        T, k, p, q, u = params(g, rows, vocab, filters + "0" if filters == "kp" else filters)
+        token, prob, status = sample(h, logits, u, T, k, p, q)
+        assert status == 0
+        verify(logits, T, k, p, q, u, token, prob)
+    h.close()
+
+
 @pytest.mark.parametrize("vocab", [6, 4096, 100003])
 def test_equal_logits(vocab):
     """All equal, and in groups of equals: kept by index."""

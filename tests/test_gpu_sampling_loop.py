@@ -84,6 +84,37 @@ def test_sampling_loop(settings):
     h.close()
 
 
+def test_sampling_in_the_other_settings():
+    """The full sequence as the window, the paged cache planned on the device, and the
+    baselines' rules, all by drawn tokens."""
+    from paper_2609_16450_gb300 import _ebd as E
+    from paper_2609_16450_gb300 import loop as lp
+    from paper_2609_16450_gb300 import runtime as rt
+    from paper_2609_16450_gb300 import sampling as sp
+    draw = dict(sampling=sp.Settings(0.8, top_p=0.9), uniforms=_uniforms)
+    res = _loop(synth.loop_tiny, paged=True, plan="device", **draw)
+    plain = _loop(synth.loop_tiny, **draw)
+    assert np.array_equal(res.tokens, plain.tokens) and res.commits == plain.commits
+    sh = synth.loop_full_tiny
+    w = rt.upload_weights(synth.make_step_inputs(sh))
+    inputs = (lambda s, p: synth.loop_window_inputs(sh, s, p), lambda p: synth.loop_kv(sh, p))
+    h = rt.Handle(lp.config_for_loop(sh, max_window=sh.gen_len), w.w_emb)
+    res = lp.run_loop(h, sh, w, *inputs, attention=False, window="full", max_steps=6, **draw)
+    assert all(c >= 1 for c in res.commits)
+    for r in res.records:
+        acc = r.accepted.astype(bool)
+        assert np.array_equal(r.after["tokens"][acc], r.argmax[acc])
+    h.close()
+    sh = synth.loop_tiny
+    w = rt.upload_weights(synth.make_step_inputs(sh))
+    inputs = (lambda s, p: synth.loop_window_inputs(sh, s, p), lambda p: synth.loop_kv(sh, p))
+    for mode in (E.EBD_DECODE_THRESHOLD, E.EBD_DECODE_TOPM):
+        h = rt.Handle(lp.config_for_loop(sh, decode_mode=mode, top_m=3), w.w_emb)
+        res = lp.run_loop(h, sh, w, *inputs, **draw)
+        assert sum(res.commits) == sh.gen_len and ((res.tokens >= 0) & (res.tokens < sh.vocab)).all()
+        h.close()
+
+
 def test_loop_refusals():
     from paper_2609_16450_gb300 import sampling as sp
     for bad in (dict(plan="device"), dict(plan="gpu"), dict(sampling=sp.Settings()),
