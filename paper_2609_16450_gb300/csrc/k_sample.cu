@@ -457,9 +457,10 @@ struct Row {
     }
     return lo;
   }
-  // sum over this and the threads before it, and over all
+  // sum over this and the threads before it, and over all; `upto`: over those before it,
+  // which is bit for bit what the thread before this one is given
   template <typename T>
-  __device__ __forceinline__ T block_scan(T x, T* part, T& total) const {
+  __device__ __forceinline__ T block_scan(T x, T* part, T& total, T* upto = nullptr) const {
     T incl = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -476,6 +477,10 @@ struct Row {
       const T y = part[i];
       if (i < warp()) before += y;
       total += y;
+    }
+    if (upto != nullptr) {
+      const T last = __shfl_up_sync(0xffffffffu, incl, 1);
+      *upto = lane() > 0 ? before + last : before;
     }
     return before + incl;
   }
@@ -553,8 +558,9 @@ struct Row {
         sum_least += least[j] = static_cast<float>(n[j]) * next;
         edge = next;
       }
-      float to_most = block_scan(sum_most, s.scan_f, all_most) - sum_most;
-      float to_least = block_scan(sum_least, reinterpret_cast<float*>(s.scan), all_least) - sum_least;
+      float to_most, to_least;
+      const float end_most = block_scan(sum_most, s.scan_f, all_most, &to_most);
+      const float end_least = block_scan(sum_least, reinterpret_cast<float*>(s.scan), all_least, &to_least);
       const float from = share * all_least * (1.f - 1e-4f);
       const float upto = fminf(fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f), all_least * (1.f - 1e-4f));
       const float middle = 0.5f * (all_most + all_least), part = share * middle;
@@ -565,7 +571,9 @@ struct Row {
       for (int j = 0; j < N; ++j) {
         const int b = threadIdx.x * N + j;
         const uint32_t next_at = at + n[j];
-        const float next_most = to_most + most[j], next_least = to_least + least[j];
+        // a thread's last bin ends where the next thread begins: nothing falls between
+        const float next_most = j < N - 1 ? to_most + most[j] : fmaxf(to_most, end_most);
+        const float next_least = j < N - 1 ? to_least + least[j] : fmaxf(to_least, end_least);
         const float to = 0.5f * (to_most + to_least), next = 0.5f * (next_most + next_least);
         if ((to_most < from || b == 0) && next_most >= from) s.p_first[0] = b, s.n_first[0] = static_cast<int>(at);
         if (to_least < upto && next_least >= upto) s.p_last[0] = b, s.n_last[0] = static_cast<int>(next_at);
@@ -1164,12 +1172,12 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
         if (rank == 0) {
           typename R::Items items;
           int n[kMaxCtas];
-          x.listed(n);
+          const bool fits = x.listed(n) <= kList;
           x.take(items, n);
           const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
           uint64_t within;
           x.block_scan((items.w[0] + items.w[1]) + (items.w[2] + items.w[3]), s.scan, within);
-          const bool there = sure || (share > over && share - over <= within);
+          const bool there = fits && (sure || (share > over && share - over <= within));
           x.template list_cut<true>(items, kept, lo, hi, share > over ? share - over : 1);
           if (least > kept.value) kept = Prefix{least, INT_MAX};
           // what is kept of the list goes to the sums of the warps that have it
