@@ -1276,13 +1276,17 @@ cudaError_t launch_sample(SampleParams p, cudaStream_t st) {
   // CTAs, at a temperature: 14 rows 27 / 20 / 18 / 16 / 16 / 15, 20 rows 27 / 20 / 19 / 17
   // / 16 / 28, 28 rows 27 / 21 / 19 / 18 / 29 / 30, 36 rows 27 / 21 / 19 / 31 / 31 / 42, 44
   // rows 27 / 21 / 34 / 32 / 31 / 44.  Many rows: two CTAs on an SM; a cluster's barriers
-  // and its launch cost more than they bring, but for long rows: 512 rows of 152064 at a
-  // temperature 185 / 162 / 192 us with 1 / 2 / 4 CTAs, of 57000 72 / 77 / 98.
+  // and its launch cost more than they bring, but for long rows, or where they even out how
+  // many CTAs an SM has: 512 rows of 152064 at a temperature 188 / 168 / 188 / 198 us with
+  // 1 / 2 / 3 / 4 CTAs, of mixed settings 241 / 195 / 203 / 220, 80 rows 109 / 76 / 66 / 62,
+  // 200 rows 164 / 114 / 101 / 104; 512 rows of 57000 at a temperature 72 / 77 with 1 / 2, by
+  // top-k and top-p 101 / 90 / 98 / 117.
   struct { int rows, ctas; } const fits[] = {{14, 8}, {20, 6}, {24, 5}, {36, 4}, {44, 3}, {76, 2}};
   int alone = 0;
   for (const auto& f : fits)
     if (alone == 0 && p.rows <= f.rows) alone = f.ctas;
-  p.ctas = alone != 0 ? alone : p.rows <= 128 || p.vocab >= 100000 ? 2 : 1;
+  const bool light = p.top_k == nullptr && p.top_p == nullptr;
+  p.ctas = alone != 0 ? alone : p.rows <= 100 ? 3 : p.rows <= 128 || p.vocab >= (light ? 100000 : 50000) ? 2 : 1;
   const int most = (p.vocab + 11999) / 12000;  // a CTA wants some logits: one row of 16000 9.2 / 8.5 / 8.0 / 8.7 us with 1 / 2 / 4 / 8
   if (p.ctas > most) p.ctas = most;
   // a slice of a row in shared memory, where it leaves room for two CTAs on an SM
