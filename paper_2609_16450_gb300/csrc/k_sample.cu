@@ -512,8 +512,10 @@ struct Row {
 
   // Counts the row's logits by bin; finds top-k's bin (s.k_bin: kBins if all that have
   // weight are wanted) with the number before it, and the bins from p_first to p_last
-  // that top-p's border lies in: for sure, and, with weights as in the middle between
-  // the bounds and 5 or 2 parts in 10^4 of their sum to either side, in all likelihood.
+  // that top-p's border lies in: for sure, by bounds of the sums (where the share's upper
+  // bound is past the row's lower one, up to the last bin), and, with weights as in the
+  // middle between the bounds and 5 or 2 parts in 10^4 of their sum to either side, in
+  // all likelihood.
   __device__ __forceinline__ void count(int k, float share) {
     Hist& h = s.hist[level++ & 1];
     const Bins bins = s.bins;
@@ -527,14 +529,16 @@ struct Row {
     uint32_t n[N] = {0, 0, 0, 0};
     gather(reinterpret_cast<const uint4*>(h.coarse) + threadIdx.x,
            [&](const uint4& v) { n[0] += v.x, n[1] += v.y, n[2] += v.z, n[3] += v.w; });
-    if (threadIdx.x < 3) {
-      s.k_bin = kBins, s.k_whole = 0;
-      s.p_first[threadIdx.x] = s.p_last[threadIdx.x] = kBins - 1, s.n_first[threadIdx.x] = 0, s.n_last[threadIdx.x] = INT_MAX;
-    }
     uint32_t all;
     const uint32_t sum = n[0] + n[1] + n[2] + n[3];
     uint32_t before = block_scan(sum, reinterpret_cast<uint32_t*>(s.scan), all) - sum;
     const uint32_t want = k > 0 ? min(static_cast<uint32_t>(k), all) : all, first = min(before, want);
+    if (threadIdx.x < 3) {
+      s.k_bin = kBins, s.k_whole = 0;
+      s.p_first[threadIdx.x] = s.p_last[threadIdx.x] = kBins - 1;
+      s.n_first[threadIdx.x] = 0, s.n_last[threadIdx.x] = static_cast<int>(want);
+    }
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       if (k > 0 && k <= all && before < want && before + n[j] >= want) {
@@ -562,7 +566,7 @@ struct Row {
       const float end_most = block_scan(sum_most, s.scan_f, all_most, &to_most);
       const float end_least = block_scan(sum_least, reinterpret_cast<float*>(s.scan), all_least, &to_least);
       const float from = share * all_least * (1.f - 1e-4f);
-      const float upto = fminf(fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f), all_least * (1.f - 1e-4f));
+      const float upto = fmaxf(share * all_most * (1.f + 1e-4f), 1e-30f);
       const float middle = 0.5f * (all_most + all_least), part = share * middle;
       const float early[2] = {part - 5e-4f * middle, part - 2e-4f * middle};
       const float late[2] = {fminf(part + 5e-4f * middle, middle * (1.f - 1e-6f)), fminf(part + 2e-4f * middle, middle * (1.f - 1e-6f))};
@@ -1124,7 +1128,8 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
     }
     by_p = by_p && least <= x.up_to(s.bound[3] - 1);  // else min-p keeps less, whatever top-p does
     // Listed are the logits of all bins that the border may lie in, or, where they are
-    // too many, of those that it should lie in: it is seen whether it does.
+    // too many, of those that it should lie in.  It is seen whether it does: what is kept
+    // above them is less than the share, and with what is listed no less.
     const bool sure = s.n_last[0] - s.n_first[0] <= kList;
     const int likely = s.n_last[1] - s.n_first[1] <= kList ? 1 : 2;
     bool list = sure || (s.n_last[likely] - s.n_first[likely] <= kList && least <= x.up_to(s.bound[2 * likely + 3] - 1));
@@ -1177,7 +1182,7 @@ __global__ void __launch_bounds__(kThreads, PER_SM) sample_kernel(const SamplePa
           const uint64_t share = sample_share(top_p, x.cluster_sum(s.rest)), over = x.cluster_sum(s.part);
           uint64_t within;
           x.block_scan((items.w[0] + items.w[1]) + (items.w[2] + items.w[3]), s.scan, within);
-          const bool there = fits && (sure || (share > over && share - over <= within));
+          const bool there = fits && share > over && share - over <= within;
           x.template list_cut<true>(items, kept, lo, hi, share > over ? share - over : 1);
           if (least > kept.value) kept = Prefix{least, INT_MAX};
           // what is kept of the list goes to the sums of the warps that have it
