@@ -843,12 +843,14 @@ struct Row {
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) hi = fmaxf(hi, s.max[i]), lo = fminf(lo, s.low[i]);
     __syncthreads();  // the caller writes them anew
-    const float scale = (kLocal - 1.f) / (hi - lo);  // not finite where there is nothing to tell apart
-    if (!(scale < 1e30f && scale > 0.f)) return lo < INFINITY ? lo : -3.402823466e38f;
+    const float scale = (kLocal - 1.f) / (hi - lo);
+    const bool apart = scale < 1e30f && scale > 0.f;  // else one bin for all
     const float x[kItems] = {a, b};
     const uint64_t one[kItems] = {a > -INFINITY ? 1u : 0u, b > -INFINITY ? 1u : 0u};
-    if (!level_of(one, static_cast<uint64_t>(most), [&](int q) { return min(static_cast<int>((hi - x[q]) * scale), kLocal - 1); }))
-      return -3.402823466e38f;
+    if (!level_of(one, static_cast<uint64_t>(most),
+                  [&](int q) { return apart ? min(static_cast<int>((hi - x[q]) * scale), kLocal - 1) : 0; }))
+      return -3.402823466e38f;  // fewer than `most`: what is wanted may lie below all of them
+    if (!apart) return lo;
     const float t = hi - (static_cast<float>(s.bin) + 1.01f) / scale;  // and room for rounding
     return fmaxf(lo, t - (fabsf(hi) + fabsf(t)) * 2.384185791015625e-7f);
   }

@@ -1,4 +1,5 @@
-"""ebd_sample where its borders are hardest to find: shares close to 1."""
+"""ebd_sample where its borders are hardest to find: shares close to 1, few tokens
+allowed."""
 import numpy as np
 import pytest
 
@@ -27,4 +28,33 @@ def test_top_p_near_one(vocab, rows, dtype):
             token, prob, status = sample(h, logits, u, t, k, p)
             assert status == 0
             verify(logits, t, k, p, None, u, token, prob)
+    h.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab,rows", [(2000, 16), (4096, 200), (152064, 16), (152064, 90)])
+def test_top_k_of_few_allowed(vocab, rows, dtype):
+    """All but a few tokens banned, and fewer threads than k with one to show: what k asks
+    for is then behind their largest, whether those are equal, nearly so, or one."""
+    h = handle(vocab)
+    allowed = [{8: 5.0, 10: 3.0}, {8: 5.0, 10: 3.0, vocab - 3: 5.0}, {9: 1.0, 11: 2.0, 1001: 2.0, 1003: -1.0, 1005: 2.0},
+               {0: 2.0 ** -95, 2: 2.0 ** -96, 1000: 2.0 ** -95 + 2.0 ** -101}, {4: 0.0, 5: -1.0, 6: -2.0, 7: -0.5},
+               {40: -3.0}, {vocab - 1: 1.0, vocab - 3: 0.5, vocab - 2: 0.0}, {i: float(i % 7) for i in range(0, 640, 2)}]
+    x = np.full((rows, vocab), -np.inf, np.float32)
+    T = np.ones(rows, np.float32)
+    for r in range(rows):
+        a = allowed[r % len(allowed)]
+        x[r, list(a)] = list(a.values())
+        if r % len(allowed) == 3:
+            T[r] = 2.0 ** -96
+    logits = torch.from_numpy(x).cuda().to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype])
+    g = np.random.default_rng(7)
+    u = g.uniform(0, 1, rows).astype(np.float32) * LAST
+    u[rows // 2:] = LAST
+    for k in (2, 3, 10, 700):
+        ks = np.full(rows, k, np.int32)
+        for p in (None, g.uniform(0.3, 1, rows).astype(np.float32)):
+            token, prob, status = sample(h, logits, u, T, ks, p)
+            assert status == 0
+            verify(logits, T, ks, p, None, u, token, prob)
     h.close()
