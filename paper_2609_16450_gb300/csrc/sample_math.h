@@ -144,9 +144,11 @@ EBD_HD uint64_t sample_share(float p, uint64_t total) {
 }
 // The unit that u in [0, 1) points at: token = the first whose sum passes it.
 EBD_HD uint64_t sample_point(float u, uint64_t total) { return sample_part(u, total, false); }
-// Least logit with weight >= q of the largest's, for (hi, lo) = T ln q in two floats.
+// Least logit with weight >= q of the largest's, for (hi, lo) = T ln q in two floats;
+// the lowest float where that lies below float's range (m + hi = -inf would make the rest
+// NaN: what is left of it then is in r).
 EBD_HD float sample_floor(float m, float hi, float lo) {
-  const float s = m + hi, b = s - m;
+  const float s = fmaxf(m + hi, -3.402823466e38f), b = s - m;
   const float r = ((m - (s - b)) + (hi - b)) + lo;  // s + r = m + T ln q
   const float f = s + r;
   return r - (f - s) > 0.f ? order_value(order_key(f + 0.f) + 1) : f;

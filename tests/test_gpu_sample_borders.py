@@ -1,5 +1,5 @@
 """ebd_sample where its borders are hardest to find: shares close to 1, few tokens
-allowed."""
+allowed, the lowest logits."""
 import numpy as np
 import pytest
 
@@ -57,4 +57,20 @@ def test_top_k_of_few_allowed(vocab, rows, dtype):
             token, prob, status = sample(h, logits, u, T, ks, p)
             assert status == 0
             verify(logits, T, ks, p, None, u, token, prob)
+    h.close()
+
+
+@pytest.mark.parametrize("vocab", [8, 5000])
+def test_min_p_below_the_lowest_logit(vocab):
+    """Every logit is the type's lowest, and what min-p asks for lies below it: past
+    float's range, where a share of equal logits is still kept by index."""
+    h = handle(vocab)
+    rows = 6
+    logits = torch.full((rows, vocab), np.finfo(np.float32).min, device="cuda")
+    T, q = np.full(rows, 1e30, np.float32), np.full(rows, 1e-7, np.float32)
+    p = np.array([0.5, 0.25, 0.75, 0.5, 0.25, 0.75], np.float32)
+    u = np.array([0, 0.5, LAST, LAST, 0.25, 0.5], np.float32)
+    token, prob, status = sample(h, logits, u, T, None, p, q)
+    assert status == 0
+    verify(logits, T, None, p, q, u, token, prob)
     h.close()
