@@ -33,6 +33,17 @@ EBD_HD float f32_of(uint32_t b) {
 #endif
 }
 
+// A product rounded by itself: never part of a fused multiply-add, whatever a compiler is
+// allowed.
+EBD_HD float rounded_product(float a, float b) {
+#ifdef __CUDA_ARCH__
+  return __fmul_rn(a, b);
+#else
+  const volatile float p = a * b;
+  return p;
+#endif
+}
+
 // Whole numbers in the order of the floats they stand for (no NaN, no -0).
 EBD_HD uint32_t order_key(float x) {
   const uint32_t b = f32_bits(x);
@@ -85,7 +96,7 @@ inline SampleEntry sample_entry(int j) {
   return {f32_bits(v) + (static_cast<uint32_t>(j) << 16), static_cast<float>((x - v) / v)};
 }
 // y, rounded: it grows as l falls, and decides alone which weights are zero
-EBD_HD float sample_depth(float m, float l, const SampleScale& c) { return (m - l) * c.hi; }
+EBD_HD float sample_depth(float m, float l, const SampleScale& c) { return rounded_product(m - l, c.hi); }
 
 // w = v + v x of a logit that has weight
 struct SampleTerm {
@@ -95,7 +106,7 @@ EBD_HD SampleTerm sample_term(float m, float l, const SampleScale& c, const Samp
   const float s = m - l;
   const float b = s - m;
   const float d = (m - (s - b)) - (l + b);  // s + d = m - l exactly
-  const float p = s * c.hi;
+  const float p = rounded_product(s, c.hi);  // e holds what this rounding leaves out
   const float e = fmaf(d, -c.hi, fmaf(s, -c.lo, fmaf(s, -c.hi, p)));  // -e above
   const float t = p + kSampleMagic;
   const float z = (p - (t - kSampleMagic)) - e;

@@ -1,5 +1,5 @@
 """ebd_sample where its borders are hardest to find: shares close to 1, few tokens
-allowed, the lowest logits."""
+allowed, the lowest logits, light tokens."""
 import numpy as np
 import pytest
 
@@ -73,4 +73,25 @@ def test_min_p_below_the_lowest_logit(vocab):
     token, prob, status = sample(h, logits, u, T, None, p, q)
     assert status == 0
     verify(logits, T, None, p, q, u, token, prob)
+    h.close()
+
+
+@pytest.mark.parametrize("T", [1.0, 0.3, 1.7])
+def test_weights_of_light_tokens(T):
+    """The lighter of two tokens, from 2^-1 down to 2^-39 of the other: its probability is
+    its weight, off by 2^-30 of itself, over a sum off by 2^-42 of the other's (twice a
+    unit), rounded to 32 bits."""
+    vocab, rows = 2, 500
+    h = handle(vocab)
+    g = np.random.default_rng(2)
+    x = np.zeros((rows, vocab), np.float32)
+    T = float(np.float32(T))
+    x[:, 0] = -g.uniform(1, 39, rows) * np.log(2) * T
+    for top in (0.0, 11.0, -3.7):
+        l = (x + np.float32(top)).astype(np.float32)
+        token, prob, status = sample(h, torch.from_numpy(l).cuda(), np.zeros(rows, np.float32), np.full(rows, T, np.float32))
+        assert status == 0 and (token == 0).all()
+        w = np.exp((l[:, 0].astype(np.float64) - l[:, 1]) / T)
+        want = w / (1 + w)
+        assert (np.abs(prob - want) <= want * (2.0 ** -24 + 2.0 ** -30 + 2.0 ** -42 + 2.0 ** -50)).all()
     h.close()
