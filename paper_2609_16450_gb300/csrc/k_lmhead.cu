@@ -808,11 +808,11 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair, LmOutp
   // of Dream-7B 305 -> 287 us, 390 rows 340 -> 333; 32 rows of LLaDA-8B 152 -> 155.
   p.stream_out = 4ll * rows * V > (96ll << 20);
   if (store && p.n_pad > 32 * kStoreSlices) p.nwg = 2;
-  const uint32_t t_bytes = out == LmOutputs::kLogits ? 0 : kTBytes * static_cast<uint32_t>(p.nwg);
+  const uint32_t t_stats = kTBytes * static_cast<uint32_t>(p.nwg);
+  const uint32_t t_bytes = out == LmOutputs::kLogits ? 0 : t_stats;
   const uint32_t st_bytes = static_cast<uint32_t>(p.n_pad) * 20u;
-  const uint32_t tail = t_bytes + ((st_bytes + 7) / 8 * 8) +
-                        (2 * 8 + 6) * 8 + 16;
-  const uint32_t budget = 232448u - 1024u - tail;
+  const uint32_t tail = ((st_bytes + 7) / 8 * 8) + (2 * 8 + 6) * 8 + 16;
+  const uint32_t budget = 232448u - 1024u - tail - t_bytes;
   // hidden bytes per k-box in one CTA: all rows, or half of them in a pair
   const uint32_t b_box = static_cast<uint32_t>(pair ? p.n_pad / 2 : p.n_pad) * 128u;
   // k-boxes (64 columns each) per pipeline stage, while keeping at least two
@@ -828,7 +828,11 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair, LmOutp
   if (kbs < 1) kbs = 1;
   if (kbs > 5) kbs = 5;
   if (kbs > p.nkb) kbs = p.nkb;
-  while (kbs > 1 && budget / (static_cast<uint32_t>(kbs) * (kATile + b_box)) < 2) --kbs;
+  // Stages end where sums are cut into segments: with or without the statistics' buffers
+  // they are the same, so that the logits are.  (33 to 48 rows alone would have five
+  // k-boxes, and take 160 us of LLaDA-8B instead of 157.)
+  const uint32_t budget_stats = 232448u - 1024u - tail - t_stats;
+  while (kbs > 1 && budget_stats / (static_cast<uint32_t>(kbs) * (kATile + b_box)) < 2) --kbs;
   p.kbs = kbs;
   p.nks = (p.nkb + kbs - 1) / kbs;
   p.seg = p.nks;
