@@ -43,12 +43,16 @@ constexpr uint32_t kATile = 128 * 128;  // 128 rows x 64 bf16
 constexpr int kTLd = 132;               // transpose buffer row stride (floats)
 constexpr uint32_t kTBytes = 32 * kTLd * 4;  // transpose buffer of one epilogue warpgroup
 constexpr int kStoreSlices = 4;         // of 32 columns that an epilogue thread holds the sums of
-// Columns of W that go into one accumulator where logits are stored, alone and in
-// pairs.  What is stored after a chunk has the time of two segments before the MMAs wait
-// for it, which the pairs feel: 390 rows of Dream-7B with 512 / 768 / 1024 / all of the
-// 3584 columns in one 370 / 340 / 329 / 322 us, 128 rows of LLaDA-8B 202 / 194 / 181 /
-// 176; errors 4.7e-7, 7.0e-7, 9.4e-7 and 3.8e-6 (a plain sum's in 32 bits 5.6e-7).
-constexpr int kStoreColumns = 512, kStoreColumnsPair = 768;
+// Columns of W that go into one accumulator where logits are stored, in whole stages
+// (single CTAs have stages of 320 columns, of 256 from 33 rows on).  Pairs have two longer
+// ones first: what is stored after a chunk has their time before the MMAs wait for it.
+// Errors (rms, of the logits' size) grow as an accumulator's columns to the power 1.5:
+// sqrt(sum n^3 / d) columns in every one would give the same.  The first two are as long
+// as keeps that at kStoreMean, 5.9e-7.  Measured in turn, us and errors of 390 rows of
+// Dream-7B with 512 columns in all / 768 in two / 768 and 640 / 768 in all: 407 4.7e-7 /
+// 368 6.0e-7 / 390 5.6e-7 / 363 7.0e-7; of 128 rows of LLaDA-8B 202 4.8e-7 / 192 5.8e-7 /
+// 192 5.5e-7 / 190 7.1e-7, a plain sum's in 32 bits being 6.1e-7.
+constexpr int kStoreColumns = 512, kStoreFirst = 768, kStoreMean = 640;
 
 __device__ __forceinline__ void state_merge(float& m, float& s, float& t, float& l2, int& idx,
                                             float bm, float bs, float bt, float bl2, int bidx) {
@@ -182,6 +186,11 @@ __device__ __forceinline__ void slice_stats(const float (&v)[32], int cc, int n_
     }
   }
   named_barrier(bar_id, 128);
+}
+
+// Where the segment of a chunk's stages ends that begins at k0 (STORE).
+__device__ __forceinline__ int seg_end(const LmParams& p, int k0) {
+  return min(k0 + (k0 < 2 * p.seg_first ? p.seg_first : p.seg), p.nks);
 }
 
 // One accumulator buffer by one epilogue warpgroup, in slices of 32 columns: each goes
@@ -494,7 +503,6 @@ __global__ void __launch_bounds__(kLmThreads, 1)
           umma_commit(&empty[st]);
       };
       // an accumulator at a time: a chunk, or (STORE) a segment of a chunk's columns
-      const int seg = STORE ? p.seg : p.nks;
       for (int u = u0, k0 = 0; u < u1 && ok; ++c) {
         const int buf = c % p.nbuf;
         const uint32_t bph = static_cast<uint32_t>(c / p.nbuf) & 1u;
@@ -502,7 +510,7 @@ __global__ void __launch_bounds__(kLmThreads, 1)
         if (!ok) break;
         tc_fence_after();
         const uint32_t d0 = tmem_u + static_cast<uint32_t>(buf * p.acc_stride);
-        const int k1 = min(k0 + seg, p.nks);
+        const int k1 = STORE ? seg_end(p, k0) : p.nks;
         for (int ks = k0; ks < k1; ++ks) {
           ok = __all_sync(0xffffffffu, mbar_wait(&full[s], ph, p.limit_ns, abort));
           if (!ok) break;
@@ -650,15 +658,16 @@ __global__ void __launch_bounds__(kLmThreads, 1)
           }
         }
       };
-      if (STORE && p.seg < p.nks) {
+      if (STORE && p.seg_first < p.nks) {
         // The tensor cores cut what they add to an accumulator, some 2^-25 of it each
         // time.  The segments of a chunk's columns have accumulators of their own, and
         // are added here, rounded: 4096 columns in one are 4.4e-6 off (of the
-        // logits' size), in 8 segments of 512 3e-7, half a plain sum's in 32 bits.
+        // logits' size), in 13 segments of 320 (up to 32 rows) 2.9e-7, half a plain sum's
+        // in 32 bits.
         float sum[kStoreSlices][32];
 #pragma unroll
         for (int i = 0; i < kStoreSlices * 32; ++i) sum[i / 32][i % 32] = 0.f;
-        for (int k0 = 0; k0 < p.nks; k0 += p.seg, ++c) {
+        for (int k0 = 0; k0 < p.nks; k0 = seg_end(p, k0), ++c) {
           if (!accumulated()) break;
           const int buf = c % p.nbuf;
 #pragma unroll
@@ -835,10 +844,23 @@ void lm_plan(LmParams& p, int rows, int V, int d, int num_sms, bool pair, LmOutp
   while (kbs > 1 && budget_stats / (static_cast<uint32_t>(kbs) * (kATile + b_box)) < 2) --kbs;
   p.kbs = kbs;
   p.nks = (p.nkb + kbs - 1) / kbs;
-  p.seg = p.nks;
+  p.seg = p.seg_first = p.nks;
   if (store && p.nbuf == 2 && p.n_pad <= 64 * kStoreSlices) {
-    const int columns = pair ? kStoreColumnsPair : kStoreColumns;
-    p.seg = kbs * 64 < columns ? columns / (kbs * 64) : 1;
+    const int stage_columns = kbs * 64;
+    p.seg = stage_columns < kStoreColumns ? kStoreColumns / stage_columns : 1;
+    p.seg_first = pair ? kStoreFirst / stage_columns : p.seg;
+    auto cubes = [](int first, int seg, int nks) {  // sum of n^3, n stages
+      long long sum = 0;
+      for (int k0 = 0, k1; k0 < nks; k0 = k1) {
+        const int end = k0 + (k0 < 2 * first ? first : seg);
+        k1 = end < nks ? end : nks;
+        sum += static_cast<long long>(k1 - k0) * (k1 - k0) * (k1 - k0);
+      }
+      return sum;
+    };
+    const long long mean = kStoreMean / stage_columns;
+    while (p.seg_first > p.seg && cubes(p.seg_first, p.seg, p.nks) > mean * mean * p.nks) --p.seg_first;
+    if (p.seg_first < p.seg) p.seg_first = p.seg;
   }
   const uint32_t stage = static_cast<uint32_t>(kbs) * (kATile + b_box);
   int stages = static_cast<int>(budget / stage);

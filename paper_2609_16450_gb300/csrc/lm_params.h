@@ -18,7 +18,8 @@ struct LmParams {
   int grid;                 // CTAs (each writes one partial per row)
   int nkb;                  // ceil(d / 64) k-blocks of 64 columns
   int kbs, nks;             // k-blocks per pipeline stage, stages per vocabulary chunk
-  int seg;                  // STORE: stages of one accumulator; nks: a chunk is not split
+  int seg_first, seg;       // STORE: stages of one accumulator, a chunk's first two and the
+                            // others; seg_first = nks: a chunk is not split
   int packed;               // W is tiled: tile (unit, k-block) at row (unit*nkb + kb)*64
   int boxed;                // CTA pairs: a stage's hidden rows (and row-major W rows) come in
                             // as one 3-D box (d a multiple of 64)
