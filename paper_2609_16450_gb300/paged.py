@@ -120,6 +120,7 @@ class PagedCache:
         shape = (n_pages, self.heads, page_size)
         el = torch.uint8 if dtype == "e4m3" else torch.bfloat16
         self.k = torch.zeros(shape + (self.dim,), dtype=el, device=device)
+        rt.check_device(h, "the cache", self.k)
         self.v = torch.zeros_like(self.k)
         self.k_scale = self.v_scale = None
         if dtype == "e4m3":

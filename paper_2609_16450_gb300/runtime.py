@@ -55,6 +55,7 @@ class Handle:
             raise E.EbdError(s, "ebd_create failed")
         self.h = h
         self.cfg = cfg
+        self.device = torch.device("cuda", torch.cuda.current_device())  # ebd_create's
         self.w_emb = None
         if w_emb is not None:
             self.bind(w_emb, stream)
@@ -76,6 +77,14 @@ class Handle:
             self.close()
         except Exception:
             pass
+
+
+def check_device(h, what: str, t: torch.Tensor):
+    """Refuses a tensor that the handle's kernels cannot read: of the host, or of another
+    device.  (A stand-in for a handle has no device and takes any.)"""
+    device = getattr(h, "device", t.device)
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the handle on {device}")
 
 
 def stream_handle(stream) -> int:

@@ -77,6 +77,7 @@ def lm_logits(h: rt.Handle, hidden: torch.Tensor, weights: rt.DeviceWeights, log
     for what, t in (("logits", logits), ("W_lm", weights.w_lm)):
         if t.device != hidden.device:
             raise ValueError(f"{what} is on {t.device}, hidden on {hidden.device}")
+    rt.check_device(h, "hidden", hidden)
     a = E.ebd_step_args()
     # the LM head takes rows as they come: any sequences that hold them
     a.batch, a.rows = c.max_batch, rows
@@ -98,6 +99,7 @@ def sample(h: rt.Handle, logits: torch.Tensor, u: torch.Tensor, token: torch.Ten
         raise ValueError(f"logits: fp32, bf16 or fp16 expected, not {logits.dtype}")
     stride = _matrix(logits, "logits", h.cfg.vocab)
     rows, dev = logits.shape[0], logits.device
+    rt.check_device(h, "logits", logits)
     a = E.ebd_sample_args()
     a.rows, a.dtype, a.logits, a.stride = rows, DTYPES[logits.dtype], logits.data_ptr(), stride
     for name, t, dtype in (("u", u, torch.float32), ("token", token, torch.int32), ("prob", prob, torch.float32),
