@@ -31,13 +31,14 @@ class Settings:
     min_p: float = 0.0
 
     def rows(self, n: int, device="cuda") -> Dict[str, Optional[torch.Tensor]]:
-        """What sample() takes for n rows; filters that are off are left out."""
+        """What sample() takes for n rows; filters that are off are left out (NaN is not off:
+        rows that have it are refused)."""
         f32 = dict(dtype=torch.float32, device=device)
         return dict(
             temperature=torch.full((n,), self.temperature, **f32),
             top_k=torch.full((n,), self.top_k, dtype=torch.int32, device=device) if self.top_k > 0 else None,
-            top_p=torch.full((n,), self.top_p, **f32) if self.top_p < 1 else None,
-            min_p=torch.full((n,), self.min_p, **f32) if self.min_p > 0 else None)
+            top_p=torch.full((n,), self.top_p, **f32) if not self.top_p >= 1 else None,
+            min_p=torch.full((n,), self.min_p, **f32) if not self.min_p <= 0 else None)
 
 
 def _matrix(t: torch.Tensor, what: str, width: int) -> int:
