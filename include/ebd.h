@@ -261,6 +261,10 @@ ebd_status ebd_lm_stats(ebd_handle* h, const ebd_step_args* a, void* stream);
  * draws x_hat instead, and kappa is the probability it was drawn with: the logits
  * go to memory, ebd_sample draws from them, and its token and prob are what
  * ebd_decide takes as argmax and conf (next to ent_norm and gap of ebd_lm_logits).
+ * A row of one token (T = 0, top_k = 1, a top_p near 0) is drawn with prob 1, which
+ * every threshold and ranking of the decision takes as certain: for argmax decoding
+ * give it conf of ebd_lm_logits, the max p, in its place.
+ * The first call of a kind loads its kernels: some milliseconds, once in a process.
  *
  * ebd_lm_logits: l = W_lm h for a->rows rows of a->hidden, as ebd_lm_stats
  * computes it, into logits[r * stride + v], fp32.  Of a's outputs conf, entropy,
@@ -284,7 +288,7 @@ typedef struct {
   const float* temperature;   /* [R] T >= 0 (0: the largest); NULL: 1            */
   const int32_t* top_k;       /* [R] k, <= 0: no limit; NULL: none               */
   const float* top_p;         /* [R] p, >= 1: no limit; NULL: none               */
-  const float* min_p;         /* [R] q, <= 0: no limit; NULL: none               */
+  const float* min_p;         /* [R] q, <= 0: no limit, 1 at most; NULL: none    */
   int32_t* token;             /* [R]                                             */
   float* prob;                /* [R] its probability among what is kept          */
 } ebd_sample_args;
@@ -292,17 +296,16 @@ typedef struct {
 /* Draws a token of every row.  With m the row's largest logit and w[v] =
  * exp((l[v] - m) / T), zero below 2^-40, tokens are taken by descending logit, ties
  * by ascending index.  K is the first k of them, N the least prefix of K (one token
- * at least) whose weight is p or more of K's, F those of N with w >= q (the first at
- * least).  token is the least v in F with the sum of w over F up to v above u times
- * that over F, prob = w[token] over that sum.  T = 0: the lowest index of the largest
- * logit, with prob 1.  Temperatures count as 1e-30 at least, unless 0, and 1e30 at
- * most.  Weights are off by 2^-30 of themselves and 2^-43 of the largest, their sums
- * are exact: results do not vary from run to run.
+ * at least) whose weight is p or more of K's, F those of N with w >= min(q, 1) (at q = 1
+ * the largest and its equals).  token is the least v in F with the sum of w over F up
+ * to v above u times that over F, prob = w[token] over that sum.  T = 0: the lowest
+ * index of the largest logit, with prob 1.  Temperatures count as 1e-30 at least,
+ * unless 0, and 1e30 at most.  Weights are off by 2^-30 of themselves and 2^-43 of the
+ * largest, their sums are exact: results do not vary from run to run.
  * Logits of -inf have no part in it.  A row with NaN, +inf, or no logit above -inf
  * records EBD_ERR_NONFINITE, one with u outside [0, 1), T negative or not finite, or
  * a NaN parameter EBD_ERR_INVALID_ARG: its token is -1 and its prob NaN, which
- * ebd_decide does not commit.  2^20 logits a row or
- * more: EBD_ERR_UNSUPPORTED. */
+ * ebd_decide does not commit.  2^20 logits a row or more: EBD_ERR_UNSUPPORTED. */
 ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream);
 
 /* ---- Vocabulary-parallel LM head (several GPUs) --------------------------

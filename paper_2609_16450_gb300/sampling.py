@@ -1,6 +1,7 @@
 """Decoding at a temperature: the logits of a step's rows in memory (ebd_lm_logits) and
 tokens drawn from them (ebd_sample), on torch tensors.  What is drawn goes into
-ebd_decide as argmax and conf.
+ebd_decide as argmax and conf; a token that was the only one to draw (temperature 0) has
+conf 1, for which lm_logits' conf may stand in.
 
     lm_logits(h, hidden, weights, logits, stats={"entropy": ent, "ent_norm": hn, "gap": gap})
     sample(h, logits, u, token, prob, temperature=t, top_k=k, top_p=p)
