@@ -1455,6 +1455,11 @@ ebd_status ebd_sample(ebd_handle* h, const ebd_sample_args* a, void* stream) {
     return fail(h, EBD_ERR_INVALID_ARG, "logits, u, token and prob must be set");
   if (!aligned(a->logits, a->dtype == EBD_LOGITS_F32 ? 4 : 2))
     return fail(h, EBD_ERR_INVALID_ARG, "logits must be aligned to a logit");
+  for (const void* v : {static_cast<const void*>(a->u), static_cast<const void*>(a->temperature),
+                        static_cast<const void*>(a->top_k), static_cast<const void*>(a->top_p),
+                        static_cast<const void*>(a->min_p), static_cast<const void*>(a->token),
+                        static_cast<const void*>(a->prob)})
+    if (!aligned(v, 4)) return fail(h, EBD_ERR_INVALID_ARG, "a row's numbers must be 4-byte aligned");
   SampleParams p{};
   p.logits = a->logits;
   p.stride = a->stride != 0 ? a->stride : vocab;
@@ -1830,6 +1835,11 @@ ebd_status ebd_paged_plan(ebd_handle* h, const ebd_paged_plan_args* a, void* str
   if (a->n_pages < 1 || a->max_pages < 1) return bad("n_pages and max_pages must be positive");
   if (!a->free_pages || !a->n_free) return bad("free_pages and n_free must be set");
   if (a->batch > 0 && (!a->add || !a->kv_len || !a->page_table)) return bad("add, kv_len and page_table must be set");
+  for (const int* v : {a->add, static_cast<const int*>(a->kv_len), static_cast<const int*>(a->page_table),
+                       static_cast<const int*>(a->free_pages), static_cast<const int*>(a->n_free),
+                       static_cast<const int*>(a->cu_rows), static_cast<const int*>(a->row_pos)})
+    if (!aligned(v, 4)) return bad("lengths, pages, offsets and positions must be 4-byte aligned");
+  if (!aligned(a->slot, 8)) return bad("slot must be 8-byte aligned");
   PagedPlanParams p{};
   p.B = a->batch;
   p.R = a->rows;
