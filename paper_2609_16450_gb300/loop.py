@@ -21,8 +21,8 @@ cached past the new window's start goes back, and the window's rows come.
 With `sampling` x_hat is drawn at a temperature (ebd_lm_logits, ebd_sample) and kappa is
 the probability it was drawn with; the decision then runs on them (ebd_decide).  Where one
 token is left to draw (temperature 0, top_k 1, a top_p near 0) that is 1, and the decision
-accepts every row that it looks at: argmax decoding, with kappa = max p, is the loop without
-`sampling`.
+accepts every row that it looks at (top-m, the first m of them): argmax decoding, with kappa =
+max p, is the loop without `sampling`.
 This module only marshals buffers; the window rule and every step of the
 method run in the library."""
 from __future__ import annotations
